@@ -41,7 +41,8 @@ typedef enum {
     TRIMMOE_ERR_OOM = -3,            /* device allocation failed */
     TRIMMOE_ERR_CUDA = -4,           /* a CUDA runtime/driver call failed */
     TRIMMOE_ERR_COVERAGE = -5,       /* an expert has no server (violates Eq. 2) */
-    TRIMMOE_ERR_DEVICE_TIMEOUT = -6  /* a kernel gave up waiting and flagged it */
+    TRIMMOE_ERR_DEVICE_TIMEOUT = -6, /* a kernel gave up waiting and flagged it */
+    TRIMMOE_ERR_CACHE = -7           /* a kernel refused a cache operation and flagged it */
 } trimmoe_status;
 
 typedef struct trimmoe* trimmoe_handle;
@@ -58,7 +59,12 @@ enum {
     TRIMMOE_DEVERR_GEMM_EPILOGUE = 3,  /* grouped GEMM: epilogue waiting for an accumulator */
     TRIMMOE_DEVERR_ROUTER = 4,         /* router logits kernel */
     TRIMMOE_DEVERR_ATTENTION = 5,      /* attention kernel (including its softmax pair barriers) */
-    TRIMMOE_DEVERR_SELFTEST = 6        /* trimmoe_watchdog_selftest */
+    TRIMMOE_DEVERR_SELFTEST = 6,       /* trimmoe_watchdog_selftest */
+    /* Reported by trimmoe_cache_stats of a cache handle. */
+    TRIMMOE_DEVERR_CACHE_ATTENTION = 7, /* cache attention kernel */
+    TRIMMOE_DEVERR_CACHE_FULL = 8,     /* step: too few free pages, or a sequence longer than max_pages */
+    TRIMMOE_DEVERR_CACHE_STATE = 9,    /* table, length or ref hold values that no call writes */
+    TRIMMOE_DEVERR_CACHE_PATH = 10     /* accept: n_acc or a path that does not fit the sequence's drafts */
 };
 
 enum { TRIMMOE_EXEC = 0, TRIMMOE_SKIP = 1, TRIMMOE_EXIT = 2, TRIMMOE_DEAD = 3 };
@@ -316,7 +322,8 @@ trimmoe_status trimmoe_reset_stats(trimmoe_handle h);
 trimmoe_status trimmoe_watchdog_selftest(trimmoe_handle h, int timeout_us, void* stream);
 
 /* Last error message of the handle ("" if none); NULL handle: the last error of
- * a call made without a handle (trimmoe_create, trimmoe_compact_noalloc). */
+ * a call made without a handle (trimmoe_create, trimmoe_compact_noalloc,
+ * trimmoe_cache_create). */
 const char* trimmoe_last_error(trimmoe_handle h);
 
 /* Free the handle and its workspaces (synchronises first).  NULL is a no-op. */
@@ -415,6 +422,167 @@ trimmoe_status trimmoe_replicate(int N, int E, int M, const float* lambda, const
 trimmoe_status trimmoe_compact_noalloc(const uint8_t* action, const uint8_t* exp_sel, int T, int k, int E,
                                        int has_shared, int32_t* perm, int32_t* group_off,
                                        int32_t* pos_pair, int32_t* pos_sh, void* stream);
+
+/* ---------------------------------------------------------------- cache --
+ * Paged key/value cache and the attention that reads it: prompts of any length,
+ * single tokens and trees of drafted tokens, for serving programs that keep
+ * sequences between steps (the attention sublayer inside trimmoe_layer_step
+ * holds whole sequences of at most 128 tokens).  The paper has no counterpart.
+ *
+ * A sequence's positions are cut into pages of page_size tokens; position p of
+ * sequence s is row p % page_size of page table[s][p / page_size].  Pages may be
+ * shared by sequences (fork); ref counts their holders, 0 = free.  All
+ * bookkeeping runs on the GPU: lengths that only the GPU knows (accepted drafts)
+ * never travel to the host, and every call is asynchronous on the given stream
+ * except create, destroy and stats.  As for trimmoe_handle, a cache is used by
+ * one stream and one host thread at a time; a program that changes streams
+ * orders them itself.
+ *
+ * A serving step is
+ *     trimmoe_cache_step     room for each sequence's new tokens, and the work list
+ *     per layer: trimmoe_cache_append, trimmoe_cache_attend
+ *     trimmoe_cache_accept / _truncate / _fork between steps
+ * The new tokens of a step are packed: those of the first listed sequence, then
+ * the second's, and so on, T = sum of q_len rows in all.
+ *
+ * bf16 rounding happens once per stored value; norms, rotations, scores, softmax
+ * statistics and sums are fp32 (probabilities are rounded to bf16 as operands
+ * of the tensor cores, their sum is that of the unrounded values).
+ *
+ * Capture: append, attend, fork, truncate, accept and compact may be captured in
+ * a CUDA graph, step too (its sequences and counts are those of the capture; the
+ * lengths are read on the GPU at replay). */
+typedef struct trimmoe_cache* trimmoe_cache_handle;
+
+/*  layers; q_heads, kv_heads (q_heads / kv_heads a whole number <= 128);
+ *  head_dim 64 or 128; page_size 16, 32, 64 or 128 tokens; n_pages pages of the
+ *  pool; max_seqs rows (<= 1024) and max_pages columns of the page table;
+ *  T_max: largest number of new tokens of a step (<= 2^20).
+ *  n_pages * kv_heads * page_size and max_pages * page_size stay below 2^31. */
+typedef struct {
+    int layers, q_heads, kv_heads, head_dim, page_size, n_pages, max_seqs, max_pages, T_max;
+} trimmoe_cache_config;
+
+/* The cache's state (device, owned by the caller, borrowed; k and v 16-byte aligned).
+ *  k, v bf16 [layers][n_pages][kv_heads][page_size][head_dim];
+ *  table int32 [max_seqs][max_pages], -1 past a sequence's pages;
+ *  length int32 [max_seqs]; ref int32 [n_pages].
+ * A new cache has table = -1, length = 0, ref = 0.  A program may also hand over
+ * state of its own making (or hold further references: ref > the holders in
+ * table keeps a page alive).  Rows of pages past a sequence's length may hold
+ * anything, NaN included. */
+typedef struct {
+    void* k;
+    void* v;
+    int32_t* table;
+    int32_t* length;
+    int32_t* ref;
+} trimmoe_cache_state;
+
+/* Validate and allocate the workspaces (work list, split-sum buffers: about
+ * 80 MB at head_dim 128).  Errors: ARG, UNSUPPORTED, OOM, CUDA; *out is NULL then. */
+trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, const trimmoe_cache_state* st,
+                                    trimmoe_cache_handle* out);
+
+/* Begin a step: q_len[i] >= 0 new tokens for each of n distinct sequences seq[i]
+ * (host arrays, read during the call; n = 0 ends the step).  Lengths grow by
+ * q_len; missing pages are taken lowest index first, in the order of the
+ * sequences; a last page that is shared and would be written is first copied
+ * into a page of its own (all layers; every holder listed in the step copies,
+ * the pages that this frees are free after the step).  Builds the work list that append and
+ * attend use until the next step, fork, truncate, accept or compact.
+ * Without enough pages nothing changes, CACHE_FULL is flagged, and append and
+ * attend do nothing until a step succeeds. */
+trimmoe_status trimmoe_cache_step(trimmoe_cache_handle c, int n, const int32_t* seq, const int32_t* q_len,
+                                  void* stream);
+
+/* Arguments of trimmoe_cache_append (device pointers; 16-byte aligned, row
+ * strides in elements and multiples of 8).
+ *  qkv bf16 [T][ld_qkv]: query heads, key heads, value heads, head_dim each, as
+ *      a fused projection leaves them;
+ *  q_out bf16 [T][ld_q]: queries, normed and rotated (may be qkv itself with
+ *      ld_q == ld_qkv);
+ *  gamma_q, gamma_k bf16 [head_dim]: RMSNorm weights of each query and key head
+ *      (both NULL: no norm), y = x / sqrt(mean(x^2) + norm_eps) * gamma;
+ *  rope_theta: base of the rotation of pairs (i, i + head_dim/2) by
+ *      pos * rope_theta^(-2i/head_dim), 0 for none;
+ *  pos int32 [T] >= 0: the tokens' positions, or NULL for their places in their
+ *      sequences (drafted trees pass depths). */
+typedef struct {
+    const void* qkv;
+    int ld_qkv;
+    void* q_out;
+    int ld_q;
+    const void* gamma_q;
+    const void* gamma_k;
+    float norm_eps, rope_theta;
+    const int32_t* pos;
+} trimmoe_append_args;
+
+/* Norm and rotate the step's queries and keys, write its keys and values into
+ * their pages of one layer. */
+trimmoe_status trimmoe_cache_append(trimmoe_cache_handle c, int layer, const trimmoe_append_args* a, void* stream);
+
+/* Arguments of trimmoe_cache_attend (device pointers as above).
+ *  q bf16 [T][ld_q], out bf16 [T][ld_out] (q_heads * head_dim columns each; out
+ *      must not overlap q);
+ *  tree uint64 [T], or NULL.  NULL: token i of a sequence's new tokens sees the
+ *      sequence's earlier positions, the new tokens before it and itself.  Else it
+ *      sees the positions before the step, and new token j of its sequence iff
+ *      bit j of its word is set (its own bit included); every q_len <= 64;
+ *  scale > 0 of the scores, 0 for 1/sqrt(head_dim).
+ * Query head h reads key/value head h / (q_heads / kv_heads).  Masked positions
+ * contribute nothing, whatever their keys and values hold; a row that sees no
+ * position is zero. */
+typedef struct {
+    const void* q;
+    int ld_q;
+    void* out;
+    int ld_out;
+    const uint64_t* tree;
+    float scale;
+} trimmoe_attend_args;
+
+trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer, const trimmoe_attend_args* a, void* stream);
+
+/* Make sequences dst[i] continuations of src[i]: dst's pages are released, then
+ * it shares all of src's (host arrays; dst distinct, none of them a source). */
+trimmoe_status trimmoe_cache_fork(trimmoe_cache_handle c, int n, const int32_t* src, const int32_t* dst,
+                                  void* stream);
+
+/* Cut sequences to at most length[i] positions and release the pages past them
+ * (host arrays; 0 frees the sequence). */
+trimmoe_status trimmoe_cache_truncate(trimmoe_cache_handle c, int n, const int32_t* seq, const int32_t* length,
+                                      void* stream);
+
+/* Keep one path of each sequence's drafts: of the q_len tokens that the last
+ * step added to seq[i], tokens path[i][0] < path[i][1] < ... (n_acc[i] of them,
+ * at most 64) move to the front, in all layers, and the sequence is cut behind
+ * them.  seq is a host array, n_acc int32 [n] and path int32 [n][ld_path] are on
+ * the device.  A sequence whose n_acc or path does not fit, or whose drafts are
+ * shared, is left as it is and CACHE_PATH is flagged. */
+trimmoe_status trimmoe_cache_accept(trimmoe_cache_handle c, int n, const int32_t* seq, const int32_t* n_acc,
+                                    const int32_t* path, int ld_path, void* stream);
+
+/* Move the pages in use to the lowest indices: those past the number in use go,
+ * in order, to the free ones below it; tables and counts follow. */
+trimmoe_status trimmoe_cache_compact(trimmoe_cache_handle c, void* stream);
+
+typedef struct {
+    int device_error;   /* 0, or the first TRIMMOE_DEVERR_* code since create / the last reset */
+    int free_pages;     /* pages with ref == 0 */
+    uint64_t launches;  /* kernels launched by the handle */
+} trimmoe_cache_stats_t;
+
+/* Synchronise the handle's last stream and read the counters; reset != 0 clears
+ * the error afterwards.  Returns CACHE or DEVICE_TIMEOUT if one was flagged. */
+trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_cache_stats_t* out, int reset);
+
+/* Last error message of the cache ("" if none). */
+const char* trimmoe_cache_last_error(trimmoe_cache_handle c);
+
+/* Free the handle and its workspaces (synchronises first).  NULL is a no-op. */
+void trimmoe_cache_destroy(trimmoe_cache_handle c);
 
 #ifdef __cplusplus
 }

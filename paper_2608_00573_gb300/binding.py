@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(PKG, "_build", "libtrimmoe.so")
 
 TRIMMOE_OK = 0
 STATUS_NAMES = {0: "OK", -1: "ERR_ARG", -2: "ERR_UNSUPPORTED", -3: "ERR_OOM", -4: "ERR_CUDA",
-                -5: "ERR_COVERAGE", -6: "ERR_DEVICE_TIMEOUT"}
+                -5: "ERR_COVERAGE", -6: "ERR_DEVICE_TIMEOUT", -7: "ERR_CACHE"}
 EXEC, SKIP, EXIT, DEAD = 0, 1, 2, 3
 
 
@@ -97,10 +97,37 @@ class trimmoe_calibration_t(C.Structure):
                                           "act_freq", "lambda_", "rho")]
 
 
+class trimmoe_cache_config(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("layers", "q_heads", "kv_heads", "head_dim", "page_size", "n_pages",
+                                       "max_seqs", "max_pages", "T_max")]
+
+
+class trimmoe_cache_state(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "table", "length", "ref")]
+
+
+class trimmoe_append_args(C.Structure):
+    _fields_ = [("qkv", C.c_void_p), ("ld_qkv", C.c_int), ("q_out", C.c_void_p), ("ld_q", C.c_int),
+                ("gamma_q", C.c_void_p), ("gamma_k", C.c_void_p), ("norm_eps", C.c_float),
+                ("rope_theta", C.c_float), ("pos", C.c_void_p)]
+
+
+class trimmoe_attend_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ld_q", C.c_int), ("out", C.c_void_p), ("ld_out", C.c_int),
+                ("tree", C.c_void_p), ("scale", C.c_float)]
+
+
+class trimmoe_cache_stats_t(C.Structure):
+    _fields_ = [("device_error", C.c_int), ("free_pages", C.c_int), ("launches", C.c_uint64)]
+
+
 EXPORTS = ("trimmoe_create", "trimmoe_layer_step", "trimmoe_forward", "trimmoe_forward_host",
            "trimmoe_stats", "trimmoe_reset_stats", "trimmoe_last_error", "trimmoe_destroy",
            "trimmoe_compact_noalloc", "trimmoe_feedback", "trimmoe_calibration_begin",
-           "trimmoe_calibration_end", "trimmoe_replicate", "trimmoe_watchdog_selftest")
+           "trimmoe_calibration_end", "trimmoe_replicate", "trimmoe_watchdog_selftest",
+           "trimmoe_cache_create", "trimmoe_cache_step", "trimmoe_cache_append", "trimmoe_cache_attend",
+           "trimmoe_cache_fork", "trimmoe_cache_truncate", "trimmoe_cache_accept", "trimmoe_cache_compact",
+           "trimmoe_cache_stats", "trimmoe_cache_last_error", "trimmoe_cache_destroy")
 
 _lib = None
 _lock = threading.Lock()
@@ -406,6 +433,206 @@ class Engine:
     def close(self):
         if getattr(self, "handle", None):
             trimmoe_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ----------------------------------------------------------- paged cache
+
+def _cache_lib():
+    """The library with the prototypes of the cache's entry points."""
+    L = lib()
+    if not getattr(L, "_cache_prototypes", False):
+        vp, i = C.c_void_p, C.c_int
+        for name, args in (("create", [vp, vp, C.POINTER(vp)]), ("step", [vp, i, vp, vp, vp]),
+                           ("append", [vp, i, vp, vp]), ("attend", [vp, i, vp, vp]), ("fork", [vp, i, vp, vp, vp]),
+                           ("truncate", [vp, i, vp, vp, vp]), ("accept", [vp, i, vp, vp, vp, i, vp]),
+                           ("compact", [vp, vp]), ("stats", [vp, vp, i])):
+            f = getattr(L, "trimmoe_cache_" + name)
+            f.argtypes, f.restype = args, i
+        L.trimmoe_cache_last_error.argtypes = [vp]
+        L.trimmoe_cache_last_error.restype = C.c_char_p
+        L.trimmoe_cache_destroy.argtypes = [vp]
+        L.trimmoe_cache_destroy.restype = None
+        L._cache_prototypes = True
+    return L
+
+
+def trimmoe_cache_create(cfg: trimmoe_cache_config, st: trimmoe_cache_state) -> C.c_void_p:
+    h = C.c_void_p()
+    _check(_cache_lib().trimmoe_cache_create(C.byref(cfg), C.byref(st), C.byref(h)))
+    return h
+
+
+class PagedCache:
+    """Keys and values of sequences kept between steps, and the attention over them.
+
+    Owns a trimmoe_cache handle and borrows the caller's tensors (all on one
+    GPU, contiguous): k, v bfloat16 [layers][n_pages][kv_heads][page][head_dim],
+    table int32 [max_seqs][max_pages] (-1: none), length int32 [max_seqs], ref
+    int32 [n_pages].  ``PagedCache.empty`` makes them for a new cache.  Calls are
+    queued on the current stream (or ``stream``); see include/trimmoe.h for
+    their rules.  Sequence lists are host sequences of ints.
+    """
+
+    def __init__(self, k, v, table, length, ref, q_heads: int, T_max: int):
+        import torch
+        self.torch = torch
+        self.handle = None
+        if k.dim() != 5 or k.shape != v.shape or table.dim() != 2 or length.dim() != 1 or ref.dim() != 1:
+            raise TrimmoeError(-1, "cache: k and v are [layers][n_pages][kv_heads][page][head_dim], table is "
+                                   "[max_seqs][max_pages], length and ref are vectors")
+        self.layers, self.n_pages, self.kv_heads, self.page, self.head_dim = k.shape
+        self.max_seqs, self.max_pages = table.shape
+        self.q_heads, self.T_max, self.device = int(q_heads), int(T_max), k.device
+        if length.shape[0] != self.max_seqs or ref.shape[0] != self.n_pages:
+            raise TrimmoeError(-1, "cache: length has one entry per table row, ref one per page")
+        for t, dt in ((k, torch.bfloat16), (v, torch.bfloat16), (table, torch.int32), (length, torch.int32),
+                      (ref, torch.int32)):
+            self._tensor(t, dt, None, "cache")
+            if not t.is_contiguous():
+                raise TrimmoeError(-1, "cache: tensors must be contiguous")
+        self.k, self.v, self.table, self.length, self.ref = k, v, table, length, ref
+        self.T = 0
+        cfg = trimmoe_cache_config(layers=self.layers, q_heads=self.q_heads, kv_heads=self.kv_heads,
+                                   head_dim=self.head_dim, page_size=self.page, n_pages=self.n_pages,
+                                   max_seqs=self.max_seqs, max_pages=self.max_pages, T_max=self.T_max)
+        st = trimmoe_cache_state(k=_ptr(k), v=_ptr(v), table=_ptr(table), length=_ptr(length), ref=_ptr(ref))
+        with torch.cuda.device(self.device):
+            # create reads length: what was queued to fill it comes first.
+            torch.cuda.current_stream().synchronize()
+            self.handle = trimmoe_cache_create(cfg, st)
+
+    @classmethod
+    def empty(cls, layers: int, n_pages: int, q_heads: int, kv_heads: int, head_dim: int, page: int, max_seqs: int,
+              max_pages: int, T_max: int, device="cuda"):
+        """A cache of n_pages free pages (page contents are left unset)."""
+        import torch
+        shape = (layers, n_pages, kv_heads, page, head_dim)
+        return cls(torch.empty(shape, dtype=torch.bfloat16, device=device),
+                   torch.empty(shape, dtype=torch.bfloat16, device=device),
+                   torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(max_seqs, dtype=torch.int32, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device), q_heads, T_max)
+
+    # checks and calls ------------------------------------------------------
+    def _tensor(self, t, dtype, shape, what):
+        if t is None:
+            return
+        if not isinstance(t, self.torch.Tensor) or t.device != self.device or t.device.type != "cuda":
+            raise TrimmoeError(-1, f"{what}: tensors must be on the cache's GPU")
+        if t.dtype != dtype:
+            raise TrimmoeError(-1, f"{what}: expected {dtype}, got {t.dtype}")
+        if shape is not None and (tuple(t.shape) != tuple(shape) or (t.numel() and t.stride(-1) != 1)):
+            raise TrimmoeError(-1, f"{what}: expected shape {tuple(shape)} with contiguous rows, got {tuple(t.shape)}")
+
+    def _rows(self, t, cols, what):
+        """Row stride of a [T][cols] tensor."""
+        self._tensor(t, self.torch.bfloat16, (self.T, cols), what)
+        return t.stride(0) if self.T > 1 else max(cols, t.stride(0))
+
+    def _new(self, cols, stream):
+        """A [T][cols] result, allocated on the stream that writes it."""
+        t = self.torch
+        with t.cuda.stream(stream):          # None: the current stream
+            return t.empty((self.T, cols), dtype=t.bfloat16, device=self.device)
+
+    @staticmethod
+    def _list(v):
+        a = np.ascontiguousarray(v, dtype=np.int32)
+        if a.ndim != 1:
+            raise TrimmoeError(-1, "cache: sequence lists have one dimension")
+        return a
+
+    def _pair(self, a, b, what):
+        a, b = self._list(a), self._list(b)
+        if a.shape != b.shape:
+            raise TrimmoeError(-1, f"{what}: lists of different lengths")
+        return a, b
+
+    def _call(self, name, *args, stream=None):
+        s = stream if stream is not None else self.torch.cuda.current_stream(self.device)
+        L = _cache_lib()
+        rc = getattr(L, "trimmoe_cache_" + name)(self.handle, *args, C.c_void_p(int(s.cuda_stream)))
+        if rc != TRIMMOE_OK:
+            raise TrimmoeError(rc, L.trimmoe_cache_last_error(self.handle).decode())
+
+    def step(self, seq, q_len, stream=None):
+        """Room for q_len[i] new tokens of sequence seq[i]; the work list of append and attend."""
+        seq, q_len = self._pair(seq, q_len, "step")
+        self._call("step", len(seq), _ptr(seq), _ptr(q_len), stream=stream)
+        self.T = int(q_len.sum())
+
+    def append(self, layer: int, qkv, q_out=None, gamma_q=None, gamma_k=None, eps: float = 1e-6, theta: float = 1e6,
+               pos=None, stream=None):
+        """Norm (with gammas) and rotate the step's queries and keys of qkv [T][(q + 2 kv heads) * head_dim], write
+        its keys and values into the cache; returns the queries [T][q_heads * head_dim] (q_out, which may be a
+        view of qkv's query columns)."""
+        t, hd = self.torch, self.head_dim
+        ld = self._rows(qkv, (self.q_heads + 2 * self.kv_heads) * hd, "append")
+        if q_out is None:
+            q_out = self._new(self.q_heads * hd, stream)
+        ld_q = self._rows(q_out, self.q_heads * hd, "append")
+        for g in (gamma_q, gamma_k):
+            self._tensor(g, t.bfloat16, (hd,), "append")
+        if pos is not None:
+            self._tensor(pos, t.int32, (self.T,), "append")
+        a = trimmoe_append_args(qkv=_ptr(qkv), ld_qkv=ld, q_out=_ptr(q_out), ld_q=ld_q, gamma_q=_ptr(gamma_q),
+                                gamma_k=_ptr(gamma_k), norm_eps=eps, rope_theta=theta, pos=_ptr(pos))
+        self._call("append", layer, C.byref(a), stream=stream)
+        return q_out
+
+    def attend(self, layer: int, q, out=None, tree=None, scale: float = 0.0, stream=None):
+        """Attention of the step's queries [T][q_heads * head_dim] over their sequences; tree: int64 [T] words, bit j
+        = sees new token j of its sequence (default: causal)."""
+        t, cols = self.torch, self.q_heads * self.head_dim
+        ld = self._rows(q, cols, "attend")
+        if out is None:
+            out = self._new(cols, stream)
+        ld_out = self._rows(out, cols, "attend")
+        if tree is not None:
+            self._tensor(tree, t.int64, (self.T,), "attend")
+        a = trimmoe_attend_args(q=_ptr(q), ld_q=ld, out=_ptr(out), ld_out=ld_out, tree=_ptr(tree), scale=scale)
+        self._call("attend", layer, C.byref(a), stream=stream)
+        return out
+
+    def fork(self, src, dst, stream=None):
+        """Sequences dst[i] become continuations of src[i] and share its pages."""
+        src, dst = self._pair(src, dst, "fork")
+        self._call("fork", len(dst), _ptr(src), _ptr(dst), stream=stream)
+
+    def truncate(self, seq, length, stream=None):
+        """Cut sequences to at most length[i] positions (0 frees them)."""
+        seq, length = self._pair(seq, length, "truncate")
+        self._call("truncate", len(seq), _ptr(seq), _ptr(length), stream=stream)
+
+    def accept(self, seq, n_acc, path, stream=None):
+        """Keep the drafts path[i][:n_acc[i]] of the last step (int32 tensors [n] and [n][depth]), moved to the front."""
+        seq = self._list(seq)
+        self._tensor(n_acc, self.torch.int32, (len(seq),), "accept")
+        if path.dim() != 2 or not path.is_contiguous():
+            raise TrimmoeError(-1, "accept: path is a contiguous [n][depth] tensor")
+        self._tensor(path, self.torch.int32, (len(seq), path.shape[1]), "accept")
+        self._call("accept", len(seq), _ptr(seq), _ptr(n_acc), _ptr(path), path.shape[1], stream=stream)
+
+    def compact(self, stream=None):
+        """Move the pages in use to the lowest indices."""
+        self._call("compact", stream=stream)
+
+    def stats(self, reset: bool = False) -> dict:
+        """Synchronises; {status, device_error, free_pages, launches}."""
+        s = trimmoe_cache_stats_t()
+        rc = _cache_lib().trimmoe_cache_stats(self.handle, C.byref(s), int(reset))
+        return dict(status=rc, device_error=s.device_error, free_pages=s.free_pages, launches=s.launches)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _cache_lib().trimmoe_cache_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libtrimmoe.so")
 SOURCES = ["trimmoe.cu", "router.cu", "decide.cu", "compact.cu", "grouped_gemm.cu", "combine.cu", "attention.cu",
-           "feedback.cu", "watchdog.cu"]
+           "feedback.cu", "watchdog.cu", "cache.cu", "cache_pages.cu", "cache_append.cu", "cache_attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -36,7 +36,7 @@ def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
     t = os.path.getmtime(obj)
-    deps = [src, os.path.join(CSRC, "internal.cuh"), os.path.join(ROOT, "include", "trimmoe.h")]
+    deps = [src, os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "cache.cuh"), os.path.join(ROOT, "include", "trimmoe.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

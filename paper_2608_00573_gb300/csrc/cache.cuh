@@ -1,0 +1,105 @@
+// Internal declarations of the paged key/value cache: device records, kernel
+// parameters and launchers.
+#pragma once
+
+#include "internal.cuh"
+
+namespace tmoe {
+
+constexpr int kCacheMaxSeqs = 1024;
+constexpr int kCacheTile = 128;        // rows of a query tile, keys of a key tile
+constexpr int kTreeMax = 64;           // drafted tokens of a sequence (mask bits)
+
+// One listed sequence of the current step.
+struct CacheSeq {
+    int seq, q_off, q_len, kv_len;     // kv_len: its length with the new tokens
+};
+
+// A group: up to two query tiles of one sequence, that is ntok consecutive new
+// tokens (a tile holds tile_tokens = 128 / (q_heads / kv_heads) tokens, all query
+// heads of one key/value head).  One item of attention work is a group and a
+// key/value head; items are ordered by group, then head.
+struct __align__(16) CacheGroup {
+    long long pre;                     // cost of one head's items before this group
+    int seq, kv_len;
+    int row, ntok;                     // first packed token, tokens
+    int first;                         // position of the first token
+    int base;                          // positions before the step
+};
+
+struct CachePlan {
+    long long total;                   // cost of all items
+    int n_groups, n_ctas;              // CTAs that share them
+    int copies;                        // pages to copy (shared last pages)
+    int ok;                            // 0: the step was refused
+};
+
+// Cost of an item in query-tile x key-tile products: its products, plus the
+// same number of products as one key tile for its start and end.
+__host__ __device__ inline int cache_tile_cost(int ntok, int tile_tokens) { return ntok > tile_tokens ? 2 : 1; }
+
+// Key tiles of a group.  Short steps count to the sequence's end, because a draft
+// mask may show any new token to any other.
+__host__ __device__ inline int cache_group_tiles(int q_len, int kv_len, int first, int ntok) {
+    const int keys = q_len <= kTreeMax ? kv_len : first + ntok;
+    return (keys + kCacheTile - 1) / kCacheTile;
+}
+
+// The handle's device state, passed to every kernel by value.
+struct CacheDev {
+    int layers, Hq, Hkv, rep, dh, page, page_shift, n_pages, max_seqs, max_pages, T_max;
+    int tile_tokens, num_sms;
+    __nv_bfloat16 *k, *v;
+    int *table, *length, *ref;
+    // workspaces
+    CachePlan* plan;
+    CacheSeq* seqs;                    // [kCacheMaxSeqs]
+    CacheGroup* groups;                // [T_max / (2 tile_tokens) + max_seqs + 1]
+    int* cta_group;                    // [num_sms + 1] group in which each CTA's share begins
+    int* slot;                         // [T_max] page row (page * page_size + place) of each new token, -1 none
+    int* pos;                          // [T_max] its position in its sequence
+    int2* copies;                      // [max(n_pages, max_seqs)] (from, to) pages
+    int* fresh;                        // [n_pages] free pages taken by a step; new place of each page (compact)
+    int* base;                         // [max_seqs] length before the sequence's last step
+    float* part_o;                     // [2 num_sms][256][dh] partial sums of split items
+    float2* part_ml;                   // [2 num_sms][256] their row maxima and sums
+    int* err;
+};
+
+// Host arrays of a call travel as kernel parameters (no staging buffer whose
+// lifetime would have to be tracked; a capture keeps them).
+template <int N>
+struct CacheList {
+    int n;
+    int a[N], b[N];
+};
+
+struct AppendParams {
+    const __nv_bfloat16* qkv;
+    __nv_bfloat16* q_out;
+    int ld_qkv, ld_q, T, norm, rope, split;
+    long long layer_off;               // elements before the layer in k and v
+    const __nv_bfloat16 *gamma_q, *gamma_k;
+    float eps;
+    const int* pos;
+    uint64_t turn[64];                 // turns per position of each pair, in units of 2^-64
+};
+
+struct AttendParams {
+    const uint64_t* tree;
+    __nv_bfloat16* out;
+    int ld_out;
+    float scale_log2;
+};
+
+cudaError_t launch_cache_step(const CacheDev& c, int n, const int* seq, const int* q_len, int T, cudaStream_t st);
+cudaError_t launch_cache_fork(const CacheDev& c, int n, const int* src, const int* dst, cudaStream_t st);
+cudaError_t launch_cache_truncate(const CacheDev& c, int n, const int* seq, const int* length, cudaStream_t st);
+cudaError_t launch_cache_accept(const CacheDev& c, int n, const int* seq, const int* n_acc, const int* path,
+                                int ld_path, cudaStream_t st);
+cudaError_t launch_cache_compact(const CacheDev& c, cudaStream_t st);
+cudaError_t launch_cache_append(const CacheDev& c, const AppendParams& p, cudaStream_t st);
+cudaError_t launch_cache_attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
+                                const CUtensorMap& tm_v, const AttendParams& p, int max_rows, cudaStream_t st);
+
+}  // namespace tmoe
