@@ -195,12 +195,11 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         return g.valid != 0;
     };
 
+    // Registers go from the first four warps to the softmax warps (80 x 128 + 208 x 256 of the
+    // 168 x 384 at launch).  The branches do not meet again before the roles end:
+    // where they meet, the compiler takes the smaller number.
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    }
-
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 0) {
         // ------------------------------------------------ segments and loads
         const CachePlan pl = *c.plan;
@@ -402,7 +401,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
         }
-    } else if (warp < 4) {
+    } else {
         // ------------------------------------------------------------ guards
         // Values of partly masked tiles: rows that nobody sees become zeros, rows
         // that some see are searched for infinities and NaN.
@@ -447,7 +446,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             cnt += 2 * nt;
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // -------------------------------------------------- softmax and output
         const int slot = (warp - 4) >> 2;
         const int qw = warp & 3;                           // TMEM lane quarter
@@ -543,13 +544,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             l *= f;
                             if (grow) m = top;
 #pragma unroll 1
-                            for (int k = 0; k < DH; k += 32) {
-                                uint32_t o[32];
-                                tmem_ld_32x32(tO + k, o);
+                            for (int k = 0; k < DH; k += 16) {
+                                uint32_t o[16];
+                                tmem_ld_32x16(tO + k, o);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                tmem_st_32x32(tO + k, o);
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                tmem_st_32x16(tO + k, o);
                             }
                         }
                     }
