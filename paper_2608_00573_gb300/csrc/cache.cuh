@@ -56,6 +56,7 @@ struct CacheDev {
     CacheSeq* seqs;                    // [kCacheMaxSeqs]
     CacheGroup* groups;                // [T_max / (2 tile_tokens) + max_seqs + 1]
     int* cta_group;                    // [num_sms + 1] group in which each CTA's share begins
+    long long* cta_begin;              // [num_sms + 1] where on the line of items it begins
     int* slot;                         // [T_max] page row (page * page_size + place) of each new token, -1 none
     int* pos;                          // [T_max] its position in its sequence
     int2* copies;                      // [max(n_pages, max_seqs)] (from, to) pages

@@ -36,6 +36,7 @@
 // Bounds: prompts the tensor cores (and the exponentials: 128 x 128 per 4 x 128 x
 // 128 x D multiply-adds); decoding HBM, each K and V row once per query tile.
 #include <algorithm>
+#include <cstddef>
 
 #include "cache.cuh"
 
@@ -78,7 +79,7 @@ struct __align__(8) Bars {
     int bad[10][2];      // guard warps' finding per ring stage
     float2 xml[128];     // odd slot's maximum and sum per row
     uint32_t tmem_base;
-    int abort_flag;
+    int abort_flag, never;
 };
 constexpr int kSegReaders = 1 + 2 + 8;   // warps that read a segment
 
@@ -106,9 +107,6 @@ __device__ __forceinline__ SegInfo seg_info(const Seg& g, int tile_tokens, bool 
     return s;
 }
 
-// Share of one CTA on the line of items, in the cost units of the plan.
-__device__ __forceinline__ long long share_begin(const CachePlan& pl, int b) { return pl.total * b / pl.n_ctas; }
-
 // Key tiles [t0, t1) of an item (n of them, `a` products each) that the stretch
 // [x0, x1) of its cost covers; stretches that meet cover meeting ranges.
 __device__ __forceinline__ void stretch_tiles(long long x0, long long x1, long long cost, int a, int n, int* t0, int* t1) {
@@ -124,6 +122,75 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Bounded wait by all lanes of a warp.  A probe sleeps until the phase ends or up to
+// about a microsecond; after 2^22 of them, some seconds, the waiter raises the CTA's
+// abort flag and the error word; it also gives up when another role has.  The loop is
+// inside the asm so that control flow stays uniform for the compiler (see elect_one).
+// Returns 0 when the phase ended, 1 when given up.
+__device__ __forceinline__ uint32_t wait_probes(uint32_t bar, uint32_t parity, uint32_t abort_flag, int* err) {
+    uint32_t gave_up;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b32 n, a;\n\t"
+        "mov.b32 n, 0;\n\t"
+        "mov.b32 %0, 0;\n\t"
+        "PROBE:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
+        "@p bra DONE;\n\t"
+        "ld.volatile.shared.b32 a, [%3];\n\t"
+        "setp.ne.b32 p, a, 0;\n\t"
+        "@p bra GONE;\n\t"
+        "add.s32 n, n, 1;\n\t"
+        "setp.lt.s32 p, n, 4194304;\n\t"
+        "@p bra PROBE;\n\t"
+        "st.volatile.shared.b32 [%3], 1;\n\t"
+        "atom.global.cas.b32 a, [%4], 0, %5;\n\t"
+        "GONE:\n\t"
+        "mov.b32 %0, 1;\n\t"
+        "DONE:\n\t}"
+        : "=&r"(gave_up)
+        : "r"(bar), "r"(parity), "r"(abort_flag), "l"(err), "n"((int)ERR_TIMEOUT_CACHE_ATTN)
+        : "memory");
+    return gave_up;
+}
+
+// One lane of a converged warp.  Products and commits stand behind it: the compiler
+// then knows that a single lane issues them and keeps their operands in uniform
+// registers (behind lane == 0 each cost some thirty instructions, more than its 64
+// cycles).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t pred = 0;
+    asm volatile("{\n\t.reg .b32 r;\n\t.reg .pred p;\n\telect.sync r|p, 0xffffffff;\n\t@p mov.s32 %0, 1;\n\t}"
+                 : "+r"(pred));
+    return pred != 0;
+}
+
+// Waits for the TMEM loads in flight; x, one of their results, is not used before.
+__device__ __forceinline__ void landed(uint32_t (&x)[32]) {
+    tmem_ld_wait();
+#pragma unroll
+    for (int j = 0; j < 32; ++j) asm volatile("" : "+r"(x[j]));
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
 
@@ -162,7 +229,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(smem_u32(&bars->seg_full[s]), 1);
             mbar_init(smem_u32(&bars->seg_empty[s]), kSegReaders);
         }
-        bars->abort_flag = 0;
+        bars->abort_flag = bars->never = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_q);
         prefetch_tmap(&tm_k);
@@ -173,33 +240,27 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tbase = bars->tmem_base;
-    volatile int* abort_flag = &bars->abort_flag;
     pdl_wait();
     pdl_trigger();
 
-    auto wait1 = [&](uint64_t* bar, uint32_t parity) {
-        return mbar_wait_bounded(smem_u32(bar), parity & 1u, abort_flag, c.err, ERR_TIMEOUT_CACHE_ATTN);
+    // (Addresses of single barriers are constants beside one base register.)
+    const uint32_t bb = sb + L::BYTES;
+    auto bar = [&](const uint64_t* b) {
+        return bb + (uint32_t)(reinterpret_cast<const uint8_t*>(b) - reinterpret_cast<const uint8_t*>(bars));
     };
-    auto wait_warp = [&](uint64_t* bar, uint32_t parity) {      // lane 0 waits for the warp
-        int ok = 1;
-        if (lane == 0) ok = wait1(bar, parity);
-        return __shfl_sync(0xffffffffu, ok, 0) != 0;
-    };
+    const uint32_t abort_at = bb + (uint32_t)offsetof(Bars, abort_flag);
+    auto wait = [&](const uint64_t* b, uint32_t parity) { return wait_probes(bar(b), parity & 1u, abort_at, c.err); };
+    auto lost = [](uint32_t gave_up) { return __any_sync(0xffffffffu, gave_up) != 0; };
     // The it-th segment of this CTA (false: none left, or aborted).
     auto next_seg = [&](int it, Seg& g) {
         const int s = it % kSegSlots;
-        if (!wait_warp(&bars->seg_full[s], it / kSegSlots)) return false;
+        if (lost(wait(&bars->seg_full[s], it / kSegSlots))) return false;
         g = bars->seg[s];
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars->seg_empty[s]));
-        return g.valid != 0;
+        if (lane == 0) mbar_arrive(bar(&bars->seg_empty[s]));
+        return __shfl_sync(0xffffffffu, g.valid, 0) != 0;
     };
 
-    // Registers go from the first four warps to the softmax warps (80 x 128 + 208 x 256 of the
-    // 168 x 384 at launch).  The branches do not meet again before the roles end:
-    // where they meet, the compiler takes the smaller number.
-    if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 0) {
         // ------------------------------------------------ segments and loads
         const CachePlan pl = *c.plan;
@@ -209,10 +270,10 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         bool ok = true;
         auto give_seg = [&](const Seg& g) {
             const int s = it % kSegSlots;
-            if (it >= kSegSlots && !wait_warp(&bars->seg_empty[s], it / kSegSlots - 1)) return false;
+            if (it >= kSegSlots && lost(wait(&bars->seg_empty[s], it / kSegSlots - 1))) return false;
             if (lane == 0) {
                 bars->seg[s] = g;
-                mbar_arrive(smem_u32(&bars->seg_full[s]));
+                mbar_arrive(bar(&bars->seg_full[s]));
             }
             ++it;
             return true;
@@ -221,8 +282,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         const int my_page = lane / L::KB, my_kb = lane % L::KB;
         int nseg = 0;
         if (pl.ok && b < pl.n_ctas) {
-            long long x = share_begin(pl, b);
-            const long long x_end = share_begin(pl, b + 1);
+            long long x = c.cta_begin[b];
+            const long long x_end = c.cta_begin[b + 1];
             int r = c.cta_group[b];
             CacheGroup g = c.groups[r];
             long long g_next = c.groups[r + 1].pre;
@@ -254,7 +315,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (!give_seg(sg)) break;
                 const SegInfo si = seg_info(sg, TT, tree);
                 // Queries, once the previous segment's products have read theirs.
-                if (nseg > 0 && !wait_warp(&bars->q_empty, nseg - 1)) break;
+                if (nseg > 0 && lost(wait(&bars->q_empty, nseg - 1))) break;
                 if (lane == 0) {
                     const uint32_t qb = smem_u32(&bars->q_full);
                     const uint32_t bytes = (uint32_t)L::KB * TT * rep * 128;
@@ -275,7 +336,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 };
                 auto load = [&](const CUtensorMap* tm, int t, int id) {
                     const int s = (int)(cnt % ST);
-                    if (cnt >= (uint32_t)ST && !wait_warp(&bars->kv_empty[s], cnt / ST - 1)) return false;
+                    if (cnt >= (uint32_t)ST && lost(wait(&bars->kv_empty[s], cnt / ST - 1))) return false;
                     const int have = max(0, min(pages_per_tile, n_pages - t * pages_per_tile));
                     const uint32_t fb = smem_u32(&bars->kv_full[s]);
                     if (lane == 0) mbar_arrive_expect_tx(fb, (uint32_t)have * c.page * 128 * L::KB);
@@ -301,107 +362,109 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
             }
         }
-        if (ok && !*abort_flag) {
+        if (ok) {
             Seg end = {};
             give_seg(end);
         }
         // The last copies have landed, and been read unless the CTA gave up, before
         // it ends.
         const uint32_t tail = min(cnt, (uint32_t)ST);
-        if (lane == 0) {
-            int never = 0;
-            for (uint32_t k = cnt - tail; k < cnt; ++k)
-                mbar_wait_bounded(smem_u32(&bars->kv_full[k % ST]), (k / ST) & 1, &never, c.err, ERR_TIMEOUT_CACHE_ATTN);
-            if (nseg > 0)
-                mbar_wait_bounded(smem_u32(&bars->q_full), (nseg - 1) & 1, &never, c.err, ERR_TIMEOUT_CACHE_ATTN);
-        }
-        __syncwarp();
-        for (uint32_t k = cnt - tail; k < cnt; ++k)
-            if (!wait_warp(&bars->kv_empty[k % ST], k / ST)) break;
+        const uint32_t never = bb + (uint32_t)offsetof(Bars, never);
+        for (uint32_t k = cnt - tail; k < cnt; ++k) wait_probes(bar(&bars->kv_full[k % ST]), (k / ST) & 1, never, c.err);
+        if (nseg > 0) wait_probes(bar(&bars->q_full), (nseg - 1) & 1, never, c.err);
+        for (uint32_t k = cnt - tail; k < cnt; ++k) wait(&bars->kv_empty[k % ST], k / ST);
     } else if (warp == 1) {
         // -------------------------------------------------------------- MMAs
+        // The ring's entries come in the order in which they are used: K of the first
+        // `lead` tiles, then V of tile i and K of tile i + lead in turn.
         constexpr uint32_t idS = idesc_bf16_f32(128, 128);
         constexpr uint32_t idO = idesc_bf16_f32(128, DH) | kIdescBMn;
-        uint32_t cnt = 0, masked = 0, np[2] = {0, 0};     // ring entries, masked tiles, P tiles of each slot
+        const uint32_t tm = __shfl_sync(0xffffffffu, tbase, 0);
+        const uint64_t d_q = smem_desc_sw128(sb + L::Q), d_k = smem_desc_sw128(sb + L::RING);
+        const uint64_t d_v = smem_desc_sw128_mn(sb + L::RING, kBox);
+        constexpr uint32_t kTile16 = L::TILE >> 4;       // a tile in a descriptor's units
+        uint32_t stage = 0, phase = 0, masked = 0, p_phase = 0, gave_up = 0;   // p_phase: one bit per slot
+        auto entry = [&]() {                             // next ring entry, once it has landed
+            const uint32_t e = stage;
+            gave_up |= wait(&bars->kv_full[e], phase);
+            if (++stage == (uint32_t)ST) {
+                stage = 0;
+                phase ^= 1u;
+            }
+            return e;
+        };
         Seg g;
-        bool ok = true;
-        for (int it = 0; ok && next_seg(it, g); ++it) {
-            if (lane == 0) {
-                const SegInfo si = seg_info(g, TT, tree);
-                const int lead = si.dual ? 1 : 2, nt = g.t1 - g.t0;
-                const int lim[2] = {si.n0, si.n1};
-                bool began[2] = {false, false};
-                auto k_entry = [&](int i) { return cnt + i + max(0, i - lead + 1); };
-                auto v_entry = [&](int i) { return cnt + i + min(nt, i + lead); };
-                auto mma_s = [&](int slot, uint32_t e) {
-                    const uint32_t qa = sb + L::Q + (si.dual ? slot * L::TILE : 0);
-                    const uint32_t ka = sb + L::RING + (e % ST) * L::TILE;
-#pragma unroll
-                    for (int kk = 0; kk < DH / 16; ++kk)
-                        tc_mma_bf16(tbase + slot * 128, smem_desc_sw128(qa + (kk >> 2) * kBox + (kk & 3) * 32),
-                                    smem_desc_sw128(ka + (kk >> 2) * kBox + (kk & 3) * 32), idS, kk ? 1u : 0u);
-                    tc_commit(smem_u32(&bars->s_full[slot]));
-                };
-                ok = wait1(&bars->q_full, it);
-                for (int i = 0; ok && i < min(lead, nt); ++i) {
-                    const uint32_t e = k_entry(i);
-                    ok = wait1(&bars->kv_full[e % ST], e / ST);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if ((si.dual || i == 0) && g.t0 + i < lim[0]) mma_s(0, e);
-                    if ((si.dual || i == 1) && g.t0 + i < lim[1]) mma_s(1, e);
-                    tc_commit(smem_u32(&bars->kv_empty[e % ST]));
-                }
-                for (int i = 0; ok && i < nt; ++i) {
-                    const int t = g.t0 + i;
-                    const uint32_t ev = v_entry(i), ek = k_entry(i + lead);
-                    const bool more = i + lead < nt;
-                    ok = wait1(&bars->kv_full[ev % ST], ev / ST);
-                    if (!ok) break;
-                    bool bad = false;
-                    if ((t + 1) * kCacheTile > si.kall) {
-                        const uint32_t gs = masked % ST;
-                        mbar_arrive(smem_u32(&bars->go[gs]));
-                        ok = wait1(&bars->guard[gs], masked / ST);
-                        if (!ok) break;
-                        bad = bars->bad[gs][0] | bars->bad[gs][1];
+        for (int it = 0; !lost(gave_up) && next_seg(it, g); ++it) {
+            const SegInfo si = seg_info(g, TT, tree);
+            auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+            const int dual = uniform(si.dual), lead = dual ? 1 : 2, nt = uniform(g.t1 - g.t0);
+            const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
+            const int first_masked = uniform(si.kall / kCacheTile - g.t0);
+            gave_up |= wait(&bars->q_full, it);
+            // Step i: O += P V of tile i, S = Q K^T of tile i + lead, slot by slot, so that
+            // a slot's products run under the other slot's softmax.  (Given up: the waits
+            // return at once, the products' results are not used.)
+#pragma unroll 1
+            for (int i = -lead; i < nt; ++i) {
+                const int next = i + lead;
+                const bool more = next < nt;
+                uint32_t ev = 0, ek = 0;
+                int bad = 0;
+                if (i >= 0) {
+                    ev = entry();
+                    if (i >= first_masked) {
+                        const uint32_t gs = masked % ST, gp = masked / ST;
                         ++masked;
+                        if (elect_one()) mbar_arrive(bar(&bars->go[gs]));
+                        gave_up |= wait(&bars->guard[gs], gp);
+                        bad = uniform(bars->bad[gs][0] | bars->bad[gs][1]);
                     }
-                    const int s0 = si.dual ? 0 : (i & 1), s1 = si.dual ? 1 : s0;
-                    for (int s = s0; s <= s1; ++s) {
-                        if (t < lim[s]) {
-                            ok = wait1(&bars->p_full[s], np[s]);
-                            if (!ok) break;
-                            ++np[s];
-                            tc_fence_after();
-                            if (!bad) {
-                                const uint32_t va = sb + L::RING + (ev % ST) * L::TILE;
+                }
+                const int s0 = dual ? 0 : (next & 1), s1 = dual ? 1 : s0;
+#pragma unroll 1
+                for (int s = s0; s <= s1; ++s) {
+                    const int ns = s ? n1 : n0;
+                    const bool here = i >= 0 && i < ns;
+                    if (here) {
+                        gave_up |= wait(&bars->p_full[s], p_phase >> s);
+                        p_phase ^= 1u << s;
+                        tc_fence_after();
+                        if (!bad) {              // else the softmax warps have done it
+                            const uint64_t va = d_v + ev * kTile16;
+                            const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128;
+                            const uint32_t began = dual ? i > 0 : i > 1;
+                            if (elect_one()) {
 #pragma unroll
                                 for (int kk = 0; kk < 8; ++kk)
-                                    tc_mma_bf16_ts(tbase + 256 + s * DH, tbase + s * 128 + kk * 8,
-                                                   smem_desc_sw128_mn(va + kk * 2048, kBox), idO,
-                                                   (began[s] || kk) ? 1u : 0u);
+                                    tc_mma_bf16_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : began);
                             }
-                            began[s] = true;
-                        }
-                        if (s == s1) tc_commit(smem_u32(&bars->kv_empty[ev % ST]));
-                        if (more && s == s0) {
-                            ok = wait1(&bars->kv_full[ek % ST], ek / ST);
-                            if (!ok) break;
-                            tc_fence_after();
-                        }
-                        if (t < lim[s]) {
-                            if (more && t + lead < lim[s]) mma_s(s, ek);
-                            else tc_commit(smem_u32(&bars->o_full[s]));
                         }
                     }
-                    if (ok && more) tc_commit(smem_u32(&bars->kv_empty[ek % ST]));
+                    if (i >= 0 && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
+                    if (more && s == s0) {
+                        ek = entry();
+                        tc_fence_after();
+                    }
+                    if (more && next < ns) {
+                        const uint64_t qa = d_q + (dual ? s * kTile16 : 0u), ka = d_k + ek * kTile16;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 0; kk < DH / 16; ++kk) {
+                                const uint32_t off = (kk >> 2) * (kBox >> 4) + (kk & 3) * (32 >> 4);
+                                tc_mma_bf16(tm + s * 128, qa + off, ka + off, idS, kk ? 1u : 0u);
+                            }
+                            tc_commit(bar(&bars->s_full[s]));
+                            if (s == s1) tc_commit(bar(&bars->kv_empty[ek]));
+                        }
+                    } else {
+                        if (here && elect_one()) tc_commit(bar(&bars->o_full[s]));
+                        if (more && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ek]));
+                    }
                 }
-                cnt += 2 * nt;
             }
-            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+            __syncwarp();
         }
-    } else {
+    } else if (warp < 4) {
         // ------------------------------------------------------------ guards
         // Values of partly masked tiles: rows that nobody sees become zeros, rows
         // that some see are searched for infinities and NaN.
@@ -418,7 +481,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 const uint32_t e = cnt + i + min(nt, i + lead);
                 // A parity names a phase only to who has seen the one before: the ring's
                 // phases are followed by the MMA warp, which says when e is there.
-                ok = wait_warp(&bars->go[masked % ST], masked / ST) && wait_warp(&bars->kv_full[e % ST], e / ST);
+                ok = !lost(wait(&bars->go[masked % ST], masked / ST) | wait(&bars->kv_full[e % ST], e / ST));
                 if (!ok) break;
                 uint8_t* v = smem + L::RING + (e % ST) * L::TILE;
                 const int lo = max(0, si.kall - t * kCacheTile), hi = max(0, min(kCacheTile, si.kmax - t * kCacheTile));
@@ -440,15 +503,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 found = __any_sync(0xffffffffu, found);
                 if (lane == 0) {
                     bars->bad[masked % ST][warp - 2] = found;
-                    mbar_arrive(smem_u32(&bars->guard[masked % ST]));
+                    mbar_arrive(bar(&bars->guard[masked % ST]));
                 }
                 ++masked;
             }
             cnt += 2 * nt;
         }
-    }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // -------------------------------------------------- softmax and output
         const int slot = (warp - 4) >> 2;
         const int qw = warp & 3;                           // TMEM lane quarter
@@ -478,31 +539,23 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             if (left == 0) {
                 // Not before this segment's queries are there: an idle slot must not
                 // count for an earlier segment.
-                ok = wait_warp(&bars->q_full, it);
+                ok = !lost(wait(&bars->q_full, it));
                 if (!ok) break;
-                if (lane == 0) mbar_arrive(smem_u32(&bars->q_empty));
+                if (lane == 0) mbar_arrive(bar(&bars->q_empty));
             }
             for (int t = g.t0; ok && t < g.t1; ++t) {
                 const bool part = (t + 1) * kCacheTile > si.kall;
                 const uint32_t mi = masked;
                 if (part) ++masked;
                 if ((!si.dual && ((t - g.t0) & 1) != slot) || t >= lim) continue;
-                ok = wait_warp(&bars->s_full[slot], ns);
+                ok = !lost(wait(&bars->s_full[slot], ns));
                 if (!ok) break;
                 ++ns;
                 tc_fence_after();
                 --left;
-                if (left == 0 && si.dual && lane == 0) mbar_arrive(smem_u32(&bars->q_empty));
+                if (left == 0 && si.dual && lane == 0) mbar_arrive(bar(&bars->q_empty));
                 uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
                 if (live) {
-                    uint32_t u[4][32];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) tmem_ld_32x32(tS + q * 32, u[q]);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) asm volatile("" : "+r"(u[q][j]));
                     if (part) {
                         // Keys of the tile that this row sees, one bit each.
 #pragma unroll
@@ -520,21 +573,37 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                 const int end = g.kv_len - k0;                     // bits past the drafts
                                 see[q] &= end >= 32 ? ~0u : end > 0 ? (1u << end) - 1u : 0u;
                             }
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (!(see[q] >> j & 1u)) u[q][j] = 0xff800000u;    // -inf
                         }
                     }
-                    float mx[4];
+                    // Two passes over the scores in TMEM (the maximum, the exponentials), 32 columns
+                    // at a time with the next load in flight: holding the row in registers
+                    // instead left too few for the rest of the loop.
+                    auto masked_out = [&](int q, uint32_t (&x)[32]) {
+                        if (!part) return;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (!(see[q] >> j & 1u)) x[j] = 0xff800000u;           // -inf
+                    };
+                    uint32_t u[2][32];
+                    float mx = -INFINITY;
+                    tmem_ld_32x32(tS, u[0]);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        mx[q] = __uint_as_float(u[q][0]);
+                        uint32_t(&x)[32] = u[q & 1];
+                        landed(x);
+                        tmem_ld_32x32(tS + ((q + 1) & 3) * 32, u[(q + 1) & 1]);    // q = 3: the second pass's first
+                        masked_out(q, x);
+                        float a[4];
 #pragma unroll
-                        for (int j = 1; j < 31; j += 2)
-                            mx[q] = max3(mx[q], __uint_as_float(u[q][j]), __uint_as_float(u[q][j + 1]));
-                        mx[q] = fmaxf(mx[q], __uint_as_float(u[q][31]));
+                        for (int k = 0; k < 4; ++k) a[k] = fmaxf(__uint_as_float(x[8 * k]), __uint_as_float(x[8 * k + 1]));
+#pragma unroll
+                        for (int j = 2; j < 8; j += 2)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                a[k] = max3(a[k], __uint_as_float(x[8 * k + j]), __uint_as_float(x[8 * k + j + 1]));
+                        mx = max3(max3(mx, a[0], a[1]), a[2], a[3]);
                     }
-                    const float top = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+                    const float top = fmaxf(m, mx);
                     if (t == begin) {
                         m = top;
                     } else {
@@ -554,32 +623,38 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             }
                         }
                     }
-                    const float ms = m == -INFINITY ? 0.f : m * sl2;               // a row without keys so far: p = 0
-                    float ls[4] = {0.f, 0.f, 0.f, 0.f};
+                    const float ms = m == -INFINITY ? 0.f : -m * sl2;              // a row without keys so far: p = 0
+                    float2 ls[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
+                        uint32_t(&x)[32] = u[q & 1];
+                        landed(x);
+                        if (q < 3) tmem_ld_32x32(tS + (q + 1) * 32, u[(q + 1) & 1]);
+                        masked_out(q, x);
                         uint32_t w[16];
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
-                            const float e0 = ex2(fmaf(__uint_as_float(u[q][j]), sl2, -ms));
-                            const float e1 = ex2(fmaf(__uint_as_float(u[q][j + 1]), sl2, -ms));
-                            ls[q] += e0;
-                            ls[q] += e1;
-                            w[j >> 1] = pack_bf16x2(e0, e1);
+                            float2 e = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])),
+                                            make_float2(sl2, sl2), make_float2(ms, ms));
+                            e.x = ex2(e.x);
+                            e.y = ex2(e.y);
+                            ls[(j >> 1) & 1] = add2(ls[(j >> 1) & 1], e);
+                            w[j >> 1] = pack_bf16x2(e.x, e.y);
                         }
                         tmem_st_32x16(tS + q * 16, w);
                     }
-                    l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+                    const float sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+                    l += sum;
                     tmem_st_wait();
                 }
                 if (part) {
-                    ok = wait_warp(&bars->guard[mi % ST], mi / ST);
+                    ok = !lost(wait(&bars->guard[mi % ST], mi / ST));
                     if (!ok) break;
                     if (live && (bars->bad[mi % ST][0] | bars->bad[mi % ST][1])) {
                         // O += P V by this warp, seen keys only.
                         const int i = t - g.t0;
                         const uint32_t e = cnt + i + min(nt, i + lead);
-                        ok = wait_warp(&bars->kv_full[e % ST], e / ST);
+                        ok = !lost(wait(&bars->kv_full[e % ST], e / ST));
                         if (!ok) break;
                         const uint8_t* v = smem + L::RING + (e % ST) * L::TILE;
                         const int keys = min(kCacheTile, si.kmax - t * kCacheTile);
@@ -624,13 +699,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars->p_full[slot]));
+                if (lane == 0) mbar_arrive(bar(&bars->p_full[slot]));
             }
             if (!ok) break;
             cnt += 2 * nt;
             // ---- the segment's result
             if (work) {
-                ok = wait_warp(&bars->o_full[slot], no);
+                ok = !lost(wait(&bars->o_full[slot], no));
                 if (!ok) break;
                 ++no;
                 tc_fence_after();
@@ -659,8 +734,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(smem_u32(&bars->x_full[qw]));
-                        mbar_arrive(smem_u32(&bars->q_empty));
+                        mbar_arrive(bar(&bars->x_full[qw]));
+                        mbar_arrive(bar(&bars->q_empty));
                     }
                 }
                 tc_fence_before();
@@ -668,7 +743,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             float fo = 1.f, fx = 0.f;
             if (joins) {
-                ok = wait_warp(&bars->x_full[qw], nx);
+                ok = !lost(wait(&bars->x_full[qw], nx));
                 if (!ok) break;
                 ++nx;
                 if (live) {
@@ -686,7 +761,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (g.part >= 0) {
                     const size_t row = (size_t)g.part * 256 + (si.dual ? slot * 128 : 0) + r;
                     po = c.part_o + row * DH;
-                    if (mine) c.part_ml[row] = make_float2(work ? m : -INFINITY, l);
+                    if (mine) c.part_ml[row] = make_float2(m, l);
                 } else {
                     out = p.out + (size_t)token * p.ld_out + (size_t)(g.head * rep + head_in_tile) * DH;
                 }
@@ -736,7 +811,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             if (!si.dual && work) {
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars->q_empty));
+                if (lane == 0) mbar_arrive(bar(&bars->q_empty));
             }
             tc_fence_before();
         }
@@ -761,19 +836,19 @@ __global__ void __launch_bounds__(128) cache_join_kernel(const __grid_constant__
     const CachePlan pl = *c.plan;
     const int b = blockIdx.x, TT = c.tile_tokens;
     if (!pl.ok || b + 1 >= pl.n_ctas) return;
-    const long long x = share_begin(pl, b + 1);            // the cut
+    const long long x = c.cta_begin[b + 1];            // the cut
     const CacheGroup g = c.groups[c.cta_group[b + 1]];
     const long long cost = c.groups[c.cta_group[b + 1] + 1].pre - g.pre, within = x - g.pre * c.Hkv;
     const int head = (int)(within / cost);
     const long long start = g.pre * c.Hkv + head * cost;
-    if (x == start || start < share_begin(pl, b)) return;  // cut between items; begun by an earlier CTA
+    if (x == start || start < c.cta_begin[b]) return;  // cut between items; begun by an earlier CTA
     const int a = cache_tile_cost(g.ntok, TT), n = (int)(cost / a) - 1;
     int t0, t1;
     stretch_tiles(0, x - start, cost, a, n, &t0, &t1);
     if (t1 == n) return;                                   // only the item's end is on the other side
     // CTAs b + 1 .. last hold the other parts.
     int last = b + 1;
-    while (last + 1 < pl.n_ctas && share_begin(pl, last + 1) < start + cost) ++last;
+    while (last + 1 < pl.n_ctas && c.cta_begin[last + 1] < start + cost) ++last;
     const int rows_tile = TT * c.rep;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rows = g.ntok > TT ? 128 + (g.ntok - TT) * c.rep : g.ntok * c.rep;
@@ -786,7 +861,7 @@ __global__ void __launch_bounds__(128) cache_join_kernel(const __grid_constant__
         auto part = [&](int k) {
             if (k == 0) return 2 * b + 1;
             int u0, u1;
-            stretch_tiles(share_begin(pl, b + k) - start, min(cost, share_begin(pl, b + k + 1) - start), cost, a, n, &u0,
+            stretch_tiles(c.cta_begin[b + k] - start, min(cost, c.cta_begin[b + k + 1] - start), cost, a, n, &u0,
                           &u1);
             return u0 < u1 ? 2 * (b + k) : -1;
         };
@@ -840,14 +915,6 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
                                          (int)smem_bytes<DH>());
     }, true);
     if (e != cudaSuccess) return e;
-    // The kernel moves registers between its warpgroups: what they ask for (80 x 128 +
-    // 208 x 256) must be within what the block is launched with, or they would wait.
-    static PerDevice regs;
-    const int nreg = regs.get([] {
-        cudaFuncAttributes fa = {};
-        return cudaFuncGetAttributes(&fa, cache_attention_kernel<DH>) == cudaSuccess ? fa.numRegs : 0;
-    });
-    if (nreg * kThreads < 80 * 128 + 208 * 256) return cudaErrorInvalidConfiguration;
     e = launch_pdl(cache_attention_kernel<DH>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
                    c, p);
     if (e != cudaSuccess) return e;

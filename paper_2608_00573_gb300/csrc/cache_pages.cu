@@ -210,8 +210,10 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
         *c.plan = CachePlan{W, n_groups, n_ctas, n_cow, 1};
     }
     __syncthreads();
+    if (i == 0 && n_ctas) c.cta_begin[n_ctas] = W;
     for (int b = i; b < n_ctas; b += kStepThreads) {
-        const long long x = W * b / n_ctas / c.Hkv;
+        const long long begin = W * b / n_ctas, x = begin / c.Hkv;
+        c.cta_begin[b] = begin;
         int r;
         if (n_groups <= kStepThreads) {
             r = find_le(s_pre, n_groups, x);
