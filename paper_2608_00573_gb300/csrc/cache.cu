@@ -205,8 +205,7 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         alloc(d.plan, 1);
         alloc(d.seqs, kCacheMaxSeqs);
         alloc(d.groups, (size_t)cfg->T_max / (2 * d.tile_tokens) + cfg->max_seqs + 1);
-        alloc(d.cta_group, (size_t)d.num_sms + 1);
-        alloc(d.cta_begin, (size_t)d.num_sms + 1);
+        alloc(d.shares, (size_t)d.num_sms);
         alloc(d.slot, cfg->T_max);
         alloc(d.pos, cfg->T_max);
         alloc(d.copies, (size_t)std::max(cfg->n_pages, cfg->max_seqs));

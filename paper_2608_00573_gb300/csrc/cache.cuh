@@ -21,22 +21,32 @@ struct CacheSeq {
 // key/value head; items are ordered by group, then head.
 struct __align__(16) CacheGroup {
     long long pre;                     // cost of one head's items before this group
+    int cost;                          // of one item: (key tiles + 1) << two query tiles
     int seq, kv_len;
     int row, ntok;                     // first packed token, tokens
     int first;                         // position of the first token
     int base;                          // positions before the step
+    int pad[3];
+};
+
+// A CTA's share of the line on which the items' costs are laid end to end.
+struct __align__(16) CacheShare {
+    long long begin, end;
+    long long within;                  // begin, from the start of the item that holds it
+    int group, head;                   // that item
+    CacheGroup g;                      // its group
 };
 
 struct CachePlan {
     long long total;                   // cost of all items
-    int n_groups, n_ctas;              // CTAs that share them
+    int n_groups;
+    int n_ctas;                        // CTAs that share the line; 0: whole items, drawn from a counter
     int copies;                        // pages to copy (shared last pages)
     int ok;                            // 0: the step was refused
+    int drawn, done;                   // items drawn beyond the first round, CTAs that have finished
 };
 
-// Cost of an item in query-tile x key-tile products: its products, plus the
-// same number of products as one key tile for its start and end.
-__host__ __device__ inline int cache_tile_cost(int ntok, int tile_tokens) { return ntok > tile_tokens ? 2 : 1; }
+__host__ __device__ inline int cache_two_tiles(int ntok, int tile_tokens) { return ntok > tile_tokens ? 1 : 0; }
 
 // Key tiles of a group.  Short steps count to the sequence's end, because a draft
 // mask may show any new token to any other.
@@ -55,8 +65,7 @@ struct CacheDev {
     CachePlan* plan;
     CacheSeq* seqs;                    // [kCacheMaxSeqs]
     CacheGroup* groups;                // [T_max / (2 tile_tokens) + max_seqs + 1]
-    int* cta_group;                    // [num_sms + 1] group in which each CTA's share begins
-    long long* cta_begin;              // [num_sms + 1] where on the line of items it begins
+    CacheShare* shares;                // [num_sms]
     int* slot;                         // [T_max] page row (page * page_size + place) of each new token, -1 none
     int* pos;                          // [T_max] its position in its sequence
     int2* copies;                      // [max(n_pages, max_seqs)] (from, to) pages

@@ -107,11 +107,13 @@ __device__ __forceinline__ SegInfo seg_info(const Seg& g, int tile_tokens, bool 
     return s;
 }
 
-// Key tiles [t0, t1) of an item (n of them, `a` products each) that the stretch
-// [x0, x1) of its cost covers; stretches that meet cover meeting ranges.
-__device__ __forceinline__ void stretch_tiles(long long x0, long long x1, long long cost, int a, int n, int* t0, int* t1) {
-    *t0 = (int)min((long long)n, (x0 + a - 1) / a);
-    *t1 = x1 >= cost ? n : (int)min((long long)n, (x1 + a - 1) / a);
+// Key tiles [t0, t1) of an item that the stretch [x0, x1) of its cost covers (two: it
+// has two query tiles); stretches that meet cover meeting ranges.
+__device__ __forceinline__ int item_tiles(int cost, int two) { return (cost >> two) - 1; }
+__device__ __forceinline__ void stretch_tiles(long long x0, long long x1, int cost, int two, int* t0, int* t1) {
+    const int n = item_tiles(cost, two);
+    *t0 = (int)min((long long)n, (x0 + two) >> two);
+    *t1 = x1 >= cost ? n : (int)min((long long)n, (x1 + two) >> two);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -265,7 +267,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         // ------------------------------------------------ segments and loads
         const CachePlan pl = *c.plan;
         const int b = blockIdx.x;
-        int it = 0;
+        int it = 0, nseg = 0;
         uint32_t cnt = 0;                       // ring entries issued
         bool ok = true;
         auto give_seg = [&](const Seg& g) {
@@ -280,68 +282,76 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         };
         const int pages_per_tile = kCacheTile >> c.page_shift;
         const int my_page = lane / L::KB, my_kb = lane % L::KB;
-        int nseg = 0;
-        if (pl.ok && b < pl.n_ctas) {
-            long long x = c.cta_begin[b];
-            const long long x_end = c.cta_begin[b + 1];
-            int r = c.cta_group[b];
-            CacheGroup g = c.groups[r];
-            long long g_next = c.groups[r + 1].pre;
-            while (ok && x < x_end) {
-                const long long cost = g_next - g.pre, within = x - g.pre * c.Hkv;
-                const int head = (int)(within / cost);
-                const long long x0 = within - head * cost, x1 = min(cost, x0 + (x_end - x));
-                const int a = cache_tile_cost(g.ntok, TT);
-                const int n = (int)(cost / a) - 1;
-                Seg sg;
-                sg.valid = 1;
-                sg.seq = g.seq;
-                sg.kv_len = g.kv_len;
-                sg.row = g.row;
-                sg.ntok = g.ntok;
-                sg.first = g.first;
-                sg.base = g.base;
-                sg.head = head;
-                stretch_tiles(x0, x1, cost, a, n, &sg.t0, &sg.t1);
-                sg.part = (sg.t0 == 0 && sg.t1 == n) ? -1 : (sg.t0 > 0 ? 2 * b : 2 * b + 1);
-                sg.pad = 0;
-                x += x1 - x0;
-                if (x >= g_next * c.Hkv && x < x_end) {
-                    ++r;
-                    g = c.groups[r];
-                    g_next = c.groups[r + 1].pre;
+        const bool my_box = lane < pages_per_tile * L::KB;
+        // Whole items are drawn from a counter, longest first; else the CTA's share of the
+        // line is walked item by item.
+        const bool whole = pl.n_ctas == 0;
+        const int items = whole ? pl.n_groups * c.Hkv : 0;
+        int item = b, group = 0, head = 0;
+        long long x = 0, x_end = 0, within = 0;
+        CacheGroup g;
+        bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
+        if (any && !whole) {
+            const CacheShare& sh = c.shares[b];
+            x = sh.begin;
+            x_end = sh.end;
+            within = sh.within;
+            group = sh.group;
+            head = sh.head;
+            g = sh.g;
+        }
+        while (ok && any) {
+            int drawn = 0;
+            Seg sg;
+            if (whole) {
+                if (lane == 0) drawn = atomicAdd(&c.plan->drawn, 1);
+                head = item % c.Hkv;
+                g = c.groups[item / c.Hkv];
+            }
+            const int two_tiles = cache_two_tiles(g.ntok, TT);
+            sg.valid = 1;
+            sg.seq = g.seq;
+            sg.kv_len = g.kv_len;
+            sg.row = g.row;
+            sg.ntok = g.ntok;
+            sg.first = g.first;
+            sg.base = g.base;
+            sg.head = head;
+            sg.pad = 0;
+            if (whole) {
+                sg.t0 = 0;
+                sg.t1 = item_tiles(g.cost, two_tiles);
+                sg.part = -1;
+            } else {
+                const long long x1 = min((long long)g.cost, within + (x_end - x));
+                stretch_tiles(within, x1, g.cost, two_tiles, &sg.t0, &sg.t1);
+                sg.part = (sg.t0 == 0 && sg.t1 == item_tiles(g.cost, two_tiles)) ? -1 : (sg.t0 > 0 ? 2 * b : 2 * b + 1);
+                x += x1 - within;
+                within = 0;
+                any = x < x_end;
+                if (any && ++head == c.Hkv) {
+                    head = 0;
+                    g = c.groups[++group];
                 }
-                if (sg.t0 >= sg.t1) continue;
+            }
+            if (sg.t0 < sg.t1) {
                 if (!give_seg(sg)) break;
                 const SegInfo si = seg_info(sg, TT, tree);
-                // Queries, once the previous segment's products have read theirs.
-                if (nseg > 0 && lost(wait(&bars->q_empty, nseg - 1))) break;
-                if (lane == 0) {
-                    const uint32_t qb = smem_u32(&bars->q_full);
-                    const uint32_t bytes = (uint32_t)L::KB * TT * rep * 128;
-                    mbar_arrive_expect_tx(qb, si.dual ? 2 * bytes : bytes);
-                    for (int s = 0; s < (si.dual ? 2 : 1); ++s)
-                        for (int kb = 0; kb < L::KB; ++kb)
-                            tma_load_3d(sb + L::Q + s * L::TILE + kb * kBox, &tm_q, kb * 64, sg.head * rep,
-                                        sg.row + s * TT, qb);
-                }
-                __syncwarp();
-                ++nseg;
-                // Keys and values: page indices of the tiles ahead travel in registers.
+                // Page indices of the tiles ahead travel in registers.
                 const int n_pages = (si.kmax + c.page - 1) >> c.page_shift;
                 const int* row = c.table + (size_t)sg.seq * c.max_pages;
                 auto page_of = [&](int t) {
                     const int j = t * pages_per_tile + my_page;
-                    return (lane < pages_per_tile * L::KB && t < sg.t1 && j < n_pages) ? row[j] : -1;
+                    return (my_box && t < sg.t1 && j < n_pages) ? row[j] : -1;
                 };
                 auto load = [&](const CUtensorMap* tm, int t, int id) {
                     const int s = (int)(cnt % ST);
                     if (cnt >= (uint32_t)ST && lost(wait(&bars->kv_empty[s], cnt / ST - 1))) return false;
                     const int have = max(0, min(pages_per_tile, n_pages - t * pages_per_tile));
-                    const uint32_t fb = smem_u32(&bars->kv_full[s]);
+                    const uint32_t fb = bar(&bars->kv_full[s]);
                     if (lane == 0) mbar_arrive_expect_tx(fb, (uint32_t)have * c.page * 128 * L::KB);
                     __syncwarp();
-                    if (lane < pages_per_tile * L::KB && my_page < have)
+                    if (my_box && my_page < have)
                         tma_load_2d(sb + L::RING + s * L::TILE + my_kb * kBox + my_page * c.page * 128, tm, my_kb * 64,
                                     (id * c.Hkv + sg.head) << c.page_shift, fb);
                     __syncwarp();
@@ -349,17 +359,46 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     return true;
                 };
                 int id0 = page_of(sg.t0), id1 = page_of(sg.t0 + 1), id2 = page_of(sg.t0 + 2);
-                ok = load(&tm_k, sg.t0, id0);
-                if (ok && !si.dual && sg.t0 + 1 < sg.t1) ok = load(&tm_k, sg.t0 + 1, id1);
-                for (int t = sg.t0; ok && t < sg.t1; ++t) {
-                    const int id3 = page_of(t + 3);
-                    ok = load(&tm_v, t, id0);
-                    const int tk = t + (si.dual ? 1 : 2);
-                    if (ok && tk < sg.t1) ok = load(&tm_k, tk, si.dual ? id1 : id2);
-                    id0 = id1;
-                    id1 = id2;
-                    id2 = id3;
+                const int lead = si.dual ? 1 : 2;
+                // K of the first `lead` tiles, the queries (once the previous segment's products
+                // have read theirs), then V of tile t and K of tile t + lead in turn.
+#pragma unroll 1
+                for (int t = sg.t0 - lead; ok && t < sg.t1; ++t) {
+                    const int tk = t + lead;
+                    if (t >= sg.t0) ok = load(&tm_v, t, id0);
+                    if (ok && tk < sg.t1) ok = load(&tm_k, tk, t < sg.t0 ? (tk == sg.t0 ? id0 : id1) : (lead == 1 ? id1 : id2));
+                    if (ok && t == sg.t0 - 1) {
+                        ok = nseg == 0 || !lost(wait(&bars->q_empty, nseg - 1));
+                        if (ok && lane == 0) {
+                            const uint32_t qb = bar(&bars->q_full);
+                            const uint32_t bytes = (uint32_t)L::KB * TT * rep * 128;
+                            mbar_arrive_expect_tx(qb, si.dual ? 2 * bytes : bytes);
+                            for (int s = 0; s < (si.dual ? 2 : 1); ++s)
+                                for (int kb = 0; kb < L::KB; ++kb)
+                                    tma_load_3d(sb + L::Q + s * L::TILE + kb * kBox, &tm_q, kb * 64, sg.head * rep,
+                                                sg.row + s * TT, qb);
+                        }
+                        __syncwarp();
+                        nseg += ok;
+                    }
+                    if (t >= sg.t0) {
+                        id0 = id1;
+                        id1 = id2;
+                        id2 = page_of(t + 3);
+                    }
                 }
+            }
+            if (whole) {
+                item = (int)gridDim.x + __shfl_sync(0xffffffffu, drawn, 0);
+                any = item < items;
+            }
+        }
+        if (lane == 0 && pl.ok && whole) {
+            // The last CTA to finish drawing leaves the counter at zero for the next call.
+            __threadfence();
+            if (atomicAdd(&c.plan->done, 1) == (int)gridDim.x - 1) {
+                c.plan->drawn = 0;
+                c.plan->done = 0;
             }
         }
         if (ok) {
@@ -404,14 +443,57 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             // Step i: O += P V of tile i, S = Q K^T of tile i + lead, slot by slot, so that
             // a slot's products run under the other slot's softmax.  (Given up: the waits
             // return at once, the products' results are not used.)
+            uint32_t ev = 0, ek = 0;
+            auto pv = [&](int s, bool began) {
+                const uint64_t va = d_v + ev * kTile16;
+                const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128;
+                if (elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        tc_mma_bf16_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : (uint32_t)began);
+                }
+            };
+            auto qk = [&](int s, bool last) {            // last: of the slots that read this key tile
+                const uint64_t qa = d_q + (dual ? s * kTile16 : 0u), ka = d_k + ek * kTile16;
+                if (elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < DH / 16; ++kk) {
+                        const uint32_t off = (kk >> 2) * (kBox >> 4) + (kk & 3) * (32 >> 4);
+                        tc_mma_bf16(tm + s * 128, qa + off, ka + off, idS, kk ? 1u : 0u);
+                    }
+                    tc_commit(bar(&bars->s_full[s]));
+                    if (last) tc_commit(bar(&bars->kv_empty[ek]));
+                }
+            };
+            // Steps below `plain` of a two-tile segment need none of the cases.
+            const int plain = dual ? min(min(n0, n1) - 1, first_masked) : 0;
+            bool have_v = false;                         // V of step i has been waited for
 #pragma unroll 1
             for (int i = -lead; i < nt; ++i) {
+                if (i >= 0 && i < plain) {
+                    if (!have_v) ev = entry();
+                    gave_up |= wait(&bars->p_full[0], p_phase);
+                    tc_fence_after();
+                    pv(0, i > 0);
+                    ek = entry();
+                    tc_fence_after();
+                    qk(0, false);
+                    gave_up |= wait(&bars->p_full[1], p_phase >> 1);
+                    p_phase ^= 3u;
+                    tc_fence_after();
+                    pv(1, i > 0);
+                    if (elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
+                    ev = entry();                        // (step i + 1 exists) under the products queued
+                    have_v = true;
+                    qk(1, true);
+                    continue;
+                }
                 const int next = i + lead;
                 const bool more = next < nt;
-                uint32_t ev = 0, ek = 0;
                 int bad = 0;
                 if (i >= 0) {
-                    ev = entry();
+                    if (!have_v) ev = entry();
+                    have_v = false;
                     if (i >= first_masked) {
                         const uint32_t gs = masked % ST, gp = masked / ST;
                         ++masked;
@@ -429,16 +511,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         gave_up |= wait(&bars->p_full[s], p_phase >> s);
                         p_phase ^= 1u << s;
                         tc_fence_after();
-                        if (!bad) {              // else the softmax warps have done it
-                            const uint64_t va = d_v + ev * kTile16;
-                            const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128;
-                            const uint32_t began = dual ? i > 0 : i > 1;
-                            if (elect_one()) {
-#pragma unroll
-                                for (int kk = 0; kk < 8; ++kk)
-                                    tc_mma_bf16_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : began);
-                            }
-                        }
+                        if (!bad) pv(s, dual ? i > 0 : i > 1);       // else the softmax warps have done it
                     }
                     if (i >= 0 && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
                     if (more && s == s0) {
@@ -446,16 +519,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         tc_fence_after();
                     }
                     if (more && next < ns) {
-                        const uint64_t qa = d_q + (dual ? s * kTile16 : 0u), ka = d_k + ek * kTile16;
-                        if (elect_one()) {
-#pragma unroll
-                            for (int kk = 0; kk < DH / 16; ++kk) {
-                                const uint32_t off = (kk >> 2) * (kBox >> 4) + (kk & 3) * (32 >> 4);
-                                tc_mma_bf16(tm + s * 128, qa + off, ka + off, idS, kk ? 1u : 0u);
-                            }
-                            tc_commit(bar(&bars->s_full[s]));
-                            if (s == s1) tc_commit(bar(&bars->kv_empty[ek]));
-                        }
+                        qk(s, s == s1);
                     } else {
                         if (here && elect_one()) tc_commit(bar(&bars->o_full[s]));
                         if (more && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ek]));
@@ -489,7 +553,10 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll
                     for (int kb = 0; kb < L::KB; ++kb)
                         *reinterpret_cast<uint4*>(v + kb * kBox + x * 16) = make_uint4(0, 0, 0, 0);
-                bool found = false;
+                // x * 0 is NaN for an infinity or a NaN, and the sum keeps it.
+                __nv_bfloat162 sum = __floats2bfloat162_rn(0.f, 0.f);
+                const __nv_bfloat162 zero = sum;
+#pragma unroll 4
                 for (int x = lo * 8 + me; x < hi * 8; x += 64)
 #pragma unroll
                     for (int kb = 0; kb < L::KB; ++kb) {
@@ -497,8 +564,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            found |= (w[k] & 0x7F80u) == 0x7F80u || (w[k] & 0x7F800000u) == 0x7F800000u;
+                            sum = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), zero, sum);
                     }
+                bool found = __hisnan(__low2bfloat16(sum)) || __hisnan(__high2bfloat16(sum));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 found = __any_sync(0xffffffffu, found);
                 if (lane == 0) {
@@ -575,24 +643,20 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             }
                         }
                     }
-                    // Two passes over the scores in TMEM (the maximum, the exponentials), 32 columns
-                    // at a time with the next load in flight: holding the row in registers
-                    // instead left too few for the rest of the loop.
-                    auto masked_out = [&](int q, uint32_t (&x)[32]) {
-                        if (!part) return;
+                    // One pass over the scores in TMEM, 32 columns (a quarter) at a time with the
+                    // next loads in flight; a quarter's maximum is found beside the exponentials
+                    // of the one before (different units).  The reference m is a whole
+                    // number, so that when it moves in the middle of a tile the probabilities
+                    // already written are scaled exactly.
+                    uint32_t u[3][32];
+                    float2 ls[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    auto maximum = [&](int q) {          // of quarter q, masked, in the exponent's unit
+                        uint32_t(&x)[32] = u[q % 3];
+                        if (part) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!(see[q] >> j & 1u)) x[j] = 0xff800000u;           // -inf
-                    };
-                    uint32_t u[2][32];
-                    float mx = -INFINITY;
-                    tmem_ld_32x32(tS, u[0]);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t(&x)[32] = u[q & 1];
-                        landed(x);
-                        tmem_ld_32x32(tS + ((q + 1) & 3) * 32, u[(q + 1) & 1]);    // q = 3: the second pass's first
-                        masked_out(q, x);
+                            for (int j = 0; j < 32; ++j)
+                                if (!(see[q] >> j & 1u)) x[j] = 0xff800000u;       // -inf
+                        }
                         float a[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) a[k] = fmaxf(__uint_as_float(x[8 * k]), __uint_as_float(x[8 * k + 1]));
@@ -601,36 +665,55 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 a[k] = max3(a[k], __uint_as_float(x[8 * k + j]), __uint_as_float(x[8 * k + j + 1]));
-                        mx = max3(max3(mx, a[0], a[1]), a[2], a[3]);
-                    }
-                    const float top = fmaxf(m, mx);
-                    if (t == begin) {
-                        m = top;
-                    } else {
-                        const bool grow = (top - m) * sl2 > 8.f;                   // also from m = -inf
+                        return fmaxf(max3(a[0], a[1], a[2]), a[3]) * sl2;
+                    };
+                    auto follow = [&](int q, float mx) { // moves m before quarter q's exponentials when it has to
+                        const bool grow = mx - m > 8.f;                            // also from m = -inf
                         if (__any_sync(0xffffffffu, grow)) {
-                            const float f = grow ? ex2((m - top) * sl2) : 1.f;
+                            const float up = ceilf(mx), d = m - up;                // m = -inf: the sums so far are 0
+                            const float f = !grow ? 1.f : d < -126.f ? 0.f : __int_as_float(((int)d + 127) << 23);
+                            if (grow) m = up;
                             l *= f;
-                            if (grow) m = top;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                ls[k].x *= f;
+                                ls[k].y *= f;
+                            }
 #pragma unroll 1
-                            for (int k = 0; k < DH; k += 16) {
-                                uint32_t o[16];
-                                tmem_ld_32x16(tO + k, o);
+                            for (int k = 0; k < q * 16; k += 16) {                 // P of the tile's earlier columns
+                                uint32_t w[16];
+                                tmem_st_wait();
+                                tmem_ld_32x16(tS + k, w);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                tmem_st_32x16(tO + k, o);
+                                for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(bf16_lo(w[j]) * f, bf16_hi(w[j]) * f);
+                                tmem_st_32x16(tS + k, w);
+                            }
+                            if (t != begin) {
+#pragma unroll 1
+                                for (int k = 0; k < DH; k += 16) {
+                                    uint32_t o[16];
+                                    tmem_ld_32x16(tO + k, o);
+                                    tmem_ld_wait();
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                    tmem_st_32x16(tO + k, o);
+                                }
                             }
                         }
-                    }
-                    const float ms = m == -INFINITY ? 0.f : -m * sl2;              // a row without keys so far: p = 0
-                    float2 ls[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    };
+                    tmem_ld_32x32(tS, u[0]);
+                    landed(u[0]);
+                    tmem_ld_32x32(tS + 32, u[1]);
+                    follow(0, maximum(0));
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        uint32_t(&x)[32] = u[q & 1];
-                        landed(x);
-                        if (q < 3) tmem_ld_32x32(tS + (q + 1) * 32, u[(q + 1) & 1]);
-                        masked_out(q, x);
+                        if (q < 3) landed(u[(q + 1) % 3]);
+                        if (q < 2) tmem_ld_32x32(tS + (q + 2) * 32, u[(q + 2) % 3]);
+                        uint32_t(&x)[32] = u[q % 3];
+                        const float ms = m == -INFINITY ? 0.f : -m;                // a row without keys so far: p = 0
+                        float mx = 0.f;
+                        if (q < 3) mx = maximum(q + 1);
                         uint32_t w[16];
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
@@ -642,6 +725,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             w[j >> 1] = pack_bf16x2(e.x, e.y);
                         }
                         tmem_st_32x16(tS + q * 16, w);
+                        if (q < 3) follow(q + 1, mx);
                     }
                     const float sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
                     l += sum;
@@ -749,8 +833,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (live) {
                     const float2 x = bars->xml[r];
                     const float top = fmaxf(m, x.x), ms = top == -INFINITY ? 0.f : top;
-                    fo = ex2((m - ms) * sl2);
-                    fx = ex2((x.x - ms) * sl2);
+                    fo = ex2(m - ms);
+                    fx = ex2(x.x - ms);
                     l = l * fo + x.y * fx;
                     m = top;
                 }
@@ -824,83 +908,87 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     }
 }
 
-// Joins the parts of cut items.  Block (b, y) takes rows [16 y, 16 y + 16) of the
-// item that CTA b of the attention began and did not finish; a warp takes a row:
-// its lanes read the parts' maxima and sums, then D / 32 columns each of the parts'
-// sums, added in the order of the keys.
+// Joins the parts of cut items.  Block (b, y) takes rows [32 y, 32 y + 32) of the
+// item that CTA b of the attention began and did not finish; a warp takes four
+// rows, a lane D / 32 columns of each; the parts are added in the order of the keys.
+// Bound: latency (a few dependent reads) and L2, 2 to 3 parts of up to 256 x D fp32
+// per cut.
 template <int DH>
-__global__ void __launch_bounds__(128) cache_join_kernel(const __grid_constant__ CacheDev c,
+__global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__ CacheDev c,
                                                          const __grid_constant__ AttendParams p) {
     pdl_wait();
     pdl_trigger();
-    const CachePlan pl = *c.plan;
-    const int b = blockIdx.x, TT = c.tile_tokens;
-    if (!pl.ok || b + 1 >= pl.n_ctas) return;
-    const long long x = c.cta_begin[b + 1];            // the cut
-    const CacheGroup g = c.groups[c.cta_group[b + 1]];
-    const long long cost = c.groups[c.cta_group[b + 1] + 1].pre - g.pre, within = x - g.pre * c.Hkv;
-    const int head = (int)(within / cost);
-    const long long start = g.pre * c.Hkv + head * cost;
-    if (x == start || start < c.cta_begin[b]) return;  // cut between items; begun by an earlier CTA
-    const int a = cache_tile_cost(g.ntok, TT), n = (int)(cost / a) - 1;
+    const int n_ctas = c.plan->n_ctas, b = blockIdx.x, TT = c.tile_tokens;
+    if (!c.plan->ok || b + 1 >= n_ctas) return;
+    // The item in which CTA b + 1 begins, if it is in its middle, and was begun by CTA b.
+    const CacheShare next = c.shares[b + 1];
+    const CacheGroup& g = next.g;
+    const long long start = next.begin - next.within;
+    if (next.within == 0 || start < c.shares[b].begin) return;
+    const int two = cache_two_tiles(g.ntok, TT), n = item_tiles(g.cost, two);
     int t0, t1;
-    stretch_tiles(0, x - start, cost, a, n, &t0, &t1);
+    stretch_tiles(0, next.within, g.cost, two, &t0, &t1);
     if (t1 == n) return;                                   // only the item's end is on the other side
-    // CTAs b + 1 .. last hold the other parts.
-    int last = b + 1;
-    while (last + 1 < pl.n_ctas && c.cta_begin[last + 1] < start + cost) ++last;
-    const int rows_tile = TT * c.rep;
+    const int rows = two ? 128 + (g.ntok - TT) * c.rep : g.ntok * c.rep;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rows = g.ntok > TT ? 128 + (g.ntok - TT) * c.rep : g.ntok * c.rep;
+    const int r0 = blockIdx.y * 32 + warp * 4;
+    if (r0 >= rows) return;
     constexpr int V = DH / 32;
-    for (int r = blockIdx.y * 16 + warp; r < min(rows, blockIdx.y * 16 + 16); r += 4) {
-        const int tile = r >> 7, in = r & 127;
-        if (in >= rows_tile) continue;
-        const int token = g.row + tile * TT + in / c.rep, h = head * c.rep + in % c.rep;
-        // Part k of the item is in buffer part(k), or none when its stretch holds no tile.
-        auto part = [&](int k) {
-            if (k == 0) return 2 * b + 1;
-            int u0, u1;
-            stretch_tiles(c.cta_begin[b + k] - start, min(cost, c.cta_begin[b + k + 1] - start), cost, a, n, &u0,
-                          &u1);
-            return u0 < u1 ? 2 * (b + k) : -1;
-        };
-        const int parts = last - b + 1;
-        float top = -INFINITY;
-        for (int k = lane; k < parts; k += 32) {
-            const int s = part(k);
-            if (s >= 0) top = fmaxf(top, c.part_ml[(size_t)s * 256 + r].x);
-        }
+    float top[4], l[4], acc[4][V];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float ms = top == -INFINITY ? 0.f : top;
-        float l = 0.f, acc[V];
+    for (int k = 0; k < 4; ++k) {
+        top[k] = -INFINITY;
+        l[k] = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.f;
-        for (int k0 = 0; k0 < parts; k0 += 32) {
-            const int k = k0 + lane, s = k < parts ? part(k) : -1;
-            float f = 0.f, lk = 0.f;
-            if (s >= 0) {
-                const float2 ml = c.part_ml[(size_t)s * 256 + r];
-                f = ex2((ml.x - ms) * p.scale_log2);
-                lk = ml.y * f;
-            }
-            const int cnt = min(32, parts - k0);
-            for (int i = 0; i < cnt; ++i) {
-                const int si = __shfl_sync(0xffffffffu, s, i);
-                const float fi = __shfl_sync(0xffffffffu, f, i);
-                l += __shfl_sync(0xffffffffu, lk, i);
-                if (si < 0 || fi == 0.f) continue;
-                const float* src = c.part_o + ((size_t)si * 256 + r) * DH + lane * V;
+        for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
+    }
+    // Running maximum over the parts: CTA b's in its second buffer, the others' in their first.
+    int s = 2 * b + 1;
+#pragma unroll 1
+    for (int k = b;;) {
+        float2 ml[4];
+        float o[4][V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] = fmaf(src[j], fi, acc[j]);
+        for (int q = 0; q < 4; ++q) {
+            const size_t row = (size_t)s * 256 + min(r0 + q, 255);
+            ml[q] = c.part_ml[row];
+            const float* src = c.part_o + row * DH + lane * V;
+            if (V == 4) {
+                const float4 f = *reinterpret_cast<const float4*>(src);
+                o[q][0] = f.x, o[q][1] = f.y, o[q][V - 2] = f.z, o[q][V - 1] = f.w;
+            } else {
+                const float2 f = *reinterpret_cast<const float2*>(src);
+                o[q][0] = f.x, o[q][1] = f.y;
             }
         }
-        const float il = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float m = fmaxf(top[q], ml[q].x), ref = m == -INFINITY ? 0.f : m;
+            const float fa = ex2(top[q] - ref), fb = ex2(ml[q].x - ref);
+            top[q] = m;
+            l[q] = l[q] * fa + ml[q].y * fb;
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[q][j] = acc[q][j] * fa + o[q][j] * fb;
+        }
+        if (t1 == n) break;
+        do {                                               // the next CTA whose stretch holds a tile
+            ++k;
+            const int from = t1;
+            stretch_tiles(0, c.shares[k].end - start, g.cost, two, &t0, &t1);
+            t0 = from;
+        } while (t0 == t1);
+        s = 2 * k;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = r0 + q, tile = r >> 7, in = r & 127;
+        if (r >= rows || in >= TT * c.rep) continue;
+        const int token = g.row + tile * TT + in / c.rep, h = next.head * c.rep + in % c.rep;
+        const float il = l[q] == 0.f ? 0.f : 1.f / l[q];
         __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + lane * V;
 #pragma unroll
         for (int j = 0; j < V; j += 2)
-            *reinterpret_cast<uint32_t*>(out + j) = pack_bf16x2(acc[j] * il, acc[j + 1] * il);
+            *reinterpret_cast<uint32_t*>(out + j) = pack_bf16x2(acc[q][j] * il, acc[q][j + 1] * il);
     }
 }
 
@@ -918,7 +1006,7 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
     e = launch_pdl(cache_attention_kernel<DH>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
                    c, p);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 15) / 16), dim3(128), 0, st, c, p);
+    return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);
 }
 
 }  // namespace

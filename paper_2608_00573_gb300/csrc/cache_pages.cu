@@ -22,7 +22,8 @@ namespace {
 constexpr int kStepThreads = 1024;
 constexpr int kCopyThreads = 256;
 constexpr int kCopyVecs = 4;           // 16-byte vectors in flight per thread
-// Smallest share of a CTA, in tile products: below it, fewer CTAs take part.
+// Smallest share of a CTA on the line of items (see CacheShare): below it, fewer
+// CTAs take part.
 constexpr int kMinShare = 3;
 
 // Exclusive prefix sum over the block; every thread gets the total.  ws: 33 entries.
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     __shared__ int s_pages[kCacheMaxSeqs + 1], s_groups[kCacheMaxSeqs + 1];
     __shared__ int s_len[kCacheMaxSeqs], s_last[kCacheMaxSeqs], s_cow[kCacheMaxSeqs];
     __shared__ long long s_pre[kStepThreads], s_wsl[33];
-    __shared__ int s_ws[33], s_bad;
+    __shared__ int s_ws[33], s_bad, s_most, s_bucket[kStepThreads];
     pdl_wait();
     pdl_trigger();
     const int i = threadIdx.x, n = l.n, TT = c.tile_tokens;
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     __syncthreads();
     if (s_bad) {
         if (i == 0) {
-            *c.plan = CachePlan{0, 0, 0, 0, 0};
+            *c.plan = CachePlan{};
             atomicCAS(c.err, 0, s_bad);
         }
         return;
@@ -177,46 +178,76 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     __syncthreads();   // s_pages has been read: it takes the token offsets
     if (i < n) s_pages[i] = at_tok;
     __syncthreads();
-    long long total = 0;
-    for (int b = 0; b < n_groups; b += kStepThreads) {
-        const int r = b + i;
+    // The work list.  Groups are numbered in the order of the sequences; when whole
+    // items will be drawn (below), they are stored longest first.
+    auto group_of = [&](int r) {
         CacheGroup g;
-        long long cost = 0;
-        if (r < n_groups) {
-            const int s = find_le(s_groups, n, r);
-            const int q_len = l.b[s], tok = (r - s_groups[s]) * 2 * TT;
-            g.seq = l.a[s];
-            g.kv_len = s_len[s] + q_len;
-            g.row = s_pages[s] + tok;
-            g.ntok = min(2 * TT, q_len - tok);
-            g.first = s_len[s] + tok;
-            g.base = s_len[s];
-            cost = (long long)cache_tile_cost(g.ntok, TT) *
-                   (cache_group_tiles(q_len, g.kv_len, g.first, g.ntok) + 1);
-        }
-        long long sum;
-        const long long pre = total + block_scan(cost, s_wsl, sum);
-        if (r < n_groups) {
-            g.pre = pre;
-            c.groups[r] = g;
-            if (n_groups <= kStepThreads) s_pre[r] = pre;
-        }
-        total += sum;
+        const int s = find_le(s_groups, n, r);
+        const int q_len = l.b[s], tok = (r - s_groups[s]) * 2 * TT;
+        g.seq = l.a[s];
+        g.kv_len = s_len[s] + q_len;
+        g.row = s_pages[s] + tok;
+        g.ntok = min(2 * TT, q_len - tok);
+        g.first = s_len[s] + tok;
+        g.base = s_len[s];
+        g.cost = (cache_group_tiles(q_len, g.kv_len, g.first, g.ntok) + 1) << cache_two_tiles(g.ntok, TT);
+        g.pre = 0;
+        return g;
+    };
+    long long cost = 0, total;
+    int most = 0;
+    for (int r = i; r < n_groups; r += kStepThreads) {
+        const int k = group_of(r).cost;
+        cost += k;
+        most = max(most, k);
     }
-    const long long W = total * c.Hkv;
-    const int n_ctas = W ? (int)max(1LL, min((long long)c.num_sms, W / kMinShare)) : 0;
-    if (i == 0) {
-        c.groups[n_groups].pre = total;
-        *c.plan = CachePlan{W, n_groups, n_ctas, n_cow, 1};
-    }
+    block_scan(cost, s_wsl, total);
+    if (i == 0) s_most = 0;
     __syncthreads();
-    if (i == 0 && n_ctas) c.cta_begin[n_ctas] = W;
+    if (i < n_groups) atomicMax(&s_most, most);
+    __syncthreads();
+    const long long W = total * c.Hkv;
+    const bool whole = 2LL * s_most * c.num_sms <= W;
+    const int n_ctas = !W || whole ? 0 : (int)max(1LL, min((long long)c.num_sms, W / kMinShare));
+    if (whole) {
+        // Counting sort by cost, costs past the last bucket together in the first one.
+        if (i < kStepThreads) s_bucket[i] = 0;
+        __syncthreads();
+        for (int r = i; r < n_groups; r += kStepThreads) atomicAdd(&s_bucket[max(0, kStepThreads - 1 - group_of(r).cost)], 1);
+        __syncthreads();
+        int all;
+        const int at = block_scan(s_bucket[i], s_ws, all);
+        s_bucket[i] = at;
+        __syncthreads();
+        for (int r = i; r < n_groups; r += kStepThreads) {
+            const CacheGroup g = group_of(r);
+            c.groups[atomicAdd(&s_bucket[max(0, kStepThreads - 1 - g.cost)], 1)] = g;
+        }
+    } else {
+        long long before = 0;
+        for (int b = 0; b < n_groups; b += kStepThreads) {
+            const int r = b + i;
+            CacheGroup g;
+            if (r < n_groups) g = group_of(r);
+            long long sum;
+            const long long pre = before + block_scan(r < n_groups ? (long long)g.cost : 0LL, s_wsl, sum);
+            if (r < n_groups) {
+                g.pre = pre;
+                c.groups[r] = g;
+                if (n_groups <= kStepThreads) s_pre[r] = pre;
+            }
+            before += sum;
+        }
+    }
+    if (i == 0) *c.plan = CachePlan{W, n_groups, n_ctas, n_cow, 1, 0, 0};
+    __syncthreads();
     for (int b = i; b < n_ctas; b += kStepThreads) {
-        const long long begin = W * b / n_ctas, x = begin / c.Hkv;
-        c.cta_begin[b] = begin;
-        int r;
+        CacheShare sh;
+        sh.begin = W * b / n_ctas;
+        sh.end = W * (b + 1) / n_ctas;
+        const long long x = sh.begin / c.Hkv;
         if (n_groups <= kStepThreads) {
-            r = find_le(s_pre, n_groups, x);
+            sh.group = find_le(s_pre, n_groups, x);
         } else {
             int lo = 0, hi = n_groups;
             while (hi - lo > 1) {
@@ -224,9 +255,13 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
                 if (c.groups[m].pre <= x) lo = m;
                 else hi = m;
             }
-            r = lo;
+            sh.group = lo;
         }
-        c.cta_group[b] = r;
+        sh.g = c.groups[sh.group];
+        sh.within = sh.begin - sh.g.pre * c.Hkv;
+        sh.head = (int)(sh.within / sh.g.cost);
+        sh.within -= (long long)sh.head * sh.g.cost;
+        c.shares[b] = sh;
     }
 }
 
@@ -415,7 +450,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_compact_kernel(const __gri
     const int movers = collect_pages(c.ref, live, c.n_pages, true, holes, &c.copies[0].x, 2, s_ws);
     __syncthreads();
     for (int k = threadIdx.x; k < movers; k += kStepThreads) c.fresh[c.copies[k].x] = c.copies[k].y;
-    if (threadIdx.x == 0) *c.plan = CachePlan{live, 0, 0, movers, 0};
+    if (threadIdx.x == 0) *c.plan = CachePlan{live, 0, 0, movers, 0, 0, 0};
 }
 
 // Tables and counts follow the moved pages.
