@@ -6,6 +6,7 @@ It raises if the compiled library is missing: there is no fallback path.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 import threading
@@ -484,6 +485,10 @@ class PagedCache:
         import torch
         self.torch = torch
         self.handle = None
+        self._lib = _cache_lib()
+        self._bf16 = torch.bfloat16
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._append_args, self._attend_args = trimmoe_append_args(), trimmoe_attend_args()
         if k.dim() != 5 or k.shape != v.shape or table.dim() != 2 or length.dim() != 1 or ref.dim() != 1:
             raise TrimmoeError(-1, "cache: k and v are [layers][n_pages][kv_heads][page][head_dim], table is "
                                    "[max_seqs][max_pages], length and ref are vectors")
@@ -499,6 +504,8 @@ class PagedCache:
                 raise TrimmoeError(-1, "cache: tensors must be contiguous")
         self.k, self.v, self.table, self.length, self.ref = k, v, table, length, ref
         self.T = 0
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         cfg = trimmoe_cache_config(layers=self.layers, q_heads=self.q_heads, kv_heads=self.kv_heads,
                                    head_dim=self.head_dim, page_size=self.page, n_pages=self.n_pages,
                                    max_seqs=self.max_seqs, max_pages=self.max_pages, T_max=self.T_max)
@@ -521,6 +528,9 @@ class PagedCache:
                    torch.zeros(n_pages, dtype=torch.int32, device=device), q_heads, T_max)
 
     # checks and calls ------------------------------------------------------
+    # A decode step calls append and attend once per layer, and on the GPU they take a
+    # few microseconds: the checks below are ordered and kept so that a call costs about
+    # as much on the host.
     def _tensor(self, t, dtype, shape, what):
         if t is None:
             return
@@ -528,106 +538,123 @@ class PagedCache:
             raise TrimmoeError(-1, f"{what}: tensors must be on the cache's GPU")
         if t.dtype != dtype:
             raise TrimmoeError(-1, f"{what}: expected {dtype}, got {t.dtype}")
-        if shape is not None and (tuple(t.shape) != tuple(shape) or (t.numel() and t.stride(-1) != 1)):
-            raise TrimmoeError(-1, f"{what}: expected shape {tuple(shape)} with contiguous rows, got {tuple(t.shape)}")
+        if shape is not None and (tuple(t.shape) != tuple(shape) or (t.numel() and not t.is_contiguous())):
+            raise TrimmoeError(-1, f"{what}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
 
     def _rows(self, t, cols, what):
         """Row stride of a [T][cols] tensor."""
-        self._tensor(t, self.torch.bfloat16, (self.T, cols), what)
-        return t.stride(0) if self.T > 1 else max(cols, t.stride(0))
+        if (isinstance(t, self.torch.Tensor) and t.dtype == self._bf16 and t.dim() == 2 and t.device == self.device):
+            n, k = t.shape
+            ld, one = t.stride()
+            if n == self.T and k == cols and (one == 1 or not n):
+                return ld if n > 1 else max(cols, ld)
+        self._tensor(t, self._bf16, None, what)
+        raise TrimmoeError(-1, f"{what}: expected shape {(self.T, cols)} with contiguous rows, got {tuple(t.shape)}")
 
     def _new(self, cols, stream):
         """A [T][cols] result, allocated on the stream that writes it."""
         t = self.torch
-        with t.cuda.stream(stream):          # None: the current stream
-            return t.empty((self.T, cols), dtype=t.bfloat16, device=self.device)
+        if stream is None:
+            return t.empty((self.T, cols), dtype=self._bf16, device=self.device)
+        with t.cuda.stream(stream):
+            return t.empty((self.T, cols), dtype=self._bf16, device=self.device)
 
     @staticmethod
     def _list(v):
-        a = np.ascontiguousarray(v, dtype=np.int32)
-        if a.ndim != 1:
-            raise TrimmoeError(-1, "cache: sequence lists have one dimension")
-        return a
+        """Host int32 list: (object that owns it, address, length, values)."""
+        if isinstance(v, np.ndarray):
+            if v.ndim != 1 or v.dtype.kind not in "iu":
+                raise TrimmoeError(-1, "cache: sequence lists are one-dimensional, of integers")
+            v = v.tolist()
+        try:
+            a = array.array("i", v)
+        except (TypeError, OverflowError) as e:
+            raise TrimmoeError(-1, f"cache: sequence lists hold 32-bit integers ({e})") from None
+        return a, a.buffer_info()[0], len(a)
 
     def _pair(self, a, b, what):
         a, b = self._list(a), self._list(b)
-        if a.shape != b.shape:
+        if a[2] != b[2]:
             raise TrimmoeError(-1, f"{what}: lists of different lengths")
         return a, b
 
-    def _call(self, name, *args, stream=None):
-        s = stream if stream is not None else self.torch.cuda.current_stream(self.device)
-        L = _cache_lib()
-        rc = getattr(L, "trimmoe_cache_" + name)(self.handle, *args, C.c_void_p(int(s.cuda_stream)))
+    def _stream(self, stream):
+        if stream is not None:
+            return int(stream.cuda_stream)
+        if self._raw_stream is not None:
+            return self._raw_stream(self.device.index)
+        return int(self.torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _done(self, rc):
         if rc != TRIMMOE_OK:
-            raise TrimmoeError(rc, L.trimmoe_cache_last_error(self.handle).decode())
+            raise TrimmoeError(rc, self._lib.trimmoe_cache_last_error(self.handle).decode())
 
     def step(self, seq, q_len, stream=None):
         """Room for q_len[i] new tokens of sequence seq[i]; the work list of append and attend."""
         seq, q_len = self._pair(seq, q_len, "step")
-        self._call("step", len(seq), _ptr(seq), _ptr(q_len), stream=stream)
-        self.T = int(q_len.sum())
+        self._done(self._lib.trimmoe_cache_step(self.handle, seq[2], seq[1], q_len[1], self._stream(stream)))
+        self.T = sum(q_len[0])
 
     def append(self, layer: int, qkv, q_out=None, gamma_q=None, gamma_k=None, eps: float = 1e-6, theta: float = 1e6,
                pos=None, stream=None):
         """Norm (with gammas) and rotate the step's queries and keys of qkv [T][(q + 2 kv heads) * head_dim], write
         its keys and values into the cache; returns the queries [T][q_heads * head_dim] (q_out, which may be a
         view of qkv's query columns)."""
-        t, hd = self.torch, self.head_dim
-        ld = self._rows(qkv, (self.q_heads + 2 * self.kv_heads) * hd, "append")
+        hd, a = self.head_dim, self._append_args
+        a.ld_qkv = self._rows(qkv, (self.q_heads + 2 * self.kv_heads) * hd, "append")
         if q_out is None:
             q_out = self._new(self.q_heads * hd, stream)
-        ld_q = self._rows(q_out, self.q_heads * hd, "append")
+        a.ld_q = self._rows(q_out, self.q_heads * hd, "append")
         for g in (gamma_q, gamma_k):
-            self._tensor(g, t.bfloat16, (hd,), "append")
-        if pos is not None:
-            self._tensor(pos, t.int32, (self.T,), "append")
-        a = trimmoe_append_args(qkv=_ptr(qkv), ld_qkv=ld, q_out=_ptr(q_out), ld_q=ld_q, gamma_q=_ptr(gamma_q),
-                                gamma_k=_ptr(gamma_k), norm_eps=eps, rope_theta=theta, pos=_ptr(pos))
-        self._call("append", layer, C.byref(a), stream=stream)
+            self._tensor(g, self._bf16, (hd,), "append")
+        self._tensor(pos, self.torch.int32, (self.T,), "append")
+        a.qkv, a.q_out, a.gamma_q, a.gamma_k, a.pos = (qkv.data_ptr(), q_out.data_ptr(), _ptr(gamma_q), _ptr(gamma_k),
+                                                       _ptr(pos))
+        a.norm_eps, a.rope_theta = eps, theta
+        self._done(self._lib.trimmoe_cache_append(self.handle, layer, C.addressof(a), self._stream(stream)))
         return q_out
 
     def attend(self, layer: int, q, out=None, tree=None, scale: float = 0.0, stream=None):
         """Attention of the step's queries [T][q_heads * head_dim] over their sequences; tree: int64 [T] words, bit j
         = sees new token j of its sequence (default: causal)."""
-        t, cols = self.torch, self.q_heads * self.head_dim
-        ld = self._rows(q, cols, "attend")
+        cols, a = self.q_heads * self.head_dim, self._attend_args
+        a.ld_q = self._rows(q, cols, "attend")
         if out is None:
             out = self._new(cols, stream)
-        ld_out = self._rows(out, cols, "attend")
-        if tree is not None:
-            self._tensor(tree, t.int64, (self.T,), "attend")
-        a = trimmoe_attend_args(q=_ptr(q), ld_q=ld, out=_ptr(out), ld_out=ld_out, tree=_ptr(tree), scale=scale)
-        self._call("attend", layer, C.byref(a), stream=stream)
+        a.ld_out = self._rows(out, cols, "attend")
+        self._tensor(tree, self.torch.int64, (self.T,), "attend")
+        a.q, a.out, a.tree, a.scale = q.data_ptr(), out.data_ptr(), _ptr(tree), scale
+        self._done(self._lib.trimmoe_cache_attend(self.handle, layer, C.addressof(a), self._stream(stream)))
         return out
 
     def fork(self, src, dst, stream=None):
         """Sequences dst[i] become continuations of src[i] and share its pages."""
         src, dst = self._pair(src, dst, "fork")
-        self._call("fork", len(dst), _ptr(src), _ptr(dst), stream=stream)
+        self._done(self._lib.trimmoe_cache_fork(self.handle, dst[2], src[1], dst[1], self._stream(stream)))
 
     def truncate(self, seq, length, stream=None):
         """Cut sequences to at most length[i] positions (0 frees them)."""
         seq, length = self._pair(seq, length, "truncate")
-        self._call("truncate", len(seq), _ptr(seq), _ptr(length), stream=stream)
+        self._done(self._lib.trimmoe_cache_truncate(self.handle, seq[2], seq[1], length[1], self._stream(stream)))
 
     def accept(self, seq, n_acc, path, stream=None):
         """Keep the drafts path[i][:n_acc[i]] of the last step (int32 tensors [n] and [n][depth]), moved to the front."""
         seq = self._list(seq)
-        self._tensor(n_acc, self.torch.int32, (len(seq),), "accept")
-        if path.dim() != 2 or not path.is_contiguous():
-            raise TrimmoeError(-1, "accept: path is a contiguous [n][depth] tensor")
-        self._tensor(path, self.torch.int32, (len(seq), path.shape[1]), "accept")
-        self._call("accept", len(seq), _ptr(seq), _ptr(n_acc), _ptr(path), path.shape[1], stream=stream)
+        self._tensor(n_acc, self.torch.int32, (seq[2],), "accept")
+        if path.dim() != 2:
+            raise TrimmoeError(-1, "accept: path is [n][depth]")
+        self._tensor(path, self.torch.int32, (seq[2], path.shape[1]), "accept")
+        self._done(self._lib.trimmoe_cache_accept(self.handle, seq[2], seq[1], n_acc.data_ptr(), path.data_ptr(),
+                                                  path.shape[1], self._stream(stream)))
 
     def compact(self, stream=None):
         """Move the pages in use to the lowest indices."""
-        self._call("compact", stream=stream)
+        self._done(self._lib.trimmoe_cache_compact(self.handle, self._stream(stream)))
 
     def stats(self, reset: bool = False) -> dict:
         """Synchronises; {status, device_error, free_pages, launches}."""
         s = trimmoe_cache_stats_t()
-        rc = _cache_lib().trimmoe_cache_stats(self.handle, C.byref(s), int(reset))
+        rc = self._lib.trimmoe_cache_stats(self.handle, C.byref(s), int(reset))
         return dict(status=rc, device_error=s.device_error, free_pages=s.free_pages, launches=s.launches)
 
     def close(self):
