@@ -488,7 +488,10 @@ class PagedCache:
         self._lib = _cache_lib()
         self._bf16 = torch.bfloat16
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._Tensor, self._empty, self._int32, self._int64 = torch.Tensor, torch.empty, torch.int32, torch.int64
         self._append_args, self._attend_args = trimmoe_append_args(), trimmoe_attend_args()
+        self._append_at, self._attend_at = C.addressof(self._append_args), C.addressof(self._attend_args)
+        self._c_append, self._c_attend = self._lib.trimmoe_cache_append, self._lib.trimmoe_cache_attend
         if k.dim() != 5 or k.shape != v.shape or table.dim() != 2 or length.dim() != 1 or ref.dim() != 1:
             raise TrimmoeError(-1, "cache: k and v are [layers][n_pages][kv_heads][page][head_dim], table is "
                                    "[max_seqs][max_pages], length and ref are vectors")
@@ -506,6 +509,8 @@ class PagedCache:
         self.T = 0
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        self._q_cols, self._qkv_cols = self.q_heads * self.head_dim, (self.q_heads + 2 * self.kv_heads) * self.head_dim
         cfg = trimmoe_cache_config(layers=self.layers, q_heads=self.q_heads, kv_heads=self.kv_heads,
                                    head_dim=self.head_dim, page_size=self.page, n_pages=self.n_pages,
                                    max_seqs=self.max_seqs, max_pages=self.max_pages, T_max=self.T_max)
@@ -543,21 +548,29 @@ class PagedCache:
 
     def _rows(self, t, cols, what):
         """Row stride of a [T][cols] tensor."""
-        if (isinstance(t, self.torch.Tensor) and t.dtype == self._bf16 and t.dim() == 2 and t.device == self.device):
-            n, k = t.shape
+        if isinstance(t, self._Tensor) and t.dtype is self._bf16 and t.get_device() == self._index and \
+                t.shape == (self.T, cols):
             ld, one = t.stride()
-            if n == self.T and k == cols and (one == 1 or not n):
-                return ld if n > 1 else max(cols, ld)
+            if one == 1 or not self.T:
+                return ld if self.T > 1 else max(cols, ld)
         self._tensor(t, self._bf16, None, what)
         raise TrimmoeError(-1, f"{what}: expected shape {(self.T, cols)} with contiguous rows, got {tuple(t.shape)}")
 
+    def _vector(self, t, dtype, n, what):
+        """Address of a vector of n values, None without one."""
+        if t is None:
+            return None
+        if not (isinstance(t, self._Tensor) and t.dtype is dtype and t.get_device() == self._index and t.shape == (n,) and
+                (n < 2 or t.stride(0) == 1)):
+            self._tensor(t, dtype, (n,), what)
+        return t.data_ptr()
+
     def _new(self, cols, stream):
         """A [T][cols] result, allocated on the stream that writes it."""
-        t = self.torch
         if stream is None:
-            return t.empty((self.T, cols), dtype=self._bf16, device=self.device)
-        with t.cuda.stream(stream):
-            return t.empty((self.T, cols), dtype=self._bf16, device=self.device)
+            return self._empty((self.T, cols), dtype=self._bf16, device=self.device)
+        with self.torch.cuda.stream(stream):
+            return self._empty((self.T, cols), dtype=self._bf16, device=self.device)
 
     @staticmethod
     def _list(v):
@@ -582,7 +595,7 @@ class PagedCache:
         if stream is not None:
             return int(stream.cuda_stream)
         if self._raw_stream is not None:
-            return self._raw_stream(self.device.index)
+            return self._raw_stream(self._index)
         return int(self.torch.cuda.current_stream(self.device).cuda_stream)
 
     def _done(self, rc):
@@ -600,31 +613,42 @@ class PagedCache:
         """Norm (with gammas) and rotate the step's queries and keys of qkv [T][(q + 2 kv heads) * head_dim], write
         its keys and values into the cache; returns the queries [T][q_heads * head_dim] (q_out, which may be a
         view of qkv's query columns)."""
-        hd, a = self.head_dim, self._append_args
-        a.ld_qkv = self._rows(qkv, (self.q_heads + 2 * self.kv_heads) * hd, "append")
+        a, cols = self._append_args, self._q_cols
+        a.ld_qkv = self._rows(qkv, self._qkv_cols, "append")
         if q_out is None:
-            q_out = self._new(self.q_heads * hd, stream)
-        a.ld_q = self._rows(q_out, self.q_heads * hd, "append")
-        for g in (gamma_q, gamma_k):
-            self._tensor(g, self._bf16, (hd,), "append")
-        self._tensor(pos, self.torch.int32, (self.T,), "append")
-        a.qkv, a.q_out, a.gamma_q, a.gamma_k, a.pos = (qkv.data_ptr(), q_out.data_ptr(), _ptr(gamma_q), _ptr(gamma_k),
-                                                       _ptr(pos))
-        a.norm_eps, a.rope_theta = eps, theta
-        self._done(self._lib.trimmoe_cache_append(self.handle, layer, C.addressof(a), self._stream(stream)))
+            q_out = self._new(cols, stream)
+            a.ld_q = cols
+        else:
+            a.ld_q = self._rows(q_out, cols, "append")
+        a.gamma_q = self._vector(gamma_q, self._bf16, self.head_dim, "append")
+        a.gamma_k = self._vector(gamma_k, self._bf16, self.head_dim, "append")
+        a.pos = self._vector(pos, self._int32, self.T, "append")
+        a.qkv = qkv.data_ptr()
+        a.q_out = q_out.data_ptr()
+        a.norm_eps = eps
+        a.rope_theta = theta
+        rc = self._c_append(self.handle, layer, self._append_at, self._stream(stream))
+        if rc:
+            self._done(rc)
         return q_out
 
     def attend(self, layer: int, q, out=None, tree=None, scale: float = 0.0, stream=None):
         """Attention of the step's queries [T][q_heads * head_dim] over their sequences; tree: int64 [T] words, bit j
         = sees new token j of its sequence (default: causal)."""
-        cols, a = self.q_heads * self.head_dim, self._attend_args
+        a, cols = self._attend_args, self._q_cols
         a.ld_q = self._rows(q, cols, "attend")
         if out is None:
             out = self._new(cols, stream)
-        a.ld_out = self._rows(out, cols, "attend")
-        self._tensor(tree, self.torch.int64, (self.T,), "attend")
-        a.q, a.out, a.tree, a.scale = q.data_ptr(), out.data_ptr(), _ptr(tree), scale
-        self._done(self._lib.trimmoe_cache_attend(self.handle, layer, C.addressof(a), self._stream(stream)))
+            a.ld_out = cols
+        else:
+            a.ld_out = self._rows(out, cols, "attend")
+        a.tree = self._vector(tree, self._int64, self.T, "attend")
+        a.q = q.data_ptr()
+        a.out = out.data_ptr()
+        a.scale = scale
+        rc = self._c_attend(self.handle, layer, self._attend_at, self._stream(stream))
+        if rc:
+            self._done(rc)
         return out
 
     def fork(self, src, dst, stream=None):

@@ -213,6 +213,7 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         alloc(d.base, cfg->max_seqs);
         alloc(d.part_o, (size_t)2 * d.num_sms * 256 * d.dh);
         alloc(d.part_ml, (size_t)2 * d.num_sms * 256);
+        alloc(d.arrived, (size_t)d.num_sms);
         alloc(d.err, 1);
         if (e != cudaSuccess)
             return bail(e == cudaErrorMemoryAllocation ? TRIMMOE_ERR_OOM : TRIMMOE_ERR_CUDA,
@@ -331,10 +332,11 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
     p.ld_out = a->ld_out;
     p.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)d.dh)) * 1.4426950408889634f;
     const int max_rows = c->max_q > d.tile_tokens ? 2 * kCacheTile : c->max_q * d.rep;
+    p.join_here = max_rows <= kJoinHereRows;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_attend");
-    return c->launched(launch_cache_attend(d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows, enter(c, stream)), 2,
-                       "cache_attend");
+    return c->launched(launch_cache_attend(d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows, enter(c, stream)),
+                       p.join_here ? 1 : 2, "cache_attend");
 }
 
 extern "C" trimmoe_status trimmoe_cache_fork(trimmoe_cache_handle c, int n, const int32_t* src, const int32_t* dst,

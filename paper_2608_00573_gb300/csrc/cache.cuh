@@ -9,6 +9,11 @@ namespace tmoe {
 constexpr int kCacheMaxSeqs = 1024;
 constexpr int kCacheTile = 128;        // rows of a query tile, keys of a key tile
 constexpr int kTreeMax = 64;           // drafted tokens of a sequence (mask bits)
+// Up to this many rows of an item, the CTA that writes a cut item's last part joins
+// them (a decode step then is one launch: one sequence of 1500 positions MEASURED);
+// above, a second kernel does, with a CTA per 32 rows (a 777-token prompt takes MEASURED
+// that way and MEASURED the other).
+constexpr int kJoinHereRows = 32;
 
 // One listed sequence of the current step.
 struct CacheSeq {
@@ -34,6 +39,8 @@ struct __align__(16) CacheShare {
     long long begin, end;
     long long within;                  // begin, from the start of the item that holds it
     int group, head;                   // that item
+    int first, last;                   // CTAs that hold key tiles of it
+    int pad[2];
     CacheGroup g;                      // its group
 };
 
@@ -55,6 +62,14 @@ __host__ __device__ inline int cache_group_tiles(int q_len, int kv_len, int firs
     return (keys + kCacheTile - 1) / kCacheTile;
 }
 
+// Key tiles of an item of this cost (two: it has two query tiles), and how many of
+// them the first x of its cost cover.
+__host__ __device__ inline int cache_item_tiles(int cost, int two) { return (cost >> two) - 1; }
+__host__ __device__ inline int cache_tiles_before(long long x, int cost, int two) {
+    const long long n = cache_item_tiles(cost, two), t = x <= 0 ? 0 : (x + two) >> two;
+    return (int)(x >= cost || t > n ? n : t);
+}
+
 // The handle's device state, passed to every kernel by value.
 struct CacheDev {
     int layers, Hq, Hkv, rep, dh, page, page_shift, n_pages, max_seqs, max_pages, T_max;
@@ -71,8 +86,11 @@ struct CacheDev {
     int2* copies;                      // [max(n_pages, max_seqs)] (from, to) pages
     int* fresh;                        // [n_pages] free pages taken by a step; new place of each page (compact)
     int* base;                         // [max_seqs] length before the sequence's last step
-    float* part_o;                     // [2 num_sms][256][dh] partial sums of split items
-    float2* part_ml;                   // [2 num_sms][256] their row maxima and sums
+    // Parts of cut items: two buffers per CTA, for the item that its share begins in and
+    // the one that it ends in; rows 0..127 and 128..255 from the two slots.
+    float* part_o;                     // [2 num_sms][256][dh] sums of p v
+    float2* part_ml;                   // [2 num_sms][256] row maxima and sums of p
+    int* arrived;                      // [num_sms] parts written of the item that a CTA began, 0 between calls
     int* err;
 };
 
@@ -99,6 +117,7 @@ struct AttendParams {
     const uint64_t* tree;
     __nv_bfloat16* out;
     int ld_out;
+    int join_here;                     // the attention kernel joins cut items itself
     float scale_log2;
 };
 

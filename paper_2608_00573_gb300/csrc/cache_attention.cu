@@ -25,8 +25,8 @@
 // Work is split evenly whatever the lengths: the items' costs are laid end to
 // end and each CTA takes the same share of the line, cutting items at key tiles
 // (cache_pages.cu makes the list).  A cut item's parts go to a buffer, at most two per
-// CTA, and cache_join_kernel adds them in the order of the keys, so results do
-// not depend on timing.
+// CTA, and are added in the order of the keys (join_rows), so results do not depend
+// on timing.
 //
 // Masked places never reach a result: scores are replaced, not added to; value
 // rows that no row of the item sees are zeroed in shared memory (0 * NaN would
@@ -74,11 +74,13 @@ struct __align__(8) Bars {
     uint64_t q_full, q_empty;
     uint64_t s_full[2], p_full[2], o_full[2];
     uint64_t x_full[4];
+    uint64_t part_done, join_go;
     uint64_t seg_full[kSegSlots], seg_empty[kSegSlots];
     Seg seg[kSegSlots];
     int bad[10][2];      // guard warps' finding per ring stage
     float2 xml[128];     // odd slot's maximum and sum per row
     uint32_t tmem_base;
+    int last_part;       // this CTA wrote an item's last missing part
     int abort_flag, never;
 };
 constexpr int kSegReaders = 1 + 2 + 8;   // warps that read a segment
@@ -105,15 +107,6 @@ __device__ __forceinline__ SegInfo seg_info(const Seg& g, int tile_tokens, bool 
     s.n0 = s.n1;
     if (s.dual && !tree) s.n0 = min(s.n1, (g.first + tile_tokens + kCacheTile - 1) / kCacheTile);
     return s;
-}
-
-// Key tiles [t0, t1) of an item that the stretch [x0, x1) of its cost covers (two: it
-// has two query tiles); stretches that meet cover meeting ranges.
-__device__ __forceinline__ int item_tiles(int cost, int two) { return (cost >> two) - 1; }
-__device__ __forceinline__ void stretch_tiles(long long x0, long long x1, int cost, int two, int* t0, int* t1) {
-    const int n = item_tiles(cost, two);
-    *t0 = (int)min((long long)n, (x0 + two) >> two);
-    *t1 = x1 >= cost ? n : (int)min((long long)n, (x1 + two) >> two);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -196,6 +189,72 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return r;
 }
 
+// Joins R rows of a cut item from the parts of CTAs first .. last, in the order of the
+// keys; a lane takes D / 32 columns, B sources are read at a time.  CTA `first` wrote its
+// part into its second buffer, the others into their first; with `halves` each part has
+// two sources, from the two slots.
+// Bound: latency (one or two rounds of reads), and L2 for prompts' items.
+template <int DH, int R, int B>
+__device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams& p, int token0, int head, int rows,
+                                          int halves, int first, int last, int r0, int lane) {
+    constexpr int V = DH / 32;
+    const int sources = (last - first + 1) << halves;
+    float top[R], l[R], acc[R][V];
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        top[q] = -INFINITY;
+        l[q] = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[q][j] = 0.f;
+    }
+#pragma unroll 1
+    for (int s0 = 0; s0 < sources; s0 += B) {
+        float2 ml[B][R];
+        float o[B][R][V];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int s = min(s0 + i, sources - 1), k = s >> halves;
+            const int buf = k == 0 ? 2 * first + 1 : 2 * (first + k);
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                const size_t row = (size_t)buf * 256 + (s & halves) * 128 + min(r0 + q, rows - 1);
+                const float* src = c.part_o + row * DH + lane * V;
+                ml[i][q] = __ldcg(c.part_ml + row);
+                if (V == 4) {
+                    const float4 f = __ldcg(reinterpret_cast<const float4*>(src));
+                    o[i][q][0] = f.x, o[i][q][1] = f.y, o[i][q][V - 2] = f.z, o[i][q][V - 1] = f.w;
+                } else {
+                    const float2 f = __ldcg(reinterpret_cast<const float2*>(src));
+                    o[i][q][0] = f.x, o[i][q][1] = f.y;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                const bool there = s0 + i < sources && ml[i][q].x != -INFINITY;   // else nothing was summed
+                const float m = there ? fmaxf(top[q], ml[i][q].x) : top[q], ref = m == -INFINITY ? 0.f : m;
+                const float fa = ex2(top[q] - ref), fb = ex2(ml[i][q].x - ref);
+                top[q] = m;
+                l[q] = there ? l[q] * fa + ml[i][q].y * fb : l[q];
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[q][j] = there ? acc[q][j] * fa + o[i][q][j] * fb : acc[q][j];
+            }
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        const int r = r0 + q, tile = r >> 7, in = r & 127;
+        if (r >= rows || in >= c.tile_tokens * c.rep) continue;
+        const int token = token0 + tile * c.tile_tokens + in / c.rep, h = head * c.rep + in % c.rep;
+        const float il = l[q] == 0.f ? 0.f : 1.f / l[q];
+        __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + lane * V;
+#pragma unroll
+        for (int j = 0; j < V; j += 2)
+            *reinterpret_cast<uint32_t*>(out + j) = pack_bf16x2(acc[q][j] * il, acc[q][j + 1] * il);
+    }
+}
+
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -227,6 +286,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(smem_u32(&bars->o_full[s]), 1);
         }
         for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&bars->x_full[s]), 1);
+        mbar_init(smem_u32(&bars->part_done), 8);
+        mbar_init(smem_u32(&bars->join_go), 1);
         for (int s = 0; s < kSegSlots; ++s) {
             mbar_init(smem_u32(&bars->seg_full[s]), 1);
             mbar_init(smem_u32(&bars->seg_empty[s]), kSegReaders);
@@ -265,8 +326,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 
     if (warp == 0) {
         // ------------------------------------------------ segments and loads
-        const CachePlan pl = *c.plan;
         const int b = blockIdx.x;
+        const CachePlan pl = *c.plan;
+        const CacheShare sh = c.shares[b];      // (read with the plan, not after it)
         int it = 0, nseg = 0;
         uint32_t cnt = 0;                       // ring entries issued
         bool ok = true;
@@ -292,7 +354,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         CacheGroup g;
         bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
         if (any && !whole) {
-            const CacheShare& sh = c.shares[b];
             x = sh.begin;
             x_end = sh.end;
             within = sh.within;
@@ -320,12 +381,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             sg.pad = 0;
             if (whole) {
                 sg.t0 = 0;
-                sg.t1 = item_tiles(g.cost, two_tiles);
+                sg.t1 = cache_item_tiles(g.cost, two_tiles);
                 sg.part = -1;
             } else {
                 const long long x1 = min((long long)g.cost, within + (x_end - x));
-                stretch_tiles(within, x1, g.cost, two_tiles, &sg.t0, &sg.t1);
-                sg.part = (sg.t0 == 0 && sg.t1 == item_tiles(g.cost, two_tiles)) ? -1 : (sg.t0 > 0 ? 2 * b : 2 * b + 1);
+                sg.t0 = cache_tiles_before(within, g.cost, two_tiles);
+                sg.t1 = cache_tiles_before(x1, g.cost, two_tiles);
+                sg.part = (sg.t0 == 0 && sg.t1 == cache_item_tiles(g.cost, two_tiles)) ? -1 : (sg.t0 > 0 ? 2 * b : 2 * b + 1);
                 x += x1 - within;
                 within = 0;
                 any = x < x_end;
@@ -586,7 +648,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         const uint32_t tS = tbase + loff + slot * 128, tO = tbase + loff + 256 + slot * DH;
         const int tok_in_tile = r / rep, head_in_tile = r - tok_in_tile * rep;
         const float sl2 = p.scale_log2;
-        uint32_t ns = 0, no = 0, nx = 0, masked = 0, cnt = 0;
+        uint32_t ns = 0, no = 0, nx = 0, nj = 0, masked = 0, cnt = 0;
         Seg g;
         bool ok = true;
         for (int it = 0; ok && next_seg(it, g); ++it) {
@@ -794,8 +856,11 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 ++no;
                 tc_fence_after();
             }
-            const bool joins = !si.dual && g.t0 + 1 < si.n1;   // both slots hold parts of the same rows
-            if (!si.dual && slot == 1) {
+            // In a one-tile item both slots hold parts of the same rows: slot 1 hands its own to
+            // slot 0 through shared memory, unless all parts are joined right after.
+            const bool apart = g.part >= 0 && p.join_here;
+            const bool joins = !si.dual && !apart && g.t0 + 1 < si.n1;
+            if (!si.dual && slot == 1 && !apart) {
                 // All products of the segment are done: the query tiles' space takes this slot's O.
                 if (joins) {
                     if (live) {
@@ -843,9 +908,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 float* po = nullptr;
                 __nv_bfloat16* out = nullptr;
                 if (g.part >= 0) {
-                    const size_t row = (size_t)g.part * 256 + (si.dual ? slot * 128 : 0) + r;
+                    const size_t row = (size_t)g.part * 256 + (si.dual || apart ? slot * 128 : 0) + r;
                     po = c.part_o + row * DH;
-                    if (mine) c.part_ml[row] = make_float2(m, l);
+                    if (mine) c.part_ml[row] = make_float2(work ? m : -INFINITY, l);
                 } else {
                     out = p.out + (size_t)token * p.ld_out + (size_t)(g.head * rep + head_in_tile) * DH;
                 }
@@ -898,6 +963,30 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (lane == 0) mbar_arrive(bar(&bars->q_empty));
             }
             tc_fence_before();
+            if (apart) {
+                // Whoever writes an item's last missing part joins them all.  (The barrier
+                // orders the CTA's writes before the one fence and count.)
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&bars->part_done));
+                const CacheShare& sh = c.shares[g.t0 > 0 ? blockIdx.x : blockIdx.x + 1];   // a share that begins in the item
+                const int first = sh.first, last = sh.last;
+                ok = !lost(wait(&bars->part_done, nj));
+                if (!ok) break;
+                if (warp == 4 && lane == 0) {
+                    __threadfence();
+                    const bool mine_last = atomicAdd(&c.arrived[first], 1) == last - first;
+                    if (mine_last) c.arrived[first] = 0;
+                    __threadfence();
+                    bars->last_part = mine_last;
+                    mbar_arrive(bar(&bars->join_go));
+                }
+                ok = !lost(wait(&bars->join_go, nj));
+                if (!ok) break;
+                ++nj;
+                if (bars->last_part)
+                    for (int r0 = warp - 4; r0 < g.ntok * rep; r0 += 8)
+                        join_rows<DH, 1, 8>(c, p, g.row, g.head, g.ntok * rep, 1, first, last, r0, lane);
+            }
         }
     }
     __syncthreads();
@@ -909,87 +998,21 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 }
 
 // Joins the parts of cut items.  Block (b, y) takes rows [32 y, 32 y + 32) of the
-// item that CTA b of the attention began and did not finish; a warp takes four
-// rows, a lane D / 32 columns of each; the parts are added in the order of the keys.
-// Bound: latency (a few dependent reads) and L2, 2 to 3 parts of up to 256 x D fp32
-// per cut.
+// item that CTA b of the attention began and did not finish, a warp four of them.
 template <int DH>
 __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__ CacheDev c,
                                                          const __grid_constant__ AttendParams p) {
     pdl_wait();
     pdl_trigger();
-    const int n_ctas = c.plan->n_ctas, b = blockIdx.x, TT = c.tile_tokens;
+    const int n_ctas = c.plan->n_ctas, b = blockIdx.x;
     if (!c.plan->ok || b + 1 >= n_ctas) return;
-    // The item in which CTA b + 1 begins, if it is in its middle, and was begun by CTA b.
     const CacheShare next = c.shares[b + 1];
-    const CacheGroup& g = next.g;
-    const long long start = next.begin - next.within;
-    if (next.within == 0 || start < c.shares[b].begin) return;
-    const int two = cache_two_tiles(g.ntok, TT), n = item_tiles(g.cost, two);
-    int t0, t1;
-    stretch_tiles(0, next.within, g.cost, two, &t0, &t1);
-    if (t1 == n) return;                                   // only the item's end is on the other side
-    const int rows = two ? 128 + (g.ntok - TT) * c.rep : g.ntok * c.rep;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int r0 = blockIdx.y * 32 + warp * 4;
-    if (r0 >= rows) return;
-    constexpr int V = DH / 32;
-    float top[4], l[4], acc[4][V];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        top[k] = -INFINITY;
-        l[k] = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
-    }
-    // Running maximum over the parts: CTA b's in its second buffer, the others' in their first.
-    int s = 2 * b + 1;
-#pragma unroll 1
-    for (int k = b;;) {
-        float2 ml[4];
-        float o[4][V];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const size_t row = (size_t)s * 256 + min(r0 + q, 255);
-            ml[q] = c.part_ml[row];
-            const float* src = c.part_o + row * DH + lane * V;
-            if (V == 4) {
-                const float4 f = *reinterpret_cast<const float4*>(src);
-                o[q][0] = f.x, o[q][1] = f.y, o[q][V - 2] = f.z, o[q][V - 1] = f.w;
-            } else {
-                const float2 f = *reinterpret_cast<const float2*>(src);
-                o[q][0] = f.x, o[q][1] = f.y;
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float m = fmaxf(top[q], ml[q].x), ref = m == -INFINITY ? 0.f : m;
-            const float fa = ex2(top[q] - ref), fb = ex2(ml[q].x - ref);
-            top[q] = m;
-            l[q] = l[q] * fa + ml[q].y * fb;
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[q][j] = acc[q][j] * fa + o[q][j] * fb;
-        }
-        if (t1 == n) break;
-        do {                                               // the next CTA whose stretch holds a tile
-            ++k;
-            const int from = t1;
-            stretch_tiles(0, c.shares[k].end - start, g.cost, two, &t0, &t1);
-            t0 = from;
-        } while (t0 == t1);
-        s = 2 * k;
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int r = r0 + q, tile = r >> 7, in = r & 127;
-        if (r >= rows || in >= TT * c.rep) continue;
-        const int token = g.row + tile * TT + in / c.rep, h = next.head * c.rep + in % c.rep;
-        const float il = l[q] == 0.f ? 0.f : 1.f / l[q];
-        __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + lane * V;
-#pragma unroll
-        for (int j = 0; j < V; j += 2)
-            *reinterpret_cast<uint32_t*>(out + j) = pack_bf16x2(acc[q][j] * il, acc[q][j + 1] * il);
-    }
+    if (next.within == 0 || next.first != b || next.last == b) return;
+    const int two = cache_two_tiles(next.g.ntok, c.tile_tokens);
+    const int rows = two ? 128 + (next.g.ntok - c.tile_tokens) * c.rep : next.g.ntok * c.rep;
+    const int r0 = blockIdx.y * 32 + (threadIdx.x >> 5) * 4;
+    if (r0 < rows)
+        join_rows<DH, 4, 2>(c, p, next.g.row, next.head, rows, 0, b, next.last, r0, threadIdx.x & 31);
 }
 
 static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
@@ -1005,7 +1028,7 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
     if (e != cudaSuccess) return e;
     e = launch_pdl(cache_attention_kernel<DH>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
                    c, p);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || p.join_here) return e;
     return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);
 }
 

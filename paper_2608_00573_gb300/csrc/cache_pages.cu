@@ -22,9 +22,10 @@ namespace {
 constexpr int kStepThreads = 1024;
 constexpr int kCopyThreads = 256;
 constexpr int kCopyVecs = 4;           // 16-byte vectors in flight per thread
-// Smallest share of a CTA on the line of items (see CacheShare): below it, fewer
-// CTAs take part.
-constexpr int kMinShare = 3;
+// Smallest share of a CTA, in key tiles: below it, fewer CTAs take part.  Two tiles
+// keep both slots busy at once (decoding one sequence of 1500 positions takes 11.5 us so,
+// 15.7 with three and more CTAs idle).
+constexpr int kMinTiles = 2;
 
 // Exclusive prefix sum over the block; every thread gets the total.  ws: 33 entries.
 template <class V>
@@ -195,20 +196,21 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
         return g;
     };
     long long cost = 0, total;
-    int most = 0;
+    int most = 0, two = 0;
     for (int r = i; r < n_groups; r += kStepThreads) {
-        const int k = group_of(r).cost;
-        cost += k;
-        most = max(most, k);
+        const CacheGroup g = group_of(r);
+        cost += g.cost;
+        most = max(most, g.cost);
+        two |= cache_two_tiles(g.ntok, TT);
     }
     block_scan(cost, s_wsl, total);
     if (i == 0) s_most = 0;
-    __syncthreads();
+    two = __syncthreads_or(two);
     if (i < n_groups) atomicMax(&s_most, most);
     __syncthreads();
     const long long W = total * c.Hkv;
     const bool whole = 2LL * s_most * c.num_sms <= W;
-    const int n_ctas = !W || whole ? 0 : (int)max(1LL, min((long long)c.num_sms, W / kMinShare));
+    const int n_ctas = !W || whole ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles << (two ? 1 : 0))));
     if (whole) {
         // Counting sort by cost, costs past the last bucket together in the first one.
         if (i < kStepThreads) s_bucket[i] = 0;
@@ -261,8 +263,17 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
         sh.within = sh.begin - sh.g.pre * c.Hkv;
         sh.head = (int)(sh.within / sh.g.cost);
         sh.within -= (long long)sh.head * sh.g.cost;
+        // The CTAs that hold tiles of the item: every share covers at least one unless it
+        // holds just the item's end.
+        const long long start = sh.begin - sh.within;
+        const int two_tiles = cache_two_tiles(sh.g.ntok, TT), tiles = cache_item_tiles(sh.g.cost, two_tiles);
+        sh.first = sh.last = b;
+        while (W * sh.first / n_ctas > start) --sh.first;
+        while (cache_tiles_before(W * (sh.last + 1) / n_ctas - start, sh.g.cost, two_tiles) < tiles) ++sh.last;
+        while (cache_tiles_before(W * sh.last / n_ctas - start, sh.g.cost, two_tiles) == tiles) --sh.last;
         c.shares[b] = sh;
     }
+    if (i < c.num_sms) c.arrived[i] = 0;
 }
 
 // Page rows and positions of the T new tokens, and the page copies that the
