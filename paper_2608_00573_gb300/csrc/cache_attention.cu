@@ -70,9 +70,11 @@ struct Seg {
 
 struct __align__(8) Bars {
     uint64_t kv_full[10], kv_empty[10];
-    uint64_t go[10], guard[10];   // masked value tile has landed / has been guarded, in the order of such tiles
+    uint64_t go[10], guard[10];   // partly masked value tile is under way / has been guarded, in the order of such tiles
     uint64_t q_full, q_empty;
-    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t s_full[2], o_full[2];
+    uint64_t p_half[2], p_full[2];   // P of a tile's first 64 keys, of all
+    uint64_t half_done[2];           // O has the first 64 keys' part
     uint64_t x_full[4];
     uint64_t part_done, join_go;
     uint64_t seg_full[kSegSlots], seg_empty[kSegSlots];
@@ -189,6 +191,67 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return r;
 }
 
+// What the softmax warps seldom do stands in functions of its own, out of the way of the
+// code that they run for every tile.
+
+// This warp's rows of O (DH columns) times f.
+template <int DH>
+__device__ __noinline__ void scale_rows(uint32_t tO, float f) {
+#pragma unroll 1
+    for (int k = 0; k < DH; k += 32) {
+        uint32_t o[32];
+        tmem_ld_32x32(tO + k, o);
+        landed(o);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+        tmem_st_32x32(tO + k, o);
+    }
+    tmem_st_wait();
+}
+
+// O += P V of keys [key0, key1) of a tile (of one half of it; see0, see1: those that the
+// row sees) for this warp's rows.  v: the tile's value rows.
+template <int DH>
+__device__ __noinline__ void pv_by_hand(uint32_t tS, uint32_t tO, const uint8_t* v, int key0, int key1, uint32_t see0,
+                                        uint32_t see1, bool first) {
+#pragma unroll 1
+    for (int k = 0; k < DH; k += 32) {
+        uint32_t o[32];
+        tmem_ld_32x32(tO + k, o);
+        landed(o);
+        float acc[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) acc[j] = first ? 0.f : __uint_as_float(o[j]);
+#pragma unroll 1
+        for (int key = key0; key < key1; ++key) {
+            __syncwarp();
+            uint32_t pw;
+            tmem_ld_32x1(tS + (key >> 1), pw);
+            tmem_ld_wait();
+            const float pk = (key & 1) ? bf16_hi(pw) : bf16_lo(pw);
+            const bool sees = ((key & 32) ? see1 : see0) >> (key & 31) & 1u;
+            const uint8_t* vr = v + (k >> 6) * kBox + key * 128;
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch) {
+                const int c16 = ((k & 63) >> 3) + ch;
+                const uint4 x = *reinterpret_cast<const uint4*>(vr + ((c16 ^ (key & 7)) << 4));
+                const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int j = ch * 8 + 2 * y;
+                    acc[j] = sees ? fmaf(pk, bf16_lo(xw[y]), acc[j]) : acc[j];
+                    acc[j + 1] = sees ? fmaf(pk, bf16_hi(xw[y]), acc[j + 1]) : acc[j + 1];
+                }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(acc[j]);
+        tmem_st_32x32(tO + k, o);
+    }
+    tmem_st_wait();
+}
+
 // Joins R rows of a cut item from the parts of CTAs first .. last, in the order of the
 // keys; a lane takes D / 32 columns, B sources are read at a time.  CTA `first` wrote its
 // part into its second buffer, the others into their first; with `halves` each part has
@@ -282,7 +345,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         mbar_init(smem_u32(&bars->q_empty), 8);
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&bars->s_full[s]), 1);
+            mbar_init(smem_u32(&bars->p_half[s]), 4);
             mbar_init(smem_u32(&bars->p_full[s]), 4);
+            mbar_init(smem_u32(&bars->half_done[s]), 1);
             mbar_init(smem_u32(&bars->o_full[s]), 1);
         }
         for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&bars->x_full[s]), 1);
@@ -324,13 +389,18 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         return __shfl_sync(0xffffffffu, g.valid, 0) != 0;
     };
 
+    // Registers go from the first four warps to the softmax warps (104 x 128 + 200 x 256 of the
+    // 168 x 384 at launch).  The two branches do not meet before the roles end: where
+    // they met, the compiler would take the smaller number for all that follows.
+    if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 0) {
         // ------------------------------------------------ segments and loads
         const int b = blockIdx.x;
         const CachePlan pl = *c.plan;
         const CacheShare sh = c.shares[b];      // (read with the plan, not after it)
         int it = 0, nseg = 0;
-        uint32_t cnt = 0;                       // ring entries issued
+        uint32_t cnt = 0, masked = 0;           // ring entries issued, partly masked value tiles among them
         bool ok = true;
         auto give_seg = [&](const Seg& g) {
             const int s = it % kSegSlots;
@@ -427,7 +497,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll 1
                 for (int t = sg.t0 - lead; ok && t < sg.t1; ++t) {
                     const int tk = t + lead;
-                    if (t >= sg.t0) ok = load(&tm_v, t, id0);
+                    if (t >= sg.t0) {
+                        ok = load(&tm_v, t, id0);
+                        if ((t + 1) * kCacheTile > si.kall) {
+                            if (lane == 0) mbar_arrive(bar(&bars->go[masked % ST]));
+                            ++masked;
+                        }
+                    }
                     if (ok && tk < sg.t1) ok = load(&tm_k, tk, t < sg.t0 ? (tk == sg.t0 ? id0 : id1) : (lead == 1 ? id1 : id2));
                     if (ok && t == sg.t0 - 1) {
                         ok = nseg == 0 || !lost(wait(&bars->q_empty, nseg - 1));
@@ -506,13 +582,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             // a slot's products run under the other slot's softmax.  (Given up: the waits
             // return at once, the products' results are not used.)
             uint32_t ev = 0, ek = 0;
-            auto pv = [&](int s, bool began) {
-                const uint64_t va = d_v + ev * kTile16;
-                const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128;
+            auto pv = [&](int s, int half, bool began) {             // keys 64 half .. 64 half + 63
+                const uint64_t va = d_v + ev * kTile16 + half * 4 * (2048 >> 4);
+                const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128 + half * 32;
                 if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
+                    for (int kk = 0; kk < 4; ++kk)
                         tc_mma_bf16_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : (uint32_t)began);
+                    if (half == 0) tc_commit(bar(&bars->half_done[s]));
                 }
             };
             auto qk = [&](int s, bool last) {            // last: of the slots that read this key tile
@@ -534,16 +611,22 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             for (int i = -lead; i < nt; ++i) {
                 if (i >= 0 && i < plain) {
                     if (!have_v) ev = entry();
+                    gave_up |= wait(&bars->p_half[0], p_phase);
+                    tc_fence_after();
+                    pv(0, 0, i > 0);
                     gave_up |= wait(&bars->p_full[0], p_phase);
                     tc_fence_after();
-                    pv(0, i > 0);
+                    pv(0, 1, true);
                     ek = entry();
                     tc_fence_after();
                     qk(0, false);
+                    gave_up |= wait(&bars->p_half[1], p_phase >> 1);
+                    tc_fence_after();
+                    pv(1, 0, i > 0);
                     gave_up |= wait(&bars->p_full[1], p_phase >> 1);
                     p_phase ^= 3u;
                     tc_fence_after();
-                    pv(1, i > 0);
+                    pv(1, 1, true);
                     if (elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
                     ev = entry();                        // (step i + 1 exists) under the products queued
                     have_v = true;
@@ -559,7 +642,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (i >= first_masked) {
                         const uint32_t gs = masked % ST, gp = masked / ST;
                         ++masked;
-                        if (elect_one()) mbar_arrive(bar(&bars->go[gs]));
                         gave_up |= wait(&bars->guard[gs], gp);
                         bad = uniform(bars->bad[gs][0] | bars->bad[gs][1]);
                     }
@@ -570,10 +652,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const int ns = s ? n1 : n0;
                     const bool here = i >= 0 && i < ns;
                     if (here) {
+                        gave_up |= wait(&bars->p_half[s], p_phase >> s);
+                        tc_fence_after();
+                        if (!bad) pv(s, 0, dual ? i > 0 : i > 1);    // else the softmax warps do it
+                        else if (elect_one()) tc_commit(bar(&bars->half_done[s]));
                         gave_up |= wait(&bars->p_full[s], p_phase >> s);
                         p_phase ^= 1u << s;
                         tc_fence_after();
-                        if (!bad) pv(s, dual ? i > 0 : i > 1);       // else the softmax warps have done it
+                        if (!bad) pv(s, 1, true);
                     }
                     if (i >= 0 && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
                     if (more && s == s0) {
@@ -590,7 +676,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             __syncwarp();
         }
-    } else if (warp < 4) {
+    } else {
         // ------------------------------------------------------------ guards
         // Values of partly masked tiles: rows that nobody sees become zeros, rows
         // that some see are searched for infinities and NaN.
@@ -605,8 +691,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 const int t = g.t0 + i;
                 if ((t + 1) * kCacheTile <= si.kall) continue;
                 const uint32_t e = cnt + i + min(nt, i + lead);
-                // A parity names a phase only to who has seen the one before: the ring's
-                // phases are followed by the MMA warp, which says when e is there.
+                // A parity names a phase only to who knows that the one before has passed: the
+                // load warp says when the entry's own phase has begun.
                 ok = !lost(wait(&bars->go[masked % ST], masked / ST) | wait(&bars->kv_full[e % ST], e / ST));
                 if (!ok) break;
                 uint8_t* v = smem + L::RING + (e % ST) * L::TILE;
@@ -639,7 +725,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             cnt += 2 * nt;
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // -------------------------------------------------- softmax and output
         const int slot = (warp - 4) >> 2;
         const int qw = warp & 3;                           // TMEM lane quarter
@@ -685,167 +773,128 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 --left;
                 if (left == 0 && si.dual && lane == 0) mbar_arrive(bar(&bars->q_empty));
                 uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
-                if (live) {
-                    if (part) {
-                        // Keys of the tile that this row sees, one bit each.
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int k0 = t * kCacheTile + q * 32;
-                            const int n = (tree ? g.base : seen) - k0;             // the first n keys
-                            see[q] = n >= 32 ? ~0u : n > 0 ? (1u << n) - 1u : 0u;
-                            if (tree) {
-                                const int d = k0 - g.base;                         // draft of the word's bit 0
-                                if (d >= 0) {
-                                    if (d < 64) see[q] |= (uint32_t)(word >> d);
-                                } else if (d > -32) {
-                                    see[q] |= (uint32_t)(word << -d);
-                                }
-                                const int end = g.kv_len - k0;                     // bits past the drafts
-                                see[q] &= end >= 32 ? ~0u : end > 0 ? (1u << end) - 1u : 0u;
-                            }
-                        }
-                    }
-                    // One pass over the scores in TMEM, 32 columns (a quarter) at a time with the
-                    // next loads in flight; a quarter's maximum is found beside the exponentials
-                    // of the one before (different units).  The reference m is a whole
-                    // number, so that when it moves in the middle of a tile the probabilities
-                    // already written are scaled exactly.
-                    uint32_t u[3][32];
-                    float2 ls[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                    auto maximum = [&](int q) {          // of quarter q, masked, in the exponent's unit
-                        uint32_t(&x)[32] = u[q % 3];
-                        if (part) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (!(see[q] >> j & 1u)) x[j] = 0xff800000u;       // -inf
-                        }
-                        float a[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) a[k] = fmaxf(__uint_as_float(x[8 * k]), __uint_as_float(x[8 * k + 1]));
-#pragma unroll
-                        for (int j = 2; j < 8; j += 2)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                a[k] = max3(a[k], __uint_as_float(x[8 * k + j]), __uint_as_float(x[8 * k + j + 1]));
-                        return fmaxf(max3(a[0], a[1], a[2]), a[3]) * sl2;
-                    };
-                    auto follow = [&](int q, float mx) { // moves m before quarter q's exponentials when it has to
-                        const bool grow = mx - m > 8.f;                            // also from m = -inf
-                        if (__any_sync(0xffffffffu, grow)) {
-                            const float up = ceilf(mx), d = m - up;                // m = -inf: the sums so far are 0
-                            const float f = !grow ? 1.f : d < -126.f ? 0.f : __int_as_float(((int)d + 127) << 23);
-                            if (grow) m = up;
-                            l *= f;
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                ls[k].x *= f;
-                                ls[k].y *= f;
-                            }
-#pragma unroll 1
-                            for (int k = 0; k < q * 16; k += 16) {                 // P of the tile's earlier columns
-                                uint32_t w[16];
-                                tmem_st_wait();
-                                tmem_ld_32x16(tS + k, w);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(bf16_lo(w[j]) * f, bf16_hi(w[j]) * f);
-                                tmem_st_32x16(tS + k, w);
-                            }
-                            if (t != begin) {
-#pragma unroll 1
-                                for (int k = 0; k < DH; k += 16) {
-                                    uint32_t o[16];
-                                    tmem_ld_32x16(tO + k, o);
-                                    tmem_ld_wait();
-#pragma unroll
-                                    for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                    tmem_st_32x16(tO + k, o);
-                                }
-                            }
-                        }
-                    };
-                    tmem_ld_32x32(tS, u[0]);
-                    landed(u[0]);
-                    tmem_ld_32x32(tS + 32, u[1]);
-                    follow(0, maximum(0));
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (q < 3) landed(u[(q + 1) % 3]);
-                        if (q < 2) tmem_ld_32x32(tS + (q + 2) * 32, u[(q + 2) % 3]);
-                        uint32_t(&x)[32] = u[q % 3];
-                        const float ms = m == -INFINITY ? 0.f : -m;                // a row without keys so far: p = 0
-                        float mx = 0.f;
-                        if (q < 3) mx = maximum(q + 1);
-                        uint32_t w[16];
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            float2 e = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])),
-                                            make_float2(sl2, sl2), make_float2(ms, ms));
-                            e.x = ex2(e.x);
-                            e.y = ex2(e.y);
-                            ls[(j >> 1) & 1] = add2(ls[(j >> 1) & 1], e);
-                            w[j >> 1] = pack_bf16x2(e.x, e.y);
-                        }
-                        tmem_st_32x16(tS + q * 16, w);
-                        if (q < 3) follow(q + 1, mx);
-                    }
-                    const float sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
-                    l += sum;
-                    tmem_st_wait();
-                }
+                bool bad = false;
                 if (part) {
                     ok = !lost(wait(&bars->guard[mi % ST], mi / ST));
                     if (!ok) break;
-                    if (live && (bars->bad[mi % ST][0] | bars->bad[mi % ST][1])) {
-                        // O += P V by this warp, seen keys only.
-                        const int i = t - g.t0;
-                        const uint32_t e = cnt + i + min(nt, i + lead);
-                        ok = !lost(wait(&bars->kv_full[e % ST], e / ST));
-                        if (!ok) break;
-                        const uint8_t* v = smem + L::RING + (e % ST) * L::TILE;
-                        const int keys = min(kCacheTile, si.kmax - t * kCacheTile);
-#pragma unroll 1
-                        for (int k = 0; k < DH; k += 32) {
-                            uint32_t o[32];
-                            tmem_ld_32x32(tO + k, o);
-                            tmem_ld_wait();
-                            float acc[32];
+                    bad = bars->bad[mi % ST][0] | bars->bad[mi % ST][1];
+                    // Keys of the tile that this row sees, one bit each.
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) acc[j] = t == begin ? 0.f : __uint_as_float(o[j]);
-#pragma unroll 1
-                            for (int key = 0; key < keys; ++key) {
-                                __syncwarp();
-                                uint32_t pw;
-                                tmem_ld_32x1(tS + (key >> 1), pw);
-                                tmem_ld_wait();
-                                const float pk = (key & 1) ? bf16_hi(pw) : bf16_lo(pw);
-                                const uint32_t sq = key < 64 ? (key < 32 ? see[0] : see[1]) : (key < 96 ? see[2] : see[3]);
-                                const bool sees = sq >> (key & 31) & 1u;
-                                const uint8_t* vr = v + (k >> 6) * kBox + key * 128;
-#pragma unroll
-                                for (int ch = 0; ch < 4; ++ch) {
-                                    const int c16 = ((k & 63) >> 3) + ch;
-                                    const uint4 x = *reinterpret_cast<const uint4*>(vr + ((c16 ^ (key & 7)) << 4));
-                                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                                    for (int y = 0; y < 4; ++y) {
-                                        const int j = ch * 8 + 2 * y;
-                                        acc[j] = sees ? fmaf(pk, bf16_lo(xw[y]), acc[j]) : acc[j];
-                                        acc[j + 1] = sees ? fmaf(pk, bf16_hi(xw[y]), acc[j + 1]) : acc[j + 1];
-                                    }
-                                }
+                    for (int q = 0; q < 4; ++q) {
+                        const int k0 = t * kCacheTile + q * 32;
+                        const int n = (tree ? g.base : seen) - k0;             // the first n keys
+                        see[q] = n >= 32 ? ~0u : n > 0 ? (1u << n) - 1u : 0u;
+                        if (tree) {
+                            const int d = k0 - g.base;                         // draft of the word's bit 0
+                            if (d >= 0) {
+                                if (d < 64) see[q] |= (uint32_t)(word >> d);
+                            } else if (d > -32) {
+                                see[q] |= (uint32_t)(word << -d);
                             }
-                            __syncwarp();
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(acc[j]);
-                            tmem_st_32x32(tO + k, o);
+                            const int end = g.kv_len - k0;                     // bits past the drafts
+                            see[q] &= end >= 32 ? ~0u : end > 0 ? (1u << end) - 1u : 0u;
                         }
-                        tmem_st_wait();
                     }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&bars->p_full[slot]));
+                // One pass over the scores in TMEM, a quarter (32 columns) at a time with the next
+                // load in flight, and P handed over in two halves, so that the first half's
+                // product runs under the second half's exponentials.  The reference m is
+                // checked once a half; when it moves, O (first half included) is scaled.
+                uint32_t u[3][32];
+                float2 ls[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                auto maximum = [&](int q) {              // of quarter q, masked, in the exponent's unit
+                    uint32_t(&x)[32] = u[q % 3];
+                    if (part) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (!(see[q] >> j & 1u)) x[j] = 0xff800000u;       // -inf
+                    }
+                    float a[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) a[k] = fmaxf(__uint_as_float(x[8 * k]), __uint_as_float(x[8 * k + 1]));
+#pragma unroll
+                    for (int j = 2; j < 8; j += 2)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            a[k] = max3(a[k], __uint_as_float(x[8 * k + j]), __uint_as_float(x[8 * k + j + 1]));
+                    return fmaxf(max3(a[0], a[1], a[2]), a[3]) * sl2;
+                };
+                auto follow = [&](int half, float mx) {  // moves m before a half's exponentials when it has to
+                    const bool grow = mx - m > 8.f;                            // also from m = -inf
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float up = ceilf(mx), f = grow ? ex2(m - up) : 1.f;   // m = -inf: the sums so far are 0
+                        if (grow) m = up;
+                        l *= f;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            ls[k].x *= f;
+                            ls[k].y *= f;
+                        }
+                        if (half || t != begin) {
+                            if (half && !bad) {
+                                ok = !lost(wait(&bars->half_done[slot], ns - 1));
+                                tc_fence_after();
+                            }
+                            scale_rows<DH>(tO, f);
+                        }
+                    }
+                };
+                auto exponentials = [&](int q) {
+                    uint32_t(&x)[32] = u[q % 3];
+                    const float ms = m == -INFINITY ? 0.f : -m;                // a row without keys so far: p = 0
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        float2 e = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])),
+                                        make_float2(sl2, sl2), make_float2(ms, ms));
+                        e.x = ex2(e.x);
+                        e.y = ex2(e.y);
+                        ls[(j >> 1) & 1] = add2(ls[(j >> 1) & 1], e);
+                        w[j >> 1] = pack_bf16x2(e.x, e.y);
+                    }
+                    tmem_st_32x16(tS + q * 16, w);
+                };
+                auto by_hand = [&](int half) {
+                    const int i = t - g.t0;
+                    const uint32_t e = cnt + i + min(nt, i + lead);
+                    ok = !lost(wait(&bars->kv_full[e % ST], e / ST));
+                    pv_by_hand<DH>(tS, tO, smem + L::RING + (e % ST) * L::TILE, 64 * half,
+                                   min(64 * half + 64, si.kmax - t * kCacheTile), half ? see[2] : see[0],
+                                   half ? see[3] : see[1], t == begin && !half);
+                };
+                auto hand_over = [&](uint64_t* b) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(b));
+                };
+                float mx = 0.f;
+                if (live) {
+                    tmem_ld_32x32(tS, u[0]);
+                    tmem_ld_32x32(tS + 32, u[1]);
+                    landed(u[0]);
+                    landed(u[1]);
+                    tmem_ld_32x32(tS + 64, u[2]);
+                    follow(0, fmaxf(maximum(0), maximum(1)));
+                    exponentials(0);
+                    landed(u[2]);
+                    tmem_ld_32x32(tS + 96, u[0]);
+                    mx = maximum(2);
+                    exponentials(1);
+                    tmem_st_wait();
+                    if (bad) by_hand(0);
+                }
+                hand_over(&bars->p_half[slot]);
+                if (live) {
+                    landed(u[0]);
+                    follow(1, fmaxf(mx, maximum(3)));
+                    exponentials(2);
+                    exponentials(3);
+                    l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+                    tmem_st_wait();
+                    if (bad) by_hand(1);
+                }
+                if (!ok) break;
+                hand_over(&bars->p_full[slot]);
             }
             if (!ok) break;
             cnt += 2 * nt;
@@ -1026,6 +1075,14 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
                                          (int)smem_bytes<DH>());
     }, true);
     if (e != cudaSuccess) return e;
+    // What the warpgroups ask for has to be within what the block is launched with, or
+    // they would wait for it.
+    static PerDevice regs;
+    const int nreg = regs.get([] {
+        cudaFuncAttributes fa = {};
+        return cudaFuncGetAttributes(&fa, cache_attention_kernel<DH>) == cudaSuccess ? fa.numRegs : 0;
+    });
+    if (nreg * kThreads < 104 * 128 + 200 * 256) return cudaErrorInvalidConfiguration;
     e = launch_pdl(cache_attention_kernel<DH>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
                    c, p);
     if (e != cudaSuccess || p.join_here) return e;
