@@ -54,7 +54,7 @@ struct Layout {
     static constexpr int KB = DH / 64;
     static constexpr int TILE = KB * kBox;
     static constexpr int STAGES = 160 * 1024 / TILE;     // ring of K and V tiles
-    static constexpr int Q = 0;                          // two query tiles; joins odd and even key tiles' O
+    static constexpr int Q = 0;                          // two query tiles
     static constexpr int RING = 2 * TILE;
     static constexpr int BYTES = RING + STAGES * TILE;
 };
@@ -75,12 +75,12 @@ struct __align__(8) Bars {
     uint64_t s_full[2], o_full[2];
     uint64_t p_half[2], p_full[2];   // P of a tile's first 64 keys, of all
     uint64_t half_done[2];           // O has the first 64 keys' part
-    uint64_t x_full[4];
+    uint64_t x_full[2][4], x_done[2][4];   // a slot's maxima and sums are there, the other slot's O has been read
     uint64_t part_done, join_go;
     uint64_t seg_full[kSegSlots], seg_empty[kSegSlots];
     Seg seg[kSegSlots];
     int bad[10][2];      // guard warps' finding per ring stage
-    float2 xml[128];     // odd slot's maximum and sum per row
+    float2 xml[2][128];  // each slot's maximum and sum per row
     uint32_t tmem_base;
     int last_part;       // this CTA wrote an item's last missing part
     int abort_flag, never;
@@ -89,7 +89,7 @@ constexpr int kSegReaders = 1 + 2 + 8;   // warps that read a segment
 
 template <int DH>
 constexpr size_t smem_bytes() {
-    return 1024 + (size_t)Layout<DH>::BYTES + sizeof(Bars);
+    return (size_t)Layout<DH>::BYTES + sizeof(Bars);
 }
 
 // What every role derives from a segment.
@@ -325,10 +325,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                        const __grid_constant__ AttendParams p) {
     using L = Layout<DH>;
     constexpr int ST = L::STAGES;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw = smem_u32(smem_raw);
-    uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+    extern __shared__ __align__(1024) uint8_t smem[];    // swizzled tiles start at multiples of 1024
     const uint32_t sb = smem_u32(smem);
+    if (sb & 1023u) {
+        if (threadIdx.x == 0) atomicCAS(c.err, 0, ERR_TIMEOUT_CACHE_ATTN);
+        return;
+    }
     Bars* bars = reinterpret_cast<Bars*>(smem + L::BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool tree = p.tree != nullptr;
@@ -350,7 +352,10 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(smem_u32(&bars->half_done[s]), 1);
             mbar_init(smem_u32(&bars->o_full[s]), 1);
         }
-        for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&bars->x_full[s]), 1);
+        for (int s = 0; s < 8; ++s) {
+            mbar_init(smem_u32(&bars->x_full[s >> 2][s & 3]), 1);
+            mbar_init(smem_u32(&bars->x_done[s >> 2][s & 3]), 1);
+        }
         mbar_init(smem_u32(&bars->part_done), 8);
         mbar_init(smem_u32(&bars->join_go), 1);
         for (int s = 0; s < kSegSlots; ++s) {
@@ -729,60 +734,68 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // -------------------------------------------------- softmax and output
+        // Little is kept in registers from tile to tile (the scores need them): the segment
+        // is read in shared memory where it is needed, and of the barriers' phases there
+        // is one bit each.
+        constexpr uint32_t kPhS = 1, kPhO = 2, kPhX = 4, kPhJ = 8;
         const int slot = (warp - 4) >> 2;
         const int qw = warp & 3;                           // TMEM lane quarter
         const int r = qw * 32 + lane;
-        const uint32_t loff = (uint32_t)(qw * 32) << 16;
-        const uint32_t tS = tbase + loff + slot * 128, tO = tbase + loff + 256 + slot * DH;
-        const int tok_in_tile = r / rep, head_in_tile = r - tok_in_tile * rep;
+        const uint32_t tS = tbase + ((uint32_t)(qw * 32) << 16) + slot * 128;
+        const uint32_t tO = tS - slot * 128 + 256 + slot * DH;
+        const int tok_in_tile = r / rep;
         const float sl2 = p.scale_log2;
-        uint32_t ns = 0, no = 0, nx = 0, nj = 0, masked = 0, cnt = 0;
-        Seg g;
-        bool ok = true;
-        for (int it = 0; ok && next_seg(it, g); ++it) {
-            const SegInfo si = seg_info(g, TT, tree);
-            const int nt = g.t1 - g.t0, lead = si.dual ? 1 : 2;
-            const int tok0 = si.dual ? slot * TT : 0;
+        uint32_t ph = 0, masked = 0, cnt = 0;
+        bool ok = true, reads_mine = false;
+        for (int it = 0; ok; ++it) {
+            if (lost(wait(&bars->seg_full[it % kSegSlots], it / kSegSlots))) break;
+            const Seg& g = bars->seg[it % kSegSlots];
+            if (!g.valid) break;
+            const bool dual = g.ntok > TT;
+            const int tok0 = dual ? slot * TT : 0;
             const int ntok = min(TT, g.ntok - tok0);       // tokens of this slot's tile
-            const bool mine = tok_in_tile < ntok;          // (rows past tile_tokens * rep have no token)
             const bool live = (qw * 32) / rep < ntok;      // some row of the warp has one
-            const int lim = slot ? si.n1 : si.n0;
-            const int step = si.dual ? 1 : 2, begin = g.t0 + (si.dual ? 0 : slot);
+            const int step = dual ? 1 : 2, begin = g.t0 + (dual ? 0 : slot);
+            int lim, first_part, mask0;                    // tiles, first partly masked one, index of a tile among those
+            {
+                const SegInfo si = seg_info(g, TT, tree);
+                lim = slot ? si.n1 : si.n0;
+                first_part = si.kall / kCacheTile;
+                const int m0 = max(g.t0, first_part);
+                mask0 = (int)masked - m0;
+                masked += max(0, g.t1 - m0);
+            }
             const bool work = begin < lim;
-            const int token = g.row + tok0 + min(tok_in_tile, ntok - 1);
-            const int seen = g.first + tok0 + min(tok_in_tile, ntok - 1) + 1;   // causal
-            const uint64_t word = (tree && live) ? p.tree[token] : 0;
             float m = -INFINITY, l = 0.f;
-            int left = work ? (lim - begin + step - 1) / step : 0;   // tiles still to come
-            if (left == 0) {
+            if (!work) {
                 // Not before this segment's queries are there: an idle slot must not
                 // count for an earlier segment.
                 ok = !lost(wait(&bars->q_full, it));
                 if (!ok) break;
                 if (lane == 0) mbar_arrive(bar(&bars->q_empty));
             }
-            for (int t = g.t0; ok && t < g.t1; ++t) {
-                const bool part = (t + 1) * kCacheTile > si.kall;
-                const uint32_t mi = masked;
-                if (part) ++masked;
-                if ((!si.dual && ((t - g.t0) & 1) != slot) || t >= lim) continue;
-                ok = !lost(wait(&bars->s_full[slot], ns));
+#pragma unroll 1
+            for (int t = begin; t < lim; t += step) {
+                ok = !lost(wait(&bars->s_full[slot], ph));
                 if (!ok) break;
-                ++ns;
+                ph ^= kPhS;
                 tc_fence_after();
-                --left;
-                if (left == 0 && si.dual && lane == 0) mbar_arrive(bar(&bars->q_empty));
+                if (t + step >= lim && lane == 0) mbar_arrive(bar(&bars->q_empty));
+                const bool part = t >= first_part;
                 uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
                 bool bad = false;
                 if (part) {
+                    const uint32_t mi = (uint32_t)(mask0 + t);
                     ok = !lost(wait(&bars->guard[mi % ST], mi / ST));
                     if (!ok) break;
                     bad = bars->bad[mi % ST][0] | bars->bad[mi % ST][1];
                     // Keys of the tile that this row sees, one bit each.
+                    const int tok = tok0 + min(tok_in_tile, ntok - 1);
+                    const int all = tree ? g.base : g.first + tok + 1;         // keys before this one are seen
+                    const uint64_t word = tree ? __ldg(p.tree + g.row + tok) : 0;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const int k0 = t * kCacheTile + q * 32;
-                        const int n = (tree ? g.base : seen) - k0;             // the first n keys
+                        const int k0 = t * kCacheTile + q * 32, n = all - k0;
                         see[q] = n >= 32 ? ~0u : n > 0 ? (1u << n) - 1u : 0u;
                         if (tree) {
                             const int d = k0 - g.base;                         // draft of the word's bit 0
@@ -832,7 +845,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         }
                         if (half || t != begin) {
                             if (half && !bad) {
-                                ok = !lost(wait(&bars->half_done[slot], ns - 1));
+                                ok = !lost(wait(&bars->half_done[slot], ph ^ kPhS));
                                 tc_fence_after();
                             }
                             scale_rows<DH>(tO, f);
@@ -855,11 +868,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     tmem_st_32x16(tS + q * 16, w);
                 };
                 auto by_hand = [&](int half) {
-                    const int i = t - g.t0;
-                    const uint32_t e = cnt + i + min(nt, i + lead);
+                    const int i = t - g.t0, nt = g.t1 - g.t0;
+                    const uint32_t e = cnt + i + min(nt, i + (dual ? 1 : 2));
                     ok = !lost(wait(&bars->kv_full[e % ST], e / ST));
+                    const int kmax = tree ? g.kv_len : g.first + g.ntok;
                     pv_by_hand<DH>(tS, tO, smem + L::RING + (e % ST) * L::TILE, 64 * half,
-                                   min(64 * half + 64, si.kmax - t * kCacheTile), half ? see[2] : see[0],
+                                   min(64 * half + 64, kmax - t * kCacheTile), half ? see[2] : see[0],
                                    half ? see[3] : see[1], t == begin && !half);
                 };
                 auto hand_over = [&](uint64_t* b) {
@@ -883,6 +897,11 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     tmem_st_wait();
                     if (bad) by_hand(0);
                 }
+                if (reads_mine) {                        // the other slot reads this one's last O
+                    ok = !lost(wait(&bars->x_done[slot ^ 1][qw], (ph / kPhX) ^ 1u));
+                    if (!ok) break;
+                    reads_mine = false;
+                }
                 hand_over(&bars->p_half[slot]);
                 if (live) {
                     landed(u[0]);
@@ -897,107 +916,74 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 hand_over(&bars->p_full[slot]);
             }
             if (!ok) break;
-            cnt += 2 * nt;
+            cnt += 2 * (g.t1 - g.t0);
             // ---- the segment's result
             if (work) {
-                ok = !lost(wait(&bars->o_full[slot], no));
+                ok = !lost(wait(&bars->o_full[slot], ph / kPhO));
                 if (!ok) break;
-                ++no;
+                ph ^= kPhO;
                 tc_fence_after();
             }
-            // In a one-tile item both slots hold parts of the same rows: slot 1 hands its own to
-            // slot 0 through shared memory, unless all parts are joined right after.
+            const bool mine = tok_in_tile < ntok;          // (rows past tile_tokens * rep have no token)
+            const int token = g.row + tok0 + min(tok_in_tile, ntok - 1);
+            // In a one-tile item both slots hold parts of the same rows: they tell each other the
+            // maxima and sums, and each puts out half of the columns, reading both O's.
+            // (Apart: parts of a cut item that are joined right after go out as they are.)
             const bool apart = g.part >= 0 && p.join_here;
-            const bool joins = !si.dual && !apart && g.t0 + 1 < si.n1;
-            if (!si.dual && slot == 1 && !apart) {
-                // All products of the segment are done: the query tiles' space takes this slot's O.
-                if (joins) {
-                    if (live) {
-#pragma unroll 1
-                        for (int k = 0; k < DH; k += 32) {
-                            uint32_t o[32];
-                            tmem_ld_32x32(tO + k, o);
-                            tmem_ld_wait();
-                            if (mine) {
-                                uint8_t* dst = smem + L::Q + r * DH * 4;
-#pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    *reinterpret_cast<uint4*>(dst + ((((k >> 2) + j) ^ (r & (DH / 4 - 1))) << 4)) =
-                                        make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                            }
-                            __syncwarp();
-                        }
-                        bars->xml[r] = make_float2(m, l);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bar(&bars->x_full[qw]));
-                        mbar_arrive(bar(&bars->q_empty));
-                    }
-                }
-                tc_fence_before();
-                continue;
-            }
+            const bool joins = !dual && !apart && g.t0 + 1 < lim;   // (without two tiles lim is the same for both)
             float fo = 1.f, fx = 0.f;
             if (joins) {
-                ok = !lost(wait(&bars->x_full[qw], nx));
+                bars->xml[slot][r] = make_float2(m, l);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&bars->x_full[slot][qw]));
+                ok = !lost(wait(&bars->x_full[slot ^ 1][qw], ph / kPhX));
                 if (!ok) break;
-                ++nx;
-                if (live) {
-                    const float2 x = bars->xml[r];
-                    const float top = fmaxf(m, x.x), ms = top == -INFINITY ? 0.f : top;
-                    fo = ex2(m - ms);
-                    fx = ex2(x.x - ms);
-                    l = l * fo + x.y * fx;
-                    m = top;
-                }
+                ph ^= kPhX;
+                tc_fence_after();
+                const float2 x = bars->xml[slot ^ 1][r];
+                const float top = fmaxf(m, x.x), ms = top == -INFINITY ? 0.f : top;
+                fo = ex2(m - ms);
+                fx = ex2(x.x - ms);
+                l = l * fo + x.y * fx;
+                m = top;
             }
-            if (live) {
+            if (live && (dual || slot == 0 || joins || apart)) {
                 float* po = nullptr;
                 __nv_bfloat16* out = nullptr;
                 if (g.part >= 0) {
-                    const size_t row = (size_t)g.part * 256 + (si.dual || apart ? slot * 128 : 0) + r;
+                    const size_t row = (size_t)g.part * 256 + (dual || apart ? slot * 128 : 0) + r;
                     po = c.part_o + row * DH;
-                    if (mine) c.part_ml[row] = make_float2(work ? m : -INFINITY, l);
+                    if (mine && !(joins && slot)) c.part_ml[row] = make_float2(work ? m : -INFINITY, l);
                 } else {
-                    out = p.out + (size_t)token * p.ld_out + (size_t)(g.head * rep + head_in_tile) * DH;
+                    out = p.out + (size_t)token * p.ld_out + (size_t)(g.head * rep + r - tok_in_tile * rep) * DH;
+                    const float il = l == 0.f ? 0.f : 1.f / l;
+                    fo *= il;
+                    fx *= il;
                 }
-                const float il = g.part >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-                fo *= il;
-                fx *= il;
+                const uint32_t tX = slot ? tO - DH : tO + DH;
+                const int k_end = joins && !slot ? DH / 2 : DH;
 #pragma unroll 1
-                for (int k = 0; k < DH; k += 32) {
-                    uint32_t o[32];
-                    if (work) {
-                        tmem_ld_32x32(tO + k, o);
-                        tmem_ld_wait();
-                    }
+                for (int k = joins && slot ? DH / 2 : 0; k < k_end; k += 16) {
+                    uint32_t o[16], y[16];
+                    if (work) tmem_ld_32x16(tO + k, o);
+                    if (joins) tmem_ld_32x16(tX + k, y);
+                    tmem_ld_wait();
+                    float f[16];
+                    // A factor or sum of 0 says that nothing was summed (O may hold anything then).
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) f[j] = work && l != 0.f && fo != 0.f ? __uint_as_float(o[j]) * fo : 0.f;
+                    if (joins)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) f[j] = fx != 0.f ? fmaf(__uint_as_float(y[j]), fx, f[j]) : f[j];
                     if (mine) {
-                        float f[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) f[j] = work && l != 0.f ? __uint_as_float(o[j]) * fo : 0.f;
-                        if (joins) {
-                            const uint8_t* src = smem + L::Q + r * DH * 4;
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const float4 x = *reinterpret_cast<const float4*>(
-                                    src + ((((k >> 2) + j) ^ (r & (DH / 4 - 1))) << 4));
-                                if (fx != 0.f) {
-                                    f[4 * j] = fmaf(x.x, fx, f[4 * j]);
-                                    f[4 * j + 1] = fmaf(x.y, fx, f[4 * j + 1]);
-                                    f[4 * j + 2] = fmaf(x.z, fx, f[4 * j + 2]);
-                                    f[4 * j + 3] = fmaf(x.w, fx, f[4 * j + 3]);
-                                }
-                            }
-                        }
                         if (po) {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 4)
+                            for (int j = 0; j < 16; j += 4)
                                 *reinterpret_cast<float4*>(po + k + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
                         } else {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 8)
+                            for (int j = 0; j < 16; j += 8)
                                 *reinterpret_cast<uint4*>(out + k + j) =
                                     make_uint4(pack_bf16x2(f[j], f[j + 1]), pack_bf16x2(f[j + 2], f[j + 3]),
                                                pack_bf16x2(f[j + 4], f[j + 5]), pack_bf16x2(f[j + 6], f[j + 7]));
@@ -1006,12 +992,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     __syncwarp();
                 }
             }
-            if (!si.dual && work) {
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&bars->q_empty));
-            }
             tc_fence_before();
+            if (joins) {
+                // The other slot's O may be overwritten: it waits for this before its next one.
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&bars->x_done[slot][qw]));
+                reads_mine = true;
+            }
             if (apart) {
                 // Whoever writes an item's last missing part joins them all.  (The barrier
                 // orders the CTA's writes before the one fence and count.)
@@ -1019,7 +1006,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (lane == 0) mbar_arrive(bar(&bars->part_done));
                 const CacheShare& sh = c.shares[g.t0 > 0 ? blockIdx.x : blockIdx.x + 1];   // a share that begins in the item
                 const int first = sh.first, last = sh.last;
-                ok = !lost(wait(&bars->part_done, nj));
+                ok = !lost(wait(&bars->part_done, ph / kPhJ));
                 if (!ok) break;
                 if (warp == 4 && lane == 0) {
                     __threadfence();
@@ -1029,13 +1016,15 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     bars->last_part = mine_last;
                     mbar_arrive(bar(&bars->join_go));
                 }
-                ok = !lost(wait(&bars->join_go, nj));
+                ok = !lost(wait(&bars->join_go, ph / kPhJ));
                 if (!ok) break;
-                ++nj;
+                ph ^= kPhJ;
                 if (bars->last_part)
                     for (int r0 = warp - 4; r0 < g.ntok * rep; r0 += 8)
                         join_rows<DH, 1, 8>(c, p, g.row, g.head, g.ntok * rep, 1, first, last, r0, lane);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&bars->seg_empty[it % kSegSlots]));
         }
     }
     __syncthreads();
