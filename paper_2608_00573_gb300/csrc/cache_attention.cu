@@ -191,24 +191,8 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return r;
 }
 
-// What the softmax warps seldom do stands in functions of its own, out of the way of the
-// code that they run for every tile.
-
-// This warp's rows of O (DH columns) times f.
-template <int DH>
-__device__ __noinline__ void scale_rows(uint32_t tO, float f) {
-#pragma unroll 1
-    for (int k = 0; k < DH; k += 32) {
-        uint32_t o[32];
-        tmem_ld_32x32(tO + k, o);
-        landed(o);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-        tmem_st_32x32(tO + k, o);
-    }
-    tmem_st_wait();
-}
-
+// Seldom used, so a function of its own, out of the way of the code that runs for every
+// tile.
 // O += P V of keys [key0, key1) of a tile (of one half of it; see0, see1: those that the
 // row sees) for this warp's rows.  v: the tile's value rows.
 template <int DH>
@@ -766,7 +750,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 masked += max(0, g.t1 - m0);
             }
             const bool work = begin < lim;
-            float m = -INFINITY, l = 0.f;
+            float m = 0.f, l = 0.f;                        // (no key seen yet: m is arbitrary)
             if (!work) {
                 // Not before this segment's queries are there: an idle slot must not
                 // count for an earlier segment.
@@ -811,17 +795,19 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 // One pass over the scores in TMEM, a quarter (32 columns) at a time with the next
                 // load in flight, and P handed over in two halves, so that the first half's
-                // product runs under the second half's exponentials.  The reference m is
-                // checked once a half; when it moves, O (first half included) is scaled.
+                // product runs under the second half's exponentials.  These start from the
+                // reference m at hand, beside the search for the half's maximum (other units);
+                // when that is more than 2^8 above m, or far below the row's first one, m
+                // moves (to a whole number), O and l are scaled, and they are repeated.
                 uint32_t u[3][32];
-                float2 ls[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                auto maximum = [&](int q) {              // of quarter q, masked, in the exponent's unit
-                    uint32_t(&x)[32] = u[q % 3];
-                    if (part) {
+                float2 ls[2];
+                auto hide = [&](int q) {                 // masked scores of quarter q
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!(see[q] >> j & 1u)) x[j] = 0xff800000u;       // -inf
-                    }
+                    for (int j = 0; j < 32; ++j)
+                        if (!(see[q] >> j & 1u)) u[q % 3][j] = 0xff800000u;        // -inf
+                };
+                auto maximum = [&](int q) {              // of quarter q, in the exponent's unit
+                    const uint32_t(&x)[32] = u[q % 3];
                     float a[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) a[k] = fmaxf(__uint_as_float(x[8 * k]), __uint_as_float(x[8 * k + 1]));
@@ -832,29 +818,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             a[k] = max3(a[k], __uint_as_float(x[8 * k + j]), __uint_as_float(x[8 * k + j + 1]));
                     return fmaxf(max3(a[0], a[1], a[2]), a[3]) * sl2;
                 };
-                auto follow = [&](int half, float mx) {  // moves m before a half's exponentials when it has to
-                    const bool grow = mx - m > 8.f;                            // also from m = -inf
-                    if (__any_sync(0xffffffffu, grow)) {
-                        const float up = ceilf(mx), f = grow ? ex2(m - up) : 1.f;   // m = -inf: the sums so far are 0
-                        if (grow) m = up;
-                        l *= f;
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            ls[k].x *= f;
-                            ls[k].y *= f;
-                        }
-                        if (half || t != begin) {
-                            if (half && !bad) {
-                                ok = !lost(wait(&bars->half_done[slot], ph ^ kPhS));
-                                tc_fence_after();
-                            }
-                            scale_rows<DH>(tO, f);
-                        }
-                    }
-                };
                 auto exponentials = [&](int q) {
-                    uint32_t(&x)[32] = u[q % 3];
-                    const float ms = m == -INFINITY ? 0.f : -m;                // a row without keys so far: p = 0
+                    const uint32_t(&x)[32] = u[q % 3];
+                    const float ms = -m;
                     uint32_t w[16];
 #pragma unroll
                     for (int j = 0; j < 32; j += 2) {
@@ -866,6 +832,38 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         w[j >> 1] = pack_bf16x2(e.x, e.y);
                     }
                     tmem_st_32x16(tS + q * 16, w);
+                };
+                auto half_tile = [&](int half) {
+                    ls[0] = ls[1] = make_float2(0.f, 0.f);
+                    const float mx = fmaxf(maximum(2 * half), maximum(2 * half + 1));
+                    exponentials(2 * half);
+                    exponentials(2 * half + 1);
+                    const bool move = mx - m > 8.f || (l == 0.f && mx - m < -8.f && mx != -INFINITY);
+                    if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
+                        const float up = ceilf(mx), f = move && l != 0.f ? ex2(m - up) : 1.f;   // l = 0: so is O
+                        if (move) m = up;
+                        l *= f;
+                        if (half || t != begin) {
+                            if (half && !bad) {
+                                ok = !lost(wait(&bars->half_done[slot], ph ^ kPhS));
+                                tc_fence_after();
+                            }
+#pragma unroll 1
+                            for (int k = 0; k < DH; k += 16) {
+                                uint32_t o[16];
+                                tmem_ld_32x16(tO + k, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                tmem_st_32x16(tO + k, o);
+                            }
+                        }
+                        ls[0] = ls[1] = make_float2(0.f, 0.f);
+                        exponentials(2 * half);
+                        exponentials(2 * half + 1);
+                    }
+                    l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+                    tmem_st_wait();
                 };
                 auto by_hand = [&](int half) {
                     const int i = t - g.t0, nt = g.t1 - g.t0;
@@ -881,21 +879,23 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(b));
                 };
-                float mx = 0.f;
                 if (live) {
                     tmem_ld_32x32(tS, u[0]);
                     tmem_ld_32x32(tS + 32, u[1]);
                     landed(u[0]);
                     landed(u[1]);
                     tmem_ld_32x32(tS + 64, u[2]);
-                    follow(0, fmaxf(maximum(0), maximum(1)));
-                    exponentials(0);
-                    landed(u[2]);
-                    tmem_ld_32x32(tS + 96, u[0]);
-                    mx = maximum(2);
-                    exponentials(1);
-                    tmem_st_wait();
+                    if (part) {
+                        hide(0);
+                        hide(1);
+                    }
+                    if (t == begin) {                    // a reference that the next tiles seldom leave
+                        const float mx = fmaxf(maximum(0), maximum(1));
+                        m = mx == -INFINITY ? 0.f : ceilf(mx);
+                    }
+                    half_tile(0);
                     if (bad) by_hand(0);
+                    tmem_ld_32x32(tS + 96, u[0]);
                 }
                 if (reads_mine) {                        // the other slot reads this one's last O
                     ok = !lost(wait(&bars->x_done[slot ^ 1][qw], (ph / kPhX) ^ 1u));
@@ -905,11 +905,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 hand_over(&bars->p_half[slot]);
                 if (live) {
                     landed(u[0]);
-                    follow(1, fmaxf(mx, maximum(3)));
-                    exponentials(2);
-                    exponentials(3);
-                    l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
-                    tmem_st_wait();
+                    landed(u[2]);
+                    if (part) {
+                        hide(2);
+                        hide(3);
+                    }
+                    half_tile(1);
                     if (bad) by_hand(1);
                 }
                 if (!ok) break;
@@ -931,6 +932,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             // (Apart: parts of a cut item that are joined right after go out as they are.)
             const bool apart = g.part >= 0 && p.join_here;
             const bool joins = !dual && !apart && g.t0 + 1 < lim;   // (without two tiles lim is the same for both)
+            if (l == 0.f) m = -INFINITY;                   // no key seen
             float fo = 1.f, fx = 0.f;
             if (joins) {
                 bars->xml[slot][r] = make_float2(m, l);
