@@ -26,13 +26,18 @@ struct trimmoe_cache {
     float theta = 0.f;                        // base of turn[]
     uint64_t turn[64];
 
-    trimmoe_status fail(trimmoe_status s, const std::string& m) {
-        err = m;
+    // Keeps "what: why" (nothing when there is no memory for it: no exception leaves a call).
+    trimmoe_status fail(trimmoe_status s, const char* what, const char* why) noexcept {
+        try {
+            err.assign(what).append(": ").append(why);
+        } catch (...) {
+            err.clear();
+        }
         return s;
     }
-    trimmoe_status launched(cudaError_t e, int n_kernels, const char* what) {
+    trimmoe_status launched(cudaError_t e, int n_kernels, const char* what) noexcept {
         if (e == cudaSuccess) e = cudaGetLastError();
-        if (e != cudaSuccess) return fail(TRIMMOE_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+        if (e != cudaSuccess) return fail(TRIMMOE_ERR_CUDA, what, cudaGetErrorString(e));
         launches += n_kernels;
         return TRIMMOE_OK;
     }
@@ -59,9 +64,9 @@ struct Range {
     ~Range() { nvtxRangePop(); }
 };
 
-trimmoe_status check_config(const trimmoe_cache_config& c, std::string& why) {
+trimmoe_status check_config(const trimmoe_cache_config& c, const char*& why) {
     auto bad = [&](trimmoe_status s, const char* m) {
-        why = std::string("cache_create: ") + m;
+        why = m;
         return s;
     };
     if (c.layers < 1 || c.q_heads < 1 || c.kv_heads < 1 || c.n_pages < 1 || c.max_seqs < 1 || c.max_pages < 1 ||
@@ -109,25 +114,25 @@ bool query_map(CUtensorMap* tm, const void* base, const CacheDev& d, int T, int 
 
 // Listed sequences: in range and distinct.
 trimmoe_status check_list(trimmoe_cache* c, const char* what, int n, const int32_t* seq, bool fresh_stamp = true) {
-    if (n < 0 || n > c->cfg.max_seqs) return c->fail(TRIMMOE_ERR_ARG, std::string(what) + ": n out of range");
-    if (n > 0 && !seq) return c->fail(TRIMMOE_ERR_ARG, std::string(what) + ": NULL argument");
+    if (n < 0 || n > c->cfg.max_seqs) return c->fail(TRIMMOE_ERR_ARG, what, "n out of range");
+    if (n > 0 && !seq) return c->fail(TRIMMOE_ERR_ARG, what, "NULL argument");
     if (fresh_stamp && ++c->call == 0) {
         std::fill(c->stamp.begin(), c->stamp.end(), 0u);
         c->call = 1;
     }
     for (int i = 0; i < n; ++i) {
         if (seq[i] < 0 || seq[i] >= c->cfg.max_seqs)
-            return c->fail(TRIMMOE_ERR_ARG, std::string(what) + ": sequence out of range");
+            return c->fail(TRIMMOE_ERR_ARG, what, "sequence out of range");
         if (c->stamp[seq[i]] == c->call)
-            return c->fail(TRIMMOE_ERR_ARG, std::string(what) + ": a sequence is listed twice");
+            return c->fail(TRIMMOE_ERR_ARG, what, "a sequence is listed twice");
         c->stamp[seq[i]] = c->call;
     }
     return TRIMMOE_OK;
 }
 
 trimmoe_status check_layer(trimmoe_cache* c, const char* what, int layer) {
-    if (layer < 0 || layer >= c->cfg.layers) return c->fail(TRIMMOE_ERR_ARG, std::string(what) + ": layer out of range");
-    if (c->T < 0) return c->fail(TRIMMOE_ERR_ARG, std::string(what) + ": no step has been begun");
+    if (layer < 0 || layer >= c->cfg.layers) return c->fail(TRIMMOE_ERR_ARG, what, "layer out of range");
+    if (c->T < 0) return c->fail(TRIMMOE_ERR_ARG, what, "no step has been begun");
     return TRIMMOE_OK;
 }
 
@@ -143,22 +148,25 @@ cudaStream_t enter(trimmoe_cache* c, void* stream) {
 
 extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, const trimmoe_cache_state* st,
                                                trimmoe_cache_handle* out) {
-    auto create_fail = [](trimmoe_status s, const std::string& m) {
-        set_global_error(m);
+    auto create_fail = [](trimmoe_status s, const char* m) noexcept {
+        try {
+            set_global_error(std::string("cache_create: ") + m);
+        } catch (...) {
+        }
         return s;
     };
-    if (!out) return create_fail(TRIMMOE_ERR_ARG, "cache_create: out is NULL");
+    if (!out) return create_fail(TRIMMOE_ERR_ARG, "out is NULL");
     *out = nullptr;
     if (!cfg || !st || !st->k || !st->v || !st->table || !st->length || !st->ref)
-        return create_fail(TRIMMOE_ERR_ARG, "cache_create: NULL argument");
+        return create_fail(TRIMMOE_ERR_ARG, "NULL argument");
     if (!aligned16(st->k) || !aligned16(st->v))
-        return create_fail(TRIMMOE_ERR_ARG, "cache_create: k and v must be 16-byte aligned");
-    std::string why;
+        return create_fail(TRIMMOE_ERR_ARG, "k and v must be 16-byte aligned");
+    const char* why = "";
     const trimmoe_status cs = check_config(*cfg, why);
     if (cs != TRIMMOE_OK) return create_fail(cs, why);
     trimmoe_cache* c = new (std::nothrow) trimmoe_cache();
-    if (!c) return create_fail(TRIMMOE_ERR_OOM, "cache_create: host allocation failed");
-    auto bail = [&](trimmoe_status s, const std::string& m) {
+    if (!c) return create_fail(TRIMMOE_ERR_OOM, "host allocation failed");
+    auto bail = [&](trimmoe_status s, const char* m) noexcept {
         trimmoe_cache_destroy(c);
         return create_fail(s, m);
     };
@@ -169,9 +177,9 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         cudaGetLastError();
         cudaDeviceProp prop;
         if (cudaGetDevice(&c->dev) != cudaSuccess || cudaGetDeviceProperties(&prop, c->dev) != cudaSuccess)
-            return bail(TRIMMOE_ERR_CUDA, "cache_create: no CUDA device");
+            return bail(TRIMMOE_ERR_CUDA, "no CUDA device");
         if (prop.major != 10 || prop.minor != 3)
-            return bail(TRIMMOE_ERR_UNSUPPORTED, "cache_create: needs compute capability 10.3");
+            return bail(TRIMMOE_ERR_UNSUPPORTED, "needs compute capability 10.3");
         d.layers = cfg->layers;
         d.Hq = cfg->q_heads;
         d.Hkv = cfg->kv_heads;
@@ -216,22 +224,21 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         alloc(d.arrived, (size_t)d.num_sms);
         alloc(d.err, 1);
         if (e != cudaSuccess)
-            return bail(e == cudaErrorMemoryAllocation ? TRIMMOE_ERR_OOM : TRIMMOE_ERR_CUDA,
-                        std::string("cache_create: ") + cudaGetErrorString(e));
+            return bail(e == cudaErrorMemoryAllocation ? TRIMMOE_ERR_OOM : TRIMMOE_ERR_CUDA, cudaGetErrorString(e));
         e = cudaMemset(d.err, 0, sizeof(int));
         if (e == cudaSuccess) e = cudaMemset(d.plan, 0, sizeof(CachePlan));
         // Without a step a sequence has no drafts to accept.
         if (e == cudaSuccess) e = cudaMemcpy(d.base, d.length, sizeof(int) * (size_t)cfg->max_seqs, cudaMemcpyDeviceToDevice);
         if (e == cudaSuccess) e = cudaDeviceSynchronize();
-        if (e != cudaSuccess) return bail(TRIMMOE_ERR_CUDA, std::string("cache_create: ") + cudaGetErrorString(e));
+        if (e != cudaSuccess) return bail(TRIMMOE_ERR_CUDA, cudaGetErrorString(e));
         c->tm_k.resize(cfg->layers);
         c->tm_v.resize(cfg->layers);
         const size_t layer = (size_t)d.n_pages * d.Hkv * d.page * d.dh;
         for (int l = 0; l < cfg->layers; ++l)
             if (!pool_map(&c->tm_k[l], d.k + l * layer, d) || !pool_map(&c->tm_v[l], d.v + l * layer, d))
-                return bail(TRIMMOE_ERR_CUDA, "cache_create: cuTensorMapEncodeTiled failed");
+                return bail(TRIMMOE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
     } catch (const std::bad_alloc&) {
-        return bail(TRIMMOE_ERR_OOM, "cache_create: host allocation failed");
+        return bail(TRIMMOE_ERR_OOM, "host allocation failed");
     }
     *out = c;
     return TRIMMOE_OK;
@@ -242,15 +249,15 @@ extern "C" trimmoe_status trimmoe_cache_step(trimmoe_cache_handle c, int n, cons
     if (!c) return TRIMMOE_ERR_ARG;
     trimmoe_status s = check_list(c, "cache_step", n, seq);
     if (s != TRIMMOE_OK) return s;
-    if (n > 0 && !q_len) return c->fail(TRIMMOE_ERR_ARG, "cache_step: NULL argument");
+    if (n > 0 && !q_len) return c->fail(TRIMMOE_ERR_ARG, "cache_step", "NULL argument");
     long long T = 0;
     int most = 0;
     for (int i = 0; i < n; ++i) {
-        if (q_len[i] < 0) return c->fail(TRIMMOE_ERR_ARG, "cache_step: q_len must be >= 0");
+        if (q_len[i] < 0) return c->fail(TRIMMOE_ERR_ARG, "cache_step", "q_len must be >= 0");
         T += q_len[i];
         most = std::max(most, q_len[i]);
     }
-    if (T > c->cfg.T_max) return c->fail(TRIMMOE_ERR_ARG, "cache_step: more than T_max new tokens");
+    if (T > c->cfg.T_max) return c->fail(TRIMMOE_ERR_ARG, "cache_step", "more than T_max new tokens");
     c->T = -1;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_step");
@@ -267,20 +274,20 @@ extern "C" trimmoe_status trimmoe_cache_append(trimmoe_cache_handle c, int layer
     if (!c) return TRIMMOE_ERR_ARG;
     const trimmoe_status s = check_layer(c, "cache_append", layer);
     if (s != TRIMMOE_OK) return s;
-    if (!a) return c->fail(TRIMMOE_ERR_ARG, "cache_append: NULL argument");
+    if (!a) return c->fail(TRIMMOE_ERR_ARG, "cache_append", "NULL argument");
     if (c->T == 0) return TRIMMOE_OK;
     const CacheDev& d = c->d;
     if (!a->qkv || !a->q_out || !a->gamma_q != !a->gamma_k)
-        return c->fail(TRIMMOE_ERR_ARG, "cache_append: NULL pointer (gamma_q and gamma_k come together)");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_append", "NULL pointer (gamma_q and gamma_k come together)");
     if (!aligned16(a->qkv) || !aligned16(a->q_out) || !aligned16(a->gamma_q) || !aligned16(a->gamma_k) ||
         a->ld_qkv % 8 || a->ld_q % 8)
-        return c->fail(TRIMMOE_ERR_ARG, "cache_append: pointers must be 16-byte aligned and row strides multiples of 8");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_append", "pointers must be 16-byte aligned and row strides multiples of 8");
     if (a->ld_qkv < (d.Hq + 2 * d.Hkv) * d.dh || a->ld_q < d.Hq * d.dh)
-        return c->fail(TRIMMOE_ERR_ARG, "cache_append: row stride shorter than a row");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_append", "row stride shorter than a row");
     if (a->gamma_q && !(a->norm_eps >= 0.f && std::isfinite(a->norm_eps)))
-        return c->fail(TRIMMOE_ERR_ARG, "cache_append: norm_eps must be finite and >= 0");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_append", "norm_eps must be finite and >= 0");
     if (!(a->rope_theta >= 0.f && std::isfinite(a->rope_theta)) || (a->rope_theta > 0.f && a->rope_theta < 1.f))
-        return c->fail(TRIMMOE_ERR_ARG, "cache_append: rope_theta must be 0 or finite and >= 1");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_append", "rope_theta must be 0 or finite and >= 1");
     if (a->rope_theta > 0.f && a->rope_theta != c->theta) {
         // theta^(-2i/D) / 2 pi turns per position, as a fraction of 2^64.
         for (int i = 0; i < d.dh / 2; ++i)
@@ -311,21 +318,21 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
     if (!c) return TRIMMOE_ERR_ARG;
     const trimmoe_status s = check_layer(c, "cache_attend", layer);
     if (s != TRIMMOE_OK) return s;
-    if (!a) return c->fail(TRIMMOE_ERR_ARG, "cache_attend: NULL argument");
+    if (!a) return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "NULL argument");
     if (c->T == 0) return TRIMMOE_OK;
     const CacheDev& d = c->d;
-    if (!a->q || !a->out) return c->fail(TRIMMOE_ERR_ARG, "cache_attend: NULL pointer");
+    if (!a->q || !a->out) return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "NULL pointer");
     if (!aligned16(a->q) || !aligned16(a->out) || a->ld_q % 8 || a->ld_out % 8 || (reinterpret_cast<uintptr_t>(a->tree) & 7u))
-        return c->fail(TRIMMOE_ERR_ARG, "cache_attend: pointers must be aligned (q, out 16 bytes) and row strides multiples of 8");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "pointers must be aligned (q, out 16 bytes) and row strides multiples of 8");
     if (a->ld_q < d.Hq * d.dh || a->ld_out < d.Hq * d.dh)
-        return c->fail(TRIMMOE_ERR_ARG, "cache_attend: row stride shorter than a row");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "row stride shorter than a row");
     if (!(a->scale >= 0.f && std::isfinite(a->scale)))
-        return c->fail(TRIMMOE_ERR_ARG, "cache_attend: scale must be finite and >= 0");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "scale must be finite and >= 0");
     if (a->tree && c->max_q > kTreeMax)
-        return c->fail(TRIMMOE_ERR_ARG, "cache_attend: a tree has at most 64 tokens per sequence");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "a tree has at most 64 tokens per sequence");
     CUtensorMap tm_q;
     if (!query_map(&tm_q, a->q, d, c->T, a->ld_q))
-        return c->fail(TRIMMOE_ERR_CUDA, "cache_attend: cuTensorMapEncodeTiled failed");
+        return c->fail(TRIMMOE_ERR_CUDA, "cache_attend", "cuTensorMapEncodeTiled failed");
     AttendParams p = {};
     p.tree = a->tree;
     p.out = static_cast<__nv_bfloat16*>(a->out);
@@ -344,12 +351,12 @@ extern "C" trimmoe_status trimmoe_cache_fork(trimmoe_cache_handle c, int n, cons
     if (!c) return TRIMMOE_ERR_ARG;
     trimmoe_status s = check_list(c, "cache_fork", n, dst);
     if (s != TRIMMOE_OK) return s;
-    if (n > 0 && !src) return c->fail(TRIMMOE_ERR_ARG, "cache_fork: NULL argument");
+    if (n > 0 && !src) return c->fail(TRIMMOE_ERR_ARG, "cache_fork", "NULL argument");
     for (int i = 0; i < n; ++i) {
         if (src[i] < 0 || src[i] >= c->cfg.max_seqs)
-            return c->fail(TRIMMOE_ERR_ARG, "cache_fork: sequence out of range");
+            return c->fail(TRIMMOE_ERR_ARG, "cache_fork", "sequence out of range");
         if (c->stamp[src[i]] == c->call)
-            return c->fail(TRIMMOE_ERR_ARG, "cache_fork: a source is also a destination");
+            return c->fail(TRIMMOE_ERR_ARG, "cache_fork", "a source is also a destination");
     }
     if (n == 0) return TRIMMOE_OK;
     c->T = -1;
@@ -363,9 +370,9 @@ extern "C" trimmoe_status trimmoe_cache_truncate(trimmoe_cache_handle c, int n, 
     if (!c) return TRIMMOE_ERR_ARG;
     const trimmoe_status s = check_list(c, "cache_truncate", n, seq);
     if (s != TRIMMOE_OK) return s;
-    if (n > 0 && !length) return c->fail(TRIMMOE_ERR_ARG, "cache_truncate: NULL argument");
+    if (n > 0 && !length) return c->fail(TRIMMOE_ERR_ARG, "cache_truncate", "NULL argument");
     for (int i = 0; i < n; ++i)
-        if (length[i] < 0) return c->fail(TRIMMOE_ERR_ARG, "cache_truncate: length must be >= 0");
+        if (length[i] < 0) return c->fail(TRIMMOE_ERR_ARG, "cache_truncate", "length must be >= 0");
     if (n == 0) return TRIMMOE_OK;
     c->T = -1;
     OnDevice on(c->dev);
@@ -380,7 +387,7 @@ extern "C" trimmoe_status trimmoe_cache_accept(trimmoe_cache_handle c, int n, co
     if (s != TRIMMOE_OK) return s;
     if (n == 0) return TRIMMOE_OK;
     if (!n_acc || ld_path < 0 || (ld_path > 0 && !path))
-        return c->fail(TRIMMOE_ERR_ARG, "cache_accept: NULL argument");
+        return c->fail(TRIMMOE_ERR_ARG, "cache_accept", "NULL argument");
     c->T = -1;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_accept");
@@ -397,7 +404,7 @@ extern "C" trimmoe_status trimmoe_cache_compact(trimmoe_cache_handle c, void* st
 
 extern "C" trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_cache_stats_t* out, int reset) {
     if (!c) return TRIMMOE_ERR_ARG;
-    if (!out) return c->fail(TRIMMOE_ERR_ARG, "cache_stats: NULL argument");
+    if (!out) return c->fail(TRIMMOE_ERR_ARG, "cache_stats", "NULL argument");
     OnDevice on(c->dev);
     cudaGetLastError();
     cudaError_t e = cudaStreamSynchronize(c->last_stream);
@@ -408,22 +415,22 @@ extern "C" trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_ca
         if (e == cudaSuccess) e = cudaMemcpy(ref.data(), c->d.ref, sizeof(int) * ref.size(), cudaMemcpyDeviceToHost);
         for (int r : ref) free_pages += r == 0;
     } catch (const std::bad_alloc&) {
-        return c->fail(TRIMMOE_ERR_OOM, "cache_stats: host allocation failed");
+        return c->fail(TRIMMOE_ERR_OOM, "cache_stats", "host allocation failed");
     }
     if (e == cudaSuccess && reset) e = cudaMemset(c->d.err, 0, sizeof code);
-    if (e != cudaSuccess) return c->fail(TRIMMOE_ERR_CUDA, std::string("cache_stats: ") + cudaGetErrorString(e));
+    if (e != cudaSuccess) return c->fail(TRIMMOE_ERR_CUDA, "cache_stats", cudaGetErrorString(e));
     out->device_error = code;
     out->free_pages = free_pages;
     out->launches = c->launches;
     if (code == TRIMMOE_DEVERR_CACHE_ATTENTION)
-        return c->fail(TRIMMOE_ERR_DEVICE_TIMEOUT, "cache: a wait of the attention kernel ran out");
+        return c->fail(TRIMMOE_ERR_DEVICE_TIMEOUT, "cache", "a wait of the attention kernel ran out");
     if (code == TRIMMOE_DEVERR_CACHE_FULL)
-        return c->fail(TRIMMOE_ERR_CACHE, "cache_step: too few free pages, or a sequence longer than max_pages");
+        return c->fail(TRIMMOE_ERR_CACHE, "cache_step", "too few free pages, or a sequence longer than max_pages");
     if (code == TRIMMOE_DEVERR_CACHE_STATE)
-        return c->fail(TRIMMOE_ERR_CACHE, "cache: table, length or ref hold invalid values");
+        return c->fail(TRIMMOE_ERR_CACHE, "cache", "table, length or ref hold invalid values");
     if (code == TRIMMOE_DEVERR_CACHE_PATH)
-        return c->fail(TRIMMOE_ERR_CACHE, "cache_accept: n_acc or path does not fit the drafts");
-    return code ? c->fail(TRIMMOE_ERR_CACHE, "cache: device error") : TRIMMOE_OK;
+        return c->fail(TRIMMOE_ERR_CACHE, "cache_accept", "n_acc or path does not fit the drafts");
+    return code ? c->fail(TRIMMOE_ERR_CACHE, "cache", "device error") : TRIMMOE_OK;
 }
 
 extern "C" const char* trimmoe_cache_last_error(trimmoe_cache_handle c) { return c ? c->err.c_str() : ""; }

@@ -452,3 +452,55 @@ def test_nothing_to_do():
     c.compact()
     assert c.length.tolist() == [0, 0, 0] and c.stats() == dict(status=0, device_error=0, free_pages=8,
                                                                 launches=c.stats()["launches"])
+
+
+def test_serving_example():
+    """The example's loop: drafted rounds leave the cache that the accepted texts alone would, and attention over it gives
+    what a fresh prefill of the same text gives."""
+    from examples.paged_serving import run
+    r = run(rounds=4, verbose=False)
+    c, text = r["cache"], r["text"]
+    assert r["stats"]["status"] == 0 and r["engine"].stats()["device_error"] == 0
+    assert c.length.tolist() == [len(t) - 1 for t in text]       # all but the last token is in the cache
+    assert r["accepted"] > 0
+    held = sum(-(-n // c.page) for n in c.length.tolist()) - 200 // c.page    # full pages of the forked prompt are shared
+    assert r["stats"]["free_pages"] == c.n_pages - held
+    # The first layer's keys depend on tokens and positions only: those of sequence 1, written round by round, equal a
+    # fresh prefill's up to the rounding of another batch's projection.
+    n = int(c.length[1])
+    got = c.k[0][c.table[1, :-(-n // c.page)].long()].transpose(0, 1).reshape(c.kv_heads, -1, c.head_dim)[:, :n].clone()
+    c.truncate([1], [0])
+    c.step([1], [n])
+    r["model"](torch.tensor(text[1][:n], device=DEV))
+    want = c.k[0][c.table[1, :-(-n // c.page)].long()].transpose(0, 1).reshape(c.kv_heads, -1, c.head_dim)[:, :n]
+    assert ((got.float() - want.float()).abs() <= 2.0 ** -6 * want.float().abs().amax()).all()
+
+
+def test_append_without_rotation_keeps_infinities():
+    c = B.PagedCache.empty(1, 4, 2, 1, 64, 16, 1, 4, T_max=4)
+    c.step([0], [3])
+    qkv = torch.randn((3, 256), device=DEV).to(torch.bfloat16)
+    qkv[1, 5], qkv[2, 130] = float("inf"), float("-inf")
+    out = c.append(0, qkv, theta=0.0)
+    assert torch.equal(out, qkv[:, :128])
+    assert torch.equal(c.k[0, int(c.table[0, 0]), 0, :3], qkv[:, 128:192])
+
+
+def test_calls_follow_the_given_stream():
+    """Work queued on a stream of its own sees what that stream did before it."""
+    c = B.PagedCache.empty(1, 64, 4, 2, 64, 16, 2, 32, T_max=300)
+    c.k.zero_(), c.v.zero_()
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        big = torch.randn((4096, 4096), device=DEV)
+        for _ in range(20):
+            big = big @ big * 1e-3
+        qkv = torch.randn((300, 512), device=DEV).to(torch.bfloat16) + (big.sum() * 0).to(torch.bfloat16)
+        c.step([0, 1], [200, 100])
+        x = c.append(0, qkv)
+        out = c.attend(0, x)
+    m = CacheModel(64, 2, 32, 16)
+    m.step([0, 1], [200, 100])
+    torch.cuda.current_stream().wait_stream(st)
+    check_attend(c, m, x, [200, 100], out, 0)
