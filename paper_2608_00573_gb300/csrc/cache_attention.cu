@@ -885,7 +885,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     landed(u[0]);
                     landed(u[1]);
                     tmem_ld_32x32(tS + 64, u[2]);
-                    if (part) {
+                    if (part && !__all_sync(0xffffffffu, (see[0] & see[1]) == ~0u)) {
                         hide(0);
                         hide(1);
                     }
@@ -906,11 +906,20 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (live) {
                     landed(u[0]);
                     landed(u[2]);
+                    if (part && !__any_sync(0xffffffffu, (see[2] | see[3]) != 0u)) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) w[j] = 0u;
+                        tmem_st_32x16(tS + 32, w);
+                        tmem_st_32x16(tS + 48, w);
+                        tmem_st_wait();
+                    } else {
                     if (part) {
                         hide(2);
                         hide(3);
                     }
                     half_tile(1);
+                    }
                     if (bad) by_hand(1);
                 }
                 if (!ok) break;
