@@ -328,7 +328,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(smem_u32(&bars->guard[s]), 2);
         }
         mbar_init(smem_u32(&bars->q_full), 1);
-        mbar_init(smem_u32(&bars->q_empty), 8);
+        mbar_init(smem_u32(&bars->q_empty), 9);              // softmax and MMA warps
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&bars->s_full[s]), 1);
             mbar_init(smem_u32(&bars->p_half[s]), 4);
@@ -567,6 +567,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
             const int first_masked = uniform(si.kall / kCacheTile - g.t0);
             gave_up |= wait(&bars->q_full, it);
+            // (Also when no slot has work here: the next segment's queries must not come
+            // before this wait has seen its own phase.)
+            if (elect_one()) mbar_arrive(bar(&bars->q_empty));
             // Step i: O += P V of tile i, S = Q K^T of tile i + lead, slot by slot, so that
             // a slot's products run under the other slot's softmax.  (Given up: the waits
             // return at once, the products' results are not used.)

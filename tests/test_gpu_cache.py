@@ -504,3 +504,15 @@ def test_calls_follow_the_given_stream():
     m.step([0, 1], [200, 100])
     torch.cuda.current_stream().wait_stream(st)
     check_attend(c, m, x, [200, 100], out, 0)
+
+
+def test_groups_that_end_before_their_sequence():
+    """Short steps count key tiles to the sequence's end; where a group's own tokens end a tile earlier, a CTA's share may
+    hold nothing but that tile."""
+    shapes, page = (16, 1, 64), 16                       # 8 tokens a query tile, groups of 16 tokens
+    for ctx in ([128 * k - 33 for k in range(1, 12)], [128 * k - 20 for k in range(1, 40, 3)]):
+        q = [64 - (i % 3) for i in range(len(ctx))]
+        cache, m, x = filled(shapes, page, ctx, q, seed=len(ctx))
+        out = cache.attend(0, x)
+        check_attend(cache, m, x, q, out, 0)
+        assert cache.stats()["device_error"] == 0
