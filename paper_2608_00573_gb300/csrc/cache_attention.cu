@@ -328,7 +328,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(smem_u32(&bars->guard[s]), 2);
         }
         mbar_init(smem_u32(&bars->q_full), 1);
-        mbar_init(smem_u32(&bars->q_empty), 9);              // softmax and MMA warps
+        mbar_init(smem_u32(&bars->q_empty), 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&bars->s_full[s]), 1);
             mbar_init(smem_u32(&bars->p_half[s]), 4);
@@ -567,9 +567,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
             const int first_masked = uniform(si.kall / kCacheTile - g.t0);
             gave_up |= wait(&bars->q_full, it);
-            // (Also when no slot has work here: the next segment's queries must not come
-            // before this wait has seen its own phase.)
-            if (elect_one()) mbar_arrive(bar(&bars->q_empty));
             // Step i: O += P V of tile i, S = Q K^T of tile i + lead, slot by slot, so that
             // a slot's products run under the other slot's softmax.  (Given up: the waits
             // return at once, the products' results are not used.)
@@ -627,6 +624,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 const int next = i + lead;
                 const bool more = next < nt;
+                if (next == nt && elect_one()) tc_commit(bar(&bars->q_empty));    // no product reads the queries any more
                 int bad = 0;
                 if (i >= 0) {
                     if (!have_v) ev = entry();
@@ -754,20 +752,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             const bool work = begin < lim;
             float m = 0.f, l = 0.f;                        // (no key seen yet: m is arbitrary)
-            if (!work) {
-                // Not before this segment's queries are there: an idle slot must not
-                // count for an earlier segment.
-                ok = !lost(wait(&bars->q_full, it));
-                if (!ok) break;
-                if (lane == 0) mbar_arrive(bar(&bars->q_empty));
-            }
 #pragma unroll 1
             for (int t = begin; t < lim; t += step) {
                 ok = !lost(wait(&bars->s_full[slot], ph));
                 if (!ok) break;
                 ph ^= kPhS;
                 tc_fence_after();
-                if (t + step >= lim && lane == 0) mbar_arrive(bar(&bars->q_empty));
                 const bool part = t >= first_part;
                 uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
                 bool bad = false;
