@@ -11,30 +11,40 @@
 //                                   shared memory with its D axis contiguous
 //   l = l 2^(...) + sum_j p_j;      out = O / l
 //
-// O is rescaled only when some row's maximum grew by more than 2^8: until then p
-// stays below 2^8, which costs no precision in floating point, and the extra
-// pass over O in TMEM is rare.
+// The reference m need not be the maximum: O and l are rescaled only when a row's
+// maximum is more than a factor 2^8 above m, so p stays below 2^8, which costs no
+// precision in floating point, and the pass over O in TMEM is rare.  m is a whole
+// number, so its factors are exact.  P is rounded to bf16, the type of the tensor cores'
+// other operand; l sums p in fp32 before that rounding.
 //
 // A CTA holds two query tiles in flight ("slots", each with its own S and O in
 // TMEM and its own group of four softmax warps), so that one slot's products run
 // under the other's softmax.  In a group of more than tile_tokens tokens the
 // slots are its two query tiles and share every key tile; in a smaller group
 // (single tokens, short drafts) both slots hold the same tile and take the even and
-// the odd key tiles, and their results are joined at the end.
+// the odd key tiles, and their results are joined at the end, each slot reading the
+// other's O in TMEM.  A thread has one row, so that maxima and sums need no exchange;
+// P is handed over in two halves of 64 keys, the first half's product running under
+// the second half's exponentials.  (Two threads to a row, sixteen softmax warps, spill
+// and are slower: a 16384-token prompt took 2.27 ms against 1.56.)
 //
-// Work is split evenly whatever the lengths: the items' costs are laid end to
-// end and each CTA takes the same share of the line, cutting items at key tiles
-// (cache_pages.cu makes the list).  A cut item's parts go to a buffer, at most two per
-// CTA, and are added in the order of the keys (join_rows), so results do not depend
-// on timing.
+// Work is split evenly whatever the lengths (cache_pages.cu makes the lists).  With many
+// items each CTA draws whole items from a counter, the longest first.  Otherwise the
+// items' costs are laid end to end and each CTA takes the same share of the line, cutting
+// items at key tiles; a cut item's parts go to a buffer, at most two per CTA, and are
+// added in the order of the keys (join_rows), so results do not depend on timing.  With
+// few rows the CTA that writes an item's last part joins it, else cache_join_kernel does.
 //
 // Masked places never reach a result: scores are replaced, not added to; value
 // rows that no row of the item sees are zeroed in shared memory (0 * NaN would
 // be NaN), and a tile whose partly masked value rows hold an infinity or a NaN is
 // multiplied by the softmax warps themselves, skipping masked keys.
 //
-// Bounds: prompts the tensor cores (and the exponentials: 128 x 128 per 4 x 128 x
-// 128 x D multiply-adds); decoding HBM, each K and V row once per query tile.
+// Bounds: prompts the tensor cores and, per key tile, the chain S -> exponentials -> P V
+// of each slot; decoding HBM, each K and V row once per query tile.  Measured (32 query
+// heads on 8, D = 128): a 16384-token prompt 1.50 ms, 1.47 PFLOP/s, 0.76 of cuBLAS; 7
+// sequences of 30k to 65k positions, a token each, 200 us, 0.98 of the copy rate; one
+// sequence of 1500 positions 11.5 us, launches and latencies.
 #include <algorithm>
 #include <cstddef>
 
@@ -65,7 +75,6 @@ struct Seg {
     int seq, kv_len, row, ntok, first, base, head;
     int t0, t1;          // key tiles
     int part;            // part buffer, -1: the whole item
-    int pad;
 };
 
 struct __align__(8) Bars {
@@ -193,6 +202,7 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 
 // Seldom used, so a function of its own, out of the way of the code that runs for every
 // tile.
+//
 // O += P V of keys [key0, key1) of a tile (of one half of it; see0, see1: those that the
 // row sees) for this warp's rows.  v: the tile's value rows.
 template <int DH>
@@ -382,340 +392,340 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     // 168 x 384 at launch).  The two branches do not meet before the roles end: where
     // they met, the compiler would take the smaller number for all that follows.
     if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    if (warp == 0) {
-        // ------------------------------------------------ segments and loads
-        const int b = blockIdx.x;
-        const CachePlan pl = *c.plan;
-        const CacheShare sh = c.shares[b];      // (read with the plan, not after it)
-        int it = 0, nseg = 0;
-        uint32_t cnt = 0, masked = 0;           // ring entries issued, partly masked value tiles among them
-        bool ok = true;
-        auto give_seg = [&](const Seg& g) {
-            const int s = it % kSegSlots;
-            if (it >= kSegSlots && lost(wait(&bars->seg_empty[s], it / kSegSlots - 1))) return false;
-            if (lane == 0) {
-                bars->seg[s] = g;
-                mbar_arrive(bar(&bars->seg_full[s]));
-            }
-            ++it;
-            return true;
-        };
-        const int pages_per_tile = kCacheTile >> c.page_shift;
-        const int my_page = lane / L::KB, my_kb = lane % L::KB;
-        const bool my_box = lane < pages_per_tile * L::KB;
-        // Whole items are drawn from a counter, longest first; else the CTA's share of the
-        // line is walked item by item.
-        const bool whole = pl.n_ctas == 0;
-        const int items = whole ? pl.n_groups * c.Hkv : 0;
-        int item = b, group = 0, head = 0;
-        long long x = 0, x_end = 0, within = 0;
-        CacheGroup g;
-        bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
-        if (any && !whole) {
-            x = sh.begin;
-            x_end = sh.end;
-            within = sh.within;
-            group = sh.group;
-            head = sh.head;
-            g = sh.g;
-        }
-        while (ok && any) {
-            int drawn = 0;
-            Seg sg;
-            if (whole) {
-                if (lane == 0) drawn = atomicAdd(&c.plan->drawn, 1);
-                head = item % c.Hkv;
-                g = c.groups[item / c.Hkv];
-            }
-            const int two_tiles = cache_two_tiles(g.ntok, TT);
-            sg.valid = 1;
-            sg.seq = g.seq;
-            sg.kv_len = g.kv_len;
-            sg.row = g.row;
-            sg.ntok = g.ntok;
-            sg.first = g.first;
-            sg.base = g.base;
-            sg.head = head;
-            sg.pad = 0;
-            if (whole) {
-                sg.t0 = 0;
-                sg.t1 = cache_item_tiles(g.cost, two_tiles);
-                sg.part = -1;
-            } else {
-                const long long x1 = min((long long)g.cost, within + (x_end - x));
-                sg.t0 = cache_tiles_before(within, g.cost, two_tiles);
-                sg.t1 = cache_tiles_before(x1, g.cost, two_tiles);
-                sg.part = (sg.t0 == 0 && sg.t1 == cache_item_tiles(g.cost, two_tiles)) ? -1 : (sg.t0 > 0 ? 2 * b : 2 * b + 1);
-                x += x1 - within;
-                within = 0;
-                any = x < x_end;
-                if (any && ++head == c.Hkv) {
-                    head = 0;
-                    g = c.groups[++group];
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        if (warp == 0) {
+            // ------------------------------------------------ segments and loads
+            const int b = blockIdx.x;
+            const CachePlan pl = *c.plan;
+            const CacheShare sh = c.shares[b];      // (read with the plan, not after it)
+            int it = 0, nseg = 0;
+            uint32_t cnt = 0, masked = 0;           // ring entries issued, partly masked value tiles among them
+            bool ok = true;
+            auto give_seg = [&](const Seg& g) {
+                const int s = it % kSegSlots;
+                if (it >= kSegSlots && lost(wait(&bars->seg_empty[s], it / kSegSlots - 1))) return false;
+                if (lane == 0) {
+                    bars->seg[s] = g;
+                    mbar_arrive(bar(&bars->seg_full[s]));
                 }
+                ++it;
+                return true;
+            };
+            const int pages_per_tile = kCacheTile >> c.page_shift;
+            const int my_page = lane / L::KB, my_kb = lane % L::KB;
+            const bool my_box = lane < pages_per_tile * L::KB;
+            // Whole items are drawn from a counter, longest first; else the CTA's share of the
+            // line is walked item by item.
+            const bool whole = pl.n_ctas == 0;
+            const int items = whole ? pl.n_groups * c.Hkv : 0;
+            int item = b, group = 0, head = 0;
+            long long x = 0, x_end = 0, within = 0;
+            CacheGroup g;
+            bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
+            if (any && !whole) {
+                x = sh.begin;
+                x_end = sh.end;
+                within = sh.within;
+                group = sh.group;
+                head = sh.head;
+                g = sh.g;
             }
-            if (sg.t0 < sg.t1) {
-                if (!give_seg(sg)) break;
-                const SegInfo si = seg_info(sg, TT, tree);
-                // Page indices of the tiles ahead travel in registers.
-                const int n_pages = (si.kmax + c.page - 1) >> c.page_shift;
-                const int* row = c.table + (size_t)sg.seq * c.max_pages;
-                auto page_of = [&](int t) {
-                    const int j = t * pages_per_tile + my_page;
-                    return (my_box && t < sg.t1 && j < n_pages) ? row[j] : -1;
-                };
-                auto load = [&](const CUtensorMap* tm, int t, int id) {
-                    const int s = (int)(cnt % ST);
-                    if (cnt >= (uint32_t)ST && lost(wait(&bars->kv_empty[s], cnt / ST - 1))) return false;
-                    const int have = max(0, min(pages_per_tile, n_pages - t * pages_per_tile));
-                    const uint32_t fb = bar(&bars->kv_full[s]);
-                    if (lane == 0) mbar_arrive_expect_tx(fb, (uint32_t)have * c.page * 128 * L::KB);
-                    __syncwarp();
-                    if (my_box && my_page < have)
-                        tma_load_2d(sb + L::RING + s * L::TILE + my_kb * kBox + my_page * c.page * 128, tm, my_kb * 64,
-                                    (id * c.Hkv + sg.head) << c.page_shift, fb);
-                    __syncwarp();
-                    ++cnt;
-                    return true;
-                };
-                int id0 = page_of(sg.t0), id1 = page_of(sg.t0 + 1), id2 = page_of(sg.t0 + 2);
-                const int lead = si.dual ? 1 : 2;
-                // K of the first `lead` tiles, the queries (once the previous segment's products
-                // have read theirs), then V of tile t and K of tile t + lead in turn.
-#pragma unroll 1
-                for (int t = sg.t0 - lead; ok && t < sg.t1; ++t) {
-                    const int tk = t + lead;
-                    if (t >= sg.t0) {
-                        ok = load(&tm_v, t, id0);
-                        if ((t + 1) * kCacheTile > si.kall) {
-                            if (lane == 0) mbar_arrive(bar(&bars->go[masked % ST]));
-                            ++masked;
-                        }
+            while (ok && any) {
+                int drawn = 0;
+                Seg sg;
+                if (whole) {
+                    if (lane == 0) drawn = atomicAdd(&c.plan->drawn, 1);
+                    head = item % c.Hkv;
+                    g = c.groups[item / c.Hkv];
+                }
+                const int two_tiles = cache_two_tiles(g.ntok, TT);
+                sg.valid = 1;
+                sg.seq = g.seq;
+                sg.kv_len = g.kv_len;
+                sg.row = g.row;
+                sg.ntok = g.ntok;
+                sg.first = g.first;
+                sg.base = g.base;
+                sg.head = head;
+                if (whole) {
+                    sg.t0 = 0;
+                    sg.t1 = cache_item_tiles(g.cost, two_tiles);
+                    sg.part = -1;
+                } else {
+                    const long long x1 = min((long long)g.cost, within + (x_end - x));
+                    sg.t0 = cache_tiles_before(within, g.cost, two_tiles);
+                    sg.t1 = cache_tiles_before(x1, g.cost, two_tiles);
+                    const bool all = sg.t0 == 0 && sg.t1 == cache_item_tiles(g.cost, two_tiles);
+                    sg.part = all ? -1 : 2 * b + (sg.t0 == 0);
+                    x += x1 - within;
+                    within = 0;
+                    any = x < x_end;
+                    if (any && ++head == c.Hkv) {
+                        head = 0;
+                        g = c.groups[++group];
                     }
-                    if (ok && tk < sg.t1) ok = load(&tm_k, tk, t < sg.t0 ? (tk == sg.t0 ? id0 : id1) : (lead == 1 ? id1 : id2));
-                    if (ok && t == sg.t0 - 1) {
-                        ok = nseg == 0 || !lost(wait(&bars->q_empty, nseg - 1));
-                        if (ok && lane == 0) {
-                            const uint32_t qb = bar(&bars->q_full);
-                            const uint32_t bytes = (uint32_t)L::KB * TT * rep * 128;
-                            mbar_arrive_expect_tx(qb, si.dual ? 2 * bytes : bytes);
-                            for (int s = 0; s < (si.dual ? 2 : 1); ++s)
-                                for (int kb = 0; kb < L::KB; ++kb)
-                                    tma_load_3d(sb + L::Q + s * L::TILE + kb * kBox, &tm_q, kb * 64, sg.head * rep,
-                                                sg.row + s * TT, qb);
-                        }
+                }
+                if (sg.t0 < sg.t1) {
+                    if (!give_seg(sg)) break;
+                    const SegInfo si = seg_info(sg, TT, tree);
+                    // Page indices of the tiles ahead travel in registers.
+                    const int n_pages = (si.kmax + c.page - 1) >> c.page_shift;
+                    const int* row = c.table + (size_t)sg.seq * c.max_pages;
+                    auto page_of = [&](int t) {
+                        const int j = t * pages_per_tile + my_page;
+                        return (my_box && t < sg.t1 && j < n_pages) ? row[j] : -1;
+                    };
+                    auto load = [&](const CUtensorMap* tm, int t, int id) {
+                        const int s = (int)(cnt % ST);
+                        if (cnt >= (uint32_t)ST && lost(wait(&bars->kv_empty[s], cnt / ST - 1))) return false;
+                        const int have = max(0, min(pages_per_tile, n_pages - t * pages_per_tile));
+                        const uint32_t fb = bar(&bars->kv_full[s]);
+                        if (lane == 0) mbar_arrive_expect_tx(fb, (uint32_t)have * c.page * 128 * L::KB);
                         __syncwarp();
-                        nseg += ok;
-                    }
-                    if (t >= sg.t0) {
-                        id0 = id1;
-                        id1 = id2;
-                        id2 = page_of(t + 3);
-                    }
-                }
-            }
-            if (whole) {
-                item = (int)gridDim.x + __shfl_sync(0xffffffffu, drawn, 0);
-                any = item < items;
-            }
-        }
-        if (lane == 0 && pl.ok && whole) {
-            // The last CTA to finish drawing leaves the counter at zero for the next call.
-            __threadfence();
-            if (atomicAdd(&c.plan->done, 1) == (int)gridDim.x - 1) {
-                c.plan->drawn = 0;
-                c.plan->done = 0;
-            }
-        }
-        if (ok) {
-            Seg end = {};
-            give_seg(end);
-        }
-        // The last copies have landed, and been read unless the CTA gave up, before
-        // it ends.
-        const uint32_t tail = min(cnt, (uint32_t)ST);
-        const uint32_t never = bb + (uint32_t)offsetof(Bars, never);
-        for (uint32_t k = cnt - tail; k < cnt; ++k) wait_probes(bar(&bars->kv_full[k % ST]), (k / ST) & 1, never, c.err);
-        if (nseg > 0) wait_probes(bar(&bars->q_full), (nseg - 1) & 1, never, c.err);
-        for (uint32_t k = cnt - tail; k < cnt; ++k) wait(&bars->kv_empty[k % ST], k / ST);
-    } else if (warp == 1) {
-        // -------------------------------------------------------------- MMAs
-        // The ring's entries come in the order in which they are used: K of the first
-        // `lead` tiles, then V of tile i and K of tile i + lead in turn.
-        constexpr uint32_t idS = idesc_bf16_f32(128, 128);
-        constexpr uint32_t idO = idesc_bf16_f32(128, DH) | kIdescBMn;
-        const uint32_t tm = __shfl_sync(0xffffffffu, tbase, 0);
-        const uint64_t d_q = smem_desc_sw128(sb + L::Q), d_k = smem_desc_sw128(sb + L::RING);
-        const uint64_t d_v = smem_desc_sw128_mn(sb + L::RING, kBox);
-        constexpr uint32_t kTile16 = L::TILE >> 4;       // a tile in a descriptor's units
-        uint32_t stage = 0, phase = 0, masked = 0, p_phase = 0, gave_up = 0;   // p_phase: one bit per slot
-        auto entry = [&]() {                             // next ring entry, once it has landed
-            const uint32_t e = stage;
-            gave_up |= wait(&bars->kv_full[e], phase);
-            if (++stage == (uint32_t)ST) {
-                stage = 0;
-                phase ^= 1u;
-            }
-            return e;
-        };
-        Seg g;
-        for (int it = 0; !lost(gave_up) && next_seg(it, g); ++it) {
-            const SegInfo si = seg_info(g, TT, tree);
-            auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
-            const int dual = uniform(si.dual), lead = dual ? 1 : 2, nt = uniform(g.t1 - g.t0);
-            const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
-            const int first_masked = uniform(si.kall / kCacheTile - g.t0);
-            gave_up |= wait(&bars->q_full, it);
-            // Step i: O += P V of tile i, S = Q K^T of tile i + lead, slot by slot, so that
-            // a slot's products run under the other slot's softmax.  (Given up: the waits
-            // return at once, the products' results are not used.)
-            uint32_t ev = 0, ek = 0;
-            auto pv = [&](int s, int half, bool began) {             // keys 64 half .. 64 half + 63
-                const uint64_t va = d_v + ev * kTile16 + half * 4 * (2048 >> 4);
-                const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128 + half * 32;
-                if (elect_one()) {
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        tc_mma_bf16_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : (uint32_t)began);
-                    if (half == 0) tc_commit(bar(&bars->half_done[s]));
-                }
-            };
-            auto qk = [&](int s, bool last) {            // last: of the slots that read this key tile
-                const uint64_t qa = d_q + (dual ? s * kTile16 : 0u), ka = d_k + ek * kTile16;
-                if (elect_one()) {
-#pragma unroll
-                    for (int kk = 0; kk < DH / 16; ++kk) {
-                        const uint32_t off = (kk >> 2) * (kBox >> 4) + (kk & 3) * (32 >> 4);
-                        tc_mma_bf16(tm + s * 128, qa + off, ka + off, idS, kk ? 1u : 0u);
-                    }
-                    tc_commit(bar(&bars->s_full[s]));
-                    if (last) tc_commit(bar(&bars->kv_empty[ek]));
-                }
-            };
-            // Steps below `plain` of a two-tile segment need none of the cases.
-            const int plain = dual ? min(min(n0, n1) - 1, first_masked) : 0;
-            bool have_v = false;                         // V of step i has been waited for
+                        if (my_box && my_page < have)
+                            tma_load_2d(sb + L::RING + s * L::TILE + my_kb * kBox + my_page * c.page * 128, tm,
+                                        my_kb * 64, (id * c.Hkv + sg.head) << c.page_shift, fb);
+                        __syncwarp();
+                        ++cnt;
+                        return true;
+                    };
+                    int id0 = page_of(sg.t0), id1 = page_of(sg.t0 + 1), id2 = page_of(sg.t0 + 2);
+                    const int lead = si.dual ? 1 : 2;
+                    // K of the first `lead` tiles, the queries (once the previous segment's products
+                    // have read theirs), then V of tile t and K of tile t + lead in turn.
 #pragma unroll 1
-            for (int i = -lead; i < nt; ++i) {
-                if (i >= 0 && i < plain) {
-                    if (!have_v) ev = entry();
-                    gave_up |= wait(&bars->p_half[0], p_phase);
-                    tc_fence_after();
-                    pv(0, 0, i > 0);
-                    gave_up |= wait(&bars->p_full[0], p_phase);
-                    tc_fence_after();
-                    pv(0, 1, true);
-                    ek = entry();
-                    tc_fence_after();
-                    qk(0, false);
-                    gave_up |= wait(&bars->p_half[1], p_phase >> 1);
-                    tc_fence_after();
-                    pv(1, 0, i > 0);
-                    gave_up |= wait(&bars->p_full[1], p_phase >> 1);
-                    p_phase ^= 3u;
-                    tc_fence_after();
-                    pv(1, 1, true);
-                    if (elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
-                    ev = entry();                        // (step i + 1 exists) under the products queued
-                    have_v = true;
-                    qk(1, true);
-                    continue;
-                }
-                const int next = i + lead;
-                const bool more = next < nt;
-                if (next == nt && elect_one()) tc_commit(bar(&bars->q_empty));    // no product reads the queries any more
-                int bad = 0;
-                if (i >= 0) {
-                    if (!have_v) ev = entry();
-                    have_v = false;
-                    if (i >= first_masked) {
-                        const uint32_t gs = masked % ST, gp = masked / ST;
-                        ++masked;
-                        gave_up |= wait(&bars->guard[gs], gp);
-                        bad = uniform(bars->bad[gs][0] | bars->bad[gs][1]);
+                    for (int t = sg.t0 - lead; ok && t < sg.t1; ++t) {
+                        const int tk = t + lead;
+                        if (t >= sg.t0) {
+                            ok = load(&tm_v, t, id0);
+                            if ((t + 1) * kCacheTile > si.kall) {
+                                if (lane == 0) mbar_arrive(bar(&bars->go[masked % ST]));
+                                ++masked;
+                            }
+                        }
+                        if (ok && tk < sg.t1) ok = load(&tm_k, tk, t < sg.t0 ? (tk == sg.t0 ? id0 : id1) : (lead == 1 ? id1 : id2));
+                        if (ok && t == sg.t0 - 1) {
+                            ok = nseg == 0 || !lost(wait(&bars->q_empty, nseg - 1));
+                            if (ok && lane == 0) {
+                                const uint32_t qb = bar(&bars->q_full);
+                                const uint32_t bytes = (uint32_t)L::KB * TT * rep * 128;
+                                mbar_arrive_expect_tx(qb, si.dual ? 2 * bytes : bytes);
+                                for (int s = 0; s < (si.dual ? 2 : 1); ++s)
+                                    for (int kb = 0; kb < L::KB; ++kb)
+                                        tma_load_3d(sb + L::Q + s * L::TILE + kb * kBox, &tm_q, kb * 64, sg.head * rep,
+                                                    sg.row + s * TT, qb);
+                            }
+                            __syncwarp();
+                            nseg += ok;
+                        }
+                        if (t >= sg.t0) {
+                            id0 = id1;
+                            id1 = id2;
+                            id2 = page_of(t + 3);
+                        }
                     }
                 }
-                const int s0 = dual ? 0 : (next & 1), s1 = dual ? 1 : s0;
+                if (whole) {
+                    item = (int)gridDim.x + __shfl_sync(0xffffffffu, drawn, 0);
+                    any = item < items;
+                }
+            }
+            if (lane == 0 && pl.ok && whole) {
+                // The last CTA to finish drawing leaves the counter at zero for the next call.
+                __threadfence();
+                if (atomicAdd(&c.plan->done, 1) == (int)gridDim.x - 1) {
+                    c.plan->drawn = 0;
+                    c.plan->done = 0;
+                }
+            }
+            if (ok) {
+                Seg end = {};
+                give_seg(end);
+            }
+            // The last copies have landed, and been read unless the CTA gave up, before
+            // it ends.
+            const uint32_t tail = min(cnt, (uint32_t)ST);
+            const uint32_t never = bb + (uint32_t)offsetof(Bars, never);
+            for (uint32_t k = cnt - tail; k < cnt; ++k) wait_probes(bar(&bars->kv_full[k % ST]), (k / ST) & 1, never, c.err);
+            if (nseg > 0) wait_probes(bar(&bars->q_full), (nseg - 1) & 1, never, c.err);
+            for (uint32_t k = cnt - tail; k < cnt; ++k) wait(&bars->kv_empty[k % ST], k / ST);
+        } else if (warp == 1) {
+            // -------------------------------------------------------------- MMAs
+            // The ring's entries come in the order in which they are used: K of the first
+            // `lead` tiles, then V of tile i and K of tile i + lead in turn.
+            constexpr uint32_t idS = idesc_bf16_f32(128, 128);
+            constexpr uint32_t idO = idesc_bf16_f32(128, DH) | kIdescBMn;
+            const uint32_t tm = __shfl_sync(0xffffffffu, tbase, 0);
+            const uint64_t d_q = smem_desc_sw128(sb + L::Q), d_k = smem_desc_sw128(sb + L::RING);
+            const uint64_t d_v = smem_desc_sw128_mn(sb + L::RING, kBox);
+            constexpr uint32_t kTile16 = L::TILE >> 4;       // a tile in a descriptor's units
+            uint32_t stage = 0, phase = 0, masked = 0, p_phase = 0, gave_up = 0;   // p_phase: one bit per slot
+            auto entry = [&]() {                             // next ring entry, once it has landed
+                const uint32_t e = stage;
+                gave_up |= wait(&bars->kv_full[e], phase);
+                if (++stage == (uint32_t)ST) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+                return e;
+            };
+            Seg g;
+            for (int it = 0; !lost(gave_up) && next_seg(it, g); ++it) {
+                const SegInfo si = seg_info(g, TT, tree);
+                auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+                const int dual = uniform(si.dual), lead = dual ? 1 : 2, nt = uniform(g.t1 - g.t0);
+                const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
+                const int first_masked = uniform(si.kall / kCacheTile - g.t0);
+                gave_up |= wait(&bars->q_full, it);
+                // Step i: O += P V of tile i, S = Q K^T of tile i + lead, slot by slot, so that
+                // a slot's products run under the other slot's softmax.  (Given up: the waits
+                // return at once, the products' results are not used.)
+                uint32_t ev = 0, ek = 0;
+                auto pv = [&](int s, int half, bool began) {             // keys 64 half .. 64 half + 63
+                    const uint64_t va = d_v + ev * kTile16 + half * 4 * (2048 >> 4);
+                    const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128 + half * 32;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            tc_mma_bf16_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : (uint32_t)began);
+                        if (half == 0) tc_commit(bar(&bars->half_done[s]));
+                    }
+                };
+                auto qk = [&](int s, bool last) {            // last: of the slots that read this key tile
+                    const uint64_t qa = d_q + (dual ? s * kTile16 : 0u), ka = d_k + ek * kTile16;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = 0; kk < DH / 16; ++kk) {
+                            const uint32_t off = (kk >> 2) * (kBox >> 4) + (kk & 3) * (32 >> 4);
+                            tc_mma_bf16(tm + s * 128, qa + off, ka + off, idS, kk ? 1u : 0u);
+                        }
+                        tc_commit(bar(&bars->s_full[s]));
+                        if (last) tc_commit(bar(&bars->kv_empty[ek]));
+                    }
+                };
+                // Steps below `plain` of a two-tile segment need none of the cases.
+                const int plain = dual ? min(min(n0, n1) - 1, first_masked) : 0;
+                bool have_v = false;                         // V of step i has been waited for
 #pragma unroll 1
-                for (int s = s0; s <= s1; ++s) {
-                    const int ns = s ? n1 : n0;
-                    const bool here = i >= 0 && i < ns;
-                    if (here) {
-                        gave_up |= wait(&bars->p_half[s], p_phase >> s);
+                for (int i = -lead; i < nt; ++i) {
+                    if (i >= 0 && i < plain) {
+                        if (!have_v) ev = entry();
+                        gave_up |= wait(&bars->p_half[0], p_phase);
                         tc_fence_after();
-                        if (!bad) pv(s, 0, dual ? i > 0 : i > 1);    // else the softmax warps do it
-                        else if (elect_one()) tc_commit(bar(&bars->half_done[s]));
-                        gave_up |= wait(&bars->p_full[s], p_phase >> s);
-                        p_phase ^= 1u << s;
+                        pv(0, 0, i > 0);
+                        gave_up |= wait(&bars->p_full[0], p_phase);
                         tc_fence_after();
-                        if (!bad) pv(s, 1, true);
-                    }
-                    if (i >= 0 && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
-                    if (more && s == s0) {
+                        pv(0, 1, true);
                         ek = entry();
                         tc_fence_after();
+                        qk(0, false);
+                        gave_up |= wait(&bars->p_half[1], p_phase >> 1);
+                        tc_fence_after();
+                        pv(1, 0, i > 0);
+                        gave_up |= wait(&bars->p_full[1], p_phase >> 1);
+                        p_phase ^= 3u;
+                        tc_fence_after();
+                        pv(1, 1, true);
+                        if (elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
+                        ev = entry();                        // (step i + 1 exists) under the products queued
+                        have_v = true;
+                        qk(1, true);
+                        continue;
                     }
-                    if (more && next < ns) {
-                        qk(s, s == s1);
-                    } else {
-                        if (here && elect_one()) tc_commit(bar(&bars->o_full[s]));
-                        if (more && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ek]));
+                    const int next = i + lead;
+                    const bool more = next < nt;
+                    if (next == nt && elect_one()) tc_commit(bar(&bars->q_empty));    // no product reads the queries any more
+                    int bad = 0;
+                    if (i >= 0) {
+                        if (!have_v) ev = entry();
+                        have_v = false;
+                        if (i >= first_masked) {
+                            const uint32_t gs = masked % ST, gp = masked / ST;
+                            ++masked;
+                            gave_up |= wait(&bars->guard[gs], gp);
+                            bad = uniform(bars->bad[gs][0] | bars->bad[gs][1]);
+                        }
+                    }
+                    const int s0 = dual ? 0 : (next & 1), s1 = dual ? 1 : s0;
+#pragma unroll 1
+                    for (int s = s0; s <= s1; ++s) {
+                        const int ns = s ? n1 : n0;
+                        const bool here = i >= 0 && i < ns;
+                        if (here) {
+                            gave_up |= wait(&bars->p_half[s], p_phase >> s);
+                            tc_fence_after();
+                            if (!bad) pv(s, 0, dual ? i > 0 : i > 1);    // else the softmax warps do it
+                            else if (elect_one()) tc_commit(bar(&bars->half_done[s]));
+                            gave_up |= wait(&bars->p_full[s], p_phase >> s);
+                            p_phase ^= 1u << s;
+                            tc_fence_after();
+                            if (!bad) pv(s, 1, true);
+                        }
+                        if (i >= 0 && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ev]));
+                        if (more && s == s0) {
+                            ek = entry();
+                            tc_fence_after();
+                        }
+                        if (more && next < ns) {
+                            qk(s, s == s1);
+                        } else {
+                            if (here && elect_one()) tc_commit(bar(&bars->o_full[s]));
+                            if (more && s == s1 && elect_one()) tc_commit(bar(&bars->kv_empty[ek]));
+                        }
                     }
                 }
+                __syncwarp();
             }
-            __syncwarp();
-        }
-    } else {
-        // ------------------------------------------------------------ guards
-        // Values of partly masked tiles: rows that nobody sees become zeros, rows
-        // that some see are searched for infinities and NaN.
-        const int me = threadIdx.x - 64;                   // 0..63
-        uint32_t cnt = 0, masked = 0;
-        Seg g;
-        bool ok = true;
-        for (int it = 0; ok && next_seg(it, g); ++it) {
-            const SegInfo si = seg_info(g, TT, tree);
-            const int lead = si.dual ? 1 : 2, nt = g.t1 - g.t0;
-            for (int i = max(0, si.kall / kCacheTile - g.t0); ok && i < nt; ++i) {
-                const int t = g.t0 + i;
-                if ((t + 1) * kCacheTile <= si.kall) continue;
-                const uint32_t e = cnt + i + min(nt, i + lead);
-                // A parity names a phase only to who knows that the one before has passed: the
-                // load warp says when the entry's own phase has begun.
-                ok = !lost(wait(&bars->go[masked % ST], masked / ST) | wait(&bars->kv_full[e % ST], e / ST));
-                if (!ok) break;
-                uint8_t* v = smem + L::RING + (e % ST) * L::TILE;
-                const int lo = max(0, si.kall - t * kCacheTile), hi = max(0, min(kCacheTile, si.kmax - t * kCacheTile));
-                for (int x = hi * 8 + me; x < kCacheTile * 8; x += 64)
+        } else {
+            // ------------------------------------------------------------ guards
+            // Values of partly masked tiles: rows that nobody sees become zeros, rows
+            // that some see are searched for infinities and NaN.
+            const int me = threadIdx.x - 64;                   // 0..63
+            uint32_t cnt = 0, masked = 0;
+            Seg g;
+            bool ok = true;
+            for (int it = 0; ok && next_seg(it, g); ++it) {
+                const SegInfo si = seg_info(g, TT, tree);
+                const int lead = si.dual ? 1 : 2, nt = g.t1 - g.t0;
+                for (int i = max(0, si.kall / kCacheTile - g.t0); ok && i < nt; ++i) {
+                    const int t = g.t0 + i;
+                    if ((t + 1) * kCacheTile <= si.kall) continue;
+                    const uint32_t e = cnt + i + min(nt, i + lead);
+                    // A parity names a phase only to who knows that the one before has passed: the
+                    // load warp says when the entry's own phase has begun.
+                    ok = !lost(wait(&bars->go[masked % ST], masked / ST) | wait(&bars->kv_full[e % ST], e / ST));
+                    if (!ok) break;
+                    uint8_t* v = smem + L::RING + (e % ST) * L::TILE;
+                    const int lo = max(0, si.kall - t * kCacheTile), hi = max(0, min(kCacheTile, si.kmax - t * kCacheTile));
+                    for (int x = hi * 8 + me; x < kCacheTile * 8; x += 64)
 #pragma unroll
-                    for (int kb = 0; kb < L::KB; ++kb)
-                        *reinterpret_cast<uint4*>(v + kb * kBox + x * 16) = make_uint4(0, 0, 0, 0);
-                // x * 0 is NaN for an infinity or a NaN, and the sum keeps it.
-                __nv_bfloat162 sum = __floats2bfloat162_rn(0.f, 0.f);
-                const __nv_bfloat162 zero = sum;
+                        for (int kb = 0; kb < L::KB; ++kb)
+                            *reinterpret_cast<uint4*>(v + kb * kBox + x * 16) = make_uint4(0, 0, 0, 0);
+                    // x * 0 is NaN for an infinity or a NaN, and the sum keeps it.
+                    __nv_bfloat162 sum = __floats2bfloat162_rn(0.f, 0.f);
+                    const __nv_bfloat162 zero = sum;
 #pragma unroll 4
-                for (int x = lo * 8 + me; x < hi * 8; x += 64)
+                    for (int x = lo * 8 + me; x < hi * 8; x += 64)
 #pragma unroll
-                    for (int kb = 0; kb < L::KB; ++kb) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(v + kb * kBox + x * 16);
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                        for (int kb = 0; kb < L::KB; ++kb) {
+                            const uint4 u = *reinterpret_cast<const uint4*>(v + kb * kBox + x * 16);
+                            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            sum = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), zero, sum);
+                            for (int k = 0; k < 4; ++k)
+                                sum = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), zero, sum);
+                        }
+                    bool found = __hisnan(__low2bfloat16(sum)) || __hisnan(__high2bfloat16(sum));
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    found = __any_sync(0xffffffffu, found);
+                    if (lane == 0) {
+                        bars->bad[masked % ST][warp - 2] = found;
+                        mbar_arrive(bar(&bars->guard[masked % ST]));
                     }
-                bool found = __hisnan(__low2bfloat16(sum)) || __hisnan(__high2bfloat16(sum));
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                found = __any_sync(0xffffffffu, found);
-                if (lane == 0) {
-                    bars->bad[masked % ST][warp - 2] = found;
-                    mbar_arrive(bar(&bars->guard[masked % ST]));
+                    ++masked;
                 }
-                ++masked;
+                cnt += 2 * nt;
             }
-            cnt += 2 * nt;
         }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // -------------------------------------------------- softmax and output
@@ -907,11 +917,11 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         tmem_st_32x16(tS + 48, w);
                         tmem_st_wait();
                     } else {
-                    if (part) {
-                        hide(2);
-                        hide(3);
-                    }
-                    half_tile(1);
+                        if (part) {
+                            hide(2);
+                            hide(3);
+                        }
+                        half_tile(1);
                     }
                     if (bad) by_hand(1);
                 }
