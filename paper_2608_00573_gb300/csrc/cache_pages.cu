@@ -27,6 +27,27 @@ constexpr int kCopyVecs = 4;           // 16-byte vectors in flight per thread
 // 15.7 with three and more CTAs idle).
 constexpr int kMinTiles = 2;
 
+__device__ __forceinline__ int from_below(int v, int o) { return __shfl_up_sync(0xffffffffu, v, o); }
+__device__ __forceinline__ long long from_below(long long v, int o) { return __shfl_up_sync(0xffffffffu, v, o); }
+
+// Four sums scanned together.
+struct Sums {
+    int fresh, tok, group, cow;
+    Sums() = default;
+    __device__ explicit Sums(int v) : fresh(v), tok(v), group(v), cow(v) {}
+    __device__ Sums(int a, int b, int c, int d) : fresh(a), tok(b), group(c), cow(d) {}
+    __device__ Sums operator+(const Sums& o) const {
+        return Sums(fresh + o.fresh, tok + o.tok, group + o.group, cow + o.cow);
+    }
+    __device__ Sums operator-(const Sums& o) const {
+        return Sums(fresh - o.fresh, tok - o.tok, group - o.group, cow - o.cow);
+    }
+};
+__device__ __forceinline__ Sums from_below(const Sums& v, int o) {
+    return Sums(__shfl_up_sync(0xffffffffu, v.fresh, o), __shfl_up_sync(0xffffffffu, v.tok, o),
+                __shfl_up_sync(0xffffffffu, v.group, o), __shfl_up_sync(0xffffffffu, v.cow, o));
+}
+
 // Exclusive prefix sum over the block; every thread gets the total.  ws: 33 entries.
 template <class V>
 __device__ V block_scan(V v, V* ws, V& total) {
@@ -34,8 +55,8 @@ __device__ V block_scan(V v, V* ws, V& total) {
     V x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const V y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
+        const V y = from_below(x, o);
+        if (lane >= o) x = x + y;
     }
     if (lane == 31) ws[warp] = x;
     __syncthreads();
@@ -44,8 +65,8 @@ __device__ V block_scan(V v, V* ws, V& total) {
         const V own = s;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const V y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += y;
+            const V y = from_below(s, o);
+            if (lane >= o) s = s + y;
         }
         ws[lane] = s - own;
         if (lane == 31) ws[32] = s;
@@ -69,25 +90,30 @@ __device__ __forceinline__ int find_le(const V* off, int n, V x) {
     return lo;
 }
 
-// Free pages (ref == 0) in [from, to), ascending, the first `want` of them into
-// list; returns how many were written.  with_live: pages in use instead.
-__device__ int collect_pages(const int* ref, int from, int to, bool live, int want, int* list, int stride, int* ws) {
+// Which of a thread's four pages p0 .. p0 + 3 below `to` are free (live: in use), a bit each.
+__device__ __forceinline__ uint32_t four_pages(const int* ref, int p0, int to, bool live) {
+    uint32_t f = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (p0 + u < to && (ref[p0 + u] > 0) == live) f |= 1u << u;
+    return f;
+}
+
+// Free pages (ref == 0; live: pages in use instead) in [from, to), ascending: put(k, page)
+// for the first `want` of them; returns how many there were, up to that.  first: this
+// thread's four_pages() at from + 4 threadIdx.x, which the caller may read early.
+template <class Put>
+__device__ int collect_pages(const int* ref, int from, int to, bool live, int want, uint32_t first, int* ws, Put put) {
     int found = 0;
     for (int b = from; b < to && found < want; b += kStepThreads * 4) {
         const int p0 = b + threadIdx.x * 4;
-        bool f[4];
-        int cnt = 0;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            f[u] = p0 + u < to && (ref[p0 + u] > 0) == live;
-            cnt += f[u];
-        }
+        const uint32_t f = b == from ? first : four_pages(ref, p0, to, live);
         int total;
-        int at = found + block_scan(cnt, ws, total);
+        int at = found + block_scan(__popc(f), ws, total);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (f[u]) {
-                if (at < want) list[(size_t)at * stride] = p0 + u;
+            if (f >> u & 1u) {
+                if (at < want) put(at, p0 + u);
                 ++at;
             }
         found += total;
@@ -101,20 +127,26 @@ __device__ int collect_pages(const int* ref, int from, int to, bool live, int wa
 template <int N>
 __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_constant__ CacheDev c,
                                                                   const __grid_constant__ CacheList<N> l) {
-    __shared__ int s_pages[kCacheMaxSeqs + 1], s_groups[kCacheMaxSeqs + 1];
-    __shared__ int s_len[kCacheMaxSeqs], s_last[kCacheMaxSeqs], s_cow[kCacheMaxSeqs];
+    __shared__ int s_seq[kCacheMaxSeqs], s_q[kCacheMaxSeqs], s_len[kCacheMaxSeqs], s_last[kCacheMaxSeqs];
+    __shared__ int s_pages[kCacheMaxSeqs], s_tok[kCacheMaxSeqs], s_groups[kCacheMaxSeqs], s_cow[kCacheMaxSeqs];
+    __shared__ int s_fresh[kStepThreads];
     __shared__ long long s_pre[kStepThreads], s_wsl[33];
-    __shared__ int s_ws[33], s_bad, s_most, s_bucket[kStepThreads];
+    __shared__ Sums s_wss[33];
+    __shared__ int s_ws[33], s_bad, s_most;
+    const int i = threadIdx.x, n = l.n, TT = c.tile_tokens;
+    int q = 0, seq = 0;
+    if (i < n) {
+        s_seq[i] = seq = l.a[i];
+        s_q[i] = q = l.b[i];
+    }
+    if (i == 0) s_bad = s_most = 0;
     pdl_wait();
     pdl_trigger();
-    const int i = threadIdx.x, n = l.n, TT = c.tile_tokens;
-    if (i == 0) s_bad = 0;
+    const uint32_t free4 = four_pages(c.ref, i * 4, c.n_pages, false);      // (on its way beside the lengths)
+    int len = i < n ? c.length[seq] : 0;
     __syncthreads();
-    int len = 0, q = 0, seq = 0, had = 0, last = -1, cow = 0, fresh = 0;
+    int had = 0, last = -1, cow = 0, fresh = 0;
     if (i < n) {
-        seq = l.a[i];
-        q = l.b[i];
-        len = c.length[seq];
         if (len < 0 || len > (long long)c.max_pages * c.page) {
             s_bad = ERR_CACHE_STATE;
             len = 0;
@@ -132,24 +164,26 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
         cow = q > 0 && (len & (c.page - 1)) && last >= 0 && c.ref[last] > 1;
         fresh = (int)min(need - had, (long long)c.max_pages) + cow;
     }
-    int n_fresh, T, n_groups, n_cow;
-    const int at_page = block_scan(fresh, s_ws, n_fresh);
-    const int at_tok = block_scan(q, s_ws, T);
-    const int at_group = block_scan((q + 2 * TT - 1) / (2 * TT), s_ws, n_groups);
-    const int at_cow = block_scan(cow, s_ws, n_cow);
+    Sums sum;
+    const Sums at = block_scan(Sums(fresh, q, (q + 2 * TT - 1) / (2 * TT), cow), s_wss, sum);
+    const int n_fresh = sum.fresh, n_groups = sum.group;
     if (i < n) {
-        s_pages[i] = at_page;
-        s_groups[i] = at_group;
+        s_pages[i] = at.fresh;
+        s_tok[i] = at.tok;
+        s_groups[i] = at.group;
         s_len[i] = len;
         s_last[i] = last;
-        s_cow[i] = cow ? at_cow : -1;
+        s_cow[i] = cow ? at.cow : -1;
     }
     __syncthreads();
-    if (!s_bad) {
-        const int found = collect_pages(c.ref, 0, c.n_pages, false, n_fresh, c.fresh, 1, s_ws);
+    if (!s_bad && n_fresh > 0) {
+        // (Shared memory holds as many as it has room for.)
+        const int found = collect_pages(c.ref, 0, c.n_pages, false, n_fresh, free4, s_ws, [&](int k, int page) {
+            (k < kStepThreads ? s_fresh : c.fresh)[k] = page;
+        });
         if (found < n_fresh && i == 0) s_bad = ERR_CACHE_FULL;
+        __syncthreads();
     }
-    __syncthreads();
     if (s_bad) {
         if (i == 0) {
             *c.plan = CachePlan{};
@@ -160,7 +194,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     // Pages: the k-th taken page belongs to the sequence whose range holds k.
     for (int k = i; k < n_fresh; k += kStepThreads) {
         const int s = find_le(s_pages, n, k);
-        const int id = c.fresh[k];
+        const int id = (k < kStepThreads ? s_fresh : c.fresh)[k];
         const int copied = s_cow[s] >= 0;
         const int first = (int)(((long long)s_len[s] + c.page - 1) >> c.page_shift) - copied;
         const int j = first + k - s_pages[s];
@@ -168,26 +202,23 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
             c.copies[s_cow[s]] = make_int2(s_last[s], id);
             atomicSub(&c.ref[s_last[s]], 1);
         }
-        c.table[(size_t)l.a[s] * c.max_pages + j] = id;
+        c.table[(size_t)s_seq[s] * c.max_pages + j] = id;
         c.ref[id] = 1;
     }
     if (i < n) {
         c.length[seq] = len + q;
         c.base[seq] = len;
-        c.seqs[i] = CacheSeq{seq, at_tok, q, len + q};
+        c.seqs[i] = CacheSeq{seq, at.tok, q, len + q};
     }
-    __syncthreads();   // s_pages has been read: it takes the token offsets
-    if (i < n) s_pages[i] = at_tok;
-    __syncthreads();
     // The work list.  Groups are numbered in the order of the sequences; when whole
     // items will be drawn (below), they are stored longest first.
     auto group_of = [&](int r) {
         CacheGroup g;
         const int s = find_le(s_groups, n, r);
-        const int q_len = l.b[s], tok = (r - s_groups[s]) * 2 * TT;
-        g.seq = l.a[s];
+        const int q_len = s_q[s], tok = (r - s_groups[s]) * 2 * TT;
+        g.seq = s_seq[s];
         g.kv_len = s_len[s] + q_len;
-        g.row = s_pages[s] + tok;
+        g.row = s_tok[s] + tok;
         g.ntok = min(2 * TT, q_len - tok);
         g.first = s_len[s] + tok;
         g.base = s_len[s];
@@ -195,35 +226,42 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
         g.pre = 0;
         return g;
     };
+    const bool few = n_groups <= kStepThreads;           // a thread has one group at most
+    CacheGroup mine;
     long long cost = 0, total;
     int most = 0, two = 0;
     for (int r = i; r < n_groups; r += kStepThreads) {
-        const CacheGroup g = group_of(r);
-        cost += g.cost;
-        most = max(most, g.cost);
-        two |= cache_two_tiles(g.ntok, TT);
+        mine = group_of(r);
+        cost += mine.cost;
+        most = max(most, mine.cost);
+        two |= cache_two_tiles(mine.ntok, TT);
     }
-    block_scan(cost, s_wsl, total);
-    if (i == 0) s_most = 0;
-    two = __syncthreads_or(two);
     if (i < n_groups) atomicMax(&s_most, most);
-    __syncthreads();
+    const long long before_mine = block_scan(cost, s_wsl, total);
+    two = __syncthreads_or(two);
     const long long W = total * c.Hkv;
     const bool whole = 2LL * s_most * c.num_sms <= W;
     const int n_ctas = !W || whole ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles << (two ? 1 : 0))));
     if (whole) {
         // Counting sort by cost, costs past the last bucket together in the first one.
-        if (i < kStepThreads) s_bucket[i] = 0;
+        auto bucket = [](int cost) { return max(0, kStepThreads - 1 - cost); };
+        int* s_bucket = s_fresh;                         // (the pages have been given out)
+        s_bucket[i] = 0;
         __syncthreads();
-        for (int r = i; r < n_groups; r += kStepThreads) atomicAdd(&s_bucket[max(0, kStepThreads - 1 - group_of(r).cost)], 1);
+        for (int r = i; r < n_groups; r += kStepThreads) atomicAdd(&s_bucket[bucket(few ? mine.cost : group_of(r).cost)], 1);
         __syncthreads();
         int all;
-        const int at = block_scan(s_bucket[i], s_ws, all);
-        s_bucket[i] = at;
+        const int start = block_scan(s_bucket[i], s_ws, all);
+        s_bucket[i] = start;
         __syncthreads();
         for (int r = i; r < n_groups; r += kStepThreads) {
-            const CacheGroup g = group_of(r);
-            c.groups[atomicAdd(&s_bucket[max(0, kStepThreads - 1 - g.cost)], 1)] = g;
+            const CacheGroup g = few ? mine : group_of(r);
+            c.groups[atomicAdd(&s_bucket[bucket(g.cost)], 1)] = g;
+        }
+    } else if (few) {
+        if (i < n_groups) {
+            mine.pre = s_pre[i] = before_mine;
+            c.groups[i] = mine;
         }
     } else {
         long long before = 0;
@@ -231,25 +269,26 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
             const int r = b + i;
             CacheGroup g;
             if (r < n_groups) g = group_of(r);
-            long long sum;
-            const long long pre = before + block_scan(r < n_groups ? (long long)g.cost : 0LL, s_wsl, sum);
+            long long part;
+            const long long pre = before + block_scan(r < n_groups ? (long long)g.cost : 0LL, s_wsl, part);
             if (r < n_groups) {
                 g.pre = pre;
                 c.groups[r] = g;
-                if (n_groups <= kStepThreads) s_pre[r] = pre;
             }
-            before += sum;
+            before += part;
         }
     }
-    if (i == 0) *c.plan = CachePlan{W, n_groups, n_ctas, n_cow, 1, 0, 0};
+    if (i == 0) *c.plan = CachePlan{W, n_groups, n_ctas, sum.cow, 1, 0, 0};
     __syncthreads();
     for (int b = i; b < n_ctas; b += kStepThreads) {
         CacheShare sh;
         sh.begin = W * b / n_ctas;
         sh.end = W * (b + 1) / n_ctas;
         const long long x = sh.begin / c.Hkv;
-        if (n_groups <= kStepThreads) {
+        if (few) {
             sh.group = find_le(s_pre, n_groups, x);
+            sh.g = group_of(sh.group);
+            sh.g.pre = s_pre[sh.group];
         } else {
             int lo = 0, hi = n_groups;
             while (hi - lo > 1) {
@@ -258,8 +297,8 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
                 else hi = m;
             }
             sh.group = lo;
+            sh.g = c.groups[lo];
         }
-        sh.g = c.groups[sh.group];
         sh.within = sh.begin - sh.g.pre * c.Hkv;
         sh.head = (int)(sh.within / sh.g.cost);
         sh.within -= (long long)sh.head * sh.g.cost;
@@ -376,10 +415,11 @@ __global__ void __launch_bounds__(256) cache_cut_kernel(const __grid_constant__ 
     }
 }
 
-// Moves the accepted drafts to the front.  dh / 8 lanes take the rows of one
-// (sequence, layer, K or V, head), each lane its own 16 bytes of every row, in
-// the order of the path: row e is written after rows e .. e + 3 were read, and
-// later rows come from behind (path[e] >= e), so rows may overlap.
+// Moves the accepted drafts to the front.  dh / 8 lanes take the K and V rows of one
+// (sequence, layer, head), each lane its own 16 bytes of every row, in the order of the
+// path: row e is written after rows e .. e + 3 were read, and later rows come from
+// behind (path[e] >= e), so rows may overlap.  Lane e looks up the e-th row's pages once,
+// for the check and for the move (and again for paths longer than the lanes).
 template <int N>
 __global__ void __launch_bounds__(256) cache_accept_kernel(const __grid_constant__ CacheDev c,
                                                            const __grid_constant__ CacheList<N> l, const int* n_acc,
@@ -389,61 +429,84 @@ __global__ void __launch_bounds__(256) cache_accept_kernel(const __grid_constant
     const int lanes = c.dh >> 3;                 // 8 or 16, a divisor of the warp
     const int lane = threadIdx.x & 31, sub = lane & (lanes - 1);
     const uint32_t mask = (lanes == 16 ? 0xffffu : 0xffu) << (lane & ~(lanes - 1));
-    const long long units = (long long)l.n * c.layers * 2 * c.Hkv;
+    const long long units = (long long)l.n * c.layers * c.Hkv;
     const long long per = 256 / lanes;
     const size_t page_elems = (size_t)c.Hkv * c.page * c.dh;
     for (long long u0 = blockIdx.x * per; u0 < units; u0 += gridDim.x * per) {
         const long long u = u0 + threadIdx.x / lanes;
         bool ok = true;
-        int i = 0, h = 0, kv = 0, layer = 0, seq = 0, base = 0, n = 0;
-        const int* mine = path;
+        int i = 0, h = 0, layer = 0, base = 0, n = 0;
+        const int *mine = path, *table = c.table;
+        int from = 0, from_id = 0, to_id = 0;    // of row e0 + sub
         if (u < units) {
             h = (int)(u % c.Hkv);
-            const long long v = u / c.Hkv;
-            kv = (int)(v & 1);
-            layer = (int)((v >> 1) % c.layers);
-            i = (int)((v >> 1) / c.layers);
-            seq = l.a[i];
+            layer = (int)(u / c.Hkv % c.layers);
+            i = (int)(u / c.Hkv / c.layers);
+            const int seq = l.a[i];
             base = c.base[seq];
             const int drafts = c.length[seq] - base;
             n = n_acc[i];
             mine = path + (size_t)i * ld_path;
+            table = c.table + (size_t)seq * c.max_pages;
             if (base < 0 || drafts < 0 || (long long)base + drafts > (long long)c.max_pages * c.page || n < 0 ||
                 n > min(min(drafts, kTreeMax), ld_path)) {
                 ok = false;
                 n = 0;
             }
             for (int e = sub; e < n; e += lanes) {
-                const int from = mine[e];
-                ok &= from >= 0 && from < drafts && (e == 0 || from > mine[e - 1]);
-                const int to_id = c.table[(size_t)seq * c.max_pages + ((base + e) >> c.page_shift)];
-                ok &= to_id >= 0 && to_id < c.n_pages && c.ref[to_id] == 1;
-                if (ok) {
-                    const int id = c.table[(size_t)seq * c.max_pages + ((base + from) >> c.page_shift)];
-                    ok &= id >= 0 && id < c.n_pages;
+                const int f = mine[e], before = e ? mine[e - 1] : -1;
+                const int t = table[(base + e) >> c.page_shift];
+                bool fits = f > before && f < drafts && t >= 0 && t < c.n_pages;
+                if (fits) {
+                    const int id = table[(base + f) >> c.page_shift];
+                    fits = id >= 0 && id < c.n_pages && c.ref[t] == 1;
+                    if (e == sub) {
+                        from = f;
+                        from_id = id;
+                        to_id = t;
+                    }
                 }
+                ok &= fits;
             }
         }
         ok = (__ballot_sync(0xffffffffu, !ok) & mask) == 0;
-        if (u >= units) continue;
-        if (layer == 0 && kv == 0 && h == 0 && sub == 0) {
+        if (u < units && layer == 0 && h == 0 && sub == 0) {
             accepted[i] = ok ? base + n : -1;
             if (!ok) atomicCAS(c.err, 0, ERR_CACHE_PATH);
         }
-        if (!ok) continue;
-        __nv_bfloat16* pool = (kv ? c.v : c.k) + ((size_t)layer * c.n_pages) * page_elems + (size_t)h * c.page * c.dh;
-        auto row = [&](int p) {
-            const int id = c.table[(size_t)seq * c.max_pages + (p >> c.page_shift)];
-            return reinterpret_cast<uint4*>(pool + (size_t)id * page_elems + (size_t)(p & (c.page - 1)) * c.dh) + sub;
-        };
-        for (int e0 = 0; e0 < n; e0 += 4) {
-            uint4 r[4];
+        if (!ok) n = 0;
+        const size_t off = (size_t)layer * c.n_pages * page_elems + (size_t)h * c.page * c.dh + sub * 8;
+        for (int e0 = 0; e0 < n; e0 += lanes) {    // (n is the same for the unit's lanes)
+            if (e0 && e0 + sub < n) {
+                from = mine[e0 + sub];
+                from_id = table[(base + from) >> c.page_shift];
+                to_id = table[(base + e0 + sub) >> c.page_shift];
+            }
+            for (int e1 = 0; e1 < lanes && e0 + e1 < n; e1 += 4) {
+                uint4 rk[4], rv[4];
+                size_t to[4];
+                bool moves[4];
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                if (e0 + w < n && mine[e0 + w] != e0 + w) r[w] = *row(base + mine[e0 + w]);
+                for (int w = 0; w < 4; ++w) {
+                    const int e = e0 + e1 + w, at = e1 + w;
+                    const int f = __shfl_sync(mask, from, at, lanes);
+                    const size_t src = __shfl_sync(mask, from_id, at, lanes) * page_elems +
+                                       (size_t)((base + f) & (c.page - 1)) * c.dh;
+                    to[w] = off + __shfl_sync(mask, to_id, at, lanes) * page_elems +
+                            (size_t)((base + e) & (c.page - 1)) * c.dh;
+                    moves[w] = e < n && f != e;
+                    if (moves[w]) {
+                        rk[w] = *reinterpret_cast<const uint4*>(c.k + off + src);
+                        rv[w] = *reinterpret_cast<const uint4*>(c.v + off + src);
+                    }
+                }
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                if (e0 + w < n && mine[e0 + w] != e0 + w) *row(base + e0 + w) = r[w];
+                for (int w = 0; w < 4; ++w)
+                    if (moves[w]) {
+                        *reinterpret_cast<uint4*>(c.k + to[w]) = rk[w];
+                        *reinterpret_cast<uint4*>(c.v + to[w]) = rv[w];
+                    }
+            }
         }
     }
 }
@@ -457,8 +520,11 @@ __global__ void __launch_bounds__(kStepThreads) cache_compact_kernel(const __gri
     int mine = 0, live;
     for (int p = threadIdx.x; p < c.n_pages; p += kStepThreads) mine += c.ref[p] > 0;
     block_scan(mine, s_ws, live);
-    const int holes = collect_pages(c.ref, 0, live, false, live, &c.copies[0].y, 2, s_ws);
-    const int movers = collect_pages(c.ref, live, c.n_pages, true, holes, &c.copies[0].x, 2, s_ws);
+    const int mine4 = threadIdx.x * 4;
+    const int holes = collect_pages(c.ref, 0, live, false, live, four_pages(c.ref, mine4, live, false), s_ws,
+                                    [&](int k, int page) { c.copies[k].y = page; });
+    const int movers = collect_pages(c.ref, live, c.n_pages, true, holes, four_pages(c.ref, live + mine4, c.n_pages, true),
+                                     s_ws, [&](int k, int page) { c.copies[k].x = page; });
     __syncthreads();
     for (int k = threadIdx.x; k < movers; k += kStepThreads) c.fresh[c.copies[k].x] = c.copies[k].y;
     if (threadIdx.x == 0) *c.plan = CachePlan{live, 0, 0, movers, 0, 0, 0};
@@ -544,7 +610,7 @@ cudaError_t accept_launch(const CacheDev& c, int n, const int* seq, const int* n
                           cudaStream_t st) {
     int* accepted = reinterpret_cast<int*>(c.copies);
     const CacheList<N> l = list_of<N>(n, seq, nullptr);
-    const long long per = 256 / (c.dh / 8), units = (long long)n * c.layers * 2 * c.Hkv;
+    const long long per = 256 / (c.dh / 8), units = (long long)n * c.layers * c.Hkv;
     const dim3 grid((unsigned)std::min<long long>((units + per - 1) / per, c.num_sms * 16));
     cudaError_t e = launch_pdl(cache_accept_kernel<N>, grid, dim3(256), 0, st, c, l, n_acc, path, ld_path, accepted);
     if (e != cudaSuccess) return e;
