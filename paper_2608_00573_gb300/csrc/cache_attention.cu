@@ -140,8 +140,10 @@ __device__ __forceinline__ uint32_t wait_probes(uint32_t bar, uint32_t parity, u
     uint32_t gave_up;
     asm volatile(
         "{\n\t.reg .pred p;\n\t.reg .b32 n, a;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "mov.b32 n, 0;\n\t"
         "mov.b32 %0, 0;\n\t"
+        "@p bra DONE;\n\t"
         "PROBE:\n\t"
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
         "@p bra DONE;\n\t"
