@@ -175,6 +175,29 @@ __device__ __forceinline__ bool elect_one() {
     return pred != 0;
 }
 
+// Products with the descriptors' upper words as constants (the lower ones, address and
+// leading offset, take no carry): less to issue per product than 64-bit sums, on the warp
+// that all others wait for (16384-token prompt 1.50 -> 1.47 ms).
+constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;   // of smem_desc_sw128 and smem_desc_sw128_mn
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
+        : "memory");
+}
+
 // Waits for the TMEM loads in flight; x, one of their results, is not used before.
 __device__ __forceinline__ void landed(uint32_t (&x)[32]) {
     tmem_ld_wait();
@@ -248,70 +271,68 @@ __device__ __noinline__ void pv_by_hand(uint32_t tS, uint32_t tO, const uint8_t*
     tmem_st_wait();
 }
 
-// Joins R rows of a cut item from the parts of CTAs first .. last, in the order of the
-// keys; a lane takes D / 32 columns, B sources are read at a time.  CTA `first` wrote its
-// part into its second buffer, the others into their first; with `halves` each part has
-// two sources, from the two slots.
-// Bound: latency (one or two rounds of reads), and L2 for prompts' items.
-template <int DH, int R, int B>
-__device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams& p, int token0, int head, int rows,
-                                          int halves, int first, int last, int r0, int lane) {
-    constexpr int V = DH / 32;
+// Part buffers hold 32 rows of 4 columns side by side, so that the threads of a warp, a row
+// each, write whole lines (with a row's columns side by side a 777-token prompt took 18.0 us
+// instead of 15.3, 24 drafted trees 96 instead of 91).
+template <int DH>
+__device__ __forceinline__ size_t part_at(size_t buf, int row, int col) {
+    return (buf * 256 + (row & ~31)) * DH + (size_t)(col >> 2) * 128 + (row & 31) * 4 + (col & 3);
+}
+
+// Joins 8 rows of a cut item, G times 16 columns of them, from the parts of CTAs first ..
+// last, in the order of the keys; a lane has a row and 4 columns of each 16, B sources are
+// read at a time.  CTA `first` wrote its part into its second buffer, the others into
+// their first; with `halves` each part has two sources, from the two slots.
+// Bound: latency (one or two rounds of reads), and L2 for prompts' items.  (Seldom run, so a
+// function of its own.)
+template <int DH, int G, int B>
+__device__ __noinline__ void join_rows(const CacheDev& c, const AttendParams& p, int token0, int head, int rows,
+                                          int halves, int first, int last, int r0, int k0, int lane) {
     const int sources = (last - first + 1) << halves;
-    float top[R], l[R], acc[R][V];
+    const int r = r0 + (lane & 7), rr = min(r, rows - 1), col = k0 + (lane >> 3) * 4;
+    float top = -INFINITY, l = 0.f, acc[G][4];
 #pragma unroll
-    for (int q = 0; q < R; ++q) {
-        top[q] = -INFINITY;
-        l[q] = 0.f;
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[q][j] = 0.f;
-    }
+        for (int j = 0; j < 4; ++j) acc[g][j] = 0.f;
 #pragma unroll 1
     for (int s0 = 0; s0 < sources; s0 += B) {
-        float2 ml[B][R];
-        float o[B][R][V];
+        float2 ml[B];
+        float4 o[B][G];
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             const int s = min(s0 + i, sources - 1), k = s >> halves;
-            const int buf = k == 0 ? 2 * first + 1 : 2 * (first + k);
+            const size_t buf = k == 0 ? 2 * first + 1 : 2 * (first + k);
+            const int row = (s & halves) * 128 + rr;
+            ml[i] = __ldcg(c.part_ml + buf * 256 + row);
 #pragma unroll
-            for (int q = 0; q < R; ++q) {
-                const size_t row = (size_t)buf * 256 + (s & halves) * 128 + min(r0 + q, rows - 1);
-                const float* src = c.part_o + row * DH + lane * V;
-                ml[i][q] = __ldcg(c.part_ml + row);
-                if (V == 4) {
-                    const float4 f = __ldcg(reinterpret_cast<const float4*>(src));
-                    o[i][q][0] = f.x, o[i][q][1] = f.y, o[i][q][V - 2] = f.z, o[i][q][V - 1] = f.w;
-                } else {
-                    const float2 f = __ldcg(reinterpret_cast<const float2*>(src));
-                    o[i][q][0] = f.x, o[i][q][1] = f.y;
-                }
-            }
+            for (int g = 0; g < G; ++g)
+                o[i][g] = __ldcg(reinterpret_cast<const float4*>(c.part_o + part_at<DH>(buf, row, col + 16 * g)));
         }
 #pragma unroll
-        for (int i = 0; i < B; ++i)
+        for (int i = 0; i < B; ++i) {
+            const bool there = s0 + i < sources && ml[i].x != -INFINITY;       // else nothing was summed
+            const float m = there ? fmaxf(top, ml[i].x) : top, ref = m == -INFINITY ? 0.f : m;
+            const float fa = ex2(top - ref), fb = ex2(ml[i].x - ref);
+            top = m;
+            l = there ? l * fa + ml[i].y * fb : l;
 #pragma unroll
-            for (int q = 0; q < R; ++q) {
-                const bool there = s0 + i < sources && ml[i][q].x != -INFINITY;   // else nothing was summed
-                const float m = there ? fmaxf(top[q], ml[i][q].x) : top[q], ref = m == -INFINITY ? 0.f : m;
-                const float fa = ex2(top[q] - ref), fb = ex2(ml[i][q].x - ref);
-                top[q] = m;
-                l[q] = there ? l[q] * fa + ml[i][q].y * fb : l[q];
+            for (int g = 0; g < G; ++g) {
+                const float x[4] = {o[i][g].x, o[i][g].y, o[i][g].z, o[i][g].w};
 #pragma unroll
-                for (int j = 0; j < V; ++j) acc[q][j] = there ? acc[q][j] * fa + o[i][q][j] * fb : acc[q][j];
+                for (int j = 0; j < 4; ++j) acc[g][j] = there ? acc[g][j] * fa + x[j] * fb : acc[g][j];
             }
+        }
     }
+    const int tile = r >> 7, in = r & 127;
+    if (r >= rows || in >= c.tile_tokens * c.rep) return;
+    const int token = token0 + tile * c.tile_tokens + in / c.rep, h = head * c.rep + in % c.rep;
+    const float il = l == 0.f ? 0.f : 1.f / l;
+    __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + col;
 #pragma unroll
-    for (int q = 0; q < R; ++q) {
-        const int r = r0 + q, tile = r >> 7, in = r & 127;
-        if (r >= rows || in >= c.tile_tokens * c.rep) continue;
-        const int token = token0 + tile * c.tile_tokens + in / c.rep, h = head * c.rep + in % c.rep;
-        const float il = l[q] == 0.f ? 0.f : 1.f / l[q];
-        __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + lane * V;
-#pragma unroll
-        for (int j = 0; j < V; j += 2)
-            *reinterpret_cast<uint32_t*>(out + j) = pack_bf16x2(acc[q][j] * il, acc[q][j + 1] * il);
-    }
+    for (int g = 0; g < G; ++g)
+        *reinterpret_cast<uint2*>(out + 16 * g) = make_uint2(pack_bf16x2(acc[g][0] * il, acc[g][1] * il),
+                                                             pack_bf16x2(acc[g][2] * il, acc[g][3] * il));
 }
 
 template <int DH>
@@ -558,8 +579,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             constexpr uint32_t idS = idesc_bf16_f32(128, 128);
             constexpr uint32_t idO = idesc_bf16_f32(128, DH) | kIdescBMn;
             const uint32_t tm = __shfl_sync(0xffffffffu, tbase, 0);
-            const uint64_t d_q = smem_desc_sw128(sb + L::Q), d_k = smem_desc_sw128(sb + L::RING);
-            const uint64_t d_v = smem_desc_sw128_mn(sb + L::RING, kBox);
+            const uint32_t d_q = (uint32_t)smem_desc_sw128(sb + L::Q), d_k = (uint32_t)smem_desc_sw128(sb + L::RING);
+            const uint32_t d_v = (uint32_t)smem_desc_sw128_mn(sb + L::RING, kBox);
             constexpr uint32_t kTile16 = L::TILE >> 4;       // a tile in a descriptor's units
             uint32_t stage = 0, phase = 0, masked = 0, p_phase = 0, gave_up = 0;   // p_phase: one bit per slot
             auto entry = [&]() {                             // next ring entry, once it has landed
@@ -584,22 +605,22 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 // return at once, the products' results are not used.)
                 uint32_t ev = 0, ek = 0;
                 auto pv = [&](int s, int half, bool began) {             // keys 64 half .. 64 half + 63
-                    const uint64_t va = d_v + ev * kTile16 + half * 4 * (2048 >> 4);
+                    const uint32_t va = d_v + ev * kTile16 + half * 4 * (2048 >> 4);
                     const uint32_t to = tm + 256 + s * DH, tp = tm + s * 128 + half * 32;
                     if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
-                            tc_mma_bf16_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : (uint32_t)began);
+                            mma_ts(to, tp + kk * 8, va + kk * (2048 >> 4), idO, kk ? 1u : (uint32_t)began);
                         if (half == 0) tc_commit(bar(&bars->half_done[s]));
                     }
                 };
                 auto qk = [&](int s, bool last) {            // last: of the slots that read this key tile
-                    const uint64_t qa = d_q + (dual ? s * kTile16 : 0u), ka = d_k + ek * kTile16;
+                    const uint32_t qa = d_q + (dual ? s * kTile16 : 0u), ka = d_k + ek * kTile16;
                     if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < DH / 16; ++kk) {
                             const uint32_t off = (kk >> 2) * (kBox >> 4) + (kk & 3) * (32 >> 4);
-                            tc_mma_bf16(tm + s * 128, qa + off, ka + off, idS, kk ? 1u : 0u);
+                            mma_ss(tm + s * 128, qa + off, ka + off, idS, kk ? 1u : 0u);
                         }
                         tc_commit(bar(&bars->s_full[s]));
                         if (last) tc_commit(bar(&bars->kv_empty[ek]));
@@ -968,9 +989,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 float* po = nullptr;
                 __nv_bfloat16* out = nullptr;
                 if (g.part >= 0) {
-                    const size_t row = (size_t)g.part * 256 + (dual || apart ? slot * 128 : 0) + r;
-                    po = c.part_o + row * DH;
-                    if (mine && !(joins && slot)) c.part_ml[row] = make_float2(work ? m : -INFINITY, l);
+                    const int row = (dual || apart ? slot * 128 : 0) + r;
+                    po = c.part_o + part_at<DH>(g.part, row, 0);
+                    if (mine && !(joins && slot)) c.part_ml[(size_t)g.part * 256 + row] = make_float2(work ? m : -INFINITY, l);
                 } else {
                     out = p.out + (size_t)token * p.ld_out + (size_t)(g.head * rep + r - tok_in_tile * rep) * DH;
                     const float il = l == 0.f ? 0.f : 1.f / l;
@@ -996,7 +1017,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         if (po) {
 #pragma unroll
                             for (int j = 0; j < 16; j += 4)
-                                *reinterpret_cast<float4*>(po + k + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+                                *reinterpret_cast<float4*>(po + (k + j) * 32) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
                         } else {
 #pragma unroll
                             for (int j = 0; j < 16; j += 8)
@@ -1036,8 +1057,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (!ok) break;
                 ph ^= kPhJ;
                 if (bars->last_part)
-                    for (int r0 = warp - 4; r0 < g.ntok * rep; r0 += 8)
-                        join_rows<DH, 1, 8>(c, p, g.row, g.head, g.ntok * rep, 1, first, last, r0, lane);
+                    for (int u = warp - 4; u < (g.ntok * rep + 7) / 8 * (DH / 16); u += 8)
+                        join_rows<DH, 1, 8>(c, p, g.row, g.head, g.ntok * rep, 1, first, last, u / (DH / 16) * 8,
+                                            u % (DH / 16) * 16, lane);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(&bars->seg_empty[it % kSegSlots]));
@@ -1052,7 +1074,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 }
 
 // Joins the parts of cut items.  Block (b, y) takes rows [32 y, 32 y + 32) of the
-// item that CTA b of the attention began and did not finish, a warp four of them.
+// item that CTA b of the attention began and did not finish, a warp half of the columns
+// of eight of them.
 template <int DH>
 __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__ CacheDev c,
                                                          const __grid_constant__ AttendParams p) {
@@ -1064,9 +1087,10 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
     if (next.within == 0 || next.first != b || next.last == b) return;
     const int two = cache_two_tiles(next.g.ntok, c.tile_tokens);
     const int rows = two ? 128 + (next.g.ntok - c.tile_tokens) * c.rep : next.g.ntok * c.rep;
-    const int r0 = blockIdx.y * 32 + (threadIdx.x >> 5) * 4;
+    const int warp = threadIdx.x >> 5, r0 = blockIdx.y * 32 + (warp >> 1) * 8;
     if (r0 < rows)
-        join_rows<DH, 4, 2>(c, p, next.g.row, next.head, rows, 0, b, next.last, r0, threadIdx.x & 31);
+        join_rows<DH, DH / 32, 2>(c, p, next.g.row, next.head, rows, 0, b, next.last, r0, (warp & 1) * (DH / 2),
+                                  threadIdx.x & 31);
 }
 
 static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
