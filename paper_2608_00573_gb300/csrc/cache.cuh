@@ -88,7 +88,7 @@ struct CacheDev {
     int* base;                         // [max_seqs] length before the sequence's last step
     // Parts of cut items: two buffers per CTA, for the item that its share begins in and
     // the one that it ends in; rows 0..127 and 128..255 from the two slots.
-    float* part_o;                     // [2 num_sms][8][dh / 4][32][4] sums of p v, 32 rows at a time
+    float* part_o;                     // [2 num_sms][256][dh] sums of p v (order within: cache_attention.cu)
     float2* part_ml;                   // [2 num_sms][256] row maxima and sums of p
     int* arrived;                      // [num_sms] parts written of the item that a CTA began, 0 between calls
     int* err;

@@ -271,25 +271,82 @@ __device__ __noinline__ void pv_by_hand(uint32_t tS, uint32_t tO, const uint8_t*
     tmem_st_wait();
 }
 
-// Part buffers hold 32 rows of 4 columns side by side, so that the threads of a warp, a row
-// each, write whole lines (with a row's columns side by side a 777-token prompt took 18.0 us
-// instead of 15.3, 24 drafted trees 96 instead of 91).
+// Parts that a second kernel joins hold 32 rows of 4 columns side by side, so that the
+// threads of a warp, a row each, write whole lines (with a row's columns side by side a
+// 777-token prompt took 18.0 us instead of 15.3, 24 drafted trees 96 instead of 91).  Those
+// that the writing CTAs join have few rows: there a row's columns are side by side, and a
+// warp reads a row at once (one sequence's token 11.9 us instead of 12.5).
 template <int DH>
 __device__ __forceinline__ size_t part_at(size_t buf, int row, int col) {
     return (buf * 256 + (row & ~31)) * DH + (size_t)(col >> 2) * 128 + (row & 31) * 4 + (col & 3);
 }
 
-// Joins 8 rows of a cut item, G times 16 columns of them, from the parts of CTAs first ..
-// last, in the order of the keys; a lane has a row and 4 columns of each 16, B sources are
-// read at a time.  CTA `first` wrote its part into its second buffer, the others into
-// their first; with `halves` each part has two sources, from the two slots.
-// Bound: latency (one or two rounds of reads), and L2 for prompts' items.  (Seldom run, so a
-// function of its own.)
-template <int DH, int G, int B>
-__device__ __noinline__ void join_rows(const CacheDev& c, const AttendParams& p, int token0, int head, int rows,
-                                          int halves, int first, int last, int r0, int k0, int lane) {
-    const int sources = (last - first + 1) << halves;
-    const int r = r0 + (lane & 7), rr = min(r, rows - 1), col = k0 + (lane >> 3) * 4;
+// One more source of a row: its maximum and sum (x), added to top and l; fa and fb are the
+// factors of what was summed before and of the source.  False: nothing was summed in it.
+__device__ __forceinline__ bool join_source(float2 x, bool there, float& top, float& l, float& fa, float& fb) {
+    there = there && x.x != -INFINITY;
+    const float m = there ? fmaxf(top, x.x) : top, ref = m == -INFINITY ? 0.f : m;
+    fa = ex2(top - ref);
+    fb = ex2(x.x - ref);
+    top = m;
+    l = there ? l * fa + x.y * fb : l;
+    return there;
+}
+
+// Joins row r of a cut item of one query tile from the parts of CTAs first .. last, in the
+// order of the keys; a lane takes D / 32 columns, eight sources are read at a time.  CTA
+// `first` wrote its part into its second buffer, the others into their first; each has two
+// sources, from the two slots.  Bound: latency, one or two rounds of reads.
+template <int DH>
+__device__ __forceinline__ void join_row(const CacheDev& c, const AttendParams& p, const Seg& g, int first, int last,
+                                         int r, int lane) {
+    constexpr int V = DH / 32, B = 8;
+    const int sources = (last - first + 1) * 2;
+    float top = -INFINITY, l = 0.f, acc[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = 0.f;
+#pragma unroll 1
+    for (int s0 = 0; s0 < sources; s0 += B) {
+        float2 ml[B];
+        float o[B][V];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int s = min(s0 + i, sources - 1), k = s >> 1;
+            const size_t row = (size_t)(k == 0 ? 2 * first + 1 : 2 * (first + k)) * 256 + (s & 1) * 128 + r;
+            const float* src = c.part_o + row * DH + lane * V;
+            ml[i] = __ldcg(c.part_ml + row);
+#pragma unroll
+            for (int j = 0; j < V; j += 2) {
+                const float2 x = __ldcg(reinterpret_cast<const float2*>(src + j));
+                o[i][j] = x.x;
+                o[i][j + 1] = x.y;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            float fa, fb;
+            const bool there = join_source(ml[i], s0 + i < sources, top, l, fa, fb);
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] = there ? acc[j] * fa + o[i][j] * fb : acc[j];
+        }
+    }
+    const int rep = c.rep;
+    const float il = l == 0.f ? 0.f : 1.f / l;
+    __nv_bfloat16* out = p.out + (size_t)(g.row + r / rep) * p.ld_out + (size_t)(g.head * rep + r % rep) * DH + lane * V;
+#pragma unroll
+    for (int j = 0; j < V; j += 2)
+        *reinterpret_cast<uint32_t*>(out + j) = pack_bf16x2(acc[j] * il, acc[j + 1] * il);
+}
+
+// Joins 8 rows of a cut item, G times 16 columns of them, likewise; a lane has a row and 4
+// columns of each 16, two sources are read at a time (each part is one: the slots have
+// joined theirs, or have rows of their own).  Bound: L2.
+template <int DH, int G>
+__device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams& p, const CacheShare& sh, int rows,
+                                          int r0, int k0, int lane) {
+    constexpr int B = 2;
+    const int sources = sh.last - sh.first + 1;
+    const int r = r0 + (lane & 7), row = min(r, rows - 1), col = k0 + (lane >> 3) * 4;
     float top = -INFINITY, l = 0.f, acc[G][4];
 #pragma unroll
     for (int g = 0; g < G; ++g)
@@ -301,9 +358,8 @@ __device__ __noinline__ void join_rows(const CacheDev& c, const AttendParams& p,
         float4 o[B][G];
 #pragma unroll
         for (int i = 0; i < B; ++i) {
-            const int s = min(s0 + i, sources - 1), k = s >> halves;
-            const size_t buf = k == 0 ? 2 * first + 1 : 2 * (first + k);
-            const int row = (s & halves) * 128 + rr;
+            const int s = min(s0 + i, sources - 1);
+            const size_t buf = s == 0 ? 2 * sh.first + 1 : 2 * (sh.first + s);
             ml[i] = __ldcg(c.part_ml + buf * 256 + row);
 #pragma unroll
             for (int g = 0; g < G; ++g)
@@ -311,11 +367,8 @@ __device__ __noinline__ void join_rows(const CacheDev& c, const AttendParams& p,
         }
 #pragma unroll
         for (int i = 0; i < B; ++i) {
-            const bool there = s0 + i < sources && ml[i].x != -INFINITY;       // else nothing was summed
-            const float m = there ? fmaxf(top, ml[i].x) : top, ref = m == -INFINITY ? 0.f : m;
-            const float fa = ex2(top - ref), fb = ex2(ml[i].x - ref);
-            top = m;
-            l = there ? l * fa + ml[i].y * fb : l;
+            float fa, fb;
+            const bool there = join_source(ml[i], s0 + i < sources, top, l, fa, fb);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const float x[4] = {o[i][g].x, o[i][g].y, o[i][g].z, o[i][g].w};
@@ -326,7 +379,7 @@ __device__ __noinline__ void join_rows(const CacheDev& c, const AttendParams& p,
     }
     const int tile = r >> 7, in = r & 127;
     if (r >= rows || in >= c.tile_tokens * c.rep) return;
-    const int token = token0 + tile * c.tile_tokens + in / c.rep, h = head * c.rep + in % c.rep;
+    const int token = sh.g.row + tile * c.tile_tokens + in / c.rep, h = sh.head * c.rep + in % c.rep;
     const float il = l == 0.f ? 0.f : 1.f / l;
     __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + col;
 #pragma unroll
@@ -987,10 +1040,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             if (live && (dual || slot == 0 || joins || apart)) {
                 float* po = nullptr;
+                int po_step = 0;                           // from column to column of a multiple of 4
                 __nv_bfloat16* out = nullptr;
                 if (g.part >= 0) {
                     const int row = (dual || apart ? slot * 128 : 0) + r;
-                    po = c.part_o + part_at<DH>(g.part, row, 0);
+                    po = c.part_o + (apart ? ((size_t)g.part * 256 + row) * DH : part_at<DH>(g.part, row, 0));
+                    po_step = apart ? 1 : 32;
                     if (mine && !(joins && slot)) c.part_ml[(size_t)g.part * 256 + row] = make_float2(work ? m : -INFINITY, l);
                 } else {
                     out = p.out + (size_t)token * p.ld_out + (size_t)(g.head * rep + r - tok_in_tile * rep) * DH;
@@ -1017,7 +1072,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         if (po) {
 #pragma unroll
                             for (int j = 0; j < 16; j += 4)
-                                *reinterpret_cast<float4*>(po + (k + j) * 32) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+                                *reinterpret_cast<float4*>(po + (k + j) * po_step) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
                         } else {
 #pragma unroll
                             for (int j = 0; j < 16; j += 8)
@@ -1057,9 +1112,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (!ok) break;
                 ph ^= kPhJ;
                 if (bars->last_part)
-                    for (int u = warp - 4; u < (g.ntok * rep + 7) / 8 * (DH / 16); u += 8)
-                        join_rows<DH, 1, 8>(c, p, g.row, g.head, g.ntok * rep, 1, first, last, u / (DH / 16) * 8,
-                                            u % (DH / 16) * 16, lane);
+                    for (int r0 = warp - 4; r0 < g.ntok * rep; r0 += 8) join_row<DH>(c, p, g, first, last, r0, lane);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(&bars->seg_empty[it % kSegSlots]));
@@ -1089,8 +1142,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
     const int rows = two ? 128 + (next.g.ntok - c.tile_tokens) * c.rep : next.g.ntok * c.rep;
     const int warp = threadIdx.x >> 5, r0 = blockIdx.y * 32 + (warp >> 1) * 8;
     if (r0 < rows)
-        join_rows<DH, DH / 32, 2>(c, p, next.g.row, next.head, rows, 0, b, next.last, r0, (warp & 1) * (DH / 2),
-                                  threadIdx.x & 31);
+        join_rows<DH, DH / 32>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
 }
 
 static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
