@@ -3,7 +3,7 @@
 // A query tile is 128 rows: tile_tokens = 128 / rep consecutive new tokens of one
 // sequence, each with the rep = q_heads / kv_heads query heads of one key/value
 // head, so that a key tile read once serves all heads that share it.  For a tile and
-// key tiles of 128 positions (FlashAttention's running softmax, in base 2):
+// key tiles of 128 positions (a running softmax, in base 2):
 //
 //   S = Q K^T                       tcgen05.mma, M = 128, N = 128, K = D -> TMEM
 //   m' = max(m, max_j s_j);  p_j = 2^(scale' (s_j - m'))   fp32, one row per thread
@@ -32,8 +32,9 @@
 // items each CTA draws whole items from a counter, the longest first.  Otherwise the
 // items' costs are laid end to end and each CTA takes the same share of the line, cutting
 // items at key tiles; a cut item's parts go to a buffer, at most two per CTA, and are
-// added in the order of the keys (join_rows), so results do not depend on timing.  With
-// few rows the CTA that writes an item's last part joins it, else cache_join_kernel does.
+// added in the order of the keys, so results do not depend on timing.  With
+// few rows the CTA that writes an item's last part joins it (join_row), else
+// cache_join_kernel does (join_rows).
 //
 // Masked places never reach a result: scores are replaced, not added to; value
 // rows that no row of the item sees are zeroed in shared memory (0 * NaN would
@@ -44,7 +45,7 @@
 // of each slot; decoding HBM, each K and V row once per query tile.  Measured (32 query
 // heads on 8, D = 128): a 16384-token prompt 1.50 ms, 1.47 PFLOP/s, 0.76 of cuBLAS; 7
 // sequences of 30k to 65k positions, a token each, 200 us, 0.98 of the copy rate; one
-// sequence of 1500 positions 11.5 us, launches and latencies.
+// sequence of 1500 positions 11.9 us, launches and latencies.
 #include <algorithm>
 #include <cstddef>
 
