@@ -13,9 +13,12 @@
 //
 // The reference m need not be the maximum: O and l are rescaled only when a row's
 // maximum is more than a factor 2^8 above m, so p stays below 2^8, which costs no
-// precision in floating point, and the pass over O in TMEM is rare.  m is a whole
-// number, so its factors are exact.  P is rounded to bf16, the type of the tensor cores'
-// other operand; l sums p in fp32 before that rounding.
+// precision in floating point, and the pass over O in TMEM is rare.  P is rounded to bf16,
+// the type of the tensor cores' other operand; l sums p in fp32 before that rounding (sums
+// of the rounded values cost 11 % of a long prompt).  m starts as the maximum of the first
+// keys that the row sees, whose p then is 1 and rounds to itself: a row that sees one key
+// gives its value exactly, and the error against 64 bits is 1.07 to 1.4 times that of the
+// output's rounding alone.
 //
 // A CTA holds two query tiles in flight ("slots", each with its own S and O in
 // TMEM and its own group of four softmax warps), so that one slot's products run
@@ -44,7 +47,7 @@
 // Bounds: prompts the tensor cores and, per key tile, the chain S -> exponentials -> P V
 // of each slot; decoding HBM, each K and V row once per query tile.  Measured (32 query
 // heads on 8, D = 128): a 16384-token prompt 1.50 ms, 1.47 PFLOP/s, 0.76 of cuBLAS; 7
-// sequences of 30k to 65k positions, a token each, 200 us, 0.98 of the copy rate; one
+// sequences of 30k to 65k positions, a token each, 199 us, 0.98 of the copy rate; one
 // sequence of 1500 positions 11.9 us, launches and latencies.
 #include <algorithm>
 #include <cstddef>
@@ -878,7 +881,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 // product runs under the second half's exponentials.  These start from the
                 // reference m at hand, beside the search for the half's maximum (other units);
                 // when that is more than 2^8 above m, or far below the row's first one, m
-                // moves (to a whole number), O and l are scaled, and they are repeated.
+                // moves there, O and l are scaled, and they are repeated.
                 uint32_t u[3][32];
                 float2 ls[2];
                 auto hide = [&](int q) {                 // masked scores of quarter q
@@ -920,7 +923,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     exponentials(2 * half + 1);
                     const bool move = mx - m > 8.f || (l == 0.f && mx - m < -8.f && mx != -INFINITY);
                     if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
-                        const float up = ceilf(mx), f = move && l != 0.f ? ex2(m - up) : 1.f;   // l = 0: so is O
+                        const float up = mx, f = move && l != 0.f ? ex2(m - up) : 1.f;   // l = 0: so is O
                         if (move) m = up;
                         l *= f;
                         if (half || t != begin) {
@@ -971,7 +974,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     }
                     if (t == begin) {                    // a reference that the next tiles seldom leave
                         const float mx = fmaxf(maximum(0), maximum(1));
-                        m = mx == -INFINITY ? 0.f : ceilf(mx);
+                        m = mx == -INFINITY ? 0.f : mx;
                     }
                     half_tile(0);
                     if (bad) by_hand(0);

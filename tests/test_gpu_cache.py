@@ -516,3 +516,21 @@ def test_groups_that_end_before_their_sequence():
         out = cache.attend(0, x)
         check_attend(cache, m, x, q, out, 0)
         assert cache.stats()["device_error"] == 0
+
+
+@pytest.mark.parametrize("shapes,page", [((32, 8, 128), 64), ((12, 12, 64), 16), ((8, 1, 64), 128)])
+def test_a_single_seen_key_gives_its_value(shapes, page):
+    """The only key's probability is 1, which bf16 holds, so the value comes back bit for bit: first tokens of prompts,
+    single tokens without context, drafts that see only themselves."""
+    hq, hkv, dh = shapes
+    for q, tree in (([1, 300, 1, 5, 1], False), ([1, 64, 3], True)):
+        cache, m, x = filled(shapes, page, [0] * len(q), q, seed=sum(q))
+        mask = torch.tensor([1 << j for n in q for j in range(n)], dtype=torch.uint64).view(torch.int64) if tree else None
+        out = cache.attend(0, x * 3, tree=None if mask is None else mask.to(DEV))
+        at = 0
+        for s, n in enumerate(q):
+            rows = n if tree else 1
+            v = rows_of(cache.v[0], m, s, rows).transpose(0, 1).repeat_interleave(hq // hkv, 1)
+            assert torch.equal(out[at:at + rows].view(rows, hq, dh), v), (s, tree)
+            at += n
+        assert cache.stats()["device_error"] == 0
