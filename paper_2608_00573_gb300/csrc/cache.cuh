@@ -10,9 +10,9 @@ constexpr int kCacheMaxSeqs = 1024;
 constexpr int kCacheTile = 128;        // rows of a query tile, keys of a key tile
 constexpr int kTreeMax = 64;           // drafted tokens of a sequence (mask bits)
 // Up to this many rows of an item, the CTA that writes a cut item's last part joins
-// them (a decode step then is one launch: one sequence of 1500 positions takes 11.5 us so,
-// 19.3 with a second kernel); above, a second kernel does, with a CTA per 32 rows (a
-// 777-token prompt of 12 heads takes 20 us so, 40 if the CTAs join).
+// them (a decode step then is one launch: one sequence of 1500 positions 11.9 us, with a
+// second kernel it took 19.3); above, a second kernel does, with a CTA per 32 rows (a
+// 777-token prompt of 12 heads 15.4 us; when it took 20, joining in the CTAs took 40).
 constexpr int kJoinHereRows = 32;
 
 // One listed sequence of the current step.
