@@ -962,6 +962,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(b));
                 };
+                // The other slot reads this one's last O: until it has, nothing is stored there, by a
+                // product or by hand (an item's first half scales nothing).
+                auto other_has_read = [&] {
+                    if (reads_mine) ok = !lost(wait(&bars->x_done[slot ^ 1][qw], (ph / kPhX) ^ 1u));
+                    reads_mine = false;
+                };
                 if (live) {
                     tmem_ld_32x32(tS, u[0]);
                     tmem_ld_32x32(tS + 32, u[1]);
@@ -977,14 +983,15 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         m = mx == -INFINITY ? 0.f : mx;
                     }
                     half_tile(0);
-                    if (bad) by_hand(0);
+                    if (bad) {
+                        other_has_read();
+                        if (!ok) break;
+                        by_hand(0);
+                    }
                     tmem_ld_32x32(tS + 96, u[0]);
                 }
-                if (reads_mine) {                        // the other slot reads this one's last O
-                    ok = !lost(wait(&bars->x_done[slot ^ 1][qw], (ph / kPhX) ^ 1u));
-                    if (!ok) break;
-                    reads_mine = false;
-                }
+                other_has_read();
+                if (!ok) break;
                 hand_over(&bars->p_half[slot]);
                 if (live) {
                     landed(u[0]);
