@@ -565,7 +565,8 @@ trimmoe_status trimmoe_cache_accept(trimmoe_cache_handle c, int n, const int32_t
                                     const int32_t* path, int ld_path, void* stream);
 
 /* Move the pages in use to the lowest indices: those past the number in use go,
- * in order, to the free ones below it; tables and counts follow. */
+ * in order, to the free ones below it; tables and counts follow.  A page with
+ * references from outside (ref above its holders in table) stays where it is. */
 trimmoe_status trimmoe_cache_compact(trimmoe_cache_handle c, void* stream);
 
 typedef struct {

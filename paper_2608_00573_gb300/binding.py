@@ -672,7 +672,8 @@ class PagedCache:
                                                   path.shape[1], self._stream(stream)))
 
     def compact(self, stream=None):
-        """Move the pages in use to the lowest indices."""
+        """Move the pages in use to the lowest indices, except those that the program holds itself (ref above the
+        page's holders in table): these stay where they are."""
         self._done(self._lib.trimmoe_cache_compact(self.handle, self._stream(stream)))
 
     def stats(self, reset: bool = False) -> dict:

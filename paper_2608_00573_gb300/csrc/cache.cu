@@ -219,6 +219,7 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         alloc(d.copies, (size_t)std::max(cfg->n_pages, cfg->max_seqs));
         alloc(d.fresh, cfg->n_pages);
         alloc(d.base, cfg->max_seqs);
+        alloc(d.holders, cfg->n_pages);
         alloc(d.part_o, (size_t)2 * d.num_sms * 256 * d.dh);
         alloc(d.part_ml, (size_t)2 * d.num_sms * 256);
         alloc(d.arrived, (size_t)d.num_sms);
@@ -227,6 +228,7 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
             return bail(e == cudaErrorMemoryAllocation ? TRIMMOE_ERR_OOM : TRIMMOE_ERR_CUDA, cudaGetErrorString(e));
         e = cudaMemset(d.err, 0, sizeof(int));
         if (e == cudaSuccess) e = cudaMemset(d.plan, 0, sizeof(CachePlan));
+        if (e == cudaSuccess) e = cudaMemset(d.holders, 0, sizeof(int) * (size_t)cfg->n_pages);
         // Without a step a sequence has no drafts to accept.
         if (e == cudaSuccess) e = cudaMemcpy(d.base, d.length, sizeof(int) * (size_t)cfg->max_seqs, cudaMemcpyDeviceToDevice);
         if (e == cudaSuccess) e = cudaDeviceSynchronize();
@@ -399,7 +401,7 @@ extern "C" trimmoe_status trimmoe_cache_compact(trimmoe_cache_handle c, void* st
     c->T = -1;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_compact");
-    return c->launched(launch_cache_compact(c->d, enter(c, stream)), 4, "cache_compact");
+    return c->launched(launch_cache_compact(c->d, enter(c, stream)), 5, "cache_compact");
 }
 
 extern "C" trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_cache_stats_t* out, int reset) {

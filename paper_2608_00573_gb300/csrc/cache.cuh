@@ -86,6 +86,7 @@ struct CacheDev {
     int2* copies;                      // [max(n_pages, max_seqs)] (from, to) pages
     int* fresh;                        // [n_pages] free pages taken by a step; new place of each page (compact)
     int* base;                         // [max_seqs] length before the sequence's last step
+    int* holders;                      // [n_pages] a page's entries in table, counted by compact, 0 between calls
     // Parts of cut items: two buffers per CTA, for the item that its share begins in and
     // the one that it ends in; rows 0..127 and 128..255 from the two slots.
     float* part_o;                     // [2 num_sms][256][dh] sums of p v (order within: cache_attention.cu)

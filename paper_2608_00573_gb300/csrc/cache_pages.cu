@@ -93,24 +93,30 @@ __device__ __forceinline__ int find_le(const V* off, int n, V x) {
     return lo;
 }
 
-// Which of a thread's four pages p0 .. p0 + 3 below `to` are free (live: in use), a bit each.
-__device__ __forceinline__ uint32_t four_pages(const int* ref, int p0, int to, bool live) {
+// A page that compaction may move: in use, and by sequences alone (holders: its entries in
+// the table).  Who holds it besides knows it by its index.
+__device__ __forceinline__ bool movable(int ref, int holders) { return ref > 0 && ref <= holders; }
+
+// Which of a thread's four pages p0 .. p0 + 3 below `to` are free (holders: movable
+// instead), a bit each.
+__device__ __forceinline__ uint32_t four_pages(const int* ref, const int* holders, int p0, int to) {
     uint32_t f = 0;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-        if (p0 + u < to && (ref[p0 + u] > 0) == live) f |= 1u << u;
+        if (p0 + u < to && (holders ? movable(ref[p0 + u], holders[p0 + u]) : ref[p0 + u] <= 0)) f |= 1u << u;
     return f;
 }
 
-// Free pages (ref == 0; live: pages in use instead) in [from, to), ascending: put(k, page)
-// for the first `want` of them; returns how many there were, up to that.  first: this
-// thread's four_pages() at from + 4 threadIdx.x, which the caller may read early.
+// Free (holders: movable) pages in [from, to), ascending: put(k, page) for the first
+// `want` of them; returns how many there were, up to that.  first: this thread's
+// four_pages() at from + 4 threadIdx.x, which the caller may read early.
 template <class Put>
-__device__ int collect_pages(const int* ref, int from, int to, bool live, int want, uint32_t first, int* ws, Put put) {
+__device__ int collect_pages(const int* ref, const int* holders, int from, int to, int want, uint32_t first, int* ws,
+                             Put put) {
     int found = 0;
     for (int b = from; b < to && found < want; b += kStepThreads * 4) {
         const int p0 = b + threadIdx.x * 4;
-        const uint32_t f = b == from ? first : four_pages(ref, p0, to, live);
+        const uint32_t f = b == from ? first : four_pages(ref, holders, p0, to);
         int total;
         int at = found + block_scan(__popc(f), ws, total);
 #pragma unroll
@@ -145,7 +151,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     if (i == 0) s_bad = s_most = 0;
     pdl_wait();
     pdl_trigger();
-    const uint32_t free4 = four_pages(c.ref, i * 4, c.n_pages, false);      // (on its way beside the lengths)
+    const uint32_t free4 = four_pages(c.ref, nullptr, i * 4, c.n_pages);      // (on its way beside the lengths)
     int len = i < n ? c.length[seq] : 0;
     __syncthreads();
     int had = 0, last = -1, cow = 0, fresh = 0;
@@ -181,7 +187,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     __syncthreads();
     if (!s_bad && n_fresh > 0) {
         // (Shared memory holds as many as it has room for.)
-        const int found = collect_pages(c.ref, 0, c.n_pages, false, n_fresh, free4, s_ws, [&](int k, int page) {
+        const int found = collect_pages(c.ref, nullptr, 0, c.n_pages, n_fresh, free4, s_ws, [&](int k, int page) {
             (k < kStepThreads ? s_fresh : c.fresh)[k] = page;
         });
         if (found < n_fresh && i == 0) s_bad = ERR_CACHE_FULL;
@@ -514,8 +520,21 @@ __global__ void __launch_bounds__(256) cache_accept_kernel(const __grid_constant
     }
 }
 
-// One block: pairs the pages in use past the number in use with the free ones
-// below it, both ascending; plan->total is that number, fresh[] the new places.
+// Compaction counts a page's entries in the table first: holders[] is 0 before, and again
+// behind cache_recount_kernel.
+__global__ void __launch_bounds__(256) cache_holders_kernel(const __grid_constant__ CacheDev c) {
+    pdl_wait();
+    pdl_trigger();
+    const long long entries = (long long)c.max_seqs * c.max_pages, step = gridDim.x * 256LL;
+    for (long long e = blockIdx.x * 256LL + threadIdx.x; e < entries; e += step) {
+        const int id = c.table[e];
+        if (id >= 0 && id < c.n_pages) atomicAdd(&c.holders[id], 1);
+    }
+}
+
+// One block: pairs the movable pages past the number in use with the free ones below it,
+// both ascending; plan->total is that number, fresh[] the new places.  (There are as many
+// free ones below as pages in use past it, movable or not.)
 __global__ void __launch_bounds__(kStepThreads) cache_compact_kernel(const __grid_constant__ CacheDev c) {
     __shared__ int s_ws[33];
     pdl_wait();
@@ -524,10 +543,11 @@ __global__ void __launch_bounds__(kStepThreads) cache_compact_kernel(const __gri
     for (int p = threadIdx.x; p < c.n_pages; p += kStepThreads) mine += c.ref[p] > 0;
     block_scan(mine, s_ws, live);
     const int mine4 = threadIdx.x * 4;
-    const int holes = collect_pages(c.ref, 0, live, false, live, four_pages(c.ref, mine4, live, false), s_ws,
+    const int holes = collect_pages(c.ref, nullptr, 0, live, live, four_pages(c.ref, nullptr, mine4, live), s_ws,
                                     [&](int k, int page) { c.copies[k].y = page; });
-    const int movers = collect_pages(c.ref, live, c.n_pages, true, holes, four_pages(c.ref, live + mine4, c.n_pages, true),
-                                     s_ws, [&](int k, int page) { c.copies[k].x = page; });
+    const int movers = collect_pages(c.ref, c.holders, live, c.n_pages, holes,
+                                     four_pages(c.ref, c.holders, live + mine4, c.n_pages), s_ws,
+                                     [&](int k, int page) { c.copies[k].x = page; });
     __syncthreads();
     for (int k = threadIdx.x; k < movers; k += kStepThreads) c.fresh[c.copies[k].x] = c.copies[k].y;
     if (threadIdx.x == 0) *c.plan = CachePlan{live, 0, 0, movers, 0, 0, 0};
@@ -543,8 +563,9 @@ __global__ void __launch_bounds__(256) cache_remap_kernel(const __grid_constant_
     for (long long e = at; e < entries; e += step) {
         const int id = c.table[e];
         if (id >= live && id < c.n_pages) {
-            if (c.ref[id] > 0) c.table[e] = c.fresh[id];
-            else atomicCAS(c.err, 0, ERR_CACHE_STATE);
+            const int ref = c.ref[id];
+            if (movable(ref, c.holders[id])) c.table[e] = c.fresh[id];
+            else if (ref <= 0) atomicCAS(c.err, 0, ERR_CACHE_STATE);
         }
     }
 }
@@ -558,6 +579,7 @@ __global__ void __launch_bounds__(256) cache_recount_kernel(const __grid_constan
         c.ref[cp.y] = c.ref[cp.x];
         c.ref[cp.x] = 0;
     }
+    for (int p = blockIdx.x * 256 + threadIdx.x; p < c.n_pages; p += gridDim.x * 256) c.holders[p] = 0;
 }
 
 template <int N>
@@ -629,11 +651,11 @@ cudaError_t launch_cache_accept(const CacheDev& c, int n, const int* seq, const 
 }
 
 cudaError_t launch_cache_compact(const CacheDev& c, cudaStream_t st) {
-    cudaError_t e = launch_pdl(cache_compact_kernel, dim3(1), dim3(kStepThreads), 0, st, c);
+    const dim3 entries(entry_blocks(c, (long long)c.max_seqs * c.max_pages));
+    cudaError_t e = launch_pdl(cache_holders_kernel, entries, dim3(256), 0, st, c);
+    if (e == cudaSuccess) e = launch_pdl(cache_compact_kernel, dim3(1), dim3(kStepThreads), 0, st, c);
     if (e == cudaSuccess) e = launch_pdl(cache_fill_kernel, dim3(c.num_sms * 6), dim3(kCopyThreads), 0, st, c, 0, 0);
-    if (e == cudaSuccess)
-        e = launch_pdl(cache_remap_kernel, dim3(entry_blocks(c, (long long)c.max_seqs * c.max_pages)), dim3(256), 0,
-                       st, c);
+    if (e == cudaSuccess) e = launch_pdl(cache_remap_kernel, entries, dim3(256), 0, st, c);
     if (e == cudaSuccess)
         e = launch_pdl(cache_recount_kernel, dim3(entry_blocks(c, c.n_pages)), dim3(256), 0, st, c);
     return e;
