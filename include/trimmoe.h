@@ -491,8 +491,9 @@ trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, const trimm
  * into a page of its own (all layers; every holder listed in the step copies,
  * the pages that this frees are free after the step).  Builds the work list that append and
  * attend use until the next step, fork, truncate, accept or compact.
- * Without enough pages nothing changes, CACHE_FULL is flagged, and append and
- * attend do nothing until a step succeeds. */
+ * Without enough pages nothing changes, CACHE_FULL is flagged, append and
+ * attend do nothing until a step succeeds, and accept leaves its sequences alone
+ * until then or until stats with reset has told the program. */
 trimmoe_status trimmoe_cache_step(trimmoe_cache_handle c, int n, const int32_t* seq, const int32_t* q_len,
                                   void* stream);
 
@@ -560,7 +561,8 @@ trimmoe_status trimmoe_cache_truncate(trimmoe_cache_handle c, int n, const int32
  * at most 64) move to the front, in all layers, and the sequence is cut behind
  * them.  seq is a host array, n_acc int32 [n] and path int32 [n][ld_path] are on
  * the device.  A sequence whose n_acc or path does not fit, or whose drafts are
- * shared, is left as it is and CACHE_PATH is flagged. */
+ * shared, is left as it is and CACHE_PATH is flagged; so is every sequence behind
+ * a step that was refused (see there), which added no drafts. */
 trimmoe_status trimmoe_cache_accept(trimmoe_cache_handle c, int n, const int32_t* seq, const int32_t* n_acc,
                                     const int32_t* path, int ld_path, void* stream);
 
@@ -576,7 +578,8 @@ typedef struct {
 } trimmoe_cache_stats_t;
 
 /* Synchronise the handle's last stream and read the counters; reset != 0 clears
- * the error afterwards.  Returns CACHE or DEVICE_TIMEOUT if one was flagged. */
+ * the error afterwards, and accept then speaks again of the last step that added
+ * tokens.  Returns CACHE or DEVICE_TIMEOUT if one was flagged. */
 trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_cache_stats_t* out, int reset);
 
 /* Last error message of the cache ("" if none). */

@@ -223,10 +223,11 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         alloc(d.part_o, (size_t)2 * d.num_sms * 256 * d.dh);
         alloc(d.part_ml, (size_t)2 * d.num_sms * 256);
         alloc(d.arrived, (size_t)d.num_sms);
-        alloc(d.err, 1);
+        alloc(d.err, 2);
         if (e != cudaSuccess)
             return bail(e == cudaErrorMemoryAllocation ? TRIMMOE_ERR_OOM : TRIMMOE_ERR_CUDA, cudaGetErrorString(e));
-        e = cudaMemset(d.err, 0, sizeof(int));
+        d.refused = d.err + 1;
+        e = cudaMemset(d.err, 0, 2 * sizeof(int));
         if (e == cudaSuccess) e = cudaMemset(d.plan, 0, sizeof(CachePlan));
         if (e == cudaSuccess) e = cudaMemset(d.holders, 0, sizeof(int) * (size_t)cfg->n_pages);
         // Without a step a sequence has no drafts to accept.
@@ -419,7 +420,7 @@ extern "C" trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_ca
     } catch (const std::bad_alloc&) {
         return c->fail(TRIMMOE_ERR_OOM, "cache_stats", "host allocation failed");
     }
-    if (e == cudaSuccess && reset) e = cudaMemset(c->d.err, 0, sizeof code);
+    if (e == cudaSuccess && reset) e = cudaMemset(c->d.err, 0, 2 * sizeof code);
     if (e != cudaSuccess) return c->fail(TRIMMOE_ERR_CUDA, "cache_stats", cudaGetErrorString(e));
     out->device_error = code;
     out->free_pages = free_pages;

@@ -93,6 +93,7 @@ struct CacheDev {
     float2* part_ml;                   // [2 num_sms][256] row maxima and sums of p
     int* arrived;                      // [num_sms] parts written of the item that a CTA began, 0 between calls
     int* err;
+    int* refused;                      // behind err: the last step was refused and stats has not reset that yet
 };
 
 // Host arrays of a call travel as kernel parameters (no staging buffer whose

@@ -197,6 +197,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
         if (i == 0) {
             *c.plan = CachePlan{};
             atomicCAS(c.err, 0, s_bad);
+            *c.refused = 1;
         }
         return;
     }
@@ -287,7 +288,10 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
             before += part;
         }
     }
-    if (i == 0) *c.plan = CachePlan{W, n_groups, n_ctas, sum.cow, 1, 0, 0};
+    if (i == 0) {
+        *c.plan = CachePlan{W, n_groups, n_ctas, sum.cow, 1, 0, 0};
+        *c.refused = 0;
+    }
     __syncthreads();
     for (int b = i; b < n_ctas; b += kStepThreads) {
         CacheShare sh;
@@ -428,7 +432,8 @@ __global__ void __launch_bounds__(256) cache_cut_kernel(const __grid_constant__ 
 // (sequence, layer, head), each lane its own 16 bytes of every row, in the order of the
 // path: row e is written after rows e .. e + 3 were read, and later rows come from
 // behind (path[e] >= e), so rows may overlap.  Lane e looks up the e-th row's pages once,
-// for the check and for the move (and again for paths longer than the lanes).
+// for the check and for the move (and again for paths longer than the lanes).  Behind a
+// refused step nothing fits: base is that of the step before, whose tokens are no drafts.
 template <int N>
 __global__ void __launch_bounds__(256) cache_accept_kernel(const __grid_constant__ CacheDev c,
                                                            const __grid_constant__ CacheList<N> l, const int* n_acc,
@@ -457,7 +462,7 @@ __global__ void __launch_bounds__(256) cache_accept_kernel(const __grid_constant
             n = n_acc[i];
             mine = path + (size_t)i * ld_path;
             table = c.table + (size_t)seq * c.max_pages;
-            if (base < 0 || drafts < 0 || (long long)base + drafts > (long long)c.max_pages * c.page || n < 0 ||
+            if (*c.refused || base < 0 || drafts < 0 || (long long)base + drafts > (long long)c.max_pages * c.page || n < 0 ||
                 n > min(min(drafts, kTreeMax), ld_path)) {
                 ok = false;
                 n = 0;

@@ -1,4 +1,5 @@
-"""What the paged cache's header promises beyond single calls."""
+"""What the paged cache's header promises beyond single calls: references held from outside, refused steps, inputs on
+other streams."""
 import pytest
 import torch
 
@@ -59,3 +60,30 @@ def test_compaction_leaves_pages_held_from_outside(page, dh):
         assert torch.equal(rows(c, s), want), s
     holders = torch.bincount(c.table[c.table >= 0].long(), minlength=40)
     assert torch.equal(holders.to(torch.int32), c.ref) and c.stats()["status"] == 0
+
+
+def test_accept_behind_a_refused_step_keeps_the_sequence():
+    """A step for drafts that finds no room adds none: an accept queued behind it must not take the tokens of the step
+    before (a prompt) for drafts and cut the sequence to a few of them."""
+    c = B.PagedCache.empty(2, 10, 4, 2, 64, 16, 3, 7, T_max=200)
+    c.k.copy_(torch.randn(c.k.shape, device=DEV))
+    c.v.copy_(torch.randn(c.v.shape, device=DEV))
+    c.step([0, 1], [100, 20])                      # 7 and 2 of the 10 pages
+    k, v, table, length, ref = (t.clone() for t in (c.k, c.v, c.table, c.length, c.ref))
+    path = ints([[0, 2, 5], [0, 1, 2]])
+    c.step([0, 1], [29, 29])                       # more than max_pages
+    c.accept([0, 1], ints([3, 3]), path)
+    for now, was in zip((c.k, c.v, c.table, c.length, c.ref), (k, v, table, length, ref)):
+        assert torch.equal(now, was)
+    # A step that succeeds ends this, for all sequences.
+    c.step([2], [5])
+    c.accept([2, 1], ints([2, 20]), ints([[1, 4] + [0] * 18, list(range(20))]))
+    assert c.length.tolist() == [100, 20, 2]
+    st = c.stats(reset=True)
+    assert st["status"] == -7 and st["device_error"] == 8
+    # So does having been told: the last step that added tokens is the prompt's again.
+    c.step([0], [29])
+    c.accept([0], ints([2]), path[:1])
+    assert c.length.tolist() == [100, 20, 2] and c.stats(reset=True)["device_error"] == 8
+    c.accept([0], ints([2]), path[:1])
+    assert c.length.tolist() == [2, 20, 2] and c.stats()["status"] == 0
