@@ -480,7 +480,8 @@ typedef struct {
 } trimmoe_cache_state;
 
 /* Validate and allocate the workspaces (work list, split-sum buffers: about
- * 40 MB at head_dim 128).  Errors: ARG, UNSUPPORTED, OOM, CUDA; *out is NULL then. */
+ * 40 MB at head_dim 128).  Waits for the device, then reads length.
+ * Errors: ARG, UNSUPPORTED, OOM, CUDA; *out is NULL then. */
 trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, const trimmoe_cache_state* st,
                                     trimmoe_cache_handle* out);
 

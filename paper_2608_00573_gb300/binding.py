@@ -516,8 +516,6 @@ class PagedCache:
                                    max_seqs=self.max_seqs, max_pages=self.max_pages, T_max=self.T_max)
         st = trimmoe_cache_state(k=_ptr(k), v=_ptr(v), table=_ptr(table), length=_ptr(length), ref=_ptr(ref))
         with torch.cuda.device(self.device):
-            # create reads length: what was queued to fill it comes first.
-            torch.cuda.current_stream().synchronize()
             self.handle = trimmoe_cache_create(cfg, st)
 
     @classmethod

@@ -230,7 +230,9 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         e = cudaMemset(d.err, 0, 2 * sizeof(int));
         if (e == cudaSuccess) e = cudaMemset(d.plan, 0, sizeof(CachePlan));
         if (e == cudaSuccess) e = cudaMemset(d.holders, 0, sizeof(int) * (size_t)cfg->n_pages);
-        // Without a step a sequence has no drafts to accept.
+        // Without a step a sequence has no drafts to accept.  (The lengths may still be on their
+        // way in any stream.)
+        if (e == cudaSuccess) e = cudaDeviceSynchronize();
         if (e == cudaSuccess) e = cudaMemcpy(d.base, d.length, sizeof(int) * (size_t)cfg->max_seqs, cudaMemcpyDeviceToDevice);
         if (e == cudaSuccess) e = cudaDeviceSynchronize();
         if (e != cudaSuccess) return bail(TRIMMOE_ERR_CUDA, cudaGetErrorString(e));
