@@ -422,7 +422,11 @@ extern "C" trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_ca
     } catch (const std::bad_alloc&) {
         return c->fail(TRIMMOE_ERR_OOM, "cache_stats", "host allocation failed");
     }
-    if (e == cudaSuccess && reset) e = cudaMemset(c->d.err, 0, 2 * sizeof code);
+    if (e == cudaSuccess && reset) {
+        // (Cleared when the call returns: what a kernel flags from then on stays.)
+        e = cudaMemsetAsync(c->d.err, 0, 2 * sizeof code, c->last_stream);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(c->last_stream);
+    }
     if (e != cudaSuccess) return c->fail(TRIMMOE_ERR_CUDA, "cache_stats", cudaGetErrorString(e));
     out->device_error = code;
     out->free_pages = free_pages;

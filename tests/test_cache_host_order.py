@@ -63,3 +63,19 @@ def test_create_reads_lengths_that_any_stream_wrote(lib):
     c.step(0x500)
     assert [lib.fake_base(s) for s in range(SEQS)] == [37] * SEQS
     lib.trimmoe_cache_destroy(c.h)
+
+
+@pytest.mark.parametrize("stream", [0x500, 0])
+def test_an_error_behind_a_reset_stays(lib, stream):
+    """stats(reset) returns when the error word is clear: what a kernel flags from then on is reported."""
+    c = Cache(lib)
+    c.step(stream)
+    assert c.stats(0) == 0
+    lib.fake_flag_error(8)
+    assert c.stats(1) == 8 and c.stats(0) == 0
+    lib.fake_flag_error(8)
+    assert c.stats(1) == 8
+    lib.fake_flag_error(10)
+    lib.fake_finish()
+    assert c.stats(0) == 10
+    lib.trimmoe_cache_destroy(c.h)
