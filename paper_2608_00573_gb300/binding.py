@@ -478,7 +478,10 @@ class PagedCache:
     table int32 [max_seqs][max_pages] (-1: none), length int32 [max_seqs], ref
     int32 [n_pages].  ``PagedCache.empty`` makes them for a new cache.  Calls are
     queued on the current stream (or ``stream``); see include/trimmoe.h for
-    their rules.  Sequence lists are host sequences of ints.
+    their rules.  Sequence lists are host sequences of ints.  With ``stream``, what
+    wrote the inputs has to be ordered before the call and what reads the result
+    behind it, as for any work on two streams; the inputs' memory is kept from
+    other uses until that stream has read them, and a result is of that stream.
     """
 
     def __init__(self, k, v, table, length, ref, q_heads: int, T_max: int):
@@ -596,6 +599,13 @@ class PagedCache:
             return self._raw_stream(self._index)
         return int(self.torch.cuda.current_stream(self.device).cuda_stream)
 
+    @staticmethod
+    def _keep(stream, *tensors):
+        """The caller may drop these at once: their memory is used again only behind `stream`."""
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
     def _done(self, rc):
         if rc != TRIMMOE_OK:
             raise TrimmoeError(rc, self._lib.trimmoe_cache_last_error(self.handle).decode())
@@ -628,6 +638,8 @@ class PagedCache:
         rc = self._c_append(self.handle, layer, self._append_at, self._stream(stream))
         if rc:
             self._done(rc)
+        if stream is not None:
+            self._keep(stream, qkv, q_out, gamma_q, gamma_k, pos)
         return q_out
 
     def attend(self, layer: int, q, out=None, tree=None, scale: float = 0.0, stream=None):
@@ -647,6 +659,8 @@ class PagedCache:
         rc = self._c_attend(self.handle, layer, self._attend_at, self._stream(stream))
         if rc:
             self._done(rc)
+        if stream is not None:
+            self._keep(stream, q, out, tree)
         return out
 
     def fork(self, src, dst, stream=None):
@@ -668,6 +682,8 @@ class PagedCache:
         self._tensor(path, self.torch.int32, (seq[2], path.shape[1]), "accept")
         self._done(self._lib.trimmoe_cache_accept(self.handle, seq[2], seq[1], n_acc.data_ptr(), path.data_ptr(),
                                                   path.shape[1], self._stream(stream)))
+        if stream is not None:
+            self._keep(stream, n_acc, path)
 
     def compact(self, stream=None):
         """Move the pages in use to the lowest indices, except those that the program holds itself (ref above the

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2608_00573_gb300 import binding as B
-from tests.test_gpu_cache import DEV
+from tests.test_gpu_cache import DEV, filled
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +87,55 @@ def test_accept_behind_a_refused_step_keeps_the_sequence():
     assert c.length.tolist() == [100, 20, 2] and c.stats(reset=True)["device_error"] == 8
     c.accept([0], ints([2]), path[:1])
     assert c.length.tolist() == [2, 20, 2] and c.stats()["status"] == 0
+
+
+def _busy(stream):
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(60_000_000)              # some 30 ms
+
+
+def test_inputs_live_until_another_stream_has_read_them():
+    """Tensors given to a call on another stream may be dropped by the caller right behind it."""
+    cache, m, x = filled((8, 2, 64), 16, [100, 300], [40, 50], seed=31, poison=False)
+    words = torch.tensor([(1 << i + 1) - 1 for n in (40, 50) for i in range(n)], dtype=torch.int64, device=DEV)
+    want = cache.attend(0, x, tree=words)
+    qkv = torch.randn((90, 12 * 64), device=DEV).to(torch.bfloat16)
+    gammas = [(1 + torch.rand(64, device=DEV)).to(torch.bfloat16) for _ in range(2)]
+    pos = torch.arange(90, dtype=torch.int32, device=DEV)
+    want_q = cache.append(1, qkv, gamma_q=gammas[0], gamma_k=gammas[1], pos=pos)
+    want_k = cache.k.clone()
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def dropped(call, *inputs):
+        """call on copies that are freed, and whose memory is written again, before the stream gets to it."""
+        copies = [t.clone() for t in inputs]
+        torch.cuda.synchronize()
+        _busy(st)
+        result = call(*copies)
+        sizes = [(t.shape, t.dtype) for t in copies]
+        del copies
+        again = [torch.full(shape, 1, dtype=dtype, device=DEV) for shape, dtype in sizes]
+        torch.cuda.synchronize()
+        del again
+        return result
+
+    assert torch.equal(dropped(lambda q, t: cache.attend(0, q, tree=t, stream=st), x, words), want)
+    cache.k[1].fill_(0.0)
+    got = dropped(lambda a, b, c, d: cache.append(1, a, gamma_q=b, gamma_k=c, pos=d, stream=st), qkv, *gammas, pos)
+    assert torch.equal(got, want_q)
+    written = cache.k[1] != 0
+    assert torch.equal(cache.k[1][written], want_k[1][written]) and int(written.sum()) > 90 * 2 * 60
+    before = cache.length.tolist()
+    dropped(lambda a, b: cache.accept([0, 1], a, b, stream=st), ints([2, 3]), ints([[0, 4, 9], [1, 2, 7]]))
+    assert cache.length.tolist() == [before[0] - 38, before[1] - 47, 0] and cache.stats()["status"] == 0
+    cache.step([0, 1], [2, 3])
+    out = torch.zeros((5, 512), dtype=torch.bfloat16, device=DEV)      # a result given by the caller
+    torch.cuda.synchronize()
+    _busy(st)
+    cache.attend(0, x[:5], out=out, stream=st)
+    at = out.data_ptr()
+    del out
+    other = torch.full((5, 512), 3.0, dtype=torch.bfloat16, device=DEV)
+    torch.cuda.synchronize()
+    assert (other == 3).all() and other.data_ptr() != at
