@@ -548,12 +548,12 @@ class PagedCache:
             raise TrimmoeError(-1, f"{what}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
 
     def _rows(self, t, cols, what):
-        """Row stride of a [T][cols] tensor."""
+        """Row stride of a [T][cols] tensor (of a single row: its length, whatever a view of it says)."""
         if isinstance(t, self._Tensor) and t.dtype is self._bf16 and t.get_device() == self._index and \
                 t.shape == (self.T, cols):
             ld, one = t.stride()
             if one == 1 or not self.T:
-                return ld if self.T > 1 else max(cols, ld)
+                return ld if self.T > 1 else cols
         self._tensor(t, self._bf16, None, what)
         raise TrimmoeError(-1, f"{what}: expected shape {(self.T, cols)} with contiguous rows, got {tuple(t.shape)}")
 

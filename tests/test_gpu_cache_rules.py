@@ -1,5 +1,5 @@
-"""What the paged cache's header promises beyond single calls: references held from outside, refused steps, inputs on
-other streams."""
+"""What the paged cache promises beyond single calls: references held from outside, refused steps, inputs on other
+streams, rows of any stride."""
 import pytest
 import torch
 
@@ -139,3 +139,20 @@ def test_inputs_live_until_another_stream_has_read_them():
     other = torch.full((5, 512), 3.0, dtype=torch.bfloat16, device=DEV)
     torch.cuda.synchronize()
     assert (other == 3).all() and other.data_ptr() != at
+
+
+def test_the_stride_of_a_single_row_means_nothing():
+    """One token's row cut out of a wider buffer, whatever the buffer's width."""
+    cache, m, _ = filled((4, 2, 64), 16, [37], [1], seed=33, poison=False)
+    wide = torch.randn((3, 1031), device=DEV).to(torch.bfloat16)
+    q, qkv = wide[:1, :256], wide[:1, 512:1024]
+    assert q.stride(0) == 1031 and q.data_ptr() % 16 == 0
+    want = cache.attend(0, q.contiguous())
+    assert torch.equal(cache.attend(0, q), want)
+    out = torch.zeros((2, 259), dtype=torch.bfloat16, device=DEV)
+    cache.attend(0, q, out=out[:1, :256])
+    assert torch.equal(out[:1, :256], want) and (out[0, 256:] == 0).all() and (out[1] == 0).all()
+    want = cache.append(0, qkv.contiguous())
+    assert torch.equal(cache.append(0, qkv), want)
+    cache.append(0, qkv, q_out=qkv[:, :256])       # in place
+    assert torch.equal(qkv[:, :256], want)
