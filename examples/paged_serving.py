@@ -10,10 +10,13 @@ longest path that the model agrees with, and drops the rest of the tree from the
 cache.  Per layer:
 
     q = cache.append(layer, norm(h) Wqkv)     norms, rotation, keys and values into pages
-    h = h + cache.attend(layer, q) Wo         prompts, single tokens or drafted trees
+    h = h + cache.attend(layer, q) Wo         live tokens of prompts, drafted trees, decoding
     engine.layer_step(layer, tokens)          skip / exit / execute and the experts
 
-The weights are random; the projections are plain matrix products.  What a round
+A token that exits keeps the state that entered the layer, and goes on supplying keys
+and values.  (The exit decision reads the state behind this attention; inside the full
+block it reads the one before it.)  The weights are random; the projections are plain
+matrix products.  What a round
 accepts is what decoding one token at a time would have produced, up to rounding.
 """
 import os
@@ -50,13 +53,17 @@ class Model:
         state = W.make_tokens(self.cfg, T=T)
         tok = self.engine.tokens_to_device(state)
         tok["hidden"].copy_(self.embed[ids])
-        h = tok["hidden"]
+        h, alive = tok["hidden"], tok["alive"]
         for layer in range(self.cfg.N):
+            entering, live = h.clone(), (alive != 0)[:, None]
+            # Every token supplies keys and values, also one that has exited; attention runs for live ones.
             x = torch.nn.functional.rms_norm(h, (self.cfg.d,), eps=1e-6)
             q = self.cache.append(layer, x @ self.w_qkv[layer], gamma_q=self.gamma_q[layer], gamma_k=self.gamma_k[layer],
                                   theta=1e4, pos=pos)
-            h += self.cache.attend(layer, q, tree=tree) @ self.w_o[layer]
+            h += torch.where(live, self.cache.attend(layer, q, tree=tree) @ self.w_o[layer], 0)
             self.engine.layer_step(layer, tok)
+            # A token that exits at a layer leaves with the state that entered it.
+            h.copy_(torch.where(live & (alive == 0)[:, None], entering, h))
         return (torch.nn.functional.rms_norm(h, (self.cfg.d,)) @ self.embed.T).argmax(-1)
 
 
