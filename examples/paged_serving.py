@@ -16,8 +16,9 @@ cache.  Per layer:
 A token that exits keeps the state that entered the layer, and goes on supplying keys
 and values.  (The exit decision reads the state behind this attention; inside the full
 block it reads the one before it.)  The weights are random; the projections are plain
-matrix products.  What a round
-accepts is what decoding one token at a time would have produced, up to rounding.
+matrix products.  A token's decisions hang on its own state and on its sequence's access
+server, so what a round accepts is what decoding one token at a time would have
+produced, up to rounding (which can tip a decision that stands at its threshold).
 """
 import os
 import sys
@@ -47,12 +48,14 @@ class Model:
         self.w_o = normal(N, q_heads * head_dim, d, std=(q_heads * head_dim) ** -0.5)
         self.gamma_q, self.gamma_k = (torch.ones(N, head_dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))
 
-    def __call__(self, ids, pos=None, tree=None):
-        """Most likely next token after each of the step's tokens (ids int64 [T])."""
+    def __call__(self, ids, pos=None, tree=None, server=0):
+        """Most likely next token after each of the step's tokens (ids int64 [T]); server: the access server of each
+        token's sequence, where the token starts (decisions hang on it, not on the place in the step)."""
         T = ids.shape[0]
         state = W.make_tokens(self.cfg, T=T)
         tok = self.engine.tokens_to_device(state)
         tok["hidden"].copy_(self.embed[ids])
+        tok["s"][:] = server
         h, alive = tok["hidden"], tok["alive"]
         for layer in range(self.cfg.N):
             entering, live = h.clone(), (alive != 0)[:, None]
@@ -97,10 +100,16 @@ def run(rounds=6, width=3, depth=3, prompts=(200, 37, 130), seed=0, verbose=True
     model = Model(cfg, heads, kv_heads, head_dim, vocab, cache, engine, seed)
     rng = np.random.default_rng(seed)
     text = [rng.integers(0, vocab, p).tolist() for p in prompts]
+    server = np.random.default_rng([seed, 1]).integers(0, cfg.M, len(prompts)).tolist()
+    server.append(server[0])
+
+    def start(per_sequence):
+        """Access server of each packed token."""
+        return torch.tensor(np.repeat(server[:len(per_sequence)], per_sequence), dtype=torch.uint8, device="cuda")
 
     # Prefill: all prompts in one step.
     cache.step(range(len(prompts)), prompts)
-    following = model(torch.tensor(sum(text, []), device="cuda"))
+    following = model(torch.tensor(sum(text, []), device="cuda"), server=start(prompts))
     ends = np.cumsum(prompts) - 1
     for s, t in enumerate(following[torch.tensor(ends, device="cuda")].tolist()):
         text[s].append(t)
@@ -125,7 +134,8 @@ def run(rounds=6, width=3, depth=3, prompts=(200, 37, 130), seed=0, verbose=True
                 d.append(int(rng.integers(0, vocab)) if guess is None else guess)
             drafts.append(d)
         pos = torch.tensor([b + k for b in base for k in deep], dtype=torch.int32, device="cuda")
-        after = model(torch.tensor(sum(drafts, []), device="cuda"), pos=pos, tree=tree).view(n, m).tolist()
+        after = model(torch.tensor(sum(drafts, []), device="cuda"), pos=pos, tree=tree, server=start([m] * n))
+        after = after.view(n, m).tolist()
         paths = [longest_path(drafts[s], after[s], parent) for s in range(n)]
         table = torch.tensor([p + [0] * (depth + 1 - len(p)) for p in paths], dtype=torch.int32, device="cuda")
         cache.accept(range(n), torch.tensor([len(p) for p in paths], dtype=torch.int32, device="cuda"), table)
