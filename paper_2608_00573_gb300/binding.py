@@ -510,8 +510,6 @@ class PagedCache:
                 raise TrimmoeError(-1, "cache: tensors must be contiguous")
         self.k, self.v, self.table, self.length, self.ref = k, v, table, length, ref
         self.T = 0
-        if self.device.type == "cuda" and self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
         self._q_cols, self._qkv_cols = self.q_heads * self.head_dim, (self.q_heads + 2 * self.kv_heads) * self.head_dim
         cfg = trimmoe_cache_config(layers=self.layers, q_heads=self.q_heads, kv_heads=self.kv_heads,
