@@ -10,10 +10,12 @@ constexpr int kCacheMaxSeqs = 1024;
 constexpr int kCacheTile = 128;        // rows of a query tile, keys of a key tile
 constexpr int kTreeMax = 64;           // drafted tokens of a sequence (mask bits)
 // Up to this many rows of an item, the CTA that writes a cut item's last part joins
-// them (a decode step then is one launch: one sequence of 1500 positions 11.9 us, with a
-// second kernel it took 19.3); above, a second kernel does, with a CTA per 32 rows (a
-// 777-token prompt of 12 heads 15.4 us; when it took 20, joining in the CTAs took 40).
-constexpr int kJoinHereRows = 32;
+// them, and a step is one launch; above, a second kernel does, with a CTA per 32 rows.
+// Here against there, 32 heads on 8, one sequence of 6000 positions: 8 rows 17.4 us
+// against 25.6, 16 rows 21.4 / 25.7, 24 rows 25.6 / 25.7, 32 rows 30.7 / 25.5, 128 rows
+// 86 / 26; 8 sequences of 1000 to 8000: 8 rows 37.7 / 39.2, 16 rows 39.9 / 39.0, 24 rows
+// 42.6 / 39.7, 32 rows 45.2 / 39.4.
+constexpr int kJoinHereRows = 16;
 
 // One listed sequence of the current step.
 struct CacheSeq {
