@@ -10,13 +10,14 @@
 // token and one or more batches of heads (4 per lane group, all queries, all keys or
 // all values); gamma and the rotation are multiplied once per token and kind of head,
 // after which an element costs three operations.  The phase pos * (theta^(-2i/D) / 2 pi)
-// is formed modulo one turn in 64-bit fixed point, exact to 2^-33 turns for any int32
-// position, so no table is read and long positions lose nothing; sine and cosine of
+// is formed modulo one turn in 64-bit fixed point, from the turns per position in double:
+// off by at most 2^-32 + pos 2^-55 turns for a position >= 0 (2^-25 at 2^30), so no table
+// is read and long positions lose nothing that bf16 shows; sine and cosine of
 // the remainder are the hardware's (off by at most 2^-20 of the pair, bf16 rounds at 2^-8).
 //
 // Bound: HBM, (Hq + 2 Hkv) D 2 bytes read and written per token; a small step is bound
 // by latency, and its tokens' batches go to different warps.  Measured (32 query heads on 8,
-// D = 128, pages of 64): 16384 tokens 61.2 us, 6.3 TB/s, 0.92 of the copy rate; 113 tokens
+// D = 128, pages of 64): 16384 tokens 61.6 us, 6.2 TB/s, 0.92 of the copy rate; 113 tokens
 // 2.8 us on the GPU.
 #include <algorithm>
 

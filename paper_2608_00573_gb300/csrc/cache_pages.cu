@@ -250,6 +250,12 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     const long long before_mine = block_scan(cost, s_wsl, total);
     two = __syncthreads_or(two);
     const long long W = total * c.Hkv;
+    // Whole items from two of the largest per CTA on.  Neither side is better throughout: with
+    // equal items a last round that is half empty costs more than cutting them, with the
+    // mixed ones of prompts it does not.  Factor 1 / 2 / 4 / never whole: 20 equal contexts
+    // of 4000 (160 items) 83 / 59 / 59 / 59 us, 39 of them 125 / 125 / 104 / 104, 40 of 900
+    // at 12 heads 46 / 46 / 54 / 54; 5 prompts of 1000 61 / 61 / 93 / 93, one of 4096
+    // 118 / 165 / 165 / 165, chunks behind prefixes 207 / 219 / 219 / 219.
     const bool whole = 2LL * s_most * c.num_sms <= W;
     const int n_ctas = !W || whole ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles << (two ? 1 : 0))));
     if (whole) {
