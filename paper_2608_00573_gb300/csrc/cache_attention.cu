@@ -17,8 +17,8 @@
 // the type of the tensor cores' other operand; l sums p in fp32 before that rounding (sums
 // of the rounded values cost 11 % of a long prompt).  m starts as the maximum of the first
 // keys that the row sees, whose p then is 1 and rounds to itself: a row that sees one key
-// gives its value exactly.  Over hundreds of keys the error against 64 bits is 0.0020 to
-// 0.0023 of the result's size, 1.2 to 1.4 times that of the output's rounding alone
+// gives its value exactly.  Over hundreds of keys the error against 64 bits is 0.0019 to
+// 0.0024 of the result's size, 1.1 to 1.45 times that of the output's rounding alone
 // (0.0016 to 0.0017, all that is left with P in 32 bits).
 //
 // A CTA holds two query tiles in flight ("slots", each with its own S and O in
@@ -50,7 +50,7 @@
 // heads on 8, D = 128): a 16384-token prompt 1.46 to 1.53 ms (by the clock that the power
 // cap leaves), 1.44 to 1.51 PFLOP/s, 0.75 to 0.78 of cuBLAS; 7 sequences of 30k to 65k
 // positions, a token each, 199 us, 0.98 of the copy rate; one sequence of 1500 positions
-// 11.7 to 13.0 us, launches and latencies.
+// 11.7 to 14.2 us, launches and latencies.
 #include <algorithm>
 #include <cstddef>
 
