@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     two = __syncthreads_or(two);
     const long long W = total * c.Hkv;
     // Whole items from two of the largest per CTA on.  Neither side is better throughout: with
-    // equal items a last round that is half empty costs more than cutting them, with the
+    // equal items a last turn that few CTAs have costs more than cutting them, with the
     // mixed ones of prompts it does not.  Factor 1 / 2 / 4 / never whole: 20 equal contexts
     // of 4000 (160 items) 83 / 59 / 59 / 59 us, 39 of them 125 / 125 / 104 / 104, 40 of 900
     // at 12 heads 46 / 46 / 54 / 54; 5 prompts of 1000 61 / 61 / 93 / 93, one of 4096
