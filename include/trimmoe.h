@@ -64,7 +64,8 @@ enum {
     TRIMMOE_DEVERR_CACHE_ATTENTION = 7, /* cache attention kernel */
     TRIMMOE_DEVERR_CACHE_FULL = 8,     /* step: too few free pages, or a sequence longer than max_pages */
     TRIMMOE_DEVERR_CACHE_STATE = 9,    /* table, length or ref hold values that no call writes */
-    TRIMMOE_DEVERR_CACHE_PATH = 10     /* accept: n_acc or a path that does not fit the sequence's drafts */
+    TRIMMOE_DEVERR_CACHE_PATH = 10,    /* accept: n_acc or a path that does not fit the sequence's drafts */
+    TRIMMOE_DEVERR_CACHE_BLOCKS = 11   /* attend_blocks: a list that is not ascending columns before the step */
 };
 
 enum { TRIMMOE_EXEC = 0, TRIMMOE_SKIP = 1, TRIMMOE_EXIT = 2, TRIMMOE_DEAD = 3 };
@@ -546,6 +547,85 @@ typedef struct {
 } trimmoe_attend_args;
 
 trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer, const trimmoe_attend_args* a, void* stream);
+
+/* ---- attention that does not read all of the cache for every sequence ---- */
+
+/* Sequences of the step that share a prompt, after trimmoe_cache_step and before its
+ * attention: the first counts[0] listed sequences form a group, the next counts[1]
+ * another one, and so on (host array; counts >= 1, their sum is the number of listed
+ * sequences).  Until the next step trimmoe_cache_attend reads the pages that all of a group's
+ * sequences with new tokens have in common at their front (whole multiples of 128
+ * positions, found on the GPU from table) once for the group, and the rest for each
+ * sequence.  The result is that of the call without groups, up to the order of
+ * fp32 sums.  A group of one sequence, or without common pages, is right too.
+ * A step of more than 65536 query rows (tokens times q_heads) is attended as
+ * without groups: its products are the bound there.
+ * The first call allocates workspaces (about 180 MB at head_dim 128) and so must not be
+ * captured; later ones may be. */
+trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, const int32_t* counts, void* stream);
+
+/* Bounds of the keys of whole pages ("blocks"), for trimmoe_cache_select: per layer, page,
+ * key/value head and key column d the least and the largest value, lo and hi, in 8 bits.
+ *  codes int8 [layers][n_pages][kv_heads][2][head_dim] (lo, then hi), scales fp32
+ *  [layers][n_pages][kv_heads]; device, the caller's, codes 16-byte aligned; both NULL: none.
+ * scale is the least power of two >= 2^-126 of which no |key| of the page and head is more
+ * than 127 times; codes are floor(lo / scale) and ceil(hi / scale).  A page with an
+ * infinity or a NaN among its keys has scale +infinity and codes 0.
+ * From this call on accept recomputes what it moves, and compact takes the bounds along
+ * with the pages.  No work is queued. */
+trimmoe_status trimmoe_cache_set_bounds(trimmoe_cache_handle c, int8_t* codes, float* scales);
+
+/* Bounds of one layer's pages that the step's new tokens filled to their end (whole != 0:
+ * of all full pages of the step's sequences), from the keys that append has
+ * written: call it behind append in every step of a layer that selects blocks. */
+trimmoe_status trimmoe_cache_summarize(trimmoe_cache_handle c, int layer, int whole, void* stream);
+
+/* Arguments of trimmoe_cache_select (device pointers; q 16-byte aligned, row stride in
+ * elements and a multiple of 8).
+ *  q bf16 [T][ld_q]: queries as append leaves them;
+ *  n >= 1: columns per list; first, last >= 0, first + last <= n;
+ *  blocks int32 [T][kv_heads][n].
+ * The blocks of a token are the F = positions before the step / page_size whole pages at
+ * the front of its sequence, by column of its page table.  A list holds all F columns
+ * if F <= n, else the first `first` ones, the last `last` ones and of the others those of
+ * highest score (equal ones: the lower column); in ascending order, -1 behind them.
+ *  score(b) = scale_b max_h u_h sum_d max(c_hd lo_bd, c_hd hi_bd)
+ * over the query heads h of the key/value head, lo and hi as 8-bit codes; u_h is the unit of
+ * head h's query (like scale, from its largest |value|) and c_hd = q_hd / u_h rounded to
+ * the nearest whole number, halves to even.  Every sum is a whole number below 2^24, so
+ * scores are exact.  A block with scale +infinity scores +infinity; a head whose query
+ * holds an infinity or a NaN scores 0 everywhere. */
+typedef struct {
+    const void* q;
+    int ld_q;
+    int n, first, last;
+    int32_t* blocks;
+} trimmoe_select_args;
+
+/* Needs trimmoe_cache_set_bounds and max_pages <= 40960. */
+trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer, const trimmoe_select_args* a, void* stream);
+
+/* Arguments of trimmoe_cache_attend_blocks (device pointers as for attend).
+ *  q, out, tree, scale as for trimmoe_cache_attend; blocks int32 [T][kv_heads][n], n >= 0.
+ * A token sees the positions of the pages in its list, for each key/value head, and of the
+ * positions from the step's first page on (positions before the step / page_size, rounded
+ * down, times page_size) those that trimmoe_cache_attend would show it.  A list holds
+ * ascending columns of whole pages before the step, then -1: of other entries (not
+ * ascending, no whole page before the step, behind a -1) those that do not fit are left
+ * out and CACHE_BLOCKS is flagged. */
+typedef struct {
+    const void* q;
+    int ld_q;
+    const int32_t* blocks;
+    int n;
+    void* out;
+    int ld_out;
+    const uint64_t* tree;
+    float scale;
+} trimmoe_blocks_args;
+
+trimmoe_status trimmoe_cache_attend_blocks(trimmoe_cache_handle c, int layer, const trimmoe_blocks_args* a,
+                                           void* stream);
 
 /* Make sequences dst[i] continuations of src[i]: dst's pages are released, then
  * it shares all of src's (host arrays; dst distinct, none of them a source). */

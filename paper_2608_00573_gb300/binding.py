@@ -118,6 +118,16 @@ class trimmoe_attend_args(C.Structure):
                 ("tree", C.c_void_p), ("scale", C.c_float)]
 
 
+class trimmoe_select_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ld_q", C.c_int), ("n", C.c_int), ("first", C.c_int), ("last", C.c_int),
+                ("blocks", C.c_void_p)]
+
+
+class trimmoe_blocks_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ld_q", C.c_int), ("blocks", C.c_void_p), ("n", C.c_int), ("out", C.c_void_p),
+                ("ld_out", C.c_int), ("tree", C.c_void_p), ("scale", C.c_float)]
+
+
 class trimmoe_cache_stats_t(C.Structure):
     _fields_ = [("device_error", C.c_int), ("free_pages", C.c_int), ("launches", C.c_uint64)]
 
@@ -128,7 +138,9 @@ EXPORTS = ("trimmoe_create", "trimmoe_layer_step", "trimmoe_forward", "trimmoe_f
            "trimmoe_calibration_end", "trimmoe_replicate", "trimmoe_watchdog_selftest",
            "trimmoe_cache_create", "trimmoe_cache_step", "trimmoe_cache_append", "trimmoe_cache_attend",
            "trimmoe_cache_fork", "trimmoe_cache_truncate", "trimmoe_cache_accept", "trimmoe_cache_compact",
-           "trimmoe_cache_stats", "trimmoe_cache_last_error", "trimmoe_cache_destroy")
+           "trimmoe_cache_stats", "trimmoe_cache_last_error", "trimmoe_cache_destroy",
+           "trimmoe_cache_share", "trimmoe_cache_set_bounds", "trimmoe_cache_summarize", "trimmoe_cache_select",
+           "trimmoe_cache_attend_blocks")
 
 _lib = None
 _lock = threading.Lock()
@@ -453,7 +465,9 @@ def _cache_lib():
         for name, args in (("create", [vp, vp, C.POINTER(vp)]), ("step", [vp, i, vp, vp, vp]),
                            ("append", [vp, i, vp, vp]), ("attend", [vp, i, vp, vp]), ("fork", [vp, i, vp, vp, vp]),
                            ("truncate", [vp, i, vp, vp, vp]), ("accept", [vp, i, vp, vp, vp, i, vp]),
-                           ("compact", [vp, vp]), ("stats", [vp, vp, i])):
+                           ("compact", [vp, vp]), ("stats", [vp, vp, i]), ("share", [vp, i, vp, vp]),
+                           ("set_bounds", [vp, vp, vp]), ("summarize", [vp, i, i, vp]), ("select", [vp, i, vp, vp]),
+                           ("attend_blocks", [vp, i, vp, vp])):
             f = getattr(L, "trimmoe_cache_" + name)
             f.argtypes, f.restype = args, i
         L.trimmoe_cache_last_error.argtypes = [vp]
@@ -476,7 +490,9 @@ class PagedCache:
     Owns a trimmoe_cache handle and borrows the caller's tensors (all on one
     GPU, contiguous): k, v bfloat16 [layers][n_pages][kv_heads][page][head_dim],
     table int32 [max_seqs][max_pages] (-1: none), length int32 [max_seqs], ref
-    int32 [n_pages].  ``PagedCache.empty`` makes them for a new cache.  Calls are
+    int32 [n_pages]; bounds, for ``summarize`` and ``select``: int8 [layers][n_pages]
+    [kv_heads][2][head_dim] and float32 [layers][n_pages][kv_heads].
+    ``PagedCache.empty`` makes them for a new cache.  Calls are
     queued on the current stream (or ``stream``); see include/trimmoe.h for
     their rules.  Sequence lists are host sequences of ints.  With ``stream``, what
     wrote the inputs has to be ordered before the call and what reads the result
@@ -484,7 +500,7 @@ class PagedCache:
     other uses until that stream has read them, and a result is of that stream.
     """
 
-    def __init__(self, k, v, table, length, ref, q_heads: int, T_max: int):
+    def __init__(self, k, v, table, length, ref, q_heads: int, T_max: int, bounds=None):
         import torch
         self.torch = torch
         self.handle = None
@@ -494,6 +510,9 @@ class PagedCache:
         self._Tensor, self._empty, self._int32, self._int64 = torch.Tensor, torch.empty, torch.int32, torch.int64
         self._append_args, self._attend_args = trimmoe_append_args(), trimmoe_attend_args()
         self._append_at, self._attend_at = C.addressof(self._append_args), C.addressof(self._attend_args)
+        self._select_args, self._blocks_args = trimmoe_select_args(), trimmoe_blocks_args()
+        self._select_at, self._blocks_at = C.addressof(self._select_args), C.addressof(self._blocks_args)
+        self._c_select, self._c_blocks = self._lib.trimmoe_cache_select, self._lib.trimmoe_cache_attend_blocks
         self._c_append, self._c_attend = self._lib.trimmoe_cache_append, self._lib.trimmoe_cache_attend
         if k.dim() != 5 or k.shape != v.shape or table.dim() != 2 or length.dim() != 1 or ref.dim() != 1:
             raise TrimmoeError(-1, "cache: k and v are [layers][n_pages][kv_heads][page][head_dim], table is "
@@ -509,6 +528,7 @@ class PagedCache:
             if not t.is_contiguous():
                 raise TrimmoeError(-1, "cache: tensors must be contiguous")
         self.k, self.v, self.table, self.length, self.ref = k, v, table, length, ref
+        self.codes = self.scales = None
         self.T = 0
         self._index = self.device.index
         self._q_cols, self._qkv_cols = self.q_heads * self.head_dim, (self.q_heads + 2 * self.kv_heads) * self.head_dim
@@ -518,18 +538,22 @@ class PagedCache:
         st = trimmoe_cache_state(k=_ptr(k), v=_ptr(v), table=_ptr(table), length=_ptr(length), ref=_ptr(ref))
         with torch.cuda.device(self.device):
             self.handle = trimmoe_cache_create(cfg, st)
+        if bounds is not None:
+            self.set_bounds(*bounds)
 
     @classmethod
     def empty(cls, layers: int, n_pages: int, q_heads: int, kv_heads: int, head_dim: int, page: int, max_seqs: int,
-              max_pages: int, T_max: int, device="cuda"):
-        """A cache of n_pages free pages (page contents are left unset)."""
+              max_pages: int, T_max: int, device="cuda", bounds: bool = False):
+        """A cache of n_pages free pages (page contents are left unset); bounds: with bounds of the pages' keys."""
         import torch
         shape = (layers, n_pages, kv_heads, page, head_dim)
         return cls(torch.empty(shape, dtype=torch.bfloat16, device=device),
                    torch.empty(shape, dtype=torch.bfloat16, device=device),
                    torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device),
                    torch.zeros(max_seqs, dtype=torch.int32, device=device),
-                   torch.zeros(n_pages, dtype=torch.int32, device=device), q_heads, T_max)
+                   torch.zeros(n_pages, dtype=torch.int32, device=device), q_heads, T_max,
+                   (torch.zeros(shape[:3] + (2, head_dim), dtype=torch.int8, device=device),
+                    torch.zeros(shape[:3], dtype=torch.float32, device=device)) if bounds else None)
 
     # checks and calls ------------------------------------------------------
     # A decode step calls append and attend once per layer, and on the GPU they take a
@@ -563,6 +587,14 @@ class PagedCache:
                 (n < 2 or t.stride(0) == 1)):
             self._tensor(t, dtype, (n,), what)
         return t.data_ptr()
+
+    def _lists(self, t, what):
+        """Columns per list of block lists [T][kv_heads][n]."""
+        if not (isinstance(t, self._Tensor) and t.dtype is self._int32 and t.get_device() == self._index and t.dim() == 3 and
+                t.shape[0] == self.T and t.shape[1] == self.kv_heads and t.is_contiguous()):
+            self._tensor(t, self._int32, None, what)
+            raise TrimmoeError(-1, f"{what}: blocks are a contiguous tensor of shape {(self.T, self.kv_heads, 'n')}")
+        return t.shape[2]
 
     def _new(self, cols, stream):
         """A [T][cols] result, allocated on the stream that writes it."""
@@ -659,6 +691,72 @@ class PagedCache:
             self._done(rc)
         if stream is not None:
             self._keep(stream, q, out, tree)
+        return out
+
+    def set_bounds(self, codes, scales):
+        """Where the bounds of the pages' keys lie (None, None: nowhere); what is there counts as theirs."""
+        shape = (self.layers, self.n_pages, self.kv_heads)
+        self._tensor(codes, self.torch.int8, shape + (2, self.head_dim), "set_bounds")
+        self._tensor(scales, self.torch.float32, shape, "set_bounds")
+        self._done(self._lib.trimmoe_cache_set_bounds(self.handle, _ptr(codes), _ptr(scales)))
+        self.codes, self.scales = codes, scales
+
+    def share(self, counts, stream=None):
+        """The step's first counts[0] listed sequences share a prompt, the next counts[1] do, and so on: until the next
+        step, attend reads the pages that a group's sequences have in common once for all of them."""
+        counts = self._list(counts)
+        self._done(self._lib.trimmoe_cache_share(self.handle, counts[2], counts[1], self._stream(stream)))
+
+    def summarize(self, layer: int, whole: bool = False, stream=None):
+        """Bounds of the keys of the pages that the step's tokens filled (whole: of all full pages of its sequences);
+        behind append, in every step of a layer that selects blocks."""
+        self._done(self._lib.trimmoe_cache_summarize(self.handle, layer, int(whole), self._stream(stream)))
+
+    def select(self, layer: int, q, n: int, first: int = 1, last: int = 1, out=None, stream=None):
+        """Lists of n whole pages before the step for each token and key/value head, int32 [T][kv_heads][n] (columns of
+        the page table, ascending, -1 behind): the first and last ones, and those whose bounds promise most."""
+        a = self._select_args
+        a.ld_q = self._rows(q, self._q_cols, "select")
+        shape = (self.T, self.kv_heads, max(0, n))
+        if out is None:
+            if stream is None:
+                out = self._empty(shape, dtype=self._int32, device=self.device)
+            else:
+                with self.torch.cuda.stream(stream):
+                    out = self._empty(shape, dtype=self._int32, device=self.device)
+        else:
+            self._tensor(out, self._int32, shape, "select")
+        a.q = q.data_ptr()
+        a.n, a.first, a.last = n, first, last
+        a.blocks = out.data_ptr()
+        rc = self._c_select(self.handle, layer, self._select_at, self._stream(stream))
+        if rc:
+            self._done(rc)
+        if stream is not None:
+            self._keep(stream, q, out)
+        return out
+
+    def attend_blocks(self, layer: int, q, blocks, out=None, tree=None, scale: float = 0.0, stream=None):
+        """Attention of the step's queries over the pages in `blocks` (lists as ``select`` writes them) and over the
+        positions from the step's first page on, the latter as ``attend`` shows them."""
+        a, cols = self._blocks_args, self._q_cols
+        a.ld_q = self._rows(q, cols, "attend_blocks")
+        a.n = self._lists(blocks, "attend_blocks")
+        if out is None:
+            out = self._new(cols, stream)
+            a.ld_out = cols
+        else:
+            a.ld_out = self._rows(out, cols, "attend_blocks")
+        a.tree = self._vector(tree, self._int64, self.T, "attend_blocks")
+        a.q = q.data_ptr()
+        a.blocks = blocks.data_ptr()
+        a.out = out.data_ptr()
+        a.scale = scale
+        rc = self._c_blocks(self.handle, layer, self._blocks_at, self._stream(stream))
+        if rc:
+            self._done(rc)
+        if stream is not None:
+            self._keep(stream, q, blocks, out, tree)
         return out
 
     def fork(self, src, dst, stream=None):

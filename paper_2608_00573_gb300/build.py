@@ -16,7 +16,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libtrimmoe.so")
 SOURCES = ["trimmoe.cu", "router.cu", "decide.cu", "compact.cu", "grouped_gemm.cu", "combine.cu", "attention.cu",
-           "feedback.cu", "watchdog.cu", "cache.cu", "cache_pages.cu", "cache_append.cu", "cache_attention.cu"]
+           "feedback.cu", "watchdog.cu", "cache.cu", "cache_pages.cu", "cache_append.cu", "cache_attention.cu",
+           "cache_blocks.cu", "cache_select.cu", "cache_blocks_attention.cu", "cache_share.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -36,7 +37,8 @@ def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
     t = os.path.getmtime(obj)
-    deps = [src, os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "cache.cuh"), os.path.join(ROOT, "include", "trimmoe.h")]
+    deps = [src, os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "cache.cuh"), os.path.join(CSRC, "cache_host.cuh"),
+            os.path.join(ROOT, "include", "trimmoe.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

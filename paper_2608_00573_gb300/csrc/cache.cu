@@ -3,66 +3,10 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
-#include <vector>
 
-#include <nvtx3/nvToolsExt.h>
-
-#include "cache.cuh"
-
-using namespace tmoe;
-
-struct trimmoe_cache {
-    trimmoe_cache_config cfg;
-    CacheDev d;
-    int dev = 0;
-    std::string err;
-    std::vector<void*> allocs;
-    std::vector<CUtensorMap> tm_k, tm_v;      // per layer: rows [n_pages * kv_heads * page][head_dim], one page and head a box
-    std::vector<uint32_t> stamp;              // per sequence: last call that listed it
-    uint32_t call = 0;
-    cudaStream_t last_stream = nullptr;
-    uint64_t launches = 0;
-    int T = -1, n = 0, max_q = 0;             // the current step (T < 0: none)
-    float theta = 0.f;                        // base of turn[]
-    uint64_t turn[64];
-
-    // Keeps "what: why" (nothing when there is no memory for it: no exception leaves a call).
-    trimmoe_status fail(trimmoe_status s, const char* what, const char* why) noexcept {
-        try {
-            err.assign(what).append(": ").append(why);
-        } catch (...) {
-            err.clear();
-        }
-        return s;
-    }
-    trimmoe_status launched(cudaError_t e, int n_kernels, const char* what) noexcept {
-        if (e == cudaSuccess) e = cudaGetLastError();
-        if (e != cudaSuccess) return fail(TRIMMOE_ERR_CUDA, what, cudaGetErrorString(e));
-        launches += n_kernels;
-        return TRIMMOE_OK;
-    }
-};
+#include "cache_host.cuh"
 
 namespace {
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// The handle's device for the duration of a call.
-struct OnDevice {
-    int prev = -1, dev;
-    explicit OnDevice(int d) : dev(d) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        if (prev != dev) cudaSetDevice(dev);
-    }
-    ~OnDevice() {
-        if (prev >= 0 && prev != dev) cudaSetDevice(prev);
-    }
-};
-
-struct Range {
-    explicit Range(const char* name) { nvtxRangePushA(name); }
-    ~Range() { nvtxRangePop(); }
-};
 
 trimmoe_status check_config(const trimmoe_cache_config& c, const char*& why) {
     auto bad = [&](trimmoe_status s, const char* m) {
@@ -85,13 +29,13 @@ trimmoe_status check_config(const trimmoe_cache_config& c, const char*& why) {
     return TRIMMOE_OK;
 }
 
-// Pool rows of one layer, a box of one page and head by 64 columns.
-bool pool_map(CUtensorMap* tm, const void* base, const CacheDev& d) {
+// Pool rows of one layer, a box of `rows` rows of a page and head by 64 columns.
+bool pool_map(CUtensorMap* tm, const void* base, const CacheDev& d, int rows) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[2] = {(cuuint64_t)d.dh, (cuuint64_t)d.n_pages * d.Hkv * d.page};
     cuuint64_t strides[1] = {(cuuint64_t)d.dh * 2};
-    cuuint32_t box[2] = {64, (cuuint32_t)d.page};
+    cuuint32_t box[2] = {64, (cuuint32_t)rows};
     cuuint32_t es[2] = {1, 1};
     return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -128,20 +72,6 @@ trimmoe_status check_list(trimmoe_cache* c, const char* what, int n, const int32
         c->stamp[seq[i]] = c->call;
     }
     return TRIMMOE_OK;
-}
-
-trimmoe_status check_layer(trimmoe_cache* c, const char* what, int layer) {
-    if (layer < 0 || layer >= c->cfg.layers) return c->fail(TRIMMOE_ERR_ARG, what, "layer out of range");
-    if (c->T < 0) return c->fail(TRIMMOE_ERR_ARG, what, "no step has been begun");
-    return TRIMMOE_OK;
-}
-
-// Sets up a call on `stream` (after its checks): clears an error that other code
-// left behind, so that the launches' own are seen.
-cudaStream_t enter(trimmoe_cache* c, void* stream) {
-    cudaGetLastError();
-    c->last_stream = (cudaStream_t)stream;
-    return c->last_stream;
 }
 
 }  // namespace
@@ -209,13 +139,14 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
                 p = static_cast<std::remove_reference_t<decltype(p)>>(q);
             }
         };
-        c->allocs.reserve(16);
+        c->allocs.reserve(24);
         alloc(d.plan, 1);
         alloc(d.seqs, kCacheMaxSeqs);
         alloc(d.groups, (size_t)cfg->T_max / (2 * d.tile_tokens) + cfg->max_seqs + 1);
         alloc(d.shares, (size_t)d.num_sms);
         alloc(d.slot, cfg->T_max);
         alloc(d.pos, cfg->T_max);
+        alloc(d.owner, cfg->T_max);
         alloc(d.copies, (size_t)std::max(cfg->n_pages, cfg->max_seqs));
         alloc(d.fresh, cfg->n_pages);
         alloc(d.base, cfg->max_seqs);
@@ -236,12 +167,16 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         if (e == cudaSuccess) e = cudaMemcpy(d.base, d.length, sizeof(int) * (size_t)cfg->max_seqs, cudaMemcpyDeviceToDevice);
         if (e == cudaSuccess) e = cudaDeviceSynchronize();
         if (e != cudaSuccess) return bail(TRIMMOE_ERR_CUDA, cudaGetErrorString(e));
-        c->tm_k.resize(cfg->layers);
-        c->tm_v.resize(cfg->layers);
         const size_t layer = (size_t)d.n_pages * d.Hkv * d.page * d.dh;
-        for (int l = 0; l < cfg->layers; ++l)
-            if (!pool_map(&c->tm_k[l], d.k + l * layer, d) || !pool_map(&c->tm_v[l], d.v + l * layer, d))
-                return bail(TRIMMOE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+        auto maps = [&](std::vector<CUtensorMap>& k, std::vector<CUtensorMap>& v, int rows) {
+            k.resize(cfg->layers);
+            v.resize(cfg->layers);
+            for (int l = 0; l < cfg->layers; ++l)
+                if (!pool_map(&k[l], d.k + l * layer, d, rows) || !pool_map(&v[l], d.v + l * layer, d, rows)) return false;
+            return true;
+        };
+        if (!maps(c->tm_k, c->tm_v, d.page) || (d.page > 64 && !maps(c->tm_k64, c->tm_v64, 64)))
+            return bail(TRIMMOE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
     } catch (const std::bad_alloc&) {
         return bail(TRIMMOE_ERR_OOM, "host allocation failed");
     }
@@ -271,6 +206,7 @@ extern "C" trimmoe_status trimmoe_cache_step(trimmoe_cache_handle c, int n, cons
     c->T = (int)T;
     c->n = n;
     c->max_q = most;
+    c->d.shared = 0;
     return TRIMMOE_OK;
 }
 
@@ -344,10 +280,12 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
     p.ld_out = a->ld_out;
     p.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)d.dh)) * 1.4426950408889634f;
     const int max_rows = c->max_q > d.tile_tokens ? 2 * kCacheTile : c->max_q * d.rep;
-    p.join_here = max_rows <= kJoinHereRows;
+    p.join_here = !d.shared && max_rows <= kJoinHereRows;
+    p.T = c->T;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_attend");
-    return c->launched(launch_cache_attend(d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows, enter(c, stream)),
+    return c->launched(launch_cache_attend(d.shared ? c->share : d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows,
+                                           enter(c, stream)),
                        p.join_here ? 1 : 2, "cache_attend");
 }
 
@@ -396,7 +334,8 @@ extern "C" trimmoe_status trimmoe_cache_accept(trimmoe_cache_handle c, int n, co
     c->T = -1;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_accept");
-    return c->launched(launch_cache_accept(c->d, n, seq, n_acc, path, ld_path, enter(c, stream)), 2, "cache_accept");
+    return c->launched(launch_cache_accept(c->d, n, seq, n_acc, path, ld_path, enter(c, stream)), c->d.codes ? 3 : 2,
+                       "cache_accept");
 }
 
 extern "C" trimmoe_status trimmoe_cache_compact(trimmoe_cache_handle c, void* stream) {
@@ -439,6 +378,8 @@ extern "C" trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_ca
         return c->fail(TRIMMOE_ERR_CACHE, "cache", "table, length or ref hold invalid values");
     if (code == TRIMMOE_DEVERR_CACHE_PATH)
         return c->fail(TRIMMOE_ERR_CACHE, "cache_accept", "n_acc or path does not fit the drafts");
+    if (code == TRIMMOE_DEVERR_CACHE_BLOCKS)
+        return c->fail(TRIMMOE_ERR_CACHE, "cache_attend_blocks", "a list is not ascending columns before the step");
     return code ? c->fail(TRIMMOE_ERR_CACHE, "cache", "device error") : TRIMMOE_OK;
 }
 

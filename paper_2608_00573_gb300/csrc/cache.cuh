@@ -33,7 +33,10 @@ struct __align__(16) CacheGroup {
     int row, ntok;                     // first packed token, tokens
     int first;                         // position of the first token
     int base;                          // positions before the step
-    int pad[3];
+    // Steps with groups of sequences (trimmoe_cache_share):
+    int t0;                            // first key tile: those before it are the group of sequences' common ones
+    int common;                        // the item is of those tiles, for all tokens of the group: kv_len and base end them
+    int part_row;                      // its parts' first row, see cache_part_row
 };
 
 // A CTA's share of the line on which the items' costs are laid end to end.
@@ -72,6 +75,21 @@ __host__ __device__ inline int cache_tiles_before(long long x, int cost, int two
     return (int)(x >= cost || t > n ? n : t);
 }
 
+// Rows of a part of an item, in a step with groups of sequences.  From 32 on they are whole
+// warps, stored 32 rows of 4 columns side by side; fewer are stored row by row.
+__host__ __device__ inline int cache_part_rows(int ntok, int tile_tokens, int rep) {
+    if (ntok > tile_tokens) return kCacheTile + (((ntok - tile_tokens) * rep + 31) & ~31);
+    return ntok * rep < 32 ? ntok * rep : (ntok * rep + 31) & ~31;
+}
+// The part of the group's item of key/value head `head` that CTA `cta` computes begins at row
+// g.part_row + (head + cta) * cache_part_rows(g): along the line of items head and CTA both
+// grow, so their sum names the pieces.
+
+// The CTA whose share of a line of cost W holds x: shares are [W b / n, W (b + 1) / n).
+__host__ __device__ inline int cache_cta_of(long long x, long long W, int n) {
+    return (int)(((x + 1) * n + W - 1) / W) - 1;
+}
+
 // The handle's device state, passed to every kernel by value.
 struct CacheDev {
     int layers, Hq, Hkv, rep, dh, page, page_shift, n_pages, max_seqs, max_pages, T_max;
@@ -85,6 +103,7 @@ struct CacheDev {
     CacheShare* shares;                // [num_sms]
     int* slot;                         // [T_max] page row (page * page_size + place) of each new token, -1 none
     int* pos;                          // [T_max] its position in its sequence
+    int* owner;                        // [T_max] its place in seqs
     int2* copies;                      // [max(n_pages, max_seqs)] (from, to) pages
     int* fresh;                        // [n_pages] free pages taken by a step; new place of each page (compact)
     int* base;                         // [max_seqs] length before the sequence's last step
@@ -94,6 +113,14 @@ struct CacheDev {
     float* part_o;                     // [2 num_sms][256][dh] sums of p v (order within: cache_attention.cu)
     float2* part_ml;                   // [2 num_sms][256] row maxima and sums of p
     int* arrived;                      // [num_sms] parts written of the item that a CTA began, 0 between calls
+    // Bounds of the keys of whole pages (trimmoe_cache_set_bounds), or NULL.
+    int8_t* codes;                     // [layers][n_pages][Hkv][2][dh]
+    float* scales;                     // [layers][n_pages][Hkv]
+    // Steps with groups of sequences: the list of items is in `groups` and the parts in part_o and
+    // part_ml as for other steps, but these are other, larger buffers (the host side chooses).
+    int shared;
+    int2* items_of;                    // [T] groups that hold a token: its own keys' and its common ones' (-1: none)
+    int* common;                       // [max_seqs] key tiles that a group of sequences has in common
     int* err;
     int* refused;                      // behind err: the last step was refused and stats has not reset that yet
 };
@@ -123,7 +150,40 @@ struct AttendParams {
     int ld_out;
     int join_here;                     // the attention kernel joins cut items itself
     float scale_log2;
+    int T;
 };
+
+// attend_blocks: q and out as for attend.
+struct BlocksParams {
+    const __nv_bfloat16* q;
+    __nv_bfloat16* out;
+    const int* blocks;                 // [T][Hkv][n]
+    const uint64_t* tree;
+    int ld_q, ld_out, T, n;
+    int row_tiles;                     // of 16 query heads of a key/value head
+    float scale_log2;
+};
+
+// Columns of the page table at most (their scores lie in shared memory).
+constexpr int kSelectPages = 40960;
+
+struct SelectParams {
+    const __nv_bfloat16* q;
+    int* blocks;                       // [T][Hkv][n]
+    int ld_q, T, n, first, last, layer;
+};
+
+// Steps with groups of sequences: rows (tokens times query heads) at most, and what that allows.
+constexpr int kShareRows = 65536;
+inline long long cache_share_groups(const CacheDev& c) {
+    return 2 * ((long long)kShareRows / c.Hq / (2 * c.tile_tokens) + c.max_seqs + 1);
+}
+// Every token has its own and at most one common part, a part's rows are at most twice its
+// tokens' (whole warps, tiles that rep does not divide), a cut adds one part of 256 rows, and
+// an item's rows begin at a multiple of 32.
+inline long long cache_share_part_rows(const CacheDev& c) {
+    return 4LL * kShareRows + 256LL * c.num_sms + 32 * cache_share_groups(c);
+}
 
 cudaError_t launch_cache_step(const CacheDev& c, int n, const int* seq, const int* q_len, int T, cudaStream_t st);
 cudaError_t launch_cache_fork(const CacheDev& c, int n, const int* src, const int* dst, cudaStream_t st);
@@ -132,7 +192,58 @@ cudaError_t launch_cache_accept(const CacheDev& c, int n, const int* seq, const 
                                 int ld_path, cudaStream_t st);
 cudaError_t launch_cache_compact(const CacheDev& c, cudaStream_t st);
 cudaError_t launch_cache_append(const CacheDev& c, const AppendParams& p, cudaStream_t st);
+// Bounds of the pages that the step filled (whole: of all full pages of its sequences) in one
+// layer; n listed sequences with at most max_q new tokens.
+cudaError_t launch_cache_bounds(const CacheDev& c, int layer, int n, int max_q, int whole, cudaStream_t st);
+// Of those that accepted drafts filled, in all layers (accepted: the accept kernel's new lengths, -1: none).
+cudaError_t launch_cache_bounds_accepted(const CacheDev& c, int n, const int* seq, const int* n_acc, const int* accepted,
+                                         cudaStream_t st);
+cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st);
+cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                                const BlocksParams& p, cudaStream_t st);
+// The list of items of a step whose listed sequences form n groups.
+cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, cudaStream_t st);
 cudaError_t launch_cache_attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                 const CUtensorMap& tm_v, const AttendParams& p, int max_rows, cudaStream_t st);
+
+// Device helpers of the attention kernels.
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Bounded wait by all lanes of a warp.  A probe sleeps until the phase ends or up to
+// about a microsecond; after 2^22 of them, some seconds, the waiter raises the CTA's
+// abort flag and the error word; it also gives up when another role has.  The loop is
+// inside the asm so that control flow stays uniform for the compiler (see elect_one).
+// Returns 0 when the phase ended, 1 when given up.
+__device__ __forceinline__ uint32_t wait_probes(uint32_t bar, uint32_t parity, uint32_t abort_flag, int* err) {
+    uint32_t gave_up;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b32 n, a;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mov.b32 n, 0;\n\t"
+        "mov.b32 %0, 0;\n\t"
+        "@p bra DONE;\n\t"
+        "PROBE:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
+        "@p bra DONE;\n\t"
+        "ld.volatile.shared.b32 a, [%3];\n\t"
+        "setp.ne.b32 p, a, 0;\n\t"
+        "@p bra GONE;\n\t"
+        "add.s32 n, n, 1;\n\t"
+        "setp.lt.s32 p, n, 4194304;\n\t"
+        "@p bra PROBE;\n\t"
+        "st.volatile.shared.b32 [%3], 1;\n\t"
+        "atom.global.cas.b32 a, [%4], 0, %5;\n\t"
+        "GONE:\n\t"
+        "mov.b32 %0, 1;\n\t"
+        "DONE:\n\t}"
+        : "=&r"(gave_up)
+        : "r"(bar), "r"(parity), "r"(abort_flag), "l"(err), "n"((int)ERR_TIMEOUT_CACHE_ATTN)
+        : "memory");
+    return gave_up;
+}
 
 }  // namespace tmoe

@@ -81,6 +81,7 @@ struct Seg {
     int seq, kv_len, row, ntok, first, base, head;
     int t0, t1;          // key tiles
     int part;            // part buffer, -1: the whole item
+    int common, part_row;   // with groups of sequences: an item of their common tiles, the first row of its part
 };
 
 struct __align__(8) Bars {
@@ -131,45 +132,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-__device__ __forceinline__ float ex2(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
-// Bounded wait by all lanes of a warp.  A probe sleeps until the phase ends or up to
-// about a microsecond; after 2^22 of them, some seconds, the waiter raises the CTA's
-// abort flag and the error word; it also gives up when another role has.  The loop is
-// inside the asm so that control flow stays uniform for the compiler (see elect_one).
-// Returns 0 when the phase ended, 1 when given up.
-__device__ __forceinline__ uint32_t wait_probes(uint32_t bar, uint32_t parity, uint32_t abort_flag, int* err) {
-    uint32_t gave_up;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b32 n, a;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "mov.b32 n, 0;\n\t"
-        "mov.b32 %0, 0;\n\t"
-        "@p bra DONE;\n\t"
-        "PROBE:\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
-        "@p bra DONE;\n\t"
-        "ld.volatile.shared.b32 a, [%3];\n\t"
-        "setp.ne.b32 p, a, 0;\n\t"
-        "@p bra GONE;\n\t"
-        "add.s32 n, n, 1;\n\t"
-        "setp.lt.s32 p, n, 4194304;\n\t"
-        "@p bra PROBE;\n\t"
-        "st.volatile.shared.b32 [%3], 1;\n\t"
-        "atom.global.cas.b32 a, [%4], 0, %5;\n\t"
-        "GONE:\n\t"
-        "mov.b32 %0, 1;\n\t"
-        "DONE:\n\t}"
-        : "=&r"(gave_up)
-        : "r"(bar), "r"(parity), "r"(abort_flag), "l"(err), "n"((int)ERR_TIMEOUT_CACHE_ATTN)
-        : "memory");
-    return gave_up;
-}
-
 // One lane of a converged warp.  Products and commits stand behind it: the compiler
 // then knows that a single lane issues them and keeps their operands in uniform
 // registers (behind lane == 0 each cost some thirty instructions, more than its 64
@@ -394,7 +356,8 @@ __device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams&
                                                              pack_bf16x2(acc[g][2] * il, acc[g][3] * il));
 }
 
-template <int DH>
+// SHARED: the items are those of a step with groups of sequences (cache_share.cu).
+template <int DH, bool SHARED>
 __global__ void __launch_bounds__(kThreads, 1)
 cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                        const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CacheDev c,
@@ -460,6 +423,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const uint32_t abort_at = bb + (uint32_t)offsetof(Bars, abort_flag);
     auto wait = [&](const uint64_t* b, uint32_t parity) { return wait_probes(bar(b), parity & 1u, abort_at, c.err); };
     auto lost = [](uint32_t gave_up) { return __any_sync(0xffffffffu, gave_up) != 0; };
+    // Common tiles are all below a segment's `base`: like a tree's, without drafts.
+    auto unmasked = [&](const Seg& g) { return tree || (SHARED && g.common); };
     // The it-th segment of this CTA (false: none left, or aborted).
     auto next_seg = [&](int it, Seg& g) {
         const int s = it % kSegSlots;
@@ -498,7 +463,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const bool my_box = lane < pages_per_tile * L::KB;
             // Whole items are drawn from a counter, longest first; else the CTA's share of the
             // line is walked item by item.
-            const bool whole = pl.n_ctas == 0;
+            const bool whole = !SHARED && pl.n_ctas == 0;
             const int items = whole ? pl.n_groups * c.Hkv : 0;
             int item = b, group = 0, head = 0;
             long long x = 0, x_end = 0, within = 0;
@@ -538,7 +503,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     sg.t0 = cache_tiles_before(within, g.cost, two_tiles);
                     sg.t1 = cache_tiles_before(x1, g.cost, two_tiles);
                     const bool all = sg.t0 == 0 && sg.t1 == cache_item_tiles(g.cost, two_tiles);
-                    sg.part = all ? -1 : 2 * b + (sg.t0 == 0);
+                    sg.part = SHARED ? 0 : all ? -1 : 2 * b + (sg.t0 == 0);
+                    if (SHARED) {
+                        sg.t0 += g.t0;
+                        sg.t1 += g.t0;
+                        sg.common = g.common;
+                        sg.part_row = g.part_row + (head + b) * cache_part_rows(g.ntok, TT, rep);
+                    }
                     x += x1 - within;
                     within = 0;
                     any = x < x_end;
@@ -549,7 +520,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 if (sg.t0 < sg.t1) {
                     if (!give_seg(sg)) break;
-                    const SegInfo si = seg_info(sg, TT, tree);
+                    const SegInfo si = seg_info(sg, TT, unmasked(sg));
                     // Page indices of the tiles ahead travel in registers.
                     const int n_pages = (si.kmax + c.page - 1) >> c.page_shift;
                     const int* row = c.table + (size_t)sg.seq * c.max_pages;
@@ -653,7 +624,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             };
             Seg g;
             for (int it = 0; !lost(gave_up) && next_seg(it, g); ++it) {
-                const SegInfo si = seg_info(g, TT, tree);
+                const SegInfo si = seg_info(g, TT, unmasked(g));
                 auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
                 const int dual = uniform(si.dual), lead = dual ? 1 : 2, nt = uniform(g.t1 - g.t0);
                 const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
@@ -767,7 +738,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             Seg g;
             bool ok = true;
             for (int it = 0; ok && next_seg(it, g); ++it) {
-                const SegInfo si = seg_info(g, TT, tree);
+                const SegInfo si = seg_info(g, TT, unmasked(g));
                 const int lead = si.dual ? 1 : 2, nt = g.t1 - g.t0;
                 for (int i = max(0, si.kall / kCacheTile - g.t0); ok && i < nt; ++i) {
                     const int t = g.t0 + i;
@@ -835,7 +806,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int step = dual ? 1 : 2, begin = g.t0 + (dual ? 0 : slot);
             int lim, first_part, mask0;                    // tiles, first partly masked one, index of a tile among those
             {
-                const SegInfo si = seg_info(g, TT, tree);
+                const SegInfo si = seg_info(g, TT, unmasked(g));
                 lim = slot ? si.n1 : si.n0;
                 first_part = si.kall / kCacheTile;
                 const int m0 = max(g.t0, first_part);
@@ -1031,7 +1002,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             // In a one-tile item both slots hold parts of the same rows: they tell each other the
             // maxima and sums, and each puts out half of the columns, reading both O's.
             // (Apart: parts of a cut item that are joined right after go out as they are.)
-            const bool apart = g.part >= 0 && p.join_here;
+            const bool apart = !SHARED && g.part >= 0 && p.join_here;
             const bool joins = !dual && !apart && g.t0 + 1 < lim;   // (without two tiles lim is the same for both)
             if (l == 0.f) m = -INFINITY;                   // no key seen
             float fo = 1.f, fx = 0.f;
@@ -1055,7 +1026,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 float* po = nullptr;
                 int po_step = 0;                           // from column to column of a multiple of 4
                 __nv_bfloat16* out = nullptr;
-                if (g.part >= 0) {
+                if (SHARED) {
+                    const size_t row = (size_t)g.part_row + (dual ? slot * 128 : 0) + r;
+                    const bool warps = cache_part_rows(g.ntok, TT, rep) >= 32;
+                    po = c.part_o + (warps ? (row & ~(size_t)31) * DH + (row & 31) * 4 : row * DH);
+                    po_step = warps ? 32 : 1;
+                    if (mine && !(joins && slot)) c.part_ml[row] = make_float2(work ? m : -INFINITY, l);
+                } else if (g.part >= 0) {
                     const int row = (dual || apart ? slot * 128 : 0) + r;
                     po = c.part_o + (apart ? ((size_t)g.part * 256 + row) * DH : part_at<DH>(g.part, row, 0));
                     po_step = apart ? 1 : 32;
@@ -1158,14 +1135,78 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
         join_rows<DH, DH / 32>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
 }
 
+// Adds the parts of a step with groups of sequences.  A warp takes a token and four query heads of
+// a key/value head, a lane a head and every eighth four columns; up to four parts are
+// read at a time, the common item's first, in the order of the keys.  Bound: L2.
+template <int DH>
+__global__ void __launch_bounds__(256) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
+                                                                const __grid_constant__ AttendParams p) {
+    constexpr int V = DH / 32, B = 4;
+    pdl_wait();
+    pdl_trigger();
+    const CachePlan pl = *c.plan;
+    if (!pl.ok) return;
+    const int quads = (c.rep + 3) / 4, lane = threadIdx.x & 31;
+    const long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (u >= (long long)p.T * c.Hkv * quads) return;
+    const int quad = (int)(u % quads), head = (int)(u / quads % c.Hkv), t = (int)(u / quads / c.Hkv);
+    const int h = min(quad * 4 + (lane >> 3), c.rep - 1), c4 = lane & 7;
+    const int2 of = c.items_of[t];
+    float top = -INFINITY, l = 0.f, acc[V][4];
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v][0] = acc[v][1] = acc[v][2] = acc[v][3] = 0.f;
+    for (int k = 0; k < 2; ++k) {
+        const int e = k ? of.x : of.y;
+        if (e < 0) continue;
+        const CacheGroup g = c.groups[e];
+        const int two = cache_two_tiles(g.ntok, c.tile_tokens), tiles = cache_item_tiles(g.cost, two);
+        const long long start = g.pre * c.Hkv + (long long)head * g.cost;
+        const int first = cache_cta_of(start, pl.total, pl.n_ctas);
+        const int last = cache_cta_of(start + ((long long)(tiles - 1) << two), pl.total, pl.n_ctas);
+        const int R = cache_part_rows(g.ntok, c.tile_tokens, c.rep), in = t - g.row;
+        const int r = (in >= c.tile_tokens ? 128 + (in - c.tile_tokens) * c.rep : in * c.rep) + h;
+        for (int b0 = first; b0 <= last; b0 += B) {
+            float2 ml[B];
+            float4 o[B][V];
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                const size_t row = (size_t)(g.part_row + (head + min(b0 + i, last)) * R + r);
+                ml[i] = __ldcg(c.part_ml + row);
+                const float* src = c.part_o + (R >= 32 ? (row & ~(size_t)31) * DH + (row & 31) * 4 : row * DH);
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    o[i][v] = __ldcg(reinterpret_cast<const float4*>(src + (v * 8 + c4) * (R >= 32 ? 128 : 4)));
+            }
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                float fa, fb;
+                const bool there = join_source(ml[i], b0 + i <= last, top, l, fa, fb);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float x[4] = {o[i][v].x, o[i][v].y, o[i][v].z, o[i][v].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[v][j] = there ? acc[v][j] * fa + x[j] * fb : acc[v][j];
+                }
+            }
+        }
+    }
+    if (quad * 4 + (lane >> 3) >= c.rep) return;
+    const float il = l == 0.f ? 0.f : 1.f / l;
+    __nv_bfloat16* out = p.out + (size_t)t * p.ld_out + (size_t)(head * c.rep + h) * DH + c4 * 4;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        *reinterpret_cast<uint2*>(out + v * 32) = make_uint2(pack_bf16x2(acc[v][0] * il, acc[v][1] * il),
+                                                             pack_bf16x2(acc[v][2] * il, acc[v][3] * il));
+}
+
 static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
 
-template <int DH>
+template <int DH, bool SHARED>
 cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                    const AttendParams& p, int max_rows, cudaStream_t st) {
     static PerDevice attr;
     cudaError_t e = (cudaError_t)attr.get([] {
-        return (int)cudaFuncSetAttribute(cache_attention_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        return (int)cudaFuncSetAttribute(cache_attention_kernel<DH, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (int)smem_bytes<DH>());
     }, true);
     if (e != cudaSuccess) return e;
@@ -1174,12 +1215,16 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
     static PerDevice regs;
     const int nreg = regs.get([] {
         cudaFuncAttributes fa = {};
-        return cudaFuncGetAttributes(&fa, cache_attention_kernel<DH>) == cudaSuccess ? fa.numRegs : 0;
+        return cudaFuncGetAttributes(&fa, cache_attention_kernel<DH, SHARED>) == cudaSuccess ? fa.numRegs : 0;
     });
     if (nreg * kThreads < 104 * 128 + 200 * 256) return cudaErrorInvalidConfiguration;
-    e = launch_pdl(cache_attention_kernel<DH>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
+    e = launch_pdl(cache_attention_kernel<DH, SHARED>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
                    c, p);
     if (e != cudaSuccess || p.join_here) return e;
+    if (SHARED) {
+        const long long units = (long long)p.T * c.Hkv * ((c.rep + 3) / 4);
+        return launch_pdl(cache_join_shared_kernel<DH>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, c, p);
+    }
     return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);
 }
 
@@ -1187,8 +1232,11 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
 
 cudaError_t launch_cache_attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                 const CUtensorMap& tm_v, const AttendParams& p, int max_rows, cudaStream_t st) {
-    return c.dh == 64 ? attend<64>(c, tm_q, tm_k, tm_v, p, max_rows, st)
-                      : attend<128>(c, tm_q, tm_k, tm_v, p, max_rows, st);
+    if (c.shared)
+        return c.dh == 64 ? attend<64, true>(c, tm_q, tm_k, tm_v, p, max_rows, st)
+                          : attend<128, true>(c, tm_q, tm_k, tm_v, p, max_rows, st);
+    return c.dh == 64 ? attend<64, false>(c, tm_q, tm_k, tm_v, p, max_rows, st)
+                      : attend<128, false>(c, tm_q, tm_k, tm_v, p, max_rows, st);
 }
 
 }  // namespace tmoe

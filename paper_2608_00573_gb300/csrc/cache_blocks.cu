@@ -1,0 +1,151 @@
+// Host side of the cache's attention that does not read all of it: groups of sequences with a
+// common prompt, bounds of blocks, their selection, attention over chosen blocks.
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "cache_host.cuh"
+
+extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, const int32_t* counts, void* stream) {
+    if (!c) return TRIMMOE_ERR_ARG;
+    if (c->T < 0) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "no step has been begun");
+    if (n < 0 || n > c->n) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "n out of range");
+    if (n > 0 && !counts) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "NULL argument");
+    long long sum = 0;
+    for (int i = 0; i < n; ++i) {
+        if (counts[i] < 1) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "counts must be >= 1");
+        sum += counts[i];
+    }
+    if (sum != c->n) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "counts must add up to the step's sequences");
+    if (c->T == 0 || (long long)c->T * c->d.Hq > kShareRows) return TRIMMOE_OK;
+    OnDevice on(c->dev);
+    Range range("trimmoe.cache_share");
+    cudaStream_t st = enter(c, stream);
+    if (!c->share.part_o) {
+        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(st, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone)
+            return c->fail(TRIMMOE_ERR_ARG, "cache_share", "the first call allocates and must not be captured");
+        CacheDev d = c->d;
+        cudaError_t e = cudaSuccess;
+        size_t had = c->allocs.size();
+        try {
+            c->allocs.reserve(had + 5);
+        } catch (const std::bad_alloc&) {
+            return c->fail(TRIMMOE_ERR_OOM, "cache_share", "host allocation failed");
+        }
+        auto alloc = [&](auto*& p, size_t count) {
+            void* q = nullptr;
+            if (e == cudaSuccess) e = cudaMalloc(&q, count * sizeof(*p));
+            if (e != cudaSuccess) return;
+            c->allocs.push_back(q);
+            p = static_cast<std::remove_reference_t<decltype(p)>>(q);
+        };
+        const size_t rows = (size_t)cache_share_part_rows(d);
+        alloc(d.groups, (size_t)cache_share_groups(d));
+        alloc(d.items_of, (size_t)kShareRows);
+        alloc(d.common, (size_t)d.max_seqs);
+        alloc(d.part_ml, rows);
+        alloc(d.part_o, rows * d.dh);
+        if (e != cudaSuccess) {
+            for (; c->allocs.size() > had; c->allocs.pop_back()) cudaFree(c->allocs.back());
+            cudaGetLastError();
+            return c->fail(e == cudaErrorMemoryAllocation ? TRIMMOE_ERR_OOM : TRIMMOE_ERR_CUDA, "cache_share",
+                           cudaGetErrorString(e));
+        }
+        c->share = d;
+    }
+    c->share.shared = 1;
+    const trimmoe_status s = c->launched(launch_cache_share(c->share, n, counts, c->n, c->T, st), 2, "cache_share");
+    // (Without its list a step cannot be attended.)
+    if (s != TRIMMOE_OK) c->T = -1;
+    else c->d.shared = 1;
+    return s;
+}
+
+extern "C" trimmoe_status trimmoe_cache_set_bounds(trimmoe_cache_handle c, int8_t* codes, float* scales) {
+    if (!c) return TRIMMOE_ERR_ARG;
+    if (!codes != !scales) return c->fail(TRIMMOE_ERR_ARG, "cache_set_bounds", "codes and scales come together");
+    if (!aligned16(codes) || (reinterpret_cast<uintptr_t>(scales) & 3u))
+        return c->fail(TRIMMOE_ERR_ARG, "cache_set_bounds", "pointers must be aligned (codes 16 bytes, scales 4)");
+    c->d.codes = codes;
+    c->d.scales = scales;
+    return TRIMMOE_OK;
+}
+
+extern "C" trimmoe_status trimmoe_cache_summarize(trimmoe_cache_handle c, int layer, int whole, void* stream) {
+    if (!c) return TRIMMOE_ERR_ARG;
+    const trimmoe_status s = check_layer(c, "cache_summarize", layer);
+    if (s != TRIMMOE_OK) return s;
+    if (!c->d.codes) return c->fail(TRIMMOE_ERR_ARG, "cache_summarize", "no bounds have been set");
+    if (c->n == 0) return TRIMMOE_OK;
+    OnDevice on(c->dev);
+    Range range("trimmoe.cache_summarize");
+    return c->launched(launch_cache_bounds(c->d, layer, c->n, c->max_q, whole != 0, enter(c, stream)), 1, "cache_summarize");
+}
+
+extern "C" trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer, const trimmoe_select_args* a, void* stream) {
+    if (!c) return TRIMMOE_ERR_ARG;
+    const trimmoe_status s = check_layer(c, "cache_select", layer);
+    if (s != TRIMMOE_OK) return s;
+    const CacheDev& d = c->d;
+    if (!a) return c->fail(TRIMMOE_ERR_ARG, "cache_select", "NULL argument");
+    if (!d.codes) return c->fail(TRIMMOE_ERR_ARG, "cache_select", "no bounds have been set");
+    if (d.max_pages > kSelectPages) return c->fail(TRIMMOE_ERR_UNSUPPORTED, "cache_select", "max_pages must be <= 40960");
+    if (a->n < 1 || a->first < 0 || a->last < 0 || a->first > a->n || a->last > a->n - a->first)
+        return c->fail(TRIMMOE_ERR_ARG, "cache_select", "n must be >= 1, first and last >= 0 and together at most n");
+    if (c->T == 0) return TRIMMOE_OK;
+    if (!a->q || !a->blocks) return c->fail(TRIMMOE_ERR_ARG, "cache_select", "NULL pointer");
+    if (!aligned16(a->q) || a->ld_q % 8 || (reinterpret_cast<uintptr_t>(a->blocks) & 3u))
+        return c->fail(TRIMMOE_ERR_ARG, "cache_select", "pointers must be aligned (q 16 bytes) and the row stride a multiple of 8");
+    if (a->ld_q < d.Hq * d.dh) return c->fail(TRIMMOE_ERR_ARG, "cache_select", "row stride shorter than a row");
+    if ((long long)c->T * d.Hkv > 0x7fffffffLL) return c->fail(TRIMMOE_ERR_UNSUPPORTED, "cache_select", "T * kv_heads must be < 2^31");
+    SelectParams p = {};
+    p.q = static_cast<const __nv_bfloat16*>(a->q);
+    p.blocks = a->blocks;
+    p.ld_q = a->ld_q;
+    p.T = c->T;
+    p.n = a->n;
+    p.first = a->first;
+    p.last = a->last;
+    p.layer = layer;
+    OnDevice on(c->dev);
+    Range range("trimmoe.cache_select");
+    return c->launched(launch_cache_select(d, p, enter(c, stream)), 1, "cache_select");
+}
+
+extern "C" trimmoe_status trimmoe_cache_attend_blocks(trimmoe_cache_handle c, int layer, const trimmoe_blocks_args* a,
+                                                      void* stream) {
+    if (!c) return TRIMMOE_ERR_ARG;
+    const char* what = "cache_attend_blocks";
+    const trimmoe_status s = check_layer(c, what, layer);
+    if (s != TRIMMOE_OK) return s;
+    if (!a) return c->fail(TRIMMOE_ERR_ARG, what, "NULL argument");
+    if (a->n < 0) return c->fail(TRIMMOE_ERR_ARG, what, "n must be >= 0");
+    if (c->T == 0) return TRIMMOE_OK;
+    const CacheDev& d = c->d;
+    if (!a->q || !a->out || (a->n > 0 && !a->blocks)) return c->fail(TRIMMOE_ERR_ARG, what, "NULL pointer");
+    if (!aligned16(a->q) || !aligned16(a->out) || a->ld_q % 8 || a->ld_out % 8 || (reinterpret_cast<uintptr_t>(a->tree) & 7u) ||
+        (reinterpret_cast<uintptr_t>(a->blocks) & 3u))
+        return c->fail(TRIMMOE_ERR_ARG, what, "pointers must be aligned (q, out 16 bytes) and row strides multiples of 8");
+    if (a->ld_q < d.Hq * d.dh || a->ld_out < d.Hq * d.dh) return c->fail(TRIMMOE_ERR_ARG, what, "row stride shorter than a row");
+    if (!(a->scale >= 0.f && std::isfinite(a->scale))) return c->fail(TRIMMOE_ERR_ARG, what, "scale must be finite and >= 0");
+    if (a->tree && c->max_q > kTreeMax) return c->fail(TRIMMOE_ERR_ARG, what, "a tree has at most 64 tokens per sequence");
+    BlocksParams p = {};
+    p.q = static_cast<const __nv_bfloat16*>(a->q);
+    p.out = static_cast<__nv_bfloat16*>(a->out);
+    p.blocks = a->blocks;
+    p.tree = a->tree;
+    p.ld_q = a->ld_q;
+    p.ld_out = a->ld_out;
+    p.T = c->T;
+    p.n = a->n;
+    p.row_tiles = (d.rep + 15) / 16;
+    if ((long long)c->T * d.Hkv * p.row_tiles > (1LL << 26)) return c->fail(TRIMMOE_ERR_UNSUPPORTED, what, "more than 2^26 items");
+    p.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)d.dh)) * 1.4426950408889634f;
+    const bool large = d.page > 64;
+    OnDevice on(c->dev);
+    Range range("trimmoe.cache_attend_blocks");
+    return c->launched(launch_cache_blocks(d, large ? c->tm_k64[layer] : c->tm_k[layer], large ? c->tm_v64[layer] : c->tm_v[layer],
+                                           p, enter(c, stream)),
+                       1, what);
+}

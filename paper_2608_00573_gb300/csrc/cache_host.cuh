@@ -1,0 +1,82 @@
+// Host side of a cache handle, shared by the files that define its entry points.
+#pragma once
+
+#include <string>
+#include <vector>
+
+#include <nvtx3/nvToolsExt.h>
+
+#include "cache.cuh"
+
+using namespace tmoe;
+
+struct trimmoe_cache {
+    trimmoe_cache_config cfg;
+    CacheDev d;
+    CacheDev share;                           // d of a step with groups of sequences (its workspaces: first cache_share)
+    int dev = 0;
+    std::string err;
+    std::vector<void*> allocs;
+    std::vector<CUtensorMap> tm_k, tm_v;      // per layer: rows [n_pages * kv_heads * page][head_dim], one page and head a box
+    std::vector<CUtensorMap> tm_k64, tm_v64;  // the same in boxes of 64 rows, for larger pages
+    std::vector<uint32_t> stamp;              // per sequence: last call that listed it
+    uint32_t call = 0;
+    cudaStream_t last_stream = nullptr;
+    uint64_t launches = 0;
+    int T = -1, n = 0, max_q = 0;             // the current step (T < 0: none)
+    float theta = 0.f;                        // base of turn[]
+    uint64_t turn[64];
+
+    // Keeps "what: why" (nothing when there is no memory for it: no exception leaves a call).
+    trimmoe_status fail(trimmoe_status s, const char* what, const char* why) noexcept {
+        try {
+            err.assign(what).append(": ").append(why);
+        } catch (...) {
+            err.clear();
+        }
+        return s;
+    }
+    trimmoe_status launched(cudaError_t e, int n_kernels, const char* what) noexcept {
+        if (e == cudaSuccess) e = cudaGetLastError();
+        if (e != cudaSuccess) return fail(TRIMMOE_ERR_CUDA, what, cudaGetErrorString(e));
+        launches += n_kernels;
+        return TRIMMOE_OK;
+    }
+};
+
+namespace {
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The handle's device for the duration of a call.
+struct OnDevice {
+    int prev = -1, dev;
+    explicit OnDevice(int d) : dev(d) {
+        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
+        if (prev != dev) cudaSetDevice(dev);
+    }
+    ~OnDevice() {
+        if (prev >= 0 && prev != dev) cudaSetDevice(prev);
+    }
+};
+
+struct Range {
+    explicit Range(const char* name) { nvtxRangePushA(name); }
+    ~Range() { nvtxRangePop(); }
+};
+
+inline trimmoe_status check_layer(trimmoe_cache* c, const char* what, int layer) {
+    if (layer < 0 || layer >= c->cfg.layers) return c->fail(TRIMMOE_ERR_ARG, what, "layer out of range");
+    if (c->T < 0) return c->fail(TRIMMOE_ERR_ARG, what, "no step has been begun");
+    return TRIMMOE_OK;
+}
+
+// Sets up a call on `stream` (after its checks): clears an error that other code
+// left behind, so that the launches' own are seen.
+inline cudaStream_t enter(trimmoe_cache* c, void* stream) {
+    cudaGetLastError();
+    c->last_stream = (cudaStream_t)stream;
+    return c->last_stream;
+}
+
+}  // namespace

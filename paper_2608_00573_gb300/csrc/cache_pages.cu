@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kCopyThreads) cache_fill_kernel(const __grid_c
     pdl_trigger();
     const int ok = c.plan->ok, copies = c.plan->copies;
     for (int t = blockIdx.x * kCopyThreads + threadIdx.x; t < T; t += gridDim.x * kCopyThreads) {
-        int slot = -1, pos = 0;
+        int slot = -1, pos = 0, owner = 0;
         if (ok) {
             int lo = 0, hi = n;
             while (hi - lo > 1) {
@@ -349,13 +349,14 @@ __global__ void __launch_bounds__(kCopyThreads) cache_fill_kernel(const __grid_c
                 if (c.seqs[m].q_off <= t) lo = m;
                 else hi = m;
             }
-            const CacheSeq s = c.seqs[lo];
+            const CacheSeq s = c.seqs[owner = lo];
             pos = s.kv_len - s.q_len + (t - s.q_off);
             slot = (c.table[(size_t)s.seq * c.max_pages + (pos >> c.page_shift)] << c.page_shift) +
                    (pos & (c.page - 1));
         }
         c.slot[t] = slot;
         c.pos[t] = pos;
+        c.owner[t] = owner;
     }
     const size_t vecs = (size_t)c.Hkv * c.page * c.dh / 8;      // 16-byte vectors of a page in one layer
     constexpr int kPart = kCopyThreads * kCopyVecs;
@@ -377,6 +378,18 @@ __global__ void __launch_bounds__(kCopyThreads) cache_fill_kernel(const __grid_c
 #pragma unroll
         for (int w = 0; w < kCopyVecs; ++w)
             if (v0 + w * kCopyThreads < vecs) dst[v0 + w * kCopyThreads] = r[w];
+    }
+    if (!c.codes) return;
+    // The pages' bounds (a page that a step copies is not full and has none yet).
+    const size_t words = (size_t)c.Hkv * c.dh / 2;              // 4-byte words of a page's codes in one layer
+    for (long long u = blockIdx.x; u < (long long)copies * c.layers; u += gridDim.x) {
+        const int2 cp = c.copies[u / c.layers];
+        const size_t first = (size_t)(u % c.layers) * c.n_pages;
+        uint32_t* codes = reinterpret_cast<uint32_t*>(c.codes);
+        for (size_t w = threadIdx.x; w < words; w += kCopyThreads)
+            codes[(first + cp.y) * words + w] = codes[(first + cp.x) * words + w];
+        for (int h = threadIdx.x; h < c.Hkv; h += kCopyThreads)
+            c.scales[(first + cp.y) * c.Hkv + h] = c.scales[(first + cp.x) * c.Hkv + h];
     }
 }
 
@@ -650,8 +663,10 @@ cudaError_t accept_launch(const CacheDev& c, int n, const int* seq, const int* n
     const dim3 grid((unsigned)std::min<long long>((units + per - 1) / per, c.num_sms * 16));
     cudaError_t e = launch_pdl(cache_accept_kernel<N>, grid, dim3(256), 0, st, c, l, n_acc, path, ld_path, accepted);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_cut_kernel<N>, dim3(entry_blocks(c, (long long)n * c.max_pages)), dim3(256), 0, st, c, l,
-                      (const int*)accepted);
+    e = launch_pdl(cache_cut_kernel<N>, dim3(entry_blocks(c, (long long)n * c.max_pages)), dim3(256), 0, st, c, l,
+                   (const int*)accepted);
+    if (e != cudaSuccess || !c.codes) return e;
+    return launch_cache_bounds_accepted(c, n, seq, n_acc, accepted, st);
 }
 }  // namespace
 

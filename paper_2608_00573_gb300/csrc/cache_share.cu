@@ -1,0 +1,273 @@
+// The list of attention items of a step whose sequences come in groups with a common
+// prompt (trimmoe_cache_share).
+//
+// A group's common positions are those of the pages that all of its sequences with new tokens
+// hold at their front, in whole key tiles.  An item is a group of query rows and a
+// key/value head, as in other steps; here there are two kinds: common items, all new
+// tokens of a group of sequences over its common tiles, without any mask, and own
+// items, the tokens of one sequence over its other tiles.  Every item's sums go to parts,
+// which cache_join_shared_kernel adds per token: the common item's in the order of the keys, then
+// its own.
+#include <algorithm>
+
+#include "cache.cuh"
+
+namespace tmoe {
+
+namespace {
+
+constexpr int kCommonThreads = 256;
+constexpr int kPlanThreads = 1024;
+constexpr int kMinTiles = 2;           // as for other steps (cache_pages.cu)
+
+// A block takes one group: the front pages that its sequences share, and how many whole key
+// tiles these fill.
+template <int N>
+__global__ void __launch_bounds__(kCommonThreads) cache_common_kernel(const __grid_constant__ CacheDev c,
+                                                                      const __grid_constant__ CacheList<N> l) {
+    __shared__ int s_pages, s_lead, s_members;
+    const int g = blockIdx.x, from = l.a[g], to = from + l.b[g];
+    if (threadIdx.x == 0) {
+        s_pages = 0x7fffffff;
+        s_lead = 0x7fffffff;
+        s_members = 0;
+    }
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    if (!c.plan->ok) return;
+    for (int i = from + threadIdx.x; i < to; i += kCommonThreads) {
+        const CacheSeq s = c.seqs[i];
+        if (s.q_len > 0) {
+            atomicMin(&s_pages, (s.kv_len - s.q_len) >> c.page_shift);
+            atomicMin(&s_lead, i);
+            atomicAdd(&s_members, 1);
+        }
+    }
+    __syncthreads();
+    if (s_members < 2) {
+        if (threadIdx.x == 0) c.common[g] = 0;
+        return;
+    }
+    // A warp takes one sequence at a time; the first difference ends it for all.
+    const int lane = threadIdx.x & 31;
+    const int* lead = c.table + (size_t)c.seqs[s_lead].seq * c.max_pages;
+    for (int i = s_lead + 1 + (threadIdx.x >> 5); i < to; i += kCommonThreads / 32) {
+        const CacheSeq s = c.seqs[i];
+        if (s.q_len == 0) continue;
+        const int* mine = c.table + (size_t)s.seq * c.max_pages;
+        for (int j0 = 0;; j0 += 128) {
+            const int end = __shfl_sync(0xffffffffu, *(volatile int*)&s_pages, 0);
+            if (j0 >= end) break;
+            int a[4], b[4], first = 0x7fffffff;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = j0 + u * 32 + lane;
+                a[u] = j < end ? lead[j] : 0;
+                b[u] = j < end ? mine[j] : 0;
+            }
+#pragma unroll
+            for (int u = 3; u >= 0; --u)
+                if (a[u] != b[u] || a[u] < 0) first = j0 + u * 32 + lane;
+            first = __reduce_min_sync(0xffffffffu, first);
+            if (lane == 0 && first != 0x7fffffff) atomicMin(&s_pages, first);
+            __syncwarp();
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) c.common[g] = (s_pages << c.page_shift) / kCacheTile;
+}
+
+template <class V>
+__device__ __forceinline__ V up(V v, int o) {
+    return __shfl_up_sync(0xffffffffu, v, o);
+}
+
+// Exclusive prefix sum over the block; every thread gets the total.
+template <class V>
+__device__ V block_sum(V v, V* ws, V& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    V x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const V y = up(x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) ws[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        V s = ws[lane];
+        const V own = s;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const V y = up(s, o);
+            if (lane >= o) s += y;
+        }
+        ws[lane] = s - own;
+        if (lane == 31) ws[32] = s;
+    }
+    __syncthreads();
+    const V r = ws[warp] + x - v;
+    total = ws[32];
+    __syncthreads();
+    return r;
+}
+
+// One block: the items of the step, their shares of the line, where their parts lie and which
+// items hold each token.  A thread takes one group of sequences, one sequence, then one
+// item's row of heads at a time.
+template <int N>
+__global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_constant__ CacheDev c,
+                                                                   const __grid_constant__ CacheList<N> l, int n_seqs, int T) {
+    __shared__ int s_common[kCacheMaxSeqs], s_begin[kCacheMaxSeqs + 1], s_own[kCacheMaxSeqs + 1];   // first items of groups, sequences
+    __shared__ int s_of[kCacheMaxSeqs];                // a sequence's group
+    __shared__ int s_wi[33];
+    __shared__ long long s_wl[33];
+    const int i = threadIdx.x, n = l.n, TT = c.tile_tokens;
+    pdl_wait();
+    pdl_trigger();
+    if (!c.plan->ok) return;
+    int tiles = 0, count = 0;
+    if (i < n) {
+        tiles = c.common[i];
+        const CacheSeq a = c.seqs[l.a[i]], z = c.seqs[l.a[i] + l.b[i] - 1];
+        if (tiles) count = (z.q_off + z.q_len - a.q_off + 2 * TT - 1) / (2 * TT);
+        for (int k = l.a[i]; k < l.a[i] + l.b[i]; ++k) s_of[k] = i;
+    }
+    int n_common, n_own;
+    const int at = block_sum(count, s_wi, n_common);
+    const int own = block_sum(i < n_seqs ? (c.seqs[i].q_len + 2 * TT - 1) / (2 * TT) : 0, s_wi, n_own);
+    if (i < n) {
+        s_common[i] = tiles;
+        s_begin[i] = at;
+    }
+    if (i < n_seqs) s_own[i] = n_common + own;
+    if (i == 0) {
+        s_begin[n] = n_common;
+        s_own[n_seqs] = n_common + n_own;
+    }
+    __syncthreads();
+    const int items = n_common + n_own;
+    // Largest k with off[k] <= x: the one whose range is not empty.
+    auto find = [](const int* off, int m, int x) {
+        int lo = 0, hi = m;
+        while (hi - lo > 1) {
+            const int k = (lo + hi) >> 1;
+            if (off[k] <= x) lo = k;
+            else hi = k;
+        }
+        return lo;
+    };
+    long long W = 0;
+    int two = 0;
+    for (int e0 = 0; e0 < items; e0 += kPlanThreads) {
+        const int e = e0 + i;
+        CacheGroup g = {};
+        if (e < n_common) {
+            const int k = find(s_begin, n, e);
+            const CacheSeq a = c.seqs[l.a[k]], z = c.seqs[l.a[k] + l.b[k] - 1];
+            const int tok = (e - s_begin[k]) * 2 * TT, all = z.q_off + z.q_len - a.q_off;
+            // (Any of the group's sequences with new tokens; their table rows agree.)
+            int lead = l.a[k];
+            while (c.seqs[lead].q_len == 0) ++lead;
+            g.seq = c.seqs[lead].seq;
+            g.kv_len = g.base = g.first = s_common[k] * kCacheTile;
+            g.row = a.q_off + tok;
+            g.ntok = min(2 * TT, all - tok);
+            g.t0 = 0;
+            g.common = 1;
+            g.cost = (s_common[k] + 1) << cache_two_tiles(g.ntok, TT);
+        } else if (e < items) {
+            const int k = find(s_own, n_seqs, e);
+            const CacheSeq s = c.seqs[k];
+            const int tok = (e - s_own[k]) * 2 * TT;
+            g.seq = s.seq;
+            g.kv_len = s.kv_len;
+            g.base = s.kv_len - s.q_len;
+            g.first = g.base + tok;
+            g.row = s.q_off + tok;
+            g.ntok = min(2 * TT, s.q_len - tok);
+            g.t0 = s_common[s_of[k]];
+            g.cost = (cache_group_tiles(s.q_len, s.kv_len, g.first, g.ntok) - g.t0 + 1) << cache_two_tiles(g.ntok, TT);
+        }
+        long long sum;
+        g.pre = W + block_sum((long long)g.cost, s_wl, sum);
+        W += sum;
+        two |= e < items && cache_two_tiles(g.ntok, TT);
+        if (e < items) c.groups[e] = g;
+    }
+    two = __syncthreads_or(two);
+    W *= c.Hkv;
+    const int n_ctas = !W ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles << (two ? 1 : 0))));
+    // Where parts lie: an item's pieces are as many as heads and cuts.
+    long long rows = 0;
+    for (int e0 = 0; e0 < items; e0 += kPlanThreads) {
+        const int e = e0 + i;
+        int mine = 0, r = 0, first = 0;
+        CacheGroup g = {};
+        if (e < items) {
+            g = c.groups[e];
+            r = cache_part_rows(g.ntok, TT, c.rep);
+            first = cache_cta_of(g.pre * c.Hkv, W, n_ctas);
+            const int last = cache_cta_of((g.pre + g.cost) * c.Hkv - 1, W, n_ctas);
+            mine = ((c.Hkv + last - first) * r + 31) & ~31;
+        }
+        long long sum;
+        const long long before = rows + block_sum((long long)mine, s_wl, sum);
+        rows += sum;
+        if (e < items) c.groups[e].part_row = (int)(before - (long long)first * r);
+    }
+    if (i == 0) {
+        c.plan->total = W;
+        c.plan->n_groups = items;
+        c.plan->n_ctas = n_ctas;
+    }
+    for (int t = i; t < T; t += kPlanThreads) {
+        const int k = c.owner[t], g = s_of[k], from = c.seqs[l.a[g]].q_off;
+        c.items_of[t] = make_int2(s_own[k] + (t - c.seqs[k].q_off) / (2 * TT),
+                                  s_common[g] ? s_begin[g] + (t - from) / (2 * TT) : -1);
+    }
+    __syncthreads();
+    for (int b = i; b < n_ctas; b += kPlanThreads) {
+        CacheShare sh;
+        sh.begin = W * b / n_ctas;
+        sh.end = W * (b + 1) / n_ctas;
+        const long long x = sh.begin / c.Hkv;
+        int lo = 0, hi = items;
+        while (hi - lo > 1) {
+            const int m = (lo + hi) >> 1;
+            if (c.groups[m].pre <= x) lo = m;
+            else hi = m;
+        }
+        sh.group = lo;
+        sh.g = c.groups[lo];
+        sh.within = sh.begin - sh.g.pre * c.Hkv;
+        sh.head = (int)(sh.within / sh.g.cost);
+        sh.within -= (long long)sh.head * sh.g.cost;
+        sh.first = sh.last = b;                        // (not used here)
+        c.shares[b] = sh;
+    }
+}
+
+template <int N>
+cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs, int T, cudaStream_t st) {
+    CacheList<N> l;
+    l.n = n;
+    int at = 0;
+    for (int i = 0; i < n; ++i) {
+        l.a[i] = at;
+        l.b[i] = counts[i];
+        at += counts[i];
+    }
+    const cudaError_t e = launch_pdl(cache_common_kernel<N>, dim3((unsigned)n), dim3(kCommonThreads), 0, st, c, l);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(cache_share_kernel<N>, dim3(1), dim3(kPlanThreads), 0, st, c, l, n_seqs, T);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, cudaStream_t st) {
+    return n <= 64 ? share_launch<64>(c, n, counts, n_seqs, T, st) : share_launch<kCacheMaxSeqs>(c, n, counts, n_seqs, T, st);
+}
+
+}  // namespace tmoe

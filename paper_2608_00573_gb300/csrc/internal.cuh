@@ -35,7 +35,8 @@ enum : int { ERR_NONE = TRIMMOE_DEVERR_NONE, ERR_TIMEOUT_PRODUCER = TRIMMOE_DEVE
              ERR_TIMEOUT_ROUTER = TRIMMOE_DEVERR_ROUTER, ERR_TIMEOUT_ATTN = TRIMMOE_DEVERR_ATTENTION,
              ERR_TIMEOUT_SELFTEST = TRIMMOE_DEVERR_SELFTEST,
              ERR_TIMEOUT_CACHE_ATTN = TRIMMOE_DEVERR_CACHE_ATTENTION, ERR_CACHE_FULL = TRIMMOE_DEVERR_CACHE_FULL,
-             ERR_CACHE_STATE = TRIMMOE_DEVERR_CACHE_STATE, ERR_CACHE_PATH = TRIMMOE_DEVERR_CACHE_PATH };
+             ERR_CACHE_STATE = TRIMMOE_DEVERR_CACHE_STATE, ERR_CACHE_PATH = TRIMMOE_DEVERR_CACHE_PATH,
+             ERR_CACHE_BLOCKS = TRIMMOE_DEVERR_CACHE_BLOCKS };
 
 // Device-side counters (trimmoe_stats_t is assembled from these).  The handle
 // keeps kCtrCopies copies, each on its own cache lines; a block of the
