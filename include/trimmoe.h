@@ -572,7 +572,8 @@ trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, const int32_t*
  * than 127 times; codes are floor(lo / scale) and ceil(hi / scale).  A page with an
  * infinity or a NaN among its keys has scale +infinity and codes 0.
  * From this call on accept recomputes what it moves, and compact takes the bounds along
- * with the pages.  No work is queued. */
+ * with the pages.  The first call allocates a workspace for select (32 MB at most, or
+ * one token's scores); no work is queued. */
 trimmoe_status trimmoe_cache_set_bounds(trimmoe_cache_handle c, int8_t* codes, float* scales);
 
 /* Bounds of one layer's pages that the step's new tokens filled to their end (whole != 0:
@@ -602,7 +603,7 @@ typedef struct {
     int32_t* blocks;
 } trimmoe_select_args;
 
-/* Needs trimmoe_cache_set_bounds and max_pages <= 40960. */
+/* Needs trimmoe_cache_set_bounds. */
 trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer, const trimmoe_select_args* a, void* stream);
 
 /* Arguments of trimmoe_cache_attend_blocks (device pointers as for attend).

@@ -147,6 +147,7 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         alloc(d.slot, cfg->T_max);
         alloc(d.pos, cfg->T_max);
         alloc(d.owner, cfg->T_max);
+        alloc(d.tokens, cfg->T_max);
         alloc(d.copies, (size_t)std::max(cfg->n_pages, cfg->max_seqs));
         alloc(d.fresh, cfg->n_pages);
         alloc(d.base, cfg->max_seqs);

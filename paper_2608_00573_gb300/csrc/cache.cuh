@@ -2,6 +2,8 @@
 // parameters and launchers.
 #pragma once
 
+#include <algorithm>
+
 #include "internal.cuh"
 
 namespace tmoe {
@@ -20,6 +22,12 @@ constexpr int kJoinHereRows = 16;
 // One listed sequence of the current step.
 struct CacheSeq {
     int seq, q_off, q_len, kv_len;     // kv_len: its length with the new tokens
+};
+
+// One new token of the current step: its sequence, the sequence's lengths with the step's tokens
+// and without, its position.
+struct __align__(16) CacheToken {
+    int seq, kv_len, base, pos;
 };
 
 // A group: up to two query tiles of one sequence, that is ntok consecutive new
@@ -103,7 +111,8 @@ struct CacheDev {
     CacheShare* shares;                // [num_sms]
     int* slot;                         // [T_max] page row (page * page_size + place) of each new token, -1 none
     int* pos;                          // [T_max] its position in its sequence
-    int* owner;                        // [T_max] its place in seqs
+    int* owner;                        // [T_max] its sequence's place in seqs
+    CacheToken* tokens;                // [T_max] valid behind a step that was not refused
     int2* copies;                      // [max(n_pages, max_seqs)] (from, to) pages
     int* fresh;                        // [n_pages] free pages taken by a step; new place of each page (compact)
     int* base;                         // [max_seqs] length before the sequence's last step
@@ -116,6 +125,7 @@ struct CacheDev {
     // Bounds of the keys of whole pages (trimmoe_cache_set_bounds), or NULL.
     int8_t* codes;                     // [layers][n_pages][Hkv][2][dh]
     float* scales;                     // [layers][n_pages][Hkv]
+    uint32_t* scores;                  // [cache_score_keys] of a choice, as ordered whole numbers
     // Steps with groups of sequences: the list of items is in `groups` and the parts in part_o and
     // part_ml as for other steps, but these are other, larger buffers (the host side chooses).
     int shared;
@@ -164,14 +174,18 @@ struct BlocksParams {
     float scale_log2;
 };
 
-// Columns of the page table at most (their scores lie in shared memory).
-constexpr int kSelectPages = 40960;
-
 struct SelectParams {
     const __nv_bfloat16* q;
     int* blocks;                       // [T][Hkv][n]
-    int ld_q, T, n, first, last, layer;
+    int ld_q, T, n, first, last, layer, max_q;
 };
+
+// Room for the scores of a choice: 8 M blocks (32 MB), fewer when no step has as many, one token's
+// at least.
+inline size_t cache_score_keys(const CacheDev& c) {
+    const size_t row = (((size_t)c.max_pages + 3) & ~size_t(3)) * c.Hkv;
+    return std::max(row, std::min(row * c.T_max, (size_t)8 << 20));
+}
 
 // Steps with groups of sequences: rows (tokens times query heads) at most, and what that allows.
 constexpr int kShareRows = 65536;
@@ -198,7 +212,7 @@ cudaError_t launch_cache_bounds(const CacheDev& c, int layer, int n, int max_q, 
 // Of those that accepted drafts filled, in all layers (accepted: the accept kernel's new lengths, -1: none).
 cudaError_t launch_cache_bounds_accepted(const CacheDev& c, int n, const int* seq, const int* n_acc, const int* accepted,
                                          cudaStream_t st);
-cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st);
+cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches);
 cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                 const BlocksParams& p, cudaStream_t st);
 // The list of items of a step whose listed sequences form n groups.

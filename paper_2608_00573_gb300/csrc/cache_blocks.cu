@@ -67,6 +67,23 @@ extern "C" trimmoe_status trimmoe_cache_set_bounds(trimmoe_cache_handle c, int8_
     if (!codes != !scales) return c->fail(TRIMMOE_ERR_ARG, "cache_set_bounds", "codes and scales come together");
     if (!aligned16(codes) || (reinterpret_cast<uintptr_t>(scales) & 3u))
         return c->fail(TRIMMOE_ERR_ARG, "cache_set_bounds", "pointers must be aligned (codes 16 bytes, scales 4)");
+    if (codes && !c->d.scores) {
+        OnDevice on(c->dev);
+        cudaGetLastError();
+        void* q = nullptr;
+        try {
+            c->allocs.reserve(c->allocs.size() + 1);
+        } catch (const std::bad_alloc&) {
+            return c->fail(TRIMMOE_ERR_OOM, "cache_set_bounds", "host allocation failed");
+        }
+        const cudaError_t e = cudaMalloc(&q, cache_score_keys(c->d) * sizeof(uint32_t));
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            return c->fail(e == cudaErrorMemoryAllocation ? TRIMMOE_ERR_OOM : TRIMMOE_ERR_CUDA, "cache_set_bounds", cudaGetErrorString(e));
+        }
+        c->allocs.push_back(q);
+        c->d.scores = static_cast<uint32_t*>(q);
+    }
     c->d.codes = codes;
     c->d.scales = scales;
     return TRIMMOE_OK;
@@ -90,7 +107,6 @@ extern "C" trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer
     const CacheDev& d = c->d;
     if (!a) return c->fail(TRIMMOE_ERR_ARG, "cache_select", "NULL argument");
     if (!d.codes) return c->fail(TRIMMOE_ERR_ARG, "cache_select", "no bounds have been set");
-    if (d.max_pages > kSelectPages) return c->fail(TRIMMOE_ERR_UNSUPPORTED, "cache_select", "max_pages must be <= 40960");
     if (a->n < 1 || a->first < 0 || a->last < 0 || a->first > a->n || a->last > a->n - a->first)
         return c->fail(TRIMMOE_ERR_ARG, "cache_select", "n must be >= 1, first and last >= 0 and together at most n");
     if (c->T == 0) return TRIMMOE_OK;
@@ -108,9 +124,12 @@ extern "C" trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer
     p.first = a->first;
     p.last = a->last;
     p.layer = layer;
+    p.max_q = c->max_q;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_select");
-    return c->launched(launch_cache_select(d, p, enter(c, stream)), 1, "cache_select");
+    int launches = 0;
+    const cudaError_t e = launch_cache_select(d, p, enter(c, stream), launches);
+    return c->launched(e, launches, "cache_select");
 }
 
 extern "C" trimmoe_status trimmoe_cache_attend_blocks(trimmoe_cache_handle c, int layer, const trimmoe_blocks_args* a,

@@ -102,11 +102,11 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         it.head = index % per / p.row_tiles;
         it.row0 = index % p.row_tiles * 16;
         it.rows = min(16, c.rep - it.row0);
-        const CacheSeq s = c.seqs[c.owner[it.t]];
+        const CacheToken s = c.tokens[it.t];
         it.seq = s.seq;
         it.kv_len = s.kv_len;
-        it.base = s.kv_len - s.q_len;
-        it.pos = it.base + it.t - s.q_off;
+        it.base = s.base;
+        it.pos = s.pos;
         it.first_own = it.base >> c.page_shift;
         it.listed = min(p.n, it.first_own);
         const int last = p.tree ? it.kv_len - 1 : it.pos;

@@ -353,6 +353,7 @@ __global__ void __launch_bounds__(kCopyThreads) cache_fill_kernel(const __grid_c
             pos = s.kv_len - s.q_len + (t - s.q_off);
             slot = (c.table[(size_t)s.seq * c.max_pages + (pos >> c.page_shift)] << c.page_shift) +
                    (pos & (c.page - 1));
+            c.tokens[t] = CacheToken{s.seq, s.kv_len, s.kv_len - s.q_len, pos};
         }
         c.slot[t] = slot;
         c.pos[t] = pos;

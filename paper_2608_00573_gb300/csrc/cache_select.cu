@@ -5,10 +5,11 @@
 //   ceil(hi / u) in 8 bits; u = 2^e, e the least one with max(|lo|, |hi|) <= 127 u
 //   score = u max_h u_h sum_d max(c_hd lo_d, c_hd hi_d),  c_h = rint(q_h / u_h)
 //
-// With q+ = max(c, 0) and q- = min(c, 0) the sum is q+ . hi + q- . lo, two dot products of
-// 8-bit numbers.  It is at most 128 * 127 * 127 < 2^24, so that every score is exact in fp32
+// With q+ = max(c, 0) and q- = min(c, 0) the sum is q- . lo + q+ . hi, a product of 8-bit numbers
+// with 2 D terms.  It is at most 128 * 127 * 127 < 2^24, so that every score is exact in fp32
 // and the order of the blocks (ties: the lower one) does not depend on how it is computed.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -139,37 +140,36 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
-__host__ __device__ inline size_t select_smem(const CacheDev& c) {
-    return (((size_t)c.max_pages * 4 + 15) & ~size_t(15)) + (size_t)c.rep * c.dh * 2;
-}
+// ------------------------------------------------------------------ queries and scores
 
-// A block takes one token and key/value head: its query heads as 8-bit codes in shared
-// memory, the blocks' scores (four lanes to a block), the n-th largest of them by four
-// counting passes over its digits, and the columns at or above it in order.
+// Query heads as columns of a matrix of 8-bit codes, 2 D rows: the negative ones first, then the
+// positive ones, so that a block's score for a head is the product of its bounds, lo first, with
+// that column.  A token has M columns (1, 2, 4), or with M = 8 a multiple of 8; those past its
+// query heads repeat the last one.  Eight columns are a group; columns past the tokens are zero.
+__host__ __device__ constexpr int columns_of(int rep) { return rep > 4 ? (rep + 7) & ~7 : rep == 3 ? 4 : rep; }
+__host__ __device__ inline int coded_columns(int rep, int tokens) { return (tokens * columns_of(rep) + 7) & ~7; }
+__host__ __device__ inline size_t coded_bytes(int rep, int dh, int tokens) { return (size_t)coded_columns(rep, tokens) * (2 * dh + 4); }
+
 template <int DH>
-__global__ void __launch_bounds__(kThreads) cache_select_kernel(const __grid_constant__ CacheDev c,
-                                                                const __grid_constant__ SelectParams p) {
-    constexpr int K = DH / 64, G = 2;                 // 16-byte pieces of a lane, blocks in flight of a lane
-    extern __shared__ __align__(16) uint32_t smem[];
-    __shared__ float s_unit[128];
-    __shared__ int s_hist[256], s_digit, s_left, s_all, s_gt[kWarps], s_eq[kWarps];
-    uint32_t* key = smem;
-    int8_t* s_pos = reinterpret_cast<int8_t*>(smem) + (((size_t)c.max_pages * 4 + 15) & ~size_t(15));
-    int8_t* s_neg = s_pos + c.rep * DH;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int t = blockIdx.x / c.Hkv, h = blockIdx.x - t * c.Hkv, n = p.n;
-    pdl_wait();
-    pdl_trigger();
-    if (!c.plan->ok) return;
-    const CacheSeq s = c.seqs[c.owner[t]];
-    const int F = (s.kv_len - s.q_len) >> c.page_shift;
-    int* out = p.blocks + ((size_t)t * c.Hkv + h) * n;
-    if (F <= n) {
-        for (int i = threadIdx.x; i < n; i += kThreads) out[i] = i < F ? i : -1;
-        return;
+struct Coded {
+    int8_t* code;                      // [columns][2 DH]
+    float* unit;                       // [columns]
+    __device__ Coded(void* at, int columns) {
+        code = static_cast<int8_t*>(at);
+        unit = reinterpret_cast<float*>(code + (size_t)columns * 2 * DH);
     }
-    for (int r = warp; r < c.rep; r += kWarps) {
-        const __nv_bfloat16* q = p.q + (size_t)t * p.ld_q + (size_t)(h * c.rep + r) * DH + lane * 2 * K;
+};
+
+// A column per warp; `tokens` of the tokens exist.
+template <int DH>
+__device__ __forceinline__ void code_queries(const CacheDev& c, const SelectParams& p, const Coded<DH>& out, int columns, int h,
+                                             int first_token, int tokens) {
+    constexpr int K = DH / 64;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = columns_of(c.rep);
+    for (int u = warp; u < columns; u += kWarps) {
+        const int k = u / per, r = min(u - k * per, c.rep - 1);
+        const bool real = k < tokens;
+        const __nv_bfloat16* q = p.q + (size_t)(first_token + (real ? k : 0)) * p.ld_q + (size_t)(h * c.rep + r) * DH + lane * 2 * K;
         uint32_t w[K], amax = 0;
 #pragma unroll
         for (int j = 0; j < K; ++j) {
@@ -178,159 +178,440 @@ __global__ void __launch_bounds__(kThreads) cache_select_kernel(const __grid_con
             amax = max(amax, max(a << 16, a & 0xffff0000u));
         }
         amax = __reduce_max_sync(0xffffffffu, amax);
-        const bool finite = amax < 0x7f800000u;
+        const bool finite = real && amax < 0x7f800000u;
         const int e = unit_exponent(__uint_as_float(amax));
         const float inv = finite ? two_to(-e) : 0.f;
-        uint16_t* pos = reinterpret_cast<uint16_t*>(s_pos + r * DH) + lane * K;
-        uint16_t* neg = reinterpret_cast<uint16_t*>(s_neg + r * DH) + lane * K;
+        uint16_t* neg = reinterpret_cast<uint16_t*>(out.code + (size_t)u * 2 * DH) + lane * K;
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             const int a = finite ? __float2int_rn(bf16_lo(w[j]) * inv) : 0, b = finite ? __float2int_rn(bf16_hi(w[j]) * inv) : 0;
-            pos[j] = (uint16_t)(max(a, 0) | max(b, 0) << 8);
             neg[j] = (uint16_t)((min(a, 0) & 0xff) | (min(b, 0) & 0xff) << 8);
+            neg[DH / 2 + j] = (uint16_t)(max(a, 0) | max(b, 0) << 8);
         }
-        if (lane == 0) s_unit[r] = finite ? two_to(e) : 0.f;
-    }
-    __syncthreads();
-    // Lane 4 b + i holds bytes 16 i .. 16 i + 15 (and 64 more) of block b's lo and hi.
-    const int part = lane & 3;
-    const int* row = c.table + (size_t)s.seq * c.max_pages;
-    const size_t layer = (size_t)p.layer * c.n_pages;
-    for (int b0 = warp * 8 * G; b0 < F; b0 += kWarps * 8 * G) {
-        int4 lo[G][K], hi[G][K];
-        float scale[G], best[G];
-        bool there[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int b = b0 + g * 8 + (lane >> 2), id = row[min(b, F - 1)];
-            there[g] = id >= 0 && id < c.n_pages;
-            const size_t unit = (layer + (there[g] ? id : 0)) * c.Hkv + h;
-            const int4* src = reinterpret_cast<const int4*>(c.codes + unit * 2 * DH) + part;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                lo[g][k] = __ldg(src + 4 * k);
-                hi[g][k] = __ldg(src + DH / 16 + 4 * k);
-            }
-            scale[g] = __ldg(c.scales + unit);
-            best[g] = -INFINITY;
-        }
-        for (int r = 0; r < c.rep; ++r) {
-            const float u = s_unit[r];
-            int4 qp[K], qn[K];
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                qp[k] = reinterpret_cast<const int4*>(s_pos + r * DH)[4 * k + part];
-                qn[k] = reinterpret_cast<const int4*>(s_neg + r * DH)[4 * k + part];
-            }
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                int sum = 0;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    sum = __dp4a(qp[k].x, hi[g][k].x, sum);
-                    sum = __dp4a(qn[k].x, lo[g][k].x, sum);
-                    sum = __dp4a(qp[k].y, hi[g][k].y, sum);
-                    sum = __dp4a(qn[k].y, lo[g][k].y, sum);
-                    sum = __dp4a(qp[k].z, hi[g][k].z, sum);
-                    sum = __dp4a(qn[k].z, lo[g][k].z, sum);
-                    sum = __dp4a(qp[k].w, hi[g][k].w, sum);
-                    sum = __dp4a(qn[k].w, lo[g][k].w, sum);
-                }
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                best[g] = fmaxf(best[g], (float)sum * u);
-            }
-        }
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int b = b0 + g * 8 + (lane >> 2);
-            if (part == 0 && b < F) {
-                // (A page without an index scores nothing; + 0 turns -0 into 0.)
-                const float x = scale[g] == INFINITY ? INFINITY : best[g] * scale[g] + 0.f;
-                key[b] = b < p.first || b >= F - p.last ? 0xffffffffu : there[g] ? ordered(x) : 0u;
-                if (!there[g]) atomicCAS(c.err, 0, ERR_CACHE_STATE);
-            }
-        }
-    }
-    // The n-th largest key: digit by digit from the top, `left` of the keys that agree so far
-    // are still wanted.
-    uint32_t prefix = 0, mask = 0;
-    int left = n;
-    bool all = false;                                 // all that agree with the digits so far are wanted
-    for (int shift = 24; shift >= 0 && !all; shift -= 8) {
-        s_hist[threadIdx.x] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < F; i += kThreads)
-            if ((key[i] & mask) == prefix) atomicAdd(&s_hist[key[i] >> shift & 255u], 1);
-        __syncthreads();
-        if (warp == 0) {
-            int mine[8], sum = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += mine[j] = s_hist[255 - lane * 8 - j];
-            int below = sum;                          // of this lane's digits and all larger ones
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, below, o);
-                if (lane >= o) below += y;
-            }
-            int before = below - sum;
-            if (before < left && below >= left) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (before < left && before + mine[j] >= left) {
-                        s_digit = 255 - lane * 8 - j;
-                        s_left = left - before;
-                        s_all = mine[j] == left - before;
-                    }
-                    before += mine[j];
-                }
-            }
-        }
-        __syncthreads();
-        prefix |= (uint32_t)s_digit << shift;
-        mask |= 255u << shift;
-        left = s_left;
-        all = s_all;
-        __syncthreads();
-    }
-    // Keys above the prefix are taken, of those that agree with it the first `left`.
-    const int per = ((F + kThreads - 1) / kThreads) * 32, i0 = warp * per, i1 = min(F, i0 + per);
-    int gt = 0, eq = 0;
-    for (int i = i0 + lane; i - lane < i1; i += 32) {
-        const uint32_t k = i < i1 ? key[i] & mask : 0u;
-        gt += __popc(__ballot_sync(0xffffffffu, i < i1 && k > prefix));
-        eq += __popc(__ballot_sync(0xffffffffu, i < i1 && k == prefix));
-    }
-    if (lane == 0) {
-        s_gt[warp] = gt;
-        s_eq[warp] = eq;
-    }
-    __syncthreads();
-    gt = eq = 0;
-    for (int w = 0; w < warp; ++w) {
-        gt += s_gt[w];
-        eq += s_eq[w];
-    }
-    const uint32_t below = (1u << lane) - 1u;
-    for (int i = i0 + lane; i - lane < i1; i += 32) {
-        const uint32_t k = i < i1 ? key[i] & mask : 0u;
-        const bool more = i < i1 && k > prefix, same = i < i1 && k == prefix;
-        const uint32_t mg = __ballot_sync(0xffffffffu, more), me = __ballot_sync(0xffffffffu, same);
-        const int g = gt + __popc(mg & below), e = eq + __popc(me & below);
-        if (more || (same && e < left)) out[g + min(e, left)] = i;
-        gt += __popc(mg);
-        eq += __popc(me);
+        if (lane == 0) out.unit[u] = finite ? two_to(e) : 0.f;
     }
 }
 
-template <int DH>
-cudaError_t select_launch(const CacheDev& c, const SelectParams& p, cudaStream_t st) {
-    static PerDevice attr;
-    const cudaError_t e = (cudaError_t)attr.get([] {
-        return (int)cudaFuncSetAttribute(cache_select_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-    }, true);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(cache_select_kernel<DH>, dim3((unsigned)(p.T * c.Hkv)), dim3(kThreads), select_smem(c), st, c, p);
+__device__ __forceinline__ void mma_s8(int (&c)[4], int a0, int a1, int a2, int a3, int b0, int b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Scores of one sequence's blocks for tokens [a, end) of the coded ones: put(token, block, key).
+// A warp takes 16 blocks from 16 `from` on, then those `stride` times as many on, below F: the 16 rows
+// of a product with 8 columns and 2 D terms in whole numbers.  The terms' order is free, so a
+// lane takes 16 bytes of a row at a time, as they lie.  (One instruction for 32 four-number products;
+// with those, and sums across lanes, the search of 48 contexts took 26 us instead of 17.)
+// ONE: all columns are one group, which stays in registers.
+template <int DH, int M, bool ONE, class Put>
+__device__ __forceinline__ void score_blocks(const CacheDev& c, int layer_at, const Coded<DH>& q, int h, int seq, int F, int a, int end,
+                                             int from, int stride, Put put) {
+    constexpr int P = DH / 32;                        // 16-byte pieces of a lane and row
+    const int lane = threadIdx.x & 31, r = lane >> 2, part = lane & 3;
+    const int* row = c.table + (size_t)seq * c.max_pages;
+    const size_t layer = (size_t)layer_at * c.n_pages;
+    const int per = columns_of(c.rep);                // (M, or a multiple of 8)
+    const int g0 = a * per / 8, g1 = (end * per + 7) / 8;
+    int4 col[P];
+    auto columns = [&](int g) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) col[k] = reinterpret_cast<const int4*>(q.code + (size_t)(g * 8 + r) * 2 * DH)[4 * k + part];
+    };
+    if (ONE) columns(g0);
+    int next[2];
+    auto look_up = [&](int b0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) next[i] = b0 + r + 8 * i < F ? row[b0 + r + 8 * i] : 0;
+    };
+    look_up(from * 16);
+    for (int b0 = from * 16; b0 < F; b0 += stride * 16) {
+        int4 x[2][P];
+        float scale[2];
+        bool there[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            there[i] = next[i] >= 0 && next[i] < c.n_pages;
+            const size_t unit = (layer + (there[i] ? next[i] : 0)) * c.Hkv + h;
+            const int4* src = reinterpret_cast<const int4*>(c.codes + unit * 2 * DH) + part;
+#pragma unroll
+            for (int k = 0; k < P; ++k) x[i][k] = __ldg(src + 4 * k);
+            scale[i] = __ldg(c.scales + unit);
+        }
+        look_up(b0 + stride * 16);
+        // (A page without an index scores nothing; + 0 turns -0 into 0.)
+        auto give = [&](int i, int t, float best) {
+            const int b = b0 + r + 8 * i;
+            if (b >= F || t < a || t >= end) return;
+            const float s = scale[i] == INFINITY ? INFINITY : best * scale[i] + 0.f;
+            put(t, b, there[i] ? ordered(s) : 0u);
+            if (!there[i]) atomicCAS(c.err, 0, ERR_CACHE_STATE);
+        };
+        float best[2] = {-INFINITY, -INFINITY};
+        for (int g = g0; g < g1; ++g) {
+            if (!ONE) columns(g);
+            int sum[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                mma_s8(sum, x[0][k].x, x[1][k].x, x[0][k].y, x[1][k].y, col[k].x, col[k].y);
+                mma_s8(sum, x[0][k].z, x[1][k].z, x[0][k].w, x[1][k].w, col[k].z, col[k].w);
+            }
+            const float2 unit = *reinterpret_cast<const float2*>(q.unit + g * 8 + part * 2);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float s0 = (float)sum[2 * i] * unit.x, s1 = (float)sum[2 * i + 1] * unit.y;
+                if (M == 1) {
+                    give(i, g * 8 + part * 2, s0);
+                    give(i, g * 8 + part * 2 + 1, s1);
+                } else {
+                    float s = fmaxf(s0, s1);
+                    if (M == 2) give(i, g * 4 + part, s);
+                    if (M >= 4) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, 1));
+                    if (M == 4 && !(part & 1)) give(i, g * 2 + (part >> 1), s);
+                    if (M == 8) {
+                        best[i] = fmaxf(best[i], fmaxf(s, __shfl_xor_sync(0xffffffffu, s, 2)));
+                        if ((g * 8 + 8) % per == 0) {
+                            if (part == 0) give(i, g * 8 / per, best[i]);
+                            best[i] = -INFINITY;
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------- choice
+
+// Scratch of a choice in shared memory.
+constexpr int kCandidates = 64;
+struct Choice {
+    uint32_t hist[288];                // counts of digits, see hist_at
+    uint32_t key[kCandidates];
+    int col[kCandidates];
+    int count;                         // candidates
+    uint32_t both[kWarps], any[kWarps];
+    int digit, left, last;             // of the digit that holds the n-th key; column of the last key taken
+    uint32_t bound;                    // that key
+};
+
+// Keys above `bound` are taken, and those equal to it up to column `last`.
+struct Cut {
+    uint32_t bound;
+    int last;
+    __device__ bool takes(uint32_t key, int col) const { return key > bound || (key == bound && col <= last); }
+};
+
+// Where a digit's count lies (a lane reads eight digits in a row: no two lanes the same bank).
+__device__ __forceinline__ int hist_at(uint32_t digit) { return (int)(digit + (digit >> 3)); }
+
+// The cut that takes the n largest of keys [lo, hi) (n < hi - lo; equal ones: lower columns first).
+// WARPS warps take part, `me` their thread; sync is their barrier.  One pass counts the keys by
+// the 8 bits below those that all agree on, one collects the keys of the digit that the n-th has,
+// which are ranked one by one; when they are many (keys in few clusters), bits are
+// decided one at a time instead.
+template <int WARPS, class Key, class Sync>
+__device__ __forceinline__ Cut cut_of(Key key, int lo, int hi, int n, int me, Choice& s, Sync sync) {
+    constexpr int THREADS = WARPS * 32;
+    const int warp = me >> 5, lane = me & 31;
+    uint32_t both = 0xffffffffu, any = 0;
+    for (int i = lo + me; i < hi; i += THREADS) {
+        const uint32_t k = key(i);
+        both &= k;
+        any |= k;
+    }
+    for (int i = me; i < 288; i += THREADS) s.hist[i] = 0;
+    if (me == 0) s.count = 0;
+    both = __reduce_and_sync(0xffffffffu, both);
+    any = __reduce_or_sync(0xffffffffu, any);
+    if (WARPS > 1) {
+        if (lane == 0) {
+            s.both[warp] = both;
+            s.any[warp] = any;
+        }
+    }
+    sync();
+    if (WARPS > 1) {
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            both &= s.both[w];
+            any |= s.any[w];
+        }
+    }
+    const int shift = max(0, 24 - __clz(both ^ any | 1u));      // the digit is the key's bits shift .. shift + 7
+    const uint32_t high = shift > 23 ? 0u : both >> (shift + 8) << (shift + 8);   // common bits above it
+    for (int i = lo + me; i < hi; i += THREADS) atomicAdd(&s.hist[hist_at(key(i) >> shift & 255u)], 1u);
+    sync();
+    if (warp == 0) {
+        int mine[8], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += mine[j] = s.hist[hist_at(255 - lane * 8 - j)];
+        int upto = sum;                               // keys of this lane's digits and larger ones
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        int before = upto - sum;
+        if (before < n && upto >= n) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (before < n && before + mine[j] >= n) {
+                    s.digit = 255 - lane * 8 - j;
+                    s.left = n - before;
+                }
+                before += mine[j];
+            }
+        }
+    }
+    sync();
+    const uint32_t low = high | (uint32_t)s.digit << shift;     // least key with the digit
+    const int left = s.left, count = (int)s.hist[hist_at(s.digit)];
+    if (left == count) return low ? Cut{low - 1, -1} : Cut{0, 0x7fffffff};     // all of the digit
+    const uint32_t mask = shift ? ~((1u << shift) - 1u) : ~0u;
+    if (count <= kCandidates) {
+        for (int i = lo + me; i < hi; i += THREADS) {
+            const uint32_t k = key(i);
+            if ((k & mask) == low) {
+                const int at = atomicAdd(&s.count, 1);
+                s.key[at] = k;
+                s.col[at] = i;
+            }
+        }
+        sync();
+        if (warp == 0) {
+#pragma unroll
+            for (int x = lane; x < kCandidates; x += 32)
+                if (x < count) {
+                    int rank = 0;
+                    for (int y = 0; y < count; ++y)
+                        rank += s.key[y] > s.key[x] || (s.key[y] == s.key[x] && s.col[y] < s.col[x]);
+                    if (rank == left - 1) {
+                        s.bound = s.key[x];
+                        s.last = s.col[x];
+                    }
+                }
+        }
+        sync();
+        return Cut{s.bound, s.last};
+    }
+    // The largest key with at least `left` of the candidates at or above it, bit by bit.
+    auto total = [&](int v) {
+        v = __reduce_add_sync(0xffffffffu, v);
+        if (WARPS == 1) return v;
+        sync();
+        if (lane == 0) s.hist[warp] = v;
+        sync();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) all += s.hist[w];
+        return all;
+    };
+    uint32_t bound = low;
+    int above = 0;                                    // candidates above all that begin with bound's decided bits
+    for (int bit = shift - 1; bit >= 0; --bit) {
+        const uint32_t t = bound | 1u << bit;
+        int at_least = 0;
+        for (int i = lo + me; i < hi; i += THREADS) {
+            const uint32_t k = key(i);
+            at_least += (k & mask) == low && k >= t;
+        }
+        at_least = total(at_least);
+        if (at_least >= left) bound = t;
+        else above = at_least;
+    }
+    // Of the keys equal to it the first left - above: the column of the last of them.
+    int tie = left - above, last = 0x7fffffff;
+    for (int i0 = lo; i0 < hi && tie > 0; i0 += THREADS) {
+        const int i = i0 + me;
+        const bool same = i < hi && key(i) == bound;
+        const uint32_t m = __ballot_sync(0xffffffffu, same);
+        int before = 0;
+        if (WARPS > 1) {
+            sync();
+            if (lane == 0) s.hist[warp] = __popc(m);
+            sync();
+            for (int w = 0; w < warp; ++w) before += s.hist[w];
+        }
+        if (same && before + __popc(m & ((1u << lane) - 1u)) == tie - 1) s.last = i;
+        tie -= total(same);
+    }
+    sync();
+    last = s.last;
+    return Cut{bound, last};
+}
+
+// A sequence's list when all of its F blocks fit, or its forced columns: [0, first) and [F - last, F).
+__device__ __forceinline__ void list_ends(int* out, int n, int F, int first, int last, int me, int threads) {
+    if (F <= n) {
+        for (int i = me; i < n; i += threads) out[i] = i < F ? i : -1;
+    } else {
+        for (int i = me; i < first; i += threads) out[i] = i;
+        for (int i = me; i < last; i += threads) out[n - last + i] = F - last + i;
+    }
+}
+
+// ------------------------------------------------------------------------------ kernels
+
+// Eight tokens and a key/value head: scores in shared memory, read from bounds that are read once
+// for the tokens of a sequence, then a warp chooses for each token.
+//
+// Bound: the dot products, D / 2 four-number products per block of keys and query head, and the
+// choice, some 300 instructions of a warp per list.
+constexpr int kTile = 8;
+__host__ __device__ inline size_t score_row(const CacheDev& c) { return ((size_t)c.max_pages + 3) & ~size_t(3); }
+__host__ __device__ inline size_t tile_bytes(const CacheDev& c) {
+    return kTile * score_row(c) * 4 + coded_bytes(c.rep, c.dh, kTile) + kWarps * sizeof(Choice);
+}
+
+template <int DH, int M>
+__global__ void __launch_bounds__(kThreads, 3) cache_select_tile_kernel(const __grid_constant__ CacheDev c,
+                                                                     const __grid_constant__ SelectParams p) {
+    extern __shared__ __align__(16) uint32_t smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n = p.n, columns = coded_columns(c.rep, kTile);
+    const size_t row_len = score_row(c);
+    const Coded<DH> q(smem + kTile * row_len, columns);
+    Choice& choice = reinterpret_cast<Choice*>(reinterpret_cast<uint8_t*>(smem + kTile * row_len) + coded_bytes(c.rep, DH, kTile))[warp];
+    const int h = blockIdx.x % c.Hkv, first_token = blockIdx.x / c.Hkv * kTile, tokens = min(kTile, p.T - first_token);
+    pdl_wait();
+    pdl_trigger();
+    if (!c.plan->ok) return;
+    code_queries<DH>(c, p, q, columns, h, first_token, tokens);
+    __syncthreads();
+    // Runs of tokens of one sequence (one run for most blocks of threads).
+    for (int a = 0; a < tokens;) {
+        const CacheToken tok = c.tokens[first_token + a];
+        const int end = min(tokens, a + tok.kv_len - tok.pos), F = tok.base >> c.page_shift;
+        if (F > n) {
+            score_blocks<DH, M, M == 1>(c, p.layer, q, h, tok.seq, F, a, end, warp, kWarps, [&](int t, int b, uint32_t key) { smem[t * row_len + b] = key; });
+            __syncthreads();
+        }
+        for (int t = a + warp; t < end; t += kWarps) {
+            int* out = p.blocks + ((size_t)(first_token + t) * c.Hkv + h) * n;
+            list_ends(out, n, F, p.first, p.last, lane, 32);
+            const int lo = p.first, hi = F - p.last, want = n - p.first - p.last;
+            if (F <= n || want == 0) continue;
+            const uint32_t* key = smem + t * row_len;
+            const Cut cut = cut_of<1>([&](int i) { return key[i]; }, lo, hi, want, lane, choice, [] { __syncwarp(); });
+            int at = p.first;
+            for (int i0 = lo; i0 < hi; i0 += 32) {
+                const int i = i0 + lane;
+                const bool take = i < hi && cut.takes(key[i], i);
+                const uint32_t m = __ballot_sync(0xffffffffu, take);
+                if (take) out[at + __popc(m & ((1u << lane) - 1u))] = i;
+                at += __popc(m);
+            }
+            __syncwarp();
+        }
+        a = end;
+        if (a < tokens) __syncthreads();              // the next run writes scores
+    }
+}
+
+// Single tokens: the scores, by as many blocks of threads per token and key/value head as fill the
+// GPU, to a buffer; then a block of threads per token and head chooses.
+//
+// Bound: HBM, 2 D + 4 bytes per block of keys and head.
+template <int DH, int M>
+__global__ void __launch_bounds__(kThreads) cache_score_kernel(const __grid_constant__ CacheDev c,
+                                                               const __grid_constant__ SelectParams p, int first_token, int split) {
+    extern __shared__ __align__(16) uint32_t smem[];
+    const int item = blockIdx.x / split, chunk = blockIdx.x - item * split;
+    const int k = item / c.Hkv, h = item - k * c.Hkv, columns = coded_columns(c.rep, 1);
+    const Coded<DH> q(smem, columns);
+    pdl_wait();
+    pdl_trigger();
+    const int ok = c.plan->ok;
+    const CacheToken tok = c.tokens[first_token + k];
+    const int F = tok.base >> c.page_shift, warp = threadIdx.x >> 5;
+    if (!ok || F <= p.n || chunk * kWarps * 16 >= F) return;
+    code_queries<DH>(c, p, q, columns, h, first_token + k, 1);
+    __syncthreads();
+    uint32_t* out = c.scores + (size_t)item * score_row(c);
+    score_blocks<DH, M, M < 8>(c, p.layer, q, h, tok.seq, F, 0, 1, chunk * kWarps + warp, split * kWarps,
+                               [&](int, int b, uint32_t key) { out[b] = key; });
+}
+
+__global__ void __launch_bounds__(kThreads) cache_choose_kernel(const __grid_constant__ CacheDev c,
+                                                                const __grid_constant__ SelectParams p, int first_token) {
+    constexpr int kHeld = 8;                          // keys of a thread that stay in registers
+    __shared__ Choice choice;
+    __shared__ int s_taken[kWarps];
+    const int item = blockIdx.x, k = item / c.Hkv, h = item - k * c.Hkv, n = p.n;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_wait();
+    pdl_trigger();
+    if (!c.plan->ok) return;
+    const int F = c.tokens[first_token + k].base >> c.page_shift;
+    int* out = p.blocks + ((size_t)(first_token + k) * c.Hkv + h) * n;
+    list_ends(out, n, F, p.first, p.last, threadIdx.x, kThreads);
+    const int lo = p.first, hi = F - p.last, want = n - p.first - p.last;
+    if (F <= n || want == 0) return;
+    const uint32_t* keys = c.scores + (size_t)item * score_row(c);
+    auto sync = [] { __syncthreads(); };
+    Cut cut;
+    if (hi - lo <= kHeld * kThreads) {
+        uint32_t held[kHeld];
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const int i = lo + j * kThreads + threadIdx.x;
+            held[j] = i < hi ? __ldcg(keys + i) : 0u;
+        }
+        auto key = [&](int i) {
+            uint32_t v = held[0];
+#pragma unroll
+            for (int j = 1; j < kHeld; ++j) v = i - lo >= j * kThreads ? held[j] : v;
+            return v;
+        };
+        cut = cut_of<kWarps>(key, lo, hi, want, threadIdx.x, choice, sync);
+    } else {
+        cut = cut_of<kWarps>([&](int i) { return __ldcg(keys + i); }, lo, hi, want, threadIdx.x, choice, sync);
+    }
+    // A warp takes a range of columns: how many, then which.
+    const int per = (hi - lo + kThreads - 1) / kThreads * 32, i0 = lo + warp * per, i1 = min(hi, i0 + per);
+    int taken = 0;
+    for (int i = i0 + lane; i - lane < i1; i += 32)
+        taken += __popc(__ballot_sync(0xffffffffu, i < i1 && cut.takes(__ldcg(keys + i), i)));
+    if (lane == 0) s_taken[warp] = taken;
+    __syncthreads();
+    int at = p.first;
+    for (int w = 0; w < warp; ++w) at += s_taken[w];
+    for (int i = i0 + lane; i - lane < i1; i += 32) {
+        const bool take = i < i1 && cut.takes(__ldcg(keys + i), i);
+        const uint32_t m = __ballot_sync(0xffffffffu, take);
+        if (take) out[at + __popc(m & ((1u << lane) - 1u))] = i;
+        at += __popc(m);
+    }
+}
+
+template <int DH, int M>
+cudaError_t select_launch(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches) {
+    // Eight tokens to a block of threads when sequences have as many and their scores fit beside
+    // those of another block.
+    if (p.max_q >= kTile && tile_bytes(c) <= 110 * 1024) {
+        static PerDevice attr;
+        const cudaError_t e = (cudaError_t)attr.get([] {
+            return (int)cudaFuncSetAttribute(cache_select_tile_kernel<DH, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024);
+        }, true);
+        if (e != cudaSuccess) return e;
+        launches = 1;
+        return launch_pdl(cache_select_tile_kernel<DH, M>, dim3((unsigned)((p.T + kTile - 1) / kTile * c.Hkv)), dim3(kThreads),
+                          tile_bytes(c), st, c, p);
+    }
+    // As many tokens at a time as the buffer has room for.
+    const int most = (int)std::min<size_t>(p.T, cache_score_keys(c) / (score_row(c) * c.Hkv));
+    const size_t smem = coded_bytes(c.rep, c.dh, 1);
+    cudaError_t e = cudaSuccess;
+    for (int t = 0; t < p.T && e == cudaSuccess; t += most) {
+        const long long items = (long long)std::min(most, p.T - t) * c.Hkv;
+        const int chunks = (c.max_pages + kWarps * 16 - 1) / (kWarps * 16);
+        const int split = (int)std::min<long long>(chunks, std::max<long long>(1, 12LL * c.num_sms / items));
+        e = launch_pdl(cache_score_kernel<DH, M>, dim3((unsigned)(items * split)), dim3(kThreads), smem, st, c, p, t, split);
+        if (e == cudaSuccess) e = launch_pdl(cache_choose_kernel, dim3((unsigned)items), dim3(kThreads), 0, st, c, p, t);
+        launches += 2;
+    }
+    return e;
 }
 
 template <int N>
@@ -361,8 +642,18 @@ cudaError_t launch_cache_bounds_accepted(const CacheDev& c, int n, const int* se
                    : accepted_launch<kCacheMaxSeqs>(c, n, seq, n_acc, accepted, st);
 }
 
-cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st) {
-    return c.dh == 64 ? select_launch<64>(c, p, st) : select_launch<128>(c, p, st);
+cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches) {
+    launches = 0;
+    auto heads = [&](auto dh) {
+        constexpr int DH = decltype(dh)::value;
+        switch (columns_of(c.rep)) {
+            case 1: return select_launch<DH, 1>(c, p, st, launches);
+            case 2: return select_launch<DH, 2>(c, p, st, launches);
+            case 4: return select_launch<DH, 4>(c, p, st, launches);
+            default: return select_launch<DH, 8>(c, p, st, launches);
+        }
+    };
+    return c.dh == 64 ? heads(std::integral_constant<int, 64>{}) : heads(std::integral_constant<int, 128>{});
 }
 
 }  // namespace tmoe

@@ -124,6 +124,11 @@ SELECT = {
     "heads_20": ((40, 2, 64), 32, [900], [2], 7, 1, 2),
     "heads_128": ((128, 1, 128), 16, [700], [1], 12, 1, 1),
     "chunk": ((8, 2, 128), 16, [700, 90], [40, 33], 6, 1, 1),
+    "chunk_runs": ((4, 4, 64), 16, [300, 20, 200, 150, 400], [3, 9, 1, 2, 17], 5, 1, 1),
+    "chunk_heads_2": ((4, 2, 128), 16, [300, 200, 400], [3, 8, 14], 5, 0, 1),
+    "chunk_heads_3": ((6, 2, 64), 32, [300, 200, 800], [5, 8, 11], 4, 1, 0),
+    "chunk_heads_7": ((7, 1, 128), 16, [300, 400], [5, 12], 4, 1, 1),
+    "heads_3": ((3, 1, 128), 16, [300, 400], [1, 2], 4, 1, 1),
     "many_blocks": ((4, 1, 64), 16, [20000], [1], 100, 1, 1),
     "some_without_tokens": ((4, 2, 128), 128, [1500, 900, 2000], [1, 0, 1], 3, 1, 1),
 }
@@ -158,6 +163,24 @@ def test_select_ties_and_odd_scores():
     x.copy_(torch.randn_like(x) * torch.exp2(torch.randint(-20, 20, (4, 1), device=DEV).bfloat16()))
     c.summarize(0, whole=True)
     assert torch.equal(c.select(0, x, 11).cpu(), select_ref(c, m, 0, x, [4], 11))
+
+
+@pytest.mark.parametrize("q", [2, 9])
+@pytest.mark.parametrize("n", [5, 60, 200, 390])
+def test_select_clustered_scores(q, n):
+    """Hundreds of equal blocks, scores in few tight clusters, scores of all magnitudes and both signs, all zero."""
+    c, m, x = with_bounds((2, 1, 64), 16, [400 * 16 + 3], [q], poison=False, seed=n)
+    ids, g = m.own[0][:400], torch.Generator(device=DEV).manual_seed(n)
+    one = torch.randn((1, 1, 16, 64), generator=g, device=DEV).bfloat16()
+    kinds = torch.randint(0, 4, (400,), generator=g, device=DEV)
+    for keys in (one.expand(400, 1, 16, 64), one * torch.tensor([1.0, 1.0, 1.0078125, -3.0], device=DEV)[kinds].view(-1, 1, 1, 1),
+                 one * torch.exp2(torch.randint(-60, 60, (400, 1, 1, 1), generator=g, device=DEV).float()) *
+                 torch.randint(-1, 2, (400, 1, 1, 1), generator=g, device=DEV), one * 0):
+        c.k[0, ids] = keys.bfloat16()
+        c.summarize(0, whole=True)
+        assert torch.equal(c.select(0, x, n).cpu(), select_ref(c, m, 0, x, [q], n))
+        assert torch.equal(c.select(0, x, n, first=0, last=0).cpu(), select_ref(c, m, 0, x, [q], n, 0, 0))
+    assert c.stats()["status"] == 0
 
 
 def lists_of(m, q, n, kv_heads, seed=0, fill=None):
