@@ -160,35 +160,46 @@ struct Coded {
     }
 };
 
-// A column per warp; `tokens` of the tokens exist.
+// Columns `from`, `from` + step and so on by this warp; `tokens` of the tokens exist.
 template <int DH>
 __device__ __forceinline__ void code_queries(const CacheDev& c, const SelectParams& p, const Coded<DH>& out, int columns, int h,
-                                             int first_token, int tokens) {
-    constexpr int K = DH / 64;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = columns_of(c.rep);
-    for (int u = warp; u < columns; u += kWarps) {
-        const int k = u / per, r = min(u - k * per, c.rep - 1);
-        const bool real = k < tokens;
-        const __nv_bfloat16* q = p.q + (size_t)(first_token + (real ? k : 0)) * p.ld_q + (size_t)(h * c.rep + r) * DH + lane * 2 * K;
-        uint32_t w[K], amax = 0;
+                                             int first_token, int tokens, int from, int step) {
+    constexpr int K = DH / 64, SIDE = 4;              // (columns whose loads are in flight together)
+    const int lane = threadIdx.x & 31, per = columns_of(c.rep);
+    for (int u0 = from; u0 < columns; u0 += SIDE * step) {
+        uint32_t w[SIDE][K];
+        bool real[SIDE];
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            w[j] = reinterpret_cast<const uint32_t*>(q)[j];
-            const uint32_t a = w[j] & 0x7fff7fffu;
-            amax = max(amax, max(a << 16, a & 0xffff0000u));
-        }
-        amax = __reduce_max_sync(0xffffffffu, amax);
-        const bool finite = real && amax < 0x7f800000u;
-        const int e = unit_exponent(__uint_as_float(amax));
-        const float inv = finite ? two_to(-e) : 0.f;
-        uint16_t* neg = reinterpret_cast<uint16_t*>(out.code + (size_t)u * 2 * DH) + lane * K;
+        for (int i = 0; i < SIDE; ++i) {
+            const int u = min(u0 + i * step, columns - 1), k = u / per, r = min(u - k * per, c.rep - 1);
+            real[i] = k < tokens;
+            const __nv_bfloat16* q = p.q + (size_t)(first_token + (real[i] ? k : 0)) * p.ld_q + (size_t)(h * c.rep + r) * DH + lane * 2 * K;
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const int a = finite ? __float2int_rn(bf16_lo(w[j]) * inv) : 0, b = finite ? __float2int_rn(bf16_hi(w[j]) * inv) : 0;
-            neg[j] = (uint16_t)((min(a, 0) & 0xff) | (min(b, 0) & 0xff) << 8);
-            neg[DH / 2 + j] = (uint16_t)(max(a, 0) | max(b, 0) << 8);
+            for (int j = 0; j < K; ++j) w[i][j] = reinterpret_cast<const uint32_t*>(q)[j];
         }
-        if (lane == 0) out.unit[u] = finite ? two_to(e) : 0.f;
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i) {
+            const int u = u0 + i * step;
+            if (u >= columns) break;
+            uint32_t amax = 0;
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const uint32_t a = w[i][j] & 0x7fff7fffu;
+                amax = max(amax, max(a << 16, a & 0xffff0000u));
+            }
+            amax = __reduce_max_sync(0xffffffffu, amax);
+            const bool finite = real[i] && amax < 0x7f800000u;
+            const int e = unit_exponent(__uint_as_float(amax));
+            const float inv = finite ? two_to(-e) : 0.f;
+            uint16_t* neg = reinterpret_cast<uint16_t*>(out.code + (size_t)u * 2 * DH) + lane * K;
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const int a = finite ? __float2int_rn(bf16_lo(w[i][j]) * inv) : 0, b = finite ? __float2int_rn(bf16_hi(w[i][j]) * inv) : 0;
+                neg[j] = (uint16_t)((min(a, 0) & 0xff) | (min(b, 0) & 0xff) << 8);
+                neg[DH / 2 + j] = (uint16_t)(max(a, 0) | max(b, 0) << 8);
+            }
+            if (lane == 0) out.unit[u] = finite ? two_to(e) : 0.f;
+        }
     }
 }
 
@@ -477,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 3) cache_select_tile_kernel(const __
     pdl_wait();
     pdl_trigger();
     if (!c.plan->ok) return;
-    code_queries<DH>(c, p, q, columns, h, first_token, tokens);
+    code_queries<DH>(c, p, q, columns, h, first_token, tokens, warp, kWarps);
     __syncthreads();
     // Runs of tokens of one sequence (one run for most blocks of threads).
     for (int a = 0; a < tokens;) {
@@ -509,79 +520,137 @@ __global__ void __launch_bounds__(kThreads, 3) cache_select_tile_kernel(const __
     }
 }
 
-// Single tokens: the scores, by as many blocks of threads per token and key/value head as fill the
-// GPU, to a buffer; then a block of threads per token and head chooses.
+// Single tokens: the scores, to a buffer; then a block of threads per token and key/value head chooses.
+// All sixteens of blocks of all tokens and heads lie on a line, token by token, and every warp takes
+// the same number of them in a row: a warp meets few tokens, whose queries it codes for
+// itself, and long sequences cost no one more than short ones.  (A block of threads for each
+// token and head, or several for long ones: 48 contexts of 4000 to 40000 took 26 us.)
 //
 // Bound: HBM, 2 D + 4 bytes per block of keys and head.
+constexpr int kSlice = 1024;                          // tokens at a time
+__host__ __device__ inline int score_warps(const CacheDev& c) {
+    const int fit = (int)(80 * 1024 / coded_bytes(c.rep, c.dh, 1));
+    return fit < kWarps ? fit : kWarps;
+}
+
 template <int DH, int M>
-__global__ void __launch_bounds__(kThreads) cache_score_kernel(const __grid_constant__ CacheDev c,
-                                                               const __grid_constant__ SelectParams p, int first_token, int split) {
+__global__ void __launch_bounds__(kThreads, 3) cache_score_kernel(const __grid_constant__ CacheDev c,
+                                                               const __grid_constant__ SelectParams p, int first_token, int tokens) {
     extern __shared__ __align__(16) uint32_t smem[];
-    const int item = blockIdx.x / split, chunk = blockIdx.x - item * split;
-    const int k = item / c.Hkv, h = item - k * c.Hkv, columns = coded_columns(c.rep, 1);
-    const Coded<DH> q(smem, columns);
+    __shared__ int s_pre[kSlice + 1];                 // sixteens of one head before each token
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int columns = columns_of(c.rep);
+    const Coded<DH> q(reinterpret_cast<uint8_t*>(smem) + warp * coded_bytes(c.rep, DH, 1), coded_columns(c.rep, 1));
     pdl_wait();
     pdl_trigger();
     const int ok = c.plan->ok;
-    const CacheToken tok = c.tokens[first_token + k];
-    const int F = tok.base >> c.page_shift, warp = threadIdx.x >> 5;
-    if (!ok || F <= p.n || chunk * kWarps * 16 >= F) return;
-    code_queries<DH>(c, p, q, columns, h, first_token + k, 1);
+    for (int t = threadIdx.x; t < tokens; t += blockDim.x) {
+        const int F = c.tokens[first_token + t].base >> c.page_shift;
+        s_pre[t] = F > p.n ? (F + 15) >> 4 : 0;
+    }
+    if (!ok) return;
     __syncthreads();
-    uint32_t* out = c.scores + (size_t)item * score_row(c);
-    score_blocks<DH, M, M < 8>(c, p.layer, q, h, tok.seq, F, 0, 1, chunk * kWarps + warp, split * kWarps,
-                               [&](int, int b, uint32_t key) { out[b] = key; });
+    if (warp == 0) {
+        int sum = 0;
+        for (int t0 = 0; t0 < tokens; t0 += 32) {
+            const int t = t0 + lane, mine = t < tokens ? s_pre[t] : 0;
+            int x = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
+            }
+            if (t < tokens) s_pre[t] = sum + x - mine;
+            sum += __shfl_sync(0xffffffffu, x, 31);
+        }
+        if (lane == 0) s_pre[tokens] = sum;
+    }
+    __syncthreads();
+    const long long all = (long long)s_pre[tokens] * c.Hkv, n_warps = (long long)gridDim.x * warps;
+    const long long w = (long long)blockIdx.x * warps + warp;
+    long long u = all * w / n_warps;
+    const long long u1 = all * (w + 1) / n_warps;
+    while (u < u1) {
+        // The last token whose sixteens begin at or before u (tokens without any share their begin with the next).
+        const int at = (int)(u / c.Hkv);
+        int lo = 0, hi = tokens;
+        while (hi - lo > 1) {
+            const int m = (lo + hi) >> 1;
+            if (s_pre[m] <= at) lo = m;
+            else hi = m;
+        }
+        const int turns = s_pre[lo + 1] - s_pre[lo], in = (int)(u - (long long)s_pre[lo] * c.Hkv);
+        const int h = in / turns, from = in - h * turns, to = (int)min((long long)turns, from + (u1 - u));
+        const CacheToken tok = c.tokens[first_token + lo];
+        code_queries<DH>(c, p, q, columns, h, first_token + lo, 1, 0, 1);
+        __syncwarp();
+        uint32_t* out = c.scores + (size_t)(lo * c.Hkv + h) * score_row(c);
+        score_blocks<DH, M, M < 8>(c, p.layer, q, h, tok.seq, min(tok.base >> c.page_shift, to * 16), 0, 1, from, 1,
+                                   [&](int, int b, uint32_t key) { out[b] = key; });
+        __syncwarp();
+        u += to - from;
+    }
 }
 
 __global__ void __launch_bounds__(kThreads) cache_choose_kernel(const __grid_constant__ CacheDev c,
                                                                 const __grid_constant__ SelectParams p, int first_token) {
     constexpr int kHeld = 8;                          // keys of a thread that stay in registers
     __shared__ Choice choice;
-    __shared__ int s_taken[kWarps];
+    __shared__ int s_taken[kHeld][kWarps];
     const int item = blockIdx.x, k = item / c.Hkv, h = item - k * c.Hkv, n = p.n;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     pdl_trigger();
-    if (!c.plan->ok) return;
-    const int F = c.tokens[first_token + k].base >> c.page_shift;
+    const int ok = c.plan->ok, F = c.tokens[first_token + k].base >> c.page_shift;
+    if (!ok) return;
     int* out = p.blocks + ((size_t)(first_token + k) * c.Hkv + h) * n;
-    list_ends(out, n, F, p.first, p.last, threadIdx.x, kThreads);
     const int lo = p.first, hi = F - p.last, want = n - p.first - p.last;
-    if (F <= n || want == 0) return;
     const uint32_t* keys = c.scores + (size_t)item * score_row(c);
-    auto sync = [] { __syncthreads(); };
-    Cut cut;
-    if (hi - lo <= kHeld * kThreads) {
-        uint32_t held[kHeld];
+    // Turn j of the threads holds the columns lo + j kThreads ..: the first kHeld turns in registers.
+    uint32_t held[kHeld];
+    if (F > n) {
 #pragma unroll
         for (int j = 0; j < kHeld; ++j) {
             const int i = lo + j * kThreads + threadIdx.x;
             held[j] = i < hi ? __ldcg(keys + i) : 0u;
         }
-        auto key = [&](int i) {
-            uint32_t v = held[0];
-#pragma unroll
-            for (int j = 1; j < kHeld; ++j) v = i - lo >= j * kThreads ? held[j] : v;
-            return v;
-        };
-        cut = cut_of<kWarps>(key, lo, hi, want, threadIdx.x, choice, sync);
-    } else {
-        cut = cut_of<kWarps>([&](int i) { return __ldcg(keys + i); }, lo, hi, want, threadIdx.x, choice, sync);
     }
-    // A warp takes a range of columns: how many, then which.
-    const int per = (hi - lo + kThreads - 1) / kThreads * 32, i0 = lo + warp * per, i1 = min(hi, i0 + per);
-    int taken = 0;
-    for (int i = i0 + lane; i - lane < i1; i += 32)
-        taken += __popc(__ballot_sync(0xffffffffu, i < i1 && cut.takes(__ldcg(keys + i), i)));
-    if (lane == 0) s_taken[warp] = taken;
-    __syncthreads();
+    list_ends(out, n, F, p.first, p.last, threadIdx.x, kThreads);
+    if (F <= n || want == 0) return;
+    auto sync = [] { __syncthreads(); };
+    const bool few = hi - lo <= kHeld * kThreads;
+    auto key = [&](int i) {
+        uint32_t v = held[0];
+#pragma unroll
+        for (int j = 1; j < kHeld; ++j) v = i - lo >= j * kThreads ? held[j] : v;
+        return v;
+    };
+    const Cut cut = few ? cut_of<kWarps>(key, lo, hi, want, threadIdx.x, choice, sync)
+                        : cut_of<kWarps>([&](int i) { return __ldcg(keys + i); }, lo, hi, want, threadIdx.x, choice, sync);
+    const uint32_t below = (1u << lane) - 1u;
     int at = p.first;
-    for (int w = 0; w < warp; ++w) at += s_taken[w];
-    for (int i = i0 + lane; i - lane < i1; i += 32) {
-        const bool take = i < i1 && cut.takes(__ldcg(keys + i), i);
-        const uint32_t m = __ballot_sync(0xffffffffu, take);
-        if (take) out[at + __popc(m & ((1u << lane) - 1u))] = i;
-        at += __popc(m);
+    for (int j0 = 0; lo + j0 * kThreads < hi; j0 += kHeld) {
+        uint32_t takes[kHeld];
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const int i = lo + (j0 + j) * kThreads + threadIdx.x;
+            const uint32_t v = j0 == 0 ? held[j] : i < hi ? __ldcg(keys + i) : 0u;
+            takes[j] = __ballot_sync(0xffffffffu, i < hi && cut.takes(v, i));
+            if (lane == 0) s_taken[j][warp] = __popc(takes[j]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            int mine = at;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const int v = s_taken[j][w];
+                mine += w < warp ? v : 0;
+                at += v;
+            }
+            if (takes[j] >> lane & 1u) out[mine + __popc(takes[j] & below)] = lo + (j0 + j) * kThreads + threadIdx.x;
+        }
+        __syncthreads();
     }
 }
 
@@ -600,15 +669,20 @@ cudaError_t select_launch(const CacheDev& c, const SelectParams& p, cudaStream_t
                           tile_bytes(c), st, c, p);
     }
     // As many tokens at a time as the buffer has room for.
-    const int most = (int)std::min<size_t>(p.T, cache_score_keys(c) / (score_row(c) * c.Hkv));
-    const size_t smem = coded_bytes(c.rep, c.dh, 1);
-    cudaError_t e = cudaSuccess;
+    const int most = (int)std::min<size_t>(std::min(p.T, kSlice), cache_score_keys(c) / (score_row(c) * c.Hkv));
+    const int warps = score_warps(c);
+    const size_t smem = coded_bytes(c.rep, c.dh, 1) * warps;
+    static PerDevice attr;
+    cudaError_t e = (cudaError_t)attr.get([] {
+        return (int)cudaFuncSetAttribute(cache_score_kernel<DH, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
+    }, true);
     for (int t = 0; t < p.T && e == cudaSuccess; t += most) {
-        const long long items = (long long)std::min(most, p.T - t) * c.Hkv;
-        const int chunks = (c.max_pages + kWarps * 16 - 1) / (kWarps * 16);
-        const int split = (int)std::min<long long>(chunks, std::max<long long>(1, 12LL * c.num_sms / items));
-        e = launch_pdl(cache_score_kernel<DH, M>, dim3((unsigned)(items * split)), dim3(kThreads), smem, st, c, p, t, split);
-        if (e == cudaSuccess) e = launch_pdl(cache_choose_kernel, dim3((unsigned)items), dim3(kThreads), 0, st, c, p, t);
+        const int tokens = std::min(most, p.T - t);
+        // As many warps as are resident, with a sixteen of blocks each at least.
+        const long long turns = (long long)tokens * c.Hkv * ((c.max_pages + 15) / 16);
+        const unsigned blocks = (unsigned)std::min<long long>(3LL * c.num_sms, (turns + warps - 1) / warps);
+        e = launch_pdl(cache_score_kernel<DH, M>, dim3(blocks), dim3(warps * 32), smem, st, c, p, t, tokens);
+        if (e == cudaSuccess) e = launch_pdl(cache_choose_kernel, dim3((unsigned)(tokens * c.Hkv)), dim3(kThreads), 0, st, c, p, t);
         launches += 2;
     }
     return e;
