@@ -283,11 +283,26 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
     const int max_rows = c->max_q > d.tile_tokens ? 2 * kCacheTile : c->max_q * d.rep;
     p.join_here = !d.shared && max_rows <= kJoinHereRows;
     p.T = c->T;
+    p.single = d.shared && c->own_splits > 0;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_attend");
-    return c->launched(launch_cache_attend(d.shared ? c->share : d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows,
-                                           enter(c, stream)),
-                       p.join_here ? 1 : 2, "cache_attend");
+    cudaStream_t st = enter(c, stream);
+    cudaError_t e = launch_cache_attend(d.shared ? c->share : d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows, st);
+    if (e == cudaSuccess && p.single) {
+        BlocksParams b = {};
+        b.q = static_cast<const __nv_bfloat16*>(a->q);
+        b.out = p.out;
+        b.tree = p.tree;
+        b.ld_q = a->ld_q;
+        b.ld_out = p.ld_out;
+        b.T = p.T;
+        b.row_tiles = 1;
+        b.splits = c->own_splits;
+        b.scale_log2 = p.scale_log2;
+        const bool large = d.page > 64;
+        e = c->own(c->share, large ? c->tm_k64[layer] : c->tm_k[layer], large ? c->tm_v64[layer] : c->tm_v[layer], b, st);
+    }
+    return c->launched(e, p.join_here ? 1 : 2, "cache_attend");
 }
 
 extern "C" trimmoe_status trimmoe_cache_fork(trimmoe_cache_handle c, int n, const int32_t* src, const int32_t* dst,

@@ -64,6 +64,7 @@ struct CachePlan {
     int copies;                        // pages to copy (shared last pages)
     int ok;                            // 0: the step was refused
     int drawn, done;                   // items drawn beyond the first round, CTAs that have finished
+    int own_apart;                     // with groups of sequences: sequences' own tiles are not on the line
 };
 
 __host__ __device__ inline int cache_two_tiles(int ntok, int tile_tokens) { return ntok > tile_tokens ? 1 : 0; }
@@ -75,11 +76,11 @@ __host__ __device__ inline int cache_group_tiles(int q_len, int kv_len, int firs
     return (keys + kCacheTile - 1) / kCacheTile;
 }
 
-// Key tiles of an item of this cost (two: it has two query tiles), and how many of
-// them the first x of its cost cover.
-__host__ __device__ inline int cache_item_tiles(int cost, int two) { return (cost >> two) - 1; }
-__host__ __device__ inline int cache_tiles_before(long long x, int cost, int two) {
-    const long long n = cache_item_tiles(cost, two), t = x <= 0 ? 0 : (x + two) >> two;
+// Key tiles of an item of this cost (two: it has two query tiles; over: what is added
+// for its beginning and end, in tiles), and how many of them the first x of its cost cover.
+__host__ __device__ inline int cache_item_tiles(int cost, int two, int over = 1) { return (cost >> two) - over; }
+__host__ __device__ inline int cache_tiles_before(long long x, int cost, int two, int over = 1) {
+    const long long n = cache_item_tiles(cost, two, over), t = x <= 0 ? 0 : (x + two) >> two;
     return (int)(x >= cost || t > n ? n : t);
 }
 
@@ -92,6 +93,10 @@ __host__ __device__ inline int cache_part_rows(int ntok, int tile_tokens, int re
 // The part of the group's item of key/value head `head` that CTA `cta` computes begins at row
 // g.part_row + (head + cta) * cache_part_rows(g): along the line of items head and CTA both
 // grow, so their sum names the pieces.
+
+// With groups of sequences an item's beginning and end count as this many tiles.  (Each costs some
+// 3 us, a tile 0.8; sequences' own items are short.)
+constexpr int kShareOver = 4;
 
 // The CTA whose share of a line of cost W holds x: shares are [W b / n, W (b + 1) / n).
 __host__ __device__ inline int cache_cta_of(long long x, long long W, int n) {
@@ -161,6 +166,7 @@ struct AttendParams {
     int join_here;                     // the attention kernel joins cut items itself
     float scale_log2;
     int T;
+    int single;                        // with groups of sequences: each has one new token at most
 };
 
 // attend_blocks: q and out as for attend.
@@ -171,6 +177,7 @@ struct BlocksParams {
     const uint64_t* tree;
     int ld_q, ld_out, T, n;
     int row_tiles;                     // of 16 query heads of a key/value head
+    int splits;                        // CTAs of an item
     float scale_log2;
 };
 
@@ -215,16 +222,64 @@ cudaError_t launch_cache_bounds_accepted(const CacheDev& c, int n, const int* se
 cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches);
 cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                 const BlocksParams& p, cudaStream_t st);
-// The list of items of a step whose listed sequences form n groups.
-cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, cudaStream_t st);
+// A step of single tokens with groups of sequences, behind the attention kernel: sequences' own
+// tiles, unless these were on its line, and the sum with the parts.
+cudaError_t launch_cache_own(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
+                             cudaStream_t st);
+// CTAs of one of `items` items with about as many stages of 64 positions.
+int cache_blocks_splits(const CacheDev& c, long long items, int stages);
+// The list of items of a step whose listed sequences form n groups.  splits: of launch_cache_own, 0 when
+// the step is not one of single tokens.
+cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st);
 cudaError_t launch_cache_attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                 const CUtensorMap& tm_v, const AttendParams& p, int max_rows, cudaStream_t st);
 
 // Device helpers of the attention kernels.
+
+// The parts of a group's item of head `head` that hold token t: rows row + i * step, i < count, of query head 0.
+struct PartList {
+    long long row;
+    int step, count;
+    __device__ bool warps() const { return step >= 32; }
+    // First value of four columns of a row, and how far the next four are.
+    template <int DH>
+    __device__ const float* at(const float* part_o, long long r) const {
+        return part_o + (warps() ? (r & ~31LL) * DH + (r & 31) * 4 : r * DH);
+    }
+    __device__ int next4() const { return warps() ? 128 : 4; }
+};
+__device__ __forceinline__ PartList part_list(const CacheDev& c, const CachePlan& pl, int group, int head, int t) {
+    if (group < 0) return PartList{0, 1, 0};
+    const CacheGroup g = c.groups[group];
+    const int two = cache_two_tiles(g.ntok, c.tile_tokens), tiles = cache_item_tiles(g.cost, two, kShareOver);
+    const long long start = g.pre * c.Hkv + (long long)head * g.cost;
+    const int first = cache_cta_of(start, pl.total, pl.n_ctas);
+    const int last = cache_cta_of(start + ((long long)(tiles - 1) << two), pl.total, pl.n_ctas);
+    PartList l;
+    l.step = cache_part_rows(g.ntok, c.tile_tokens, c.rep);
+    l.count = last - first + 1;
+    const int in = t - g.row;
+    l.row = g.part_row + (long long)(head + first) * l.step +
+            (in >= c.tile_tokens ? 128 + (in - c.tile_tokens) * c.rep : in * c.rep);
+    return l;
+}
+
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+// One more source of a row: its maximum and sum (x), added to top and l; fa and fb are the
+// factors of what was summed before and of the source.  False: nothing was summed in it.
+__device__ __forceinline__ bool join_source(float2 x, bool there, float& top, float& l, float& fa, float& fb) {
+    there = there && x.x != -INFINITY;
+    const float m = there ? fmaxf(top, x.x) : top, ref = m == -INFINITY ? 0.f : m;
+    fa = ex2(top - ref);
+    fb = ex2(x.x - ref);
+    top = m;
+    l = there ? l * fa + x.y * fb : l;
+    return there;
 }
 
 // Bounded wait by all lanes of a warp.  A probe sleeps until the phase ends or up to

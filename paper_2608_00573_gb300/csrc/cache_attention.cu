@@ -249,18 +249,6 @@ __device__ __forceinline__ size_t part_at(size_t buf, int row, int col) {
     return (buf * 256 + (row & ~31)) * DH + (size_t)(col >> 2) * 128 + (row & 31) * 4 + (col & 3);
 }
 
-// One more source of a row: its maximum and sum (x), added to top and l; fa and fb are the
-// factors of what was summed before and of the source.  False: nothing was summed in it.
-__device__ __forceinline__ bool join_source(float2 x, bool there, float& top, float& l, float& fa, float& fb) {
-    there = there && x.x != -INFINITY;
-    const float m = there ? fmaxf(top, x.x) : top, ref = m == -INFINITY ? 0.f : m;
-    fa = ex2(top - ref);
-    fb = ex2(x.x - ref);
-    top = m;
-    l = there ? l * fa + x.y * fb : l;
-    return there;
-}
-
 // Joins row r of a cut item of one query tile from the parts of CTAs first .. last, in the
 // order of the keys; a lane takes D / 32 columns, eight sources are read at a time.  CTA
 // `first` wrote its part into its second buffer, the others into their first; each has two
@@ -500,8 +488,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     sg.part = -1;
                 } else {
                     const long long x1 = min((long long)g.cost, within + (x_end - x));
-                    sg.t0 = cache_tiles_before(within, g.cost, two_tiles);
-                    sg.t1 = cache_tiles_before(x1, g.cost, two_tiles);
+                    constexpr int over = SHARED ? kShareOver : 1;
+                    sg.t0 = cache_tiles_before(within, g.cost, two_tiles, over);
+                    sg.t1 = cache_tiles_before(x1, g.cost, two_tiles, over);
                     const bool all = sg.t0 == 0 && sg.t1 == cache_item_tiles(g.cost, two_tiles);
                     sg.part = SHARED ? 0 : all ? -1 : 2 * b + (sg.t0 == 0);
                     if (SHARED) {
@@ -1135,66 +1124,57 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
         join_rows<DH, DH / 32>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
 }
 
-// Adds the parts of a step with groups of sequences.  A warp takes a token and four query heads of
-// a key/value head, a lane a head and every eighth four columns; up to four parts are
-// read at a time, the common item's first, in the order of the keys.  Bound: L2.
+// Adds the parts of a step with groups of sequences.  A warp takes a token, four query heads of a
+// key/value head and 64 columns, a lane a head and eight of them; eight parts are read at a
+// time, the common item's first, in the order of the keys.  Bound: L2.
 template <int DH>
 __global__ void __launch_bounds__(256) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
                                                                 const __grid_constant__ AttendParams p) {
-    constexpr int V = DH / 32, B = 4;
+    constexpr int B = 8;
     pdl_wait();
     pdl_trigger();
     const CachePlan pl = *c.plan;
-    if (!pl.ok) return;
     const int quads = (c.rep + 3) / 4, lane = threadIdx.x & 31;
-    const long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), u = w / (DH / 64);
     if (u >= (long long)p.T * c.Hkv * quads) return;
     const int quad = (int)(u % quads), head = (int)(u / quads % c.Hkv), t = (int)(u / quads / c.Hkv);
-    const int h = min(quad * 4 + (lane >> 3), c.rep - 1), c4 = lane & 7;
+    const int h = min(quad * 4 + (lane >> 3), c.rep - 1), col = (int)(w % (DH / 64)) * 64 + (lane & 7) * 4;
     const int2 of = c.items_of[t];
-    float top = -INFINITY, l = 0.f, acc[V][4];
+    if (!pl.ok) return;
+    const PartList l0 = part_list(c, pl, of.y, head, t), l1 = part_list(c, pl, of.x, head, t);
+    const int n = l0.count + l1.count;
+    float top = -INFINITY, l = 0.f, acc[2][4] = {};
+    for (int b0 = 0; b0 < n; b0 += B) {
+        float2 ml[B];
+        float4 o[B][2];
 #pragma unroll
-    for (int v = 0; v < V; ++v) acc[v][0] = acc[v][1] = acc[v][2] = acc[v][3] = 0.f;
-    for (int k = 0; k < 2; ++k) {
-        const int e = k ? of.x : of.y;
-        if (e < 0) continue;
-        const CacheGroup g = c.groups[e];
-        const int two = cache_two_tiles(g.ntok, c.tile_tokens), tiles = cache_item_tiles(g.cost, two);
-        const long long start = g.pre * c.Hkv + (long long)head * g.cost;
-        const int first = cache_cta_of(start, pl.total, pl.n_ctas);
-        const int last = cache_cta_of(start + ((long long)(tiles - 1) << two), pl.total, pl.n_ctas);
-        const int R = cache_part_rows(g.ntok, c.tile_tokens, c.rep), in = t - g.row;
-        const int r = (in >= c.tile_tokens ? 128 + (in - c.tile_tokens) * c.rep : in * c.rep) + h;
-        for (int b0 = first; b0 <= last; b0 += B) {
-            float2 ml[B];
-            float4 o[B][V];
+        for (int i = 0; i < B; ++i) {
+            const int k = min(b0 + i, n - 1);
+            const bool own = k >= l0.count;
+            const long long row = (own ? l1.row + (long long)(k - l0.count) * l1.step : l0.row + (long long)k * l0.step) + h;
+            const bool warps = own ? l1.warps() : l0.warps();
+            const float* src = c.part_o + (warps ? (row & ~31LL) * DH + (row & 31) * 4 + col * 32 : row * DH + col);
+            ml[i] = __ldcg(c.part_ml + row);
+            o[i][0] = __ldcg(reinterpret_cast<const float4*>(src));
+            o[i][1] = __ldcg(reinterpret_cast<const float4*>(src + (warps ? 1024 : 32)));
+        }
 #pragma unroll
-            for (int i = 0; i < B; ++i) {
-                const size_t row = (size_t)(g.part_row + (head + min(b0 + i, last)) * R + r);
-                ml[i] = __ldcg(c.part_ml + row);
-                const float* src = c.part_o + (R >= 32 ? (row & ~(size_t)31) * DH + (row & 31) * 4 : row * DH);
+        for (int i = 0; i < B; ++i) {
+            float fa, fb;
+            const bool there = join_source(ml[i], b0 + i < n, top, l, fa, fb);
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    o[i][v] = __ldcg(reinterpret_cast<const float4*>(src + (v * 8 + c4) * (R >= 32 ? 128 : 4)));
-            }
+            for (int v = 0; v < 2; ++v) {
+                const float x[4] = {o[i][v].x, o[i][v].y, o[i][v].z, o[i][v].w};
 #pragma unroll
-            for (int i = 0; i < B; ++i) {
-                float fa, fb;
-                const bool there = join_source(ml[i], b0 + i <= last, top, l, fa, fb);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float x[4] = {o[i][v].x, o[i][v].y, o[i][v].z, o[i][v].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[v][j] = there ? acc[v][j] * fa + x[j] * fb : acc[v][j];
-                }
+                for (int j = 0; j < 4; ++j) acc[v][j] = there ? acc[v][j] * fa + x[j] * fb : acc[v][j];
             }
         }
     }
     if (quad * 4 + (lane >> 3) >= c.rep) return;
     const float il = l == 0.f ? 0.f : 1.f / l;
-    __nv_bfloat16* out = p.out + (size_t)t * p.ld_out + (size_t)(head * c.rep + h) * DH + c4 * 4;
+    __nv_bfloat16* out = p.out + (size_t)t * p.ld_out + (size_t)(head * c.rep + h) * DH + col;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < 2; ++v)
         *reinterpret_cast<uint2*>(out + v * 32) = make_uint2(pack_bf16x2(acc[v][0] * il, acc[v][1] * il),
                                                              pack_bf16x2(acc[v][2] * il, acc[v][3] * il));
 }
@@ -1222,7 +1202,8 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
                    c, p);
     if (e != cudaSuccess || p.join_here) return e;
     if (SHARED) {
-        const long long units = (long long)p.T * c.Hkv * ((c.rep + 3) / 4);
+        if (p.single) return e;                        // (launch_cache_own joins)
+        const long long units = (long long)p.T * c.Hkv * ((c.rep + 3) / 4) * (DH / 64);
         return launch_pdl(cache_join_shared_kernel<DH>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, c, p);
     }
     return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);

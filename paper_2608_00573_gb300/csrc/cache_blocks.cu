@@ -55,7 +55,11 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         c->share = d;
     }
     c->share.shared = 1;
-    const trimmoe_status s = c->launched(launch_cache_share(c->share, n, counts, c->n, c->T, st), 2, "cache_share");
+    // Single tokens: up to 16 query heads of a key/value head are a tile of the kernel that reads
+    // sequences' own pages.
+    c->own = launch_cache_own;
+    c->own_splits = c->max_q == 1 && c->d.rep <= 16 ? cache_blocks_splits(c->d, (long long)c->T * c->d.Hkv, 1 << 20) : 0;
+    const trimmoe_status s = c->launched(launch_cache_share(c->share, n, counts, c->n, c->T, c->own_splits, st), 2, "cache_share");
     // (Without its list a step cannot be attended.)
     if (s != TRIMMOE_OK) c->T = -1;
     else c->d.shared = 1;
@@ -159,6 +163,7 @@ extern "C" trimmoe_status trimmoe_cache_attend_blocks(trimmoe_cache_handle c, in
     p.T = c->T;
     p.n = a->n;
     p.row_tiles = (d.rep + 15) / 16;
+    p.splits = cache_blocks_splits(d, (long long)c->T * d.Hkv * p.row_tiles, std::max(1, (int)std::min(1LL << 20, (long long)a->n * d.page / 64)));
     if ((long long)c->T * d.Hkv * p.row_tiles > (1LL << 26)) return c->fail(TRIMMOE_ERR_UNSUPPORTED, what, "more than 2^26 items");
     p.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)d.dh)) * 1.4426950408889634f;
     const bool large = d.page > 64;

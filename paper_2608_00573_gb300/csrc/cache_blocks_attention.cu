@@ -49,6 +49,7 @@ struct __align__(8) Bars {
     int first[8][4];           // of the stage's pages: first position, kHidden or kWhole
     float2 ml[kReaders][16];   // the warps' maxima and sums
     float2 mine[16];           // the CTA's
+    PartList parts[2];         // OWN: the common item's parts, the sequence's own ones
     int abort_flag, never;
 };
 
@@ -61,10 +62,14 @@ struct Item {
     int stages;
 };
 
-template <int DH>
+// OWN: no lists; the token's sequence from its group's common tiles on, and then the common tiles'
+// parts, which the attention kernel before this one has written.  Nothing but these is
+// read behind that kernel's end: whatever comes before it has ended when it lets this one start.
+template <int DH, bool OWN>
 __global__ void __launch_bounds__(kThreads)
 cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                    const __grid_constant__ CacheDev c, const __grid_constant__ BlocksParams p, int splits) {
+                    const __grid_constant__ CacheDev c, const __grid_constant__ BlocksParams p) {
+    const int splits = p.splits;
     using S = Stage<DH>;
     constexpr int ST = S::COUNT;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -83,9 +88,12 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         prefetch_tmap(&tm_v);
     }
     __syncthreads();
-    pdl_wait();
-    pdl_trigger();
-    if (!c.plan->ok) return;                           // (all CTAs)
+    if (!OWN) {
+        pdl_wait();
+        pdl_trigger();
+    }
+    const CachePlan pl = *c.plan;
+    if (!pl.ok) return;                                // (all CTAs)
     if (sb & 1023u) {                                  // swizzled tiles start at multiples of 1024
         if (threadIdx.x == 0) atomicCAS(c.err, 0, ERR_TIMEOUT_CACHE_ATTN);
         return;
@@ -107,13 +115,21 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         it.kv_len = s.kv_len;
         it.base = s.base;
         it.pos = s.pos;
-        it.first_own = it.base >> c.page_shift;
-        it.listed = min(p.n, it.first_own);
+        int2 items = make_int2(-1, -1);
+        if (OWN) {
+            items = c.items_of[it.t];
+            it.first_own = items.y < 0 ? 0 : c.groups[items.y].kv_len >> c.page_shift;
+            it.listed = 0;
+            if (threadIdx.x < 2) bars->parts[threadIdx.x] = part_list(c, pl, threadIdx.x ? items.x : items.y, it.head, it.t);
+        } else {
+            it.first_own = it.base >> c.page_shift;
+            it.listed = min(p.n, it.first_own);
+        }
         const int last = p.tree ? it.kv_len - 1 : it.pos;
         it.subs = c.page > kStageKeys ? c.page / kStageKeys : 1;
         const int boxes = (it.listed + (last >> c.page_shift) - it.first_own + 1) * it.subs;
         const int per_stage = max(1, kStageKeys >> c.page_shift);
-        it.stages = (boxes + per_stage - 1) / per_stage;
+        it.stages = OWN && !pl.own_apart ? 0 : (boxes + per_stage - 1) / per_stage;
     }
     const int per_stage = max(1, kStageKeys >> c.page_shift), box_rows = kStageKeys / per_stage;
     const int g0 = (int)((long long)it.stages * rank / splits), g1 = (int)((long long)it.stages * (rank + 1) / splits);
@@ -328,6 +344,44 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     __syncthreads();
     auto rescale = [](float part, float top) { return part == -INFINITY ? 0.f : ex2(part - top); };   // (no key seen: no part)
     __nv_bfloat16* out = p.out + (size_t)it.t * p.ld_out + (size_t)(it.head * c.rep + it.row0) * DH;
+    if (OWN) {
+        pdl_wait();
+        pdl_trigger();
+    }
+    // Two columns of a row: the other parts first, in the order of the keys, then what is here; its output.
+    auto put_out = [&](int r, int col, float top, float sum, float a, float b) {
+        if (OWN) {
+            float t0 = -INFINITY, s0 = 0.f, a0 = 0.f, b0 = 0.f, fa, fb;
+            const int n0 = bars->parts[0].count, n = n0 + bars->parts[1].count;
+            constexpr int SIDE = 8;
+            for (int k0 = 0; k0 < n; k0 += SIDE) {
+                float2 ml[SIDE], v[SIDE];
+#pragma unroll
+                for (int i = 0; i < SIDE; ++i) {
+                    const int k = min(k0 + i, n - 1);
+                    const PartList& l = bars->parts[k >= n0];
+                    const long long row = l.row + (long long)(k >= n0 ? k - n0 : k) * l.step + r;
+                    ml[i] = __ldcg(c.part_ml + row);
+                    v[i] = __ldcg(reinterpret_cast<const float2*>(l.at<DH>(c.part_o, row) + (col >> 2) * l.next4() + (col & 3)));
+                }
+#pragma unroll
+                for (int i = 0; i < SIDE; ++i)
+                    if (join_source(ml[i], k0 + i < n, t0, s0, fa, fb)) {
+                        a0 = a0 * fa + v[i].x * fb;
+                        b0 = b0 * fa + v[i].y * fb;
+                    }
+            }
+            if (join_source(make_float2(top, sum), true, t0, s0, fa, fb)) {
+                a0 = a0 * fa + a * fb;
+                b0 = b0 * fa + b * fb;
+            }
+            sum = s0;
+            a = a0;
+            b = b0;
+        }
+        const float il = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<uint32_t*>(out + (size_t)r * DH + col) = pack_bf16x2(a * il, b * il);
+    };
     for (int x = threadIdx.x; x < it.rows * (DH / 2); x += kThreads) {
         const int r = x / (DH / 2), col = x % (DH / 2) * 2;
         float top = -INFINITY, sum = 0.f, a = 0.f, b = 0.f;
@@ -342,8 +396,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             b = ml.x == -INFINITY ? b : fmaf(v.y, f, b);
         }
         if (splits == 1) {
-            const float il = sum == 0.f ? 0.f : 1.f / sum;
-            *reinterpret_cast<uint32_t*>(out + (size_t)r * DH + col) = pack_bf16x2(a * il, b * il);
+            put_out(r, col, top, sum, a, b);
         } else {
             *reinterpret_cast<float2*>(own + r * DH + col) = make_float2(a, b);
             if (col == 0) bars->mine[r] = make_float2(top, sum);
@@ -368,13 +421,12 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             a = ml.x == -INFINITY ? a : fmaf(v.x, f, a);
             b = ml.x == -INFINITY ? b : fmaf(v.y, f, b);
         }
-        const float il = sum == 0.f ? 0.f : 1.f / sum;
-        *reinterpret_cast<uint32_t*>(out + (size_t)r * DH + col) = pack_bf16x2(a * il, b * il);
+        put_out(r, col, top, sum, a, b);
     }
     cluster_sync();                                    // nobody ends while others read its sums
 }
 
-template <int DH>
+template <int DH, bool OWN>
 cudaError_t blocks_launch(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                           cudaStream_t st) {
     constexpr size_t smem = Stage<DH>::COUNT * Stage<DH>::BYTES + sizeof(Bars);
@@ -382,16 +434,11 @@ cudaError_t blocks_launch(const CacheDev& c, const CUtensorMap& tm_k, const CUte
     static_assert(Stage<DH>::COUNT <= 8, "barriers");
     static PerDevice attr;
     cudaError_t e = (cudaError_t)attr.get([] {
-        return (int)cudaFuncSetAttribute(cache_blocks_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        return (int)cudaFuncSetAttribute(cache_blocks_kernel<DH, OWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     }, true);
     if (e != cudaSuccess) return e;
-    // As many CTAs to an item as fill the GPU, with a stage each at least.
-    const long long items = (long long)p.T * c.Hkv * p.row_tiles;
-    const int stages = std::max(1, p.n * c.page / kStageKeys);
-    int splits = 1;
-    while (splits < 8 && items * splits * 2 <= 2LL * c.num_sms && splits * 2 <= stages + 1) splits *= 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(items * splits));
+    cfg.gridDim = dim3((unsigned)((long long)p.T * c.Hkv * p.row_tiles * p.splits));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -399,18 +446,30 @@ cudaError_t blocks_launch(const CacheDev& c, const CUtensorMap& tm_k, const CUte
     a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     a[0].val.programmaticStreamSerializationAllowed = 1;
     a[1].id = cudaLaunchAttributeClusterDimension;
-    a[1].val.clusterDim.x = (unsigned)splits;
+    a[1].val.clusterDim.x = (unsigned)p.splits;
     a[1].val.clusterDim.y = a[1].val.clusterDim.z = 1;
     cfg.attrs = a;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, cache_blocks_kernel<DH>, tm_k, tm_v, c, p, splits);
+    return cudaLaunchKernelEx(&cfg, cache_blocks_kernel<DH, OWN>, tm_k, tm_v, c, p);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                                 cudaStream_t st) {
-    return c.dh == 64 ? blocks_launch<64>(c, tm_k, tm_v, p, st) : blocks_launch<128>(c, tm_k, tm_v, p, st);
+    return c.dh == 64 ? blocks_launch<64, false>(c, tm_k, tm_v, p, st) : blocks_launch<128, false>(c, tm_k, tm_v, p, st);
+}
+
+cudaError_t launch_cache_own(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
+                             cudaStream_t st) {
+    return c.dh == 64 ? blocks_launch<64, true>(c, tm_k, tm_v, p, st) : blocks_launch<128, true>(c, tm_k, tm_v, p, st);
+}
+
+// As many CTAs to an item as fill the GPU twice, with a stage each at least.
+int cache_blocks_splits(const CacheDev& c, long long items, int stages) {
+    int splits = 1;
+    while (splits < 8 && items * splits * 2 <= 2LL * c.num_sms && splits * 2 <= stages + 1) splits *= 2;
+    return splits;
 }
 
 }  // namespace tmoe

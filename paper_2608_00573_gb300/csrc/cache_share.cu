@@ -19,6 +19,7 @@ namespace {
 constexpr int kCommonThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kMinTiles = 2;           // as for other steps (cache_pages.cu)
+constexpr long long kShareBytes = 40LL << 20;   // common pages are read for each sequence when that costs less
 
 // A block takes one group: the front pages that its sequences share, and how many whole key
 // tiles these fill.
@@ -118,7 +119,9 @@ __device__ V block_sum(V v, V* ws, V& total) {
 // item's row of heads at a time.
 template <int N>
 __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_constant__ CacheDev c,
-                                                                   const __grid_constant__ CacheList<N> l, int n_seqs, int T) {
+                                                                   const __grid_constant__ CacheList<N> l, int n_seqs, int T,
+                                                                   int splits) {
+    __shared__ int s_max;
     __shared__ int s_common[kCacheMaxSeqs], s_begin[kCacheMaxSeqs + 1], s_own[kCacheMaxSeqs + 1];   // first items of groups, sequences
     __shared__ int s_of[kCacheMaxSeqs];                // a sequence's group
     __shared__ int s_wi[33];
@@ -128,17 +131,42 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     pdl_trigger();
     if (!c.plan->ok) return;
     int tiles = 0, count = 0;
+    if (i == 0) s_max = 0;
     if (i < n) {
         tiles = c.common[i];
-        const CacheSeq a = c.seqs[l.a[i]], z = c.seqs[l.a[i] + l.b[i] - 1];
-        if (tiles) count = (z.q_off + z.q_len - a.q_off + 2 * TT - 1) / (2 * TT);
         for (int k = l.a[i]; k < l.a[i] + l.b[i]; ++k) s_of[k] = i;
     }
+    int tok = 0;                                       // the group's tokens
+    if (i < n) {
+        const CacheSeq a = c.seqs[l.a[i]], z = c.seqs[l.a[i] + l.b[i] - 1];
+        tok = z.q_off + z.q_len - a.q_off;
+    }
+    bool apart = splits > 0;
+    if (apart) {
+        // Single tokens: what sharing saves is read from L2 otherwise, at twice HBM's rate and
+        // more, and the second kernel alone has less to wait for.
+        long long saved;
+        block_sum((long long)tiles * max(0, tok - 1), s_wl, saved);
+        if (saved * kCacheTile * c.Hkv * c.dh * 4 < kShareBytes) tiles = 0;
+    }
+    if (i < n) s_common[i] = tiles;
+    __syncthreads();
+    CacheSeq mine = {};
+    if (i < n_seqs) mine = c.seqs[i];
+    if (apart) {
+        // The second kernel's CTAs take whole sequences, cut in `splits`: unless a few are far longer
+        // than the others.
+        const int stages = i < n_seqs && mine.q_len ? (mine.kv_len - s_common[s_of[i]] * kCacheTile + 63) / 64 : 0;
+        if (stages) atomicMax(&s_max, stages);
+        long long sum;
+        block_sum((long long)stages, s_wl, sum);
+        apart = (long long)s_max / splits <= sum * c.Hkv / c.num_sms + 16;
+    }
+    if (tiles) count = (tok + 2 * TT - 1) / (2 * TT);
     int n_common, n_own;
     const int at = block_sum(count, s_wi, n_common);
-    const int own = block_sum(i < n_seqs ? (c.seqs[i].q_len + 2 * TT - 1) / (2 * TT) : 0, s_wi, n_own);
+    const int own = block_sum(apart ? 0 : (mine.q_len + 2 * TT - 1) / (2 * TT), s_wi, n_own);
     if (i < n) {
-        s_common[i] = tiles;
         s_begin[i] = at;
     }
     if (i < n_seqs) s_own[i] = n_common + own;
@@ -176,7 +204,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
             g.ntok = min(2 * TT, all - tok);
             g.t0 = 0;
             g.common = 1;
-            g.cost = (s_common[k] + 1) << cache_two_tiles(g.ntok, TT);
+            g.cost = (s_common[k] + kShareOver) << cache_two_tiles(g.ntok, TT);
         } else if (e < items) {
             const int k = find(s_own, n_seqs, e);
             const CacheSeq s = c.seqs[k];
@@ -188,7 +216,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
             g.row = s.q_off + tok;
             g.ntok = min(2 * TT, s.q_len - tok);
             g.t0 = s_common[s_of[k]];
-            g.cost = (cache_group_tiles(s.q_len, s.kv_len, g.first, g.ntok) - g.t0 + 1) << cache_two_tiles(g.ntok, TT);
+            g.cost = (cache_group_tiles(s.q_len, s.kv_len, g.first, g.ntok) - g.t0 + kShareOver) << cache_two_tiles(g.ntok, TT);
         }
         long long sum;
         g.pre = W + block_sum((long long)g.cost, s_wl, sum);
@@ -221,10 +249,11 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         c.plan->total = W;
         c.plan->n_groups = items;
         c.plan->n_ctas = n_ctas;
+        c.plan->own_apart = apart;
     }
     for (int t = i; t < T; t += kPlanThreads) {
         const int k = c.owner[t], g = s_of[k], from = c.seqs[l.a[g]].q_off;
-        c.items_of[t] = make_int2(s_own[k] + (t - c.seqs[k].q_off) / (2 * TT),
+        c.items_of[t] = make_int2(apart ? -1 : s_own[k] + (t - c.seqs[k].q_off) / (2 * TT),
                                   s_common[g] ? s_begin[g] + (t - from) / (2 * TT) : -1);
     }
     __syncthreads();
@@ -250,7 +279,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
 }
 
 template <int N>
-cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs, int T, cudaStream_t st) {
+cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st) {
     CacheList<N> l;
     l.n = n;
     int at = 0;
@@ -261,13 +290,14 @@ cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs
     }
     const cudaError_t e = launch_pdl(cache_common_kernel<N>, dim3((unsigned)n), dim3(kCommonThreads), 0, st, c, l);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_share_kernel<N>, dim3(1), dim3(kPlanThreads), 0, st, c, l, n_seqs, T);
+    return launch_pdl(cache_share_kernel<N>, dim3(1), dim3(kPlanThreads), 0, st, c, l, n_seqs, T, splits);
 }
 
 }  // namespace
 
-cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, cudaStream_t st) {
-    return n <= 64 ? share_launch<64>(c, n, counts, n_seqs, T, st) : share_launch<kCacheMaxSeqs>(c, n, counts, n_seqs, T, st);
+cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st) {
+    return n <= 64 ? share_launch<64>(c, n, counts, n_seqs, T, splits, st)
+                   : share_launch<kCacheMaxSeqs>(c, n, counts, n_seqs, T, splits, st);
 }
 
 }  // namespace tmoe
