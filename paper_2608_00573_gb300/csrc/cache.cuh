@@ -76,11 +76,11 @@ __host__ __device__ inline int cache_group_tiles(int q_len, int kv_len, int firs
     return (keys + kCacheTile - 1) / kCacheTile;
 }
 
-// Key tiles of an item of this cost (two: it has two query tiles; over: what is added
-// for its beginning and end, in tiles), and how many of them the first x of its cost cover.
-__host__ __device__ inline int cache_item_tiles(int cost, int two, int over = 1) { return (cost >> two) - over; }
-__host__ __device__ inline int cache_tiles_before(long long x, int cost, int two, int over = 1) {
-    const long long n = cache_item_tiles(cost, two, over), t = x <= 0 ? 0 : (x + two) >> two;
+// Key tiles of an item of this cost (two: it has two query tiles), and how many of
+// them the first x of its cost cover.
+__host__ __device__ inline int cache_item_tiles(int cost, int two) { return (cost >> two) - 1; }
+__host__ __device__ inline int cache_tiles_before(long long x, int cost, int two) {
+    const long long n = cache_item_tiles(cost, two), t = x <= 0 ? 0 : (x + two) >> two;
     return (int)(x >= cost || t > n ? n : t);
 }
 
@@ -94,9 +94,17 @@ __host__ __device__ inline int cache_part_rows(int ntok, int tile_tokens, int re
 // g.part_row + (head + cta) * cache_part_rows(g): along the line of items head and CTA both
 // grow, so their sum names the pieces.
 
-// With groups of sequences an item's beginning and end count as this many tiles.  (Each costs some
-// 3 us, a tile 0.8; sequences' own items are short.)
-constexpr int kShareOver = 4;
+// With groups of sequences: cost of a key tile (both query tiles', when an item has two) and of an
+// item's beginning and end, in about 0.47 us (measured: 0.92, 1.43 and 3.2 us; sequences' own items are
+// short, so this matters more than in other steps).
+__host__ __device__ inline int share_tile(int two) { return 2 + two; }
+constexpr int kShareEnds = 7;
+__host__ __device__ inline int share_tiles(int cost, int two) { return (cost - kShareEnds) / share_tile(two); }
+// Key tiles that the first x of an item's cost cover.
+__host__ __device__ inline int share_tiles_before(long long x, int cost, int two) {
+    const long long n = share_tiles(cost, two), t = x <= 0 ? 0 : (x + share_tile(two) - 1) / share_tile(two);
+    return (int)(t > n ? n : t);
+}
 
 // The CTA whose share of a line of cost W holds x: shares are [W b / n, W (b + 1) / n).
 __host__ __device__ inline int cache_cta_of(long long x, long long W, int n) {
@@ -136,6 +144,7 @@ struct CacheDev {
     int shared;
     int2* items_of;                    // [T] groups that hold a token: its own keys' and its common ones' (-1: none)
     int* common;                       // [max_seqs] key tiles that a group of sequences has in common
+    int2* cut;                         // [groups][Hkv] first CTA that holds tiles of an item, how many do
     int* err;
     int* refused;                      // behind err: the last step was refused and stats has not reset that yet
 };
@@ -197,7 +206,8 @@ inline size_t cache_score_keys(const CacheDev& c) {
 // Steps with groups of sequences: rows (tokens times query heads) at most, and what that allows.
 constexpr int kShareRows = 65536;
 inline long long cache_share_groups(const CacheDev& c) {
-    return 2 * ((long long)kShareRows / c.Hq / (2 * c.tile_tokens) + c.max_seqs + 1);
+    const long long T = kShareRows / c.Hq;
+    return 2 * std::min(T, T / (2 * c.tile_tokens) + c.max_seqs + 1);
 }
 // Every token has its own and at most one common part, a part's rows are at most twice its
 // tokens' (whole warps, tiles that rep does not divide), a cut adds one part of 256 rows, and
@@ -241,25 +251,16 @@ struct PartList {
     long long row;
     int step, count;
     __device__ bool warps() const { return step >= 32; }
-    // First value of four columns of a row, and how far the next four are.
-    template <int DH>
-    __device__ const float* at(const float* part_o, long long r) const {
-        return part_o + (warps() ? (r & ~31LL) * DH + (r & 31) * 4 : r * DH);
-    }
-    __device__ int next4() const { return warps() ? 128 : 4; }
 };
-__device__ __forceinline__ PartList part_list(const CacheDev& c, const CachePlan& pl, int group, int head, int t) {
+__device__ __forceinline__ PartList part_list(const CacheDev& c, int group, int head, int t) {
     if (group < 0) return PartList{0, 1, 0};
+    const int2 cut = c.cut[(size_t)group * c.Hkv + head];
     const CacheGroup g = c.groups[group];
-    const int two = cache_two_tiles(g.ntok, c.tile_tokens), tiles = cache_item_tiles(g.cost, two, kShareOver);
-    const long long start = g.pre * c.Hkv + (long long)head * g.cost;
-    const int first = cache_cta_of(start, pl.total, pl.n_ctas);
-    const int last = cache_cta_of(start + ((long long)(tiles - 1) << two), pl.total, pl.n_ctas);
     PartList l;
     l.step = cache_part_rows(g.ntok, c.tile_tokens, c.rep);
-    l.count = last - first + 1;
+    l.count = cut.y;
     const int in = t - g.row;
-    l.row = g.part_row + (long long)(head + first) * l.step +
+    l.row = g.part_row + (long long)(head + cut.x) * l.step +
             (in >= c.tile_tokens ? 128 + (in - c.tile_tokens) * c.rep : in * c.rep);
     return l;
 }
@@ -280,6 +281,41 @@ __device__ __forceinline__ bool join_source(float2 x, bool there, float& top, fl
     top = m;
     l = there ? l * fa + x.y * fb : l;
     return there;
+}
+
+// Adds a source's four columns of a row.  (Without a branch: loads would be moved behind it, one by one.)
+__device__ __forceinline__ void add_source(float2 ml, float4 x, bool there, float& top, float& l, float (&a)[4]) {
+    float fa, fb;
+    there = join_source(ml, there, top, l, fa, fb);
+    a[0] = there ? a[0] * fa + x.x * fb : a[0];
+    a[1] = there ? a[1] * fa + x.y * fb : a[1];
+    a[2] = there ? a[2] * fa + x.z * fb : a[2];
+    a[3] = there ? a[3] * fa + x.w * fb : a[3];
+}
+// Adds four columns of query head `row` from two lists of parts, the first one's first; twelve reads are in
+// flight.
+template <int DH>
+__device__ __forceinline__ void add_parts(const CacheDev& c, const PartList (&parts)[2], int row, int col, float& top, float& l,
+                                          float (&a)[4]) {
+    constexpr int B = 12;
+    const PartList p0 = parts[0], p1 = parts[1];
+    const int n = p0.count + p1.count;
+    for (int k0 = 0; k0 < n; k0 += B) {
+        float2 ml[B];
+        float4 x[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int k = min(k0 + i, n - 1);
+            const bool second = k >= p0.count;
+            const long long at = (second ? p1.row + (long long)(k - p0.count) * p1.step : p0.row + (long long)k * p0.step) + row;
+            const bool warps = second ? p1.warps() : p0.warps();
+            const float* src = c.part_o + (warps ? (at & ~31LL) * DH + (at & 31) * 4 + col * 32 : at * DH + col);
+            ml[i] = __ldcg(c.part_ml + at);
+            x[i] = __ldcg(reinterpret_cast<const float4*>(src));
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i) add_source(ml[i], x[i], k0 + i < n, top, l, a);
+    }
 }
 
 // Bounded wait by all lanes of a warp.  A probe sleeps until the phase ends or up to

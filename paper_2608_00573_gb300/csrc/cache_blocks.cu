@@ -29,7 +29,7 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         cudaError_t e = cudaSuccess;
         size_t had = c->allocs.size();
         try {
-            c->allocs.reserve(had + 5);
+            c->allocs.reserve(had + 6);
         } catch (const std::bad_alloc&) {
             return c->fail(TRIMMOE_ERR_OOM, "cache_share", "host allocation failed");
         }
@@ -44,6 +44,7 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         alloc(d.groups, (size_t)cache_share_groups(d));
         alloc(d.items_of, (size_t)kShareRows);
         alloc(d.common, (size_t)d.max_seqs);
+        alloc(d.cut, (size_t)cache_share_groups(d) * d.Hkv);
         alloc(d.part_ml, rows);
         alloc(d.part_o, rows * d.dh);
         if (e != cudaSuccess) {

@@ -1,5 +1,6 @@
 // Attention of each new token over pages that it is told to read (a list per key/value
-// head) and over the positions from its step's first page on.
+// head) and over the positions from its step's first page on; and, for single tokens of
+// sequences with a common prompt (cache_share.cu), over each sequence's own pages.
 //
 // An item is a token, a key/value head and up to 16 of the query heads that share it.
 // No two items have a list in common, so that a tile of the tensor cores has the item's 1
@@ -9,15 +10,19 @@
 // TMEM would hold the same rows.
 //
 // A stage is 64 listed positions: pages, or halves of pages of 128, as boxes of the cache's
-// tensor maps, with their values.  One warp finds the pages and starts the copies; four
-// warps take 16 positions of every stage each, with sums of their own:
+// tensor maps, with their values.  One warp draws items, finds their pages and keeps the
+// copies going, into the next item while this one is computed.  Four warps take 16 positions of every
+// stage each, with sums of their own:
 //
 //   S = Q K^T (16 x 16);  m' = max(m, max s);  p = 2^(scale' s - m');  l += sum p;  O = O 2^(m - m') + P V
 //
 // (m moves only when a score is more than 2^8 above it; P is rounded to bf16, the
 // type of the product's operand, l sums p before that rounding; the first key's p is 1.)
-// An item's stages are cut among the CTAs of a cluster, whose sums meet in distributed
-// shared memory: first the four warps', then the CTAs', always in the same order.
+// At an item's end the warps' sums are added in shared memory.  (With columns instead of
+// positions shared out for P V, and maxima and P handed on at every stage, no sums would have to be
+// added, but two barriers a stage cost more: 800 tokens' chunks 593 us against 446.)  When there are
+// few items, an item's stages are cut among the CTAs of a cluster, whose sums meet in
+// distributed shared memory.  Sums are always added in the same order.
 //
 // Masked positions (of the last pages: later tokens, other branches of a tree, places
 // that no position uses yet) never reach a result: scores are replaced and value
@@ -35,6 +40,15 @@ constexpr int kThreads = (kReaders + 1) * 32;
 constexpr int kStageKeys = 64;
 constexpr int kHidden = -1, kWhole = -2;               // what a stage's pages are, else their first position
 
+// What the loading warp says of an item.
+struct Item {
+    int valid;
+    int t, head, row0, rows;   // token, key/value head, query heads of it
+    int base, kv_len, pos;
+    int g0, g1;                // stages
+    PartList parts[2];         // OWN: the common item's parts, the sequence's own ones
+};
+
 template <int DH>
 struct Stage {
     static constexpr int KB = DH / 64;
@@ -44,23 +58,36 @@ struct Stage {
     static constexpr int COUNT = 96 * 1024 / BYTES;    // two CTAs to an SM
 };
 
-struct __align__(8) Bars {
-    uint64_t full[8], empty[8];
+template <int DH>
+struct __align__(128) Shared {
+    uint8_t stage[Stage<DH>::COUNT][Stage<DH>::BYTES]; // (first: swizzled tiles start at multiples of 1024)
+    __nv_bfloat16 q[16][DH];   // the item's queries
+    float2 swap[2][DH / 8][32];   // sums of eight rows that one warp gives another, as the lanes hold them
+    float2 ml[kReaders][16];   // the warps' maxima and sums of p
+    float2 mine[16];           // the CTA's (clusters)
+    uint64_t full[8], empty[8], q_full, q_empty;
     int first[8][4];           // of the stage's pages: first position, kHidden or kWhole
-    float2 ml[kReaders][16];   // the warps' maxima and sums
-    float2 mine[16];           // the CTA's
-    PartList parts[2];         // OWN: the common item's parts, the sequence's own ones
+    Item item;
+    PartList parts[2];         // OWN: the item's, for its end
     int abort_flag, never;
 };
 
-// What an item's item is about.
-struct Item {
-    int t, head, row0, rows;   // token, key/value head, query heads of it
-    int seq, base, kv_len, pos;
-    int listed, first_own;     // entries of the list that count, first page of the step's own
-    int subs;                  // boxes of a page's rows (pages of 128: two)
-    int stages;
-};
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// Barriers of the four multiplying warps.
+__device__ __forceinline__ void readers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool readers_any(bool x) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r)
+                 : "r"((uint32_t)x)
+                 : "memory");
+    return r != 0;
+}
 
 // OWN: no lists; the token's sequence from its group's common tiles on, and then the common tiles'
 // parts, which the attention kernel before this one has written.  Nothing but these is
@@ -69,20 +96,21 @@ template <int DH, bool OWN>
 __global__ void __launch_bounds__(kThreads)
 cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                     const __grid_constant__ CacheDev c, const __grid_constant__ BlocksParams p) {
-    const int splits = p.splits;
     using S = Stage<DH>;
     constexpr int ST = S::COUNT;
     extern __shared__ __align__(1024) uint8_t smem[];
+    Shared<DH>& sh = *reinterpret_cast<Shared<DH>*>(smem);
     const uint32_t sb = smem_u32(smem);
-    Bars* bars = reinterpret_cast<Bars*>(smem + ST * S::BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % splits, index = blockIdx.x / splits;
+    const int splits = p.splits, rank = blockIdx.x % splits;
     if (threadIdx.x == 0) {
         for (int s = 0; s < ST; ++s) {
-            mbar_init(smem_u32(&bars->full[s]), 1);
-            mbar_init(smem_u32(&bars->empty[s]), kReaders);
+            mbar_init(smem_u32(&sh.full[s]), 1);
+            mbar_init(smem_u32(&sh.empty[s]), kReaders);
         }
-        bars->abort_flag = bars->never = 0;
+        mbar_init(smem_u32(&sh.q_full), 1);
+        mbar_init(smem_u32(&sh.q_empty), kReaders);
+        sh.abort_flag = sh.never = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_k);
         prefetch_tmap(&tm_v);
@@ -94,334 +122,373 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     }
     const CachePlan pl = *c.plan;
     if (!pl.ok) return;                                // (all CTAs)
-    if (sb & 1023u) {                                  // swizzled tiles start at multiples of 1024
+    if (sb & 1023u) {
         if (threadIdx.x == 0) atomicCAS(c.err, 0, ERR_TIMEOUT_CACHE_ATTN);
         return;
     }
-    const uint32_t abort_at = smem_u32(&bars->abort_flag);
+    const uint32_t abort_at = smem_u32(&sh.abort_flag);
     auto wait = [&](uint64_t* b, uint32_t parity) {
         return __any_sync(0xffffffffu, wait_probes(smem_u32(b), parity & 1u, abort_at, c.err)) != 0;
     };
-
-    Item it;
-    {
-        const int per = c.Hkv * p.row_tiles;
-        it.t = index / per;
-        it.head = index % per / p.row_tiles;
-        it.row0 = index % p.row_tiles * 16;
-        it.rows = min(16, c.rep - it.row0);
-        const CacheToken s = c.tokens[it.t];
-        it.seq = s.seq;
-        it.kv_len = s.kv_len;
-        it.base = s.base;
-        it.pos = s.pos;
-        int2 items = make_int2(-1, -1);
-        if (OWN) {
-            items = c.items_of[it.t];
-            it.first_own = items.y < 0 ? 0 : c.groups[items.y].kv_len >> c.page_shift;
-            it.listed = 0;
-            if (threadIdx.x < 2) bars->parts[threadIdx.x] = part_list(c, pl, threadIdx.x ? items.x : items.y, it.head, it.t);
-        } else {
-            it.first_own = it.base >> c.page_shift;
-            it.listed = min(p.n, it.first_own);
-        }
-        const int last = p.tree ? it.kv_len - 1 : it.pos;
-        it.subs = c.page > kStageKeys ? c.page / kStageKeys : 1;
-        const int boxes = (it.listed + (last >> c.page_shift) - it.first_own + 1) * it.subs;
-        const int per_stage = max(1, kStageKeys >> c.page_shift);
-        it.stages = OWN && !pl.own_apart ? 0 : (boxes + per_stage - 1) / per_stage;
-    }
+    const int page_boxes = c.page > kStageKeys ? c.page / kStageKeys : 1;     // boxes of a page's rows (pages of 128: two)
     const int per_stage = max(1, kStageKeys >> c.page_shift), box_rows = kStageKeys / per_stage;
-    const int g0 = (int)((long long)it.stages * rank / splits), g1 = (int)((long long)it.stages * (rank + 1) / splits);
-
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};   // rows lane / 4 and lane / 4 + 8
-    float o[DH / 8][4];
-#pragma unroll
-    for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    const int items = p.T * c.Hkv * p.row_tiles;
 
     if (warp == kReaders) {
-        // ------------------------------------------------------------------ loads
-        // Lane i looks up box i of 32, the next 32 while these are copied.
-        const int* list = p.blocks + ((size_t)it.t * c.Hkv + it.head) * p.n;
-        const int* row = c.table + (size_t)it.seq * c.max_pages;
-        const int boxes_end = g1 * per_stage;
-        struct Box {
-            int id, first;                             // page, first position (kWhole, kHidden)
-        };
-        auto look_up = [&](int b) {
-            Box x{0, kHidden};
-            const int j = b / it.subs, sub = b - j * it.subs;
-            if (b >= boxes_end) return x;
-            int col;
-            bool fits = true;
-            if (j < it.listed) {
-                col = list[j];
-                if (col == -1) {
-                    fits = false;
-                } else {
-                    const int before = j ? list[j - 1] : -1;
-                    fits = col >= 0 && col < it.first_own && (j == 0 || (before >= 0 && col > before));
-                    if (!fits) atomicCAS(c.err, 0, ERR_CACHE_BLOCKS);
-                }
-            } else {
-                col = it.first_own + j - it.listed;
-                if (col >= c.max_pages || (col << c.page_shift) >= it.kv_len) fits = false;
-            }
-            if (!fits) return x;
-            x.id = row[col];
-            if (x.id < 0 || x.id >= c.n_pages) {
-                atomicCAS(c.err, 0, ERR_CACHE_STATE);
-                return x;
-            }
-            x.first = j < it.listed ? kWhole : (col << c.page_shift) + sub * box_rows;
-            return x;
-        };
-        int b0 = g0 * per_stage;
-        Box now = look_up(b0 + lane), next = look_up(b0 + 32 + lane);
+        // ------------------------------------------------------------ items and loads
+        uint32_t issued = 0, n_items = 0;
         bool ok = true;
-        uint32_t issued = 0;
-        for (int g = g0; ok && g < g1; ++g) {
-            const int at = g * per_stage - b0;         // (per_stage divides 32)
-            const int s = (int)(issued % ST);
-            if (issued >= (uint32_t)ST) ok = !wait(&bars->empty[s], issued / ST - 1);
+        int index = blockIdx.x / splits;
+        while (ok && index < items) {
+            // The next item (single CTAs; clusters have one each).
+            int drawn = items;
+            if (splits == 1 && lane == 0) drawn = (int)gridDim.x + atomicAdd(&c.plan->drawn, 1);
+            Item it;
+            it.valid = 1;
+            const int per = c.Hkv * p.row_tiles;
+            it.t = index / per;
+            it.head = index % per / p.row_tiles;
+            it.row0 = index % p.row_tiles * 16;
+            it.rows = min(16, c.rep - it.row0);
+            const CacheToken tok = c.tokens[it.t];
+            it.base = tok.base;
+            it.kv_len = tok.kv_len;
+            it.pos = tok.pos;
+            int listed = 0, first_own = 0;             // entries of the list that count, first page of the step's own
+            if (OWN) {
+                const int2 of = c.items_of[it.t];
+                first_own = of.y < 0 ? 0 : c.groups[of.y].kv_len >> c.page_shift;
+                it.parts[0] = part_list(c, of.y, it.head, it.t);
+                it.parts[1] = part_list(c, of.x, it.head, it.t);
+            } else {
+                first_own = it.base >> c.page_shift;
+                listed = min(p.n, first_own);
+            }
+            const int last = p.tree ? it.kv_len - 1 : it.pos;
+            const int boxes = (listed + (last >> c.page_shift) - first_own + 1) * page_boxes;
+            const int stages = OWN && !pl.own_apart ? 0 : (boxes + per_stage - 1) / per_stage;
+            it.g0 = (int)((long long)stages * rank / splits);
+            it.g1 = (int)((long long)stages * (rank + 1) / splits);
+            // Lane i looks up box i of 32, the next 32 while these are copied.
+            const int* list = p.blocks + ((size_t)it.t * c.Hkv + it.head) * p.n;
+            const int* row = c.table + (size_t)tok.seq * c.max_pages;
+            const int boxes_end = it.g1 * per_stage;
+            struct Box {
+                int id, first;                         // page, first position (kWhole, kHidden)
+            };
+            auto look_up = [&](int b) {
+                Box x{0, kHidden};
+                const int j = b / page_boxes, sub = b - j * page_boxes;
+                if (b >= boxes_end) return x;
+                int col;
+                bool fits = true;
+                if (j < listed) {
+                    col = list[j];
+                    if (col == -1) {
+                        fits = false;
+                    } else {
+                        const int before = j ? list[j - 1] : -1;
+                        fits = col >= 0 && col < first_own && (j == 0 || (before >= 0 && col > before));
+                        if (!fits) atomicCAS(c.err, 0, ERR_CACHE_BLOCKS);
+                    }
+                } else {
+                    col = first_own + j - listed;
+                    if (col >= c.max_pages || (col << c.page_shift) >= it.kv_len) fits = false;
+                }
+                if (!fits) return x;
+                x.id = row[col];
+                if (x.id < 0 || x.id >= c.n_pages) {
+                    atomicCAS(c.err, 0, ERR_CACHE_STATE);
+                    return x;
+                }
+                x.first = j < listed ? kWhole : (col << c.page_shift) + sub * box_rows;
+                return x;
+            };
+            int b0 = it.g0 * per_stage;
+            Box now = look_up(b0 + lane), next = look_up(b0 + 32 + lane);
+            // The readers have taken what was said of the item before, and its queries.
+            if (n_items) ok = !wait(&sh.q_empty, n_items - 1);
             if (!ok) break;
-            const int i = lane / (2 * S::KB), kb = lane % S::KB, is_v = lane / S::KB & 1;
-            const int id = __shfl_sync(0xffffffffu, now.id, (at + i) & 31), first = __shfl_sync(0xffffffffu, now.first, (at + i) & 31);
-            const bool mine = i < per_stage, there = mine && first != kHidden;
-            const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, there));
-            if (mine && kb == 0 && !is_v) bars->first[s][i] = first;
-            __syncwarp();
-            const uint32_t fb = smem_u32(&bars->full[s]);
-            if (lane == 0) mbar_arrive_expect_tx(fb, boxes * box_rows * 128);
-            __syncwarp();
-            if (there) {
-                const int sub = (g * per_stage + i) % it.subs;
-                tma_load_2d(sb + s * S::BYTES + is_v * S::TILE + kb * S::SLAB + i * box_rows * 128, is_v ? &tm_v : &tm_k, kb * 64,
-                            (int)((((size_t)id * c.Hkv + it.head) << c.page_shift) + sub * box_rows), fb);
+            if (lane == 0) {
+                sh.item = it;
+                const uint32_t bytes = (uint32_t)it.rows * DH * 2;
+                mbar_arrive_expect_tx(smem_u32(&sh.q_full), bytes);
+                bulk_load(smem_u32(sh.q), p.q + (size_t)it.t * p.ld_q + (size_t)(it.head * c.rep + it.row0) * DH, bytes, smem_u32(&sh.q_full));
             }
             __syncwarp();
-            ++issued;
-            if (at + per_stage == 32) {
-                b0 += 32;
-                now = next;
-                next = look_up(b0 + 32 + lane);
+            ++n_items;
+            for (int g = it.g0; g < it.g1; ++g) {
+                const int at = g * per_stage - b0;     // (per_stage divides 32)
+                const int s = (int)(issued % ST);
+                if (issued >= (uint32_t)ST) ok = !wait(&sh.empty[s], issued / ST - 1);
+                if (!ok) break;
+                const int i = lane / (2 * S::KB), kb = lane % S::KB, is_v = lane / S::KB & 1;
+                const int id = __shfl_sync(0xffffffffu, now.id, (at + i) & 31), first = __shfl_sync(0xffffffffu, now.first, (at + i) & 31);
+                const bool mine = i < per_stage, there = mine && first != kHidden;
+                const uint32_t n = __popc(__ballot_sync(0xffffffffu, there));
+                if (mine && kb == 0 && !is_v) sh.first[s][i] = first;
+                __syncwarp();
+                const uint32_t fb = smem_u32(&sh.full[s]);
+                if (lane == 0) mbar_arrive_expect_tx(fb, n * box_rows * 128);
+                __syncwarp();
+                if (there) {
+                    const int sub = (g * per_stage + i) % page_boxes;
+                    tma_load_2d(sb + s * S::BYTES + is_v * S::TILE + kb * S::SLAB + i * box_rows * 128, is_v ? &tm_v : &tm_k, kb * 64,
+                                (int)((((size_t)id * c.Hkv + it.head) << c.page_shift) + sub * box_rows), fb);
+                }
+                __syncwarp();
+                ++issued;
+                if (at + per_stage == 32) {
+                    b0 += 32;
+                    now = next;
+                    next = look_up(b0 + 32 + lane);
+                }
             }
+            index = __shfl_sync(0xffffffffu, drawn, 0);
+        }
+        // The last CTA to finish drawing leaves the counter at zero for the next call.
+        if (splits == 1 && lane == 0) {
+            __threadfence();
+            if (atomicAdd(&c.plan->done, 1) == (int)gridDim.x - 1) {
+                c.plan->drawn = 0;
+                c.plan->done = 0;
+            }
+        }
+        if (ok && n_items) ok = !wait(&sh.q_empty, n_items - 1);
+        if (ok && lane == 0) {
+            sh.item.valid = 0;
+            mbar_arrive(smem_u32(&sh.q_full));
         }
         // The copies have landed before the CTA ends, also one that gave up.
-        const uint32_t never = smem_u32(&bars->never), tail = min(issued, (uint32_t)ST);
-        for (uint32_t k = issued - tail; k < issued; ++k) wait_probes(smem_u32(&bars->full[k % ST]), (k / ST) & 1, never, c.err);
+        const uint32_t never = smem_u32(&sh.never), tail = min(issued, (uint32_t)ST);
+        for (uint32_t k = issued - tail; k < issued; ++k) wait_probes(smem_u32(&sh.full[k % ST]), (k / ST) & 1, never, c.err);
+        if (n_items && !ok) wait_probes(smem_u32(&sh.q_full), (n_items - 1) & 1, never, c.err);
+        __syncwarp();
     } else {
-        // --------------------------------------------------------------- products
+        // ------------------------------------------------------------------ products
         const int r = lane >> 2, q2 = (lane & 3) * 2;
-        uint32_t qa[DH / 16][4];
-        {
-            const __nv_bfloat16* q = p.q + (size_t)it.t * p.ld_q + (size_t)(it.head * c.rep + it.row0) * DH + q2;
-            auto word = [&](int row, int col) {
-                return row < it.rows ? __ldg(reinterpret_cast<const uint32_t*>(q + (size_t)row * DH + col)) : 0u;
-            };
-#pragma unroll
-            for (int k = 0; k < DH / 16; ++k) {
-                qa[k][0] = word(r, k * 16);
-                qa[k][1] = word(r + 8, k * 16);
-                qa[k][2] = word(r, k * 16 + 8);
-                qa[k][3] = word(r + 8, k * 16 + 8);
-            }
-        }
-        const uint64_t tree = p.tree ? __ldg(p.tree + it.t) : 0;
-        const bool two = it.rows > 8;                  // the tile's lower half has rows
         const int k16 = warp * 16, box = k16 / box_rows;
         // ldmatrix rows: keys of K by halves of 8 columns, keys of V by halves of 8 keys.
         const int krow = k16 + (lane >> 4) * 8 + (lane & 7), kcol = (lane >> 3) & 1;
         const int vrow = k16 + ((lane >> 3) & 1) * 8 + (lane & 7), vcol = lane >> 4;
-        bool ok = true;
         uint32_t at = 0;
-        for (int g = g0; ok && g < g1; ++g, ++at) {
-            const int s = (int)(at % ST);
-            ok = !wait(&bars->full[s], at / ST);
-            if (!ok) break;
-            const int first = bars->first[s][box];
-            uint32_t see = 0;                          // keys of the 16 that the token sees
-            if (first == kWhole) {
-                see = 0xffffu;
-            } else if (first != kHidden) {
-                const int key = first + (k16 & (box_rows - 1));
-                const int all = p.tree ? it.base : it.pos + 1, n = all - key;
-                see = n >= 16 ? 0xffffu : n > 0 ? (1u << n) - 1u : 0u;
-                if (p.tree) {
-                    const int d = key - it.base, end = it.kv_len - key;
-                    if (d >= 0) {
-                        if (d < 64) see |= (uint32_t)(tree >> d) & 0xffffu;
-                    } else if (d > -16) {
-                        see |= (uint32_t)(tree << -d) & 0xffffu;
-                    }
-                    see &= end >= 16 ? 0xffffu : end > 0 ? (1u << end) - 1u : 0u;
-                }
-            }
-            if (see) {
-                const uint32_t kt = sb + s * S::BYTES, vt = kt + S::TILE;
-                float sc[2][4] = {};
+        bool waited = false, lost = false;             // lost: a wait ran out; all go on to the next barrier
+        for (uint32_t n = 0;; ++n) {
+            lost |= wait(&sh.q_full, n);
+            if (readers_any(lost) || !sh.item.valid) break;
+            const Item it = sh.item;
+            if (OWN && threadIdx.x < 2) sh.parts[threadIdx.x] = sh.item.parts[threadIdx.x];   // (read behind the item's barriers)
+            uint32_t qa[DH / 16][4];
+            {
+                auto word = [&](int row, int col) {
+                    return row < it.rows ? *reinterpret_cast<const uint32_t*>(&sh.q[row][col + q2]) : 0u;
+                };
 #pragma unroll
                 for (int k = 0; k < DH / 16; ++k) {
-                    uint32_t b[4];
-                    ldmatrix_x4(b, kt + (k >> 2) * S::SLAB + krow * 128 + ((((k & 3) * 2 + kcol) ^ (krow & 7)) << 4));
-                    const uint32_t b0[2] = {b[0], b[1]}, b1[2] = {b[2], b[3]};
-                    mma_bf16_16816(sc[0], qa[k], b0);
-                    mma_bf16_16816(sc[1], qa[k], b1);
-                }
-                uint32_t pa[4] = {0, 0, 0, 0};
-                float f[2] = {1.f, 1.f};
-                bool moved = false;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (i && !two) break;
-                    float x[4] = {sc[0][2 * i] * p.scale_log2, sc[0][2 * i + 1] * p.scale_log2,
-                                  sc[1][2 * i] * p.scale_log2, sc[1][2 * i + 1] * p.scale_log2};
-                    if (see != 0xffffu) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (!(see >> (q2 + (j & 1) + (j >> 1) * 8) & 1u)) x[j] = -INFINITY;
-                    }
-                    float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                    if (mx > m[i] + 8.f || m[i] == -INFINITY) {
-                        f[i] = m[i] == -INFINITY ? 0.f : ex2(m[i] - mx);
-                        m[i] = mx;
-                        moved = true;
-                    }
-                    const float ref = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = ex2(x[j] - ref);
-                    l[i] = l[i] * f[i] + ((x[0] + x[1]) + (x[2] + x[3]));
-                    pa[i] = pack_bf16x2(x[0], x[1]);
-                    pa[2 + i] = pack_bf16x2(x[2], x[3]);
-                }
-                if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-                    for (int i = 0; i < DH / 8; ++i) {
-                        o[i][0] *= f[0];
-                        o[i][1] *= f[0];
-                        o[i][2] *= f[1];
-                        o[i][3] *= f[1];
-                    }
-                }
-                const uint32_t z0 = (see >> q2 & 1u ? 0xffffu : 0u) | (see >> (q2 + 1) & 1u ? 0xffff0000u : 0u);
-                const uint32_t z1 = (see >> (q2 + 8) & 1u ? 0xffffu : 0u) | (see >> (q2 + 9) & 1u ? 0xffff0000u : 0u);
-#pragma unroll
-                for (int k = 0; k < DH / 16; ++k) {
-                    uint32_t b[4];
-                    ldmatrix_x4_trans(b, vt + (k >> 2) * S::SLAB + vrow * 128 + ((((k & 3) * 2 + vcol) ^ (vrow & 7)) << 4));
-                    const uint32_t b0[2] = {b[0] & z0, b[1] & z1}, b1[2] = {b[2] & z0, b[3] & z1};
-                    mma_bf16_16816(o[2 * k], pa, b0);
-                    mma_bf16_16816(o[2 * k + 1], pa, b1);
+                    qa[k][0] = word(r, k * 16);
+                    qa[k][1] = word(r + 8, k * 16);
+                    qa[k][2] = word(r, k * 16 + 8);
+                    qa[k][3] = word(r + 8, k * 16 + 8);
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars->empty[s]));
-        }
-        // Sums of the row's four lanes.
+            if (lane == 0) mbar_arrive(smem_u32(&sh.q_empty));
+            const uint64_t tree = p.tree ? __ldg(p.tree + it.t) : 0;
+            const bool two = it.rows > 8;              // the tile's lower half has rows
+            float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};   // rows lane / 4 and lane / 4 + 8
+            float o[DH / 8][4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-        }
-    }
-    __syncthreads();                                   // the stages are free: all copies have landed and been read
-    // ------------------------------------------------------------------- joins
-    float* parts = reinterpret_cast<float*>(smem);     // [kReaders][16][DH], then the CTA's [16][DH]
-    float* own = parts + kReaders * 16 * DH;
-    if (warp < kReaders) {
-        const int r = lane >> 2, q2 = (lane & 3) * 2;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (r + 8 * i < it.rows) {
-                if ((lane & 3) == 0) bars->ml[warp][r + 8 * i] = make_float2(m[i], l[i]);
-                float* to = parts + (warp * 16 + r + 8 * i) * DH + q2;
-#pragma unroll
-                for (int k = 0; k < DH / 8; ++k) *reinterpret_cast<float2*>(to + k * 8) = make_float2(o[k][2 * i], o[k][2 * i + 1]);
-            }
-    }
-    __syncthreads();
-    auto rescale = [](float part, float top) { return part == -INFINITY ? 0.f : ex2(part - top); };   // (no key seen: no part)
-    __nv_bfloat16* out = p.out + (size_t)it.t * p.ld_out + (size_t)(it.head * c.rep + it.row0) * DH;
-    if (OWN) {
-        pdl_wait();
-        pdl_trigger();
-    }
-    // Two columns of a row: the other parts first, in the order of the keys, then what is here; its output.
-    auto put_out = [&](int r, int col, float top, float sum, float a, float b) {
-        if (OWN) {
-            float t0 = -INFINITY, s0 = 0.f, a0 = 0.f, b0 = 0.f, fa, fb;
-            const int n0 = bars->parts[0].count, n = n0 + bars->parts[1].count;
-            constexpr int SIDE = 8;
-            for (int k0 = 0; k0 < n; k0 += SIDE) {
-                float2 ml[SIDE], v[SIDE];
-#pragma unroll
-                for (int i = 0; i < SIDE; ++i) {
-                    const int k = min(k0 + i, n - 1);
-                    const PartList& l = bars->parts[k >= n0];
-                    const long long row = l.row + (long long)(k >= n0 ? k - n0 : k) * l.step + r;
-                    ml[i] = __ldcg(c.part_ml + row);
-                    v[i] = __ldcg(reinterpret_cast<const float2*>(l.at<DH>(c.part_o, row) + (col >> 2) * l.next4() + (col & 3)));
-                }
-#pragma unroll
-                for (int i = 0; i < SIDE; ++i)
-                    if (join_source(ml[i], k0 + i < n, t0, s0, fa, fb)) {
-                        a0 = a0 * fa + v[i].x * fb;
-                        b0 = b0 * fa + v[i].y * fb;
+            for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+            for (int g = it.g0; g < it.g1 && !lost; ++g, ++at) {
+                const int s = (int)(at % ST);
+                lost |= wait(&sh.full[s], at / ST);
+                const int first = sh.first[s][box];
+                uint32_t see = 0;                      // keys of the 16 that the token sees
+                if (first == kWhole) {
+                    see = 0xffffu;
+                } else if (first != kHidden) {
+                    const int key = first + (k16 & (box_rows - 1));
+                    const int all = p.tree ? it.base : it.pos + 1, k = all - key;
+                    see = k >= 16 ? 0xffffu : k > 0 ? (1u << k) - 1u : 0u;
+                    if (p.tree) {
+                        const int d = key - it.base, end = it.kv_len - key;
+                        if (d >= 0) {
+                            if (d < 64) see |= (uint32_t)(tree >> d) & 0xffffu;
+                        } else if (d > -16) {
+                            see |= (uint32_t)(tree << -d) & 0xffffu;
+                        }
+                        see &= end >= 16 ? 0xffffu : end > 0 ? (1u << end) - 1u : 0u;
                     }
-            }
-            if (join_source(make_float2(top, sum), true, t0, s0, fa, fb)) {
-                a0 = a0 * fa + a * fb;
-                b0 = b0 * fa + b * fb;
-            }
-            sum = s0;
-            a = a0;
-            b = b0;
-        }
-        const float il = sum == 0.f ? 0.f : 1.f / sum;
-        *reinterpret_cast<uint32_t*>(out + (size_t)r * DH + col) = pack_bf16x2(a * il, b * il);
-    };
-    for (int x = threadIdx.x; x < it.rows * (DH / 2); x += kThreads) {
-        const int r = x / (DH / 2), col = x % (DH / 2) * 2;
-        float top = -INFINITY, sum = 0.f, a = 0.f, b = 0.f;
+                }
+                if (see) {
+                    const uint32_t kt = sb + s * S::BYTES, vt = kt + S::TILE;
+                    float sc[2][4] = {};
 #pragma unroll
-        for (int w = 0; w < kReaders; ++w) top = fmaxf(top, bars->ml[w][r].x);
+                    for (int k = 0; k < DH / 16; ++k) {
+                        uint32_t b[4];
+                        ldmatrix_x4(b, kt + (k >> 2) * S::SLAB + krow * 128 + ((((k & 3) * 2 + kcol) ^ (krow & 7)) << 4));
+                        const uint32_t b0[2] = {b[0], b[1]}, b1[2] = {b[2], b[3]};
+                        mma_bf16_16816(sc[0], qa[k], b0);
+                        mma_bf16_16816(sc[1], qa[k], b1);
+                    }
+                    uint32_t pa[4] = {0, 0, 0, 0};
+                    float f[2] = {1.f, 1.f};
+                    bool moved = false;
 #pragma unroll
-        for (int w = 0; w < kReaders; ++w) {
-            const float2 ml = bars->ml[w][r], v = *reinterpret_cast<const float2*>(parts + (w * 16 + r) * DH + col);
-            const float f = rescale(ml.x, top);
-            sum = ml.x == -INFINITY ? sum : fmaf(ml.y, f, sum);
-            a = ml.x == -INFINITY ? a : fmaf(v.x, f, a);
-            b = ml.x == -INFINITY ? b : fmaf(v.y, f, b);
-        }
-        if (splits == 1) {
-            put_out(r, col, top, sum, a, b);
-        } else {
-            *reinterpret_cast<float2*>(own + r * DH + col) = make_float2(a, b);
-            if (col == 0) bars->mine[r] = make_float2(top, sum);
+                    for (int i = 0; i < 2; ++i) {
+                        if (i && !two) break;
+                        float x[4] = {sc[0][2 * i] * p.scale_log2, sc[0][2 * i + 1] * p.scale_log2,
+                                      sc[1][2 * i] * p.scale_log2, sc[1][2 * i + 1] * p.scale_log2};
+                        if (see != 0xffffu) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (!(see >> (q2 + (j & 1) + (j >> 1) * 8) & 1u)) x[j] = -INFINITY;
+                        }
+                        float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                        if (mx > m[i] + 8.f || m[i] == -INFINITY) {
+                            f[i] = m[i] == -INFINITY ? 0.f : ex2(m[i] - mx);
+                            m[i] = mx;
+                            moved = true;
+                        }
+                        const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = ex2(x[j] - ref);
+                        l[i] = l[i] * f[i] + ((x[0] + x[1]) + (x[2] + x[3]));
+                        pa[i] = pack_bf16x2(x[0], x[1]);
+                        pa[2 + i] = pack_bf16x2(x[2], x[3]);
+                    }
+                    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                        for (int i = 0; i < DH / 8; ++i) {
+                            o[i][0] *= f[0];
+                            o[i][1] *= f[0];
+                            o[i][2] *= f[1];
+                            o[i][3] *= f[1];
+                        }
+                    }
+                    const uint32_t z0 = (see >> q2 & 1u ? 0xffffu : 0u) | (see >> (q2 + 1) & 1u ? 0xffff0000u : 0u);
+                    const uint32_t z1 = (see >> (q2 + 8) & 1u ? 0xffffu : 0u) | (see >> (q2 + 9) & 1u ? 0xffff0000u : 0u);
+#pragma unroll
+                    for (int k = 0; k < DH / 16; ++k) {
+                        uint32_t b[4];
+                        ldmatrix_x4_trans(b, vt + (k >> 2) * S::SLAB + vrow * 128 + ((((k & 3) * 2 + vcol) ^ (vrow & 7)) << 4));
+                        const uint32_t b0[2] = {b[0] & z0, b[1] & z1}, b1[2] = {b[2] & z0, b[3] & z1};
+                        mma_bf16_16816(o[2 * k], pa, b0);
+                        mma_bf16_16816(o[2 * k + 1], pa, b1);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.empty[s]));
+            }
+            // -------------------------------------------------------------- the item's result
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+                if ((lane & 3) == 0) sh.ml[warp][r + 8 * i] = make_float2(m[i], l[i]);
+            }
+            readers_sync();
+            // All warps' sums relative to the largest maximum.
+            float top[2], sum[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                top[i] = -INFINITY;
+                sum[i] = 0.f;
+#pragma unroll
+                for (int w = 0; w < kReaders; ++w) top[i] = fmaxf(top[i], sh.ml[w][r + 8 * i].x);
+#pragma unroll
+                for (int w = 0; w < kReaders; ++w) {
+                    const float2 ml = sh.ml[w][r + 8 * i];
+                    sum[i] += ml.x == -INFINITY ? 0.f : ml.y * ex2(ml.x - top[i]);
+                }
+                const float f = m[i] == -INFINITY ? 0.f : ex2(m[i] - top[i]);
+#pragma unroll
+                for (int k = 0; k < DH / 8; ++k) {
+                    o[k][2 * i] *= f;
+                    o[k][2 * i + 1] *= f;
+                }
+            }
+            if (OWN && !waited) {
+                pdl_wait();
+                pdl_trigger();
+                waited = true;
+            }
+            __nv_bfloat16* out = p.out + (size_t)it.t * p.ld_out + (size_t)(it.head * c.rep + it.row0) * DH;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (i && !two) break;
+                // Warps 2 and 3 give theirs to 0 and 1, warp 1 gives the sum to 0.
+                if (warp >= 2)
+#pragma unroll
+                    for (int k = 0; k < DH / 8; ++k) sh.swap[warp - 2][k][lane] = make_float2(o[k][2 * i], o[k][2 * i + 1]);
+                readers_sync();
+                if (warp < 2)
+#pragma unroll
+                    for (int k = 0; k < DH / 8; ++k) {
+                        const float2 x = sh.swap[warp][k][lane];
+                        o[k][2 * i] += x.x;
+                        o[k][2 * i + 1] += x.y;
+                        if (warp == 1) sh.swap[1][k][lane] = make_float2(o[k][2 * i], o[k][2 * i + 1]);
+                    }
+                readers_sync();
+                // The rows' result: in a cluster where the stages were (its item is the CTA's last).
+                float* own = splits > 1 ? reinterpret_cast<float*>(smem) + 8 * i * DH : reinterpret_cast<float*>(sh.swap[0]);
+                if (warp == 0) {
+#pragma unroll
+                    for (int k = 0; k < DH / 8; ++k) {
+                        const float2 x = sh.swap[1][k][lane];
+                        *reinterpret_cast<float2*>(own + r * DH + k * 8 + q2) = make_float2(o[k][2 * i] + x.x, o[k][2 * i + 1] + x.y);
+                    }
+                    if ((lane & 3) == 0) sh.mine[r + 8 * i] = make_float2(top[i], sum[i]);
+                }
+                readers_sync();
+                if (splits > 1) continue;
+                // Four columns of a row a thread: the other parts first, in the order of the keys, then what is here.
+                // (Rows side by side: so they lie in parts.)
+                const int rows = min(8, it.rows - 8 * i);
+                for (int e = threadIdx.x; e < rows * (DH / 4); e += kReaders * 32) {
+                    const int col = e / rows * 4, row = e % rows;
+                    float t = -INFINITY, s = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (OWN) add_parts<DH>(c, sh.parts, 8 * i + row, col, t, s, a);
+                    add_source(sh.mine[8 * i + row], *reinterpret_cast<const float4*>(own + row * DH + col), true, t, s, a);
+                    const float il = s == 0.f ? 0.f : 1.f / s;
+                    *reinterpret_cast<uint2*>(out + (size_t)(8 * i + row) * DH + col) =
+                        make_uint2(pack_bf16x2(a[0] * il, a[1] * il), pack_bf16x2(a[2] * il, a[3] * il));
+                }
+                readers_sync();
+            }
+            if (splits > 1) break;                     // (a cluster has one item)
         }
     }
     if (splits == 1) return;
+    // ------------------------------------------------------------------- clusters
     cluster_sync();
-    const uint32_t own_at = smem_u32(own), ml_at = smem_u32(bars->mine);
-    auto peer = [](uint32_t at, uint32_t cta) {
+    const Item& it = sh.item;                          // (kept: the loading warp says no more than that there are no more)
+    const uint32_t own_at = sb, ml_at = smem_u32(sh.mine);
+    auto peer2 = [](uint32_t at, uint32_t cta) {
         float2 v;
         asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(mapa_shared(at, cta)) : "memory");
         return v;
     };
-    for (int x = rank * kThreads + threadIdx.x; x < it.rows * (DH / 2); x += splits * kThreads) {
-        const int r = x / (DH / 2), col = x % (DH / 2) * 2;
-        float top = -INFINITY, sum = 0.f, a = 0.f, b = 0.f;
-        for (int w = 0; w < splits; ++w) top = fmaxf(top, peer(ml_at + r * 8, w).x);
-        for (int w = 0; w < splits; ++w) {
-            const float2 ml = peer(ml_at + r * 8, w), v = peer(own_at + (r * DH + col) * 4, w);
-            const float f = rescale(ml.x, top);
-            sum = ml.x == -INFINITY ? sum : fmaf(ml.y, f, sum);
-            a = ml.x == -INFINITY ? a : fmaf(v.x, f, a);
-            b = ml.x == -INFINITY ? b : fmaf(v.y, f, b);
+    auto peer4 = [](uint32_t at, uint32_t cta) {
+        float4 v;
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(mapa_shared(at, cta)) : "memory");
+        return v;
+    };
+    __nv_bfloat16* out = p.out + (size_t)it.t * p.ld_out + (size_t)(it.head * c.rep + it.row0) * DH;
+    for (int e = rank * kThreads + threadIdx.x; e < it.rows * (DH / 4); e += splits * kThreads) {
+        const int col = e / it.rows * 4, row = e % it.rows;
+        float top = -INFINITY, sum = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+        if (OWN) {
+            pdl_wait();
+            add_parts<DH>(c, sh.parts, row, col, top, sum, a);
         }
-        put_out(r, col, top, sum, a, b);
+        for (int w = 0; w < splits; ++w) add_source(peer2(ml_at + row * 8, w), peer4(own_at + (row * DH + col) * 4, w), true, top, sum, a);
+        const float il = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<uint2*>(out + (size_t)row * DH + col) = make_uint2(pack_bf16x2(a[0] * il, a[1] * il),
+                                                                             pack_bf16x2(a[2] * il, a[3] * il));
     }
     cluster_sync();                                    // nobody ends while others read its sums
 }
@@ -429,16 +496,17 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 template <int DH, bool OWN>
 cudaError_t blocks_launch(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                           cudaStream_t st) {
-    constexpr size_t smem = Stage<DH>::COUNT * Stage<DH>::BYTES + sizeof(Bars);
-    static_assert((kReaders + 1) * 16 * DH * 4 <= Stage<DH>::COUNT * Stage<DH>::BYTES, "joins fit the stages");
+    constexpr size_t smem = sizeof(Shared<DH>);
+    static_assert(smem + 1024 <= 228 * 1024 / 2, "two CTAs to an SM");
     static_assert(Stage<DH>::COUNT <= 8, "barriers");
     static PerDevice attr;
     cudaError_t e = (cudaError_t)attr.get([] {
         return (int)cudaFuncSetAttribute(cache_blocks_kernel<DH, OWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     }, true);
     if (e != cudaSuccess) return e;
+    const long long items = (long long)p.T * c.Hkv * p.row_tiles;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((long long)p.T * c.Hkv * p.row_tiles * p.splits));
+    cfg.gridDim = dim3((unsigned)(p.splits == 1 ? std::min<long long>(items, 2LL * c.num_sms) : items * p.splits));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
             g.ntok = min(2 * TT, all - tok);
             g.t0 = 0;
             g.common = 1;
-            g.cost = (s_common[k] + kShareOver) << cache_two_tiles(g.ntok, TT);
+            g.cost = s_common[k] * share_tile(cache_two_tiles(g.ntok, TT)) + kShareEnds;
         } else if (e < items) {
             const int k = find(s_own, n_seqs, e);
             const CacheSeq s = c.seqs[k];
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
             g.row = s.q_off + tok;
             g.ntok = min(2 * TT, s.q_len - tok);
             g.t0 = s_common[s_of[k]];
-            g.cost = (cache_group_tiles(s.q_len, s.kv_len, g.first, g.ntok) - g.t0 + kShareOver) << cache_two_tiles(g.ntok, TT);
+            g.cost = (cache_group_tiles(s.q_len, s.kv_len, g.first, g.ntok) - g.t0) * share_tile(cache_two_tiles(g.ntok, TT)) + kShareEnds;
         }
         long long sum;
         g.pre = W + block_sum((long long)g.cost, s_wl, sum);
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     }
     two = __syncthreads_or(two);
     W *= c.Hkv;
-    const int n_ctas = !W ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles << (two ? 1 : 0))));
+    const int n_ctas = !W ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles * share_tile(two ? 1 : 0))));
     // Where parts lie: an item's pieces are as many as heads and cuts.
     long long rows = 0;
     for (int e0 = 0; e0 < items; e0 += kPlanThreads) {
@@ -244,6 +244,15 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         const long long before = rows + block_sum((long long)mine, s_wl, sum);
         rows += sum;
         if (e < items) c.groups[e].part_row = (int)(before - (long long)first * r);
+    }
+    __syncthreads();
+    for (int k = i; k < items * c.Hkv; k += kPlanThreads) {
+        const int e = k / c.Hkv;
+        const int cost = c.groups[e].cost, step = share_tile(cache_two_tiles(c.groups[e].ntok, TT));
+        const long long start = c.groups[e].pre * c.Hkv + (long long)(k - e * c.Hkv) * cost;
+        const int first = cache_cta_of(start, W, n_ctas);
+        const int tiles = share_tiles(cost, step - 2);
+        c.cut[k] = make_int2(first, cache_cta_of(start + (long long)(tiles - 1) * step, W, n_ctas) - first + 1);
     }
     if (i == 0) {
         c.plan->total = W;
