@@ -302,7 +302,8 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
         const bool large = d.page > 64;
         e = c->own(c->share, large ? c->tm_k64[layer] : c->tm_k[layer], large ? c->tm_v64[layer] : c->tm_v[layer], b, st);
     }
-    return c->launched(e, p.join_here ? 1 : 2, "cache_attend");
+    if (e == cudaSuccess && d.shared) e = c->join(c->share, p, st);
+    return c->launched(e, (p.join_here ? 1 : 2) + p.single, "cache_attend");
 }
 
 extern "C" trimmoe_status trimmoe_cache_fork(trimmoe_cache_handle c, int n, const int32_t* src, const int32_t* dst,

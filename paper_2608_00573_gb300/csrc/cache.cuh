@@ -65,6 +65,7 @@ struct CachePlan {
     int ok;                            // 0: the step was refused
     int drawn, done;                   // items drawn beyond the first round, CTAs that have finished
     int own_apart;                     // with groups of sequences: sequences' own tiles are not on the line
+    int serial;                        // of the step (a list with groups is of the step with its number)
 };
 
 __host__ __device__ inline int cache_two_tiles(int ntok, int tile_tokens) { return ntok > tile_tokens ? 1 : 0; }
@@ -95,10 +96,12 @@ __host__ __device__ inline int cache_part_rows(int ntok, int tile_tokens, int re
 // grow, so their sum names the pieces.
 
 // With groups of sequences: cost of a key tile (both query tiles', when an item has two) and of an
-// item's beginning and end, in about 0.47 us (measured: 0.92, 1.43 and 3.2 us; sequences' own items are
-// short, so this matters more than in other steps).
-__host__ __device__ inline int share_tile(int two) { return 2 + two; }
-constexpr int kShareEnds = 7;
+// item's beginning and end, in kShareUnit us.  (Measured: 0.9 to 1.5, 1.4 to 1.9 and 3.2 to 4.4 us;
+// sequences' own items are short, so this matters more than in other steps: with a tile and an end
+// alike, the last CTA of 12 drafted trees ended at 97 us, the others at 63.)
+constexpr float kShareUnit = 0.25f;
+__host__ __device__ inline int share_tile(int two) { return 5 + two; }
+constexpr int kShareEnds = 16;
 __host__ __device__ inline int share_tiles(int cost, int two) { return (cost - kShareEnds) / share_tile(two); }
 // Key tiles that the first x of an item's cost cover.
 __host__ __device__ inline int share_tiles_before(long long x, int cost, int two) {
@@ -139,10 +142,12 @@ struct CacheDev {
     int8_t* codes;                     // [layers][n_pages][Hkv][2][dh]
     float* scales;                     // [layers][n_pages][Hkv]
     uint32_t* scores;                  // [cache_score_keys] of a choice, as ordered whole numbers
-    // Steps with groups of sequences: the list of items is in `groups` and the parts in part_o and
-    // part_ml as for other steps, but these are other, larger buffers (the host side chooses).
+    // Steps with groups of sequences: the list of items is in plan, shares and groups and the parts in
+    // part_o and part_ml as for other steps, but these are other buffers (the host side chooses).
     int shared;
-    int2* items_of;                    // [T] groups that hold a token: its own keys' and its common ones' (-1: none)
+    const CachePlan* step_plan;        // the step's own plan
+    int4* items_of;                    // [T] groups that hold a token: its own keys' and its common ones' (-1: none); first own
+                                       // page; 1 if its own keys are not on the line
     int* common;                       // [max_seqs] key tiles that a group of sequences has in common
     int2* cut;                         // [groups][Hkv] first CTA that holds tiles of an item, how many do
     int* err;
@@ -205,16 +210,18 @@ inline size_t cache_score_keys(const CacheDev& c) {
 
 // Steps with groups of sequences: rows (tokens times query heads) at most, and what that allows.
 constexpr int kShareRows = 65536;
-inline long long cache_share_groups(const CacheDev& c) {
-    const long long T = kShareRows / c.Hq;
-    return 2 * std::min(T, T / (2 * c.tile_tokens) + c.max_seqs + 1);
-}
 // Every token has its own and at most one common part, a part's rows are at most twice its
 // tokens' (whole warps, tiles that rep does not divide), a cut adds one part of 256 rows, and
-// an item's rows begin at a multiple of 32.
-inline long long cache_share_part_rows(const CacheDev& c) {
-    return 4LL * kShareRows + 256LL * c.num_sms + 32 * cache_share_groups(c);
+// an item's rows begin at a multiple of 32.  Own parts that are not on the line lie behind those that
+// common ones can take, row by row: [T][Hq].
+__host__ __device__ inline long long cache_share_groups(const CacheDev& c) {
+    const long long T = kShareRows / c.Hq, n = T / (2 * c.tile_tokens) + c.max_seqs + 1;
+    return 2 * (T < n ? T : n);
 }
+__host__ __device__ inline long long cache_own_rows(const CacheDev& c) {
+    return 2LL * kShareRows + 256LL * c.num_sms + 32 * cache_share_groups(c);
+}
+inline long long cache_share_part_rows(const CacheDev& c) { return 2LL * kShareRows + cache_own_rows(c); }
 
 cudaError_t launch_cache_step(const CacheDev& c, int n, const int* seq, const int* q_len, int T, cudaStream_t st);
 cudaError_t launch_cache_fork(const CacheDev& c, int n, const int* src, const int* dst, cudaStream_t st);
@@ -232,12 +239,21 @@ cudaError_t launch_cache_bounds_accepted(const CacheDev& c, int n, const int* se
 cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches);
 cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                 const BlocksParams& p, cudaStream_t st);
-// A step of single tokens with groups of sequences, behind the attention kernel: sequences' own
-// tiles, unless these were on its line, and the sum with the parts.
+// A step of single tokens with groups of sequences, beside the attention kernel: sequences' own
+// tiles, unless these are on its line.
 cudaError_t launch_cache_own(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                              cudaStream_t st);
+// Behind both: the sums of a step's parts.
+cudaError_t launch_cache_join(const CacheDev& c, const AttendParams& p, cudaStream_t st);
 // CTAs of one of `items` items with about as many stages of 64 positions.
 int cache_blocks_splits(const CacheDev& c, long long items, int stages);
+// A list with groups is not of the last step (a captured attend replayed without its share).
+__device__ __forceinline__ bool share_stale(const CacheDev& c, const CachePlan& pl) {
+    const bool stale = pl.serial != c.step_plan->serial;
+    if (stale && blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(c.err, 0, ERR_CACHE_STATE);
+    return stale;
+}
+
 // The list of items of a step whose listed sequences form n groups.  splits: of launch_cache_own, 0 when
 // the step is not one of single tokens.
 cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st);
@@ -252,7 +268,9 @@ struct PartList {
     int step, count;
     __device__ bool warps() const { return step >= 32; }
 };
-__device__ __forceinline__ PartList part_list(const CacheDev& c, int group, int head, int t) {
+__device__ __forceinline__ PartList part_list(const CacheDev& c, const int4& of, bool own, int head, int t) {
+    const int group = own ? of.x : of.y;
+    if (own && of.w) return PartList{cache_own_rows(c) + (long long)t * c.Hq + head * c.rep, 1, 1};
     if (group < 0) return PartList{0, 1, 0};
     const int2 cut = c.cut[(size_t)group * c.Hkv + head];
     const CacheGroup g = c.groups[group];
@@ -292,12 +310,10 @@ __device__ __forceinline__ void add_source(float2 ml, float4 x, bool there, floa
     a[2] = there ? a[2] * fa + x.z * fb : a[2];
     a[3] = there ? a[3] * fa + x.w * fb : a[3];
 }
-// Adds four columns of query head `row` from two lists of parts, the first one's first; twelve reads are in
-// flight.
-template <int DH>
+// Adds four columns of query head `row` from two lists of parts, the first one's first; B are read at a time.
+template <int DH, int B>
 __device__ __forceinline__ void add_parts(const CacheDev& c, const PartList (&parts)[2], int row, int col, float& top, float& l,
                                           float (&a)[4]) {
-    constexpr int B = 12;
     const PartList p0 = parts[0], p1 = parts[1];
     const int n = p0.count + p1.count;
     for (int k0 = 0; k0 < n; k0 += B) {

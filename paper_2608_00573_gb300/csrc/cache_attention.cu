@@ -457,6 +457,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             long long x = 0, x_end = 0, within = 0;
             CacheGroup g;
             bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
+            if (SHARED && any) any = !share_stale(c, pl);
             if (any && !whole) {
                 x = sh.begin;
                 x_end = sh.end;
@@ -1123,38 +1124,6 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
         join_rows<DH, DH / 32>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
 }
 
-// Adds the parts of a step with groups of sequences.  A block takes a token and up to eight key/value
-// heads, whose lists of parts it looks up first; a thread then takes four columns of a query
-// head at a time, the common item's parts first, in the order of the keys.  Neighbouring
-// threads take the heads that share a key/value head: their rows of a part lie side by side (with
-// neighbouring columns instead the join of 12 trees took 27 us).  Bound: L2.
-constexpr int kJoinHeads = 8;
-template <int DH>
-__global__ void __launch_bounds__(256, 2) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
-                                                                const __grid_constant__ AttendParams p) {
-    __shared__ PartList s_parts[kJoinHeads][2];
-    const int blocks = (c.Hkv + kJoinHeads - 1) / kJoinHeads;
-    const int t = blockIdx.x / blocks, head0 = blockIdx.x % blocks * kJoinHeads, heads = min(kJoinHeads, c.Hkv - head0);
-    pdl_wait();
-    pdl_trigger();
-    const int ok = c.plan->ok;
-    if (threadIdx.x < 2 * heads) {
-        const int k = threadIdx.x >> 1, own = threadIdx.x & 1;
-        const int2 of = c.items_of[t];
-        s_parts[k][own] = part_list(c, own ? of.x : of.y, head0 + k, t);
-    }
-    if (!ok) return;
-    __syncthreads();
-    for (int e = threadIdx.x; e < heads * c.rep * (DH / 4); e += 256) {
-        const int x = e / c.rep, k = x / (DH / 4), col = x % (DH / 4) * 4, row = e - x * c.rep;
-        float top = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-        add_parts<DH>(c, s_parts[k], row, col, top, l, a);
-        const float il = l == 0.f ? 0.f : 1.f / l;
-        *reinterpret_cast<uint2*>(p.out + (size_t)t * p.ld_out + (size_t)((head0 + k) * c.rep + row) * DH + col) =
-            make_uint2(pack_bf16x2(a[0] * il, a[1] * il), pack_bf16x2(a[2] * il, a[3] * il));
-    }
-}
-
 static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
 
 template <int DH, bool SHARED>
@@ -1177,11 +1146,7 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
     e = launch_pdl(cache_attention_kernel<DH, SHARED>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
                    c, p);
     if (e != cudaSuccess || p.join_here) return e;
-    if (SHARED) {
-        if (p.single) return e;                        // (launch_cache_own joins)
-        return launch_pdl(cache_join_shared_kernel<DH>, dim3((unsigned)(p.T * ((c.Hkv + kJoinHeads - 1) / kJoinHeads))), dim3(256), 0,
-                          st, c, p);
-    }
+    if (SHARED) return e;                              // (launch_cache_join)
     return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);
 }
 

@@ -46,7 +46,7 @@ struct Item {
     int t, head, row0, rows;   // token, key/value head, query heads of it
     int base, kv_len, pos;
     int g0, g1;                // stages
-    PartList parts[2];         // OWN: the common item's parts, the sequence's own ones
+    int part;                  // OWN: there are common tiles
 };
 
 template <int DH>
@@ -68,7 +68,6 @@ struct __align__(128) Shared {
     uint64_t full[8], empty[8], q_full, q_empty;
     int first[8][4];           // of the stage's pages: first position, kHidden or kWhole
     Item item;
-    PartList parts[2];         // OWN: the item's, for its end
     int abort_flag, never;
 };
 
@@ -89,9 +88,10 @@ __device__ __forceinline__ bool readers_any(bool x) {
     return r != 0;
 }
 
-// OWN: no lists; the token's sequence from its group's common tiles on, and then the common tiles'
-// parts, which the attention kernel before this one has written.  Nothing but these is
-// read behind that kernel's end: whatever comes before it has ended when it lets this one start.
+// OWN: no lists; the token's sequence from its group's common tiles on.  The sums are a part beside those of the
+// common tiles, or the result when there are none.  This kernel runs beside the attention kernel
+// before it, which lets it start when all that comes before has ended, and waits for that kernel
+// only at its own end.
 template <int DH, bool OWN>
 __global__ void __launch_bounds__(kThreads)
 cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -111,17 +111,19 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         mbar_init(smem_u32(&sh.q_full), 1);
         mbar_init(smem_u32(&sh.q_empty), kReaders);
         sh.abort_flag = sh.never = 0;
+        sh.item.rows = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_k);
         prefetch_tmap(&tm_v);
     }
     __syncthreads();
-    if (!OWN) {
-        pdl_wait();
-        pdl_trigger();
-    }
+    if (!OWN) pdl_wait();
+    pdl_trigger();
     const CachePlan pl = *c.plan;
-    if (!pl.ok) return;                                // (all CTAs)
+    if (!pl.ok || (OWN && (!pl.own_apart || share_stale(c, pl)))) {     // (all CTAs)
+        if (OWN) pdl_wait();
+        return;
+    }
     if (sb & 1023u) {
         if (threadIdx.x == 0) atomicCAS(c.err, 0, ERR_TIMEOUT_CACHE_ATTN);
         return;
@@ -133,16 +135,34 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const int page_boxes = c.page > kStageKeys ? c.page / kStageKeys : 1;     // boxes of a page's rows (pages of 128: two)
     const int per_stage = max(1, kStageKeys >> c.page_shift), box_rows = kStageKeys / per_stage;
     const int items = p.T * c.Hkv * p.row_tiles;
+    // Four columns of a row: its sums (ml: maximum and sum of p) as a part, or the result.
+    auto put = [&](const Item& it, __nv_bfloat16* out, int row, int col, float2 ml, float4 x) {
+        if (OWN && it.part) {
+            const long long at = cache_own_rows(c) + (long long)it.t * c.Hq + it.head * c.rep + row;
+            *reinterpret_cast<float4*>(c.part_o + at * DH + col) = x;
+            if (col == 0) c.part_ml[at] = ml;
+        } else {
+            const float il = ml.y == 0.f ? 0.f : 1.f / ml.y;
+            *reinterpret_cast<uint2*>(out + (size_t)row * DH + col) = make_uint2(pack_bf16x2(x.x * il, x.y * il), pack_bf16x2(x.z * il, x.w * il));
+        }
+    };
 
     if (warp == kReaders) {
         // ------------------------------------------------------------ items and loads
         uint32_t issued = 0, n_items = 0;
         bool ok = true;
+        // OWN: all items are drawn (CTAs on the attention kernel's SMs begin when it has ended), else each CTA has
+        // its first one.
         int index = blockIdx.x / splits;
+        const int given = OWN ? 0 : (int)gridDim.x;
+        if (OWN && splits == 1) {
+            if (lane == 0) index = atomicAdd(&c.plan->drawn, 1);
+            index = __shfl_sync(0xffffffffu, index, 0);
+        }
         while (ok && index < items) {
             // The next item (single CTAs; clusters have one each).
             int drawn = items;
-            if (splits == 1 && lane == 0) drawn = (int)gridDim.x + atomicAdd(&c.plan->drawn, 1);
+            if (splits == 1 && lane == 0) drawn = given + atomicAdd(&c.plan->drawn, 1);
             Item it;
             it.valid = 1;
             const int per = c.Hkv * p.row_tiles;
@@ -155,18 +175,18 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             it.kv_len = tok.kv_len;
             it.pos = tok.pos;
             int listed = 0, first_own = 0;             // entries of the list that count, first page of the step's own
+            it.part = 0;
             if (OWN) {
-                const int2 of = c.items_of[it.t];
-                first_own = of.y < 0 ? 0 : c.groups[of.y].kv_len >> c.page_shift;
-                it.parts[0] = part_list(c, of.y, it.head, it.t);
-                it.parts[1] = part_list(c, of.x, it.head, it.t);
+                const int4 of = c.items_of[it.t];
+                first_own = of.z;
+                it.part = of.y >= 0;
             } else {
                 first_own = it.base >> c.page_shift;
                 listed = min(p.n, first_own);
             }
             const int last = p.tree ? it.kv_len - 1 : it.pos;
             const int boxes = (listed + (last >> c.page_shift) - first_own + 1) * page_boxes;
-            const int stages = OWN && !pl.own_apart ? 0 : (boxes + per_stage - 1) / per_stage;
+            const int stages = (boxes + per_stage - 1) / per_stage;
             it.g0 = (int)((long long)stages * rank / splits);
             it.g1 = (int)((long long)stages * (rank + 1) / splits);
             // Lane i looks up box i of 32, the next 32 while these are copied.
@@ -272,12 +292,11 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         const int krow = k16 + (lane >> 4) * 8 + (lane & 7), kcol = (lane >> 3) & 1;
         const int vrow = k16 + ((lane >> 3) & 1) * 8 + (lane & 7), vcol = lane >> 4;
         uint32_t at = 0;
-        bool waited = false, lost = false;             // lost: a wait ran out; all go on to the next barrier
+        bool lost = false;                             // lost: a wait ran out; all go on to the next barrier
         for (uint32_t n = 0;; ++n) {
             lost |= wait(&sh.q_full, n);
             if (readers_any(lost) || !sh.item.valid) break;
             const Item it = sh.item;
-            if (OWN && threadIdx.x < 2) sh.parts[threadIdx.x] = sh.item.parts[threadIdx.x];   // (read behind the item's barriers)
             uint32_t qa[DH / 16][4];
             {
                 auto word = [&](int row, int col) {
@@ -410,11 +429,6 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                     o[k][2 * i + 1] *= f;
                 }
             }
-            if (OWN && !waited) {
-                pdl_wait();
-                pdl_trigger();
-                waited = true;
-            }
             __nv_bfloat16* out = p.out + (size_t)it.t * p.ld_out + (size_t)(it.head * c.rep + it.row0) * DH;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -445,24 +459,19 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                 }
                 readers_sync();
                 if (splits > 1) continue;
-                // Four columns of a row a thread: the other parts first, in the order of the keys, then what is here.
-                // (Rows side by side: so they lie in parts.)
-                const int rows = min(8, it.rows - 8 * i);
-                for (int e = threadIdx.x; e < rows * (DH / 4); e += kReaders * 32) {
-                    const int col = e / rows * 4, row = e % rows;
-                    float t = -INFINITY, s = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (OWN) add_parts<DH>(c, sh.parts, 8 * i + row, col, t, s, a);
-                    add_source(sh.mine[8 * i + row], *reinterpret_cast<const float4*>(own + row * DH + col), true, t, s, a);
-                    const float il = s == 0.f ? 0.f : 1.f / s;
-                    *reinterpret_cast<uint2*>(out + (size_t)(8 * i + row) * DH + col) =
-                        make_uint2(pack_bf16x2(a[0] * il, a[1] * il), pack_bf16x2(a[2] * il, a[3] * il));
+                for (int e = threadIdx.x; e < min(8, it.rows - 8 * i) * (DH / 4); e += kReaders * 32) {
+                    const int row = e / (DH / 4), col = e % (DH / 4) * 4;
+                    put(it, out, 8 * i + row, col, sh.mine[8 * i + row], *reinterpret_cast<const float4*>(own + row * DH + col));
                 }
                 readers_sync();
             }
             if (splits > 1) break;                     // (a cluster has one item)
         }
     }
-    if (splits == 1) return;
+    if (splits == 1) {
+        if (OWN) pdl_wait();
+        return;
+    }
     // ------------------------------------------------------------------- clusters
     cluster_sync();
     const Item& it = sh.item;                          // (kept: the loading warp says no more than that there are no more)
@@ -479,18 +488,13 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     __nv_bfloat16* out = p.out + (size_t)it.t * p.ld_out + (size_t)(it.head * c.rep + it.row0) * DH;
     for (int e = rank * kThreads + threadIdx.x; e < it.rows * (DH / 4); e += splits * kThreads) {
-        const int col = e / it.rows * 4, row = e % it.rows;
+        const int row = e / (DH / 4), col = e % (DH / 4) * 4;
         float top = -INFINITY, sum = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-        if (OWN) {
-            pdl_wait();
-            add_parts<DH>(c, sh.parts, row, col, top, sum, a);
-        }
         for (int w = 0; w < splits; ++w) add_source(peer2(ml_at + row * 8, w), peer4(own_at + (row * DH + col) * 4, w), true, top, sum, a);
-        const float il = sum == 0.f ? 0.f : 1.f / sum;
-        *reinterpret_cast<uint2*>(out + (size_t)row * DH + col) = make_uint2(pack_bf16x2(a[0] * il, a[1] * il),
-                                                                             pack_bf16x2(a[2] * il, a[3] * il));
+        put(it, out, row, col, make_float2(top, sum), make_float4(a[0], a[1], a[2], a[3]));
     }
     cluster_sync();                                    // nobody ends while others read its sums
+    if (OWN) pdl_wait();
 }
 
 template <int DH, bool OWN>

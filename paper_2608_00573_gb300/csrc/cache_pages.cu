@@ -152,6 +152,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     pdl_wait();
     pdl_trigger();
     const uint32_t free4 = four_pages(c.ref, nullptr, i * 4, c.n_pages);      // (on its way beside the lengths)
+    const int serial = c.plan->serial;
     int len = i < n ? c.length[seq] : 0;
     __syncthreads();
     int had = 0, last = -1, cow = 0, fresh = 0;
@@ -195,7 +196,9 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
     }
     if (s_bad) {
         if (i == 0) {
-            *c.plan = CachePlan{};
+            CachePlan none{};
+            none.serial = serial + 1;
+            *c.plan = none;
             atomicCAS(c.err, 0, s_bad);
             *c.refused = 1;
         }
@@ -295,7 +298,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_step_kernel(const __grid_c
         }
     }
     if (i == 0) {
-        *c.plan = CachePlan{W, n_groups, n_ctas, sum.cow, 1, 0, 0};
+        *c.plan = CachePlan{W, n_groups, n_ctas, sum.cow, 1, 0, 0, 0, serial + 1};
         *c.refused = 0;
     }
     __syncthreads();
@@ -575,7 +578,7 @@ __global__ void __launch_bounds__(kStepThreads) cache_compact_kernel(const __gri
                                      [&](int k, int page) { c.copies[k].x = page; });
     __syncthreads();
     for (int k = threadIdx.x; k < movers; k += kStepThreads) c.fresh[c.copies[k].x] = c.copies[k].y;
-    if (threadIdx.x == 0) *c.plan = CachePlan{live, 0, 0, movers, 0, 0, 0};
+    if (threadIdx.x == 0) *c.plan = CachePlan{live, 0, 0, movers, 0, 0, 0, 0, c.plan->serial + 1};
 }
 
 // Tables and counts follow the moved pages.

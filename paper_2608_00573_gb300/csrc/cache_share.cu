@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kCommonThreads) cache_common_kernel(const __gr
     __syncthreads();
     pdl_wait();
     pdl_trigger();
-    if (!c.plan->ok) return;
+    if (!c.step_plan->ok) return;
     for (int i = from + threadIdx.x; i < to; i += kCommonThreads) {
         const CacheSeq s = c.seqs[i];
         if (s.q_len > 0) {
@@ -129,7 +129,14 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     const int i = threadIdx.x, n = l.n, TT = c.tile_tokens;
     pdl_wait();
     pdl_trigger();
-    if (!c.plan->ok) return;
+    if (!c.step_plan->ok) {
+        if (i == 0) {
+            CachePlan none{};
+            none.serial = c.step_plan->serial;
+            *c.plan = none;
+        }
+        return;
+    }
     int tiles = 0, count = 0;
     if (i == 0) s_max = 0;
     if (i < n) {
@@ -142,6 +149,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         tok = z.q_off + z.q_len - a.q_off;
     }
     bool apart = splits > 0;
+    long long own_stages = 0;
     if (apart) {
         // Single tokens: what sharing saves is read from L2 otherwise, at twice HBM's rate and
         // more, and the second kernel alone has less to wait for.
@@ -161,6 +169,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         long long sum;
         block_sum((long long)stages, s_wl, sum);
         apart = (long long)s_max / splits <= sum * c.Hkv / c.num_sms + 16;
+        own_stages = sum;
     }
     if (tiles) count = (tok + 2 * TT - 1) / (2 * TT);
     int n_common, n_own;
@@ -226,7 +235,15 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     }
     two = __syncthreads_or(two);
     W *= c.Hkv;
-    const int n_ctas = !W ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles * share_tile(two ? 1 : 0))));
+    int n_ctas = !W ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles * share_tile(two ? 1 : 0))));
+    if (apart && n_ctas) {
+        // The second kernel's CTAs read sequences' own pages beside this one's: as many SMs as let both end
+        // together, in us (a CTA begins and ends in 6, and its tiles take 1.3 times as long beside
+        // the other kernel's traffic; own pages at HBM's rate).
+        const float a = W * (1.3f * kShareUnit), b = own_stages * (64.f * 4.f / 6.5e6f) * c.Hkv * c.dh * c.num_sms;
+        const float t = max(12.f, (a + b) / c.num_sms + 4.f);
+        n_ctas = min(n_ctas, (int)(a / (t - 6.f)) + 1);
+    }
     // Where parts lie: an item's pieces are as many as heads and cuts.
     long long rows = 0;
     for (int e0 = 0; e0 < items; e0 += kPlanThreads) {
@@ -248,22 +265,17 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     __syncthreads();
     for (int k = i; k < items * c.Hkv; k += kPlanThreads) {
         const int e = k / c.Hkv;
-        const int cost = c.groups[e].cost, step = share_tile(cache_two_tiles(c.groups[e].ntok, TT));
+        const int cost = c.groups[e].cost, two_tiles = cache_two_tiles(c.groups[e].ntok, TT), step = share_tile(two_tiles);
         const long long start = c.groups[e].pre * c.Hkv + (long long)(k - e * c.Hkv) * cost;
         const int first = cache_cta_of(start, W, n_ctas);
-        const int tiles = share_tiles(cost, step - 2);
+        const int tiles = share_tiles(cost, two_tiles);
         c.cut[k] = make_int2(first, cache_cta_of(start + (long long)(tiles - 1) * step, W, n_ctas) - first + 1);
     }
-    if (i == 0) {
-        c.plan->total = W;
-        c.plan->n_groups = items;
-        c.plan->n_ctas = n_ctas;
-        c.plan->own_apart = apart;
-    }
+    if (i == 0) *c.plan = CachePlan{W, items, n_ctas, 0, 1, 0, 0, apart, c.step_plan->serial};
     for (int t = i; t < T; t += kPlanThreads) {
         const int k = c.owner[t], g = s_of[k], from = c.seqs[l.a[g]].q_off;
-        c.items_of[t] = make_int2(apart ? -1 : s_own[k] + (t - c.seqs[k].q_off) / (2 * TT),
-                                  s_common[g] ? s_begin[g] + (t - from) / (2 * TT) : -1);
+        c.items_of[t] = make_int4(apart ? -1 : s_own[k] + (t - c.seqs[k].q_off) / (2 * TT),
+                                  s_common[g] ? s_begin[g] + (t - from) / (2 * TT) : -1, s_common[g] * kCacheTile >> c.page_shift, apart);
     }
     __syncthreads();
     for (int b = i; b < n_ctas; b += kPlanThreads) {
@@ -287,6 +299,43 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     }
 }
 
+// Adds the parts of a step with groups of sequences.  A block takes a token and some key/value heads
+// (about as many columns as threads, by four), whose lists of parts it looks up first; a thread then takes four columns of a query
+// head at a time, the common item's parts first, in the order of the keys.  Neighbouring
+// threads take the heads that share a key/value head: their rows of a part lie side by side (with
+// neighbouring columns instead the join of 12 trees took 27 us).  Bound: L2.
+constexpr int kJoinHeads = 16;
+inline __host__ __device__ int join_heads(const CacheDev& c) {
+    const int n = 1024 / (c.rep * c.dh);
+    return n < 1 ? 1 : n < kJoinHeads ? n : kJoinHeads;
+}
+template <int DH>
+__global__ void __launch_bounds__(256, 4) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
+                                                                   const __grid_constant__ AttendParams p) {
+    __shared__ PartList s_parts[kJoinHeads][2];
+    const int most = join_heads(c), blocks = (c.Hkv + most - 1) / most;
+    const int t = blockIdx.x / blocks, head0 = blockIdx.x % blocks * most, heads = min(most, c.Hkv - head0);
+    pdl_wait();
+    pdl_trigger();
+    const CachePlan pl = *c.plan;
+    if (!pl.ok || share_stale(c, pl)) return;          // (a refused step has written no items)
+    // A token whose only source is its own pages has its result already.
+    if (pl.own_apart && c.items_of[t].y < 0) return;
+    if (threadIdx.x < 2 * heads) {
+        const int k = threadIdx.x >> 1, own = threadIdx.x & 1;
+        s_parts[k][own] = part_list(c, c.items_of[t], own, head0 + k, t);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < heads * c.rep * (DH / 4); e += 256) {
+        const int x = e / c.rep, k = x / (DH / 4), col = x % (DH / 4) * 4, row = e - x * c.rep;
+        float top = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+        add_parts<DH, 6>(c, s_parts[k], row, col, top, l, a);
+        const float il = l == 0.f ? 0.f : 1.f / l;
+        *reinterpret_cast<uint2*>(p.out + (size_t)t * p.ld_out + (size_t)((head0 + k) * c.rep + row) * DH + col) =
+            make_uint2(pack_bf16x2(a[0] * il, a[1] * il), pack_bf16x2(a[2] * il, a[3] * il));
+    }
+}
+
 template <int N>
 cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st) {
     CacheList<N> l;
@@ -307,6 +356,12 @@ cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs
 cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st) {
     return n <= 64 ? share_launch<64>(c, n, counts, n_seqs, T, splits, st)
                    : share_launch<kCacheMaxSeqs>(c, n, counts, n_seqs, T, splits, st);
+}
+
+cudaError_t launch_cache_join(const CacheDev& c, const AttendParams& p, cudaStream_t st) {
+    const dim3 grid((unsigned)(p.T * ((c.Hkv + join_heads(c) - 1) / join_heads(c))));
+    return c.dh == 64 ? launch_pdl(cache_join_shared_kernel<64>, grid, dim3(256), 0, st, c, p)
+                      : launch_pdl(cache_join_shared_kernel<128>, grid, dim3(256), 0, st, c, p);
 }
 
 }  // namespace tmoe

@@ -209,6 +209,37 @@ def test_graph_replays_on_new_lengths():
     assert cache.stats()["device_error"] == 0
 
 
+def test_a_captured_attend_of_another_step():
+    """An attend captured with groups reads the list of its share: replayed behind a step without one it is
+    refused and leaves its output; plain attends captured before are as they were."""
+    cache, m, step, g = grouped((8, 2, 128), 16, [300], [4], [0, 3, 7, 1], slots=8)
+    step(range(4), [1] * 4)
+    x = torch.randn((4, 1024), generator=g, device=DEV).to(torch.bfloat16)
+    plain, out = torch.empty_like(x), torch.empty_like(x)
+    cache.attend(0, x)
+    one, two = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(one):
+        cache.attend(0, x, out=plain)
+    cache.share([4])
+    with torch.cuda.graph(two):
+        cache.attend(0, x, out=out)
+    for again in (True, False):
+        fill(cache, m, g)
+        out.fill_(3)
+        one.replay()
+        two.replay()
+        check_attend(cache, m, x, [1] * 4, plain, 0)
+        if again:
+            check_attend(cache, m, x, [1] * 4, out, 0)
+            assert cache.stats()["device_error"] == 0
+            step(range(4), [1] * 4)                  # and no share
+    assert (out == 3).all() and cache.stats(reset=True)["device_error"] == 9
+    cache.share([4])
+    two.replay()
+    check_attend(cache, m, x, [1] * 4, out, 0)
+    assert cache.stats()["device_error"] == 0
+
+
 def test_a_refused_step():
     cache, m, step, g = grouped((8, 2, 64), 16, [300], [3], [0] * 3)
     step(range(3), [1] * 3)
