@@ -283,7 +283,7 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
     const int max_rows = c->max_q > d.tile_tokens ? 2 * kCacheTile : c->max_q * d.rep;
     p.join_here = !d.shared && max_rows <= kJoinHereRows;
     p.T = c->T;
-    p.single = d.shared && c->own_splits > 0;
+    p.single = d.shared && c->single;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_attend");
     cudaStream_t st = enter(c, stream);
@@ -297,7 +297,7 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
         b.ld_out = p.ld_out;
         b.T = p.T;
         b.row_tiles = 1;
-        b.splits = c->own_splits;
+        b.splits = 1;
         b.scale_log2 = p.scale_log2;
         const bool large = d.page > 64;
         e = c->own(c->share, large ? c->tm_k64[layer] : c->tm_k[layer], large ? c->tm_v64[layer] : c->tm_v[layer], b, st);

@@ -57,14 +57,14 @@ struct __align__(16) CacheShare {
     CacheGroup g;                      // its group
 };
 
-struct CachePlan {
+struct __align__(16) CachePlan {
     long long total;                   // cost of all items
     int n_groups;
     int n_ctas;                        // CTAs that share the line; 0: whole items, drawn from a counter
     int copies;                        // pages to copy (shared last pages)
     int ok;                            // 0: the step was refused
     int drawn, done;                   // items drawn beyond the first round, CTAs that have finished
-    int own_apart;                     // with groups of sequences: sequences' own tiles are not on the line
+    int pieces;                        // with groups of sequences and single tokens: what is not on the line
     int serial;                        // of the step (a list with groups is of the step with its number)
 };
 
@@ -84,6 +84,25 @@ __host__ __device__ inline int cache_tiles_before(long long x, int cost, int two
     const long long n = cache_item_tiles(cost, two), t = x <= 0 ? 0 : (x + two) >> two;
     return (int)(x >= cost || t > n ? n : t);
 }
+
+// Steps of single tokens with groups of sequences: a piece of a sequence's own pages, for its token, or of a
+// small group's common ones, for up to 16 rows (tokens by query heads of a key/value head).
+struct __align__(16) CachePiece {
+    int seq, tok, rows, whole;         // first token; whole: every position is seen
+    int g0, g1, first_page, kv_len;    // stages of 64 positions from that page on; end of what is seen
+    int part_row, head_step;           // part: row of the first key/value head, rows from head to head; -1: the result
+    int pad[2];
+};
+constexpr int kPieceCuts = 24;         // of one sequence's or group's pages at most
+constexpr int kPieces = 8192;          // 1024 tokens', 512 groups' two and 3 CTAs' shares more, with room to spare
+
+// Where a token's parts are: pieces of its own pages and of common ones (rows of the first query head of the
+// first key/value head, and how many), or items of the line (-1: none).
+struct __align__(16) TokenParts {
+    int own_row, own_n, own_item;
+    int common_row, common_n, common_step, common_item;
+    int pad;
+};
 
 // Rows of a part of an item, in a step with groups of sequences.  From 32 on they are whole
 // warps, stored 32 rows of 4 columns side by side; fewer are stored row by row.
@@ -146,8 +165,8 @@ struct CacheDev {
     // part_o and part_ml as for other steps, but these are other buffers (the host side chooses).
     int shared;
     const CachePlan* step_plan;        // the step's own plan
-    int4* items_of;                    // [T] groups that hold a token: its own keys' and its common ones' (-1: none); first own
-                                       // page; 1 if its own keys are not on the line
+    TokenParts* parts_of;              // [T]
+    CachePiece* pieces;                // [kPieces]
     int* common;                       // [max_seqs] key tiles that a group of sequences has in common
     int2* cut;                         // [groups][Hkv] first CTA that holds tiles of an item, how many do
     int* err;
@@ -212,16 +231,16 @@ inline size_t cache_score_keys(const CacheDev& c) {
 constexpr int kShareRows = 65536;
 // Every token has its own and at most one common part, a part's rows are at most twice its
 // tokens' (whole warps, tiles that rep does not divide), a cut adds one part of 256 rows, and
-// an item's rows begin at a multiple of 32.  Own parts that are not on the line lie behind those that
-// common ones can take, row by row: [T][Hq].
+// an item's rows begin at a multiple of 32.  Pieces' parts lie row by row behind those that common ones can
+// take: one for each token and of each kind, and 64 K rows more where pages are cut.
 __host__ __device__ inline long long cache_share_groups(const CacheDev& c) {
     const long long T = kShareRows / c.Hq, n = T / (2 * c.tile_tokens) + c.max_seqs + 1;
     return 2 * (T < n ? T : n);
 }
-__host__ __device__ inline long long cache_own_rows(const CacheDev& c) {
+__host__ __device__ inline long long cache_piece_rows(const CacheDev& c) {
     return 2LL * kShareRows + 256LL * c.num_sms + 32 * cache_share_groups(c);
 }
-inline long long cache_share_part_rows(const CacheDev& c) { return 2LL * kShareRows + cache_own_rows(c); }
+inline long long cache_share_part_rows(const CacheDev& c) { return 3LL * kShareRows + cache_piece_rows(c); }
 
 cudaError_t launch_cache_step(const CacheDev& c, int n, const int* seq, const int* q_len, int T, cudaStream_t st);
 cudaError_t launch_cache_fork(const CacheDev& c, int n, const int* src, const int* dst, cudaStream_t st);
@@ -239,48 +258,65 @@ cudaError_t launch_cache_bounds_accepted(const CacheDev& c, int n, const int* se
 cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches);
 cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                 const BlocksParams& p, cudaStream_t st);
-// A step of single tokens with groups of sequences, beside the attention kernel: sequences' own
-// tiles, unless these are on its line.
+// A step of single tokens with groups of sequences, beside the attention kernel: the pieces.
 cudaError_t launch_cache_own(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                              cudaStream_t st);
 // Behind both: the sums of a step's parts.
 cudaError_t launch_cache_join(const CacheDev& c, const AttendParams& p, cudaStream_t st);
 // CTAs of one of `items` items with about as many stages of 64 positions.
 int cache_blocks_splits(const CacheDev& c, long long items, int stages);
+// A record as it is in L2.  A kernel that runs beside the one before it, and reads what kernels before that
+// one have written without a wait of its own, may find older contents in L1.
+template <class R>
+__device__ __forceinline__ R from_l2(const R* at) {
+    static_assert(sizeof(R) % 16 == 0, "whole 16-byte words");
+    union {
+        R r;
+        int4 w[sizeof(R) / 16];
+    } u;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(R) / 16); ++i) u.w[i] = __ldcg(reinterpret_cast<const int4*>(at) + i);
+    return u.r;
+}
+
 // A list with groups is not of the last step (a captured attend replayed without its share).
 __device__ __forceinline__ bool share_stale(const CacheDev& c, const CachePlan& pl) {
-    const bool stale = pl.serial != c.step_plan->serial;
+    const bool stale = pl.serial != __ldcg(&c.step_plan->serial);
     if (stale && blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(c.err, 0, ERR_CACHE_STATE);
     return stale;
 }
 
-// The list of items of a step whose listed sequences form n groups.  splits: of launch_cache_own, 0 when
-// the step is not one of single tokens.
-cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st);
+// The list of items of a step whose listed sequences form n groups.  single: each has one new token at most,
+// and launch_cache_own runs too.
+cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int single, cudaStream_t st);
 cudaError_t launch_cache_attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                 const CUtensorMap& tm_v, const AttendParams& p, int max_rows, cudaStream_t st);
 
 // Device helpers of the attention kernels.
 
-// The parts of a group's item of head `head` that hold token t: rows row + i * step, i < count, of query head 0.
+// Parts that hold a token: rows row + i * step, i < count, of query head 0 of a key/value head; warps: stored
+// 32 rows of 4 columns side by side.
 struct PartList {
     long long row;
     int step, count;
-    __device__ bool warps() const { return step >= 32; }
+    bool warps;
 };
-__device__ __forceinline__ PartList part_list(const CacheDev& c, const int4& of, bool own, int head, int t) {
-    const int group = own ? of.x : of.y;
-    if (own && of.w) return PartList{cache_own_rows(c) + (long long)t * c.Hq + head * c.rep, 1, 1};
-    if (group < 0) return PartList{0, 1, 0};
-    const int2 cut = c.cut[(size_t)group * c.Hkv + head];
-    const CacheGroup g = c.groups[group];
-    PartList l;
-    l.step = cache_part_rows(g.ntok, c.tile_tokens, c.rep);
-    l.count = cut.y;
-    const int in = t - g.row;
-    l.row = g.part_row + (long long)(head + cut.x) * l.step +
-            (in >= c.tile_tokens ? 128 + (in - c.tile_tokens) * c.rep : in * c.rep);
-    return l;
+__device__ __forceinline__ PartList item_parts(const CacheDev& c, int item, int head, int t) {
+    if (item < 0) return PartList{0, 0, 0, false};
+    const int2 cut = c.cut[(size_t)item * c.Hkv + head];
+    const CacheGroup g = c.groups[item];
+    const int rows = cache_part_rows(g.ntok, c.tile_tokens, c.rep), in = t - g.row;
+    return PartList{g.part_row + (long long)(head + cut.x) * rows +
+                        (in >= c.tile_tokens ? 128 + (in - c.tile_tokens) * c.rep : in * c.rep),
+                    rows, cut.y, rows >= 32};
+}
+__device__ __forceinline__ PartList own_parts(const CacheDev& c, const TokenParts& p, int head, int t) {
+    if (p.own_n) return PartList{p.own_row + (long long)head * p.own_n * c.rep, c.rep, p.own_n, false};
+    return item_parts(c, p.own_item, head, t);
+}
+__device__ __forceinline__ PartList common_parts(const CacheDev& c, const TokenParts& p, int head, int t) {
+    if (p.common_n) return PartList{p.common_row + (long long)head * p.common_n * p.common_step, p.common_step, p.common_n, false};
+    return item_parts(c, p.common_item, head, t);
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -324,7 +360,7 @@ __device__ __forceinline__ void add_parts(const CacheDev& c, const PartList (&pa
             const int k = min(k0 + i, n - 1);
             const bool second = k >= p0.count;
             const long long at = (second ? p1.row + (long long)(k - p0.count) * p1.step : p0.row + (long long)k * p0.step) + row;
-            const bool warps = second ? p1.warps() : p0.warps();
+            const bool warps = second ? p1.warps : p0.warps;
             const float* src = c.part_o + (warps ? (at & ~31LL) * DH + (at & 31) * 4 + col * 32 : at * DH + col);
             ml[i] = __ldcg(c.part_ml + at);
             x[i] = __ldcg(reinterpret_cast<const float4*>(src));

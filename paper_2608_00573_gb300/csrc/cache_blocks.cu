@@ -29,7 +29,7 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         cudaError_t e = cudaSuccess;
         size_t had = c->allocs.size();
         try {
-            c->allocs.reserve(had + 8);
+            c->allocs.reserve(had + 9);
         } catch (const std::bad_alloc&) {
             return c->fail(TRIMMOE_ERR_OOM, "cache_share", "host allocation failed");
         }
@@ -45,7 +45,8 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         alloc(d.plan, 1);
         alloc(d.shares, (size_t)d.num_sms);
         alloc(d.groups, (size_t)cache_share_groups(d));
-        alloc(d.items_of, (size_t)kShareRows);
+        alloc(d.parts_of, (size_t)kShareRows / d.Hq + 1);
+        alloc(d.pieces, (size_t)kPieces);
         alloc(d.common, (size_t)d.max_seqs);
         alloc(d.cut, (size_t)cache_share_groups(d) * d.Hkv);
         alloc(d.part_ml, rows);
@@ -60,11 +61,11 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
     }
     c->share.shared = 1;
     // Single tokens: up to 16 query heads of a key/value head are a tile of the kernel that reads
-    // sequences' own pages.
+    // pieces.
     c->own = launch_cache_own;
     c->join = launch_cache_join;
-    c->own_splits = c->max_q == 1 && c->d.rep <= 16 ? cache_blocks_splits(c->d, (long long)c->T * c->d.Hkv, 1 << 20) : 0;
-    const trimmoe_status s = c->launched(launch_cache_share(c->share, n, counts, c->n, c->T, c->own_splits, st), 2, "cache_share");
+    c->single = c->max_q == 1 && c->d.rep <= 16;
+    const trimmoe_status s = c->launched(launch_cache_share(c->share, n, counts, c->n, c->T, c->single, st), 2, "cache_share");
     // (Without its list a step cannot be attended.)
     if (s != TRIMMOE_OK) c->T = -1;
     else c->d.shared = 1;

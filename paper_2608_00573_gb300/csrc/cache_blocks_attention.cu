@@ -46,7 +46,7 @@ struct Item {
     int t, head, row0, rows;   // token, key/value head, query heads of it
     int base, kv_len, pos;
     int g0, g1;                // stages
-    int part;                  // OWN: there are common tiles
+    int part;                  // OWN: row of its part, -1: it is the result
 };
 
 template <int DH>
@@ -68,6 +68,7 @@ struct __align__(128) Shared {
     uint64_t full[8], empty[8], q_full, q_empty;
     int first[8][4];           // of the stage's pages: first position, kHidden or kWhole
     Item item;
+    CachePlan plan;
     int abort_flag, never;
 };
 
@@ -88,10 +89,9 @@ __device__ __forceinline__ bool readers_any(bool x) {
     return r != 0;
 }
 
-// OWN: no lists; the token's sequence from its group's common tiles on.  The sums are a part beside those of the
-// common tiles, or the result when there are none.  This kernel runs beside the attention kernel
-// before it, which lets it start when all that comes before has ended, and waits for that kernel
-// only at its own end.
+// OWN: no lists; an item is a piece (cache_share.cu) of a key/value head, whose sums are a part, or the result when it
+// is its token's only one.  This kernel runs beside the attention kernel before it, which lets it start
+// when all that comes before has ended, and waits for that kernel only at its own end.
 template <int DH, bool OWN>
 __global__ void __launch_bounds__(kThreads)
 cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -115,13 +115,29 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         fence_barrier_init();
         prefetch_tmap(&tm_k);
         prefetch_tmap(&tm_v);
+        if (!OWN) pdl_wait();
+        sh.plan = from_l2(c.plan);                     // (once: the number drawn grows meanwhile, and all have to agree on it)
     }
     __syncthreads();
     if (!OWN) pdl_wait();
     pdl_trigger();
-    const CachePlan pl = *c.plan;
-    if (!pl.ok || (OWN && (!pl.own_apart || share_stale(c, pl)))) {     // (all CTAs)
+    const CachePlan pl = sh.plan;
+    const int items = OWN ? pl.pieces * c.Hkv : p.T * c.Hkv * p.row_tiles;
+    if (!pl.ok || (OWN && share_stale(c, pl))) {       // (all CTAs)
         if (OWN) pdl_wait();
+        return;
+    }
+    // The last CTA to finish drawing leaves the counter at zero for the next call.
+    auto drawn_all = [&] {
+        __threadfence();
+        if (atomicAdd(&c.plan->done, 1) == (int)gridDim.x - 1) {
+            c.plan->drawn = 0;
+            c.plan->done = 0;
+        }
+    };
+    if (OWN && pl.drawn >= items) {                    // (a CTA that began late)
+        if (threadIdx.x == 0) drawn_all();
+        pdl_wait();
         return;
     }
     if (sb & 1023u) {
@@ -134,11 +150,10 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     const int page_boxes = c.page > kStageKeys ? c.page / kStageKeys : 1;     // boxes of a page's rows (pages of 128: two)
     const int per_stage = max(1, kStageKeys >> c.page_shift), box_rows = kStageKeys / per_stage;
-    const int items = p.T * c.Hkv * p.row_tiles;
     // Four columns of a row: its sums (ml: maximum and sum of p) as a part, or the result.
     auto put = [&](const Item& it, __nv_bfloat16* out, int row, int col, float2 ml, float4 x) {
-        if (OWN && it.part) {
-            const long long at = cache_own_rows(c) + (long long)it.t * c.Hq + it.head * c.rep + row;
+        if (OWN && it.part >= 0) {
+            const long long at = it.part + row;
             *reinterpret_cast<float4*>(c.part_o + at * DH + col) = x;
             if (col == 0) c.part_ml[at] = ml;
         } else {
@@ -150,6 +165,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (warp == kReaders) {
         // ------------------------------------------------------------ items and loads
         uint32_t issued = 0, n_items = 0;
+        const long long piece_end = cache_piece_rows(c) + 3LL * kShareRows - 16;
         bool ok = true;
         // OWN: all items are drawn (CTAs on the attention kernel's SMs begin when it has ended), else each CTA has
         // its first one.
@@ -165,33 +181,54 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             if (splits == 1 && lane == 0) drawn = given + atomicAdd(&c.plan->drawn, 1);
             Item it;
             it.valid = 1;
-            const int per = c.Hkv * p.row_tiles;
-            it.t = index / per;
-            it.head = index % per / p.row_tiles;
-            it.row0 = index % p.row_tiles * 16;
-            it.rows = min(16, c.rep - it.row0);
-            const CacheToken tok = c.tokens[it.t];
-            it.base = tok.base;
-            it.kv_len = tok.kv_len;
-            it.pos = tok.pos;
-            int listed = 0, first_own = 0;             // entries of the list that count, first page of the step's own
-            it.part = 0;
+            int listed = 0, first_own = 0;             // entries of the list that count, first page of the step's own (OWN: of the piece)
+            int seq;
+            bool all_seen = false;
             if (OWN) {
-                const int4 of = c.items_of[it.t];
-                first_own = of.z;
-                it.part = of.y >= 0;
+                const CachePiece pc = from_l2(c.pieces + index / c.Hkv);
+                it.head = index % c.Hkv;
+                it.t = pc.tok;
+                it.row0 = 0;
+                it.rows = pc.rows;
+                it.kv_len = pc.kv_len;
+                it.base = it.pos = pc.kv_len - 1;
+                it.g0 = pc.g0;
+                it.g1 = pc.g1;
+                it.part = pc.part_row < 0 ? -1 : pc.part_row + it.head * pc.head_step;
+                first_own = pc.first_page;
+                seq = pc.seq;
+                all_seen = pc.whole;
+                // (Whatever it is, it names nothing that is not there.)
+                if (it.rows < 1 || it.rows > 16 || it.t < 0 || it.t + (it.rows - 1) / c.rep >= p.T || it.g0 < 0 ||
+                    it.g1 > (c.max_pages << c.page_shift) / kStageKeys + 1 || seq < 0 || seq >= c.max_seqs || first_own < 0 ||
+                    pc.part_row < -1 || it.part >= piece_end) {
+                    if (lane == 0) atomicCAS(c.err, 0, ERR_CACHE_STATE);
+                    index = __shfl_sync(0xffffffffu, drawn, 0);
+                    continue;
+                }
             } else {
+                const int per = c.Hkv * p.row_tiles;
+                it.t = index / per;
+                it.head = index % per / p.row_tiles;
+                it.row0 = index % p.row_tiles * 16;
+                it.rows = min(16, c.rep - it.row0);
+                const CacheToken tok = c.tokens[it.t];
+                it.base = tok.base;
+                it.kv_len = tok.kv_len;
+                it.pos = tok.pos;
+                it.part = -1;
+                seq = tok.seq;
                 first_own = it.base >> c.page_shift;
                 listed = min(p.n, first_own);
+                const int last = p.tree ? it.kv_len - 1 : it.pos;
+                const int boxes = (listed + (last >> c.page_shift) - first_own + 1) * page_boxes;
+                const int stages = (boxes + per_stage - 1) / per_stage;
+                it.g0 = (int)((long long)stages * rank / splits);
+                it.g1 = (int)((long long)stages * (rank + 1) / splits);
             }
-            const int last = p.tree ? it.kv_len - 1 : it.pos;
-            const int boxes = (listed + (last >> c.page_shift) - first_own + 1) * page_boxes;
-            const int stages = (boxes + per_stage - 1) / per_stage;
-            it.g0 = (int)((long long)stages * rank / splits);
-            it.g1 = (int)((long long)stages * (rank + 1) / splits);
             // Lane i looks up box i of 32, the next 32 while these are copied.
             const int* list = p.blocks + ((size_t)it.t * c.Hkv + it.head) * p.n;
-            const int* row = c.table + (size_t)tok.seq * c.max_pages;
+            const int* row = c.table + (size_t)seq * c.max_pages;
             const int boxes_end = it.g1 * per_stage;
             struct Box {
                 int id, first;                         // page, first position (kWhole, kHidden)
@@ -216,12 +253,12 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                     if (col >= c.max_pages || (col << c.page_shift) >= it.kv_len) fits = false;
                 }
                 if (!fits) return x;
-                x.id = row[col];
+                x.id = OWN ? __ldcg(row + col) : row[col];
                 if (x.id < 0 || x.id >= c.n_pages) {
                     atomicCAS(c.err, 0, ERR_CACHE_STATE);
                     return x;
                 }
-                x.first = j < listed ? kWhole : (col << c.page_shift) + sub * box_rows;
+                x.first = j < listed || all_seen ? kWhole : (col << c.page_shift) + sub * box_rows;
                 return x;
             };
             int b0 = it.g0 * per_stage;
@@ -229,12 +266,16 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             // The readers have taken what was said of the item before, and its queries.
             if (n_items) ok = !wait(&sh.q_empty, n_items - 1);
             if (!ok) break;
+            // (A piece of common pages has several tokens' queries.)
+            const int q_rows = OWN ? c.rep : it.rows;
             if (lane == 0) {
                 sh.item = it;
-                const uint32_t bytes = (uint32_t)it.rows * DH * 2;
-                mbar_arrive_expect_tx(smem_u32(&sh.q_full), bytes);
-                bulk_load(smem_u32(sh.q), p.q + (size_t)it.t * p.ld_q + (size_t)(it.head * c.rep + it.row0) * DH, bytes, smem_u32(&sh.q_full));
+                mbar_arrive_expect_tx(smem_u32(&sh.q_full), (uint32_t)it.rows * DH * 2);
             }
+            __syncwarp();
+            if (lane * q_rows < it.rows)
+                bulk_load(smem_u32(sh.q[lane * q_rows]), p.q + (size_t)(it.t + lane) * p.ld_q + (size_t)(it.head * c.rep + it.row0) * DH,
+                          (uint32_t)q_rows * DH * 2, smem_u32(&sh.q_full));
             __syncwarp();
             ++n_items;
             for (int g = it.g0; g < it.g1; ++g) {
@@ -266,14 +307,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             }
             index = __shfl_sync(0xffffffffu, drawn, 0);
         }
-        // The last CTA to finish drawing leaves the counter at zero for the next call.
-        if (splits == 1 && lane == 0) {
-            __threadfence();
-            if (atomicAdd(&c.plan->done, 1) == (int)gridDim.x - 1) {
-                c.plan->drawn = 0;
-                c.plan->done = 0;
-            }
-        }
+        if (splits == 1 && lane == 0) drawn_all();
         if (ok && n_items) ok = !wait(&sh.q_empty, n_items - 1);
         if (ok && lane == 0) {
             sh.item.valid = 0;
@@ -312,7 +346,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.q_empty));
-            const uint64_t tree = p.tree ? __ldg(p.tree + it.t) : 0;
+            const uint64_t tree = p.tree ? __ldcg(p.tree + it.t) : 0;
             const bool two = it.rows > 8;              // the tile's lower half has rows
             float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};   // rows lane / 4 and lane / 4 + 8
             float o[DH / 8][4];
@@ -510,7 +544,9 @@ cudaError_t blocks_launch(const CacheDev& c, const CUtensorMap& tm_k, const CUte
     if (e != cudaSuccess) return e;
     const long long items = (long long)p.T * c.Hkv * p.row_tiles;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.splits == 1 ? std::min<long long>(items, 2LL * c.num_sms) : items * p.splits));
+    cfg.gridDim = dim3((unsigned)(OWN              ? 2LL * c.num_sms
+                                  : p.splits == 1 ? std::min<long long>(items, 2LL * c.num_sms)
+                                                  : items * p.splits));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

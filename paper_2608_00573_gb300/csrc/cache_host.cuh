@@ -24,11 +24,11 @@ struct trimmoe_cache {
     cudaStream_t last_stream = nullptr;
     uint64_t launches = 0;
     int T = -1, n = 0, max_q = 0;             // the current step (T < 0: none)
-    // With groups of sequences: what attend launches beside the attention kernel for single tokens, CTAs per
-    // item (0: nothing), and what it launches behind both (set by cache_share).
+    // With groups of sequences: what attend launches beside the attention kernel for single tokens and what
+    // behind both (set by cache_share).
     cudaError_t (*own)(const CacheDev&, const CUtensorMap&, const CUtensorMap&, const BlocksParams&, cudaStream_t) = nullptr;
     cudaError_t (*join)(const CacheDev&, const AttendParams&, cudaStream_t) = nullptr;
-    int own_splits = 0;
+    bool single = false;
     float theta = 0.f;                        // base of turn[]
     uint64_t turn[64];
 

@@ -120,10 +120,10 @@ __device__ V block_sum(V v, V* ws, V& total) {
 template <int N>
 __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_constant__ CacheDev c,
                                                                    const __grid_constant__ CacheList<N> l, int n_seqs, int T,
-                                                                   int splits) {
-    __shared__ int s_max;
+                                                                   int single) {
     __shared__ int s_common[kCacheMaxSeqs], s_begin[kCacheMaxSeqs + 1], s_own[kCacheMaxSeqs + 1];   // first items of groups, sequences
     __shared__ int s_of[kCacheMaxSeqs];                // a sequence's group
+    __shared__ int s_row[kCacheMaxSeqs], s_cuts[kCacheMaxSeqs];        // pieces of small groups: parts' first row, cuts
     __shared__ int s_wi[33];
     __shared__ long long s_wl[33];
     const int i = threadIdx.x, n = l.n, TT = c.tile_tokens;
@@ -138,7 +138,6 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         return;
     }
     int tiles = 0, count = 0;
-    if (i == 0) s_max = 0;
     if (i < n) {
         tiles = c.common[i];
         for (int k = l.a[i]; k < l.a[i] + l.b[i]; ++k) s_of[k] = i;
@@ -148,33 +147,83 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         const CacheSeq a = c.seqs[l.a[i]], z = c.seqs[l.a[i] + l.b[i] - 1];
         tok = z.q_off + z.q_len - a.q_off;
     }
-    bool apart = splits > 0;
-    long long own_stages = 0;
-    if (apart) {
-        // Single tokens: what sharing saves is read from L2 otherwise, at twice HBM's rate and
-        // more, and the second kernel alone has less to wait for.
+    CacheSeq mine = {};
+    if (i < n_seqs) mine = c.seqs[i];
+    int pieces = 0;
+    float piece_bytes = 0.f;
+    if (single) {
+        // Groups whose rows fill at most two tiles of 16 are read in pieces, as sequences' own pages are; for
+        // larger ones the 128-row tiles of the attention kernel read common pages.  Where those
+        // save little, each sequence reads them itself: from L2, and nothing has to be waited for.
+        const int per = 16 / c.rep, row_tiles = (tok + per - 1) / per;
+        const bool small = row_tiles <= 2;
         long long saved;
-        block_sum((long long)tiles * max(0, tok - 1), s_wl, saved);
-        if (saved * kCacheTile * c.Hkv * c.dh * 4 < kShareBytes) tiles = 0;
+        block_sum(small ? 0LL : (long long)tiles * (tok - 1), s_wl, saved);
+        if (!small && saved * kCacheTile * c.Hkv * c.dh * 4 < kShareBytes) tiles = 0;
+        if (i < n) s_common[i] = tiles;
+        __syncthreads();
+        // Stages of 64 positions of one head; a piece has as many as give each of two CTAs an SM three pieces,
+        // but few enough not to be a long wait, and a sequence not more than kPieceCuts of them.
+        const int common = small ? tiles * (kCacheTile / 64) : 0;
+        const int own = mine.q_len ? (mine.kv_len - s_common[s_of[i]] * kCacheTile + 63) / 64 : 0;
+        long long all;
+        block_sum((long long)common * row_tiles + own, s_wl, all);
+        piece_bytes = (float)all * c.Hkv * (64 * 4) * c.dh;
+        const int share = (int)(all * c.Hkv / (2 * c.num_sms)) + 1;
+        const int most = share < 6 ? max(2, share) : max(4, (share + 2) / 3);
+        auto cuts_of = [&](int stages) { return min(kPieceCuts, (stages + most - 1) / most); };
+        const int common_cuts = cuts_of(common), own_cuts = cuts_of(own);
+        int n_group, n_own;
+        const int first_group = block_sum(common_cuts * row_tiles, s_wi, n_group);
+        const int first_own = n_group + block_sum(own_cuts, s_wi, n_own);
+        pieces = n_group + n_own;
+        int row, rows = common_cuts * c.Hkv * tok * c.rep, all_rows;
+        row = block_sum(rows + own_cuts * c.Hkv * c.rep, s_wi, all_rows) + (int)cache_piece_rows(c);
+        if (i < n) {
+            s_row[i] = row;
+            s_cuts[i] = common_cuts;
+        }
+        if (common_cuts) {
+            // (Any of the group's sequences with new tokens; their table rows agree.)
+            int lead = l.a[i];
+            while (c.seqs[lead].q_len == 0) ++lead;
+            const CacheSeq s = c.seqs[lead];
+            for (int x = 0; x < common_cuts * row_tiles; ++x) {
+                const int cut = x % common_cuts, tile = x / common_cuts;
+                c.pieces[first_group + x] = CachePiece{s.seq, s.q_off + tile * per, min(per, tok - tile * per) * c.rep, 1,
+                                                       common * cut / common_cuts, common * (cut + 1) / common_cuts, 0, tiles * kCacheTile,
+                                                       row + (cut * tok + tile * per) * c.rep, common_cuts * tok * c.rep, {0, 0}};
+            }
+        }
+        __syncthreads();
+        if (own_cuts) {
+            const int g = s_of[i], from = s_common[g] * kCacheTile >> c.page_shift;
+            const int first = row + rows;
+            const bool direct = own_cuts == 1 && !s_common[g];
+            for (int x = 0; x < own_cuts; ++x)
+                c.pieces[first_own + x] = CachePiece{mine.seq, mine.q_off, c.rep, 0, (int)((long long)own * x / own_cuts),
+                                                     (int)((long long)own * (x + 1) / own_cuts), from, mine.kv_len,
+                                                     direct ? -1 : first + x * c.rep, own_cuts * c.rep, {0, 0}};
+            TokenParts p = {};
+            p.own_row = first;
+            p.own_n = own_cuts;
+            p.own_item = p.common_item = -1;
+            if (s_cuts[g]) {
+                p.common_row = s_row[g] + (mine.q_off - c.seqs[l.a[g]].q_off) * c.rep;
+                p.common_n = s_cuts[g];
+                p.common_step = (c.seqs[l.a[g] + l.b[g] - 1].q_off + c.seqs[l.a[g] + l.b[g] - 1].q_len - c.seqs[l.a[g]].q_off) * c.rep;
+            }
+            c.parts_of[mine.q_off] = p;
+        }
+        __syncthreads();
+        if (small) tiles = 0;                          // (from here on: what is on the line)
     }
     if (i < n) s_common[i] = tiles;
     __syncthreads();
-    CacheSeq mine = {};
-    if (i < n_seqs) mine = c.seqs[i];
-    if (apart) {
-        // The second kernel's CTAs take whole sequences, cut in `splits`: unless a few are far longer
-        // than the others.
-        const int stages = i < n_seqs && mine.q_len ? (mine.kv_len - s_common[s_of[i]] * kCacheTile + 63) / 64 : 0;
-        if (stages) atomicMax(&s_max, stages);
-        long long sum;
-        block_sum((long long)stages, s_wl, sum);
-        apart = (long long)s_max / splits <= sum * c.Hkv / c.num_sms + 16;
-        own_stages = sum;
-    }
     if (tiles) count = (tok + 2 * TT - 1) / (2 * TT);
     int n_common, n_own;
     const int at = block_sum(count, s_wi, n_common);
-    const int own = block_sum(apart ? 0 : (mine.q_len + 2 * TT - 1) / (2 * TT), s_wi, n_own);
+    const int own = block_sum(single ? 0 : (mine.q_len + 2 * TT - 1) / (2 * TT), s_wi, n_own);
     if (i < n) {
         s_begin[i] = at;
     }
@@ -236,11 +285,11 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     two = __syncthreads_or(two);
     W *= c.Hkv;
     int n_ctas = !W ? 0 : (int)max(1LL, min((long long)c.num_sms, W / (kMinTiles * share_tile(two ? 1 : 0))));
-    if (apart && n_ctas) {
-        // The second kernel's CTAs read sequences' own pages beside this one's: as many SMs as let both end
-        // together, in us (a CTA begins and ends in 6, and its tiles take 1.3 times as long beside
-        // the other kernel's traffic; own pages at HBM's rate).
-        const float a = W * (1.3f * kShareUnit), b = own_stages * (64.f * 4.f / 6.5e6f) * c.Hkv * c.dh * c.num_sms;
+    if (single && n_ctas) {
+        // The second kernel's CTAs read pieces beside this one's: as many SMs as let both end together, in us (a CTA
+        // begins and ends in 6, and its tiles take 1.6 times as long beside the other kernel's
+        // traffic; pieces at HBM's rate).
+        const float a = W * (1.6f * kShareUnit), b = piece_bytes / 6.5e6f * c.num_sms;
         const float t = max(12.f, (a + b) / c.num_sms + 4.f);
         n_ctas = min(n_ctas, (int)(a / (t - 6.f)) + 1);
     }
@@ -271,11 +320,12 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         const int tiles = share_tiles(cost, two_tiles);
         c.cut[k] = make_int2(first, cache_cta_of(start + (long long)(tiles - 1) * step, W, n_ctas) - first + 1);
     }
-    if (i == 0) *c.plan = CachePlan{W, items, n_ctas, 0, 1, 0, 0, apart, c.step_plan->serial};
+    if (i == 0) *c.plan = CachePlan{W, items, n_ctas, 0, 1, 0, 0, pieces, c.step_plan->serial};
     for (int t = i; t < T; t += kPlanThreads) {
         const int k = c.owner[t], g = s_of[k], from = c.seqs[l.a[g]].q_off;
-        c.items_of[t] = make_int4(apart ? -1 : s_own[k] + (t - c.seqs[k].q_off) / (2 * TT),
-                                  s_common[g] ? s_begin[g] + (t - from) / (2 * TT) : -1, s_common[g] * kCacheTile >> c.page_shift, apart);
+        const int item = s_common[g] ? s_begin[g] + (t - from) / (2 * TT) : -1;
+        if (single) c.parts_of[t].common_item = item;
+        else c.parts_of[t] = TokenParts{0, 0, s_own[k] + (t - c.seqs[k].q_off) / (2 * TT), 0, 0, 0, item, 0};
     }
     __syncthreads();
     for (int b = i; b < n_ctas; b += kPlanThreads) {
@@ -319,11 +369,12 @@ __global__ void __launch_bounds__(256, 4) cache_join_shared_kernel(const __grid_
     pdl_trigger();
     const CachePlan pl = *c.plan;
     if (!pl.ok || share_stale(c, pl)) return;          // (a refused step has written no items)
-    // A token whose only source is its own pages has its result already.
-    if (pl.own_apart && c.items_of[t].y < 0) return;
+    // A token whose only part is one piece has its result already.
+    const TokenParts of = c.parts_of[t];
+    if (of.own_n == 1 && !of.common_n && of.common_item < 0) return;
     if (threadIdx.x < 2 * heads) {
         const int k = threadIdx.x >> 1, own = threadIdx.x & 1;
-        s_parts[k][own] = part_list(c, c.items_of[t], own, head0 + k, t);
+        s_parts[k][own] = own ? own_parts(c, of, head0 + k, t) : common_parts(c, of, head0 + k, t);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < heads * c.rep * (DH / 4); e += 256) {
@@ -337,7 +388,7 @@ __global__ void __launch_bounds__(256, 4) cache_join_shared_kernel(const __grid_
 }
 
 template <int N>
-cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st) {
+cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int single, cudaStream_t st) {
     CacheList<N> l;
     l.n = n;
     int at = 0;
@@ -348,14 +399,14 @@ cudaError_t share_launch(const CacheDev& c, int n, const int* counts, int n_seqs
     }
     const cudaError_t e = launch_pdl(cache_common_kernel<N>, dim3((unsigned)n), dim3(kCommonThreads), 0, st, c, l);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_share_kernel<N>, dim3(1), dim3(kPlanThreads), 0, st, c, l, n_seqs, T, splits);
+    return launch_pdl(cache_share_kernel<N>, dim3(1), dim3(kPlanThreads), 0, st, c, l, n_seqs, T, single);
 }
 
 }  // namespace
 
-cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int splits, cudaStream_t st) {
-    return n <= 64 ? share_launch<64>(c, n, counts, n_seqs, T, splits, st)
-                   : share_launch<kCacheMaxSeqs>(c, n, counts, n_seqs, T, splits, st);
+cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int n_seqs, int T, int single, cudaStream_t st) {
+    return n <= 64 ? share_launch<64>(c, n, counts, n_seqs, T, single, st)
+                   : share_launch<kCacheMaxSeqs>(c, n, counts, n_seqs, T, single, st);
 }
 
 cudaError_t launch_cache_join(const CacheDev& c, const AttendParams& p, cudaStream_t st) {

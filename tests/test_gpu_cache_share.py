@@ -64,6 +64,12 @@ CASES = {
     "heads_128": ((128, 1, 64), 64, [260], [4], 10, lambda s: 1),
     "no_groups": ((8, 2, 128), 64, [300, 5, 128, 1000], [1, 1, 1, 1], 7, lambda s: 1 + s),
     "large_groups": ((4, 4, 128), 64, [2000], [300], 100, lambda s: 1),
+    "small_groups": ((8, 2, 128), 16, [1500, 300, 4000, 130], [4, 8, 3, 9], 300, lambda s: 1),
+    "small_and_large": ((12, 12, 64), 32, [5000, 2000, 700], [50, 16, 31], 900, lambda s: 1),
+    "one_far_longer": ((4, 2, 128), 64, [200, 20000], [5, 1], 30, lambda s: 1),
+    "heads_3": ((9, 3, 64), 128, [700, 500], [4, 11], 200, lambda s: 1),
+    "heads_16": ((16, 1, 128), 64, [2500, 400], [2, 3], 70, lambda s: 1),
+    "many_sequences": ((4, 2, 64), 16, [300, 130] * 30, [5, 12] * 30, 60, lambda s: int(s % 7 != 0)),
     "all_idle_but_one": ((8, 2, 128), 64, [700], [4], 50, lambda s: int(s == 2)),
     "first_idle": ((8, 2, 128), 64, [700, 400], [4, 3], 50, lambda s: int(s not in (0, 1, 4))),
 }
