@@ -272,8 +272,9 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
         return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "scale must be finite and >= 0");
     if (a->tree && c->max_q > kTreeMax)
         return c->fail(TRIMMOE_ERR_ARG, "cache_attend", "a tree has at most 64 tokens per sequence");
+    const bool single = d.shared && c->single, alone = single && c->small;
     CUtensorMap tm_q;
-    if (!query_map(&tm_q, a->q, d, c->T, a->ld_q))
+    if (!alone && !query_map(&tm_q, a->q, d, c->T, a->ld_q))
         return c->fail(TRIMMOE_ERR_CUDA, "cache_attend", "cuTensorMapEncodeTiled failed");
     AttendParams p = {};
     p.tree = a->tree;
@@ -283,12 +284,12 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
     const int max_rows = c->max_q > d.tile_tokens ? 2 * kCacheTile : c->max_q * d.rep;
     p.join_here = !d.shared && max_rows <= kJoinHereRows;
     p.T = c->T;
-    p.single = d.shared && c->single;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_attend");
     cudaStream_t st = enter(c, stream);
-    cudaError_t e = launch_cache_attend(d.shared ? c->share : d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows, st);
-    if (e == cudaSuccess && p.single) {
+    cudaError_t e = cudaSuccess;
+    if (!alone) e = launch_cache_attend(d.shared ? c->share : d, tm_q, c->tm_k[layer], c->tm_v[layer], p, max_rows, st);
+    if (e == cudaSuccess && single) {
         BlocksParams b = {};
         b.q = static_cast<const __nv_bfloat16*>(a->q);
         b.out = p.out;
@@ -298,12 +299,13 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
         b.T = p.T;
         b.row_tiles = 1;
         b.splits = 1;
+        b.alone = alone;
         b.scale_log2 = p.scale_log2;
         const bool large = d.page > 64;
         e = c->own(c->share, large ? c->tm_k64[layer] : c->tm_k[layer], large ? c->tm_v64[layer] : c->tm_v[layer], b, st);
     }
     if (e == cudaSuccess && d.shared) e = c->join(c->share, p, st);
-    return c->launched(e, (p.join_here ? 1 : 2) + p.single, "cache_attend");
+    return c->launched(e, (p.join_here || alone ? 1 : 2) + single, "cache_attend");
 }
 
 extern "C" trimmoe_status trimmoe_cache_fork(trimmoe_cache_handle c, int n, const int32_t* src, const int32_t* dst,

@@ -94,7 +94,7 @@ struct __align__(16) CachePiece {
     int pad[2];
 };
 constexpr int kPieceCuts = 24;         // of one sequence's or group's pages at most
-constexpr int kPieces = 8192;          // 1024 tokens', 512 groups' two and 3 CTAs' shares more, with room to spare
+constexpr int kPieces = 8192;          // 1024 tokens', 512 groups' two and 5 times two CTAs an SM more, with room to spare
 
 // Where a token's parts are: pieces of its own pages and of common ones (rows of the first query head of the
 // first key/value head, and how many), or items of the line (-1: none).
@@ -199,7 +199,6 @@ struct AttendParams {
     int join_here;                     // the attention kernel joins cut items itself
     float scale_log2;
     int T;
-    int single;                        // with groups of sequences: each has one new token at most
 };
 
 // attend_blocks: q and out as for attend.
@@ -211,6 +210,7 @@ struct BlocksParams {
     int ld_q, ld_out, T, n;
     int row_tiles;                     // of 16 query heads of a key/value head
     int splits;                        // CTAs of an item
+    int alone;                         // pieces: there is no attention kernel to run beside
     float scale_log2;
 };
 
@@ -226,6 +226,10 @@ inline size_t cache_score_keys(const CacheDev& c) {
     const size_t row = (((size_t)c.max_pages + 3) & ~size_t(3)) * c.Hkv;
     return std::max(row, std::min(row * c.T_max, (size_t)8 << 20));
 }
+
+// Steps of single tokens with groups of sequences: groups with at most this many tiles of 16 rows are small.
+constexpr int kSmallTiles = 2;
+__host__ __device__ inline int small_tiles(int tokens, int rep) { return (tokens + 16 / rep - 1) / (16 / rep); }
 
 // Steps with groups of sequences: rows (tokens times query heads) at most, and what that allows.
 constexpr int kShareRows = 65536;

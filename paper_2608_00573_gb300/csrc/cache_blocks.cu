@@ -12,7 +12,9 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
     if (n < 0 || n > c->n) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "n out of range");
     if (n > 0 && !counts) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "NULL argument");
     long long sum = 0;
+    int most = 0;
     for (int i = 0; i < n; ++i) {
+        most = std::max(most, counts[i]);
         if (counts[i] < 1) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "counts must be >= 1");
         sum += counts[i];
     }
@@ -65,6 +67,7 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
     c->own = launch_cache_own;
     c->join = launch_cache_join;
     c->single = c->max_q == 1 && c->d.rep <= 16;
+    c->small = c->single && small_tiles(most, c->d.rep) <= kSmallTiles;
     const trimmoe_status s = c->launched(launch_cache_share(c->share, n, counts, c->n, c->T, c->single, st), 2, "cache_share");
     // (Without its list a step cannot be attended.)
     if (s != TRIMMOE_OK) c->T = -1;

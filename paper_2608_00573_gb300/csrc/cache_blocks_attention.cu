@@ -69,6 +69,7 @@ struct __align__(128) Shared {
     int first[8][4];           // of the stage's pages: first position, kHidden or kWhole
     Item item;
     CachePlan plan;
+    int first_item;
     int abort_flag, never;
 };
 
@@ -91,7 +92,8 @@ __device__ __forceinline__ bool readers_any(bool x) {
 
 // OWN: no lists; an item is a piece (cache_share.cu) of a key/value head, whose sums are a part, or the result when it
 // is its token's only one.  This kernel runs beside the attention kernel before it, which lets it start
-// when all that comes before has ended, and waits for that kernel only at its own end.
+// when all that comes before has ended, and waits for that kernel only at its own end (alone: all groups are
+// small, and there is no such kernel).
 template <int DH, bool OWN>
 __global__ void __launch_bounds__(kThreads)
 cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -115,11 +117,13 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         fence_barrier_init();
         prefetch_tmap(&tm_k);
         prefetch_tmap(&tm_v);
-        if (!OWN) pdl_wait();
-        sh.plan = from_l2(c.plan);                     // (once: the number drawn grows meanwhile, and all have to agree on it)
+        if (!OWN || p.alone) pdl_wait();
+        // (All have to agree on the plan, whose counters change, and on the first item, so they are read once.)
+        sh.first_item = OWN ? atomicAdd(&c.plan->drawn, 1) : 0;
+        sh.plan = from_l2(c.plan);
     }
     __syncthreads();
-    if (!OWN) pdl_wait();
+    if (!OWN || p.alone) pdl_wait();
     pdl_trigger();
     const CachePlan pl = sh.plan;
     const int items = OWN ? pl.pieces * c.Hkv : p.T * c.Hkv * p.row_tiles;
@@ -135,7 +139,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             c.plan->done = 0;
         }
     };
-    if (OWN && pl.drawn >= items) {                    // (a CTA that began late)
+    if (OWN && sh.first_item >= items) {               // (a CTA that began late)
         if (threadIdx.x == 0) drawn_all();
         pdl_wait();
         return;
@@ -171,10 +175,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         // its first one.
         int index = blockIdx.x / splits;
         const int given = OWN ? 0 : (int)gridDim.x;
-        if (OWN && splits == 1) {
-            if (lane == 0) index = atomicAdd(&c.plan->drawn, 1);
-            index = __shfl_sync(0xffffffffu, index, 0);
-        }
+        if (OWN) index = sh.first_item;
         while (ok && index < items) {
             // The next item (single CTAs; clusters have one each).
             int drawn = items;

@@ -28,7 +28,7 @@ struct trimmoe_cache {
     // behind both (set by cache_share).
     cudaError_t (*own)(const CacheDev&, const CUtensorMap&, const CUtensorMap&, const BlocksParams&, cudaStream_t) = nullptr;
     cudaError_t (*join)(const CacheDev&, const AttendParams&, cudaStream_t) = nullptr;
-    bool single = false;
+    bool single = false, small = false;       // groups of single tokens; and all of them small
     float theta = 0.f;                        // base of turn[]
     uint64_t turn[64];
 

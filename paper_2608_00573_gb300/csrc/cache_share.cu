@@ -152,11 +152,11 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     int pieces = 0;
     float piece_bytes = 0.f;
     if (single) {
-        // Groups whose rows fill at most two tiles of 16 are read in pieces, as sequences' own pages are; for
+        // Small groups' common pages are read in pieces, as sequences' own pages are; for
         // larger ones the 128-row tiles of the attention kernel read common pages.  Where those
         // save little, each sequence reads them itself: from L2, and nothing has to be waited for.
-        const int per = 16 / c.rep, row_tiles = (tok + per - 1) / per;
-        const bool small = row_tiles <= 2;
+        const int per = 16 / c.rep, row_tiles = small_tiles(tok, c.rep);
+        const bool small = row_tiles <= kSmallTiles;
         long long saved;
         block_sum(small ? 0LL : (long long)tiles * (tok - 1), s_wl, saved);
         if (!small && saved * kCacheTile * c.Hkv * c.dh * 4 < kShareBytes) tiles = 0;
@@ -359,8 +359,9 @@ inline __host__ __device__ int join_heads(const CacheDev& c) {
     const int n = 1024 / (c.rep * c.dh);
     return n < 1 ? 1 : n < kJoinHeads ? n : kJoinHeads;
 }
-template <int DH>
-__global__ void __launch_bounds__(256, 4) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
+// B: parts that a thread reads at a time; with few blocks of threads their latency is what counts.
+template <int DH, int B>
+__global__ void __launch_bounds__(256, B > 6 ? 2 : 4) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
                                                                    const __grid_constant__ AttendParams p) {
     __shared__ PartList s_parts[kJoinHeads][2];
     const int most = join_heads(c), blocks = (c.Hkv + most - 1) / most;
@@ -380,7 +381,7 @@ __global__ void __launch_bounds__(256, 4) cache_join_shared_kernel(const __grid_
     for (int e = threadIdx.x; e < heads * c.rep * (DH / 4); e += 256) {
         const int x = e / c.rep, k = x / (DH / 4), col = x % (DH / 4) * 4, row = e - x * c.rep;
         float top = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-        add_parts<DH, 6>(c, s_parts[k], row, col, top, l, a);
+        add_parts<DH, B>(c, s_parts[k], row, col, top, l, a);
         const float il = l == 0.f ? 0.f : 1.f / l;
         *reinterpret_cast<uint2*>(p.out + (size_t)t * p.ld_out + (size_t)((head0 + k) * c.rep + row) * DH + col) =
             make_uint2(pack_bf16x2(a[0] * il, a[1] * il), pack_bf16x2(a[2] * il, a[3] * il));
@@ -411,8 +412,12 @@ cudaError_t launch_cache_share(const CacheDev& c, int n, const int* counts, int 
 
 cudaError_t launch_cache_join(const CacheDev& c, const AttendParams& p, cudaStream_t st) {
     const dim3 grid((unsigned)(p.T * ((c.Hkv + join_heads(c) - 1) / join_heads(c))));
-    return c.dh == 64 ? launch_pdl(cache_join_shared_kernel<64>, grid, dim3(256), 0, st, c, p)
-                      : launch_pdl(cache_join_shared_kernel<128>, grid, dim3(256), 0, st, c, p);
+    const bool few = grid.x <= 2u * c.num_sms;
+    if (c.dh == 64)
+        return few ? launch_pdl(cache_join_shared_kernel<64, 12>, grid, dim3(256), 0, st, c, p)
+                   : launch_pdl(cache_join_shared_kernel<64, 6>, grid, dim3(256), 0, st, c, p);
+    return few ? launch_pdl(cache_join_shared_kernel<128, 12>, grid, dim3(256), 0, st, c, p)
+               : launch_pdl(cache_join_shared_kernel<128, 6>, grid, dim3(256), 0, st, c, p);
 }
 
 }  // namespace tmoe
