@@ -119,7 +119,7 @@ __host__ __device__ inline int cache_part_rows(int ntok, int tile_tokens, int re
 // sequences' own items are short, so this matters more than in other steps: with a tile and an end
 // alike, the last CTA of 12 drafted trees ended at 97 us, the others at 63.)
 constexpr float kShareUnit = 0.25f;
-__host__ __device__ inline int share_tile(int two) { return 5 + two; }
+__host__ __device__ inline int share_tile(int two) { return two ? 7 : 5; }
 constexpr int kShareEnds = 16;
 __host__ __device__ inline int share_tiles(int cost, int two) { return (cost - kShareEnds) / share_tile(two); }
 // Key tiles that the first x of an item's cost cover.
