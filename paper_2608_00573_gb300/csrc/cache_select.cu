@@ -702,7 +702,7 @@ cudaError_t select_launch(const CacheDev& c, const SelectParams& p, cudaStream_t
     // block; one to a block for few tokens of short sequences (one launch less: 312 blocks 7.7 us
     // instead of 8.6, and 3 us less on the host).
     if (p.max_q >= kTile && tile_bytes<kTile>(c) <= kTileBytes) return tile_launch<DH, M, kTile>(c, p, st, launches);
-    if (p.T * c.Hkv <= 64 && c.max_pages <= 1024 && tile_bytes<1>(c) <= kTileBytes) return tile_launch<DH, M, 1>(c, p, st, launches);
+    if ((long long)p.T * c.Hkv <= 64 && c.max_pages <= 1024 && tile_bytes<1>(c) <= kTileBytes) return tile_launch<DH, M, 1>(c, p, st, launches);
     // As many tokens at a time as the buffer has room for.
     const int most = (int)std::min<size_t>(std::min(p.T, kSlice), cache_score_keys(c) / (score_row(c) * c.Hkv));
     const int warps = score_warps(c);
