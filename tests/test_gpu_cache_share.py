@@ -114,6 +114,43 @@ def test_attend_shared_tree(shapes, page):
     assert cache.stats()["device_error"] == 0
 
 
+@pytest.mark.parametrize("shapes,sizes", [((8, 2, 128), [3, 1, 30]), ((12, 12, 64), [20, 2]), ((40, 2, 64), [3, 4])])
+def test_single_tokens_by_their_masks(shapes, sizes):
+    """A mask without the token's own bit shows it the positions before the step alone."""
+    n = sum(sizes)
+    cache, m, step, g = grouped(shapes, 16, [300] * len(sizes), sizes, [s % 40 for s in range(n)], slots=8)
+    q = [int(s != 1) for s in range(n)]
+    step(range(n), q)
+    fill(cache, m, g)
+    for s in range(n):                               # the new key and value may hold anything when nobody sees them
+        if q[s] and s % 3 == 0:
+            page, place = m.row(s, m.len[s] - 1)
+            cache.k[1, page, :, place] = float("nan")
+            cache.v[1, page, :, place] = float("inf")
+    words = [int(s % 3 != 0) | (s % 2) << 5 for s in range(n) if q[s]]
+    x = torch.randn((sum(q), shapes[0] * shapes[2]), generator=g, device=DEV).to(torch.bfloat16)
+    cache.share(sizes)
+    check_attend(cache, m, x, q, cache.attend(1, x, tree=torch.tensor(words, device=DEV)), 1, tree=words)
+    assert cache.stats()["device_error"] == 0
+
+
+def test_in_place_of_wider_rows_and_another_stream():
+    """Queries and results in rows of wider buffers; share and attend on another stream."""
+    cache, m, step, g = grouped((8, 2, 64), 32, [400, 90], [40, 3], [s % 70 for s in range(43)], slots=8)
+    step(range(43), [1] * 43)
+    fill(cache, m, g)
+    wide = torch.randn((43, 1024), generator=g, device=DEV).to(torch.bfloat16)
+    out = torch.full((43, 776), 5.0, device=DEV).bfloat16()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    cache.share([40, 3], stream=s)
+    cache.attend(0, wide[:, 256:768], out=out[:, 128:640], stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    check_attend(cache, m, wide[:, 256:768].contiguous(), [1] * 43, out[:, 128:640], 0)
+    assert (out[:, :128] == 5).all() and (out[:, 640:] == 5).all()
+    assert cache.stats()["device_error"] == 0
+
+
 def test_values_that_are_not_finite():
     """In the common part they reach every row that sees them, in masked places none."""
     cache, m, step, g = grouped((8, 2, 128), 32, [400], [5], [3, 40, 7, 0, 70])
