@@ -96,6 +96,12 @@ struct __align__(16) CachePiece {
 constexpr int kPieceCuts = 24;         // of one sequence's or group's pages at most
 constexpr int kPieces = 8192;          // 1024 tokens', 512 groups' two and 5 times two CTAs an SM more, with room to spare
 
+// Parts that hold a token: rows row + i * step, i < count, of query head 0 of a key/value head; warps: stored
+// 32 rows of 4 columns side by side.
+struct __align__(16) PartList {
+    int row, step, count, warps;
+};
+
 // Where a token's parts are: pieces of its own pages and of common ones (rows of the first query head of the
 // first key/value head, and how many), or items of the line (-1: none).
 struct __align__(16) TokenParts {
@@ -166,6 +172,7 @@ struct CacheDev {
     int shared;
     const CachePlan* step_plan;        // the step's own plan
     TokenParts* parts_of;              // [T]
+    PartList* lists;                   // [T][Hkv][2] where a token's parts are: common ones, own ones
     CachePiece* pieces;                // [kPieces]
     int* common;                       // [max_seqs] key tiles that a group of sequences has in common
     int2* cut;                         // [groups][Hkv] first CTA that holds tiles of an item, how many do
@@ -298,28 +305,21 @@ cudaError_t launch_cache_attend(const CacheDev& c, const CUtensorMap& tm_q, cons
 
 // Device helpers of the attention kernels.
 
-// Parts that hold a token: rows row + i * step, i < count, of query head 0 of a key/value head; warps: stored
-// 32 rows of 4 columns side by side.
-struct PartList {
-    long long row;
-    int step, count;
-    bool warps;
-};
 __device__ __forceinline__ PartList item_parts(const CacheDev& c, int item, int head, int t) {
-    if (item < 0) return PartList{0, 0, 0, false};
+    if (item < 0) return PartList{0, 0, 0, 0};
     const int2 cut = c.cut[(size_t)item * c.Hkv + head];
     const CacheGroup g = c.groups[item];
     const int rows = cache_part_rows(g.ntok, c.tile_tokens, c.rep), in = t - g.row;
-    return PartList{g.part_row + (long long)(head + cut.x) * rows +
+    return PartList{g.part_row + (head + cut.x) * rows +
                         (in >= c.tile_tokens ? 128 + (in - c.tile_tokens) * c.rep : in * c.rep),
                     rows, cut.y, rows >= 32};
 }
 __device__ __forceinline__ PartList own_parts(const CacheDev& c, const TokenParts& p, int head, int t) {
-    if (p.own_n) return PartList{p.own_row + (long long)head * p.own_n * c.rep, c.rep, p.own_n, false};
+    if (p.own_n) return PartList{p.own_row + head * p.own_n * c.rep, c.rep, p.own_n, 0};
     return item_parts(c, p.own_item, head, t);
 }
 __device__ __forceinline__ PartList common_parts(const CacheDev& c, const TokenParts& p, int head, int t) {
-    if (p.common_n) return PartList{p.common_row + (long long)head * p.common_n * p.common_step, p.common_step, p.common_n, false};
+    if (p.common_n) return PartList{p.common_row + head * p.common_n * p.common_step, p.common_step, p.common_n, 0};
     return item_parts(c, p.common_item, head, t);
 }
 
@@ -352,9 +352,8 @@ __device__ __forceinline__ void add_source(float2 ml, float4 x, bool there, floa
 }
 // Adds four columns of query head `row` from two lists of parts, the first one's first; B are read at a time.
 template <int DH, int B>
-__device__ __forceinline__ void add_parts(const CacheDev& c, const PartList (&parts)[2], int row, int col, float& top, float& l,
-                                          float (&a)[4]) {
-    const PartList p0 = parts[0], p1 = parts[1];
+__device__ __forceinline__ void add_parts(const CacheDev& c, const PartList& p0, const PartList& p1, int row, int col, float& top,
+                                          float& l, float (&a)[4]) {
     const int n = p0.count + p1.count;
     for (int k0 = 0; k0 < n; k0 += B) {
         float2 ml[B];
@@ -363,7 +362,7 @@ __device__ __forceinline__ void add_parts(const CacheDev& c, const PartList (&pa
         for (int i = 0; i < B; ++i) {
             const int k = min(k0 + i, n - 1);
             const bool second = k >= p0.count;
-            const long long at = (second ? p1.row + (long long)(k - p0.count) * p1.step : p0.row + (long long)k * p0.step) + row;
+            const long long at = (second ? p1.row + (k - p0.count) * p1.step : p0.row + k * p0.step) + row;
             const bool warps = second ? p1.warps : p0.warps;
             const float* src = c.part_o + (warps ? (at & ~31LL) * DH + (at & 31) * 4 + col * 32 : at * DH + col);
             ml[i] = __ldcg(c.part_ml + at);

@@ -31,7 +31,7 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         cudaError_t e = cudaSuccess;
         size_t had = c->allocs.size();
         try {
-            c->allocs.reserve(had + 9);
+            c->allocs.reserve(had + 10);
         } catch (const std::bad_alloc&) {
             return c->fail(TRIMMOE_ERR_OOM, "cache_share", "host allocation failed");
         }
@@ -49,6 +49,7 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         alloc(d.groups, (size_t)cache_share_groups(d));
         alloc(d.parts_of, (size_t)kShareRows / d.Hq + 1);
         alloc(d.pieces, (size_t)kPieces);
+        alloc(d.lists, ((size_t)kShareRows / d.Hq + 1) * d.Hkv * 2);
         alloc(d.common, (size_t)d.max_seqs);
         alloc(d.cut, (size_t)cache_share_groups(d) * d.Hkv);
         alloc(d.part_ml, rows);

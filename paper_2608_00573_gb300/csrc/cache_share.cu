@@ -292,6 +292,10 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         const float a = W * (1.6f * kShareUnit), b = piece_bytes / 6.5e6f * c.num_sms;
         const float t = max(12.f, (a + b) / c.num_sms + 4.f);
         n_ctas = min(n_ctas, (int)(a / (t - 6.f)) + 1);
+        // (A whole number of CTAs to an item, where there are as many: one that begins a second item
+        // ends 6 us later.)
+        const int all = items * c.Hkv;
+        if (n_ctas > all) n_ctas -= n_ctas % all;
     }
     // Where parts lie: an item's pieces are as many as heads and cuts.
     long long rows = 0;
@@ -328,6 +332,12 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         else c.parts_of[t] = TokenParts{0, 0, s_own[k] + (t - c.seqs[k].q_off) / (2 * TT), 0, 0, 0, item, 0};
     }
     __syncthreads();
+    for (int k = i; k < T * c.Hkv; k += kPlanThreads) {
+        const int t = k / c.Hkv, head = k - t * c.Hkv;
+        const TokenParts of = c.parts_of[t];
+        c.lists[2 * (size_t)k] = common_parts(c, of, head, t);
+        c.lists[2 * (size_t)k + 1] = own_parts(c, of, head, t);
+    }
     for (int b = i; b < n_ctas; b += kPlanThreads) {
         CacheShare sh;
         sh.begin = W * b / n_ctas;
@@ -363,25 +373,21 @@ inline __host__ __device__ int join_heads(const CacheDev& c) {
 template <int DH, int B>
 __global__ void __launch_bounds__(256, B > 6 ? 2 : 4) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
                                                                    const __grid_constant__ AttendParams p) {
-    __shared__ PartList s_parts[kJoinHeads][2];
+    __shared__ PartList s_parts[kJoinHeads * 2];
     const int most = join_heads(c), blocks = (c.Hkv + most - 1) / most;
     const int t = blockIdx.x / blocks, head0 = blockIdx.x % blocks * most, heads = min(most, c.Hkv - head0);
     pdl_wait();
     pdl_trigger();
     const CachePlan pl = *c.plan;
-    if (!pl.ok || share_stale(c, pl)) return;          // (a refused step has written no items)
-    // A token whose only part is one piece has its result already.
-    const TokenParts of = c.parts_of[t];
-    if (of.own_n == 1 && !of.common_n && of.common_item < 0) return;
-    if (threadIdx.x < 2 * heads) {
-        const int k = threadIdx.x >> 1, own = threadIdx.x & 1;
-        s_parts[k][own] = own ? own_parts(c, of, head0 + k, t) : common_parts(c, of, head0 + k, t);
-    }
+    if (threadIdx.x < 2 * heads) s_parts[threadIdx.x] = c.lists[((size_t)t * c.Hkv + head0) * 2 + threadIdx.x];
     __syncthreads();
+    if (!pl.ok || share_stale(c, pl)) return;          // (a refused step has written no lists)
+    // A token whose only part is one piece has its result already.
+    if (pl.pieces && s_parts[0].count == 0 && s_parts[1].count == 1) return;
     for (int e = threadIdx.x; e < heads * c.rep * (DH / 4); e += 256) {
         const int x = e / c.rep, k = x / (DH / 4), col = x % (DH / 4) * 4, row = e - x * c.rep;
         float top = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-        add_parts<DH, B>(c, s_parts[k], row, col, top, l, a);
+        add_parts<DH, B>(c, s_parts[2 * k], s_parts[2 * k + 1], row, col, top, l, a);
         const float il = l == 0.f ? 0.f : 1.f / l;
         *reinterpret_cast<uint2*>(p.out + (size_t)t * p.ld_out + (size_t)((head0 + k) * c.rep + row) * DH + col) =
             make_uint2(pack_bf16x2(a[0] * il, a[1] * il), pack_bf16x2(a[2] * il, a[3] * il));
