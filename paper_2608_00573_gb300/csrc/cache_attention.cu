@@ -52,7 +52,7 @@
 // positions, a token each, 199 us, 0.98 of the copy rate; one sequence of 1500 positions
 // 11.7 to 14.2 us, launches and latencies.
 #include <algorithm>
-#include <cstddef>
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -81,10 +81,15 @@ struct Seg {
     int seq, kv_len, row, ntok, first, base, head;
     int t0, t1;          // key tiles
     int part;            // part buffer, -1: the whole item
-    int common, part_row;   // with groups of sequences: an item of their common tiles, the first row of its part
+};
+// With groups of sequences: an item of their common tiles, the first row of its part.
+struct SharedSeg : Seg {
+    int common, part_row;
 };
 
-struct __align__(8) Bars {
+template <bool SHARED>
+struct __align__(8) BarsOf {
+    using SegT = std::conditional_t<SHARED, SharedSeg, Seg>;
     uint64_t kv_full[10], kv_empty[10];
     uint64_t go[10], guard[10];   // partly masked value tile is under way / has been guarded, in the order of such tiles
     uint64_t q_full, q_empty;
@@ -94,7 +99,7 @@ struct __align__(8) Bars {
     uint64_t x_full[2][4], x_done[2][4];   // a slot's maxima and sums are there, the other slot's O has been read
     uint64_t part_done, join_go;
     uint64_t seg_full[kSegSlots], seg_empty[kSegSlots];
-    Seg seg[kSegSlots];
+    SegT seg[kSegSlots];
     int bad[10][2];      // guard warps' finding per ring stage
     float2 xml[2][128];  // each slot's maximum and sum per row
     uint32_t tmem_base;
@@ -103,9 +108,9 @@ struct __align__(8) Bars {
 };
 constexpr int kSegReaders = 1 + 2 + 8;   // warps that read a segment
 
-template <int DH>
+template <int DH, bool SHARED>
 constexpr size_t smem_bytes() {
-    return (size_t)Layout<DH>::BYTES + sizeof(Bars);
+    return (size_t)Layout<DH>::BYTES + sizeof(BarsOf<SHARED>);
 }
 
 // What every role derives from a segment.
@@ -358,6 +363,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if (threadIdx.x == 0) atomicCAS(c.err, 0, ERR_TIMEOUT_CACHE_ATTN);
         return;
     }
+    using Bars = BarsOf<SHARED>;
+    using SegT = typename Bars::SegT;
     Bars* bars = reinterpret_cast<Bars*>(smem + L::BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool tree = p.tree != nullptr;
@@ -405,16 +412,19 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 
     // (Addresses of single barriers are constants beside one base register.)
     const uint32_t bb = sb + L::BYTES;
-    auto bar = [&](const uint64_t* b) {
+    auto bar = [&](const void* b) {
         return bb + (uint32_t)(reinterpret_cast<const uint8_t*>(b) - reinterpret_cast<const uint8_t*>(bars));
     };
-    const uint32_t abort_at = bb + (uint32_t)offsetof(Bars, abort_flag);
+    const uint32_t abort_at = bar(&bars->abort_flag);
     auto wait = [&](const uint64_t* b, uint32_t parity) { return wait_probes(bar(b), parity & 1u, abort_at, c.err); };
     auto lost = [](uint32_t gave_up) { return __any_sync(0xffffffffu, gave_up) != 0; };
     // Common tiles are all below a segment's `base`: like a tree's, without drafts.
-    auto unmasked = [&](const Seg& g) { return tree || (SHARED && g.common); };
+    auto unmasked = [&](const SegT& g) {
+        if constexpr (SHARED) return tree || g.common;
+        else return tree;
+    };
     // The it-th segment of this CTA (false: none left, or aborted).
-    auto next_seg = [&](int it, Seg& g) {
+    auto next_seg = [&](int it, SegT& g) {
         const int s = it % kSegSlots;
         if (lost(wait(&bars->seg_full[s], it / kSegSlots))) return false;
         g = bars->seg[s];
@@ -436,7 +446,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             int it = 0, nseg = 0;
             uint32_t cnt = 0, masked = 0;           // ring entries issued, partly masked value tiles among them
             bool ok = true;
-            auto give_seg = [&](const Seg& g) {
+            auto give_seg = [&](const SegT& g) {
                 const int s = it % kSegSlots;
                 if (it >= kSegSlots && lost(wait(&bars->seg_empty[s], it / kSegSlots - 1))) return false;
                 if (lane == 0) {
@@ -468,7 +478,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             while (ok && any) {
                 int drawn = 0;
-                Seg sg;
+                SegT sg;
                 if (whole) {
                     if (lane == 0) drawn = atomicAdd(&c.plan->drawn, 1);
                     head = item % c.Hkv;
@@ -493,7 +503,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     sg.t1 = SHARED ? share_tiles_before(x1, g.cost, two_tiles) : cache_tiles_before(x1, g.cost, two_tiles);
                     const bool all = sg.t0 == 0 && sg.t1 == cache_item_tiles(g.cost, two_tiles);
                     sg.part = SHARED ? 0 : all ? -1 : 2 * b + (sg.t0 == 0);
-                    if (SHARED) {
+                    if constexpr (SHARED) {
                         sg.t0 += g.t0;
                         sg.t1 += g.t0;
                         sg.common = g.common;
@@ -581,13 +591,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
             }
             if (ok) {
-                Seg end = {};
+                SegT end = {};
                 give_seg(end);
             }
             // The last copies have landed, and been read unless the CTA gave up, before
             // it ends.
             const uint32_t tail = min(cnt, (uint32_t)ST);
-            const uint32_t never = bb + (uint32_t)offsetof(Bars, never);
+            const uint32_t never = bar(&bars->never);
             for (uint32_t k = cnt - tail; k < cnt; ++k) wait_probes(bar(&bars->kv_full[k % ST]), (k / ST) & 1, never, c.err);
             if (nseg > 0) wait_probes(bar(&bars->q_full), (nseg - 1) & 1, never, c.err);
             for (uint32_t k = cnt - tail; k < cnt; ++k) wait(&bars->kv_empty[k % ST], k / ST);
@@ -611,7 +621,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 return e;
             };
-            Seg g;
+            SegT g;
             for (int it = 0; !lost(gave_up) && next_seg(it, g); ++it) {
                 const SegInfo si = seg_info(g, TT, unmasked(g));
                 auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
@@ -724,7 +734,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             // that some see are searched for infinities and NaN.
             const int me = threadIdx.x - 64;                   // 0..63
             uint32_t cnt = 0, masked = 0;
-            Seg g;
+            SegT g;
             bool ok = true;
             for (int it = 0; ok && next_seg(it, g); ++it) {
                 const SegInfo si = seg_info(g, TT, unmasked(g));
@@ -786,7 +796,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         bool ok = true, reads_mine = false;
         for (int it = 0; ok; ++it) {
             if (lost(wait(&bars->seg_full[it % kSegSlots], it / kSegSlots))) break;
-            const Seg& g = bars->seg[it % kSegSlots];
+            const SegT& g = bars->seg[it % kSegSlots];
             if (!g.valid) break;
             const bool dual = g.ntok > TT;
             const int tok0 = dual ? slot * TT : 0;
@@ -1015,7 +1025,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 float* po = nullptr;
                 int po_step = 0;                           // from column to column of a multiple of 4
                 __nv_bfloat16* out = nullptr;
-                if (SHARED) {
+                if constexpr (SHARED) {
                     const size_t row = (size_t)g.part_row + (dual ? slot * 128 : 0) + r;
                     const bool warps = cache_part_rows(g.ntok, TT, rep) >= 32;
                     po = c.part_o + (warps ? (row & ~(size_t)31) * DH + (row & 31) * 4 : row * DH);
@@ -1124,7 +1134,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
         join_rows<DH, DH / 32>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
 }
 
-static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
+static_assert(smem_bytes<128, true>() <= 227 * 1024 && smem_bytes<64, true>() <= 227 * 1024, "shared memory of a block");
 
 template <int DH, bool SHARED>
 cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
@@ -1132,7 +1142,7 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
     static PerDevice attr;
     cudaError_t e = (cudaError_t)attr.get([] {
         return (int)cudaFuncSetAttribute(cache_attention_kernel<DH, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)smem_bytes<DH>());
+                                         (int)smem_bytes<DH, SHARED>());
     }, true);
     if (e != cudaSuccess) return e;
     // What the warpgroups ask for has to be within what the block is launched with, or
@@ -1143,7 +1153,7 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
         return cudaFuncGetAttributes(&fa, cache_attention_kernel<DH, SHARED>) == cudaSuccess ? fa.numRegs : 0;
     });
     if (nreg * kThreads < 104 * 128 + 200 * 256) return cudaErrorInvalidConfiguration;
-    e = launch_pdl(cache_attention_kernel<DH, SHARED>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH>(), st, tm_q, tm_k, tm_v,
+    e = launch_pdl(cache_attention_kernel<DH, SHARED>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH, SHARED>(), st, tm_q, tm_k, tm_v,
                    c, p);
     if (e != cudaSuccess || p.join_here) return e;
     if (SHARED) return e;                              // (launch_cache_join)
