@@ -42,20 +42,6 @@ bool pool_map(CUtensorMap* tm, const void* base, const CacheDev& d, int rows) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Query rows [T][Hq][dh] with row stride ld, a box of one tile (its tokens by the heads of
-// a key/value head) by 64 columns.
-bool query_map(CUtensorMap* tm, const void* base, const CacheDev& d, int T, int ld) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    cuuint64_t dims[3] = {(cuuint64_t)d.dh, (cuuint64_t)d.Hq, (cuuint64_t)T};
-    cuuint64_t strides[2] = {(cuuint64_t)d.dh * 2, (cuuint64_t)ld * 2};
-    cuuint32_t box[3] = {64, (cuuint32_t)d.rep, (cuuint32_t)d.tile_tokens};
-    cuuint32_t es[3] = {1, 1, 1};
-    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // Listed sequences: in range and distinct.
 trimmoe_status check_list(trimmoe_cache* c, const char* what, int n, const int32_t* seq, bool fresh_stamp = true) {
     if (n < 0 || n > c->cfg.max_seqs) return c->fail(TRIMMOE_ERR_ARG, what, "n out of range");

@@ -199,7 +199,15 @@ struct AppendParams {
     uint64_t turn[64];                 // turns per position of each pair, in units of 2^-64
 };
 
+// Lists of pages as bits, for the attention kernel to mask with (cache_attend_blocks).
+struct PageLists {
+    uint32_t* mask;                    // [T][Hkv][words], or NULL: lists are followed instead
+    int words;
+    long long stages;                  // of 64 listed positions, all tokens and heads (and 16 of their rows)
+};
+
 struct AttendParams {
+    PageLists lists;
     const uint64_t* tree;
     __nv_bfloat16* out;
     int ld_out;
@@ -219,6 +227,7 @@ struct BlocksParams {
     int splits;                        // CTAs of an item
     int alone;                         // pieces: there is no attention kernel to run beside
     float scale_log2;
+    PageLists lists;
 };
 
 struct SelectParams {
@@ -269,6 +278,8 @@ cudaError_t launch_cache_bounds_accepted(const CacheDev& c, int n, const int* se
 cudaError_t launch_cache_select(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches);
 cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                 const BlocksParams& p, cudaStream_t st);
+// Its lists as bits (p.lists).
+cudaError_t launch_cache_masks(const CacheDev& c, const BlocksParams& p, cudaStream_t st);
 // A step of single tokens with groups of sequences, beside the attention kernel: the pieces.
 cudaError_t launch_cache_own(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                              cudaStream_t st);
@@ -288,6 +299,13 @@ __device__ __forceinline__ R from_l2(const R* at) {
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(R) / 16); ++i) u.w[i] = __ldcg(reinterpret_cast<const int4*>(at) + i);
     return u.r;
+}
+
+// Whether the step's lists are masks of an attention over all pages (else each is followed).  The products of
+// a key tile and a query tile cost a CTA kDenseCost, a followed stage kStageCost, in ns an SM.
+constexpr int kDenseCost = 1000, kStageCost = 380;
+__device__ __forceinline__ bool lists_dense(const PageLists& l, const CachePlan& pl) {
+    return l.mask && pl.total * kDenseCost <= l.stages * kStageCost;
 }
 
 // A list with groups is not of the last step (a captured attend replayed without its share).

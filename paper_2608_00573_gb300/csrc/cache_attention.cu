@@ -75,6 +75,10 @@ struct Layout {
     static constexpr int BYTES = RING + STAGES * TILE;
 };
 
+// Kinds of steps: whose sequences all read for themselves, with groups of sequences (cache_share.cu), and
+// whose tokens see the pages of their lists alone (cache_attend_blocks).
+constexpr int kPlain = 0, kShared = 1, kListed = 2;
+
 // A CTA's piece of an item.
 struct Seg {
     int valid;
@@ -87,9 +91,9 @@ struct SharedSeg : Seg {
     int common, part_row;
 };
 
-template <bool SHARED>
+template <int MODE>
 struct __align__(8) BarsOf {
-    using SegT = std::conditional_t<SHARED, SharedSeg, Seg>;
+    using SegT = std::conditional_t<MODE == kShared, SharedSeg, Seg>;
     uint64_t kv_full[10], kv_empty[10];
     uint64_t go[10], guard[10];   // partly masked value tile is under way / has been guarded, in the order of such tiles
     uint64_t q_full, q_empty;
@@ -108,9 +112,9 @@ struct __align__(8) BarsOf {
 };
 constexpr int kSegReaders = 1 + 2 + 8;   // warps that read a segment
 
-template <int DH, bool SHARED>
+template <int DH, int MODE>
 constexpr size_t smem_bytes() {
-    return (size_t)Layout<DH>::BYTES + sizeof(BarsOf<SHARED>);
+    return (size_t)Layout<DH>::BYTES + sizeof(BarsOf<MODE>);
 }
 
 // What every role derives from a segment.
@@ -349,21 +353,21 @@ __device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams&
                                                              pack_bf16x2(acc[g][2] * il, acc[g][3] * il));
 }
 
-// SHARED: the items are those of a step with groups of sequences (cache_share.cu).
-template <int DH, bool SHARED>
+template <int DH, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
 cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                        const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CacheDev c,
                        const __grid_constant__ AttendParams p) {
     using L = Layout<DH>;
     constexpr int ST = L::STAGES;
+    constexpr bool SHARED = MODE == kShared, LISTED = MODE == kListed;
     extern __shared__ __align__(1024) uint8_t smem[];    // swizzled tiles start at multiples of 1024
     const uint32_t sb = smem_u32(smem);
     if (sb & 1023u) {
         if (threadIdx.x == 0) atomicCAS(c.err, 0, ERR_TIMEOUT_CACHE_ATTN);
         return;
     }
-    using Bars = BarsOf<SHARED>;
+    using Bars = BarsOf<MODE>;
     using SegT = typename Bars::SegT;
     Bars* bars = reinterpret_cast<Bars*>(smem + L::BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -423,6 +427,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if constexpr (SHARED) return tree || g.common;
         else return tree;
     };
+    // (What a list leaves out can be anywhere: every tile is partly masked.)
+    auto info = [&](const SegT& g) {
+        SegInfo s = seg_info(g, TT, unmasked(g));
+        if (LISTED) s.kall = 0;
+        return s;
+    };
     // The it-th segment of this CTA (false: none left, or aborted).
     auto next_seg = [&](int it, SegT& g) {
         const int s = it % kSegSlots;
@@ -468,6 +478,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             CacheGroup g;
             bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
             if (SHARED && any) any = !share_stale(c, pl);
+            if (LISTED && any) any = lists_dense(p.lists, pl);
             if (any && !whole) {
                 x = sh.begin;
                 x_end = sh.end;
@@ -519,7 +530,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 if (sg.t0 < sg.t1) {
                     if (!give_seg(sg)) break;
-                    const SegInfo si = seg_info(sg, TT, unmasked(sg));
+                    const SegInfo si = info(sg);
                     // Page indices of the tiles ahead travel in registers.
                     const int n_pages = (si.kmax + c.page - 1) >> c.page_shift;
                     const int* row = c.table + (size_t)sg.seq * c.max_pages;
@@ -623,7 +634,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             };
             SegT g;
             for (int it = 0; !lost(gave_up) && next_seg(it, g); ++it) {
-                const SegInfo si = seg_info(g, TT, unmasked(g));
+                const SegInfo si = info(g);
                 auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
                 const int dual = uniform(si.dual), lead = dual ? 1 : 2, nt = uniform(g.t1 - g.t0);
                 const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
@@ -737,7 +748,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             SegT g;
             bool ok = true;
             for (int it = 0; ok && next_seg(it, g); ++it) {
-                const SegInfo si = seg_info(g, TT, unmasked(g));
+                const SegInfo si = info(g);
                 const int lead = si.dual ? 1 : 2, nt = g.t1 - g.t0;
                 for (int i = max(0, si.kall / kCacheTile - g.t0); ok && i < nt; ++i) {
                     const int t = g.t0 + i;
@@ -805,7 +816,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int step = dual ? 1 : 2, begin = g.t0 + (dual ? 0 : slot);
             int lim, first_part, mask0;                    // tiles, first partly masked one, index of a tile among those
             {
-                const SegInfo si = seg_info(g, TT, unmasked(g));
+                const SegInfo si = info(g);
                 lim = slot ? si.n1 : si.n0;
                 first_part = si.kall / kCacheTile;
                 const int m0 = max(g.t0, first_part);
@@ -814,8 +825,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             const bool work = begin < lim;
             float m = 0.f, l = 0.f;                        // (no key seen yet: m is arbitrary)
+            uint32_t listed = 0;                           // LISTED: 32 pages from a multiple of 32 on
 #pragma unroll 1
             for (int t = begin; t < lim; t += step) {
+                const int page0 = LISTED ? t << 7 >> c.page_shift : 0;
+                if (LISTED && (t == begin || (page0 & 31) == 0 || (!dual && (page0 & 31) == kCacheTile >> c.page_shift))) {
+                    const int tok = g.row + tok0 + max(0, min(tok_in_tile, ntok - 1));
+                    listed = __ldcg(p.lists.mask + ((size_t)tok * c.Hkv + g.head) * p.lists.words + (page0 >> 5));
+                }
                 ok = !lost(wait(&bars->s_full[slot], ph));
                 if (!ok) break;
                 ph ^= kPhS;
@@ -846,6 +863,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             const int end = g.kv_len - k0;                     // bits past the drafts
                             see[q] &= end >= 32 ? ~0u : end > 0 ? (1u << end) - 1u : 0u;
                         }
+                        if (LISTED) {
+                            const uint32_t pages = listed >> (page0 & 31);
+                            if (c.page_shift >= 5) {
+                                see[q] &= pages >> (q * 32 >> c.page_shift) & 1u ? ~0u : 0u;
+                            } else {
+                                see[q] &= (pages >> (2 * q) & 1u ? 0xffffu : 0u) | (pages >> (2 * q + 1) & 1u ? 0xffff0000u : 0u);
+                            }
+                        }
                     }
                 }
                 // One pass over the scores in TMEM, a quarter (32 columns) at a time with the next
@@ -857,6 +882,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 uint32_t u[3][32];
                 float2 ls[2];
                 auto hide = [&](int q) {                 // masked scores of quarter q
+                    if (LISTED && __all_sync(0xffffffffu, see[q] + 1u <= 1u)) {
+                        const bool none = see[q] == 0;   // (pages from 32 positions on: all or nothing)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (none) u[q % 3][j] = 0xff800000u;
+                        return;
+                    }
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
                         if (!(see[q] >> j & 1u)) u[q % 3][j] = 0xff800000u;        // -inf
@@ -893,7 +925,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const float mx = fmaxf(maximum(2 * half), maximum(2 * half + 1));
                     exponentials(2 * half);
                     exponentials(2 * half + 1);
-                    const bool move = mx - m > 8.f || (l == 0.f && mx - m < -8.f && mx != -INFINITY);
+                    // (A list's first seen keys may come late: m starts with them.)
+                    const bool move = mx - m > 8.f || (l == 0.f && mx != -INFINITY && (LISTED ? mx != m : mx - m < -8.f));
                     if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
                         const float up = mx, f = move && l != 0.f ? ex2(m - up) : 1.f;   // l = 0: so is O
                         if (move) m = up;
@@ -940,7 +973,26 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (reads_mine) ok = !lost(wait(&bars->x_done[slot ^ 1][qw], (ph / kPhX) ^ 1u));
                     reads_mine = false;
                 };
-                if (live) {
+                // A half of which no row of the warp sees a key: P is zero.
+                auto nothing = [&](int half) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) w[j] = 0u;
+                    tmem_st_32x16(tS + half * 32, w);
+                    tmem_st_32x16(tS + half * 32 + 16, w);
+                    tmem_st_wait();
+                };
+                if (LISTED && live && !__any_sync(0xffffffffu, (see[0] | see[1]) != 0u)) {
+                    tmem_ld_32x32(tS + 64, u[2]);
+                    tmem_ld_32x32(tS + 96, u[0]);
+                    landed(u[2]);
+                    nothing(0);
+                    if (bad) {
+                        other_has_read();
+                        if (!ok) break;
+                        by_hand(0);
+                    }
+                } else if (live) {
                     tmem_ld_32x32(tS, u[0]);
                     tmem_ld_32x32(tS + 32, u[1]);
                     landed(u[0]);
@@ -969,14 +1021,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     landed(u[0]);
                     landed(u[2]);
                     if (part && !__any_sync(0xffffffffu, (see[2] | see[3]) != 0u)) {
-                        uint32_t w[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = 0u;
-                        tmem_st_32x16(tS + 32, w);
-                        tmem_st_32x16(tS + 48, w);
-                        tmem_st_wait();
+                        nothing(1);
                     } else {
-                        if (part) {
+                        if (part && !(LISTED && __all_sync(0xffffffffu, (see[2] & see[3]) == ~0u))) {
                             hide(2);
                             hide(3);
                         }
@@ -1124,7 +1171,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
     pdl_wait();
     pdl_trigger();
     const int n_ctas = c.plan->n_ctas, b = blockIdx.x;
-    if (!c.plan->ok || b + 1 >= n_ctas) return;
+    if (!c.plan->ok || b + 1 >= n_ctas || (p.lists.mask && !lists_dense(p.lists, *c.plan))) return;
     const CacheShare next = c.shares[b + 1];
     if (next.within == 0 || next.first != b || next.last == b) return;
     const int two = cache_two_tiles(next.g.ntok, c.tile_tokens);
@@ -1134,15 +1181,15 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
         join_rows<DH, DH / 32>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
 }
 
-static_assert(smem_bytes<128, true>() <= 227 * 1024 && smem_bytes<64, true>() <= 227 * 1024, "shared memory of a block");
+static_assert(smem_bytes<128, kShared>() <= 227 * 1024 && smem_bytes<64, kShared>() <= 227 * 1024, "shared memory of a block");
 
-template <int DH, bool SHARED>
+template <int DH, int MODE>
 cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                    const AttendParams& p, int max_rows, cudaStream_t st) {
     static PerDevice attr;
     cudaError_t e = (cudaError_t)attr.get([] {
-        return (int)cudaFuncSetAttribute(cache_attention_kernel<DH, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)smem_bytes<DH, SHARED>());
+        return (int)cudaFuncSetAttribute(cache_attention_kernel<DH, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)smem_bytes<DH, MODE>());
     }, true);
     if (e != cudaSuccess) return e;
     // What the warpgroups ask for has to be within what the block is launched with, or
@@ -1150,13 +1197,13 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
     static PerDevice regs;
     const int nreg = regs.get([] {
         cudaFuncAttributes fa = {};
-        return cudaFuncGetAttributes(&fa, cache_attention_kernel<DH, SHARED>) == cudaSuccess ? fa.numRegs : 0;
+        return cudaFuncGetAttributes(&fa, cache_attention_kernel<DH, MODE>) == cudaSuccess ? fa.numRegs : 0;
     });
     if (nreg * kThreads < 104 * 128 + 200 * 256) return cudaErrorInvalidConfiguration;
-    e = launch_pdl(cache_attention_kernel<DH, SHARED>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH, SHARED>(), st, tm_q, tm_k, tm_v,
+    e = launch_pdl(cache_attention_kernel<DH, MODE>, dim3(c.num_sms), dim3(kThreads), smem_bytes<DH, MODE>(), st, tm_q, tm_k, tm_v,
                    c, p);
     if (e != cudaSuccess || p.join_here) return e;
-    if (SHARED) return e;                              // (launch_cache_join)
+    if (MODE == kShared) return e;                              // (launch_cache_join)
     return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);
 }
 
@@ -1164,11 +1211,14 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
 
 cudaError_t launch_cache_attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                 const CUtensorMap& tm_v, const AttendParams& p, int max_rows, cudaStream_t st) {
+    if (p.lists.mask)
+        return c.dh == 64 ? attend<64, kListed>(c, tm_q, tm_k, tm_v, p, max_rows, st)
+                          : attend<128, kListed>(c, tm_q, tm_k, tm_v, p, max_rows, st);
     if (c.shared)
-        return c.dh == 64 ? attend<64, true>(c, tm_q, tm_k, tm_v, p, max_rows, st)
-                          : attend<128, true>(c, tm_q, tm_k, tm_v, p, max_rows, st);
-    return c.dh == 64 ? attend<64, false>(c, tm_q, tm_k, tm_v, p, max_rows, st)
-                      : attend<128, false>(c, tm_q, tm_k, tm_v, p, max_rows, st);
+        return c.dh == 64 ? attend<64, kShared>(c, tm_q, tm_k, tm_v, p, max_rows, st)
+                          : attend<128, kShared>(c, tm_q, tm_k, tm_v, p, max_rows, st);
+    return c.dh == 64 ? attend<64, kPlain>(c, tm_q, tm_k, tm_v, p, max_rows, st)
+                      : attend<128, kPlain>(c, tm_q, tm_k, tm_v, p, max_rows, st);
 }
 
 }  // namespace tmoe

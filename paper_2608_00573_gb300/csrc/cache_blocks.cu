@@ -6,6 +6,39 @@
 
 #include "cache_host.cuh"
 
+namespace {
+
+constexpr int kStageRows = 64;                // positions of a stage of the kernel that follows lists
+
+// Room for the step's lists as bits: for all of T_max when that is 64 MB at most.  (None: the lists are followed.)
+bool room_for_masks(trimmoe_cache* c, cudaStream_t st) {
+    const size_t row = (size_t)c->d.Hkv * ((c->d.max_pages + 31) / 32);
+    if (!c->masks) {
+        const size_t words = std::min(row * c->d.T_max, (size_t)16 << 20);
+        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+        if (row > words || cudaStreamIsCapturing(st, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone) {
+            cudaGetLastError();
+            return false;
+        }
+        try {
+            c->allocs.reserve(c->allocs.size() + 1);
+        } catch (const std::bad_alloc&) {
+            return false;
+        }
+        void* q = nullptr;
+        if (cudaMalloc(&q, words * sizeof(uint32_t)) != cudaSuccess) {
+            cudaGetLastError();
+            return false;
+        }
+        c->allocs.push_back(q);
+        c->masks = static_cast<uint32_t*>(q);
+        c->mask_words = words;
+    }
+    return row * c->T <= c->mask_words;
+}
+
+}  // namespace
+
 extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, const int32_t* counts, void* stream) {
     if (!c) return TRIMMOE_ERR_ARG;
     if (c->T < 0) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "no step has been begun");
@@ -179,7 +212,30 @@ extern "C" trimmoe_status trimmoe_cache_attend_blocks(trimmoe_cache_handle c, in
     const bool large = d.page > 64;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_attend_blocks");
+    cudaStream_t st = enter(c, stream);
+    // Tokens of prompts: where their lists name much of what their sequences hold, 128 rows at a time over all
+    // pages, with the lists as masks, is faster (lists_dense decides by the lengths, on the GPU).  Not for
+    // lists that are followed in 60 us.
+    const long long stages = (long long)p.T * d.Hkv * p.row_tiles * std::max(1LL, (long long)p.n * d.page / kStageRows);
+    int launches = 1;
+    if (c->max_q * d.rep >= kCacheTile / 2 && stages * kStageCost >= 60000LL * d.num_sms && room_for_masks(c, st)) {
+        p.lists = PageLists{c->masks, (d.max_pages + 31) / 32, stages};
+        AttendParams m = {};
+        m.lists = p.lists;
+        m.tree = p.tree;
+        m.out = p.out;
+        m.ld_out = p.ld_out;
+        m.scale_log2 = p.scale_log2;
+        m.T = p.T;
+        CUtensorMap tm_q;
+        if (!query_map(&tm_q, a->q, d, c->T, a->ld_q)) return c->fail(TRIMMOE_ERR_CUDA, what, "cuTensorMapEncodeTiled failed");
+        const int max_rows = c->max_q > d.tile_tokens ? 2 * kCacheTile : c->max_q * d.rep;
+        cudaError_t e = launch_cache_masks(d, p, st);
+        if (e == cudaSuccess) e = launch_cache_attend(d, tm_q, c->tm_k[layer], c->tm_v[layer], m, max_rows, st);
+        if (e != cudaSuccess) return c->launched(e, 0, what);
+        launches += 3;
+    }
     return c->launched(launch_cache_blocks(d, large ? c->tm_k64[layer] : c->tm_k[layer], large ? c->tm_v64[layer] : c->tm_v[layer],
-                                           p, enter(c, stream)),
-                       1, what);
+                                           p, st),
+                       launches, what);
 }

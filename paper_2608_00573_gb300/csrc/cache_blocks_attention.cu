@@ -127,7 +127,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     pdl_trigger();
     const CachePlan pl = sh.plan;
     const int items = OWN ? pl.pieces * c.Hkv : p.T * c.Hkv * p.row_tiles;
-    if (!pl.ok || (OWN && share_stale(c, pl))) {       // (all CTAs)
+    if (!pl.ok || (OWN ? share_stale(c, pl) : lists_dense(p.lists, pl))) {       // (all CTAs)
         if (OWN) pdl_wait();
         return;
     }
@@ -532,6 +532,46 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (OWN) pdl_wait();
 }
 
+// Lists as bits: a warp takes a token and key/value head, a window of pages at a time.  Pages from the step's
+// first one on are seen as far as positions are.  Entries that do not fit are left out and flagged.
+constexpr int kMaskWarps = 8, kMaskWords = 128;
+__global__ void __launch_bounds__(kMaskWarps * 32) cache_masks_kernel(const __grid_constant__ CacheDev c,
+                                                                      const __grid_constant__ BlocksParams p) {
+    __shared__ uint32_t s_bits[kMaskWarps][kMaskWords];
+    const int lane = threadIdx.x & 31, words = p.lists.words;
+    uint32_t* bits = s_bits[threadIdx.x >> 5];
+    pdl_wait();
+    pdl_trigger();
+    const CachePlan pl = *c.plan;
+    if (!pl.ok || !lists_dense(p.lists, pl)) return;
+    for (long long i = (long long)blockIdx.x * kMaskWarps + (threadIdx.x >> 5); i < (long long)p.T * c.Hkv;
+         i += (long long)gridDim.x * kMaskWarps) {
+        const CacheToken tok = c.tokens[i / c.Hkv];
+        const int own = tok.base >> c.page_shift, listed = min(p.n, own), end = (tok.kv_len - 1 >> c.page_shift) / 32 + 1;
+        const int* list = p.blocks + (size_t)i * p.n;
+        for (int w0 = 0; w0 < end; w0 += kMaskWords) {
+            for (int w = lane; w < kMaskWords; w += 32) {
+                const int n = own - (w0 + w) * 32;     // pages of the word before the step's own
+                bits[w] = n >= 32 ? 0u : n > 0 ? ~0u << n : ~0u;
+            }
+            __syncwarp();
+            for (int j = lane; j < listed; j += 32) {
+                const int col = list[j], before = j ? list[j - 1] : -1;
+                if (col == -1) continue;
+                if (col < 0 || col >= own || (j && (before < 0 || col <= before))) {
+                    atomicCAS(c.err, 0, ERR_CACHE_BLOCKS);
+                    continue;
+                }
+                const int w = (col >> 5) - w0;
+                if (w >= 0 && w < kMaskWords) atomicOr(&bits[w], 1u << (col & 31));
+            }
+            __syncwarp();
+            for (int w = lane; w < min(kMaskWords, end - w0); w += 32) p.lists.mask[(size_t)i * words + w0 + w] = bits[w];
+            __syncwarp();
+        }
+    }
+}
+
 template <int DH, bool OWN>
 cudaError_t blocks_launch(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                           cudaStream_t st) {
@@ -567,6 +607,11 @@ cudaError_t blocks_launch(const CacheDev& c, const CUtensorMap& tm_k, const CUte
 cudaError_t launch_cache_blocks(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,
                                 cudaStream_t st) {
     return c.dh == 64 ? blocks_launch<64, false>(c, tm_k, tm_v, p, st) : blocks_launch<128, false>(c, tm_k, tm_v, p, st);
+}
+
+cudaError_t launch_cache_masks(const CacheDev& c, const BlocksParams& p, cudaStream_t st) {
+    const long long blocks = ((long long)p.T * c.Hkv + kMaskWarps - 1) / kMaskWarps;
+    return launch_pdl(cache_masks_kernel, dim3((unsigned)std::min<long long>(blocks, 8LL * c.num_sms)), dim3(kMaskWarps * 32), 0, st, c, p);
 }
 
 cudaError_t launch_cache_own(const CacheDev& c, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const BlocksParams& p,

@@ -29,6 +29,8 @@ struct trimmoe_cache {
     cudaError_t (*own)(const CacheDev&, const CUtensorMap&, const CUtensorMap&, const BlocksParams&, cudaStream_t) = nullptr;
     cudaError_t (*join)(const CacheDev&, const AttendParams&, cudaStream_t) = nullptr;
     bool single = false, small = false;       // groups of single tokens; and all of them small
+    uint32_t* masks = nullptr;                // room for lists as bits (attend_blocks)
+    size_t mask_words = 0;
     float theta = 0.f;                        // base of turn[]
     uint64_t turn[64];
 
@@ -74,6 +76,20 @@ inline trimmoe_status check_layer(trimmoe_cache* c, const char* what, int layer)
     if (layer < 0 || layer >= c->cfg.layers) return c->fail(TRIMMOE_ERR_ARG, what, "layer out of range");
     if (c->T < 0) return c->fail(TRIMMOE_ERR_ARG, what, "no step has been begun");
     return TRIMMOE_OK;
+}
+
+// Query rows [T][Hq][dh] with row stride ld, a box of one tile (its tokens by the heads of
+// a key/value head) by 64 columns.
+inline bool query_map(CUtensorMap* tm, const void* base, const CacheDev& d, int T, int ld) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)d.dh, (cuuint64_t)d.Hq, (cuuint64_t)T};
+    cuuint64_t strides[2] = {(cuuint64_t)d.dh * 2, (cuuint64_t)ld * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)d.rep, (cuuint32_t)d.tile_tokens};
+    cuuint32_t es[3] = {1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Sets up a call on `stream` (after its checks): clears an error that other code

@@ -67,8 +67,8 @@ def select_ref(cache, m, layer, x, q, n, first=1, last=1):
     return out
 
 
-def check_blocks(cache, m, x, q, blocks, out, layer, tree=None, scale=None, heads=None):
-    """attend_blocks against attend_ref, token by token."""
+def check_blocks(cache, m, x, q, blocks, out, layer, tree=None, scale=None, heads=None, tokens=None):
+    """attend_blocks against attend_ref, token by token (heads, tokens: those that are looked at)."""
     dh, rep, page = cache.head_dim, cache.q_heads // cache.kv_heads, cache.page
     lists = blocks.cpu().tolist()
     t = 0
@@ -78,7 +78,7 @@ def check_blocks(cache, m, x, q, blocks, out, layer, tree=None, scale=None, head
         if new:
             k, v = rows_of(cache.k[layer], m, s, kv), rows_of(cache.v[layer], m, s, kv)
         for i in range(new):
-            for g in heads or range(cache.kv_heads):
+            for g in (heads or range(cache.kv_heads)) if tokens is None or t in tokens else ():
                 seen = torch.zeros(1, kv, dtype=torch.bool, device=x.device)
                 for b in lists[t][g]:
                     if b >= 0:

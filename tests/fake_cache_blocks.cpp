@@ -34,6 +34,7 @@ using St = cudaStream_t;
 cudaError_t launch_cache_bounds(const CacheDev&, int, int, int, int whole, St) { return note(whole ? "bounds_whole" : "bounds"); }
 cudaError_t launch_cache_select(const CacheDev&, const SelectParams&, St, int& launches) { return launches = 2, note("select"); }
 cudaError_t launch_cache_blocks(const CacheDev&, const CUtensorMap&, const CUtensorMap&, const BlocksParams&, St) { return note("blocks"); }
+cudaError_t launch_cache_masks(const CacheDev&, const BlocksParams&, St) { return note("masks"); }
 cudaError_t launch_cache_own(const CacheDev&, const CUtensorMap&, const CUtensorMap&, const BlocksParams&, St) { return note("own"); }
 cudaError_t launch_cache_join(const CacheDev&, const AttendParams&, St) { return note("join"); }
 cudaError_t launch_cache_share(const CacheDev&, int, const int*, int, int, int single, St) { return note(single ? "share_single" : "share"); }

@@ -254,6 +254,97 @@ def test_all_blocks_are_attend():
     check_blocks(cache, m, x, q, blocks, cache.attend_blocks(0, x, blocks, scale=0.03), 0, scale=0.03)
 
 
+# Prompts whose lists are masks of an attention over all pages (many listed positions a token, against the sequence's
+# length), and one whose lists are followed.
+MANY = {
+    "page64": ((8, 2, 128), 64, [1500, 900, 64], [400, 300, 100], 16),
+    "page16_d64": ((6, 6, 64), 16, [2000, 37], [200, 50], 80),
+    "page32_heads_17": ((17, 1, 128), 32, [2500, 131], [400, 100], 50),
+    "page128_d64": ((4, 2, 64), 128, [3000], [700], 12),
+    "heads_3": ((6, 2, 128), 16, [1000, 700, 15], [331, 1, 400], 72),
+    "windows": ((2, 1, 128), 16, [70000], [128], 800),
+    "followed": ((16, 8, 64), 64, [60000], [400], 8),
+}
+
+
+def some_tokens(q, n, seed):
+    ends = [e for s in range(len(q)) for e in (sum(q[:s]), sum(q[:s + 1]) - 1)]
+    return set(ends) | set(random.Random(seed).sample(range(sum(q)), n))
+
+
+@pytest.mark.parametrize("fill", [None, "some"])
+@pytest.mark.parametrize("name", MANY)
+def test_attend_blocks_of_prompts(name, fill):
+    shapes, page, ctx, q, n = MANY[name]
+    cache, m, x = filled(shapes, page, ctx, q, seed=4)
+    blocks = lists_of(m, q, n, shapes[1], fill=fill)
+    before = cache.stats()["launches"]
+    out = cache.attend_blocks(1, x, blocks)
+    assert cache.stats()["launches"] - before == 4
+    check_blocks(cache, m, x, q, blocks, out, 1, tokens=some_tokens(q, 40, 1))
+    assert torch.equal(cache.attend_blocks(1, x, blocks), out)
+    assert cache.stats()["device_error"] == 0
+
+
+def test_attend_blocks_of_prompts_values_that_are_not_finite():
+    """Infinities and NaN reach the tokens whose lists name them, and no others; entries that do not fit are left out."""
+    shapes, page, ctx, q, n = MANY["page64"]
+    cache, m, x = filled(shapes, page, ctx, q, seed=6)
+    cache.v[0, m.own[0][3], 1, 5, 7] = float("inf")
+    cache.v[0, m.own[0][4], 0, 63, 100] = float("nan")
+    cache.k[0, m.own[0][9], 0, 1, 1] = float("nan")
+    cache.k[0, m.own[1][2], 1, 8, 0] = float("inf")
+    cache.v[0, m.own[1][15], 1, 2, 3] = float("-inf")           # a new token's
+    blocks = lists_of(m, q, n, 2, fill="some")
+    out = cache.attend_blocks(0, x, blocks)
+    check_blocks(cache, m, x, q, blocks, out, 0, tokens=some_tokens(q, 60, 2))
+    assert cache.stats()["device_error"] == 0
+    bad = blocks.clone()
+    bad[7, 1, :4] = torch.tensor([5, 1, 3, 4], dtype=torch.int32, device=DEV)
+    bad[7, 1, 4:] = -1
+    out = cache.attend_blocks(0, x, bad)
+    assert cache.stats(reset=True)["device_error"] == 11
+    bad[7, 1, :4] = torch.tensor([3, 4, 5, -1], dtype=torch.int32, device=DEV)
+    check_blocks(cache, m, x, q, bad, out, 0, tokens={6, 7, 8})
+
+
+def test_attend_blocks_of_many_trees():
+    shapes, page, ctx, q = (8, 2, 128), 64, [1700 + 91 * i for i in range(8)], [64] * 6 + [33, 50]
+    cache, m, x = filled(shapes, page, ctx, q, seed=3)
+    rng = random.Random(8)
+    words = [rng.getrandbits(64) for _ in range(sum(q))]
+    words[70] = 0
+    tree = torch.tensor([w - (1 << 64) if w >> 63 else w for w in words], dtype=torch.int64, device=DEV)
+    blocks = lists_of(m, q, 28, 2, fill="some")
+    blocks[70] = -1
+    out = cache.attend_blocks(0, x, blocks, tree=tree)
+    check_blocks(cache, m, x, q, blocks, out, 0, tree=words, tokens=some_tokens(q, 30, 3) | {70})
+    assert cache.stats()["device_error"] == 0
+
+
+def test_attend_blocks_of_prompts_in_graphs():
+    """Captured before any call of that kind (its workspace is not there then) and after one."""
+    shapes, page, ctx, q, n = MANY["page64"]
+    cache, m, x = filled(shapes, page, ctx, q, seed=4)
+    blocks = lists_of(m, q, n, 2)
+    outs, counts = [], []
+    for _ in range(2):
+        out = torch.zeros_like(x)
+        g = torch.cuda.CUDAGraph()
+        before = cache.stats()["launches"]
+        with torch.cuda.graph(g):
+            cache.attend_blocks(1, x, blocks, out=out)
+        counts.append(cache.stats()["launches"] - before)
+        g.replay()
+        g.replay()
+        outs.append(out)
+        eager = cache.attend_blocks(1, x, blocks)
+    assert counts == [1, 4]
+    for out in outs:
+        check_blocks(cache, m, x, q, blocks, out, 1, tokens=some_tokens(q, 20, 5))
+    assert torch.equal(outs[1], eager)
+
+
 def test_a_single_seen_key_gives_its_value():
     cache, m, x = filled((8, 2, 128), 16, [160], [3], seed=2)
     tree = torch.tensor([1, 2, 4], device=DEV)
