@@ -64,7 +64,8 @@ struct __align__(16) CachePlan {
     int copies;                        // pages to copy (shared last pages)
     int ok;                            // 0: the step was refused
     int drawn, done;                   // items drawn beyond the first round, CTAs that have finished
-    int pieces;                        // with groups of sequences and single tokens: what is not on the line
+    int pieces;                        // with groups of sequences and single tokens: what is not on the line; lists as
+                                       // masks: items to be computed again
     int serial;                        // of the step (a list with groups is of the step with its number)
 };
 
@@ -201,9 +202,12 @@ struct AppendParams {
 
 // Lists of pages as bits, for the attention kernel to mask with (cache_attend_blocks).
 struct PageLists {
-    uint32_t* mask;                    // [T][Hkv][words], or NULL: lists are followed instead
+    uint32_t* mask;                    // [T][Hkv][words + 2], or NULL: lists are followed instead
     int words;
     long long stages;                  // of 64 listed positions, all tokens and heads (and 16 of their rows)
+    __host__ __device__ uint32_t* bits(long long item) const { return mask + item * (words + 2); }
+    __device__ uint32_t* mark(long long item) const { return bits(item) + words; }        // the item is computed again
+    __device__ uint32_t* marked(long long i) const { return bits(i) + words + 1; }        // i-th such item
 };
 
 struct AttendParams {
@@ -301,11 +305,15 @@ __device__ __forceinline__ R from_l2(const R* at) {
     return u.r;
 }
 
-// Whether the step's lists are masks of an attention over all pages (else each is followed).  The products of
-// a key tile and a query tile cost a CTA kDenseCost, a followed stage kStageCost, in ns an SM.
-constexpr int kDenseCost = 1000, kStageCost = 380;
-__device__ __forceinline__ bool lists_dense(const PageLists& l, const CachePlan& pl) {
-    return l.mask && pl.total * kDenseCost <= l.stages * kStageCost;
+// Whether the step's lists are masks of an attention over all pages (else each is followed), in ns of an SM:
+// that attention takes kDenseEnds, with its launches, and kDenseCost for a key tile and a query tile; a followed stage
+// kStageCost.  Measured, 800 tokens of 3 chunks, masks against lists, 32 heads on 8, 24 pages of 64: behind 6000 to
+// 15000 positions 168 us / 436, 15000 to 30000 308 / 432, 30000 to 60000 582 / 447; 16 heads on 16, 96 pages of
+// 16: 148 / 1174, 280 / 1184; 12 heads of 64 columns, 40 pages of 32: 84 / 458, 141 / 456; 20 times 17 tokens behind
+// 2000 to 9000, 32 heads on 8: 93 / 177; 64 tokens behind 16000, 32 pages: 47 / 53.
+constexpr int kDenseEnds = 33000, kDenseCost = 1050, kStageCost = 420;
+__device__ __forceinline__ bool lists_dense(const CacheDev& c, const PageLists& l, const CachePlan& pl) {
+    return l.mask && (long long)kDenseEnds * c.num_sms + pl.total * kDenseCost <= l.stages * kStageCost;
 }
 
 // A list with groups is not of the last step (a captured attend replayed without its share).

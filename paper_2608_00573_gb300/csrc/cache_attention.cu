@@ -40,10 +40,16 @@
 // few rows the CTA that writes an item's last part joins it (join_row), else
 // cache_join_kernel does (join_rows).
 //
+// With lists of pages (cache_attend_blocks) a row's keys of other pages get p = 2^-inf: sixteens of keys have
+// their own reference in the exponent, -m or -inf, so that a mask costs one selection per 16 scores.
+// (Scores replaced one by one, and halves that no row lists left out: 800 tokens' chunks 275 and 303 us,
+// this way 168; an attention without lists takes 156.)  All tiles are read, and there is no union of
+// lists: with 32 tokens to a query tile it is nearly everything unless neighbours agree.
+//
 // Masked places never reach a result: scores are replaced, not added to; value
 // rows that no row of the item sees are zeroed in shared memory (0 * NaN would
 // be NaN), and a tile whose partly masked value rows hold an infinity or a NaN is
-// multiplied by the softmax warps themselves, skipping masked keys.
+// multiplied by the softmax warps themselves, skipping masked keys.  (Lists: mark_item.)
 //
 // Bounds: prompts the tensor cores and, per key tile, the chain S -> exponentials -> P V
 // of each slot; decoding HBM, each K and V row once per query tile.  Measured (32 query
@@ -303,6 +309,16 @@ __device__ __forceinline__ void join_row(const CacheDev& c, const AttendParams& 
         *reinterpret_cast<uint32_t*>(out + j) = pack_bf16x2(acc[j] * il, acc[j + 1] * il);
 }
 
+// With lists as masks, keys and values that a list leaves out are multiplied by p = 0, which is NaN where
+// they are not finite.  A token and key/value head with such a result is marked, and the kernel that follows lists
+// computes it again.  (Searching all value tiles beforehand, as partly masked ones are, took 800
+// tokens' chunks 46 us more: shared memory is what these products wait for.)
+__device__ __noinline__ void mark_item(const CacheDev& c, const PageLists& l, int token, int head) {
+    const int item = token * c.Hkv + head;
+    if (atomicExch(l.mark(item), 1u)) return;
+    *l.marked(atomicAdd(&c.plan->pieces, 1)) = (uint32_t)item;
+}
+
 // Joins 8 rows of a cut item, G times 16 columns of them, likewise; a lane has a row and 4
 // columns of each 16, two sources are read at a time (each part is one: the slots have
 // joined theirs, or have rows of their own).  Bound: L2.
@@ -347,6 +363,14 @@ __device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams&
     const int token = sh.g.row + tile * c.tile_tokens + in / c.rep, h = sh.head * c.rep + in % c.rep;
     const float il = l == 0.f ? 0.f : 1.f / l;
     __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + col;
+    if (p.lists.mask) {
+        float sum = il * 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum = fmaf(acc[g][j], 0.f, sum);
+        if (sum != 0.f) mark_item(c, p.lists, token, sh.head);
+    }
 #pragma unroll
     for (int g = 0; g < G; ++g)
         *reinterpret_cast<uint2*>(out + 16 * g) = make_uint2(pack_bf16x2(acc[g][0] * il, acc[g][1] * il),
@@ -427,12 +451,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if constexpr (SHARED) return tree || g.common;
         else return tree;
     };
-    // (What a list leaves out can be anywhere: every tile is partly masked.)
-    auto info = [&](const SegT& g) {
-        SegInfo s = seg_info(g, TT, unmasked(g));
-        if (LISTED) s.kall = 0;
-        return s;
-    };
+    auto info = [&](const SegT& g) { return seg_info(g, TT, unmasked(g)); };
     // The it-th segment of this CTA (false: none left, or aborted).
     auto next_seg = [&](int it, SegT& g) {
         const int s = it % kSegSlots;
@@ -478,7 +497,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             CacheGroup g;
             bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
             if (SHARED && any) any = !share_stale(c, pl);
-            if (LISTED && any) any = lists_dense(p.lists, pl);
+            if (LISTED && any) any = lists_dense(c, p.lists, pl);
             if (any && !whole) {
                 x = sh.begin;
                 x_end = sh.end;
@@ -831,7 +850,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 const int page0 = LISTED ? t << 7 >> c.page_shift : 0;
                 if (LISTED && (t == begin || (page0 & 31) == 0 || (!dual && (page0 & 31) == kCacheTile >> c.page_shift))) {
                     const int tok = g.row + tok0 + max(0, min(tok_in_tile, ntok - 1));
-                    listed = __ldcg(p.lists.mask + ((size_t)tok * c.Hkv + g.head) * p.lists.words + (page0 >> 5));
+                    listed = __ldcg(p.lists.bits((long long)tok * c.Hkv + g.head) + (page0 >> 5));
                 }
                 ok = !lost(wait(&bars->s_full[slot], ph));
                 if (!ok) break;
@@ -863,16 +882,18 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             const int end = g.kv_len - k0;                     // bits past the drafts
                             see[q] &= end >= 32 ? ~0u : end > 0 ? (1u << end) - 1u : 0u;
                         }
-                        if (LISTED) {
-                            const uint32_t pages = listed >> (page0 & 31);
-                            if (c.page_shift >= 5) {
-                                see[q] &= pages >> (q * 32 >> c.page_shift) & 1u ? ~0u : 0u;
-                            } else {
-                                see[q] &= (pages >> (2 * q) & 1u ? 0xffffu : 0u) | (pages >> (2 * q + 1) & 1u ? 0xffff0000u : 0u);
-                            }
-                        }
                     }
                 }
+                // LISTED: sixteens of keys whose page is in the row's list, or one of the step's own.
+                uint32_t sixteens = ~0u;
+                if (LISTED) {
+                    const uint32_t x = listed >> (page0 & 31);
+                    sixteens = c.page_shift == 4   ? x
+                               : c.page_shift == 5 ? (x & 1u) * 3u | (x & 2u) * 6u | (x & 4u) * 12u | (x & 8u) * 24u
+                               : c.page_shift == 6 ? (x & 1u) * 15u | (x & 2u) * 120u
+                                                   : (x & 1u) * 255u;
+                }
+                auto in_list = [&](int i) { return !LISTED || (sixteens >> i & 1u); };
                 // One pass over the scores in TMEM, a quarter (32 columns) at a time with the next
                 // load in flight, and P handed over in two halves, so that the first half's
                 // product runs under the second half's exponentials.  These start from the
@@ -882,13 +903,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 uint32_t u[3][32];
                 float2 ls[2];
                 auto hide = [&](int q) {                 // masked scores of quarter q
-                    if (LISTED && __all_sync(0xffffffffu, see[q] + 1u <= 1u)) {
-                        const bool none = see[q] == 0;   // (pages from 32 positions on: all or nothing)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (none) u[q % 3][j] = 0xff800000u;
-                        return;
-                    }
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
                         if (!(see[q] >> j & 1u)) u[q % 3][j] = 0xff800000u;        // -inf
@@ -903,14 +917,18 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             a[k] = max3(a[k], __uint_as_float(x[8 * k + j]), __uint_as_float(x[8 * k + j + 1]));
+                    if (LISTED)
+                        return fmaxf(in_list(2 * q) ? fmaxf(a[0], a[1]) : -INFINITY, in_list(2 * q + 1) ? fmaxf(a[2], a[3]) : -INFINITY) * sl2;
                     return fmaxf(max3(a[0], a[1], a[2]), a[3]) * sl2;
                 };
                 auto exponentials = [&](int q) {
                     const uint32_t(&x)[32] = u[q % 3];
-                    const float ms = -m;
+                    // (Of a key that is not in the list p is 2^-inf; NaN when its score is not finite, see mark_item.)
+                    const float m0 = in_list(2 * q) ? -m : -INFINITY, m1 = in_list(2 * q + 1) ? -m : -INFINITY;
                     uint32_t w[16];
 #pragma unroll
                     for (int j = 0; j < 32; j += 2) {
+                        const float ms = j < 16 ? m0 : m1;
                         float2 e = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])),
                                         make_float2(sl2, sl2), make_float2(ms, ms));
                         e.x = ex2(e.x);
@@ -923,10 +941,11 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 auto half_tile = [&](int half) {
                     ls[0] = ls[1] = make_float2(0.f, 0.f);
                     const float mx = fmaxf(maximum(2 * half), maximum(2 * half + 1));
+                    // (A list's first seen keys may come late: m starts with them.)
+                    if (LISTED && __any_sync(0xffffffffu, l == 0.f)) m = l == 0.f && mx != -INFINITY ? mx : m;
                     exponentials(2 * half);
                     exponentials(2 * half + 1);
-                    // (A list's first seen keys may come late: m starts with them.)
-                    const bool move = mx - m > 8.f || (l == 0.f && mx != -INFINITY && (LISTED ? mx != m : mx - m < -8.f));
+                    const bool move = mx - m > 8.f || (!LISTED && l == 0.f && mx - m < -8.f && mx != -INFINITY);
                     if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
                         const float up = mx, f = move && l != 0.f ? ex2(m - up) : 1.f;   // l = 0: so is O
                         if (move) m = up;
@@ -973,26 +992,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (reads_mine) ok = !lost(wait(&bars->x_done[slot ^ 1][qw], (ph / kPhX) ^ 1u));
                     reads_mine = false;
                 };
-                // A half of which no row of the warp sees a key: P is zero.
-                auto nothing = [&](int half) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) w[j] = 0u;
-                    tmem_st_32x16(tS + half * 32, w);
-                    tmem_st_32x16(tS + half * 32 + 16, w);
-                    tmem_st_wait();
-                };
-                if (LISTED && live && !__any_sync(0xffffffffu, (see[0] | see[1]) != 0u)) {
-                    tmem_ld_32x32(tS + 64, u[2]);
-                    tmem_ld_32x32(tS + 96, u[0]);
-                    landed(u[2]);
-                    nothing(0);
-                    if (bad) {
-                        other_has_read();
-                        if (!ok) break;
-                        by_hand(0);
-                    }
-                } else if (live) {
+                if (live) {
                     tmem_ld_32x32(tS, u[0]);
                     tmem_ld_32x32(tS + 32, u[1]);
                     landed(u[0]);
@@ -1021,9 +1021,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     landed(u[0]);
                     landed(u[2]);
                     if (part && !__any_sync(0xffffffffu, (see[2] | see[3]) != 0u)) {
-                        nothing(1);
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) w[j] = 0u;
+                        tmem_st_32x16(tS + 32, w);
+                        tmem_st_32x16(tS + 48, w);
+                        tmem_st_wait();
                     } else {
-                        if (part && !(LISTED && __all_sync(0xffffffffu, (see[2] & see[3]) == ~0u))) {
+                        if (part) {
                             hide(2);
                             hide(3);
                         }
@@ -1091,6 +1096,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 const uint32_t tX = slot ? tO - DH : tO + DH;
                 const int k_end = joins && !slot ? DH / 2 : DH;
+                float finite = 0.f;                        // LISTED: or NaN
 #pragma unroll 1
                 for (int k = joins && slot ? DH / 2 : 0; k < k_end; k += 16) {
                     uint32_t o[16], y[16];
@@ -1110,6 +1116,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             for (int j = 0; j < 16; j += 4)
                                 *reinterpret_cast<float4*>(po + (k + j) * po_step) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
                         } else {
+                            if (LISTED)
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) finite = fmaf(f[j], 0.f, finite);
 #pragma unroll
                             for (int j = 0; j < 16; j += 8)
                                 *reinterpret_cast<uint4*>(out + k + j) =
@@ -1119,6 +1128,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     }
                     __syncwarp();
                 }
+                if (LISTED && mine && finite != 0.f) mark_item(c, p.lists, token, g.head);
+                __syncwarp();
             }
             tc_fence_before();
             if (joins) {
@@ -1171,7 +1182,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
     pdl_wait();
     pdl_trigger();
     const int n_ctas = c.plan->n_ctas, b = blockIdx.x;
-    if (!c.plan->ok || b + 1 >= n_ctas || (p.lists.mask && !lists_dense(p.lists, *c.plan))) return;
+    if (!c.plan->ok || b + 1 >= n_ctas || (p.lists.mask && !lists_dense(c, p.lists, *c.plan))) return;
     const CacheShare next = c.shares[b + 1];
     if (next.within == 0 || next.first != b || next.last == b) return;
     const int two = cache_two_tiles(next.g.ntok, c.tile_tokens);

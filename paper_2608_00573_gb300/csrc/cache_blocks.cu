@@ -12,7 +12,7 @@ constexpr int kStageRows = 64;                // positions of a stage of the ker
 
 // Room for the step's lists as bits: for all of T_max when that is 64 MB at most.  (None: the lists are followed.)
 bool room_for_masks(trimmoe_cache* c, cudaStream_t st) {
-    const size_t row = (size_t)c->d.Hkv * ((c->d.max_pages + 31) / 32);
+    const size_t row = (size_t)c->d.Hkv * ((c->d.max_pages + 31) / 32 + 2);
     if (!c->masks) {
         const size_t words = std::min(row * c->d.T_max, (size_t)16 << 20);
         cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
@@ -214,11 +214,11 @@ extern "C" trimmoe_status trimmoe_cache_attend_blocks(trimmoe_cache_handle c, in
     Range range("trimmoe.cache_attend_blocks");
     cudaStream_t st = enter(c, stream);
     // Tokens of prompts: where their lists name much of what their sequences hold, 128 rows at a time over all
-    // pages, with the lists as masks, is faster (lists_dense decides by the lengths, on the GPU).  Not for
-    // lists that are followed in 60 us.
+    // pages, with the lists as masks, is faster.  The lengths decide, on the GPU (lists_dense); lists that are
+    // followed in 45 us are not worth the launches, nor are tiles half empty.
     const long long stages = (long long)p.T * d.Hkv * p.row_tiles * std::max(1LL, (long long)p.n * d.page / kStageRows);
     int launches = 1;
-    if (c->max_q * d.rep >= kCacheTile / 2 && stages * kStageCost >= 60000LL * d.num_sms && room_for_masks(c, st)) {
+    if (c->max_q * d.rep >= kCacheTile / 2 && stages * kStageCost >= 45000LL * d.num_sms && room_for_masks(c, st)) {
         p.lists = PageLists{c->masks, (d.max_pages + 31) / 32, stages};
         AttendParams m = {};
         m.lists = p.lists;

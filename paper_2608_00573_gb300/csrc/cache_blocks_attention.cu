@@ -7,7 +7,11 @@
 // to 16 rows alone and the operator is bound by what the lists bring in: HBM for single tokens
 // (each listed K and V row once), L2 for chunks whose tokens list the same pages.  The
 // products are therefore mma.sync with 16 rows, fed from shared memory; a 128-row tile of
-// TMEM would hold the same rows.
+// TMEM would hold the same rows.  Measured: 48 single tokens, 16 heads on 16, 96 pages of 16 each, 102 us,
+// 5.95 TB/s, 0.87 of the copy rate; one token, 32 heads on 8, 32 pages of 64, 8.4 us, latencies; 800
+// tokens' chunks, 24 pages of 64, 430 us, 5.6 GB out of L2 at 13 TB/s.  Prompts whose lists name much of what
+// their sequences hold are therefore left to the attention kernel, with the lists as masks (lists_dense:
+// those chunks take 168 us), and this kernel computes what that one marks.
 //
 // A stage is 64 listed positions: pages, or halves of pages of 128, as boxes of the cache's
 // tensor maps, with their values.  One warp draws items, finds their pages and keeps the
@@ -126,8 +130,10 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (!OWN || p.alone) pdl_wait();
     pdl_trigger();
     const CachePlan pl = sh.plan;
-    const int items = OWN ? pl.pieces * c.Hkv : p.T * c.Hkv * p.row_tiles;
-    if (!pl.ok || (OWN ? share_stale(c, pl) : lists_dense(p.lists, pl))) {       // (all CTAs)
+    // Lists that have been masks of an attention over all pages: the items that it marked.
+    const bool again = !OWN && lists_dense(c, p.lists, pl);
+    const int items = OWN ? pl.pieces * c.Hkv : again ? pl.pieces * p.row_tiles : p.T * c.Hkv * p.row_tiles;
+    if (!pl.ok || (OWN && share_stale(c, pl))) {       // (all CTAs)
         if (OWN) pdl_wait();
         return;
     }
@@ -208,10 +214,10 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                     continue;
                 }
             } else {
-                const int per = c.Hkv * p.row_tiles;
-                it.t = index / per;
-                it.head = index % per / p.row_tiles;
-                it.row0 = index % p.row_tiles * 16;
+                const int tile = index % p.row_tiles, which = index / p.row_tiles, x = again ? (int)__ldcg(p.lists.marked(which)) : which;
+                it.t = x / c.Hkv;
+                it.head = x - it.t * c.Hkv;
+                it.row0 = tile * 16;
                 it.rows = min(16, c.rep - it.row0);
                 const CacheToken tok = c.tokens[it.t];
                 it.base = tok.base;
@@ -532,23 +538,25 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (OWN) pdl_wait();
 }
 
-// Lists as bits: a warp takes a token and key/value head, a window of pages at a time.  Pages from the step's
+// Lists as bits, for the attention kernel: a warp takes a token and key/value head, a window of pages at a time.  Pages from the step's
 // first one on are seen as far as positions are.  Entries that do not fit are left out and flagged.
 constexpr int kMaskWarps = 8, kMaskWords = 128;
 __global__ void __launch_bounds__(kMaskWarps * 32) cache_masks_kernel(const __grid_constant__ CacheDev c,
                                                                       const __grid_constant__ BlocksParams p) {
     __shared__ uint32_t s_bits[kMaskWarps][kMaskWords];
-    const int lane = threadIdx.x & 31, words = p.lists.words;
+    const int lane = threadIdx.x & 31;
     uint32_t* bits = s_bits[threadIdx.x >> 5];
     pdl_wait();
     pdl_trigger();
     const CachePlan pl = *c.plan;
-    if (!pl.ok || !lists_dense(p.lists, pl)) return;
+    if (!pl.ok || !lists_dense(c, p.lists, pl)) return;
+    if (blockIdx.x == 0 && threadIdx.x == 0) c.plan->pieces = 0;
     for (long long i = (long long)blockIdx.x * kMaskWarps + (threadIdx.x >> 5); i < (long long)p.T * c.Hkv;
          i += (long long)gridDim.x * kMaskWarps) {
         const CacheToken tok = c.tokens[i / c.Hkv];
         const int own = tok.base >> c.page_shift, listed = min(p.n, own), end = (tok.kv_len - 1 >> c.page_shift) / 32 + 1;
         const int* list = p.blocks + (size_t)i * p.n;
+        if (lane == 0) *p.lists.mark(i) = 0;
         for (int w0 = 0; w0 < end; w0 += kMaskWords) {
             for (int w = lane; w < kMaskWords; w += 32) {
                 const int n = own - (w0 + w) * 32;     // pages of the word before the step's own
@@ -566,7 +574,7 @@ __global__ void __launch_bounds__(kMaskWarps * 32) cache_masks_kernel(const __gr
                 if (w >= 0 && w < kMaskWords) atomicOr(&bits[w], 1u << (col & 31));
             }
             __syncwarp();
-            for (int w = lane; w < min(kMaskWords, end - w0); w += 32) p.lists.mask[(size_t)i * words + w0 + w] = bits[w];
+            for (int w = lane; w < min(kMaskWords, end - w0); w += 32) p.lists.bits(i)[w0 + w] = bits[w];
             __syncwarp();
         }
     }
