@@ -211,13 +211,13 @@ struct PageLists {
 };
 
 struct AttendParams {
-    PageLists lists;
     const uint64_t* tree;
     __nv_bfloat16* out;
     int ld_out;
     int join_here;                     // the attention kernel joins cut items itself
     float scale_log2;
     int T;
+    PageLists lists;
 };
 
 // attend_blocks: q and out as for attend.

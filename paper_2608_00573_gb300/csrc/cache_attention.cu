@@ -58,6 +58,7 @@
 // positions, a token each, 199 us, 0.98 of the copy rate; one sequence of 1500 positions
 // 11.7 to 14.2 us, launches and latencies.
 #include <algorithm>
+#include <cstddef>
 #include <type_traits>
 
 #include "cache.cuh"
@@ -92,9 +93,14 @@ struct Seg {
     int t0, t1;          // key tiles
     int part;            // part buffer, -1: the whole item
 };
-// With groups of sequences: an item of their common tiles, the first row of its part.
-struct SharedSeg : Seg {
-    int common, part_row;
+// With groups of sequences, the same and more (of its own, so that offsets in BarsOf are constants, and other steps'
+// code stays as it is: with two words more in Seg ragged prompts took 55.9 us instead of 54.9).
+struct SharedSeg {
+    int valid;
+    int seq, kv_len, row, ntok, first, base, head;
+    int t0, t1;
+    int part;
+    int common, part_row;   // an item of the common tiles, the first row of its part
 };
 
 template <int MODE>
@@ -131,7 +137,8 @@ struct SegInfo {
     int kall;            // positions that every row sees
 };
 
-__device__ __forceinline__ SegInfo seg_info(const Seg& g, int tile_tokens, bool tree) {
+template <class S>
+__device__ __forceinline__ SegInfo seg_info(const S& g, int tile_tokens, bool tree) {
     SegInfo s;
     s.dual = g.ntok > tile_tokens;
     s.kmax = tree ? g.kv_len : g.first + g.ntok;
@@ -268,8 +275,8 @@ __device__ __forceinline__ size_t part_at(size_t buf, int row, int col) {
 // order of the keys; a lane takes D / 32 columns, eight sources are read at a time.  CTA
 // `first` wrote its part into its second buffer, the others into their first; each has two
 // sources, from the two slots.  Bound: latency, one or two rounds of reads.
-template <int DH>
-__device__ __forceinline__ void join_row(const CacheDev& c, const AttendParams& p, const Seg& g, int first, int last,
+template <int DH, class S>
+__device__ __forceinline__ void join_row(const CacheDev& c, const AttendParams& p, const S& g, int first, int last,
                                          int r, int lane) {
     constexpr int V = DH / 32, B = 8;
     const int sources = (last - first + 1) * 2;
@@ -322,7 +329,7 @@ __device__ __noinline__ void mark_item(const CacheDev& c, const PageLists& l, in
 // Joins 8 rows of a cut item, G times 16 columns of them, likewise; a lane has a row and 4
 // columns of each 16, two sources are read at a time (each part is one: the slots have
 // joined theirs, or have rows of their own).  Bound: L2.
-template <int DH, int G>
+template <int DH, int G, bool LISTED>
 __device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams& p, const CacheShare& sh, int rows,
                                           int r0, int k0, int lane) {
     constexpr int B = 2;
@@ -363,7 +370,7 @@ __device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams&
     const int token = sh.g.row + tile * c.tile_tokens + in / c.rep, h = sh.head * c.rep + in % c.rep;
     const float il = l == 0.f ? 0.f : 1.f / l;
     __nv_bfloat16* out = p.out + (size_t)token * p.ld_out + (size_t)h * DH + col;
-    if (p.lists.mask) {
+    if constexpr (LISTED) {
         float sum = il * 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g)
@@ -440,10 +447,10 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 
     // (Addresses of single barriers are constants beside one base register.)
     const uint32_t bb = sb + L::BYTES;
-    auto bar = [&](const void* b) {
+    auto bar = [&](const uint64_t* b) {
         return bb + (uint32_t)(reinterpret_cast<const uint8_t*>(b) - reinterpret_cast<const uint8_t*>(bars));
     };
-    const uint32_t abort_at = bar(&bars->abort_flag);
+    const uint32_t abort_at = bb + (uint32_t)offsetof(Bars, abort_flag);
     auto wait = [&](const uint64_t* b, uint32_t parity) { return wait_probes(bar(b), parity & 1u, abort_at, c.err); };
     auto lost = [](uint32_t gave_up) { return __any_sync(0xffffffffu, gave_up) != 0; };
     // Common tiles are all below a segment's `base`: like a tree's, without drafts.
@@ -451,7 +458,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if constexpr (SHARED) return tree || g.common;
         else return tree;
     };
-    auto info = [&](const SegT& g) { return seg_info(g, TT, unmasked(g)); };
     // The it-th segment of this CTA (false: none left, or aborted).
     auto next_seg = [&](int it, SegT& g) {
         const int s = it % kSegSlots;
@@ -497,7 +503,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             CacheGroup g;
             bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
             if (SHARED && any) any = !share_stale(c, pl);
-            if (LISTED && any) any = lists_dense(c, p.lists, pl);
+            if constexpr (LISTED) any = any && lists_dense(c, p.lists, pl);
             if (any && !whole) {
                 x = sh.begin;
                 x_end = sh.end;
@@ -549,7 +555,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 if (sg.t0 < sg.t1) {
                     if (!give_seg(sg)) break;
-                    const SegInfo si = info(sg);
+                    const SegInfo si = seg_info(sg, TT, unmasked(sg));
                     // Page indices of the tiles ahead travel in registers.
                     const int n_pages = (si.kmax + c.page - 1) >> c.page_shift;
                     const int* row = c.table + (size_t)sg.seq * c.max_pages;
@@ -627,7 +633,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             // The last copies have landed, and been read unless the CTA gave up, before
             // it ends.
             const uint32_t tail = min(cnt, (uint32_t)ST);
-            const uint32_t never = bar(&bars->never);
+            const uint32_t never = bb + (uint32_t)offsetof(Bars, never);
             for (uint32_t k = cnt - tail; k < cnt; ++k) wait_probes(bar(&bars->kv_full[k % ST]), (k / ST) & 1, never, c.err);
             if (nseg > 0) wait_probes(bar(&bars->q_full), (nseg - 1) & 1, never, c.err);
             for (uint32_t k = cnt - tail; k < cnt; ++k) wait(&bars->kv_empty[k % ST], k / ST);
@@ -653,7 +659,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             };
             SegT g;
             for (int it = 0; !lost(gave_up) && next_seg(it, g); ++it) {
-                const SegInfo si = info(g);
+                const SegInfo si = seg_info(g, TT, unmasked(g));
                 auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
                 const int dual = uniform(si.dual), lead = dual ? 1 : 2, nt = uniform(g.t1 - g.t0);
                 const int n0 = uniform(si.n0 - g.t0), n1 = uniform(si.n1 - g.t0);   // the slots' tiles, from the segment's first
@@ -767,7 +773,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             SegT g;
             bool ok = true;
             for (int it = 0; ok && next_seg(it, g); ++it) {
-                const SegInfo si = info(g);
+                const SegInfo si = seg_info(g, TT, unmasked(g));
                 const int lead = si.dual ? 1 : 2, nt = g.t1 - g.t0;
                 for (int i = max(0, si.kall / kCacheTile - g.t0); ok && i < nt; ++i) {
                     const int t = g.t0 + i;
@@ -835,7 +841,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int step = dual ? 1 : 2, begin = g.t0 + (dual ? 0 : slot);
             int lim, first_part, mask0;                    // tiles, first partly masked one, index of a tile among those
             {
-                const SegInfo si = info(g);
+                const SegInfo si = seg_info(g, TT, unmasked(g));
                 lim = slot ? si.n1 : si.n0;
                 first_part = si.kall / kCacheTile;
                 const int m0 = max(g.t0, first_part);
@@ -844,13 +850,15 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             const bool work = begin < lim;
             float m = 0.f, l = 0.f;                        // (no key seen yet: m is arbitrary)
-            uint32_t listed = 0;                           // LISTED: 32 pages from a multiple of 32 on
+            [[maybe_unused]] uint32_t listed = 0;          // LISTED: 32 pages from a multiple of 32 on
 #pragma unroll 1
             for (int t = begin; t < lim; t += step) {
-                const int page0 = LISTED ? t << 7 >> c.page_shift : 0;
-                if (LISTED && (t == begin || (page0 & 31) == 0 || (!dual && (page0 & 31) == kCacheTile >> c.page_shift))) {
-                    const int tok = g.row + tok0 + max(0, min(tok_in_tile, ntok - 1));
-                    listed = __ldcg(p.lists.bits((long long)tok * c.Hkv + g.head) + (page0 >> 5));
+                if constexpr (LISTED) {
+                    const int page = (t << 7 >> c.page_shift) & 31;
+                    if (t == begin || page == 0 || (!dual && page == kCacheTile >> c.page_shift)) {
+                        const int tok = g.row + tok0 + max(0, min(tok_in_tile, ntok - 1));
+                        listed = __ldcg(p.lists.bits((long long)tok * c.Hkv + g.head) + (t << 7 >> c.page_shift >> 5));
+                    }
                 }
                 ok = !lost(wait(&bars->s_full[slot], ph));
                 if (!ok) break;
@@ -885,15 +893,15 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     }
                 }
                 // LISTED: sixteens of keys whose page is in the row's list, or one of the step's own.
-                uint32_t sixteens = ~0u;
-                if (LISTED) {
-                    const uint32_t x = listed >> (page0 & 31);
+                [[maybe_unused]] uint32_t sixteens = ~0u;
+                if constexpr (LISTED) {
+                    const uint32_t x = listed >> ((t << 7 >> c.page_shift) & 31);
                     sixteens = c.page_shift == 4   ? x
                                : c.page_shift == 5 ? (x & 1u) * 3u | (x & 2u) * 6u | (x & 4u) * 12u | (x & 8u) * 24u
                                : c.page_shift == 6 ? (x & 1u) * 15u | (x & 2u) * 120u
                                                    : (x & 1u) * 255u;
                 }
-                auto in_list = [&](int i) { return !LISTED || (sixteens >> i & 1u); };
+                auto in_list = [&](int i) { return (sixteens >> i & 1u) != 0; };
                 // One pass over the scores in TMEM, a quarter (32 columns) at a time with the next
                 // load in flight, and P handed over in two halves, so that the first half's
                 // product runs under the second half's exponentials.  These start from the
@@ -917,18 +925,20 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             a[k] = max3(a[k], __uint_as_float(x[8 * k + j]), __uint_as_float(x[8 * k + j + 1]));
-                    if (LISTED)
+                    if constexpr (LISTED)
                         return fmaxf(in_list(2 * q) ? fmaxf(a[0], a[1]) : -INFINITY, in_list(2 * q + 1) ? fmaxf(a[2], a[3]) : -INFINITY) * sl2;
-                    return fmaxf(max3(a[0], a[1], a[2]), a[3]) * sl2;
+                    else
+                        return fmaxf(max3(a[0], a[1], a[2]), a[3]) * sl2;
                 };
                 auto exponentials = [&](int q) {
                     const uint32_t(&x)[32] = u[q % 3];
-                    // (Of a key that is not in the list p is 2^-inf; NaN when its score is not finite, see mark_item.)
-                    const float m0 = in_list(2 * q) ? -m : -INFINITY, m1 = in_list(2 * q + 1) ? -m : -INFINITY;
+                    float ms = -m;
                     uint32_t w[16];
 #pragma unroll
                     for (int j = 0; j < 32; j += 2) {
-                        const float ms = j < 16 ? m0 : m1;
+                        // (Of a key that is not in the list p is 2^-inf; NaN when its score is not finite, see mark_item.)
+                        if constexpr (LISTED)
+                            if (j % 16 == 0) ms = in_list(2 * q + j / 16) ? -m : -INFINITY;
                         float2 e = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])),
                                         make_float2(sl2, sl2), make_float2(ms, ms));
                         e.x = ex2(e.x);
@@ -942,10 +952,11 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     ls[0] = ls[1] = make_float2(0.f, 0.f);
                     const float mx = fmaxf(maximum(2 * half), maximum(2 * half + 1));
                     // (A list's first seen keys may come late: m starts with them.)
-                    if (LISTED && __any_sync(0xffffffffu, l == 0.f)) m = l == 0.f && mx != -INFINITY ? mx : m;
+                    if constexpr (LISTED)
+                        if (__any_sync(0xffffffffu, l == 0.f)) m = l == 0.f && mx != -INFINITY ? mx : m;
                     exponentials(2 * half);
                     exponentials(2 * half + 1);
-                    const bool move = mx - m > 8.f || (!LISTED && l == 0.f && mx - m < -8.f && mx != -INFINITY);
+                    const bool move = mx - m > 8.f || (l == 0.f && mx - m < -8.f && mx != -INFINITY);
                     if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
                         const float up = mx, f = move && l != 0.f ? ex2(m - up) : 1.f;   // l = 0: so is O
                         if (move) m = up;
@@ -1096,7 +1107,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 const uint32_t tX = slot ? tO - DH : tO + DH;
                 const int k_end = joins && !slot ? DH / 2 : DH;
-                float finite = 0.f;                        // LISTED: or NaN
+                [[maybe_unused]] float finite = 0.f;       // LISTED: or NaN
 #pragma unroll 1
                 for (int k = joins && slot ? DH / 2 : 0; k < k_end; k += 16) {
                     uint32_t o[16], y[16];
@@ -1116,7 +1127,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             for (int j = 0; j < 16; j += 4)
                                 *reinterpret_cast<float4*>(po + (k + j) * po_step) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
                         } else {
-                            if (LISTED)
+                            if constexpr (LISTED)
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) finite = fmaf(f[j], 0.f, finite);
 #pragma unroll
@@ -1128,8 +1139,10 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     }
                     __syncwarp();
                 }
-                if (LISTED && mine && finite != 0.f) mark_item(c, p.lists, token, g.head);
-                __syncwarp();
+                if constexpr (LISTED) {
+                    if (mine && finite != 0.f) mark_item(c, p.lists, token, g.head);
+                    __syncwarp();
+                }
             }
             tc_fence_before();
             if (joins) {
@@ -1176,20 +1189,22 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 // Joins the parts of cut items.  Block (b, y) takes rows [32 y, 32 y + 32) of the
 // item that CTA b of the attention began and did not finish, a warp half of the columns
 // of eight of them.
-template <int DH>
+template <int DH, bool LISTED>
 __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__ CacheDev c,
                                                          const __grid_constant__ AttendParams p) {
     pdl_wait();
     pdl_trigger();
     const int n_ctas = c.plan->n_ctas, b = blockIdx.x;
-    if (!c.plan->ok || b + 1 >= n_ctas || (p.lists.mask && !lists_dense(c, p.lists, *c.plan))) return;
+    if (!c.plan->ok || b + 1 >= n_ctas) return;
+    if constexpr (LISTED)
+        if (!lists_dense(c, p.lists, *c.plan)) return;
     const CacheShare next = c.shares[b + 1];
     if (next.within == 0 || next.first != b || next.last == b) return;
     const int two = cache_two_tiles(next.g.ntok, c.tile_tokens);
     const int rows = two ? 128 + (next.g.ntok - c.tile_tokens) * c.rep : next.g.ntok * c.rep;
     const int warp = threadIdx.x >> 5, r0 = blockIdx.y * 32 + (warp >> 1) * 8;
     if (r0 < rows)
-        join_rows<DH, DH / 32>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
+        join_rows<DH, DH / 32, LISTED>(c, p, next, rows, r0, (warp & 1) * (DH / 2), threadIdx.x & 31);
 }
 
 static_assert(smem_bytes<128, kShared>() <= 227 * 1024 && smem_bytes<64, kShared>() <= 227 * 1024, "shared memory of a block");
@@ -1215,7 +1230,7 @@ cudaError_t attend(const CacheDev& c, const CUtensorMap& tm_q, const CUtensorMap
                    c, p);
     if (e != cudaSuccess || p.join_here) return e;
     if (MODE == kShared) return e;                              // (launch_cache_join)
-    return launch_pdl(cache_join_kernel<DH>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);
+    return launch_pdl(cache_join_kernel<DH, MODE == kListed>, dim3(c.num_sms, (max_rows + 31) / 32), dim3(256), 0, st, c, p);
 }
 
 }  // namespace
