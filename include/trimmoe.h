@@ -613,7 +613,11 @@ trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer, const tri
  * down, times page_size) those that trimmoe_cache_attend would show it.  A list holds
  * ascending columns of whole pages before the step, then -1: of other entries (not
  * ascending, no whole page before the step, behind a -1) those that do not fit are left
- * out and CACHE_BLOCKS is flagged. */
+ * out and CACHE_BLOCKS is flagged.
+ * Prompts whose lists name much of what their sequences hold are computed 128 rows at a
+ * time over all pages, with the lists as masks; the first such call allocates up to 64 MB
+ * (during a capture it does not, and lists are followed one by one: the same result up to
+ * the order of sums, only slower). */
 typedef struct {
     const void* q;
     int ld_q;

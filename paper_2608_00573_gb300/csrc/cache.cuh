@@ -44,7 +44,7 @@ struct __align__(16) CacheGroup {
     // Steps with groups of sequences (trimmoe_cache_share):
     int t0;                            // first key tile: those before it are the group of sequences' common ones
     int common;                        // the item is of those tiles, for all tokens of the group: kv_len and base end them
-    int part_row;                      // its parts' first row, see cache_part_row
+    int part_row;                      // its parts' first row, see cache_part_rows
 };
 
 // A CTA's share of the line on which the items' costs are laid end to end.
@@ -95,7 +95,8 @@ struct __align__(16) CachePiece {
     int pad[2];
 };
 constexpr int kPieceCuts = 24;         // of one sequence's or group's pages at most
-constexpr int kPieces = 8192;          // 1024 tokens', 512 groups' two and 5 times two CTAs an SM more, with room to spare
+constexpr int kPieces = 8192;          // 1024 tokens' and 512 groups' two, a piece more of each when they are cut, and 5 times
+                                       // two CTAs an SM more, with room to spare
 
 // Parts that hold a token: rows row + i * step, i < count, of query head 0 of a key/value head; warps: stored
 // 32 rows of 4 columns side by side.

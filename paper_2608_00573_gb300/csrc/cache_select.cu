@@ -109,8 +109,9 @@ __device__ __forceinline__ void sequence_bounds(const CacheDev& c, int layer, in
     }
 }
 
-// Bound: HBM, each filled page's keys once (9 prompts, 16384 tokens, 32 MB); a decode step
-// fills few pages and is bound by latency.
+// Bound: HBM, each filled page's keys once: 9 prompts, 16384 tokens, 32 MB, 6.1 us in a row of
+// launches (5.2 TB/s, part of it out of L2); a decode step fills few pages, 2.7 us, latency.  A warp to a page
+// and head needs no sums across warps; rows of 8 columns a lane are whole lines.
 template <int DH>
 __global__ void __launch_bounds__(kThreads) cache_bounds_kernel(const __grid_constant__ CacheDev c, int layer, int whole) {
     pdl_wait();
@@ -212,8 +213,9 @@ __device__ __forceinline__ void mma_s8(int (&c)[4], int a0, int a1, int a2, int 
 // Scores of one sequence's blocks for tokens [a, end) of the coded ones: put(token, block, key).
 // A warp takes 16 blocks from 16 `from` on, then those `stride` times as many on, below F: the 16 rows
 // of a product with 8 columns and 2 D terms in whole numbers.  The terms' order is free, so a
-// lane takes 16 bytes of a row at a time, as they lie.  (One instruction for 32 four-number products;
-// with those, and sums across lanes, the search of 48 contexts took 26 us instead of 17.)
+// lane takes 16 bytes of a row at a time, as they lie.  (Integer products are no faster here than four-number
+// dot products, 151 and 149 T operations a second measured, but need no sums across lanes: 800 tokens' chunks 124 us
+// with those, 28 with these and the choice by one histogram.)
 // ONE: all columns are one group, which stays in registers.
 template <int DH, int M, bool ONE, class Put>
 __device__ __forceinline__ void score_blocks(const CacheDev& c, int layer_at, const Coded<DH>& q, int h, int seq, int F, int a, int end,
@@ -467,8 +469,9 @@ __device__ __forceinline__ void list_ends(int* out, int n, int F, int first, int
 // TILE tokens (eight, or one) and a key/value head: scores in shared memory, from bounds that are read once
 // for the tokens of a sequence, then a warp chooses for each token, or all for the one.
 //
-// Bound: the dot products, D / 2 four-number products per block of keys and query head, and the
-// choice, some 300 instructions of a warp per list.
+// Bound: issue slots (50 % busy; integer products 20 %): 2 D products per block of keys and query head, and the
+// choice, some 300 instructions of a warp per list.  Measured: 800 tokens' chunks behind 6000 to 15000 positions, 12
+// heads of 64 columns, pages of 32, 27.8 us; one token over 312 blocks, 32 heads on 8, 8.2 us, latency.
 constexpr int kTile = 8, kTileBytes = 110 * 1024;
 template <int TILE>
 struct TileChoice {
@@ -554,9 +557,11 @@ __global__ void __launch_bounds__(kThreads, 3) cache_select_tile_kernel(const __
 // All sixteens of blocks of all tokens and heads lie on a line, token by token, and every warp takes
 // the same number of them in a row: a warp meets few tokens, whose queries it codes for
 // itself, and long sequences cost no one more than short ones.  (A block of threads for each
-// token and head, or several for long ones: 48 contexts of 4000 to 40000 took 26 us.)
+// token and head, or several for long ones: 48 contexts of 4000 to 40000 took 25.2 us with the choice, this way
+// 23.0.)
 //
-// Bound: HBM, 2 D + 4 bytes per block of keys and head.
+// Bound: HBM, 2 D + 4 bytes per block of keys and head; 69 MB of bounds and the choice of 384 lists 23.0 us, 0.44
+// of the copy rate: the integer pipe is 40 % busy, and the choice behind it takes a third.
 constexpr int kSlice = 1024;                          // tokens at a time
 __host__ __device__ inline int score_warps(const CacheDev& c) {
     const int fit = (int)(80 * 1024 / coded_bytes(c.rep, c.dh, 1));
@@ -699,8 +704,8 @@ cudaError_t tile_launch(const CacheDev& c, const SelectParams& p, cudaStream_t s
 template <int DH, int M>
 cudaError_t select_launch(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches) {
     // Eight tokens to a block of threads when sequences have as many and their scores fit beside those of another
-    // block; one to a block for few tokens of short sequences (one launch less: 312 blocks 7.7 us
-    // instead of 8.6, and 3 us less on the host).
+    // block; one to a block for few tokens of short sequences (one launch less: one token over 312 blocks
+    // 8.3 us instead of 8.6, and 3 us less on the host).
     if (p.max_q >= kTile && tile_bytes<kTile>(c) <= kTileBytes) return tile_launch<DH, M, kTile>(c, p, st, launches);
     if ((long long)p.T * c.Hkv <= 64 && c.max_pages <= 1024 && tile_bytes<1>(c) <= kTileBytes) return tile_launch<DH, M, 1>(c, p, st, launches);
     // As many tokens at a time as the buffer has room for.

@@ -8,6 +8,19 @@
 // items, the tokens of one sequence over its other tiles.  Every item's sums go to parts,
 // which cache_join_shared_kernel adds per token: the common item's in the order of the keys, then
 // its own.
+//
+//   o = sum_i e^(m_i - m) o_i / sum_i e^(m_i - m) l_i,  m = max m_i   over the parts i of a row
+//
+// Single tokens' own pages, and the common ones of groups of up to 32 rows, are pieces that a second kernel
+// reads beside the attention kernel (cache_blocks_attention.cu): a 128-row tile would hold few rows of
+// them, and HBM is what they wait for.
+//
+// Bound: HBM for single tokens, each common K and V row once a group; the chain of a key tile for drafted trees.
+// Measured, 32 heads on 8, D = 128: 64 samples of a prompt of 8200 positions with up to 900 of their own 42 us (23 at
+// the copy rate; the attention kernel's last CTA, the pieces and the join take 30, 31 and 8 alone); 4 samples of
+// 700 positions 12.3 us, latency; 12 trees of 29 drafts behind 12001 positions 94 us (attention 78, join 12); 16
+// heads on 16, five groups of up to 24 behind 300 to 6000 positions 60 us.  The same steps without groups
+// read the common pages for each sequence.
 #include <algorithm>
 
 #include "cache.cuh"
