@@ -177,11 +177,12 @@ extern "C" trimmoe_status trimmoe_cache_step(trimmoe_cache_handle c, int n, cons
     trimmoe_status s = check_list(c, "cache_step", n, seq);
     if (s != TRIMMOE_OK) return s;
     if (n > 0 && !q_len) return c->fail(TRIMMOE_ERR_ARG, "cache_step", "NULL argument");
-    long long T = 0;
+    long long T = 0, triangle = 0;
     int most = 0;
     for (int i = 0; i < n; ++i) {
         if (q_len[i] < 0) return c->fail(TRIMMOE_ERR_ARG, "cache_step", "q_len must be >= 0");
         T += q_len[i];
+        triangle += q_len[i] * (q_len[i] + 1LL) / 2;
         most = std::max(most, q_len[i]);
     }
     if (T > c->cfg.T_max) return c->fail(TRIMMOE_ERR_ARG, "cache_step", "more than T_max new tokens");
@@ -193,6 +194,7 @@ extern "C" trimmoe_status trimmoe_cache_step(trimmoe_cache_handle c, int n, cons
     c->T = (int)T;
     c->n = n;
     c->max_q = most;
+    c->triangle = triangle;
     c->d.shared = 0;
     return TRIMMOE_OK;
 }

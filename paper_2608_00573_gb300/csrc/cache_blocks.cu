@@ -216,9 +216,10 @@ extern "C" trimmoe_status trimmoe_cache_attend_blocks(trimmoe_cache_handle c, in
     // Tokens of prompts: where their lists name much of what their sequences hold, 128 rows at a time over all
     // pages, with the lists as masks, is faster.  The lengths decide, on the GPU (lists_dense); lists that are
     // followed in 45 us are not worth the launches, nor are tiles half empty.
-    const long long stages = (long long)p.T * d.Hkv * p.row_tiles * std::max(1LL, (long long)p.n * d.page / kStageRows);
+    const long long rows = (long long)p.T * std::max(1LL, (long long)p.n * d.page / kStageRows) + c->triangle / kStageRows;
+    const long long stages = rows * d.Hkv * p.row_tiles;
     int launches = 1;
-    if (c->max_q * d.rep >= kCacheTile / 2 && stages * kStageCost >= 45000LL * d.num_sms && room_for_masks(c, st)) {
+    if (c->max_q >= (kCacheTile / 2 + d.rep - 1) / d.rep && stages * kStageCost >= 45000LL * d.num_sms && room_for_masks(c, st)) {
         p.lists = PageLists{c->masks, (d.max_pages + 31) / 32, stages};
         AttendParams m = {};
         m.lists = p.lists;

@@ -308,6 +308,35 @@ def test_attend_blocks_of_prompts_values_that_are_not_finite():
     check_blocks(cache, m, x, q, bad, out, 0, tokens={6, 7, 8})
 
 
+def test_attend_blocks_of_a_fresh_prompt():
+    """Nothing comes before the step, so that lists are empty: attend, 128 rows at a time."""
+    shapes, page, q = (8, 2, 128), 64, [2000, 1, 130]
+    cache, m, x = filled(shapes, page, [0, 700, 63], q, seed=8)
+    blocks = lists_of(m, q, 20, 2)
+    before = cache.stats()["launches"]
+    out = cache.attend_blocks(0, x, blocks)
+    assert cache.stats()["launches"] - before == 4
+    check_blocks(cache, m, x, q, blocks, out, 0, tokens=some_tokens(q, 30, 7))
+    assert torch.equal(cache.attend_blocks(0, x, torch.full((sum(q), 2, 0), -1, dtype=torch.int32, device=DEV))[:2000], out[:2000])
+
+
+def test_attend_blocks_of_prompts_beside_queries_and_with_groups():
+    """Results beside the queries in rows of one buffer; steps with groups of sequences."""
+    shapes, page, ctx, q, n = MANY["page64"]
+    cache, m, x = filled(shapes, page, ctx, q, seed=4)
+    cache.v[1, m.own[0][3], 1, 5, 7] = float("nan")
+    blocks = lists_of(m, q, n, 2, fill="some")
+    eager = cache.attend_blocks(1, x, blocks)
+    check_blocks(cache, m, x, q, blocks, eager, 1, tokens=some_tokens(q, 20, 9))
+    both = torch.cat([x, torch.zeros_like(x)], 1)
+    before = cache.stats()["launches"]
+    cache.attend_blocks(1, both[:, :1024], blocks, out=both[:, 1024:])
+    assert cache.stats()["launches"] - before == 4
+    assert torch.equal(both[:, 1024:].view(torch.int16), eager.view(torch.int16)) and torch.equal(both[:, :1024], x)
+    cache.share([2, 1])
+    assert torch.equal(cache.attend_blocks(1, x, blocks).view(torch.int16), eager.view(torch.int16))
+
+
 def test_attend_blocks_of_many_trees():
     shapes, page, ctx, q = (8, 2, 128), 64, [1700 + 91 * i for i in range(8)], [64] * 6 + [33, 50]
     cache, m, x = filled(shapes, page, ctx, q, seed=3)
