@@ -125,9 +125,11 @@ __host__ __device__ inline int cache_part_rows(int ntok, int tile_tokens, int re
 // With groups of sequences: cost of a key tile (both query tiles', when an item has two) and of an
 // item's beginning and end, in kShareUnit us.  (Measured: 0.9 to 1.5, 1.4 to 1.9 and 3.2 to 4.4 us;
 // sequences' own items are short, so this matters more than in other steps: with a tile and an end
-// alike, the last CTA of 12 drafted trees ended at 97 us, the others at 63.)
+// alike, the last CTA of 12 drafted trees ended at 97 us, the others at 63.  As 7, 4 and 16 here: those trees 94.0 us,
+// 4 groups of 2 to 9 trees of 29, 16 heads on 16, 104; as 7, 5, 16 95.5 and 107, 8, 5, 16 94.8 and 104, 6, 5, 16 97
+// and 111, 7, 6, 16 98 and 110, 7, 5, 12 95.7 and 106, 7, 5, 28 97.6 and 110.)
 constexpr float kShareUnit = 0.25f;
-__host__ __device__ inline int share_tile(int two) { return two ? 7 : 5; }
+__host__ __device__ inline int share_tile(int two) { return two ? 7 : 4; }
 constexpr int kShareEnds = 16;
 __host__ __device__ inline int share_tiles(int cost, int two) { return (cost - kShareEnds) / share_tile(two); }
 // Key tiles that the first x of an item's cost cover.

@@ -382,9 +382,11 @@ inline __host__ __device__ int join_heads(const CacheDev& c) {
     const int n = 1024 / (c.rep * c.dh);
     return n < 1 ? 1 : n < kJoinHeads ? n : kJoinHeads;
 }
-// B: parts that a thread reads at a time; with few blocks of threads their latency is what counts.
+// B: parts that a thread reads at a time.  With few blocks of threads their latency is what counts (64 samples, 12 at a
+// time 42 us, 6 at a time 44); with many, how many threads an SM holds (12 trees 3 at a time with 6 blocks an SM 92.5 us, 4 with
+// 5 93.5, 6 with 4 95, 2 with 8 94, 12 with 2 102; 6 prompts of 200 to 400 tokens behind a common 6000 212 / 216 / 228 / 216 / 259).
 template <int DH, int B>
-__global__ void __launch_bounds__(256, B > 6 ? 2 : 4) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
+__global__ void __launch_bounds__(256, B > 3 ? 2 : 6) cache_join_shared_kernel(const __grid_constant__ CacheDev c,
                                                                    const __grid_constant__ AttendParams p) {
     __shared__ PartList s_parts[kJoinHeads * 2];
     const int most = join_heads(c), blocks = (c.Hkv + most - 1) / most;
@@ -434,9 +436,9 @@ cudaError_t launch_cache_join(const CacheDev& c, const AttendParams& p, cudaStre
     const bool few = grid.x <= 2u * c.num_sms;
     if (c.dh == 64)
         return few ? launch_pdl(cache_join_shared_kernel<64, 12>, grid, dim3(256), 0, st, c, p)
-                   : launch_pdl(cache_join_shared_kernel<64, 6>, grid, dim3(256), 0, st, c, p);
+                   : launch_pdl(cache_join_shared_kernel<64, 3>, grid, dim3(256), 0, st, c, p);
     return few ? launch_pdl(cache_join_shared_kernel<128, 12>, grid, dim3(256), 0, st, c, p)
-               : launch_pdl(cache_join_shared_kernel<128, 6>, grid, dim3(256), 0, st, c, p);
+               : launch_pdl(cache_join_shared_kernel<128, 3>, grid, dim3(256), 0, st, c, p);
 }
 
 }  // namespace tmoe
