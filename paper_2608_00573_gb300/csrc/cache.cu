@@ -115,6 +115,7 @@ extern "C" trimmoe_status trimmoe_cache_create(const trimmoe_cache_config* cfg, 
         d.length = st->length;
         d.ref = st->ref;
         c->stamp.assign(cfg->max_seqs, 0u);
+        c->q_len.assign(cfg->max_seqs, 0);
         cudaError_t e = cudaSuccess;
         auto alloc = [&](auto*& p, size_t n) {
             if (e != cudaSuccess) return;
@@ -195,6 +196,7 @@ extern "C" trimmoe_status trimmoe_cache_step(trimmoe_cache_handle c, int n, cons
     c->n = n;
     c->max_q = most;
     c->triangle = triangle;
+    std::copy(q_len, q_len + n, c->q_len.begin());
     c->d.shared = 0;
     return TRIMMOE_OK;
 }

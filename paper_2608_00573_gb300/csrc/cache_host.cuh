@@ -24,6 +24,7 @@ struct trimmoe_cache {
     cudaStream_t last_stream = nullptr;
     uint64_t launches = 0;
     int T = -1, n = 0, max_q = 0;             // the current step (T < 0: none)
+    std::vector<int> q_len;                   // [max_seqs] of its listed sequences
     long long triangle = 0;                   // pairs of new tokens of a sequence, the later one sees the other or is it
     // With groups of sequences: what attend launches beside the attention kernel for single tokens and what
     // behind both (set by cache_share).

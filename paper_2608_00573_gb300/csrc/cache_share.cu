@@ -18,9 +18,9 @@
 // Bound: HBM for single tokens, each common K and V row once a group; the chain of a key tile for drafted trees.
 // Measured, 32 heads on 8, D = 128: 64 samples of a prompt of 8200 positions with up to 900 of their own 42 us (23 at
 // the copy rate; the attention kernel's last CTA, the pieces and the join take 30, 31 and 8 alone); 4 samples of
-// 700 positions 12.3 us, latency; 12 trees of 29 drafts behind 12001 positions 94 us (attention 78, join 12); 16
+// 700 positions 12.0 us, latency; 24 trees of 16 drafts behind 5000 positions 67 us; 16
 // heads on 16, five groups of up to 24 behind 300 to 6000 positions 60 us.  The same steps without groups
-// read the common pages for each sequence.
+// read the common pages for each sequence (when, and what both sides take: trimmoe_cache_share).
 #include <algorithm>
 
 #include "cache.cuh"

@@ -178,6 +178,22 @@ def test_what_attend_launches(lib):
         assert c.launched() == ["share"]
 
 
+def test_groups_that_fill_as_many_tiles_as_their_sequences(lib):
+    """64 tokens to a tile: groups are taken up when they halve the tiles."""
+    with Cache(lib, T_max=400) as c:
+        for q, counts, want in (((60, 60, 60), [3], []), ((20, 20, 20), [3], ["share"]), ((32, 32, 1), [3], []),
+                                ((31, 32, 1), [3], ["share"]), ((2, 2, 2), [1, 1, 1], []), ((2, 2, 0), [2, 1], ["share"])):
+            c.step(*q)
+            c.launched()
+            assert c.share(*counts)[0] == 0 and c.launched() == want, q
+            assert c.attend() == ["join"] * len(want)
+        c.step(20, 20, 20)
+        c.share(3)
+        c.share(1, 1, 1)                              # the last one counts
+        c.launched()
+        assert c.attend() == []
+
+
 def test_bounds_and_selection_refuse(lib):
     with Cache(lib) as c:
         p = c.p

@@ -71,6 +71,9 @@ CASES = {
     "heads_16": ((16, 1, 128), 64, [2500, 400], [2, 3], 70, lambda s: 1),
     "many_sequences": ((4, 2, 64), 16, [300, 130] * 30, [5, 12] * 30, 60, lambda s: int(s % 7 != 0)),
     "all_idle_but_one": ((8, 2, 128), 64, [700], [4], 50, lambda s: int(s == 2)),
+    "ragged_few": ((8, 2, 128), 64, [513], [40], 200, lambda s: 129 if s == 3 else s % 8),
+    "ragged_few_d64": ((12, 12, 64), 32, [900, 300], [12, 5], 100, lambda s: 1 + s * 3 % 11),
+    "ragged_few_heads_7": ((14, 2, 128), 16, [2000, 130], [30, 12], 300, lambda s: 1 + s % 4),
     "first_idle": ((8, 2, 128), 64, [700, 400], [4, 3], 50, lambda s: int(s not in (0, 1, 4))),
 }
 
@@ -97,18 +100,23 @@ def test_attend_shared(name):
     assert cache.stats()["device_error"] == 0
 
 
+@pytest.mark.parametrize("large", [False, True])
 @pytest.mark.parametrize("shapes,page", [((8, 2, 128), 64), ((6, 6, 64), 16), ((40, 5, 128), 128)])
-def test_attend_shared_tree(shapes, page):
-    sizes, q = [3, 4], [17, 64, 1, 40, 64, 33, 2]
-    cache, m, step, g = grouped(shapes, page, [400, 131], sizes, [0, 40, 5, 3, 100, 64, 17], slots=8)
-    step(range(7), q)
+def test_attend_shared_tree(shapes, page, large):
+    """Large trees fill query tiles by themselves (but with one query head each) and are attended as without groups."""
+    sizes, q = ([3, 4], [17, 64, 1, 40, 64, 33, 2]) if large else ([6, 9], [5, 12, 1, 9, 3, 12, 8, 2, 11, 4, 12, 1, 6, 7, 3])
+    n = sum(sizes)
+    cache, m, step, g = grouped(shapes, page, [400, 131], sizes, [(s * 40) % 101 for s in range(n)], slots=8)
+    step(range(n), q)
     fill(cache, m, g)
     x = torch.randn((sum(q), shapes[0] * shapes[2]), generator=g, device=DEV).to(torch.bfloat16)
     rng = random.Random(5)
     words = [rng.getrandbits(64) for _ in range(sum(q))]
     words[0] = 0
     tree = torch.tensor([w - (1 << 64) if w >> 63 else w for w in words], dtype=torch.int64, device=DEV)
+    before = cache.stats()["launches"]
     cache.share(sizes)
+    assert cache.stats()["launches"] - before == (0 if large and shapes[0] > shapes[1] else 2)
     check_attend(cache, m, x, q, cache.attend(1, x, tree=tree), 1, tree=words)
     check_attend(cache, m, x, q, cache.attend(1, x, tree=tree, scale=0.05), 1, tree=words, scale=0.05)
     assert cache.stats()["device_error"] == 0
@@ -182,13 +190,16 @@ def test_groups_that_share_nothing():
 
 def test_more_rows_than_groups_are_made_for():
     """65536 query rows and one more token: with groups, then as without."""
-    for q in (255, 256):
-        cache, m, step, g = grouped((128, 1, 64), 64, [200], [2], [0, 0], slots=8)
-        step(range(2), [257, q])
+    for last in (16, 17):
+        q = [16] * 255 + [last]
+        cache, m, step, g = grouped((16, 16, 64), 64, [200], [256], [0] * 256, slots=2, layers=1, T_max=4097)
+        step(range(256), q)
         fill(cache, m, g)
-        x = torch.randn((257 + q, 128 * 64), generator=g, device=DEV).to(torch.bfloat16)
-        cache.share([2])
-        check_attend(cache, m, x, [257, q], cache.attend(0, x), 0)
+        x = torch.randn((sum(q), 16 * 64), generator=g, device=DEV).to(torch.bfloat16)
+        before = cache.stats()["launches"]
+        cache.share([256])
+        assert cache.stats()["launches"] - before == (2 if last == 16 else 0)
+        check_attend(cache, m, x, q, cache.attend(0, x), 0)
         assert cache.stats()["device_error"] == 0
 
 
