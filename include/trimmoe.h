@@ -559,9 +559,11 @@ trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer, const tri
  * sequence.  The result is that of the call without groups, up to the order of
  * fp32 sums.  A group of one sequence, or without common pages, is right too.
  * A step of more than 65536 query rows (tokens times q_heads) is attended as
- * without groups, and so is one of several tokens per sequence that fill more than half as
- * many tiles of 128 rows (tokens times q_heads / kv_heads) group by group as they do sequence by
- * sequence: products are the bound there.
+ * without groups.  So is one of several tokens per sequence (or more than 16 query heads
+ * per key/value head) whose tokens fill more than half as many tiles of 128 rows (tokens
+ * times q_heads / kv_heads) group by group as they do sequence by sequence, groups of one
+ * left out, or where groups of one have four fifths of the tiles: products are the bound
+ * there.
  * The first call allocates workspaces (about 225 MB at head_dim 128) and so must not be
  * captured; later ones may be. */
 trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, const int32_t* counts, void* stream);

@@ -57,19 +57,21 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
     // that read common pages out of L2 each for itself are as fast.  (With groups against without, 12 trees behind a common
     // 12000 positions, 32 heads on 8: 2 tokens each, 0.08 of the tiles, 31 us / 76; 8, 0.25, 49 / 77; 16, 0.5, 65 / 84; 20,
     // 0.67, 74 / 85; 24, 0.75, 86 / 85; 29, 0.92, 92 / 85; behind 2000: 4 tokens 27 / 33; 12, 0.42, 34 / 33; 16, 36 / 33; 24,
-    // 41 / 34; 6 prompts of 200 to 400 behind 6000 211 / 185.)
+    // 41 / 34; 6 prompts of 200 to 400 behind 6000 211 / 185.)  Nor where groups of one have most of the tiles: all items' parts are
+    // joined then (of 32 trees of 8 tokens behind 6000 positions 32, 16, 8, 4 in a group: 68, 100, 105, 104 us, without 99; 16 heads on
+    // 16, 3000: 69, 107, 121, 126, without 125).
     if (c->max_q > 1 || c->d.rep > 16) {
         auto tiles = [&](long long tokens) { return (tokens + c->d.tile_tokens - 1) / c->d.tile_tokens; };
-        long long shared = 0, alone = 0;
+        long long shared = 0, alone = 0, others = 0;
         for (int i = 0, at = 0; i < n; ++i) {
             long long tokens = 0;
             for (int k = 0; k < counts[i]; ++k, ++at) {
                 tokens += c->q_len[at];
-                alone += tiles(c->q_len[at]);
+                (counts[i] > 1 ? alone : others) += tiles(c->q_len[at]);
             }
-            shared += tiles(tokens);
+            if (counts[i] > 1) shared += tiles(tokens);
         }
-        if (2 * shared > alone) {
+        if (2 * shared > alone || 4 * alone <= others) {
             c->d.shared = 0;
             return TRIMMOE_OK;
         }

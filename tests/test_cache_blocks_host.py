@@ -182,7 +182,8 @@ def test_groups_that_fill_as_many_tiles_as_their_sequences(lib):
     """64 tokens to a tile: groups are taken up when they halve the tiles."""
     with Cache(lib, T_max=400) as c:
         for q, counts, want in (((60, 60, 60), [3], []), ((20, 20, 20), [3], ["share"]), ((32, 32, 1), [3], []),
-                                ((31, 32, 1), [3], ["share"]), ((2, 2, 2), [1, 1, 1], []), ((2, 2, 0), [2, 1], ["share"])):
+                                ((31, 32, 1), [3], ["share"]), ((2, 2, 2), [1, 1, 1], []), ((2, 2, 0), [2, 1], ["share"]),
+                                ((2, 2, 200), [2, 1], ["share"]), ((2, 0, 250), [2, 1], [])):
             c.step(*q)
             c.launched()
             assert c.share(*counts)[0] == 0 and c.launched() == want, q
