@@ -358,22 +358,21 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
-// One more source of a row: its maximum and sum (x), added to top and l; fa and fb are the
-// factors of what was summed before and of the source.  False: nothing was summed in it.
-__device__ __forceinline__ bool join_source(float2 x, bool there, float& top, float& l, float& fa, float& fb) {
-    there = there && x.x != -INFINITY;
+// One more source of a row (there: it is one): its maximum and sum (x), added to top and l; fa and fb are the
+// factors of what was summed before and of the source.  A source that saw nothing is (-inf, 0) and adds 0.  The
+// maximum says nothing of NaN, which fmaxf leaves out: (-inf, NaN) is a source of NaN scores, and they stay.
+__device__ __forceinline__ void join_source(float2 x, bool there, float& top, float& l, float& fa, float& fb) {
     const float m = there ? fmaxf(top, x.x) : top, ref = m == -INFINITY ? 0.f : m;
     fa = ex2(top - ref);
     fb = ex2(x.x - ref);
     top = m;
     l = there ? l * fa + x.y * fb : l;
-    return there;
 }
 
 // Adds a source's four columns of a row.  (Without a branch: loads would be moved behind it, one by one.)
 __device__ __forceinline__ void add_source(float2 ml, float4 x, bool there, float& top, float& l, float (&a)[4]) {
     float fa, fb;
-    there = join_source(ml, there, top, l, fa, fb);
+    join_source(ml, there, top, l, fa, fb);
     a[0] = there ? a[0] * fa + x.x * fb : a[0];
     a[1] = there ? a[1] * fa + x.y * fb : a[1];
     a[2] = there ? a[2] * fa + x.z * fb : a[2];

@@ -303,7 +303,8 @@ __device__ __forceinline__ void join_row(const CacheDev& c, const AttendParams& 
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             float fa, fb;
-            const bool there = join_source(ml[i], s0 + i < sources, top, l, fa, fb);
+            const bool there = s0 + i < sources && ml[i].x != -INFINITY;   // (-inf: no key seen, see part_ml's writer)
+            join_source(ml[i], there, top, l, fa, fb);
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[j] = there ? acc[j] * fa + o[i][j] * fb : acc[j];
         }
@@ -356,7 +357,8 @@ __device__ __forceinline__ void join_rows(const CacheDev& c, const AttendParams&
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             float fa, fb;
-            const bool there = join_source(ml[i], s0 + i < sources, top, l, fa, fb);
+            const bool there = s0 + i < sources && ml[i].x != -INFINITY;   // (-inf: no key seen, see part_ml's writer)
+            join_source(ml[i], there, top, l, fa, fb);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const float x[4] = {o[i][g].x, o[i][g].y, o[i][g].z, o[i][g].w};

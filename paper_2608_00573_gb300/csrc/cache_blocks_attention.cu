@@ -450,7 +450,8 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                 if ((lane & 3) == 0) sh.ml[warp][r + 8 * i] = make_float2(m[i], l[i]);
             }
             readers_sync();
-            // All warps' sums relative to the largest maximum.
+            // All warps' sums relative to the largest maximum; those of a warp that saw nothing, or no score above
+            // -inf, are times 0.  (Not left out: where its scores are NaN its maximum is -inf and its sums are NaN.)
             float top[2], sum[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -458,12 +459,13 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                 sum[i] = 0.f;
 #pragma unroll
                 for (int w = 0; w < kReaders; ++w) top[i] = fmaxf(top[i], sh.ml[w][r + 8 * i].x);
+                const float ref = top[i] == -INFINITY ? 0.f : top[i];
 #pragma unroll
                 for (int w = 0; w < kReaders; ++w) {
                     const float2 ml = sh.ml[w][r + 8 * i];
-                    sum[i] += ml.x == -INFINITY ? 0.f : ml.y * ex2(ml.x - top[i]);
+                    sum[i] += ml.y * ex2(ml.x - ref);
                 }
-                const float f = m[i] == -INFINITY ? 0.f : ex2(m[i] - top[i]);
+                const float f = ex2(m[i] - ref);
 #pragma unroll
                 for (int k = 0; k < DH / 8; ++k) {
                     o[k][2 * i] *= f;
