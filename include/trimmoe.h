@@ -63,7 +63,8 @@ enum {
     /* Reported by trimmoe_cache_stats of a cache handle. */
     TRIMMOE_DEVERR_CACHE_ATTENTION = 7, /* cache attention kernel */
     TRIMMOE_DEVERR_CACHE_FULL = 8,     /* step: too few free pages, or a sequence longer than max_pages */
-    TRIMMOE_DEVERR_CACHE_STATE = 9,    /* table, length or ref hold values that no call writes */
+    TRIMMOE_DEVERR_CACHE_STATE = 9,    /* table, length or ref hold values that no call writes, or an attend that was
+                                          captured with groups met others (trimmoe_cache_share) */
     TRIMMOE_DEVERR_CACHE_PATH = 10,    /* accept: n_acc or a path that does not fit the sequence's drafts */
     TRIMMOE_DEVERR_CACHE_BLOCKS = 11   /* attend_blocks: a list that is not ascending columns before the step */
 };
@@ -565,7 +566,11 @@ trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer, const tri
  * left out, or where groups of one have four fifths of the tiles: products are the bound
  * there.
  * The first call allocates workspaces (about 225 MB at head_dim 128) and so must not be
- * captured; later ones may be. */
+ * captured; later ones may be.  A captured attend reads the list that it finds: replayed behind a
+ * later step it needs a share of that step that takes its groups up, of as many tokens, single ones or not as those
+ * of its capture.  One that was captured with small groups alone (single tokens, at most two tiles
+ * of 16 rows each, 16 / (q_heads / kv_heads) tokens to a tile) does not serve larger ones with a common prompt.
+ * Where these do not hold it writes nothing and CACHE_STATE is flagged. */
 trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, const int32_t* counts, void* stream);
 
 /* Bounds of the keys of whole pages ("blocks"), for trimmoe_cache_select: per layer, page,

@@ -274,6 +274,8 @@ extern "C" trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer
     const int max_rows = c->max_q > d.tile_tokens ? 2 * kCacheTile : c->max_q * d.rep;
     p.join_here = !d.shared && max_rows <= kJoinHereRows;
     p.T = c->T;
+    p.single = single;
+    p.alone = alone;
     OnDevice on(c->dev);
     Range range("trimmoe.cache_attend");
     cudaStream_t st = enter(c, stream);
@@ -384,7 +386,8 @@ extern "C" trimmoe_status trimmoe_cache_stats(trimmoe_cache_handle c, trimmoe_ca
     if (code == TRIMMOE_DEVERR_CACHE_FULL)
         return c->fail(TRIMMOE_ERR_CACHE, "cache_step", "too few free pages, or a sequence longer than max_pages");
     if (code == TRIMMOE_DEVERR_CACHE_STATE)
-        return c->fail(TRIMMOE_ERR_CACHE, "cache", "table, length or ref hold invalid values");
+        return c->fail(TRIMMOE_ERR_CACHE, "cache",
+                       "table, length or ref hold invalid values, or an attend captured with groups met other ones");
     if (code == TRIMMOE_DEVERR_CACHE_PATH)
         return c->fail(TRIMMOE_ERR_CACHE, "cache_accept", "n_acc or path does not fit the drafts");
     if (code == TRIMMOE_DEVERR_CACHE_BLOCKS)

@@ -67,6 +67,8 @@ struct __align__(16) CachePlan {
     int pieces;                        // with groups of sequences and single tokens: what is not on the line; lists as
                                        // masks: items to be computed again
     int serial;                        // of the step (a list with groups is of the step with its number)
+    // Lists with groups: what the attend that reads them has to be made for.
+    int tokens, single;                // of the step; of single tokens (pieces and common items, see launch_cache_own)
 };
 
 __host__ __device__ inline int cache_two_tiles(int ntok, int tile_tokens) { return ntok > tile_tokens ? 1 : 0; }
@@ -221,6 +223,7 @@ struct AttendParams {
     float scale_log2;
     int T;
     PageLists lists;
+    int single, alone;                 // with groups: of single tokens; all of them small (no attention kernel)
 };
 
 // attend_blocks: q and out as for attend.
@@ -319,9 +322,12 @@ __device__ __forceinline__ bool lists_dense(const CacheDev& c, const PageLists& 
     return l.mask && (long long)kDenseEnds * c.num_sms + pl.total * kDenseCost <= l.stages * kStageCost;
 }
 
-// A list with groups is not of the last step (a captured attend replayed without its share).
-__device__ __forceinline__ bool share_stale(const CacheDev& c, const CachePlan& pl) {
-    const bool stale = pl.serial != __ldcg(&c.step_plan->serial);
+// A list with groups is not one that this attend's launches compute: it is not of the last step (a captured attend
+// replayed without its share), of another number of tokens, of single tokens and the launches are not, or the other way
+// round, or has common items and there is no attention kernel for them (alone).
+__device__ __forceinline__ bool share_stale(const CacheDev& c, const CachePlan& pl, int tokens, int single, int alone) {
+    const bool stale = pl.serial != __ldcg(&c.step_plan->serial) || pl.tokens != tokens || pl.single != single ||
+                       (alone && pl.n_groups);
     if (stale && blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(c.err, 0, ERR_CACHE_STATE);
     return stale;
 }

@@ -504,7 +504,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             long long x = 0, x_end = 0, within = 0;
             CacheGroup g;
             bool any = pl.ok && (whole ? b < items : b < pl.n_ctas);
-            if (SHARED && any) any = !share_stale(c, pl);
+            if (SHARED && any) any = !share_stale(c, pl, p.T, p.single, 0);
             if constexpr (LISTED) any = any && lists_dense(c, p.lists, pl);
             if (any && !whole) {
                 x = sh.begin;

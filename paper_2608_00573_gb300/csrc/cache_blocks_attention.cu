@@ -133,10 +133,6 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     // Lists that have been masks of an attention over all pages: the items that it marked.
     const bool again = !OWN && lists_dense(c, p.lists, pl);
     const int items = OWN ? pl.pieces * c.Hkv : again ? pl.pieces * p.row_tiles : p.T * c.Hkv * p.row_tiles;
-    if (!pl.ok || (OWN && share_stale(c, pl))) {       // (all CTAs)
-        if (OWN) pdl_wait();
-        return;
-    }
     // The last CTA to finish drawing leaves the counter at zero for the next call.
     auto drawn_all = [&] {
         __threadfence();
@@ -145,6 +141,13 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             c.plan->done = 0;
         }
     };
+    if (!pl.ok || (OWN && share_stale(c, pl, p.T, 1, p.alone))) {       // (all CTAs)
+        if (OWN) {                                     // (the list may be the next call's: what was drawn goes back)
+            if (threadIdx.x == 0) drawn_all();
+            pdl_wait();
+        }
+        return;
+    }
     if (OWN && sh.first_item >= items) {               // (a CTA that began late)
         if (threadIdx.x == 0) drawn_all();
         pdl_wait();

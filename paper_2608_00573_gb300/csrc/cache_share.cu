@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         const int tiles = share_tiles(cost, two_tiles);
         c.cut[k] = make_int2(first, cache_cta_of(start + (long long)(tiles - 1) * step, W, n_ctas) - first + 1);
     }
-    if (i == 0) *c.plan = CachePlan{W, items, n_ctas, 0, 1, 0, 0, pieces, c.step_plan->serial};
+    if (i == 0) *c.plan = CachePlan{W, items, n_ctas, 0, 1, 0, 0, pieces, c.step_plan->serial, T, single};
     for (int t = i; t < T; t += kPlanThreads) {
         const int k = c.owner[t], g = s_of[k], from = c.seqs[l.a[g]].q_off;
         const int item = s_common[g] ? s_begin[g] + (t - from) / (2 * TT) : -1;
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(256, B > 3 ? 2 : 6) cache_join_shared_kernel(c
     const CachePlan pl = *c.plan;
     if (threadIdx.x < 2 * heads) s_parts[threadIdx.x] = c.lists[((size_t)t * c.Hkv + head0) * 2 + threadIdx.x];
     __syncthreads();
-    if (!pl.ok || share_stale(c, pl)) return;          // (a refused step has written no lists)
+    if (!pl.ok || share_stale(c, pl, p.T, p.single, p.alone)) return;     // (a refused step has written no lists)
     // A token whose only part is one piece has its result already.
     if (pl.pieces && s_parts[0].count == 0 && s_parts[1].count == 1) return;
     for (int e = threadIdx.x; e < heads * c.rep * (DH / 4); e += 256) {
