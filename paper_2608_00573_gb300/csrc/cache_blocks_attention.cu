@@ -466,7 +466,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
                 for (int w = 0; w < kReaders; ++w) {
                     const float2 ml = sh.ml[w][r + 8 * i];
-                    sum[i] += ml.y * ex2(ml.x - ref);
+                    sum[i] += __fmul_rn(ml.y, ex2(ml.x - ref));
                 }
                 const float f = ex2(m[i] - ref);
 #pragma unroll
