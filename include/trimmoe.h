@@ -620,9 +620,10 @@ trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer, const tri
  * A token sees the positions of the pages in its list, for each key/value head, and of the
  * positions from the step's first page on (positions before the step / page_size, rounded
  * down, times page_size) those that trimmoe_cache_attend would show it.  A list holds
- * ascending columns of whole pages before the step, then -1: of other entries (not
- * ascending, no whole page before the step, behind a -1) those that do not fit are left
- * out and CACHE_BLOCKS is flagged.
+ * ascending columns of whole pages before the step, then -1.  Other entries (no whole page before
+ * the step, not larger than the entry before, behind a -1, behind as many entries as there are such pages)
+ * are left out and CACHE_BLOCKS is flagged; behind an entry out of this order a page that is named
+ * again counts once, and entries from the 4097th on are left out.
  * Prompts whose lists name much of what their sequences hold are computed 128 rows at a
  * time over all pages, with the lists as masks; the first such call allocates up to 64 MB
  * (during a capture it does not, and lists are followed one by one: the same result up to
