@@ -645,6 +645,8 @@ class PagedCache:
         seq, q_len = self._pair(seq, q_len, "step")
         self._done(self._lib.trimmoe_cache_step(self.handle, seq[2], seq[1], q_len[1], self._stream(stream)))
         self.T = sum(q_len[0])
+        if stream is not None:
+            self._keep(stream, self.codes, self.scales)
 
     def append(self, layer: int, qkv, q_out=None, gamma_q=None, gamma_k=None, eps: float = 1e-6, theta: float = 1e6,
                pos=None, stream=None):
@@ -694,7 +696,8 @@ class PagedCache:
         return out
 
     def set_bounds(self, codes, scales):
-        """Where the bounds of the pages' keys lie (None, None: nowhere); what is there counts as theirs."""
+        """Where the bounds of the pages' keys lie (None, None: nowhere); what is there counts as theirs.  The cache
+        drops those that it had; a captured graph goes on using them."""
         shape = (self.layers, self.n_pages, self.kv_heads)
         self._tensor(codes, self.torch.int8, shape + (2, self.head_dim), "set_bounds")
         self._tensor(scales, self.torch.float32, shape, "set_bounds")
@@ -711,6 +714,8 @@ class PagedCache:
         """Bounds of the keys of the pages that the step's tokens filled (whole: of all full pages of its sequences);
         behind append, in every step of a layer that selects blocks."""
         self._done(self._lib.trimmoe_cache_summarize(self.handle, layer, int(whole), self._stream(stream)))
+        if stream is not None:
+            self._keep(stream, self.codes, self.scales)
 
     def select(self, layer: int, q, n: int, first: int = 1, last: int = 1, out=None, stream=None):
         """Lists of n whole pages before the step for each token and key/value head, int32 [T][kv_heads][n] (columns of
@@ -733,7 +738,7 @@ class PagedCache:
         if rc:
             self._done(rc)
         if stream is not None:
-            self._keep(stream, q, out)
+            self._keep(stream, q, out, self.codes, self.scales)
         return out
 
     def attend_blocks(self, layer: int, q, blocks, out=None, tree=None, scale: float = 0.0, stream=None):
@@ -779,12 +784,14 @@ class PagedCache:
         self._done(self._lib.trimmoe_cache_accept(self.handle, seq[2], seq[1], n_acc.data_ptr(), path.data_ptr(),
                                                   path.shape[1], self._stream(stream)))
         if stream is not None:
-            self._keep(stream, n_acc, path)
+            self._keep(stream, n_acc, path, self.codes, self.scales)
 
     def compact(self, stream=None):
         """Move the pages in use to the lowest indices, except those that the program holds itself (ref above the
         page's holders in table): these stay where they are."""
         self._done(self._lib.trimmoe_cache_compact(self.handle, self._stream(stream)))
+        if stream is not None:
+            self._keep(stream, self.codes, self.scales)
 
     def stats(self, reset: bool = False) -> dict:
         """Synchronises; {status, device_error, free_pages, launches}."""
