@@ -32,7 +32,6 @@ namespace {
 constexpr int kCommonThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kMinTiles = 2;           // as for other steps (cache_pages.cu)
-constexpr long long kShareBytes = 40LL << 20;   // common pages are read for each sequence when that costs less
 
 // A block takes one group: the front pages that its sequences share, and how many whole key
 // tiles these fill.
@@ -166,13 +165,11 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     float piece_bytes = 0.f;
     if (single) {
         // Small groups' common pages are read in pieces, as sequences' own pages are; for
-        // larger ones the 128-row tiles of the attention kernel read common pages.  Where those
-        // save little, each sequence reads them itself: from L2, and nothing has to be waited for.
+        // larger ones the 128-row tiles of the attention kernel read common pages.  (Short ones too: left to
+        // their sequences where that cost less than 40 MB, 40 samples of 300 positions took 21.7 us instead of 17.2,
+        // 20 of 300 18.2 instead of 13.7, 12 of 700 18.7 instead of 17.2; 32 heads on 8.)
         const int per = 16 / c.rep, row_tiles = small_tiles(tok, c.rep);
         const bool small = row_tiles <= kSmallTiles;
-        long long saved;
-        block_sum(small ? 0LL : (long long)tiles * (tok - 1), s_wl, saved);
-        if (!small && saved * kCacheTile * c.Hkv * c.dh * 4 < kShareBytes) tiles = 0;
         if (i < n) s_common[i] = tiles;
         __syncthreads();
         // Stages of 64 positions of one head; a piece has as many as give each of two CTAs an SM three pieces,
@@ -301,14 +298,19 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
     if (single && n_ctas) {
         // The second kernel's CTAs read pieces beside this one's: as many SMs as let both end together, in us (a CTA
         // begins and ends in 6, and its tiles take 1.6 times as long beside the other kernel's
-        // traffic; pieces at HBM's rate).
+        // traffic; pieces at HBM's rate).  Measured, as here and with other constants: 64 samples of 8200 positions with up
+        // to 900 of their own, 32 heads on 8: 41.3 us; 1.2 or 2.0 times 41.8, 43.4; at 5.5 or 7.5 TB/s 42.1, 43.5.  32 of 12000, up
+        // to 150: 33.0; 30.2, 33.9; 30.2, 33.9; ends of 4 or 8 us 27.3, 34.7.  64 of 8000, up to 100, 16 heads on 16: 37.8;
+        // 40.6, 43.6; 37.8, 37.8; 37.8, 43.6; + 2 or 6 instead of + 4 43.8, 37.8.  12 of 700, 32 on 8: 15.8; at least 8 or 16 us
+        // instead of 12 14.3, 17.7; 16 of 3000 16.8; 18.1, 18.9.
         const float a = W * (1.6f * kShareUnit), b = piece_bytes / 6.5e6f * c.num_sms;
         const float t = max(12.f, (a + b) / c.num_sms + 4.f);
         n_ctas = min(n_ctas, (int)(a / (t - 6.f)) + 1);
-        // (A whole number of CTAs to an item, where there are as many: one that begins a second item
-        // ends 6 us later.)
+        // A whole number of CTAs to an item, where there are as many, the nearest one: a CTA that begins a second item
+        // ends 6 us later.  (Nearest, the next below, as it comes: 64 of 8000, up to 1000 of their own, 16 heads on 16, 71.5 us,
+        // 118, 75.4; 40 of 20000 52.8, 52.8, 55.8; 64 of 8200, 32 on 8, 41.2, 42.0, 41.0; 4 times 16 of 1000 25.2, 22.7, 24.5.)
         const int all = items * c.Hkv;
-        if (n_ctas > all) n_ctas -= n_ctas % all;
+        if (n_ctas > all) n_ctas = min(c.num_sms, (n_ctas + all / 2) / all * all);
     }
     // Where parts lie: an item's pieces are as many as heads and cuts.
     long long rows = 0;
