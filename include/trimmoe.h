@@ -602,8 +602,9 @@ trimmoe_status trimmoe_cache_summarize(trimmoe_cache_handle c, int layer, int wh
  *  score(b) = scale_b max_h u_h sum_d max(c_hd lo_bd, c_hd hi_bd)
  * over the query heads h of the key/value head, lo and hi as 8-bit codes; u_h is the unit of
  * head h's query (like scale, from its largest |value|) and c_hd = q_hd / u_h rounded to
- * the nearest whole number, halves to even.  Every sum is a whole number below 2^24, so
- * scores are exact.  A block with scale +infinity scores +infinity; a head whose query
+ * the nearest whole number, halves to even.  Every sum is a whole number below 2^24 and units are
+ * powers of two, so scores are exact as long as sum * u_h and that * scale_b are in fp32's normal
+ * range (above it they are infinite, below it coarser or 0, in that order of products).  A block with scale +infinity scores +infinity; a head whose query
  * holds an infinity or a NaN scores 0 everywhere. */
 typedef struct {
     const void* q;

@@ -6,8 +6,9 @@
 //   score = u max_h u_h sum_d max(c_hd lo_d, c_hd hi_d),  c_h = rint(q_h / u_h)
 //
 // With q+ = max(c, 0) and q- = min(c, 0) the sum is q- . lo + q+ . hi, a product of 8-bit numbers
-// with 2 D terms.  It is at most 128 * 127 * 127 < 2^24, so that every score is exact in fp32
-// and the order of the blocks (ties: the lower one) does not depend on how it is computed.
+// with 2 D terms.  It is at most 128 * 127 * 127 < 2^24, so that every score is exact in fp32 (but where
+// its products with the units leave the normal range) and the order of the blocks (ties: the lower one) does not
+// depend on how the sum is computed.
 #include <algorithm>
 #include <type_traits>
 

@@ -138,3 +138,35 @@ def test_chunks_in_long_tables(heads, dh):
     narrow.summarize(1, whole=True)
     check(narrow, m2, x2, q, 20, 1)
     assert math.prod(narrow.k.shape) == math.prod(c.k.shape)
+
+
+@pytest.mark.parametrize("q,launches", [([1, 1], 1), ([1] * 40, 2), ([20, 9], 1)])
+@pytest.mark.parametrize("keys,queries", [(100, 100), (-100, -90), (120, -120), (60, -126), (-126, 30)])
+def test_scores_outside_of_single_precision(q, launches, keys, queries):
+    """A score is the product of a sum, the query's unit and the block's scale, each step in fp32: infinite above its range,
+    coarser or zero below, and of equal ones the lower columns are taken."""
+    ctx = [16 * 200, 16 * 90] + [16 * 30] * (len(q) - 2)
+    c, m, x = with_bounds((4, 2, 64), 16, ctx, q, poison=False)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    lift = torch.exp2(torch.randint(keys - 6, keys + 1, (c.n_pages, 2, 1, 1), generator=g, device=DEV).double())
+    c.k[1] = (torch.randn(c.k[1].shape, generator=g, device=DEV).double().clamp(-3.9, 3.9) * lift).bfloat16()
+    x.copy_((torch.randn(x.shape, generator=g, device=DEV).double().clamp(-3.9, 3.9) * 2.0 ** queries).bfloat16())
+    c.summarize(1, whole=True)
+    before = c.stats()["launches"]
+    got = c.select(1, x, 9)
+    assert c.stats()["launches"] - before == launches
+    t = 0
+    for s, new in enumerate(q):
+        full = ctx[s] // 16
+        ids = torch.tensor(m.own[s][:full], device=DEV)
+        y = x[t:t + new].double().view(new, 2, 2, 64)
+        u = units(y.abs().amax(-1, keepdim=True))
+        y = torch.round(y / u)
+        lo, hi = c.codes[1][ids].double().unbind(2)
+        whole = torch.einsum("tgrd,fgd->tgrf", y.clamp(max=0), lo) + torch.einsum("tgrd,fgd->tgrf", y.clamp(min=0), hi)
+        score = (whole.float() * u.float()).amax(2) * c.scales[1][ids].t()
+        rest = torch.argsort(-score[..., 1:full - 1], dim=-1, stable=True)[..., :7] + 1
+        ends = torch.tensor([0, full - 1], device=DEV).expand(new, 2, 2)
+        assert torch.equal(got[t:t + new], torch.cat([ends, rest], -1).sort(-1)[0].int()), s
+        t += new
+    assert c.stats()["status"] == 0
