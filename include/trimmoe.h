@@ -451,9 +451,10 @@ trimmoe_status trimmoe_compact_noalloc(const uint8_t* action, const uint8_t* exp
  * statistics and sums are fp32 (probabilities are rounded to bf16 as operands
  * of the tensor cores, their sum is that of the unrounded values).
  *
- * Capture: append, attend, fork, truncate, accept and compact may be captured in
- * a CUDA graph, step too (its sequences and counts are those of the capture; the
- * lengths are read on the GPU at replay). */
+ * Capture: append, attend, fork, truncate, accept, compact, summarize, select and
+ * attend_blocks may be captured in a CUDA graph, step and share too (their sequences and
+ * counts are those of the capture; the lengths are read on the GPU at replay), share but not
+ * the first one.  An attend that is captured behind a share needs one at replay (see there). */
 typedef struct trimmoe_cache* trimmoe_cache_handle;
 
 /*  layers; q_heads, kv_heads (q_heads / kv_heads a whole number <= 128);
@@ -564,7 +565,9 @@ trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer, const tri
  * per key/value head) whose tokens fill more than half as many tiles of 128 rows (tokens
  * times q_heads / kv_heads) group by group as they do sequence by sequence, groups of one
  * left out, or where groups of one have four fifths of the tiles: products are the bound
- * there.
+ * there.  Groups gain most behind long prompts; pairs of sequences with many tokens behind fewer than
+ * some 2000 positions are up to a quarter slower than without.  The call itself is two launches,
+ * 9 to 25 us, once for all layers of a step.
  * The first call allocates workspaces (about 225 MB at head_dim 128) and so must not be
  * captured; later ones may be.  A captured attend reads the list that it finds: replayed behind a
  * later step it needs a share of that step that takes its groups up, of as many tokens, single ones or not as those
@@ -613,7 +616,8 @@ typedef struct {
     int32_t* blocks;
 } trimmoe_select_args;
 
-/* Needs trimmoe_cache_set_bounds. */
+/* Needs trimmoe_cache_set_bounds.  (Prompts are chosen for eight tokens at a time with tables of up to some
+ * 3400 columns; with wider ones, max_pages, token by token, which takes four to five times as long and more.) */
 trimmoe_status trimmoe_cache_select(trimmoe_cache_handle c, int layer, const trimmoe_select_args* a, void* stream);
 
 /* Arguments of trimmoe_cache_attend_blocks (device pointers as for attend).

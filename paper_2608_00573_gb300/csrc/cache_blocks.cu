@@ -54,12 +54,16 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
     if (sum != c->n) return c->fail(TRIMMOE_ERR_ARG, "cache_share", "counts must add up to the step's sequences");
     if (c->T == 0 || (long long)c->T * c->d.Hq > kShareRows) return TRIMMOE_OK;
     // Query tiles of the groups' common pages against those of the sequences by themselves.  Not half as many: sequences
-    // that read common pages out of L2 each for itself are as fast.  (With groups against without, 12 trees behind a common
-    // 12000 positions, 32 heads on 8: 2 tokens each, 0.08 of the tiles, 31 us / 76; 8, 0.25, 49 / 77; 16, 0.5, 65 / 84; 20,
-    // 0.67, 74 / 85; 24, 0.75, 86 / 85; 29, 0.92, 92 / 85; behind 2000: 4 tokens 27 / 33; 12, 0.42, 34 / 33; 16, 36 / 33; 24,
-    // 41 / 34; 6 prompts of 200 to 400 behind 6000 211 / 185.)  Nor where groups of one have most of the tiles: all items' parts are
-    // joined then (of 32 trees of 8 tokens behind 6000 positions 32, 16, 8, 4 in a group: 68, 100, 105, 104 us, without 99; 16 heads on
-    // 16, 3000: 69, 107, 121, 126, without 125).
+    // that read common pages out of L2 each for itself are as fast.  (With groups against without, 12 trees with up to 2000
+    // positions of their own behind a common 12000, 32 heads on 8: 2 tokens each, 0.08 of the tiles, 31 us / 76; 8, 0.25, 49 / 77;
+    // 16, 0.5, 65 / 84; 20, 0.67, 74 / 85; 24, 0.75, 86 / 85; 29, 0.92, 92 / 85; behind 2000: 24 41 / 34; 6 prompts of 200
+    // to 400 behind 6000 211 / 185.)  The prefix's length counts too, but only the GPU knows it; with up to 200 positions of their own,
+    // with / without: 12 trees of 8 behind 300, 1000, 4000, 12000 15.9 / 17.1, 19.4 / 22.9, 27.4 / 35.9, 41.3 / 70.5; of 16 (0.5) 17.3 /
+    // 17.5, 22.6 / 23.1, 32.8 / 36.9, 55.4 / 76.9; 12 pairs of trees of 16 (0.5) 25.1 / 22.5, 35.3 / 31.7, 57.2 / 71.5, 112 /
+    // 187; 16 heads on 16 36.1 / 28.6, 55.1 / 53.1, 107 / 160, 237 / 444: pairs behind a short prompt lose.
+    // Nor where groups of one have four fifths of the tiles: all items' parts are joined then.  (Of 32 trees of 8 tokens 16, 8, 4 in
+    // a group, the others with prompts of their own: behind 1000 positions 39.4 / 38.8, 41.4 / 39.5, 42.1 / 39.8, behind 6000
+    // 89.6 / 96.8, 109 / 119, 123 / 130; 16 heads on 16 65.8 / 67.2, 69.1 / 67.3, 70.5 / 67.4 and 180 / 304, 236 / 304, 263 / 305.)
     if (c->max_q > 1 || c->d.rep > 16) {
         auto tiles = [&](long long tokens) { return (tokens + c->d.tile_tokens - 1) / c->d.tile_tokens; };
         long long shared = 0, alone = 0, others = 0;

@@ -470,8 +470,8 @@ __device__ __forceinline__ void list_ends(int* out, int n, int F, int first, int
 // TILE tokens (eight, or one) and a key/value head: scores in shared memory, from bounds that are read once
 // for the tokens of a sequence, then a warp chooses for each token, or all for the one.
 //
-// Bound: issue slots (50 % busy; integer products 20 %): 2 D products per block of keys and query head, and the
-// choice, some 300 instructions of a warp per list.  Measured: 800 tokens' chunks behind 6000 to 15000 positions, 12
+// Bound: the chain of a list, which one warp makes (passes over its scores with atomics and barriers between, some 300
+// instructions); issue slots are 50 % busy, integer products, 2 D per block of keys and query head, 20 %.  Measured: 800 tokens' chunks behind 6000 to 15000 positions, 12
 // heads of 64 columns, pages of 32, 27.8 us; one token over 312 blocks, 32 heads on 8, 8.2 us, latency.
 constexpr int kTile = 8, kTileBytes = 110 * 1024;
 template <int TILE>
@@ -706,7 +706,11 @@ template <int DH, int M>
 cudaError_t select_launch(const CacheDev& c, const SelectParams& p, cudaStream_t st, int& launches) {
     // Eight tokens to a block of threads when sequences have as many and their scores fit beside those of another
     // block; one to a block for few tokens of short sequences (one launch less: one token over 312 blocks
-    // 8.3 us instead of 8.6, and 3 us less on the host).
+    // 8.3 us instead of 8.6, and 3 us less on the host).  Both hold scores for all columns of the table, whose width decides,
+    // because the host does not know the lengths: 800 tokens' chunks behind 6000 to 15000 positions, 12 heads of 64 columns, pages of
+    // 32, take 33 us with 480 columns, 34 with 1480, 43 with 2480 and 2980 (two blocks to an SM instead of three), and token by token
+    // 175 with 3980, 222 with 8670, 504 with 30480 (slices of fewer tokens); 32 heads on 8, pages of 64, 33, 33, 37, 37,
+    // 103, 143, 292.  48 single tokens 23.0 with 1240 to 9430 columns, 34.5 with 31240.
     if (p.max_q >= kTile && tile_bytes<kTile>(c) <= kTileBytes) return tile_launch<DH, M, kTile>(c, p, st, launches);
     if ((long long)p.T * c.Hkv <= 64 && c.max_pages <= 1024 && tile_bytes<1>(c) <= kTileBytes) return tile_launch<DH, M, 1>(c, p, st, launches);
     // As many tokens at a time as the buffer has room for.

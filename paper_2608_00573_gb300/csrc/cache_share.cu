@@ -16,11 +16,24 @@
 // them, and HBM is what they wait for.
 //
 // Bound: HBM for single tokens, each common K and V row once a group; the chain of a key tile for drafted trees.
-// Measured, 32 heads on 8, D = 128: 64 samples of a prompt of 8200 positions with up to 900 of their own 42 us (23 at
+// Measured, 32 heads on 8, D = 128: 64 samples of a prompt of 8200 positions with up to 900 of their own 41.5 us (23 at
 // the copy rate; the attention kernel's last CTA, the pieces and the join take 30, 31 and 8 alone); 4 samples of
-// 700 positions 12.0 us, latency; 24 trees of 16 drafts behind 5000 positions 67 us; 16
-// heads on 16, five groups of up to 24 behind 300 to 6000 positions 60 us.  The same steps without groups
-// read the common pages for each sequence (when, and what both sides take: trimmoe_cache_share).
+// 700 positions 11.9 us, latency; 24 trees of 16 drafts behind 5000 positions 67 us; 16
+// heads on 16, five groups of up to 24 behind 300 to 6000 positions 58 us.
+//
+// Single tokens are always taken up.  An attend without groups / with them, us, 32 heads on 8, pages of 64, up to 128 positions of
+// their own, behind 300, 1000, 3000, 8000 and 30000 common ones:
+//   one group of 2    10.9 / 10.1   12.0 / 10.3   17.8 / 12.8   21.8 / 17.8   40.2 / 33.1
+//   of 4              11.1 / 11.7   16.2 / 12.4   20.9 / 17.5   27.8 / 20.1   61.3 / 35.1
+//   of 16             18.2 / 14.4   24.5 / 16.2   35.2 / 16.3   64.0 / 27.0    195 / 41.6
+//   of 64             30.1 / 19.1   50.7 / 20.5    106 / 22.8    244 / 34.5    854 / 55.8
+//   16 groups of 2    25.3 / 17.3   36.8 / 22.8   61.5 / 45.5    159 / 89.8    553 / 288
+//   64 groups of 1    30.9 / 26.9   56.8 / 55.2    134 / 126     320 / 306    1147 / 1094
+// (the last share nothing: pieces of equal size).  16 heads on 16, pages of 16, one group of 4: 12.5 / 10.3, 19.3 / 11.5, 27.6 / 15.9,
+// 51.7 / 22.4, 161 / 59.4.  Of 100 such pairs two lose, the group of 4 behind 300 and, on 16 heads, one sequence alone
+// behind 30000, 49.9 / 57.0.  The list itself (two launches, once a step for all its layers) takes 9 to 16 us in a row of
+// launches, 25 behind 30000 positions for 64 sequences, 56 where their pages are of 16.  Several tokens per sequence:
+// trimmoe_cache_share.
 #include <algorithm>
 
 #include "cache.cuh"
@@ -308,7 +321,8 @@ __global__ void __launch_bounds__(kPlanThreads) cache_share_kernel(const __grid_
         n_ctas = min(n_ctas, (int)(a / (t - 6.f)) + 1);
         // A whole number of CTAs to an item, where there are as many, the nearest one: a CTA that begins a second item
         // ends 6 us later.  (Nearest, the next below, as it comes: 64 of 8000, up to 1000 of their own, 16 heads on 16, 71.5 us,
-        // 118, 75.4; 40 of 20000 52.8, 52.8, 55.8; 64 of 8200, 32 on 8, 41.2, 42.0, 41.0; 4 times 16 of 1000 25.2, 22.7, 24.5.)
+        // 118, 75.4; 40 of 20000 52.8, 52.8, 55.8; 64 of 8200, 32 on 8, 41.2, 42.0, 41.0; 12 of 700 15.8, 17.2, 16.1; but 4 times 16 of
+        // 1000 25.2, 22.7, 24.5, and 16 of 8000 27.0 instead of the next below's 24.3.)
         const int all = items * c.Hkv;
         if (n_ctas > all) n_ctas = min(c.num_sms, (n_ctas + all / 2) / all * all);
     }
