@@ -538,7 +538,7 @@ trimmoe_status trimmoe_cache_append(trimmoe_cache_handle c, int layer, const tri
  *  scale > 0 of the scores, 0 for 1/sqrt(head_dim).
  * Query head h reads key/value head h / (q_heads / kv_heads).  Masked positions
  * contribute nothing, whatever their keys and values hold; a row that sees no
- * position is zero. */
+ * position, or whose scores are all -infinity, is zero. */
 typedef struct {
     const void* q;
     int ld_q;

@@ -471,8 +471,9 @@ __device__ __forceinline__ void list_ends(int* out, int n, int F, int first, int
 // for the tokens of a sequence, then a warp chooses for each token, or all for the one.
 //
 // Bound: the chain of a list, which one warp makes (passes over its scores with atomics and barriers between, some 300
-// instructions); issue slots are 50 % busy, integer products, 2 D per block of keys and query head, 20 %.  Measured: 800 tokens' chunks behind 6000 to 15000 positions, 12
-// heads of 64 columns, pages of 32, 27.8 us; one token over 312 blocks, 32 heads on 8, 8.2 us, latency.
+// instructions); issue slots are 50 % busy, integer products, 2 D per block of keys and query head, 20 %.  Measured: 800
+// tokens' chunks behind 6000 to 15000 positions, 12 heads of 64 columns, pages of 32, 27.8 us; one token over 312 blocks,
+// 32 heads on 8, 8.2 us, latency.
 constexpr int kTile = 8, kTileBytes = 110 * 1024;
 template <int TILE>
 struct TileChoice {
