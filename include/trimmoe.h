@@ -567,13 +567,14 @@ trimmoe_status trimmoe_cache_attend(trimmoe_cache_handle c, int layer, const tri
  * left out, or where groups of one have four fifths of the tiles: products are the bound
  * there.  Groups gain most behind long prompts; pairs of sequences with many tokens behind fewer than
  * some 2000 positions are up to a quarter slower than without.  The call itself is two launches,
- * 9 to 25 us, once for all layers of a step.
- * The first call allocates workspaces (about 225 MB at head_dim 128) and so must not be
- * captured; later ones may be.  A captured attend reads the list that it finds: replayed behind a
- * later step it needs a share of that step that takes its groups up, of as many tokens, single ones or not as those
- * of its capture.  One that was captured with small groups alone (single tokens, at most two tiles
- * of 16 rows each, 16 / (q_heads / kv_heads) tokens to a tile) does not serve larger ones with a common prompt.
- * Where these do not hold it writes nothing and CACHE_STATE is flagged. */
+ * 9 to 16 us (25 to 56 for 64 sequences of 30000 positions), once for all layers of a step.
+ * The first call allocates workspaces (at head_dim 128 about 31 MB, and 2 KB for each query row of the
+ * largest step: 170 MB for 65536) and so must not be captured; later ones may be.
+ * A captured attend reads the list that it finds: replayed behind a later step it needs a share of
+ * that step that takes its groups up, of as many tokens, single ones or not as those of its
+ * capture.  One that was captured with small groups alone (single tokens, at most two tiles of 16
+ * rows each, 16 / (q_heads / kv_heads) tokens to a tile) does not serve larger ones with a
+ * common prompt.  Where these do not hold it writes nothing and CACHE_STATE is flagged. */
 trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, const int32_t* counts, void* stream);
 
 /* Bounds of the keys of whole pages ("blocks"), for trimmoe_cache_select: per layer, page,
@@ -607,7 +608,8 @@ trimmoe_status trimmoe_cache_summarize(trimmoe_cache_handle c, int layer, int wh
  * head h's query (like scale, from its largest |value|) and c_hd = q_hd / u_h rounded to
  * the nearest whole number, halves to even.  Every sum is a whole number below 2^24 and units are
  * powers of two, so scores are exact as long as sum * u_h and that * scale_b are in fp32's normal
- * range (above it they are infinite, below it coarser or 0, in that order of products).  A block with scale +infinity scores +infinity; a head whose query
+ * range (above it they are infinite, below it coarser or 0, in that order of products).
+ * A block with scale +infinity scores +infinity; a head whose query
  * holds an infinity or a NaN scores 0 everywhere. */
 typedef struct {
     const void* q;

@@ -257,20 +257,28 @@ inline size_t cache_score_keys(const CacheDev& c) {
 constexpr int kSmallTiles = 2;
 __host__ __device__ inline int small_tiles(int tokens, int rep) { return (tokens + 16 / rep - 1) / (16 / rep); }
 
-// Steps with groups of sequences: rows (tokens times query heads) at most, and what that allows.
+// Steps with groups of sequences: rows (tokens times query heads) at most, and what that allows in a cache whose steps
+// have T_max tokens.
 constexpr int kShareRows = 65536;
+__host__ __device__ inline int cache_share_tokens(const CacheDev& c) {
+    const int most = kShareRows / c.Hq;
+    return c.T_max < most ? c.T_max : most;
+}
 // Every token has its own and at most one common part, a part's rows are at most twice its
 // tokens' (whole warps, tiles that rep does not divide), a cut adds one part of 256 rows, and
-// an item's rows begin at a multiple of 32.  Pieces' parts lie row by row behind those that common ones can
-// take: one for each token and of each kind, and 64 K rows more where pages are cut.
+// an item's rows begin at a multiple of 32.  Of single tokens common parts alone are on the line; pieces' parts lie row by
+// row behind those: one for each token and of each kind, and 16 rows more for a cut and head, of which there
+// are fewer than 6 an SM (cache_share_kernel).
 __host__ __device__ inline long long cache_share_groups(const CacheDev& c) {
-    const long long T = kShareRows / c.Hq, n = T / (2 * c.tile_tokens) + c.max_seqs + 1;
+    const long long T = cache_share_tokens(c), n = T / (2 * c.tile_tokens) + c.max_seqs + 1;
     return 2 * (T < n ? T : n);
 }
 __host__ __device__ inline long long cache_piece_rows(const CacheDev& c) {
-    return 2LL * kShareRows + 256LL * c.num_sms + 32 * cache_share_groups(c);
+    return 2LL * cache_share_tokens(c) * c.Hq + 256LL * c.num_sms + 32 * cache_share_groups(c);
 }
-inline long long cache_share_part_rows(const CacheDev& c) { return 3LL * kShareRows + cache_piece_rows(c); }
+__host__ __device__ inline long long cache_share_part_rows(const CacheDev& c) {
+    return cache_piece_rows(c) + 2LL * cache_share_tokens(c) * c.Hq + 128LL * c.num_sms;
+}
 
 cudaError_t launch_cache_step(const CacheDev& c, int n, const int* seq, const int* q_len, int T, cudaStream_t st);
 cudaError_t launch_cache_fork(const CacheDev& c, int n, const int* src, const int* dst, cudaStream_t st);

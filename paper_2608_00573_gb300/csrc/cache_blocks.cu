@@ -107,9 +107,9 @@ extern "C" trimmoe_status trimmoe_cache_share(trimmoe_cache_handle c, int n, con
         alloc(d.plan, 1);
         alloc(d.shares, (size_t)d.num_sms);
         alloc(d.groups, (size_t)cache_share_groups(d));
-        alloc(d.parts_of, (size_t)kShareRows / d.Hq + 1);
+        alloc(d.parts_of, (size_t)cache_share_tokens(d));
         alloc(d.pieces, (size_t)kPieces);
-        alloc(d.lists, ((size_t)kShareRows / d.Hq + 1) * d.Hkv * 2);
+        alloc(d.lists, (size_t)cache_share_tokens(d) * d.Hkv * 2);
         alloc(d.common, (size_t)d.max_seqs);
         alloc(d.cut, (size_t)cache_share_groups(d) * d.Hkv);
         alloc(d.part_ml, rows);

@@ -216,7 +216,7 @@ cache_blocks_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (warp == kReaders) {
         // ------------------------------------------------------------ items and loads
         uint32_t issued = 0, n_items = 0;
-        const long long piece_end = cache_piece_rows(c) + 3LL * kShareRows - 16;
+        const long long piece_end = cache_share_part_rows(c) - 16;
         bool ok = true;
         // OWN: all items are drawn (CTAs on the attention kernel's SMs begin when it has ended), else each CTA has
         // its first one.
