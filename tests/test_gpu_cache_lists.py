@@ -99,22 +99,20 @@ def test_bad_lists_of_prompts(shapes, page):
     cache, m, x = filled(shapes, page, ctx, q, seed=5)
     blocks = lists_of(m, q, n, shapes[1])
     right = blocks.clone()
-    rng, at = random.Random(3), {}
+    rng, at = random.Random(3), set()
     for t in rng.sample(range(500), 60):
         bad, means = rng.choice(BAD + [(LONG, list(range(14)))])
         h = rng.randrange(shapes[1])
         blocks[t, h], right[t, h] = padded([bad], n)[0], padded([sorted(means)], n)[0]
-        at[t] = bad
+        at.add(t)
     a = followed(cache, x, blocks)
     assert cache.stats(reset=True)["device_error"] == 11
     b = cache.attend_blocks(0, x, blocks)
     assert cache.stats(reset=True)["device_error"] == 11
     assert (a != b).any(1).float().mean() > 0.5      # (that was by masks)
-    check_blocks(cache, m, x, q, right, a, 0, tokens=set(at))
-    check_blocks(cache, m, x, q, right, b, 0, tokens=set(at))
-    for out in (a, b):                               # the same pages in another notation
-        assert torch.equal(out[[t for t in range(500) if t not in at]], (a if out is a else b)[[t for t in range(500) if t not in at]])
-    again = cache.attend_blocks(0, x, right)
+    check_blocks(cache, m, x, q, right, a, 0, tokens=at)
+    check_blocks(cache, m, x, q, right, b, 0, tokens=at)
+    again = cache.attend_blocks(0, x, right)         # the same pages in another notation
     assert torch.equal(again, b) and cache.stats()["device_error"] == 0
 
 
